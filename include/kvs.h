@@ -11,7 +11,10 @@
  *                 chunk buffers (KV is retained in complete 256-token chunks,
  *                 Sec. 5.1, Workload);
  *   kvs_query_bw  measures the host link and HBM on this GPU and picks, per
- *                 direction, how host-resident chunks are moved.
+ *                 direction, how host-resident chunks are moved;
+ *   kvs_append, kvs_attend, kvs_weigh, kvs_evict  are a model's work on the paged
+ *                 cache in between: new tokens' keys and values, attention over
+ *                 the cache, the weight each token received, eviction by it.
  *
  * The arguments follow the paper's statement of a retrieval: the matched
  * prefix tokens of each request, where its KV objects sit in the fast tier
@@ -462,6 +465,187 @@ int64_t kvs_stat_launches(void);
 int kvs_retrieve_noalloc(const kvs_geometry* geom, const kvs_paged_cache* cache,
                          const kvs_request* requests, int32_t num_requests,
                          void* cuda_stream, uint32_t flags);
+
+/* ======================================================================
+ * A model's work on the paged cache, between a retrieval and the next store-back.
+ *
+ * A forward step takes each request's new tokens behind the prefix that kvs_retrieve
+ * brought: kvs_append rotates their queries and keys and writes keys and values into
+ * the planes, kvs_attend attends over the whole cache, kvs_weigh adds up the attention
+ * weight that each cached token received and kvs_evict keeps the tokens of the most
+ * weight.  Each call works on one layer (kvs_evict: on all) of the planes above.
+ *
+ * Unlike a retrieval's, the lengths and block tables of a step are DEVICE arrays, as a
+ * serving loop keeps them: the calls read them on the GPU, plan nothing on the host,
+ * allocate nothing, and can be captured into a graph.  Calls are enqueued on the
+ * caller's stream and return; tensors must stay valid until the stream has passed them.
+ * A length, row range or block id outside the stated bounds is not followed: what it
+ * concerns is left out (cached tokens read as zeros, output rows unwritten) and
+ * KVS_ERR_BOUNDS recorded for kvs_check_errors().  With KVS_F_VALIDATE (the only flag)
+ * a call synchronises the stream and returns that code itself.
+ *
+ * geom->elem_bytes must be 2, head_dim a multiple of 8 up to 128, and every address and
+ * stride a multiple of 16 bytes (KVS_ERR_UNSUPPORTED otherwise); chunk_tokens is unused.
+ * ====================================================================== */
+#define KVS_DTYPE_BF16 1
+#define KVS_DTYPE_F16  2
+
+/* The requests of one forward step.  Request r's new tokens are rows q_starts[r] up to
+ * q_starts[r + 1] of the step's tensors; kv_lens[r] tokens are in its cache, the new ones
+ * (the last) among them.  Token t of request r is in slot
+ * block_tables[r * table_stride + t / B] * B + t % B. */
+typedef struct kvs_step {
+    const int32_t* block_tables;    /* device [num_requests][table_stride]              */
+    const int32_t* kv_lens;         /* device [num_requests]                            */
+    const int32_t* q_starts;        /* device [num_requests + 1]; NULL: one row each    */
+    int32_t num_requests;           /* up to 65535                                      */
+    int32_t table_stride;           /* entries of a table, at least max_kv / B          */
+    int32_t total_q;                /* rows of the step's tensors                       */
+    int32_t max_q;                  /* no request has more new tokens ...               */
+    int32_t max_kv;                 /* ... or cached ones                               */
+    int32_t dtype;                  /* KVS_DTYPE_* of planes and tensors                */
+} kvs_step;
+
+/* A tensor [rows][heads][head_dim] with contiguous heads; strides in elements. */
+typedef struct kvs_rows {
+    void*   base;
+    int64_t row_stride;
+    int64_t head_stride;
+} kvs_rows;
+
+/* Rotary positions.  Pair j of a head's first rot_dim dims -- dims (j, j + rot_dim / 2),
+ * or (2j, 2j + 1) if interleaved -- is turned by position * (turns[j][0] + turns[j][1])
+ * whole turns, and multiplied by scale; the other dims pass unchanged.  A frequency is
+ * the sum of two binary32 numbers, so that the angle at position 10^6 is as exact as at
+ * 1.  kvs_rope_turns() fills the table for the usual scalings. */
+typedef struct kvs_rope {
+    const float* turns;             /* device [rot_dim / 2][2]                          */
+    int32_t rot_dim;                /* even, up to head_dim                             */
+    int32_t interleaved;
+    float   scale;
+    int32_t reserved;
+} kvs_rope;
+
+#define KVS_ROPE_PLAIN  0   /* base^(-2j / rot_dim) radians per position                 */
+#define KVS_ROPE_LINEAR 1   /* ... divided by factor                                     */
+#define KVS_ROPE_NTK    2   /* plain with base * factor^(rot_dim / (rot_dim - 2))        */
+#define KVS_ROPE_BANDS  3   /* by wavelength: plain below context / high, divided by
+                               factor above context / low, and in between a mean that
+                               goes linearly with context / wavelength                   */
+#define KVS_ROPE_YARN   4   /* by the index j: plain below the pair that turns `high`
+                               times within the context, divided by factor above the one
+                               that turns `low` times, a linear mean in between; scale
+                               0.1 ln(factor) + 1 (Peng et al., 2023)                    */
+typedef struct kvs_rope_spec {
+    int32_t rot_dim;
+    int32_t kind;                   /* KVS_ROPE_*                                       */
+    double  base;                   /* above 1                                          */
+    double  factor;                 /* at least 1                                       */
+    double  context;                /* BANDS, YARN: the length the model was trained on */
+    double  low, high;              /* BANDS, YARN: 0 < low < high                      */
+} kvs_rope_spec;
+/* Fills turns_out[rot_dim / 2][2] (HOST memory) and *scale_out. */
+int kvs_rope_turns(const kvs_rope_spec* spec, float* turns_out, float* scale_out);
+
+/*
+ * Append: for every new token (row n, cached as token t of its request),
+ *     q_out[n] = rotated q[n],  plane[2*layer][slot(t)] = rotated k[n],
+ *     plane[2*layer + 1][slot(t)] = v[n].
+ * positions[n] (device int32, NULL: t) is the token's rotary position, which differs
+ * from t once tokens were evicted; |position| up to 2^24.  rope NULL: nothing is
+ * rotated.  q may be NULL (keys and values only, or to rotate no queries); q_out may be
+ * q itself.  New tokens beyond kv_lens (more new tokens than cached ones) are not
+ * appended, only their queries rotated.  Products and sums are binary32, rounded once.
+ */
+typedef struct kvs_append_args {
+    kvs_rows q, q_out;              /* [total_q][num_q_heads][head_dim]                 */
+    kvs_rows k, v;                  /* [total_q][H][head_dim]                           */
+    const int32_t*  positions;
+    const kvs_rope* rope;
+    int32_t num_q_heads;
+    int32_t reserved;
+} kvs_append_args;
+int kvs_append(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
+               const kvs_append_args* args, void* cuda_stream, uint32_t flags);
+
+/*
+ * Attention of each request's new tokens over its cached ones.  Query head i reads KV
+ * head i / (num_q_heads / H).  The i-th of n new tokens is the cached token
+ * p = kv_len - n + i; it sees the cached tokens t < kv_len with t <= p (if causal) and
+ * t > p - window (if window > 0):
+ *     out[row][head] = sum_t softmax_t(scale * q . k_t) v_t,   lse = log sum_t exp(scale * q . k_t).
+ * A token that sees nothing gets zeros and lse = -infinity.  What the planes hold beyond
+ * kv_len, or outside what a request's tokens see, may be anything (NaN too) and reaches
+ * no output; a non-finite value of a token that some row of the request sees may reach
+ * all of its rows.  causal = 0 attends to an encoder's states, or to a prefix alone.
+ * Scores, softmax statistics and sums are binary32; the weights are rounded to dtype for
+ * the product with V.  The workspace is device memory of kvs_attend_workspace() bytes
+ * (any contents, 16-byte aligned, not shared by calls that may overlap on the GPU).
+ */
+typedef struct kvs_attend_args {
+    kvs_rows q, out;                /* [total_q][num_q_heads][head_dim]                 */
+    float*   lse;                   /* device [total_q][num_q_heads], or NULL           */
+    void*    workspace;             /* may be NULL where kvs_attend_workspace() is 0    */
+    int64_t  workspace_bytes;
+    float    scale;
+    int32_t  causal;
+    int32_t  window;
+    int32_t  num_q_heads;
+} kvs_attend_args;
+int kvs_attend(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
+               const kvs_attend_args* args, void* cuda_stream, uint32_t flags);
+/* Bytes of workspace that kvs_attend needs for this step, or a KVS_ERR_* code (negative). */
+int64_t kvs_attend_workspace(const kvs_geometry* geom, const kvs_step* step, int32_t num_q_heads);
+
+/*
+ * Accumulated attention weight, from the lse that kvs_attend returned for the same
+ * arguments: for every request r, KV head h and cached token t < kv_len,
+ *     weights[r * request_stride + h * head_stride + t] =
+ *         decay * weights[...] + sum over the new tokens and h's query heads of exp(scale * q . k_t - lse).
+ * decay = 0 overwrites (what was there is not read); sums are binary32, in a fixed order.
+ */
+typedef struct kvs_weigh_args {
+    kvs_rows q;                     /* [total_q][num_q_heads][head_dim]                 */
+    const float* lse;               /* device [total_q][num_q_heads]                    */
+    float*   weights;               /* device, rows of at least max_kv                  */
+    int64_t  request_stride, head_stride;
+    float    scale;
+    float    decay;
+    int32_t  causal;
+    int32_t  window;
+    int32_t  num_q_heads;
+    int32_t  reserved;
+} kvs_weigh_args;
+int kvs_weigh(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
+              const kvs_weigh_args* args, void* cuda_stream, uint32_t flags);
+
+/*
+ * Eviction, all layers at once (rows of q are not used; total_q and max_q may be 0).
+ * For every layer l, request r and KV head h, J = min(kv_len, budget) cached tokens are
+ * kept: the first `sinks`, the last `recent` and, of the others, those of the largest
+ * weights[l * layer_stride + r * request_stride + h * head_stride + t] (the lower index
+ * of equal ones; NaN counts as less than every number).  In their order, the j-th kept
+ * token of a head is copied to token j of the request's new blocks (slot by dst_tables):
+ *     kept[l][r][h][j] = t,  planes[..][slot_dst(j)][h] = planes[..][slot(t)][h],
+ *     new_weights[l][r][h][j] = weights[l, r, h, t],  new_lens[r] = J,
+ * and kept = -1, new_weights = 0 for J <= j < budget.  Heads keep different tokens: the
+ * new blocks hold each head's own, and rotary positions go on from the old length.  The
+ * source blocks are only read and may be shared between requests; the new blocks must be
+ * none of them and named once (not checked).  weights and new_weights must not overlap.
+ */
+typedef struct kvs_evict_args {
+    const float*   weights;         /* device                                           */
+    int64_t        layer_stride, request_stride, head_stride;
+    const int32_t* dst_tables;      /* device [num_requests][dst_stride]                */
+    int32_t        dst_stride;      /* at least budget / B                              */
+    int32_t        budget;          /* at least 1                                       */
+    int32_t        sinks, recent;   /* together at most budget                          */
+    int32_t*       kept;            /* device [L][num_requests][H][budget]              */
+    float*         new_weights;     /* device [L][num_requests][H][budget], or NULL     */
+    int32_t*       new_lens;        /* device [num_requests], not kv_lens; or NULL      */
+} kvs_evict_args;
+int kvs_evict(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step,
+              const kvs_evict_args* args, void* cuda_stream, uint32_t flags);
 
 /* ======================================================================
  * Fast tier: the objects retrieval reads from, and their protection.

@@ -29,6 +29,7 @@
 
 #include "kvs.h"
 #include "kvs_internal.h"
+#include "kvs_ops.h"
 
 namespace kvs {
 namespace {
@@ -1391,6 +1392,28 @@ int hostlink_grid(bool retrieve) {
         return 0;
     }
     return std::max(8, sms / 3);          // the built-in default of get_state
+}
+
+int ops_device(int32_t** err, int* sms) {
+    std::lock_guard<std::mutex> lk(g_mu);
+    DevState* st = nullptr;
+    const int rc = get_state(&st);
+    if (rc) return rc;
+    *err = st->err;
+    *sms = st->sms;
+    return KVS_OK;
+}
+
+void ops_launched(int n) {
+    std::lock_guard<std::mutex> lk(g_mu);
+    g_launches += n;
+}
+
+int ops_read_error(cudaStream_t s) {
+    std::lock_guard<std::mutex> lk(g_mu);
+    DevState* st = nullptr;
+    const int rc = get_state(&st);
+    return rc ? rc : read_error_word(*st, s);
 }
 
 }  // namespace kvs

@@ -63,6 +63,9 @@ KVS_VARIANT_DMA = 3
 VARIANT_NAMES = {1: "hostlink", 2: "hbmcopy", 3: "dma"}
 KVS_KERNEL_LDG = 1
 KVS_KERNEL_TMA = 2
+KVS_DTYPE_BF16 = 1
+KVS_DTYPE_F16 = 2
+KVS_ROPE_PLAIN, KVS_ROPE_LINEAR, KVS_ROPE_NTK, KVS_ROPE_BANDS, KVS_ROPE_YARN = 0, 1, 2, 3, 4
 
 EXPORTED = ("kvs_retrieve", "kvs_store", "kvs_query_bw", "kvs_get_choice", "kvs_check_errors",
             "kvs_enqueue_error_read",
@@ -71,7 +74,8 @@ EXPORTED = ("kvs_retrieve", "kvs_store", "kvs_query_bw", "kvs_get_choice", "kvs_
             "kvs_retrieve_fp8", "kvs_store_fp8", "kvs_retrieve_fp8_layers", "kvs_store_fp8_layers", "kvs_tune",
             "kvs_tier_create", "kvs_tier_destroy", "kvs_tier_commit", "kvs_tier_staged",
             "kvs_tier_begin_retrieval", "kvs_tier_end_retrieval", "kvs_tier_cancel", "kvs_tier_ordinary",
-            "kvs_tier_claim_state", "kvs_tier_object", "kvs_tier_stats_get", "kvs_tier_slot")
+            "kvs_tier_claim_state", "kvs_tier_object", "kvs_tier_stats_get", "kvs_tier_slot",
+            "kvs_rope_turns", "kvs_append", "kvs_attend", "kvs_attend_workspace", "kvs_weigh", "kvs_evict")
 KVS_CLAIM_NONE, KVS_CLAIM_PLANNED, KVS_CLAIM_STAGING, KVS_CLAIM_STAGE_READY = 0, 1, 2, 3
 KVS_CLAIM_TRANSFERRING, KVS_CLAIM_RELEASED, KVS_CLAIM_CANCELLED, KVS_CLAIM_ORDINARY = 4, 5, 6, 7
 CLAIM_NAMES = {0: "None", 1: "Planned", 2: "Staging", 3: "StageReady", 4: "Transferring",
@@ -152,6 +156,53 @@ class kvs_tier_stats(ctypes.Structure):
                 ("completed", ctypes.c_int64), ("protected_object_seconds", ctypes.c_double)]
 
 
+class kvs_step(ctypes.Structure):
+    _fields_ = [("block_tables", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("q_starts", ctypes.c_void_p),
+                ("num_requests", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("total_q", ctypes.c_int32),
+                ("max_q", ctypes.c_int32), ("max_kv", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class kvs_rows(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class kvs_rope(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class kvs_rope_spec(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("kind", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("context", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double)]
+
+
+class kvs_append_args(ctypes.Structure):
+    _fields_ = [("q", kvs_rows), ("q_out", kvs_rows), ("k", kvs_rows), ("v", kvs_rows),
+                ("positions", ctypes.c_void_p), ("rope", ctypes.c_void_p), ("num_q_heads", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class kvs_attend_args(ctypes.Structure):
+    _fields_ = [("q", kvs_rows), ("out", kvs_rows), ("lse", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_int64), ("scale", ctypes.c_float), ("causal", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("num_q_heads", ctypes.c_int32)]
+
+
+class kvs_weigh_args(ctypes.Structure):
+    _fields_ = [("q", kvs_rows), ("lse", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("request_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("decay", ctypes.c_float), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("num_q_heads", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class kvs_evict_args(ctypes.Structure):
+    _fields_ = [("weights", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("request_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("dst_tables", ctypes.c_void_p), ("dst_stride", ctypes.c_int32),
+                ("budget", ctypes.c_int32), ("sinks", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("kept", ctypes.c_void_p), ("new_weights", ctypes.c_void_p), ("new_lens", ctypes.c_void_p)]
+
+
 # ---- library loading ------------------------------------------------------
 _lock = threading.Lock()
 _lib = None
@@ -221,6 +272,16 @@ def lib():
                                    ctypes.POINTER(kvs_request), ctypes.c_int32, P, ctypes.c_uint32,
                                    ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(kvs_tune_report)]
             L.kvs_tune.restype = ctypes.c_int
+            for name in ("kvs_append", "kvs_attend", "kvs_weigh"):
+                fn = getattr(L, name)
+                fn.argtypes = [P, P, P, ctypes.c_int32, P, P, ctypes.c_uint32]
+                fn.restype = ctypes.c_int
+            L.kvs_evict.argtypes = [P, P, P, P, P, ctypes.c_uint32]
+            L.kvs_evict.restype = ctypes.c_int
+            L.kvs_attend_workspace.argtypes = [P, P, ctypes.c_int32]
+            L.kvs_attend_workspace.restype = ctypes.c_int64
+            L.kvs_rope_turns.argtypes = [P, P, ctypes.POINTER(ctypes.c_float)]
+            L.kvs_rope_turns.restype = ctypes.c_int
             L.kvs_query_bw.argtypes = [ctypes.POINTER(kvs_bw_report), P, ctypes.c_int64]
             L.kvs_query_bw.restype = ctypes.c_int
             L.kvs_get_choice.argtypes = [ctypes.POINTER(kvs_bw_report)]
@@ -529,6 +590,211 @@ def kvs_store_fp8_layers(geom, planes, num_blocks, requests, layers_per_step, la
     ready = _wait_events(ready_events)
     return _layers_call("kvs_store_fp8_layers", geom, planes, num_blocks, requests, layers_per_step, ready,
                         _events(layer_events), stream, flags)
+
+
+# ---- a model's work on the paged cache --------------------------------------
+class Step:
+    """The requests of one forward step, marshalled once for all of its calls: geometry and
+    planes of the cache, and the device arrays (``kvs_step``) that a serving loop keeps.
+
+    ``block_tables`` [requests, blocks], ``kv_lens`` [requests] and ``q_starts`` [requests + 1]
+    are int32 tensors on the GPU, whose contents may change from call to call within
+    ``max_kv`` cached and ``max_q`` new tokens of a request and ``total_q`` rows; without
+    ``q_starts`` every request has one new token.  The tensors are kept alive with the step."""
+
+    def __init__(self, geom, planes, num_blocks: int, block_tables, kv_lens, q_starts=None, max_kv: int | None = None,
+                 total_q: int | None = None, max_q: int | None = None, dtype: int = KVS_DTYPE_BF16):
+        self.geom = _geometry(geom)
+        for name, t, dims in (("block_tables", block_tables, 2), ("kv_lens", kv_lens, 1), ("q_starts", q_starts, 1)):
+            if t is not None:
+                _int32_tensor(name, t, dims)
+        R, W = int(block_tables.shape[0]), int(block_tables.shape[1])
+        if len(kv_lens) != R or (q_starts is not None and len(q_starts) != R + 1):
+            raise ValueError("kv_lens has one entry per request, q_starts one more")
+        if len(planes) != 2 * self.geom.num_layers:
+            raise ValueError(f"{len(planes)} planes, {2 * self.geom.num_layers} are needed")
+        self._keep = (block_tables, kv_lens, q_starts, planes)
+        if block_tables.stride(1) != 1:
+            raise ValueError("a request's block table must be contiguous")
+        if q_starts is not None and (total_q is None or max_q is None):
+            raise ValueError("q_starts needs total_q and max_q")
+        self.planes = np.array([_addr(p) for p in planes], dtype=np.uint64)
+        self.cache = kvs_paged_cache(ctypes.cast(int(self.planes.ctypes.data), ctypes.POINTER(ctypes.c_void_p)), int(num_blocks))
+        stride = int(block_tables.stride(0)) if R > 1 else W
+        if stride < W:
+            raise ValueError("block tables overlap")
+        self.total_q = R if total_q is None else int(total_q)
+        self.max_kv = W * self.geom.block_size if max_kv is None else int(max_kv)
+        if self.max_kv > W * self.geom.block_size:
+            raise KvsError(KVS_ERR_BOUNDS, f"tables of {W} blocks do not hold max_kv = {self.max_kv}")
+        self.step = kvs_step(_addr(block_tables), _addr(kv_lens), _addr(q_starts), R, stride, self.total_q,
+                             (1 if R else 0) if max_q is None else int(max_q), self.max_kv, int(dtype))
+        self.refs = ctypes.byref(self.geom), ctypes.byref(self.cache), ctypes.byref(self.step)
+
+    @property
+    def torch_dtype(self):
+        import torch
+        return torch.float16 if self.step.dtype == KVS_DTYPE_F16 else torch.bfloat16
+
+
+def _int32_tensor(name, t, dims):
+    import torch
+    if t.dtype != torch.int32 or t.dim() != dims:
+        raise ValueError(f"{name}: an int32 tensor of {dims} dimension(s) is needed")
+    if dims == 1 and t.numel() > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name}: must be contiguous")
+
+
+def _f32(name, t, shape, contiguous=True):
+    import torch
+    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or (contiguous and not t.is_contiguous()):
+        raise ValueError(f"{name}: a {'contiguous ' if contiguous else ''}float32 tensor of shape {tuple(shape)} is needed")
+    return t.data_ptr()
+
+
+def _rows(name, step, t, heads) -> kvs_rows:
+    """kvs_rows of a tensor [total_q, heads, head_dim] with contiguous heads."""
+    if t.dtype != step.torch_dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, the step's is {step.torch_dtype}")
+    if t.dim() != 3 or t.shape[0] != step.total_q or t.shape[2] != step.geom.head_dim or (heads and t.shape[1] != heads):
+        raise ValueError(f"{name}: shape {tuple(t.shape)} is not [{step.total_q}, {heads or 'heads'}, {step.geom.head_dim}]")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name}: a head's elements must be contiguous")
+    return kvs_rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+@dataclass
+class Rope:
+    """Rotary positions: ``turns`` float32 [rot_dim / 2, 2] on the GPU (see :func:`kvs_rope_turns`)."""
+    turns: object
+    rot_dim: int
+    interleaved: bool = False
+    scale: float = 1.0
+
+    def __post_init__(self):
+        _f32("turns", self.turns, (self.rot_dim // 2, 2))
+        self.struct = kvs_rope(self.turns.data_ptr(), int(self.rot_dim), int(bool(self.interleaved)), float(self.scale), 0)
+        self.ref = ctypes.addressof(self.struct)
+
+
+def kvs_rope_turns(rot_dim: int, base: float = 10000.0, kind: int = KVS_ROPE_PLAIN, factor: float = 1.0,
+                   context: float = 0.0, low: float = 0.0, high: float = 0.0):
+    """(turns, scale): the float32 [rot_dim / 2, 2] table of the given scaling as a numpy array,
+    to be moved to the GPU for :class:`Rope`, and the factor that goes with it."""
+    spec = kvs_rope_spec(int(rot_dim), int(kind), float(base), float(factor), float(context), float(low), float(high))
+    out, scale = np.zeros((max(1, int(rot_dim) // 2), 2), dtype=np.float32), ctypes.c_float(0.0)
+    _check(lib().kvs_rope_turns(ctypes.byref(spec), out.ctypes.data, ctypes.byref(scale)))
+    return out, float(scale.value)
+
+
+def kvs_append(step: Step, layer: int, q, k, v, q_out=None, rope: Rope | None = None, positions=None,
+               stream=None, flags: int = 0) -> int:
+    """Rotate the new tokens' queries ``q`` [total_q, query heads, head_dim] into ``q_out`` (default:
+    in place) and keys ``k``, and append ``k`` and ``v`` [total_q, KV heads, head_dim] to the planes of
+    ``layer``.  ``positions``: int32 [total_q] on the GPU (default: the tokens' places in the cache);
+    ``q`` may be None."""
+    a = kvs_append_args()
+    if q is not None:
+        a.q = _rows("q", step, q, 0)
+        a.num_q_heads = q.shape[1]
+        a.q_out = a.q if q_out is None else _rows("q_out", step, q_out, q.shape[1])
+    H = step.geom.num_kv_heads
+    a.k, a.v = _rows("k", step, k, H), _rows("v", step, v, H)
+    if positions is not None:
+        _int32_tensor("positions", positions, 1)
+        if positions.shape[0] != step.total_q:
+            raise ValueError("positions has one entry per row")
+        a.positions = positions.data_ptr()
+    if rope is not None:
+        a.rope = rope.ref
+    g, c, s = step.refs
+    return _check(lib().kvs_append(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+
+
+def kvs_attend_workspace(step: Step, num_q_heads: int) -> int:
+    """Bytes of workspace that :func:`kvs_attend` needs for this step."""
+    g, _, s = step.refs
+    n = int(lib().kvs_attend_workspace(g, s, int(num_q_heads)))
+    if n < 0:
+        _check(n)
+    return n
+
+
+def kvs_attend(step: Step, layer: int, q, out, lse=None, scale: float | None = None, causal: bool = True, window: int = 0,
+               workspace=None, stream=None, flags: int = 0) -> int:
+    """Attention of the new tokens' queries ``q`` [total_q, query heads, head_dim] over the cached keys
+    and values of ``layer`` into ``out`` (the same shape); ``lse`` (float32 [total_q, query heads],
+    optional) receives log sum exp of the scaled scores.  ``scale`` defaults to head_dim ** -0.5;
+    ``workspace``: a uint8 tensor of :func:`kvs_attend_workspace` bytes (may be None if that is 0)."""
+    a = kvs_attend_args()
+    a.q = _rows("q", step, q, 0)
+    a.out = _rows("out", step, out, q.shape[1])
+    a.num_q_heads = q.shape[1]
+    if lse is not None:
+        a.lse = _f32("lse", lse, q.shape[:2])
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    a.scale = step.geom.head_dim ** -0.5 if scale is None else scale
+    a.causal, a.window = bool(causal), window
+    g, c, s = step.refs
+    return _check(lib().kvs_attend(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+
+
+def kvs_weigh(step: Step, layer: int, q, lse, weights, scale: float | None = None, decay: float = 1.0, causal: bool = True,
+              window: int = 0, stream=None, flags: int = 0) -> int:
+    """Add to ``weights`` (float32 [requests, KV heads, at least max_kv]) times ``decay`` the attention
+    weight that the new tokens gave to each cached token: ``q`` and the mask as for
+    :func:`kvs_attend`, ``lse`` what it returned."""
+    a = kvs_weigh_args()
+    a.q = _rows("q", step, q, 0)
+    a.num_q_heads = q.shape[1]
+    a.lse = _f32("lse", lse, q.shape[:2])
+    R, H = step.step.num_requests, step.geom.num_kv_heads
+    if weights.dim() != 3 or weights.shape[2] < step.max_kv or weights.stride(2) != 1:
+        raise ValueError("weights: [requests, KV heads, at least max_kv], contiguous in its last dimension")
+    a.weights = _f32("weights", weights, (R, H, weights.shape[2]), contiguous=False)
+    a.request_stride, a.head_stride = weights.stride(0), weights.stride(1)
+    a.scale = step.geom.head_dim ** -0.5 if scale is None else scale
+    a.decay, a.causal, a.window = decay, bool(causal), window
+    g, c, s = step.refs
+    return _check(lib().kvs_weigh(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+
+
+def kvs_evict(step: Step, weights, dst_tables, budget: int, sinks: int, recent: int, kept, new_weights=None, new_lens=None,
+              stream=None, flags: int = 0) -> int:
+    """Keep at most ``budget`` cached tokens of every head and layer: the first ``sinks``, the last
+    ``recent`` and those of the largest ``weights`` (float32 [layers, requests, KV heads, at least
+    max_kv]).  Their keys and values are copied to the blocks of ``dst_tables`` (int32 [requests,
+    blocks]); ``kept`` (int32) and ``new_weights`` (float32, optional) [layers, requests, KV heads,
+    budget] and ``new_lens`` (int32 [requests], optional) receive which they were, their weights
+    and how many."""
+    import torch
+    L, R, H = step.geom.num_layers, step.step.num_requests, step.geom.num_kv_heads
+    if weights.dim() != 4 or weights.shape[3] < step.max_kv or weights.stride(3) != 1:
+        raise ValueError("weights: [layers, requests, KV heads, at least max_kv], contiguous in its last dimension")
+    a = kvs_evict_args()
+    a.weights = _f32("weights", weights, (L, R, H, weights.shape[3]), contiguous=False)
+    a.layer_stride, a.request_stride, a.head_stride = weights.stride(0), weights.stride(1), weights.stride(2)
+    _int32_tensor("dst_tables", dst_tables, 2)
+    if dst_tables.shape[0] != R or dst_tables.stride(1) != 1 or (R > 1 and dst_tables.stride(0) < dst_tables.shape[1]):
+        raise ValueError("dst_tables: one contiguous row per request")
+    a.dst_tables = dst_tables.data_ptr()
+    a.dst_stride = dst_tables.stride(0) if R > 1 else dst_tables.shape[1]
+    if dst_tables.shape[1] * step.geom.block_size < min(step.max_kv, budget):
+        raise KvsError(KVS_ERR_BOUNDS, f"new tables of {dst_tables.shape[1]} blocks do not hold {min(step.max_kv, budget)} tokens")
+    a.budget, a.sinks, a.recent = int(budget), int(sinks), int(recent)
+    if kept.dtype != torch.int32 or tuple(kept.shape) != (L, R, H, budget) or not kept.is_contiguous():
+        raise ValueError(f"kept: a contiguous int32 tensor of shape {(L, R, H, budget)} is needed")
+    a.kept = kept.data_ptr()
+    if new_weights is not None:
+        a.new_weights = _f32("new_weights", new_weights, (L, R, H, budget))
+    if new_lens is not None:
+        _int32_tensor("new_lens", new_lens, 1)
+        if new_lens.shape[0] != R:
+            raise ValueError("new_lens has one entry per request")
+        a.new_lens = new_lens.data_ptr()
+    g, c, s = step.refs
+    return _check(lib().kvs_evict(g, c, s, ctypes.byref(a), _stream(stream), flags))
 
 
 # ---- fast tier ------------------------------------------------------------

@@ -1,0 +1,315 @@
+"""The model operators on the paged cache against their definitions in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import ops_ref
+from ops_ref import Small
+from paper_2609_35065_gb300 import kvs
+
+pytestmark = pytest.mark.gpu
+
+
+def _attend(sm, causal=True, window=0, scale=None, decode=False, lse=True, stream=None):
+    step, q, _, _, _cache = sm.on_gpu(kvs, decode)
+    heads = sm.H * sm.G
+    out = torch.full((sm.N, heads, sm.D), 7.0, dtype=q.dtype, device="cuda")
+    z = torch.full((sm.N, heads), 7.0, device="cuda") if lse else None
+    ws = torch.full((kvs.kvs_attend_workspace(step, heads),), 255, dtype=torch.uint8, device="cuda")
+    kvs.kvs_attend(step, 0, q, out, z, scale, causal, window, ws, stream, kvs.KVS_F_VALIDATE)
+    return out, z
+
+
+def _check_attend(sm, causal=True, window=0, scale=None, decode=False):
+    out, z = _attend(sm, causal, window, scale, decode)
+    want, bound, lse, lse_bound = sm.attend(sm.D ** -0.5 if scale is None else scale, causal, window)
+    off = np.abs(out.double().cpu().numpy() - want)
+    assert (off <= bound).all(), (off / bound).max()
+    z = z.double().cpu().numpy()
+    empty = np.isneginf(lse)
+    assert (np.isneginf(z) == empty).all()
+    assert (np.abs(z[~empty] - lse[~empty]) <= lse_bound[~empty]).all()
+    assert (out[torch.from_numpy(empty).cuda()] == 0).all()
+    return out, z
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,H,G", [(128, 2, 4), (64, 3, 7), (80, 1, 1), (96, 2, 5), (8, 2, 3), (120, 1, 16), (128, 1, 40)])
+def test_decode_steps(dtype, D, H, G):
+    _check_attend(Small([1] * 6, [1, 2, 17, 128, 129, 700], H, G, D, dtype=dtype), decode=True)
+
+
+@pytest.mark.parametrize("B", [1, 3, 8, 16, 48, 256])
+def test_block_sizes(B):
+    _check_attend(Small([1, 5, 40], [300, 77, 513], 2, 4, 64, B))
+
+
+@pytest.mark.parametrize("new,lens", [
+    ([1], [1]), ([0, 3, 0], [5, 3, 0]), ([16], [16]), ([17], [33]), ([130], [130]), ([129, 1, 64], [1000, 999, 64]),
+    ([200], [513]), ([256], [256]), ([257], [2049]), ([5, 5], [4, 0]), ([300, 2], [260, 1000])])
+@pytest.mark.parametrize("G,D,dtype", [(4, 128, "bf16"), (5, 64, "f16"), (1, 128, "f16"), (8, 128, "bf16")])
+def test_chunks(new, lens, G, D, dtype):
+    _check_attend(Small(new, lens, 2, G, D, dtype=dtype))
+
+
+@pytest.mark.parametrize("window", [1, 7, 64, 129, 5000])
+@pytest.mark.parametrize("new,lens", [([1, 1], [500, 3]), ([200, 3], [700, 400]), ([6], [4])])
+def test_windows(window, new, lens):
+    _check_attend(Small(new, lens, 2, 4, 128), window=window)
+    _check_attend(Small(new, lens, 2, 4, 128), causal=False, window=window)
+
+
+@pytest.mark.parametrize("new,lens", [([3, 40], [1, 300]), ([130, 7], [129, 0]), ([300], [50])])
+def test_every_cached_token_is_seen_without_causality(new, lens):
+    _check_attend(Small(new, lens, 2, 4, 64), causal=False)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1.0, -0.3, 4.0])
+@pytest.mark.parametrize("new", [1, 150])
+def test_scales_and_peaked_rows(scale, new):
+    """Scores of +-100: rows whose softmax is one token, maxima that grow along the keys."""
+    sm = Small([new], [900], 2, 4, 64, spread=2.0)
+    k = sm.cache[0].view(-1, sm.H, sm.D)
+    at = sm.slots(0, np.arange(900))
+    k[at] *= torch.linspace(0.1, 2.0, 900)[:, None, None].to(k.dtype)
+    _check_attend(sm, scale=scale)
+
+
+@pytest.mark.parametrize("new,T", [(1, 20000), (3, 9001), (140, 8200)])
+def test_long_caches_are_split_and_joined(new, T):
+    sm = Small([new], [T], 1, 4, 128)
+    _check_attend(sm)
+
+
+def test_the_result_does_not_depend_on_the_neighbours():
+    """A request's rows come out the same bits alone and in a batch that is split alike, and from call to call."""
+    sm = Small([2, 150, 1], [700, 650, 350], 2, 4, 128)
+    a, za = _attend(sm)
+    for _ in range(3):
+        b, zb = _attend(sm)
+        assert torch.equal(a, b) and torch.equal(za, zb)
+
+
+def test_lse_may_be_left_out():
+    sm = Small([3], [100])
+    assert torch.equal(_attend(sm, lse=False)[0], _attend(sm)[0])
+
+
+def test_attention_on_another_stream():
+    sm = Small([2, 150], [700, 650], 2, 4, 128)
+    want = _attend(sm)[0]
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    assert torch.equal(_attend(sm, stream=s)[0], want)
+
+
+def test_a_graph_follows_the_lengths():
+    """A captured call reads lengths, tables and queries anew."""
+    sm = Small([1, 1], [700, 300], 2, 4, 128)
+    step, q, _, _, cache = sm.on_gpu(kvs, decode=True)
+    out, z = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    ws = torch.zeros(kvs.kvs_attend_workspace(step, q.shape[1]), dtype=torch.uint8, device="cuda")
+    out, lens = torch.zeros(2, sm.H * sm.G, sm.D, dtype=q.dtype, device="cuda"), step._keep[1]
+    s = torch.cuda.Stream()
+    kvs.kvs_attend(step, 0, q, out, z, None, True, 0, ws, s)
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        kvs.kvs_attend(step, 0, q, out, z, None, True, 0, ws, torch.cuda.current_stream())
+    for lengths in ([700, 300], [699, 1], [33, 0]):
+        lens.copy_(torch.tensor(lengths, dtype=torch.int32))
+        g.replay()
+        torch.cuda.synchronize()
+        sm.lens = lengths
+        want, bound, *_ = sm.attend(sm.D ** -0.5)
+        assert (np.abs(out.double().cpu().numpy() - want) <= bound).all()
+
+
+def test_out_of_bounds_entries_are_recorded_and_not_followed():
+    sm = Small([1, 1], [40, 40], 2, 4, 64)
+    sm.tables[1, 1] = sm.num_blocks
+    with pytest.raises(kvs.KvsError) as ei:
+        _attend(sm, decode=True)
+    assert ei.value.code == kvs.KVS_ERR_BOUNDS
+    good = Small([1, 1], [40, 40], 2, 4, 64)
+    assert torch.equal(_attend(good, decode=True)[0], _attend(good, decode=True)[0])     # the word is clear again
+    step, q, _, _, _ = good.on_gpu(kvs)
+    out = torch.full_like(q, 7.0).contiguous()
+    step._keep[1][1] = step.max_kv + 1
+    ws = torch.zeros(kvs.kvs_attend_workspace(step, q.shape[1]) + 16, dtype=torch.uint8, device="cuda")
+    kvs.kvs_attend(step, 0, q, out, None, None, True, 0, ws)
+    with pytest.raises(kvs.KvsError):
+        kvs.kvs_check_errors()
+    assert (out[1] == 7.0).all() or (out[1] == 0.0).all()
+
+
+# ---- weights ----------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,lens,H,G,D,B,causal,window,decay", [
+    ([1, 1, 1], [1, 130, 700], 2, 4, 128, 16, True, 0, 0.5), ([1], [257], 1, 1, 64, 1, True, 0, 1.0), ([3, 0, 40], [50, 9, 300], 2, 7, 80, 16, True, 0, 0.0),
+    ([130], [128], 2, 4, 64, 16, True, 0, 0.9), ([200, 1], [600, 600], 1, 5, 128, 32, True, 100, 0.9), ([20], [90], 2, 3, 96, 3, False, 0, 1.0),
+    ([260], [900], 1, 8, 128, 16, True, 0, 1.0), ([4], [0], 2, 2, 64, 16, True, 0, 1.0), ([7], [300], 1, 40, 128, 16, False, 5, 0.25)])
+def test_weights(dtype, new, lens, H, G, D, B, causal, window, decay):
+    sm = Small(new, lens, H, G, D, B, dtype)
+    step, q, _, _, _cache = sm.on_gpu(kvs)
+    scale = D ** -0.5
+    lse = sm.attend(scale, causal, window)[2].astype(np.float32)
+    S = max(max(lens), 1) + 3
+    before = np.random.default_rng(1).random((sm.R, H, S)).astype(np.float32)
+    step.step.max_kv = step.max_kv = max(lens)
+    w = torch.from_numpy(before).cuda()
+    if decay == 0.0:
+        w[:] = float("nan")
+    kvs.kvs_weigh(step, 0, q, torch.from_numpy(lse).cuda(), w, None, decay, causal, window, None, kvs.KVS_F_VALIDATE)
+    want, bound = sm.weigh(lse, before, decay, scale, causal, window)
+    got = w.double().cpu().numpy()
+    for r, T in enumerate(lens):
+        off = np.abs(got[r, :, :T] - want[r, :, :T])
+        assert (off <= bound[r, :, :T]).all(), (off / bound[r, :, :T]).max()
+        rest = w.cpu().numpy()[r, :, T:]
+        assert np.isnan(rest).all() if decay == 0.0 else (rest == before[r, :, T:]).all()
+
+
+def test_weights_add_up_to_the_rows():
+    """Every row spreads a weight of one over the tokens it sees."""
+    sm = Small([3, 150], [700, 420], 2, 4, 128)
+    step, q, _, _, _cache = sm.on_gpu(kvs)
+    out, z = torch.empty(q.shape, dtype=q.dtype, device="cuda"), torch.empty(q.shape[:2], device="cuda")
+    ws = torch.empty(kvs.kvs_attend_workspace(step, q.shape[1]), dtype=torch.uint8, device="cuda")
+    kvs.kvs_attend(step, 0, q, out, z, workspace=ws)
+    w = torch.zeros(2, 2, step.max_kv, device="cuda")
+    kvs.kvs_weigh(step, 0, q, z, w)
+    total = w.double().sum(-1).cpu().numpy()
+    rows = np.array(sm.new)[:, None] * sm.G
+    assert (np.abs(total / rows - 1) < 1e-4).all()
+
+
+# ---- append -----------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,rot,inter", [(128, 128, False), (128, 64, False), (128, 128, True), (64, 64, False), (80, 80, False), (80, 20, True),
+                                         (96, 24, False), (8, 8, False), (8, 2, True), (120, 40, False), (128, 6, False), (72, 32, False)])
+@pytest.mark.parametrize("new,lens", [([1, 1], [1, 40]), ([3, 0, 33], [3, 7, 100])])
+def test_append(dtype, D, rot, inter, new, lens):
+    sm = Small(new, lens, 2, 3, D, dtype=dtype)
+    step, q, k, v, cache = sm.on_gpu(kvs, decode=new == [1, 1])
+    turns, scale = kvs.kvs_rope_turns(rot, 10000.0)
+    positions = np.random.default_rng(2).integers(0, 200000, sm.N).astype(np.int32)
+    positions[0] = 1 << 24
+    rope = kvs.Rope(torch.from_numpy(turns).cuda(), rot, inter, 1.5)
+    q_out = torch.empty(q.shape, dtype=q.dtype, device="cuda")
+    before = cache.clone()
+    kvs.kvs_append(step, 0, q, k, v, q_out, rope, torch.from_numpy(positions).cuda(), None, kvs.KVS_F_VALIDATE)
+    want = before.view(2, -1, sm.H, D).clone()
+    at = np.concatenate([sm.slots(r, np.arange(T - n, T)) for r, (n, T) in enumerate(zip(new, lens))])
+    unit = ops_ref.UNIT[dtype]
+    got_k = cache.view(2, -1, sm.H, D)[0, at]
+    for x, got in ((q, q_out), (k, got_k)):
+        x = x.double().cpu().numpy()
+        y = ops_ref.rotate(x, positions, turns, rot, inter, 1.5)
+        y[..., rot:] = x[..., rot:]
+        off = np.abs(got.double().cpu().numpy() - y)
+        big = np.abs(x).max(-1, keepdims=True)
+        assert (off <= unit * np.abs(y) + 1.5 * 2.0 ** -19 * big + 2.0 ** -25).all()
+        assert (off[..., rot:] == 0).all()
+    want[0, at], want[1, at] = got_k, v
+    assert torch.equal(cache.view(torch.int16), want.view(cache.shape).view(torch.int16))
+
+
+def test_append_in_place_without_rope_and_without_queries():
+    sm = Small([4], [20], 2, 3, 64)
+    step, q, k, v, cache = sm.on_gpu(kvs)
+    at = sm.slots(0, np.arange(16, 20))
+    kvs.kvs_append(step, 0, None, k, v)
+    flat = cache.view(2, -1, sm.H, sm.D)
+    assert torch.equal(flat[0, at], k) and torch.equal(flat[1, at], v)
+    turns, _ = kvs.kvs_rope_turns(64)
+    rope = kvs.Rope(torch.from_numpy(turns).cuda(), 64)
+    out = torch.empty_like(q).contiguous()
+    kvs.kvs_append(step, 0, q, k, v, out, rope)
+    kvs.kvs_append(step, 0, q, k, v, None, rope)                  # positions: the tokens' places
+    assert torch.equal(q, out)
+    pos = torch.arange(16, 20, dtype=torch.int32, device="cuda")
+    step2, q2, k2, v2, _ = sm.on_gpu(kvs)
+    kvs.kvs_append(step2, 0, q2, k2, v2, out, rope, pos)
+    assert torch.equal(q, out)
+
+
+def test_tokens_beyond_the_cache_are_not_appended():
+    sm = Small([5], [3], 2, 2, 64)
+    step, q, k, v, cache = sm.on_gpu(kvs)
+    before = cache.clone()
+    kvs.kvs_append(step, 0, q, k, v, None, None, None, None, kvs.KVS_F_VALIDATE)
+    at = sm.slots(0, np.arange(3))
+    want = before.view(2, -1, sm.H, sm.D)
+    want[0, at], want[1, at] = k[2:], v[2:]
+    assert torch.equal(cache.view(torch.int16), before.view(torch.int16))
+
+
+# ---- eviction ---------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("lens,budget,sinks,recent,B,D,L,H", [
+    ([100, 37, 0, 1], 40, 4, 8, 16, 64, 2, 2), ([3000, 1025], 1024, 0, 0, 16, 128, 1, 3), ([513], 1, 0, 1, 8, 80, 3, 1),
+    ([600, 599], 77, 70, 7, 1, 8, 2, 2), ([65, 2048], 64, 1, 0, 32, 96, 1, 4)])
+@pytest.mark.parametrize("kind", ["random", "ties", "odd"])
+def test_evict(dtype, lens, budget, sinks, recent, B, D, L, H, kind):
+    Wd = -(-budget // B)
+    R = len(lens)
+    sm = Small([0] * R, lens, H, 1, D, B, dtype, L=L, extra_blocks=R * Wd + 3)
+    step, _, _, _, cache = sm.on_gpu(kvs)
+    rng = np.random.default_rng(3)
+    S = step.max_kv + 5
+    w = rng.random((L, R, H, S)).astype(np.float32)
+    if kind == "ties":
+        w = np.floor(w * 4).astype(np.float32)
+    if kind == "odd":
+        pick = rng.integers(0, 8, w.shape)
+        w = np.where(pick == 0, np.nan, np.where(pick == 1, np.inf, np.where(pick == 2, -w, np.where(pick == 3, -0.0, np.where(pick == 4, 0.0, w))))).astype(np.float32)
+        w[..., 1::7] = -np.inf
+    free = np.setdiff1d(np.arange(sm.num_blocks), sm.tables.numpy().ravel())
+    dst = torch.from_numpy(rng.permutation(free)[: R * Wd].reshape(R, Wd).astype(np.int32))
+    kept = torch.full((L, R, H, budget), -7, dtype=torch.int32, device="cuda")
+    nw = torch.full((L, R, H, budget), -7.0, device="cuda")
+    nl = torch.full((R,), -7, dtype=torch.int32, device="cuda")
+    before = cache.clone()
+    kvs.kvs_evict(step, torch.from_numpy(w).cuda(), dst.cuda(), budget, sinks, recent, kept, nw, nl, None, kvs.KVS_F_VALIDATE)
+    want = ops_ref.evict(w, lens, budget, sinks, recent)
+    assert (kept.cpu().numpy() == want).all()
+    assert nl.tolist() == [min(T, budget) for T in lens]
+    want_w, flat = np.zeros(want.shape, np.float32), before.view(2 * L, -1, H, D).clone()
+    src = before.view(2 * L, -1, H, D)
+    for l in range(L):
+        for r in range(R):
+            J = min(lens[r], budget)
+            if not J:
+                continue
+            j = np.arange(J)
+            to = torch.from_numpy(dst[r].numpy().astype(np.int64)[j // B] * B + j % B).cuda()
+            for h in range(H):
+                want_w[l, r, h, :J] = w[l, r, h, want[l, r, h, :J]]
+                at = torch.from_numpy(sm.slots(r, want[l, r, h, :J])).cuda()
+                for p in (2 * l, 2 * l + 1):
+                    flat[p, to, h] = src[p, at, h]
+    assert np.array_equal(nw.cpu().numpy().view(np.uint32), want_w.view(np.uint32))
+    assert torch.equal(cache.view(torch.int16), flat.view(cache.shape).view(torch.int16))
+
+
+def test_a_step_through_all_operators():
+    """Append, attend, weigh, evict, and attend again over what was kept: with every token kept,
+    the second attention is the first."""
+    sm = Small([3, 1], [90, 64], 2, 4, 64, extra_blocks=20)
+    step, q, k, v, cache = sm.on_gpu(kvs)
+    turns, scale = kvs.kvs_rope_turns(64)
+    kvs.kvs_append(step, 0, q, k, v, None, kvs.Rope(torch.from_numpy(turns).cuda(), 64, scale=scale))
+    out, z = torch.empty(q.shape, dtype=q.dtype, device="cuda"), torch.empty(q.shape[:2], device="cuda")
+    kvs.kvs_attend(step, 0, q, out, z, workspace=torch.empty(kvs.kvs_attend_workspace(step, 8), dtype=torch.uint8, device="cuda"))
+    w = torch.zeros(1, 2, 2, step.max_kv, device="cuda")
+    kvs.kvs_weigh(step, 0, q, z, w[0])
+    free = np.setdiff1d(np.arange(sm.num_blocks), sm.tables.numpy().ravel())[:12].reshape(2, 6)
+    dst = torch.from_numpy(free.astype(np.int32)).cuda()
+    kept = torch.empty(1, 2, 2, 96, dtype=torch.int32, device="cuda")
+    lens = torch.empty(2, dtype=torch.int32, device="cuda")
+    kvs.kvs_evict(step, w, dst, 96, 4, 8, kept, None, lens)
+    again = kvs.Step((1, 2, 64, 2, 16, 16), [cache[0], cache[1]], sm.num_blocks, dst, lens, step._keep[2], total_q=4, max_q=3)
+    out2 = torch.empty_like(out)
+    kvs.kvs_attend(again, 0, q, out2, workspace=torch.empty(kvs.kvs_attend_workspace(again, 8) + 16, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(out, out2)
