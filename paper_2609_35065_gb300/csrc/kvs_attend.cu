@@ -322,19 +322,36 @@ cudaError_t attend_rows(const AttendJob& j, cudaStream_t s) {
 
 }  // namespace
 
-int attend_splits(int requests, int kv_heads, int group, int max_q, int max_kv, int head_dim, int sms) {
-    const int64_t tiles = ((int64_t)max_q * group + kRows - 1) / kRows * kv_heads * requests;
-    if (tiles == 0) return 1;
-    const int64_t most = (max_kv + 255) / 256;                   // a part of at least 256 keys
-    int64_t n = (2 * (int64_t)sms + tiles - 1) / tiles;
-    if (n > most) n = most;
-    if (n > 256) n = 256;
-    return n < 1 ? 1 : (int)n;
+AttendPlan attend_plan(const StepView& st, int sms) {
+    const int64_t rows = (int64_t)st.max_q * st.group, units = (int64_t)st.kv_heads * st.requests;
+    AttendPlan p{rows > 32, 1};
+    if (p.tc) {
+        // One CTA of 256 rows to an SM: as many parts as keep the number of waves times a
+        // part's steps (of 128 keys, and about four of start and end) lowest.
+        const int64_t tiles = (rows + 255) / 256 * units, steps = (st.max_kv + 127) / 128;
+        int64_t best = -1;
+        for (int64_t n = 1; n <= 64 && n <= (steps + 1) / 2; ++n) {
+            const int64_t cost = (tiles * n + sms - 1) / sms * ((steps + n - 1) / n + 4);
+            if (best < 0 || cost < best) {
+                best = cost;
+                p.splits = (int)n;
+            }
+        }
+        return p;
+    }
+    const int64_t tiles = (rows + kRows - 1) / kRows * units, most = (st.max_kv + 255) / 256;      // a part of at least 256 keys
+    if (tiles > 0) {
+        int64_t n = (2 * (int64_t)sms + tiles - 1) / tiles;
+        n = n > most ? most : n;
+        p.splits = (int)(n < 1 ? 1 : n > 256 ? 256 : n);
+    }
+    return p;
 }
 
 int launch_attend(const AttendJob& j, bool half, cudaStream_t s) {
     cudaError_t e;
-    if (j.step.head_dim <= 64) e = half ? attend_rows<true, 64, 3>(j, s) : attend_rows<false, 64, 3>(j, s);
+    if (j.tc) e = launch_attend_tc(j, half, s);
+    else if (j.step.head_dim <= 64) e = half ? attend_rows<true, 64, 3>(j, s) : attend_rows<false, 64, 3>(j, s);
     else e = half ? attend_rows<true, 128, 3>(j, s) : attend_rows<false, 128, 3>(j, s);
     if (e != cudaSuccess) return -(int)e;
     if (j.splits == 1) return 1;

@@ -1,0 +1,446 @@
+// kvs_attend_tc.cu -- attention of many packed rows: the products on the tensor cores.
+//
+// A CTA holds 256 packed rows (row = token * group + head) of one KV head as two tiles of 128
+// and goes over the keys 128 at a time:
+//
+//     S = Q K^T  (tensor memory)  ->  P = 2^(c S - c m)  (registers, back over S)  ->  O += P V
+//
+// While one tile's softmax runs on its warpgroup, the tensor cores work on the other's.
+// Warpgroups 0 and 1: a tile's softmax each, a row to a thread, so that maxima and sums need
+// no exchange.  Warpgroup 2 loads K and V through a ring of 32 KiB tiles: TMA boxes of whole
+// blocks where the block size allows, cp.async row by row otherwise and for the tiles that
+// hold the ends of what may be read (there, rows outside become zeros).  One thread of
+// warpgroup 3 issues the products.
+//
+// The running maximum m that O and the sums refer to is raised only when a row's maximum
+// outgrows it by 2^8: until then P is up to 2^8 instead of 1, which costs binary32 sums and
+// 16-bit floating P nothing, and O need not be rescaled, which most tiles then never do.
+//
+// Products run in the order in which one thread issues them, which the reuse of S's columns
+// for P relies on: S of the next tile is issued behind the product that reads P.
+#include "kvs_ops.cuh"
+#include "kvs_tcgen05.cuh"
+
+namespace kvs {
+namespace {
+
+constexpr int kM = 128, kN = 128;                  // rows of a tile, keys of a step
+constexpr int kThreads = 512;
+constexpr float kNone = -INFINITY;
+constexpr float kRaise = 8.0f;                     // log2 by which P may exceed 1
+
+template <int DP>
+struct Plan {
+    static constexpr int tile = kN * DP * 2;       // bytes of a tile of Q, K or V
+    static constexpr int stages = DP == 128 ? 5 : 8;
+    static constexpr int bars = 2 * kM * DP * 2 + stages * tile;
+    static constexpr int bytes = bars + 256 + 1024;
+};
+
+struct Bars {
+    uint32_t q, full, free, s, p, o;
+    __device__ Bars(uint32_t at, int stages) : q(at), full(at + 8), free(full + 8 * stages), s(free + 8 * stages), p(s + 16), o(p + 16) {}
+};
+
+template <bool HALF, int DP>
+__global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j, const __grid_constant__ CUtensorMap k_map,
+                                                                    const __grid_constant__ CUtensorMap v_map, int32_t boxes) {
+    extern __shared__ char raw[];
+    using N = Num<HALF>;
+    using P = Plan<DP>;
+    const StepView& st = j.step;
+    const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
+    const uint32_t ring = base + 2 * P::tile, ctl = base + P::bars;
+    const Bars bar(ctl, P::stages);
+    const uint32_t tmem_at = bar.o + 8;
+    const int wg = threadIdx.x >> 7, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    const int32_t tiles = gridDim.x / j.splits, split = blockIdx.x % j.splits;
+    const int32_t r = blockIdx.z, h = blockIdx.y;
+    // The last rows see the most keys: they come first, so that no long CTA starts last.
+    const int32_t row0 = (tiles - 1 - (int32_t)(blockIdx.x / j.splits)) * 2 * kM;
+    const Request q = load_request(st, r);
+    const int32_t rows = min(2 * kM, q.n * st.group - row0);
+    if (rows <= 0) return;
+    Span all = seen_by(q, row0 / st.group, (row0 + rows - 1) / st.group, j.causal, j.window);
+    const int32_t first = all.lo / kN, steps_all = all.hi > all.lo ? (all.hi + kN - 1) / kN - first : 0;
+    const int32_t j0 = first + (int32_t)((int64_t)steps_all * split / j.splits);
+    const int32_t steps = first + (int32_t)((int64_t)steps_all * (split + 1) / j.splits) - j0;
+    const int32_t* table = st.tables + (int64_t)r * st.table_stride;
+
+    if (threadIdx.x == 0) {
+        mbar_init(bar.q, 256);
+        for (int i = 0; i < P::stages; ++i) {
+            mbar_init(bar.full + 8 * i, 4);                   // a loading warp each
+            mbar_init(bar.free + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar.s + 8 * i, 1);
+            mbar_init(bar.p + 8 * i, 128);
+        }
+        mbar_init(bar.o, 1);
+        mbar_init_fence();
+    }
+    if (warp == 12) tmem_alloc(tmem_at, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at) : "memory");
+    auto s_at = [&](int t) { return tmem + 128u * t; };
+    auto o_at = [&](int t) { return tmem + 256u + (uint32_t)DP * t; };
+
+    // A wait that does not end is recorded; every role then leaves its loop (the others' waits end too).
+    auto wait = [&](uint32_t b, uint32_t parity) {
+        if (mbar_wait(b, parity, kWaitLimitNs)) return true;
+        record_error(st.err, KVS_ERR_TIMEOUT);
+        return false;
+    };
+
+    if (wg == 2) {
+        // ---- K and V: tile i is K (even) or V (odd) of step i / 2 ------------------
+        regs_dec<56>();
+        const int t = threadIdx.x - 256;
+        int pending = -1;                                    // cp.async tile not yet announced
+        auto announce = [&]() {
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.full + 8 * pending);
+            pending = -1;
+        };
+        int32_t i = 0;
+        for (; i < 2 * steps; ++i) {
+            const int stage = i % P::stages;
+            if (i >= P::stages) {
+                const bool ok = lane != 0 || wait(bar.free + 8 * stage, (i / P::stages - 1) & 1);
+                if (!__all_sync(0xffffffffu, ok)) break;
+            }
+            const uint32_t dst = ring + stage * P::tile;
+            const int32_t t0 = (j0 + (i >> 1)) * kN;
+            const bool is_v = i & 1;
+            // Beyond the cache, and before what the rows see, V has to be zeros; K may be anything there.
+            const bool whole = t0 >= all.lo && t0 + kN <= q.T;
+            if (boxes && (whole || !is_v)) {
+                if (pending >= 0) {
+                    cp_wait<0>();
+                    announce();
+                }
+                if (t >= 32) {
+                    if (lane == 0) mbar_arrive(bar.full + 8 * stage);
+                } else {
+                    const int32_t box = min(st.block_size, kN), count = (min(kN, q.T - t0) + box - 1) / box;
+                    if (lane == 0) mbar_expect_tx(bar.full + 8 * stage, (uint32_t)count * box * DP * 2);
+                    __syncwarp();
+                    if (lane < count) {
+                        const uint32_t tok = t0 + lane * box, blk = block_of(st, tok);
+                        int32_t b = __ldg(table + blk);
+                        if ((uint32_t)b >= (uint32_t)st.num_blocks) {
+                            record_error(st.err, KVS_ERR_BOUNDS);
+                            b = st.num_blocks;               // reads as zeros
+                        }
+                        const CUtensorMap* m = is_v ? &v_map : &k_map;
+#pragma unroll
+                        for (int c = 0; c < DP / 64; ++c)
+                            tma_load_4d(dst + c * kN * 128 + lane * box * 128, m, 64 * c, h, tok - blk * st.block_size, b, bar.full + 8 * stage);
+                    }
+                    __syncwarp();
+                }
+            } else {
+                const char* plane = is_v ? j.v_plane : j.k_plane;
+                // a row to 16 threads; a thread looks its rows' places up once for all its vectors
+                constexpr int CH = DP / 8;
+#pragma unroll 4
+                for (int v = t; v < kN * CH; v += 128) {
+                    const int k = v / CH, c = v % CH;
+                    const int32_t tok = t0 + k;
+                    const int64_t row = tok >= all.lo && tok < q.T ? row_of(st, table, tok) : -1;
+                    const bool there = row >= 0 && 8 * c < st.head_dim;
+                    cp_async16(dst + (c >> 3) * kN * 128 + k * 128 + (((c & 7) ^ (k & 7)) << 4),
+                               plane + (there ? 2 * (row + (int64_t)h * st.head_dim + 8 * c) : 0), there);
+                }
+                cp_commit();
+                if (pending >= 0) {
+                    cp_wait<1>();
+                    announce();
+                }
+                pending = stage;
+            }
+        }
+        cp_wait<0>();
+        if (pending >= 0) announce();
+        // Before the CTA leaves, every load has landed (all of them have when the products are done).
+        if (i < 2 * steps)
+            for (int k = i - P::stages < 0 ? 0 : i - P::stages; k < i; ++k)
+                mbar_wait(bar.full + 8 * (k % P::stages), (k / P::stages) & 1, kWaitLimitNs);
+    } else if (wg == 3) {
+        regs_dec<56>();
+        if (warp == 12 && lane == 0 && steps > 0) {
+            // ---- the products --------------------------------------------------------
+            constexpr uint32_t id_s = tc_idesc(HALF, kN, false), id_o = tc_idesc(HALF, DP, true);
+            auto issue_s = [&](int t, int stage) {
+                const uint32_t qa = base + t * P::tile, kb = ring + stage * P::tile;
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k) {
+                    const uint32_t off = (k >> 2) * kN * 128 + (k & 3) * 32;
+                    tc_mma_ss(s_at(t), tc_desc(qa + off, 16, 1024), tc_desc(kb + off, 16, 1024), id_s, k > 0);
+                }
+                tc_commit(bar.s + 8 * t);
+            };
+            auto issue_o = [&](int t, int stage, bool add) {
+                const uint32_t vb = ring + stage * P::tile;
+#pragma unroll
+                for (int k = 0; k < kN / 16; ++k)
+                    tc_mma_ts(o_at(t), s_at(t) + 8 * k, tc_desc(vb + k * 2048, kN * 128, 1024), id_o, add || k > 0);
+            };
+            auto stage_of = [&](int32_t i) { return i % P::stages; };
+            auto filled = [&](int32_t i) { return wait(bar.full + 8 * (i % P::stages), (i / P::stages) & 1); };
+            bool ok = wait(bar.q, 0) && filled(0);
+            if (ok) {
+                tc_fence_after();
+                issue_s(0, 0);
+                issue_s(1, 0);
+                tc_commit(bar.free);
+            }
+            for (int32_t k = 0; ok && k < steps; ++k) {
+                const bool more = k + 1 < steps;
+                const int vs = stage_of(2 * k + 1), ks = stage_of(2 * k + 2);
+                ok = filled(2 * k + 1) && wait(bar.p, k & 1);
+                if (!ok) break;
+                tc_fence_after();
+                issue_o(0, vs, k > 0);
+                if (more) {
+                    ok = filled(2 * k + 2);
+                    if (!ok) break;
+                    issue_s(0, ks);
+                }
+                ok = wait(bar.p + 8, k & 1);
+                if (!ok) break;
+                tc_fence_after();
+                issue_o(1, vs, k > 0);
+                tc_commit(bar.free + 8 * vs);
+                if (more) {
+                    issue_s(1, ks);
+                    tc_commit(bar.free + 8 * ks);
+                }
+            }
+            tc_commit(bar.o);
+            if (!ok) mbar_wait(bar.o, 0, kWaitLimitNs);
+        }
+        __syncwarp();
+    } else {
+        // ---- softmax: tile wg, one row to a thread -----------------------------------
+        regs_inc<200>();
+        const int t = threadIdx.x & 127;
+        const uint32_t qdst = base + wg * P::tile;
+        {
+            // Q: 16-byte vectors; a negative scale's sign goes into Q, so that maxima of S are those of the scores
+            constexpr int CH = DP / 8;
+            const uint32_t flip = j.scale_log2 < 0.0f ? 0x80008000u : 0u;
+#pragma unroll 4
+            for (int v = t; v < kM * CH; v += 128) {
+                const int i = v / CH, c = v % CH, p = row0 + wg * kM + i;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (wg * kM + i < rows && 8 * c < st.head_dim) {
+                    const int32_t tok = p / st.group, head = h * st.group + (p - tok * st.group);
+                    x = __ldg(reinterpret_cast<const uint4*>(j.q.base + 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)head * j.q.head + 8 * c)));
+                    x.x ^= flip;
+                    x.y ^= flip;
+                    x.z ^= flip;
+                    x.w ^= flip;
+                }
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                             :: "r"(qdst + (c >> 3) * kM * 128 + i * 128 + (((c & 7) ^ (i & 7)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+            }
+            fence_async_smem();
+            mbar_arrive(bar.q);
+        }
+        const float c = fmaxf(fabsf(j.scale_log2), 1e-36f);         // a zero scale keeps -infinity * c what it is
+        const int32_t p = row0 + wg * kM + t, tok = p / st.group, head = h * st.group + (p - tok * st.group);
+        const bool live = wg * kM + t < rows;
+        Span see{0, 0};
+        if (live) see = seen_by(q, tok, tok, j.causal, j.window);
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // lane 32 (warp % 4) of tensor memory
+        float m = kNone, l0 = 0.0f, l1 = 0.0f;
+        bool ok = true;
+        for (int32_t k = 0; k < steps; ++k) {
+            ok = __all_sync(0xffffffffu, wait(bar.s + 8 * wg, k & 1));
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t sr[kN];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) tmem_ld32(sr + 32 * b, s_at(wg) + lanes + 32 * b);
+            tmem_wait_ld();
+#pragma unroll
+            for (int b = 0; b < 4; ++b) tmem_loaded32(sr + 32 * b);
+            float* s = reinterpret_cast<float*>(sr);
+            const int32_t t0 = (j0 + k) * kN;
+            const bool edge = t0 < see.lo || t0 + kN > see.hi;
+            if (__any_sync(0xffffffffu, edge)) {
+                const int32_t a = see.lo - t0, b = see.hi - t0;
+#pragma unroll
+                for (int n = 0; n < kN; ++n) s[n] = n >= a && n < b ? s[n] : kNone;
+            }
+            float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+            for (int n = 4; n < kN; n += 8) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mx[e] = n + 4 + e < kN ? fmaxf(fmaxf(mx[e], s[n + e]), s[n + 4 + e]) : fmaxf(mx[e], s[n + e]);
+            }
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            // raise the reference? (m = -infinity: nothing was summed yet, O is zero or not yet written)
+            const bool raise = top > m && !((top - m) * c <= kRaise);
+            if (__any_sync(0xffffffffu, raise)) {
+                const float f = raise && m != kNone ? exp2_fast((m - top) * c) : 1.0f;
+                if (raise) m = top;
+                l0 *= f;
+                l1 *= f;
+                if (k > 0) {
+                    // the products before are done: this step's S was issued behind them
+#pragma unroll
+                    for (int b = 0; b < DP / 32; ++b) {
+                        uint32_t o[32];
+                        tmem_ld32(o, o_at(wg) + lanes + 32 * b);
+                        tmem_wait_ld();
+                        tmem_loaded32(o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_st32(o_at(wg) + lanes + 32 * b, o);
+                    }
+                }
+            }
+            const float off = m == kNone ? 0.0f : -m * c;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                uint32_t pk[32];
+#pragma unroll
+                for (int n = 0; n < 32; ++n) {
+                    float x = s[64 * b + 2 * n], y = s[64 * b + 2 * n + 1];
+                    fma2(x, y, c, off);
+                    x = exp2_fast(x);
+                    y = exp2_fast(y);
+                    add2(l0, l1, x, y);
+                    pk[n] = N::pack(x, y);
+                }
+                tmem_st32(s_at(wg) + lanes + 32 * b, pk);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(bar.p + 8 * wg);
+        }
+        // ---- the rows' results --------------------------------------------------------
+        if (steps > 0 && ok) ok = __all_sync(0xffffffffu, wait(bar.o, 0));
+        tc_fence_after();
+        const float l = l0 + l1;
+        const int64_t heads = (int64_t)st.kv_heads * st.group, row = (int64_t)(q.q0 + tok) * heads + head;
+        const int64_t all_rows = st.total_q * heads, at = split * all_rows + row;
+        const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+        const float m2 = m == kNone ? kNone : m * c;
+        if (ok) {
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b) {
+                uint32_t o[32];
+                if (steps > 0) {
+                    tmem_ld32(o, o_at(wg) + lanes + 32 * b);
+                    tmem_wait_ld();
+                    tmem_loaded32(o);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0;
+                }
+                if (l == 0.0f) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0;
+                }
+                if (live) {
+                    if (j.splits == 1) {
+                        char* dst = j.out.base + 2 * ((int64_t)(q.q0 + tok) * j.out.row + (int64_t)head * j.out.head + 32 * b);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (32 * b + 8 * e >= st.head_dim) break;
+                            uint4 w;
+                            uint32_t* pw = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+                                pw[x] = N::pack(__uint_as_float(o[8 * e + 2 * x]) * inv, __uint_as_float(o[8 * e + 2 * x + 1]) * inv);
+                            *reinterpret_cast<uint4*>(dst + 16 * e) = w;
+                        }
+                    } else {
+                        float* dst = j.partial + at * st.head_dim + 32 * b;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            if (32 * b + 4 * e >= st.head_dim) break;
+                            *reinterpret_cast<uint4*>(dst + 4 * e) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        }
+                    }
+                }
+            }
+            if (live) {
+                if (j.splits == 1) {
+                    if (j.lse) j.lse[row] = l == 0.0f ? kNone : (m2 + log2f(l)) * 0.69314718055994531f;
+                } else {
+                    reinterpret_cast<float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim)[at] = make_float2(m2, l);
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 12) tmem_dealloc(tmem, 512);
+}
+
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encoder() {
+    static const EncodeFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q{};
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        cudaGetLastError();
+        return (EncodeFn)f;
+    }();
+    return fn;
+}
+
+}  // namespace
+
+// The map of a plane [NB][B][H][D], in boxes of whole blocks (or 128 tokens of one) of one
+// head's 64 elements.  False where blocks do not tile 128 tokens, or the map is refused.
+bool plane_map(CUtensorMap* map, const StepView& st, const void* plane, bool half) {
+    const int B = st.block_size;
+    if (B % 8 || (128 % B && B % 128) || st.head_dim < 64 || !encoder()) return false;
+    const cuuint64_t d = st.head_dim, h = st.kv_heads;
+    const cuuint64_t dims[4] = {d, h, (cuuint64_t)B, (cuuint64_t)st.num_blocks};
+    const cuuint64_t strides[3] = {d * 2, d * h * 2, d * h * 2 * B};
+    if (strides[2] >= 1ull << 40) return false;
+    const cuuint32_t box[4] = {64, 1, (cuuint32_t)(B < 128 ? B : 128), 1}, one[4] = {1, 1, 1, 1};
+    return encoder()(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(plane), dims, strides, box,
+                     one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+namespace {
+
+template <bool HALF, int DP>
+cudaError_t attend_tc(const AttendJob& j, cudaStream_t s) {
+    auto* k = kvs_attend_tc_kernel<HALF, DP>;
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<DP>::bytes);
+    if (e != cudaSuccess) return e;
+    CUtensorMap km{}, vm{};
+    const bool boxes = plane_map(&km, j.step, j.k_plane, HALF) && plane_map(&vm, j.step, j.v_plane, HALF);
+    const int64_t tiles = ((int64_t)j.step.max_q * j.step.group + 2 * kM - 1) / (2 * kM);
+    k<<<dim3((unsigned)(tiles * j.splits), j.step.kv_heads, j.step.requests), kThreads, Plan<DP>::bytes, s>>>(j, km, vm, boxes);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tc(const AttendJob& j, bool half, cudaStream_t s) {
+    if (j.step.head_dim <= 64) return half ? attend_tc<true, 64>(j, s) : attend_tc<false, 64>(j, s);
+    return half ? attend_tc<true, 128>(j, s) : attend_tc<false, 128>(j, s);
+}
+
+}  // namespace kvs

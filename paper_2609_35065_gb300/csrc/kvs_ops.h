@@ -48,7 +48,7 @@ struct AttendJob {
     float    scale_log2;             // scale * log2(e)
     int32_t  causal, window;
     int32_t  splits;
-    int32_t  sms;
+    int32_t  tc;                     // 1: on the tensor cores' kernel
 };
 
 struct WeighJob {
@@ -80,8 +80,13 @@ int launch_append(const AppendJob& j, bool half, cudaStream_t s);
 int launch_attend(const AttendJob& j, bool half, cudaStream_t s);
 int launch_weigh(const WeighJob& j, bool half, cudaStream_t s);
 int launch_evict(const EvictJob& j, cudaStream_t s);
-// Parts that attention splits a request's cached tokens into, by the step's bounds alone.
-int attend_splits(int requests, int kv_heads, int group, int max_q, int max_kv, int head_dim, int sms);
+// How attention goes about a step, by its bounds alone: the kernel, and the parts that a
+// request's cached tokens are split into.
+struct AttendPlan {
+    int tc, splits;
+};
+AttendPlan attend_plan(const StepView& st, int sms);
+cudaError_t launch_attend_tc(const AttendJob& j, bool half, cudaStream_t s);
 
 // The current device's error word and number of SMs (kvs_api.cpp); allocates them at the first call.
 int ops_device(int32_t** err, int* sms);

@@ -180,7 +180,7 @@ int append_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
 }
 
 int64_t workspace_bytes(const StepView& v, int sms) {
-    const int n = attend_splits(v.requests, v.kv_heads, v.group, v.max_q, v.max_kv, v.head_dim, sms);
+    const int n = attend_plan(v, sms).splits;
     return n <= 1 ? 0 : (int64_t)n * v.total_q * v.kv_heads * v.group * (v.head_dim + 2) * 4;
 }
 
@@ -202,10 +202,12 @@ int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     j.scale_log2 = a->scale * kLog2e;
     j.causal = a->causal != 0;
     j.window = a->window;
-    KVS_TRY(ops_device(&j.step.err, &j.sms));
-    const StepView& v = j.step;
-    j.splits = attend_splits(v.requests, v.kv_heads, v.group, v.max_q, v.max_kv, v.head_dim, j.sms);
-    const int64_t need = workspace_bytes(v, j.sms);
+    int sms;
+    KVS_TRY(ops_device(&j.step.err, &sms));
+    const AttendPlan plan = attend_plan(j.step, sms);
+    j.tc = plan.tc;
+    j.splits = plan.splits;
+    const int64_t need = workspace_bytes(j.step, sms);
     if (need > 0) {
         if (!a->workspace) return ops_fail(KVS_ERR_INVALID_ARG, "workspace is NULL, %lld bytes are needed", (long long)need);
         if (a->workspace_bytes < need)

@@ -1,0 +1,116 @@
+// kvs_tcgen05.cuh -- the fifth-generation tensor cores (tcgen05.mma with accumulators in
+// tensor memory) and tiled TMA loads, as inline PTX.
+//
+// Operand tiles in shared memory are rows of 64 16-bit elements (128 bytes) in the 128-byte
+// swizzle: the 16-byte vector c of row r lies at r * 128 + ((c ^ (r & 7)) << 4) from a
+// 1024-byte aligned base.  Wider rows are further such tiles behind.
+#pragma once
+
+#include <cstdint>
+#include <cuda.h>
+
+#include "kvs_async.cuh"
+
+namespace kvs {
+namespace {
+
+// ---- tensor memory -----------------------------------------------------------
+// A whole warp allocates (columns: a power of two from 32 to 512); the address lands in shared memory.
+__device__ __forceinline__ void tmem_alloc(uint32_t smem_out, uint32_t columns) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_out), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc(uint32_t addr, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(addr), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Generic writes to shared memory before this are seen by the tensor cores and TMA after it.
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+#define KVS_R8(r, k) "=r"(r[k]), "=r"(r[k + 1]), "=r"(r[k + 2]), "=r"(r[k + 3]), "=r"(r[k + 4]), "=r"(r[k + 5]), "=r"(r[k + 6]), "=r"(r[k + 7])
+#define KVS_I8(r, k) "r"(r[k]), "r"(r[k + 1]), "r"(r[k + 2]), "r"(r[k + 3]), "r"(r[k + 4]), "r"(r[k + 5]), "r"(r[k + 6]), "r"(r[k + 7])
+#define KVS_U8(r, k) "+r"(r[k]), "+r"(r[k + 1]), "+r"(r[k + 2]), "+r"(r[k + 3]), "+r"(r[k + 4]), "+r"(r[k + 5]), "+r"(r[k + 6]), "+r"(r[k + 7])
+
+// 32 columns of the thread's lane (a warp reads lanes 32 (warp % 4) ...); valid after tmem_wait_ld.
+__device__ __forceinline__ void tmem_ld32(uint32_t* r, uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : KVS_R8(r, 0), KVS_R8(r, 8), KVS_R8(r, 16), KVS_R8(r, 24) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        :: KVS_I8(r, 0), KVS_I8(r, 8), KVS_I8(r, 16), KVS_I8(r, 24), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Keeps the compiler from using r[0..32) before the wait that this stands behind.
+__device__ __forceinline__ void tmem_loaded32(uint32_t* r) {
+    asm volatile("" : KVS_U8(r, 0), KVS_U8(r, 8), KVS_U8(r, 16), KVS_U8(r, 24) :: "memory");
+}
+
+// ---- matrix products ---------------------------------------------------------
+// Shared-memory operand.  K-major (rows are M or N, contiguous in K): stride = bytes between
+// groups of eight rows.  MN-major (rows are K, contiguous in M or N): stride = bytes between
+// groups of eight K rows, lead = bytes between groups of 64 columns.
+__device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t lead, uint32_t stride) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 |
+           1ull << 46 | 2ull << 61;
+}
+// 16-bit operands, 32-bit accumulators, M = 128.
+__host__ __device__ constexpr uint32_t tc_idesc(bool half, int n, bool b_mn_major) {
+    return 1u << 4 | (half ? 0u : 1u) << 7 | (half ? 0u : 1u) << 10 | (b_mn_major ? 1u : 0u) << 16 | (uint32_t)(n / 8) << 17 | 8u << 24;
+}
+// d (+)= a b over 16 elements of K, both operands in shared memory.
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+// ... with a in tensor memory: lane = row, two elements to a column.
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+// One arrival on `bar` when all products that this thread issued are done.
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+
+// ---- tiled loads of the paged planes -----------------------------------------
+// A box of [rows of a block][64 elements of one head]; the plane's map is [NB][B][H][D].  A
+// coordinate beyond the plane (a head dim's end, a block that there is not) reads as zeros.
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int32_t d, int32_t h, int32_t t, int32_t b, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        :: "r"(dst), "l"(map), "r"(bar), "r"(d), "r"(h), "r"(t), "r"(b) : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N)); }
+
+// Barrier of `threads` threads under a number of its own (1 to 15).
+__device__ __forceinline__ void bar_some(int id, int threads) { asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory"); }
+
+// (a0, a1) * (b, b) + (c, c), and sums, two binary32 numbers at a time.
+__device__ __forceinline__ void fma2(float& x, float& y, float b, float c) {
+    asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %2};\n\tmov.b64 r, {%3, %3};\n\t"
+        "fma.rn.f32x2 p, p, q, r;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(x), "+f"(y) : "f"(b), "f"(c));
+}
+__device__ __forceinline__ void add2(float& x, float& y, float a, float b) {
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\t"
+        "add.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+
+}  // namespace
+}  // namespace kvs
