@@ -18,7 +18,6 @@
 //
 // Products run in the order in which one thread issues them, which the reuse of S's columns
 // for P relies on: S of the next tile is issued behind the product that reads P.
-#include "kvs_ops.cuh"
 #include "kvs_tcgen05.cuh"
 
 namespace kvs {
@@ -76,7 +75,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar.s + 8 * i, 1);
-            mbar_init(bar.p + 8 * i, 128);
+            mbar_init(bar.p + 8 * i, 4);
         }
         mbar_init(bar.o, 1);
         mbar_init_fence();
@@ -128,36 +127,10 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                 if (t >= 32) {
                     if (lane == 0) mbar_arrive(bar.full + 8 * stage);
                 } else {
-                    const int32_t box = min(st.block_size, kN), count = (min(kN, q.T - t0) + box - 1) / box;
-                    if (lane == 0) mbar_expect_tx(bar.full + 8 * stage, (uint32_t)count * box * DP * 2);
-                    __syncwarp();
-                    if (lane < count) {
-                        const uint32_t tok = t0 + lane * box, blk = block_of(st, tok);
-                        int32_t b = __ldg(table + blk);
-                        if ((uint32_t)b >= (uint32_t)st.num_blocks) {
-                            record_error(st.err, KVS_ERR_BOUNDS);
-                            b = st.num_blocks;               // reads as zeros
-                        }
-                        const CUtensorMap* m = is_v ? &v_map : &k_map;
-#pragma unroll
-                        for (int c = 0; c < DP / 64; ++c)
-                            tma_load_4d(dst + c * kN * 128 + lane * box * 128, m, 64 * c, h, tok - blk * st.block_size, b, bar.full + 8 * stage);
-                    }
-                    __syncwarp();
+                    tile_boxes<DP>(dst, is_v ? &v_map : &k_map, st, table, h, t0, q.T, bar.full + 8 * stage, lane);
                 }
             } else {
-                const char* plane = is_v ? j.v_plane : j.k_plane;
-                // a row to 16 threads; a thread looks its rows' places up once for all its vectors
-                constexpr int CH = DP / 8;
-#pragma unroll 4
-                for (int v = t; v < kN * CH; v += 128) {
-                    const int k = v / CH, c = v % CH;
-                    const int32_t tok = t0 + k;
-                    const int64_t row = tok >= all.lo && tok < q.T ? row_of(st, table, tok) : -1;
-                    const bool there = row >= 0 && 8 * c < st.head_dim;
-                    cp_async16(dst + (c >> 3) * kN * 128 + k * 128 + (((c & 7) ^ (k & 7)) << 4),
-                               plane + (there ? 2 * (row + (int64_t)h * st.head_dim + 8 * c) : 0), there);
-                }
+                tile_rows<DP>(dst, is_v ? j.v_plane : j.k_plane, st, table, h, t0, all.lo, q.T, t);
                 cp_commit();
                 if (pending >= 0) {
                     cp_wait<1>();
@@ -241,7 +214,8 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                 const int i = v / CH, c = v % CH, p = row0 + wg * kM + i;
                 uint4 x = make_uint4(0, 0, 0, 0);
                 if (wg * kM + i < rows && 8 * c < st.head_dim) {
-                    const int32_t tok = p / st.group, head = h * st.group + (p - tok * st.group);
+                    int32_t g;
+                    const int32_t tok = token_of(st, p, g), head = h * st.group + g;
                     x = __ldg(reinterpret_cast<const uint4*>(j.q.base + 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)head * j.q.head + 8 * c)));
                     x.x ^= flip;
                     x.y ^= flip;
@@ -255,7 +229,8 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
             mbar_arrive(bar.q);
         }
         const float c = fmaxf(fabsf(j.scale_log2), 1e-36f);         // a zero scale keeps -infinity * c what it is
-        const int32_t p = row0 + wg * kM + t, tok = p / st.group, head = h * st.group + (p - tok * st.group);
+        int32_t g;
+        const int32_t tok = token_of(st, row0 + wg * kM + t, g), head = h * st.group + g;
         const bool live = wg * kM + t < rows;
         Span see{0, 0};
         if (live) see = seen_by(q, tok, tok, j.causal, j.window);
@@ -325,7 +300,8 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
             }
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(bar.p + 8 * wg);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.p + 8 * wg);
         }
         // ---- the rows' results --------------------------------------------------------
         if (steps > 0 && ok) ok = __all_sync(0xffffffffu, wait(bar.o, 0));
@@ -407,9 +383,7 @@ EncodeFn encoder() {
 
 }  // namespace
 
-// The map of a plane [NB][B][H][D], in boxes of whole blocks (or 128 tokens of one) of one
-// head's 64 elements.  False where blocks do not tile 128 tokens, or the map is refused.
-bool plane_map(CUtensorMap* map, const StepView& st, const void* plane, bool half) {
+bool plane_map(void* map, const StepView& st, const void* plane, bool half) {
     const int B = st.block_size;
     if (B % 8 || (128 % B && B % 128) || st.head_dim < 64 || !encoder()) return false;
     const cuuint64_t d = st.head_dim, h = st.kv_heads;
@@ -417,7 +391,7 @@ bool plane_map(CUtensorMap* map, const StepView& st, const void* plane, bool hal
     const cuuint64_t strides[3] = {d * 2, d * h * 2, d * h * 2 * B};
     if (strides[2] >= 1ull << 40) return false;
     const cuuint32_t box[4] = {64, 1, (cuuint32_t)(B < 128 ? B : 128), 1}, one[4] = {1, 1, 1, 1};
-    return encoder()(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(plane), dims, strides, box,
+    return encoder()((CUtensorMap*)map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(plane), dims, strides, box,
                      one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

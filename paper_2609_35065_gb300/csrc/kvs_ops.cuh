@@ -46,6 +46,13 @@ __device__ __forceinline__ uint32_t block_of(const StepView& st, uint32_t t) {
     return (uint32_t)(((uint64_t)t * st.block_m) >> st.block_p);
 }
 
+// Token and query head (of the KV head's) of a packed row.
+__device__ __forceinline__ int32_t token_of(const StepView& st, int32_t p, int32_t& g) {
+    const int32_t t = (int32_t)(((uint64_t)(uint32_t)p * st.group_m) >> st.group_p);
+    g = p - t * st.group;
+    return t;
+}
+
 // Element offset of cached token t's row in a plane; negative (and recorded) where the
 // table names a block that the cache does not have.
 __device__ __forceinline__ int64_t row_of(const StepView& st, const int32_t* table, uint32_t t) {

@@ -22,6 +22,7 @@ struct StepView {
     int32_t  num_blocks;
     int32_t  kv_heads, head_dim;
     int32_t  group;                  // query heads per KV head
+    uint32_t group_m, group_p;       // p / group = (p * group_m) >> group_p
 };
 
 struct RowsView {
@@ -78,7 +79,7 @@ struct EvictJob {
 // Each enqueues its kernels and returns how many (negative: a cudaError_t, negated).
 int launch_append(const AppendJob& j, bool half, cudaStream_t s);
 int launch_attend(const AttendJob& j, bool half, cudaStream_t s);
-int launch_weigh(const WeighJob& j, bool half, cudaStream_t s);
+int launch_weigh(const WeighJob& j, bool half, int sms, cudaStream_t s);
 int launch_evict(const EvictJob& j, cudaStream_t s);
 // How attention goes about a step, by its bounds alone: the kernel, and the parts that a
 // request's cached tokens are split into.
@@ -86,6 +87,9 @@ struct AttendPlan {
     int tc, splits;
 };
 AttendPlan attend_plan(const StepView& st, int sms);
+// A plane's TMA map (a CUtensorMap at `map`) in boxes of whole blocks, or of 128 tokens of one,
+// of one head's 64 elements; false where blocks do not tile 128 tokens (kvs_attend_tc.cu).
+bool plane_map(void* map, const StepView& st, const void* plane, bool half);
 cudaError_t launch_attend_tc(const AttendJob& j, bool half, cudaStream_t s);
 
 // The current device's error word and number of SMs (kvs_api.cpp); allocates them at the first call.

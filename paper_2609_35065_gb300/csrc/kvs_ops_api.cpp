@@ -79,6 +79,9 @@ int view_of(const kvs_geometry* g, const kvs_step* s, int32_t q_heads, StepView&
     v.kv_heads = g->num_kv_heads;
     v.head_dim = g->head_dim;
     v.group = q_heads > 0 ? q_heads / g->num_kv_heads : 0;
+    const FastDiv gd = make_fastdiv((uint32_t)(v.group ? v.group : 1));
+    v.group_m = gd.m;
+    v.group_p = gd.p;
     if ((int64_t)s->max_q * (v.group ? v.group : 1) > INT32_MAX / 2)
         return ops_fail(KVS_ERR_UNSUPPORTED, "max_q times the query heads of a KV head is above 2^30");
     return KVS_OK;
@@ -248,7 +251,7 @@ int weigh_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* 
     j.window = a->window;
     int sms;
     KVS_TRY(ops_device(&j.step.err, &sms));
-    return done(launch_weigh(j, st->dtype == KVS_DTYPE_F16, s), s, flags);
+    return done(launch_weigh(j, st->dtype == KVS_DTYPE_F16, sms, s), s, flags);
 }
 
 int evict_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* st, const kvs_evict_args* a, cudaStream_t s, uint32_t flags) {

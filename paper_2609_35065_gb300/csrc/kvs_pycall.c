@@ -9,6 +9,9 @@
  *
  * What it replaces cost 10 to 16 us for one chunk and 80 us for 128, most of a small
  * call; this takes about 1 us and 25 us.
+ *
+ * append, attend and weigh do the same for the model operators' tensors: whatever is not
+ * plainly right (a type, a shape, a stride) is left to the binding, which says what is wrong.
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -277,7 +280,234 @@ out:
     Py_RETURN_NONE;
 }
 
-static PyMethodDef methods[] = {{"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, NULL}, {NULL, NULL, 0, NULL}};
+/* ---- the model operators ------------------------------------------------- */
+static PyObject *s_dtype, *s_shape, *s_stride, *s_cuda_stream, *s_ref;
+
+/* `n` entries of a tuple (or subclass) of ints; 1 / 0. */
+static int int_tuple(PyObject* o, int n, int64_t* out) {
+    if (!o || !PyTuple_Check(o) || PyTuple_GET_SIZE(o) != n) return 0;
+    for (int k = 0; k < n; ++k)
+        if (!small_int(PyTuple_GET_ITEM(o, k), 0, INT64_MAX, &out[k])) return 0;
+    return 1;
+}
+
+typedef struct {
+    uint64_t at;
+    int64_t  shape[3], stride[3];
+} Tensor;
+
+/* A tensor of `dims` dimensions and of that dtype: 1, 0 (something else), -1 (exception). */
+static int read_tensor(PyObject* o, PyObject* dtype, int dims, Tensor* t) {
+    PyObject* x = PyObject_GetAttr(o, s_dtype);
+    int ok = x == dtype;
+    Py_XDECREF(x);
+    if (ok) {
+        x = PyObject_GetAttr(o, s_shape);
+        ok = int_tuple(x, dims, t->shape);
+        Py_XDECREF(x);
+    }
+    if (ok) {
+        x = PyObject_CallMethodNoArgs(o, s_stride);
+        ok = int_tuple(x, dims, t->stride);
+        Py_XDECREF(x);
+    }
+    if (PyErr_Occurred()) PyErr_Clear();
+    return ok ? address(o, &t->at) : 0;
+}
+
+typedef struct {
+    const kvs_geometry*    geom;
+    const kvs_paged_cache* cache;
+    const kvs_step*        step;
+} StepRef;
+
+/* fn, step (the three structs' addresses), dtype, float32, int32, layer, stream, flags: what every operator begins with. */
+enum { V_FN, V_STEP, V_DTYPE, V_F32, V_I32, V_LAYER, V_STREAM, V_FLAGS, V_MORE };
+
+static int read_common(PyObject* const* v, int64_t* fn, StepRef* st, int64_t* layer, int64_t* stream, int64_t* flags) {
+    if (!small_int(v[V_FN], 1, INT64_MAX, fn) || !PyBytes_CheckExact(v[V_STEP]) || PyBytes_GET_SIZE(v[V_STEP]) != (Py_ssize_t)sizeof *st ||
+        !small_int(v[V_LAYER], INT32_MIN, INT32_MAX, layer) || !small_int(v[V_FLAGS], 0, UINT32_MAX, flags))
+        return 0;
+    memcpy(st, PyBytes_AS_STRING(v[V_STEP]), sizeof *st);
+    *stream = 0;
+    if (v[V_STREAM] == Py_None || small_int(v[V_STREAM], 0, INT64_MAX, stream)) return 1;
+    PyObject* h = PyObject_GetAttr(v[V_STREAM], s_cuda_stream);
+    const int ok = h && small_int(h, 0, INT64_MAX, stream);
+    Py_XDECREF(h);
+    if (PyErr_Occurred()) PyErr_Clear();
+    return ok;
+}
+
+/* kvs_rows of a tensor [total_q, heads, head_dim]; *heads 0: any number, which it gets. */
+static int read_rows(PyObject* o, PyObject* dtype, const StepRef* st, int64_t* heads, kvs_rows* r) {
+    Tensor t;
+    const int ok = read_tensor(o, dtype, 3, &t);
+    if (ok != 1) return ok;
+    if (t.shape[0] != st->step->total_q || t.shape[2] != st->geom->head_dim || t.stride[2] != 1 || t.shape[1] > INT32_MAX ||
+        (*heads && t.shape[1] != *heads))
+        return 0;
+    *heads = t.shape[1];
+    r->base = (void*)(uintptr_t)t.at;
+    r->row_stride = t.stride[0];
+    r->head_stride = t.stride[1];
+    return 1;
+}
+
+/* A contiguous float32 tensor [total_q, heads]. */
+static int read_lse(PyObject* o, PyObject* f32, const StepRef* st, int64_t heads, void** out) {
+    Tensor t;
+    const int ok = read_tensor(o, f32, 2, &t);
+    if (ok != 1) return ok;
+    if (t.shape[0] != st->step->total_q || t.shape[1] != heads || (heads > 1 && t.stride[1] != 1) || (t.shape[0] > 1 && t.stride[0] != heads)) return 0;
+    *out = (void*)(uintptr_t)t.at;
+    return 1;
+}
+
+static int read_float(PyObject* o, float* out) {
+    if (!PyFloat_CheckExact(o)) return 0;
+    *out = (float)PyFloat_AS_DOUBLE(o);
+    return 1;
+}
+
+static int read_bool(PyObject* o, int32_t* out) {
+    *out = o == Py_True;
+    return o == Py_True || o == Py_False;
+}
+
+typedef int (*op_fn)(const kvs_geometry*, const kvs_paged_cache*, const kvs_step*, int32_t, const void*, void*, uint32_t);
+
+static PyObject* run_op(int got, int64_t fn, const StepRef* st, int64_t layer, const void* args, int64_t stream, int64_t flags) {
+    if (got < 0) return NULL;
+    if (got == 0) Py_RETURN_NONE;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((op_fn)(uintptr_t)fn)(st->geom, st->cache, st->step, (int32_t)layer, args, (void*)(uintptr_t)stream, (uint32_t)flags);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+#define TRY(call)                   \
+    do {                            \
+        if (got == 1) got = (call); \
+    } while (0)
+
+/* ..., q, k, v, q_out, rope, positions */
+static PyObject* append(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
+    (void)self;
+    int64_t fn, layer, stream, flags;
+    StepRef st;
+    kvs_append_args a;
+    memset(&a, 0, sizeof a);
+    if (nv != V_MORE + 6) {
+        PyErr_SetString(PyExc_TypeError, "append takes 14 arguments");
+        return NULL;
+    }
+    int got = read_common(v, &fn, &st, &layer, &stream, &flags);
+    PyObject* const* w = v + V_MORE;
+    int64_t heads = 0;
+    if (w[0] != Py_None) {
+        TRY(read_rows(w[0], v[V_DTYPE], &st, &heads, &a.q));
+        a.num_q_heads = (int32_t)heads;
+        if (w[3] == Py_None) a.q_out = a.q;
+        else TRY(read_rows(w[3], v[V_DTYPE], &st, &heads, &a.q_out));
+    }
+    int64_t H = got == 1 ? st.geom->num_kv_heads : 1;
+    TRY(read_rows(w[1], v[V_DTYPE], &st, &H, &a.k));
+    TRY(read_rows(w[2], v[V_DTYPE], &st, &H, &a.v));
+    if (w[4] != Py_None && got == 1) {
+        PyObject* ref = PyObject_GetAttr(w[4], s_ref);
+        int64_t x = 0;
+        got = ref && small_int(ref, 1, INT64_MAX, &x);
+        Py_XDECREF(ref);
+        if (PyErr_Occurred()) PyErr_Clear();
+        a.rope = (const kvs_rope*)(uintptr_t)x;
+    }
+    if (w[5] != Py_None) {
+        Tensor t;
+        TRY(read_tensor(w[5], v[V_I32], 1, &t));
+        if (got == 1) {
+            got = t.shape[0] == st.step->total_q && (t.shape[0] <= 1 || t.stride[0] == 1);
+            a.positions = (const int32_t*)(uintptr_t)t.at;
+        }
+    }
+    return run_op(got, fn, &st, layer, &a, stream, flags);
+}
+
+/* ..., q, out, lse, scale, causal, window, workspace, uint8 */
+static PyObject* attend(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
+    (void)self;
+    int64_t fn, layer, stream, flags, window = 0;
+    StepRef st;
+    kvs_attend_args a;
+    memset(&a, 0, sizeof a);
+    if (nv != V_MORE + 8) {
+        PyErr_SetString(PyExc_TypeError, "attend takes 16 arguments");
+        return NULL;
+    }
+    int got = read_common(v, &fn, &st, &layer, &stream, &flags);
+    PyObject* const* w = v + V_MORE;
+    int64_t heads = 0;
+    TRY(read_rows(w[0], v[V_DTYPE], &st, &heads, &a.q));
+    TRY(read_rows(w[1], v[V_DTYPE], &st, &heads, &a.out));
+    if (w[2] != Py_None) {
+        void* p = NULL;
+        TRY(read_lse(w[2], v[V_F32], &st, heads, &p));
+        a.lse = (float*)p;
+    }
+    TRY(read_float(w[3], &a.scale));
+    TRY(read_bool(w[4], &a.causal));
+    TRY(small_int(w[5], INT32_MIN, INT32_MAX, &window));
+    if (w[6] != Py_None) {
+        Tensor t;
+        TRY(read_tensor(w[6], w[7], 1, &t));
+        if (got == 1) {
+            got = t.stride[0] == 1 || t.shape[0] <= 1;
+            a.workspace = (void*)(uintptr_t)t.at;
+            a.workspace_bytes = t.shape[0];
+        }
+    }
+    a.window = (int32_t)window;
+    a.num_q_heads = (int32_t)heads;
+    return run_op(got, fn, &st, layer, &a, stream, flags);
+}
+
+/* ..., q, lse, weights, scale, decay, causal, window */
+static PyObject* weigh(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
+    (void)self;
+    int64_t fn, layer, stream, flags, window = 0;
+    StepRef st;
+    kvs_weigh_args a;
+    memset(&a, 0, sizeof a);
+    if (nv != V_MORE + 7) {
+        PyErr_SetString(PyExc_TypeError, "weigh takes 15 arguments");
+        return NULL;
+    }
+    int got = read_common(v, &fn, &st, &layer, &stream, &flags);
+    PyObject* const* w = v + V_MORE;
+    int64_t heads = 0;
+    void* p = NULL;
+    Tensor t;
+    TRY(read_rows(w[0], v[V_DTYPE], &st, &heads, &a.q));
+    TRY(read_lse(w[1], v[V_F32], &st, heads, &p));
+    TRY(read_tensor(w[2], v[V_F32], 3, &t));
+    if (got == 1) {
+        got = t.shape[0] == st.step->num_requests && t.shape[1] == st.geom->num_kv_heads && t.shape[2] >= st.step->max_kv && t.stride[2] == 1;
+        a.weights = (float*)(uintptr_t)t.at;
+        a.request_stride = t.stride[0];
+        a.head_stride = t.stride[1];
+    }
+    TRY(read_float(w[3], &a.scale));
+    TRY(read_float(w[4], &a.decay));
+    TRY(read_bool(w[5], &a.causal));
+    TRY(small_int(w[6], INT32_MIN, INT32_MAX, &window));
+    a.lse = (const float*)p;
+    a.window = (int32_t)window;
+    a.num_q_heads = (int32_t)heads;
+    return run_op(got, fn, &st, layer, &a, stream, flags);
+}
+
+#define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
+static PyMethodDef methods[] = {METHOD(call), METHOD(append), METHOD(attend), METHOD(weigh), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "kvs_pycall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit_kvs_pycall(void) {
@@ -288,5 +518,10 @@ PyMODINIT_FUNC PyInit_kvs_pycall(void) {
     s_num_tokens = PyUnicode_InternFromString("num_tokens");
     s_base = PyUnicode_InternFromString("base");
     s_residency = PyUnicode_InternFromString("residency");
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_shape = PyUnicode_InternFromString("shape");
+    s_stride = PyUnicode_InternFromString("stride");
+    s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+    s_ref = PyUnicode_InternFromString("ref");
     return PyModule_Create(&module);
 }

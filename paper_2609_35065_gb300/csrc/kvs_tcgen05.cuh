@@ -10,6 +10,7 @@
 #include <cuda.h>
 
 #include "kvs_async.cuh"
+#include "kvs_ops.cuh"
 
 namespace kvs {
 namespace {
@@ -92,6 +93,43 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
         :: "r"(dst), "l"(map), "r"(bar), "r"(d), "r"(h), "r"(t), "r"(b) : "memory");
+}
+
+// 128 cached tokens from t0 of one KV head, as a tile at dst.  By boxes: one warp, whose lane
+// 0 arrives on `bar` with the bytes; tokens beyond the cache's last block are left as they are.
+template <int DP>
+__device__ __forceinline__ void tile_boxes(uint32_t dst, const CUtensorMap* map, const StepView& st, const int32_t* table, int32_t h, int32_t t0, int32_t T,
+                                           uint32_t bar, int lane) {
+    const int32_t box = min(st.block_size, 128), count = (min(128, T - t0) + box - 1) / box;
+    if (lane == 0) mbar_expect_tx(bar, (uint32_t)count * box * DP * 2);
+    __syncwarp();
+    if (lane < count) {
+        const uint32_t tok = t0 + lane * box, blk = block_of(st, tok);
+        int32_t b = __ldg(table + blk);
+        if ((uint32_t)b >= (uint32_t)st.num_blocks) {
+            record_error(st.err, KVS_ERR_BOUNDS);
+            b = st.num_blocks;                                   // reads as zeros
+        }
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c)
+            tma_load_4d(dst + c * 128 * 128 + lane * box * 128, map, 64 * c, h, tok - blk * st.block_size, b, bar);
+    }
+    __syncwarp();
+}
+// By rows: 128 threads, of which this is t, with cp.async; tokens outside [lo, hi) become zeros.
+template <int DP>
+__device__ __forceinline__ void tile_rows(uint32_t dst, const char* plane, const StepView& st, const int32_t* table, int32_t h, int32_t t0, int32_t lo, int32_t hi,
+                                          int t) {
+    constexpr int CH = DP / 8;                                   // 16-byte vectors of a row
+#pragma unroll 4
+    for (int v = t; v < 128 * CH; v += 128) {
+        const int k = v / CH, c = v % CH;
+        const int32_t tok = t0 + k;
+        const int64_t row = tok >= lo && tok < hi ? row_of(st, table, tok) : -1;
+        const bool there = row >= 0 && 8 * c < st.head_dim;
+        cp_async16(dst + (c >> 3) * 128 * 128 + k * 128 + (((c & 7) ^ (k & 7)) << 4),
+                   plane + (there ? 2 * (row + (int64_t)h * st.head_dim + 8 * c) : 0), there);
+    }
 }
 
 template <int N>

@@ -1,97 +1,393 @@
 // kvs_weigh.cu -- accumulated attention weight of the cached tokens.
 //
-//     w_t = decay * w_t + sum over rows of e^(scale q . k_t - lse)
+//     w_t = decay * w_t + sum over rows of 2^(c q . k_t - lse'),  c = scale log2(e), lse' = lse log2(e)
 //
-// with every row's lse known, so that a key's sum needs no other key.
-#include "kvs_async.cuh"
-#include "kvs_ops.cuh"
+// With every row's lse known a key's sum needs no other key: keys go to different CTAs, warps
+// or lanes, and no sum is shared.  Rows are packed as in attention (row = token * group + head).
+#include "kvs_tcgen05.cuh"
 
 namespace kvs {
 namespace {
 
-constexpr int kThreads = 128;
-constexpr int kQRows = 16;
+constexpr float kLog2e = 1.4426950408889634f;
 
-// A thread per key, whose dims stay in registers; the rows go by in shared memory.
-template <bool HALF, int DP>
-__global__ void __launch_bounds__(kThreads) kvs_weigh_kernel(WeighJob j) {
-    using N = Num<HALF>;
-    __shared__ __align__(16) float rows_q[kQRows][DP];
-    __shared__ float rows_lse[kQRows];
-    __shared__ int32_t rows_lo[kQRows], rows_hi[kQRows];
-    const StepView& st = j.step;
-    const int32_t h = blockIdx.y, r = blockIdx.z;
-    const Request q = load_request(st, r);
-    const int32_t t = blockIdx.x * kThreads + threadIdx.x;
-    if ((int32_t)(blockIdx.x * kThreads) >= q.T) return;
-    const int32_t* table = st.tables + (int64_t)r * st.table_stride;
-    const int64_t row = t < q.T ? row_of(st, table, t) : -1;
-    uint32_t k[DP / 2];
-#pragma unroll
-    for (int c = 0; c < DP / 8; ++c) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (row >= 0 && 8 * c < st.head_dim)
-            v = __ldg(reinterpret_cast<const uint4*>(j.k_plane + 2 * (row + (int64_t)h * st.head_dim + 8 * c)));
-        k[4 * c] = v.x;
-        k[4 * c + 1] = v.y;
-        k[4 * c + 2] = v.z;
-        k[4 * c + 3] = v.w;
-    }
-    float sum = 0.0f;
-    const int32_t total = q.n * st.group;
-    for (int32_t p0 = 0; p0 < total; p0 += kQRows) {
-        __syncthreads();
-        for (int v = threadIdx.x; v < kQRows * DP; v += kThreads) {
-            const int i = v / DP, d = v % DP;
-            const int32_t p = p0 + i, tok = q.q0 + p / st.group, head = h * st.group + p % st.group;
-            float x = 0.0f;
-            if (p < total && d < st.head_dim)
-                x = N::to(reinterpret_cast<const typename N::T*>(j.q.base)[(int64_t)tok * j.q.row + (int64_t)head * j.q.head + d]);
-            rows_q[i][d] = x;
-        }
-        if (threadIdx.x < kQRows) {
-            const int32_t p = p0 + threadIdx.x;
-            Span s{0, 0};
-            float e = 0.0f;
-            if (p < total) {
-                const int32_t i = p / st.group;
-                s = seen_by(q, i, i, j.causal, j.window);
-                e = j.lse[(int64_t)(q.q0 + i) * (st.kv_heads * st.group) + h * st.group + p % st.group] * 1.4426950408889634f;
-            }
-            rows_lo[threadIdx.x] = s.lo;
-            rows_hi[threadIdx.x] = s.hi;
-            rows_lse[threadIdx.x] = e;
-        }
-        __syncthreads();
-        for (int i = 0; i < kQRows; ++i) {
-            float a = 0.0f, b = 0.0f;
-#pragma unroll
-            for (int c = 0; c < DP / 2; ++c) {
-                const float2 kv = N::to2(k[c]);
-                a = fmaf(kv.x, rows_q[i][2 * c], a);
-                b = fmaf(kv.y, rows_q[i][2 * c + 1], b);
-            }
-            if (t >= rows_lo[i] && t < rows_hi[i]) sum += exp2_fast((a + b) * j.scale_log2 - rows_lse[i]);
-        }
-    }
-    if (t < q.T) {
-        float* w = j.weights + r * j.request_stride + h * j.head_stride + t;
-        *w = j.decay == 0.0f ? sum : fmaf(j.decay, *w, sum);
-    }
+// Packed rows [first, end) that see cached token t (all of them do between); and of a whole
+// tile of keys, the rows that see any.
+struct RowSpan {
+    int64_t first, end;
+};
+__device__ __forceinline__ RowSpan rows_seeing(const StepView& st, const Request& q, int32_t t_lo, int32_t t_hi, int32_t causal, int32_t window) {
+    const int64_t base = q.T - q.n;                              // position of new token 0
+    RowSpan s{0, q.n};
+    if (causal) s.first = max((int64_t)0, t_lo - base);
+    if (window > 0) s.end = min((int64_t)q.n, t_hi + window - base);
+    s.first *= st.group;
+    s.end = max(s.first, s.end * st.group);
+    return s;
 }
 
+__device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t h, int32_t t, float sum) {
+    float* w = j.weights + r * j.request_stride + h * j.head_stride + t;
+    *w = j.decay == 0.0f ? sum : fmaf(j.decay, *w, sum);
+}
+
+// ---------------------------------------------------------------------------
+// Many rows: S^T = K Q^T on the tensor cores, a tile of 128 keys (the accumulator's lanes)
+// per CTA and the rows 128 at a time (its columns), so that a thread sums its key's weights
+// in registers.  Two warpgroups take the row tiles in turn, from two accumulators; a third
+// loads the next ones, and one thread issues the products.  Bound by the exponentials: one
+// for each score, against 128 products.
+//
+// Where there are fewer key tiles than SMs, a cluster of CTAs shares a key tile's row tiles
+// and joins its sums, in the CTAs' order, through distributed shared memory.
+// ---------------------------------------------------------------------------
+constexpr int kThreads = 416, kStages = 3;
+
+template <int DP>
+struct WPlan {
+    static constexpr int tile = 128 * DP * 2;
+    static constexpr int lse = tile * (1 + kStages);             // [stages][128] binary32, times log2(e)
+    static constexpr int sums = lse + kStages * 512;             // [2][128]
+    static constexpr int bars = sums + 1024;
+    static constexpr int bytes = bars + 256 + 1024;
+};
+
+template <bool HALF, int DP>
+__global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap k_map, int32_t boxes, int32_t share) {
+    extern __shared__ char raw[];
+    using P = WPlan<DP>;
+    const StepView& st = j.step;
+    const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
+    char* mem = raw + (base - smem_u32(raw));
+    const uint32_t ring = base + P::tile, ctl = base + P::bars;
+    const uint32_t b_k = ctl, b_full = ctl + 8, b_free = b_full + 8 * kStages, b_s = b_free + 8 * kStages, b_e = b_s + 16, b_done = b_e + 16, tmem_at = b_done + 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = threadIdx.x >> 7;
+    const int32_t r = blockIdx.z, h = blockIdx.y, rank = blockIdx.x % share, t0 = (blockIdx.x / share) * 128;
+    const Request q = load_request(st, r);
+    if (t0 >= q.T) return;                                       // the whole cluster
+    const int32_t* table = st.tables + (int64_t)r * st.table_stride;
+    const RowSpan any = rows_seeing(st, q, t0, min(t0 + 127, q.T - 1), j.causal, j.window);
+    const int32_t tile0 = (int32_t)(any.first / 128), tiles = any.end > any.first ? (int32_t)((any.end + 127) / 128) - tile0 : 0;
+    const int32_t mine = (tiles - rank + share - 1) / share;     // row tiles tile0 + rank + share * i
+    const int32_t total = q.n * st.group;
+
+    if (threadIdx.x == 0) {
+        mbar_init(b_k, 4);
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(b_full + 8 * i, 4);
+            mbar_init(b_free + 8 * i, 5);                        // the products, and the four warps that read lse
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(b_s + 8 * i, 1);
+            mbar_init(b_e + 8 * i, 4);
+        }
+        mbar_init(b_done, 1);
+        mbar_init_fence();
+    }
+    if (warp == 12) tmem_alloc(tmem_at, 256);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at) : "memory");
+    auto wait = [&](uint32_t b, uint32_t parity) {
+        if (mbar_wait(b, parity, kWaitLimitNs)) return true;
+        record_error(st.err, KVS_ERR_TIMEOUT);
+        return false;
+    };
+
+    float sum = 0.0f;
+    const int t = threadIdx.x & 127;
+    if (wg == 2) {
+        // ---- loads ----------------------------------------------------------------
+        uint32_t pending = 0;
+        auto announce = [&]() {
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(pending);
+            pending = 0;
+        };
+        if (mine > 0) {
+            if (boxes) {
+                if (warp == 8) tile_boxes<DP>(base, &k_map, st, table, h, t0, q.T, b_k, lane);
+                else if (lane == 0) mbar_arrive(b_k);
+            } else {
+                tile_rows<DP>(base, j.k_plane, st, table, h, t0, 0, q.T, t);
+                cp_commit();
+                pending = b_k;
+            }
+        }
+        for (int32_t i = 0; i < mine; ++i) {
+            const int stage = i % kStages;
+            if (i >= kStages) {
+                const bool ok = lane != 0 || wait(b_free + 8 * stage, (i / kStages - 1) & 1);
+                if (!__all_sync(0xffffffffu, ok)) break;
+            }
+            const int32_t p0 = (tile0 + rank + share * i) * 128;
+            const uint32_t dst = ring + stage * P::tile;
+            constexpr int CH = DP / 8;
+#pragma unroll 4
+            for (int v = t; v < 128 * CH; v += 128) {
+                const int k = v / CH, c = v % CH;
+                const bool there = p0 + k < total && 8 * c < st.head_dim;
+                int32_t g;
+                const int32_t tok = token_of(st, min(p0 + k, total - 1), g);
+                cp_async16(dst + (c >> 3) * 128 * 128 + k * 128 + (((c & 7) ^ (k & 7)) << 4),
+                           j.q.base + (there ? 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)(h * st.group + g) * j.q.head + 8 * c) : 0), there);
+            }
+            cp_commit();
+            float e = INFINITY;                                  // rows that there are not weigh nothing
+            if (p0 + t < total) {
+                int32_t g;
+                const int32_t tok = token_of(st, p0 + t, g);
+                e = __ldg(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + h * st.group + g) * kLog2e;
+            }
+            reinterpret_cast<float*>(mem + P::lse)[stage * 128 + t] = e;
+            if (pending) {
+                cp_wait<1>();
+                announce();
+            }
+            pending = b_full + 8 * stage;
+        }
+        cp_wait<0>();
+        if (pending) announce();
+        if (boxes && mine > 0) mbar_wait(b_k, 0, kWaitLimitNs);  // nothing is in flight when the CTA leaves
+    } else if (wg == 3) {
+        if (lane == 0 && mine > 0) {
+            // ---- the products -------------------------------------------------------
+            constexpr uint32_t id = tc_idesc(HALF, 128, false);
+            bool ok = wait(b_k, 0);
+            for (int32_t i = 0; ok && i < mine; ++i) {
+                const int stage = i % kStages, acc = i & 1;
+                ok = wait(b_full + 8 * stage, (i / kStages) & 1) && (i < 2 || wait(b_e + 8 * acc, ((i >> 1) - 1) & 1));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t qb = ring + stage * P::tile;
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k) {
+                    const uint32_t off = (k >> 2) * 128 * 128 + (k & 3) * 32;
+                    tc_mma_ss(tmem + 128 * acc, tc_desc(base + off, 16, 1024), tc_desc(qb + off, 16, 1024), id, k > 0);
+                }
+                tc_commit(b_free + 8 * stage);
+                tc_commit(b_s + 8 * acc);
+            }
+            // the last products are waited for by their readers; after a failure, here
+            if (!ok) {
+                tc_commit(b_done);
+                mbar_wait(b_done, 0, kWaitLimitNs);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---- sums: a key to a thread ---------------------------------------------------
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+        const bool live = t0 + t < q.T;
+        const RowSpan see = rows_seeing(st, q, t0 + t, t0 + t, j.causal, j.window);
+        for (int32_t i = wg; i < mine; i += 2) {
+            const int stage = i % kStages;
+            if (!__all_sync(0xffffffffu, wait(b_s + 8 * wg, (i >> 1) & 1))) break;
+            tc_fence_after();
+            const int64_t p0 = (int64_t)(tile0 + rank + share * i) * 128;
+            const int32_t a = (int32_t)max((int64_t)0, min((int64_t)128, see.first - p0));
+            const int32_t b = live ? (int32_t)max((int64_t)0, min((int64_t)128, see.end - p0)) : 0;
+            const bool edge = __any_sync(0xffffffffu, a > 0 || b < 128);
+            const float4* lse = reinterpret_cast<const float4*>(mem + P::lse) + stage * 32;
+            float x0 = 0.0f, x1 = 0.0f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t sr[32];
+                tmem_ld32(sr, tmem + 128 * wg + lanes + 32 * c);
+                tmem_wait_ld();
+                tmem_loaded32(sr);
+                float* s = reinterpret_cast<float*>(sr);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float4 z = lse[8 * c + e];
+                    s[4 * e] = exp2_fast(fmaf(s[4 * e], j.scale_log2, -z.x));
+                    s[4 * e + 1] = exp2_fast(fmaf(s[4 * e + 1], j.scale_log2, -z.y));
+                    s[4 * e + 2] = exp2_fast(fmaf(s[4 * e + 2], j.scale_log2, -z.z));
+                    s[4 * e + 3] = exp2_fast(fmaf(s[4 * e + 3], j.scale_log2, -z.w));
+                }
+                if (edge) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) s[e] = 32 * c + e >= a && 32 * c + e < b ? s[e] : 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) add2(x0, x1, s[e], s[e + 1]);
+            }
+            sum += x0 + x1;
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(b_e + 8 * wg);
+                mbar_arrive(b_free + 8 * stage);
+            }
+        }
+        reinterpret_cast<float*>(mem + P::sums)[threadIdx.x] = sum;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 12) tmem_dealloc(tmem, 256);
+    const float* sums = reinterpret_cast<const float*>(mem + P::sums);
+    if (share == 1) {
+        if (threadIdx.x < 128 && t0 + t < q.T) add_weight(j, r, h, t0 + t, sums[t] + sums[128 + t]);
+        return;
+    }
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    if (rank == 0 && threadIdx.x < 128 && t0 + t < q.T) {
+        float x = 0.0f;
+        for (int32_t k = 0; k < share; ++k) {
+            uint32_t at;
+            float u, v;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(base + P::sums + 4 * t), "r"(k));
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u) : "r"(at) : "memory");
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at + 512) : "memory");
+            x += u + v;
+        }
+        add_weight(j, r, h, t0 + t, x);
+    }
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+
+// ---------------------------------------------------------------------------
+// Few rows (a decode step): a warp takes 32 keys straight into the fragments of
+// mma.m16n8k16, and the rows 16 at a time.  The sum over a head's dims has no order, so lane 4i + c takes 16 contiguous
+// bytes of key i (dims 32 k + 8 c ...) for what the instruction calls dims 2c, 2c + 1, 2c + 8
+// and 2c + 9 of two of its steps, for keys and rows alike: no shared memory, no shuffles.
+// Bound by HBM: K is read once.
+// ---------------------------------------------------------------------------
+constexpr int kRowWarps = 8, kRowKeys = 32;
+
 template <bool HALF>
-cudaError_t weigh(const WeighJob& j, cudaStream_t s) {
-    const dim3 grid((j.step.max_kv + kThreads - 1) / kThreads, j.step.kv_heads, j.step.requests);
-    if (j.step.head_dim <= 64) kvs_weigh_kernel<HALF, 64><<<grid, kThreads, 0, s>>>(j);
-    else kvs_weigh_kernel<HALF, 128><<<grid, kThreads, 0, s>>>(j);
-    return cudaGetLastError();
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (HALF)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <bool HALF, int DP>
+__global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(WeighJob j) {
+    constexpr int K = DP / 32;                                   // 16-byte vectors of a lane and key
+    const StepView& st = j.step;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, i = lane >> 2;
+    const int32_t h = blockIdx.y, r = blockIdx.z;
+    const Request q = load_request(st, r);
+    const int32_t t0 = (blockIdx.x * kRowWarps + warp) * kRowKeys;
+    if (t0 >= q.T) return;
+    const int32_t* table = st.tables + (int64_t)r * st.table_stride;
+    // keys t0 + 8 n + i
+    uint4 kv[4][K];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int32_t t = t0 + 8 * n + i;
+        const int64_t row = t < q.T ? row_of(st, table, t) : -1;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            kv[n][k] = make_uint4(0, 0, 0, 0);
+            const int32_t d = 32 * k + 8 * c;
+            if (row >= 0 && d < st.head_dim) kv[n][k] = *reinterpret_cast<const uint4*>(j.k_plane + 2 * (row + (int64_t)h * st.head_dim + d));
+        }
+    }
+    const int32_t total = q.n * st.group;
+    float sums[8];                                               // keys 8 n + 2 c and + 1
+#pragma unroll
+    for (int n = 0; n < 8; ++n) sums[n] = 0.0f;
+    for (int32_t p0 = 0; p0 < total; p0 += 16) {
+        // rows p0 + i and p0 + i + 8
+        uint4 qv[2][K];
+        float lse[2];
+        Span see[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const int32_t p = p0 + i + 8 * m;
+            int32_t g = 0;
+            const int32_t tok = token_of(st, p, g), head = h * st.group + g;
+            see[m] = Span{0, 0};
+            lse[m] = 0.0f;
+            if (p < total) {
+                see[m] = seen_by(q, tok, tok, j.causal, j.window);
+                lse[m] = __ldg(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + head) * kLog2e;
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                qv[m][k] = make_uint4(0, 0, 0, 0);
+                const int32_t d = 32 * k + 8 * c;
+                if (p < total && d < st.head_dim)
+                    qv[m][k] = __ldg(reinterpret_cast<const uint4*>(j.q.base + 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)head * j.q.head + d)));
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                mma<HALF>(s, qv[0][k].x, qv[1][k].x, qv[0][k].y, qv[1][k].y, kv[n][k].x, kv[n][k].y);
+                mma<HALF>(s, qv[0][k].z, qv[1][k].z, qv[0][k].w, qv[1][k].w, kv[n][k].z, kv[n][k].w);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int32_t t = t0 + 8 * n + 2 * c + e;
+                float x = 0.0f;
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+                    if (t >= see[m].lo && t < see[m].hi) x += exp2_fast(fmaf(s[2 * m + e], j.scale_log2, -lse[m]));
+                sums[2 * n + e] += x;
+            }
+        }
+    }
+    // the rows' sums join over the lanes of one c; lane 4 i + c writes key 8 (i / 2) + 2 c + i % 2
+    float mine = 0.0f;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) sums[n] += __shfl_xor_sync(0xffffffffu, sums[n], d);
+        if (i == n) mine = sums[n];
+    }
+    const int32_t t = t0 + 8 * (i >> 1) + 2 * c + (i & 1);
+    if (t < q.T) add_weight(j, r, h, t, mine);
+}
+
+template <bool HALF, int DP>
+cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
+    const StepView& st = j.step;
+    const int64_t rows = (int64_t)st.max_q * st.group;
+    if (rows <= 64) {
+        const unsigned x = (unsigned)((st.max_kv + kRowWarps * kRowKeys - 1) / (kRowWarps * kRowKeys));
+        kvs_weigh_rows_kernel<HALF, DP><<<dim3(x, st.kv_heads, st.requests), kRowWarps * 32, 0, s>>>(j);
+        return cudaGetLastError();
+    }
+    auto* k = kvs_weigh_tc_kernel<HALF, DP>;
+    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, WPlan<DP>::bytes);
+    if (e != cudaSuccess) return e;
+    CUtensorMap map{};
+    const bool boxes = plane_map(&map, st, j.k_plane, HALF);
+    const int64_t x = (st.max_kv + 127) / 128, tiles = x * st.kv_heads * st.requests, row_tiles = (rows + 127) / 128;
+    int share = 1;
+    while (share < 8 && tiles * share * 2 <= sms && share * 2 <= row_tiles) share *= 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(x * share), st.kv_heads, st.requests);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = WPlan<DP>::bytes;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = share;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = share > 1;
+    return cudaLaunchKernelEx(&cfg, k, j, map, (int32_t)boxes, (int32_t)share);
 }
 
 }  // namespace
 
-int launch_weigh(const WeighJob& j, bool half, cudaStream_t s) {
-    const cudaError_t e = half ? weigh<true>(j, s) : weigh<false>(j, s);
+int launch_weigh(const WeighJob& j, bool half, int sms, cudaStream_t s) {
+    cudaError_t e;
+    if (j.step.head_dim <= 64) e = half ? weigh<true, 64>(j, sms, s) : weigh<false, 64>(j, sms, s);
+    else e = half ? weigh<true, 128>(j, sms, s) : weigh<false, 128>(j, sms, s);
     return e == cudaSuccess ? 1 : -(int)e;
 }
 

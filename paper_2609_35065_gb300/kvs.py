@@ -207,6 +207,7 @@ class kvs_evict_args(ctypes.Structure):
 _lock = threading.Lock()
 _lib = None
 _pycall = None              # the extension's call(), once the library is loaded
+_ops = None                 # the extension, which also marshals the model operators' calls
 _address: dict = {}         # addresses of the functions it may call
 
 
@@ -216,7 +217,7 @@ def lib_path() -> str:
 
 def lib():
     """Load ``libkvs.so`` (building it first if sources are newer).  Raises if impossible."""
-    global _lib, _pycall
+    global _lib, _pycall, _ops
     if _lib is not None:
         return _lib
     with _lock:
@@ -301,9 +302,11 @@ def lib():
             L.kvs_selftest_wait_timeout.argtypes = [P, ctypes.c_int64]
             L.kvs_selftest_wait_timeout.restype = ctypes.c_int
             for name in ("kvs_retrieve", "kvs_store", "kvs_retrieve_noalloc", "kvs_retrieve_fp8", "kvs_store_fp8",
-                         "kvs_retrieve_layers", "kvs_store_layers", "kvs_retrieve_fp8_layers", "kvs_store_fp8_layers"):
+                         "kvs_retrieve_layers", "kvs_store_layers", "kvs_retrieve_fp8_layers", "kvs_store_fp8_layers",
+                         "kvs_append", "kvs_attend", "kvs_weigh"):
                 _address[name] = ctypes.cast(getattr(L, name), P).value
             _pycall = _build.load_pycall()
+            _ops = getattr(_pycall, "__self__", None)
             _lib = L
     return _lib
 
@@ -630,11 +633,16 @@ class Step:
         self.step = kvs_step(_addr(block_tables), _addr(kv_lens), _addr(q_starts), R, stride, self.total_q,
                              (1 if R else 0) if max_q is None else int(max_q), self.max_kv, int(dtype))
         self.refs = ctypes.byref(self.geom), ctypes.byref(self.cache), ctypes.byref(self.step)
-
-    @property
-    def torch_dtype(self):
         import torch
-        return torch.float16 if self.step.dtype == KVS_DTYPE_F16 else torch.bfloat16
+        if dtype not in (KVS_DTYPE_BF16, KVS_DTYPE_F16):
+            raise KvsError(KVS_ERR_INVALID_ARG, f"dtype must be KVS_DTYPE_BF16 or KVS_DTYPE_F16 (got {dtype})")
+        self.torch_dtype = torch.float16 if dtype == KVS_DTYPE_F16 else torch.bfloat16
+        # what the extension takes of a step: the structs' addresses, and the tensors' types
+        self.ext = (np.array([ctypes.addressof(x) for x in (self.geom, self.cache, self.step)], dtype=np.uint64).tobytes(),
+                    self.torch_dtype, torch.float32, torch.int32)
+        self.byte = torch.uint8
+        self.scale = self.geom.head_dim ** -0.5
+        lib()
 
 
 def _int32_tensor(name, t, dims):
@@ -693,6 +701,10 @@ def kvs_append(step: Step, layer: int, q, k, v, q_out=None, rope: Rope | None = 
     in place) and keys ``k``, and append ``k`` and ``v`` [total_q, KV heads, head_dim] to the planes of
     ``layer``.  ``positions``: int32 [total_q] on the GPU (default: the tokens' places in the cache);
     ``q`` may be None."""
+    if _ops is not None:
+        rc = _ops.append(_address["kvs_append"], *step.ext, layer, stream, flags, q, k, v, q_out, rope, positions)
+        if rc is not None:
+            return _check(rc)
     a = kvs_append_args()
     if q is not None:
         a.q = _rows("q", step, q, 0)
@@ -726,6 +738,12 @@ def kvs_attend(step: Step, layer: int, q, out, lse=None, scale: float | None = N
     and values of ``layer`` into ``out`` (the same shape); ``lse`` (float32 [total_q, query heads],
     optional) receives log sum exp of the scaled scores.  ``scale`` defaults to head_dim ** -0.5;
     ``workspace``: a uint8 tensor of :func:`kvs_attend_workspace` bytes (may be None if that is 0)."""
+    if scale is None:
+        scale = step.scale
+    if _ops is not None:
+        rc = _ops.attend(_address["kvs_attend"], *step.ext, layer, stream, flags, q, out, lse, scale, causal, window, workspace, step.byte)
+        if rc is not None:
+            return _check(rc)
     a = kvs_attend_args()
     a.q = _rows("q", step, q, 0)
     a.out = _rows("out", step, out, q.shape[1])
@@ -734,8 +752,7 @@ def kvs_attend(step: Step, layer: int, q, out, lse=None, scale: float | None = N
         a.lse = _f32("lse", lse, q.shape[:2])
     if workspace is not None:
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    a.scale = step.geom.head_dim ** -0.5 if scale is None else scale
-    a.causal, a.window = bool(causal), window
+    a.scale, a.causal, a.window = scale, bool(causal), window
     g, c, s = step.refs
     return _check(lib().kvs_attend(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
 
@@ -745,6 +762,12 @@ def kvs_weigh(step: Step, layer: int, q, lse, weights, scale: float | None = Non
     """Add to ``weights`` (float32 [requests, KV heads, at least max_kv]) times ``decay`` the attention
     weight that the new tokens gave to each cached token: ``q`` and the mask as for
     :func:`kvs_attend`, ``lse`` what it returned."""
+    if scale is None:
+        scale = step.scale
+    if _ops is not None:
+        rc = _ops.weigh(_address["kvs_weigh"], *step.ext, layer, stream, flags, q, lse, weights, scale, decay, causal, window)
+        if rc is not None:
+            return _check(rc)
     a = kvs_weigh_args()
     a.q = _rows("q", step, q, 0)
     a.num_q_heads = q.shape[1]
@@ -754,8 +777,7 @@ def kvs_weigh(step: Step, layer: int, q, lse, weights, scale: float | None = Non
         raise ValueError("weights: [requests, KV heads, at least max_kv], contiguous in its last dimension")
     a.weights = _f32("weights", weights, (R, H, weights.shape[2]), contiguous=False)
     a.request_stride, a.head_stride = weights.stride(0), weights.stride(1)
-    a.scale = step.geom.head_dim ** -0.5 if scale is None else scale
-    a.decay, a.causal, a.window = decay, bool(causal), window
+    a.scale, a.decay, a.causal, a.window = scale, decay, bool(causal), window
     g, c, s = step.refs
     return _check(lib().kvs_weigh(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
 
