@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
 
     // A wait that does not end is recorded; every role then leaves its loop (the others' waits end too).
     auto wait = [&](uint32_t b, uint32_t parity) {
-        if (mbar_wait(b, parity, kWaitLimitNs)) return true;
+        if (tc_wait(b, parity)) return true;
         record_error(st.err, KVS_ERR_TIMEOUT);
         return false;
     };
@@ -147,57 +147,78 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                 mbar_wait(bar.full + 8 * (k % P::stages), (k / P::stages) & 1, kWaitLimitNs);
     } else if (wg == 3) {
         regs_dec<56>();
-        if (warp == 12 && lane == 0 && steps > 0) {
-            // ---- the products --------------------------------------------------------
+        if (warp == 12 && steps > 0) {
+            // ---- the products: the warp waits together, one lane issues ------------------
             constexpr uint32_t id_s = tc_idesc(HALF, kN, false), id_o = tc_idesc(HALF, DP, true);
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+            const uint64_t q_desc = tc_desc(base, 16, 1024), k_desc = tc_desc(ring, 16, 1024), v_desc = tc_desc(ring, kN * 128, 1024);
             auto issue_s = [&](int t, int stage) {
-                const uint32_t qa = base + t * P::tile, kb = ring + stage * P::tile;
+                const uint64_t a = tc_ahead(q_desc, t * P::tile), b = tc_ahead(k_desc, stage * P::tile);
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k) {
                     const uint32_t off = (k >> 2) * kN * 128 + (k & 3) * 32;
-                    tc_mma_ss(s_at(t), tc_desc(qa + off, 16, 1024), tc_desc(kb + off, 16, 1024), id_s, k > 0);
+                    tc_mma_ss(tm + 128 * t, tc_ahead(a, off), tc_ahead(b, off), id_s, k > 0);
                 }
                 tc_commit(bar.s + 8 * t);
             };
             auto issue_o = [&](int t, int stage, bool add) {
-                const uint32_t vb = ring + stage * P::tile;
+                const uint64_t b = tc_ahead(v_desc, stage * P::tile);
 #pragma unroll
                 for (int k = 0; k < kN / 16; ++k)
-                    tc_mma_ts(o_at(t), s_at(t) + 8 * k, tc_desc(vb + k * 2048, kN * 128, 1024), id_o, add || k > 0);
+                    tc_mma_ts(tm + 256 + DP * t, tm + 128 * t + 8 * k, tc_ahead(b, k * 2048), id_o, add || k > 0);
             };
-            auto stage_of = [&](int32_t i) { return i % P::stages; };
-            auto filled = [&](int32_t i) { return wait(bar.full + 8 * (i % P::stages), (i / P::stages) & 1); };
-            bool ok = wait(bar.q, 0) && filled(0);
+            auto filled = [&](int32_t stage, int32_t round) { return wait(bar.full + 8 * stage, round & 1); };
+            bool ok = __all_sync(0xffffffffu, wait(bar.q, 0) && filled(0, 0));
             if (ok) {
                 tc_fence_after();
-                issue_s(0, 0);
-                issue_s(1, 0);
-                tc_commit(bar.free);
+                if (elect_one()) {
+                    issue_s(0, 0);
+                    issue_s(1, 0);
+                    tc_commit(bar.free);
+                }
+                __syncwarp();
             }
+            int32_t stage = 1, round = 0;                    // of the next tile of the ring
             for (int32_t k = 0; ok && k < steps; ++k) {
                 const bool more = k + 1 < steps;
-                const int vs = stage_of(2 * k + 1), ks = stage_of(2 * k + 2);
-                ok = filled(2 * k + 1) && wait(bar.p, k & 1);
+                const int32_t vs = stage, vr = round;
+                if (++stage == P::stages) {
+                    stage = 0;
+                    ++round;
+                }
+                ok = __all_sync(0xffffffffu, filled(vs, vr) && wait(bar.p, k & 1));
                 if (!ok) break;
                 tc_fence_after();
-                issue_o(0, vs, k > 0);
+                if (elect_one()) issue_o(0, vs, k > 0);
+                __syncwarp();
+                const int32_t ks = stage;
                 if (more) {
-                    ok = filled(2 * k + 2);
+                    ok = __all_sync(0xffffffffu, filled(ks, round));
                     if (!ok) break;
-                    issue_s(0, ks);
+                    if (elect_one()) issue_s(0, ks);
+                    __syncwarp();
+                    if (++stage == P::stages) {
+                        stage = 0;
+                        ++round;
+                    }
                 }
-                ok = wait(bar.p + 8, k & 1);
+                ok = __all_sync(0xffffffffu, wait(bar.p + 8, k & 1));
                 if (!ok) break;
                 tc_fence_after();
-                issue_o(1, vs, k > 0);
-                tc_commit(bar.free + 8 * vs);
-                if (more) {
-                    issue_s(1, ks);
-                    tc_commit(bar.free + 8 * ks);
+                if (elect_one()) {
+                    issue_o(1, vs, k > 0);
+                    tc_commit(bar.free + 8 * vs);
+                    if (more) {
+                        issue_s(1, ks);
+                        tc_commit(bar.free + 8 * ks);
+                    }
                 }
+                __syncwarp();
             }
-            tc_commit(bar.o);
-            if (!ok) mbar_wait(bar.o, 0, kWaitLimitNs);
+            if (elect_one()) {
+                tc_commit(bar.o);
+                if (!ok) mbar_wait(bar.o, 0, kWaitLimitNs);
+            }
         }
         __syncwarp();
     } else {
@@ -392,6 +413,20 @@ bool plane_map(void* map, const StepView& st, const void* plane, bool half) {
     if (strides[2] >= 1ull << 40) return false;
     const cuuint32_t box[4] = {64, 1, (cuuint32_t)(B < 128 ? B : 128), 1}, one[4] = {1, 1, 1, 1};
     return encoder()((CUtensorMap*)map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(plane), dims, strides, box,
+                     one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool rows_map(void* map, const StepView& st, const RowsView& rows, bool half) {
+    if (st.group > 128 || st.head_dim < 64 || !encoder()) return false;
+    const int heads = st.kv_heads * st.group;
+    const cuuint64_t d = st.head_dim;
+    const cuuint64_t dims[3] = {d, (cuuint64_t)heads, (cuuint64_t)st.total_q};
+    // a dimension of one entry has no stride of its own
+    const cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)rows.head * 2 : d * 2, st.total_q > 1 ? (cuuint64_t)rows.row * 2 : d * 2 * heads};
+    if (!strides[0] || !strides[1] || strides[0] >= 1ull << 40 || strides[1] >= 1ull << 40) return false;
+    const cuuint32_t box[3] = {64, (cuuint32_t)st.group, (cuuint32_t)(128 / st.group)}, one[3] = {1, 1, 1};
+    return encoder()((CUtensorMap*)map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, rows.base, dims, strides, box,
                      one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

@@ -90,6 +90,9 @@ AttendPlan attend_plan(const StepView& st, int sms);
 // A plane's TMA map (a CUtensorMap at `map`) in boxes of whole blocks, or of 128 tokens of one,
 // of one head's 64 elements; false where blocks do not tile 128 tokens (kvs_attend_tc.cu).
 bool plane_map(void* map, const StepView& st, const void* plane, bool half);
+// The same of a step's rows, in boxes of one KV head's query heads by as many tokens as make
+// at most 128 packed rows.
+bool rows_map(void* map, const StepView& st, const RowsView& rows, bool half);
 cudaError_t launch_attend_tc(const AttendJob& j, bool half, cudaStream_t s);
 
 // The current device's error word and number of SMs (kvs_api.cpp); allocates them at the first call.

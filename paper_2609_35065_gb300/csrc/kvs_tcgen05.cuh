@@ -67,6 +67,29 @@ __device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t lead, uint32
 __host__ __device__ constexpr uint32_t tc_idesc(bool half, int n, bool b_mn_major) {
     return 1u << 4 | (half ? 0u : 1u) << 7 | (half ? 0u : 1u) << 10 | (b_mn_major ? 1u : 0u) << 16 | (uint32_t)(n / 8) << 17 | 8u << 24;
 }
+// The operand `bytes` further on.
+__device__ __forceinline__ uint64_t tc_ahead(uint64_t desc, uint32_t bytes) { return desc + (bytes >> 4); }
+// One lane of a converged warp, the same at every call.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+// Bounded wait like mbar_wait, for loops that wait often: the timer, which is slow to read, is
+// looked at once in 64 tries (each of which suspends the thread for a while).
+__device__ __forceinline__ bool tc_wait_long(uint32_t bar, uint32_t parity) {
+    const uint64_t t0 = global_ns();
+    do {
+        for (int i = 0; i < 64; ++i)
+            if (mbar_try_wait(bar, parity)) return true;
+    } while (global_ns() - t0 < kWaitLimitNs);
+    return false;
+}
+__device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < 8; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    return tc_wait_long(bar, parity);
+}
 // d (+)= a b over 16 elements of K, both operands in shared memory.
 __device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile(
@@ -95,6 +118,12 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
         :: "r"(dst), "l"(map), "r"(bar), "r"(d), "r"(h), "r"(t), "r"(b) : "memory");
 }
 
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int32_t d, int32_t h, int32_t n, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        :: "r"(dst), "l"(map), "r"(bar), "r"(d), "r"(h), "r"(n) : "memory");
+}
+
 // 128 cached tokens from t0 of one KV head, as a tile at dst.  By boxes: one warp, whose lane
 // 0 arrives on `bar` with the bytes; tokens beyond the cache's last block are left as they are.
 template <int DP>
@@ -116,13 +145,13 @@ __device__ __forceinline__ void tile_boxes(uint32_t dst, const CUtensorMap* map,
     }
     __syncwarp();
 }
-// By rows: 128 threads, of which this is t, with cp.async; tokens outside [lo, hi) become zeros.
-template <int DP>
+// By rows: THREADS threads, of which this is t, with cp.async; tokens outside [lo, hi) become zeros.
+template <int DP, int THREADS = 128>
 __device__ __forceinline__ void tile_rows(uint32_t dst, const char* plane, const StepView& st, const int32_t* table, int32_t h, int32_t t0, int32_t lo, int32_t hi,
                                           int t) {
     constexpr int CH = DP / 8;                                   // 16-byte vectors of a row
 #pragma unroll 4
-    for (int v = t; v < 128 * CH; v += 128) {
+    for (int v = t; v < 128 * CH; v += THREADS) {
         const int k = v / CH, c = v % CH;
         const int32_t tok = t0 + k;
         const int64_t row = tok >= lo && tok < hi ? row_of(st, table, tok) : -1;
@@ -144,6 +173,11 @@ __device__ __forceinline__ void bar_some(int id, int threads) { asm volatile("ba
 __device__ __forceinline__ void fma2(float& x, float& y, float b, float c) {
     asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %2};\n\tmov.b64 r, {%3, %3};\n\t"
         "fma.rn.f32x2 p, p, q, r;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(x), "+f"(y) : "f"(b), "f"(c));
+}
+// (x, y) * (b, b) + (c, d)
+__device__ __forceinline__ void fma2(float& x, float& y, float b, float c, float d) {
+    asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %2};\n\tmov.b64 r, {%3, %4};\n\t"
+        "fma.rn.f32x2 p, p, q, r;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(x), "+f"(y) : "f"(b), "f"(c), "f"(d));
 }
 __device__ __forceinline__ void add2(float& x, float& y, float a, float b) {
     asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\t"

@@ -33,73 +33,118 @@ __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t
 
 // ---------------------------------------------------------------------------
 // Many rows: S^T = K Q^T on the tensor cores, a tile of 128 keys (the accumulator's lanes)
-// per CTA and the rows 128 at a time (its columns), so that a thread sums its key's weights
-// in registers.  Two warpgroups take the row tiles in turn, from two accumulators; a third
-// loads the next ones, and one thread issues the products.  Bound by the exponentials: one
-// for each score, against 128 products.
+// per CTA and the rows in tiles of at most 128 (its columns), so that a thread sums its key's
+// weights in registers.  Two warpgroups take the row tiles in turn, from four accumulators; in
+// the third one warp issues the products, one loads the next row tiles (TMA boxes of whole
+// tokens; cp.async by three warps where the rows have no such boxes) and two their lse.
+// Bound by the exponentials, one for each score, and as much by the products.
 //
 // Where there are fewer key tiles than SMs, a cluster of CTAs shares a key tile's row tiles
 // and joins its sums, in the CTAs' order, through distributed shared memory.
 // ---------------------------------------------------------------------------
-constexpr int kThreads = 416, kStages = 3;
+constexpr int kThreads = 384, kStages = 5, kAccs = 4;
 
 template <int DP>
 struct WPlan {
     static constexpr int tile = 128 * DP * 2;
-    static constexpr int lse = tile * (1 + kStages);             // [stages][128] binary32, times log2(e)
+    static constexpr int lse = tile * (1 + kStages);             // [stages][128] binary32, times -log2(e)
     static constexpr int sums = lse + kStages * 512;             // [2][128]
     static constexpr int bars = sums + 1024;
     static constexpr int bytes = bars + 256 + 1024;
 };
 
 template <bool HALF, int DP>
-__global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap k_map, int32_t boxes, int32_t share) {
+__global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap k_map,
+                                                                   const __grid_constant__ CUtensorMap q_map, int32_t k_boxes, int32_t q_boxes, int32_t share) {
     extern __shared__ char raw[];
     using P = WPlan<DP>;
     const StepView& st = j.step;
     const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
     char* mem = raw + (base - smem_u32(raw));
     const uint32_t ring = base + P::tile, ctl = base + P::bars;
-    const uint32_t b_k = ctl, b_full = ctl + 8, b_free = b_full + 8 * kStages, b_s = b_free + 8 * kStages, b_e = b_s + 16, b_done = b_e + 16, tmem_at = b_done + 8;
+    const uint32_t b_k = ctl, b_full = ctl + 8, b_free = b_full + 8 * kStages, b_s = b_free + 8 * kStages, b_e = b_s + 8 * kAccs, b_done = b_e + 8 * kAccs,
+                   tmem_at = b_done + 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = threadIdx.x >> 7;
     const int32_t r = blockIdx.z, h = blockIdx.y, rank = blockIdx.x % share, t0 = (blockIdx.x / share) * 128;
     const Request q = load_request(st, r);
     if (t0 >= q.T) return;                                       // the whole cluster
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
+    const int32_t per = q_boxes ? 128 / st.group * st.group : 128;      // rows of a tile
     const RowSpan any = rows_seeing(st, q, t0, min(t0 + 127, q.T - 1), j.causal, j.window);
-    const int32_t tile0 = (int32_t)(any.first / 128), tiles = any.end > any.first ? (int32_t)((any.end + 127) / 128) - tile0 : 0;
+    const int32_t tile0 = (int32_t)(any.first / per), tiles = any.end > any.first ? (int32_t)((any.end + per - 1) / per) - tile0 : 0;
     const int32_t mine = (tiles - rank + share - 1) / share;     // row tiles tile0 + rank + share * i
     const int32_t total = q.n * st.group;
 
     if (threadIdx.x == 0) {
-        mbar_init(b_k, 4);
+        mbar_init(b_k, 3);
         for (int i = 0; i < kStages; ++i) {
-            mbar_init(b_full + 8 * i, 4);
+            mbar_init(b_full + 8 * i, 3);                        // the loading warps
             mbar_init(b_free + 8 * i, 5);                        // the products, and the four warps that read lse
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kAccs; ++i) {
             mbar_init(b_s + 8 * i, 1);
             mbar_init(b_e + 8 * i, 4);
         }
         mbar_init(b_done, 1);
         mbar_init_fence();
     }
-    if (warp == 12) tmem_alloc(tmem_at, 256);
+    if (warp == 8) tmem_alloc(tmem_at, 128 * kAccs);
+    // rows that no box fills are zeros for good, and weigh nothing
+    for (int i = threadIdx.x; i < (128 - per) * (DP / 8) * kStages; i += kThreads) {
+        const int stage = i / ((128 - per) * (DP / 8)), v = i % ((128 - per) * (DP / 8)), row = per + v / (DP / 8), c = v % (DP / 8);
+        *reinterpret_cast<uint4*>(mem + P::tile * (1 + stage) + (c >> 3) * 128 * 128 + row * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+    }
+    fence_async_smem();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at) : "memory");
     auto wait = [&](uint32_t b, uint32_t parity) {
-        if (mbar_wait(b, parity, kWaitLimitNs)) return true;
+        if (tc_wait(b, parity)) return true;
         record_error(st.err, KVS_ERR_TIMEOUT);
         return false;
     };
 
     float sum = 0.0f;
     const int t = threadIdx.x & 127;
-    if (wg == 2) {
-        // ---- loads ----------------------------------------------------------------
+    if (warp == 8) {
+        // ---- the products: the warp waits together, one lane issues ----------------------
+        constexpr uint32_t id = tc_idesc(HALF, 128, false);
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint64_t k_desc = tc_desc(base, 16, 1024), q_desc = tc_desc(ring, 16, 1024);
+        bool ok = mine <= 0 || __all_sync(0xffffffffu, wait(b_k, 0));
+        int32_t stage = 0, round = 0;
+        for (int32_t i = 0; ok && i < mine; ++i) {
+            const int32_t acc = i % kAccs;
+            ok = __all_sync(0xffffffffu, wait(b_full + 8 * stage, round & 1) && (i < kAccs || wait(b_e + 8 * acc, (i / kAccs - 1) & 1)));
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t b = tc_ahead(q_desc, stage * P::tile);
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k) {
+                    const uint32_t off = (k >> 2) * 128 * 128 + (k & 3) * 32;
+                    tc_mma_ss(tm + 128 * acc, tc_ahead(k_desc, off), tc_ahead(b, off), id, k > 0);
+                }
+                tc_commit(b_free + 8 * stage);
+                tc_commit(b_s + 8 * acc);
+            }
+            __syncwarp();
+            if (++stage == kStages) {
+                stage = 0;
+                ++round;
+            }
+        }
+        // the last products are waited for by their readers; after a failure, here
+        if (!ok && elect_one()) {
+            tc_commit(b_done);
+            mbar_wait(b_done, 0, kWaitLimitNs);
+        }
+        __syncwarp();
+    } else if (wg == 2) {
+        // ---- loads: warp 9 the rows, warps 10 and 11 their lse; by rows all three both ------
+        const int u = threadIdx.x - 9 * 32;                      // 0 to 95
         uint32_t pending = 0;
         auto announce = [&]() {
             fence_async_smem();
@@ -108,127 +153,142 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
             pending = 0;
         };
         if (mine > 0) {
-            if (boxes) {
-                if (warp == 8) tile_boxes<DP>(base, &k_map, st, table, h, t0, q.T, b_k, lane);
+            if (k_boxes) {
+                if (warp == 9) tile_boxes<DP>(base, &k_map, st, table, h, t0, q.T, b_k, lane);
                 else if (lane == 0) mbar_arrive(b_k);
             } else {
-                tile_rows<DP>(base, j.k_plane, st, table, h, t0, 0, q.T, t);
+                tile_rows<DP, 96>(base, j.k_plane, st, table, h, t0, 0, q.T, u);
                 cp_commit();
                 pending = b_k;
             }
         }
-        for (int32_t i = 0; i < mine; ++i) {
-            const int stage = i % kStages;
-            if (i >= kStages) {
-                const bool ok = lane != 0 || wait(b_free + 8 * stage, (i / kStages - 1) & 1);
+        // lse of the rows u and u + 96 (by boxes: of u - 32 and u + 32, by two warps) of tile i
+        const int a0 = q_boxes ? u - 32 : u, a1 = q_boxes ? u + 32 : u + 96;
+        auto lse_of = [&](int32_t i, int row) {
+            const int64_t p = (int64_t)(tile0 + rank + share * i) * per + row;
+            if (i >= mine || row < 0 || row >= per || p >= total) return -INFINITY;       // weighs nothing
+            int32_t g;
+            const int32_t tok = token_of(st, (int32_t)p, g);
+            return -kLog2e * __ldg(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + h * st.group + g);
+        };
+        float e0 = lse_of(0, a0), e1 = lse_of(0, a1);
+        int32_t stage = 0, round = 0, i = 0;
+        for (; i < mine; ++i) {
+            if (round > 0) {
+                const bool ok = lane != 0 || wait(b_free + 8 * stage, (round - 1) & 1);
                 if (!__all_sync(0xffffffffu, ok)) break;
             }
-            const int32_t p0 = (tile0 + rank + share * i) * 128;
+            const int32_t p0 = (tile0 + rank + share * i) * per;
             const uint32_t dst = ring + stage * P::tile;
-            constexpr int CH = DP / 8;
+            float* lse = reinterpret_cast<float*>(mem + P::lse) + stage * 128;
+            if (!q_boxes || warp > 9) {
+                if (a0 < 128) lse[a0] = e0;
+                if (a1 < 128) lse[a1] = e1;
+                e0 = lse_of(i + 1, a0);
+                e1 = lse_of(i + 1, a1);
+            }
+            if (q_boxes) {
+                if (pending) {
+                    cp_wait<0>();
+                    announce();
+                }
+                if (warp == 9) {
+                    if (lane == 0) {
+                        mbar_expect_tx(b_full + 8 * stage, (uint32_t)per * DP * 2);
+#pragma unroll
+                        for (int c = 0; c < DP / 64; ++c)
+                            tma_load_3d(dst + c * 128 * 128, &q_map, 64 * c, h * st.group, q.q0 + p0 / st.group, b_full + 8 * stage);
+                    }
+                    __syncwarp();
+                } else {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(b_full + 8 * stage);
+                }
+            } else {
+                constexpr int CH = DP / 8;
 #pragma unroll 4
-            for (int v = t; v < 128 * CH; v += 128) {
-                const int k = v / CH, c = v % CH;
-                const bool there = p0 + k < total && 8 * c < st.head_dim;
-                int32_t g;
-                const int32_t tok = token_of(st, min(p0 + k, total - 1), g);
-                cp_async16(dst + (c >> 3) * 128 * 128 + k * 128 + (((c & 7) ^ (k & 7)) << 4),
-                           j.q.base + (there ? 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)(h * st.group + g) * j.q.head + 8 * c) : 0), there);
+                for (int v = u; v < 128 * CH; v += 96) {
+                    const int k = v / CH, c = v % CH;
+                    const bool there = p0 + k < total && 8 * c < st.head_dim;
+                    int32_t g;
+                    const int32_t tok = token_of(st, min(p0 + k, total - 1), g);
+                    cp_async16(dst + (c >> 3) * 128 * 128 + k * 128 + (((c & 7) ^ (k & 7)) << 4),
+                               j.q.base + (there ? 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)(h * st.group + g) * j.q.head + 8 * c) : 0), there);
+                }
+                cp_commit();
+                if (pending) {
+                    cp_wait<1>();
+                    announce();
+                }
+                pending = b_full + 8 * stage;
             }
-            cp_commit();
-            float e = INFINITY;                                  // rows that there are not weigh nothing
-            if (p0 + t < total) {
-                int32_t g;
-                const int32_t tok = token_of(st, p0 + t, g);
-                e = __ldg(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + h * st.group + g) * kLog2e;
+            if (++stage == kStages) {
+                stage = 0;
+                ++round;
             }
-            reinterpret_cast<float*>(mem + P::lse)[stage * 128 + t] = e;
-            if (pending) {
-                cp_wait<1>();
-                announce();
-            }
-            pending = b_full + 8 * stage;
         }
         cp_wait<0>();
         if (pending) announce();
-        if (boxes && mine > 0) mbar_wait(b_k, 0, kWaitLimitNs);  // nothing is in flight when the CTA leaves
-    } else if (wg == 3) {
-        if (lane == 0 && mine > 0) {
-            // ---- the products -------------------------------------------------------
-            constexpr uint32_t id = tc_idesc(HALF, 128, false);
-            bool ok = wait(b_k, 0);
-            for (int32_t i = 0; ok && i < mine; ++i) {
-                const int stage = i % kStages, acc = i & 1;
-                ok = wait(b_full + 8 * stage, (i / kStages) & 1) && (i < 2 || wait(b_e + 8 * acc, ((i >> 1) - 1) & 1));
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t qb = ring + stage * P::tile;
-#pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const uint32_t off = (k >> 2) * 128 * 128 + (k & 3) * 32;
-                    tc_mma_ss(tmem + 128 * acc, tc_desc(base + off, 16, 1024), tc_desc(qb + off, 16, 1024), id, k > 0);
-                }
-                tc_commit(b_free + 8 * stage);
-                tc_commit(b_s + 8 * acc);
-            }
-            // the last products are waited for by their readers; after a failure, here
-            if (!ok) {
-                tc_commit(b_done);
-                mbar_wait(b_done, 0, kWaitLimitNs);
-            }
-        }
-        __syncwarp();
+        // every load has landed when its sums are done; after a failure, wait for them here
+        if (warp == 9 && mine > 0) mbar_wait(b_k, 0, kWaitLimitNs);
+        if (i < mine)
+            for (int k = i < kStages ? 0 : i - kStages; k < i; ++k) mbar_wait(b_full + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs);
     } else {
         // ---- sums: a key to a thread ---------------------------------------------------
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
         const bool live = t0 + t < q.T;
         const RowSpan see = rows_seeing(st, q, t0 + t, t0 + t, j.causal, j.window);
+        const float c = j.scale_log2;
         for (int32_t i = wg; i < mine; i += 2) {
-            const int stage = i % kStages;
-            if (!__all_sync(0xffffffffu, wait(b_s + 8 * wg, (i >> 1) & 1))) break;
+            const int stage = i % kStages, acc = i % kAccs;
+            if (!__all_sync(0xffffffffu, wait(b_full + 8 * stage, (i / kStages) & 1) && wait(b_s + 8 * acc, (i / kAccs) & 1))) break;
             tc_fence_after();
-            const int64_t p0 = (int64_t)(tile0 + rank + share * i) * 128;
+            const int64_t p0 = (int64_t)(tile0 + rank + share * i) * per;
             const int32_t a = (int32_t)max((int64_t)0, min((int64_t)128, see.first - p0));
             const int32_t b = live ? (int32_t)max((int64_t)0, min((int64_t)128, see.end - p0)) : 0;
-            const bool edge = __any_sync(0xffffffffu, a > 0 || b < 128);
+            const bool edge = __any_sync(0xffffffffu, a > 0 || b < per);
             const float4* lse = reinterpret_cast<const float4*>(mem + P::lse) + stage * 32;
             float x0 = 0.0f, x1 = 0.0f;
+            uint32_t sr[2][32];
+            tmem_ld32(sr[0], tmem + 128 * acc + lanes);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t sr[32];
-                tmem_ld32(sr, tmem + 128 * wg + lanes + 32 * c);
+            for (int k = 0; k < 4; ++k) {
                 tmem_wait_ld();
-                tmem_loaded32(sr);
-                float* s = reinterpret_cast<float*>(sr);
+                tmem_loaded32(sr[k & 1]);
+                if (k < 3) {
+                    tmem_ld32(sr[(k + 1) & 1], tmem + 128 * acc + lanes + 32 * (k + 1));
+                } else {
+                    // the accumulator is read
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(b_e + 8 * acc);
+                }
+                float* s = reinterpret_cast<float*>(sr[k & 1]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float4 z = lse[8 * c + e];
-                    s[4 * e] = exp2_fast(fmaf(s[4 * e], j.scale_log2, -z.x));
-                    s[4 * e + 1] = exp2_fast(fmaf(s[4 * e + 1], j.scale_log2, -z.y));
-                    s[4 * e + 2] = exp2_fast(fmaf(s[4 * e + 2], j.scale_log2, -z.z));
-                    s[4 * e + 3] = exp2_fast(fmaf(s[4 * e + 3], j.scale_log2, -z.w));
+                    const float4 z = lse[8 * k + e];
+                    fma2(s[4 * e], s[4 * e + 1], c, z.x, z.y);
+                    fma2(s[4 * e + 2], s[4 * e + 3], c, z.z, z.w);
                 }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) s[e] = exp2_fast(s[e]);
                 if (edge) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) s[e] = 32 * c + e >= a && 32 * c + e < b ? s[e] : 0.0f;
+                    for (int e = 0; e < 32; ++e) s[e] = 32 * k + e >= a && 32 * k + e < b ? s[e] : 0.0f;
                 }
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) add2(x0, x1, s[e], s[e + 1]);
             }
             sum += x0 + x1;
-            tc_fence_before();
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(b_e + 8 * wg);
-                mbar_arrive(b_free + 8 * stage);
-            }
+            if (lane == 0) mbar_arrive(b_free + 8 * stage);      // lse of this stage is read
         }
         reinterpret_cast<float*>(mem + P::sums)[threadIdx.x] = sum;
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 12) tmem_dealloc(tmem, 256);
+    if (warp == 8) tmem_dealloc(tmem, 128 * kAccs);
     const float* sums = reinterpret_cast<const float*>(mem + P::sums);
     if (share == 1) {
         if (threadIdx.x < 128 && t0 + t < q.T) add_weight(j, r, h, t0 + t, sums[t] + sums[128 + t]);
@@ -363,8 +423,8 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     auto* k = kvs_weigh_tc_kernel<HALF, DP>;
     cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, WPlan<DP>::bytes);
     if (e != cudaSuccess) return e;
-    CUtensorMap map{};
-    const bool boxes = plane_map(&map, st, j.k_plane, HALF);
+    CUtensorMap km{}, qm{};
+    const bool k_boxes = plane_map(&km, st, j.k_plane, HALF), q_boxes = rows_map(&qm, st, j.q, HALF);
     const int64_t x = (st.max_kv + 127) / 128, tiles = x * st.kv_heads * st.requests, row_tiles = (rows + 127) / 128;
     int share = 1;
     while (share < 8 && tiles * share * 2 <= sms && share * 2 <= row_tiles) share *= 2;
@@ -379,7 +439,7 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = share > 1;
-    return cudaLaunchKernelEx(&cfg, k, j, map, (int32_t)boxes, (int32_t)share);
+    return cudaLaunchKernelEx(&cfg, k, j, km, qm, (int32_t)k_boxes, (int32_t)q_boxes, (int32_t)share);
 }
 
 }  // namespace
