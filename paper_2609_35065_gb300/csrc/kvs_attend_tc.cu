@@ -108,8 +108,15 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
             pending = -1;
         };
         int32_t i = 0;
+        // K's and V's tiles of a step are in the same blocks; the next step's are looked up a step ahead
+        Box box{}, next{};
+        if (boxes && steps > 0) next = box_of<DP, 4>(st, table, j0 * kN, q.T, warp & 3, lane);
         for (; i < 2 * steps; ++i) {
             const int stage = i % P::stages;
+            if (boxes && !(i & 1)) {
+                box = next;
+                if (i + 2 < 2 * steps) next = box_of<DP, 4>(st, table, (j0 + (i >> 1) + 1) * kN, q.T, warp & 3, lane);
+            }
             if (i >= P::stages) {
                 const bool ok = lane != 0 || wait(bar.free + 8 * stage, (i / P::stages - 1) & 1);
                 if (!__all_sync(0xffffffffu, ok)) break;
@@ -124,11 +131,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                     cp_wait<0>();
                     announce();
                 }
-                if (t >= 32) {
-                    if (lane == 0) mbar_arrive(bar.full + 8 * stage);
-                } else {
-                    tile_boxes<DP>(dst, is_v ? &v_map : &k_map, st, table, h, t0, q.T, bar.full + 8 * stage, lane);
-                }
+                tile_boxes<DP>(dst, is_v ? &v_map : &k_map, st, h, box, bar.full + 8 * stage, lane);
             } else {
                 tile_rows<DP>(dst, is_v ? j.v_plane : j.k_plane, st, table, h, t0, all.lo, q.T, t);
                 cp_commit();

@@ -124,24 +124,39 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
         :: "r"(dst), "l"(map), "r"(bar), "r"(d), "r"(h), "r"(n) : "memory");
 }
 
-// 128 cached tokens from t0 of one KV head, as a tile at dst.  By boxes: one warp, whose lane
-// 0 arrives on `bar` with the bytes; tokens beyond the cache's last block are left as they are.
-template <int DP>
-__device__ __forceinline__ void tile_boxes(uint32_t dst, const CUtensorMap* map, const StepView& st, const int32_t* table, int32_t h, int32_t t0, int32_t T,
-                                           uint32_t bar, int lane) {
-    const int32_t box = min(st.block_size, 128), count = (min(128, T - t0) + box - 1) / box;
-    if (lane == 0) mbar_expect_tx(bar, (uint32_t)count * box * DP * 2);
-    __syncwarp();
-    if (lane < count) {
-        const uint32_t tok = t0 + lane * box, blk = block_of(st, tok);
-        int32_t b = __ldg(table + blk);
-        if ((uint32_t)b >= (uint32_t)st.num_blocks) {
+// 128 cached tokens from t0 of one KV head, as a tile at dst; tokens beyond the cache's last
+// block are left as they are.  By boxes: WARPS warps, of which this is w, take a share of them
+// each -- issuing one takes a warp about 120 cycles -- and arrive on `bar` with its bytes.  A
+// lane's box is known ahead of the tile (box_of), so that its table entry is there when it is.
+struct Box {
+    int32_t block, row, at;                                      // block (num_blocks: reads as zeros), first token in it, token of the tile
+};
+template <int DP, int WARPS>
+__device__ __forceinline__ Box box_of(const StepView& st, const int32_t* table, int32_t t0, int32_t T, int w, int lane) {
+    constexpr int HALVES = DP / 64;
+    const int32_t size = min(st.block_size, 128), i = (lane / HALVES) * WARPS + w;      // this lane's box of the tile
+    Box x{-1, 0, i * size};
+    const int32_t tok = t0 + x.at;
+    if (x.at < 128 && tok < T) {
+        const uint32_t blk = block_of(st, tok);
+        x.block = __ldg(table + blk);
+        x.row = tok - blk * st.block_size;
+        if ((uint32_t)x.block >= (uint32_t)st.num_blocks) {
             record_error(st.err, KVS_ERR_BOUNDS);
-            b = st.num_blocks;                                   // reads as zeros
+            x.block = st.num_blocks;
         }
-#pragma unroll
-        for (int c = 0; c < DP / 64; ++c)
-            tma_load_4d(dst + c * 128 * 128 + lane * box * 128, map, 64 * c, h, tok - blk * st.block_size, b, bar);
+    }
+    return x;
+}
+template <int DP>
+__device__ __forceinline__ void tile_boxes(uint32_t dst, const CUtensorMap* map, const StepView& st, int32_t h, const Box& x, uint32_t bar, int lane) {
+    constexpr int HALVES = DP / 64;
+    const int count = __popc(__ballot_sync(0xffffffffu, x.block >= 0));
+    if (lane == 0) mbar_expect_tx(bar, (uint32_t)count * min(st.block_size, 128) * 128);
+    __syncwarp();
+    if (x.block >= 0) {
+        const int c = lane % HALVES;
+        tma_load_4d(dst + c * 128 * 128 + x.at * 128, map, 64 * c, h, x.row, x.block, bar);
     }
     __syncwarp();
 }

@@ -154,8 +154,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         };
         if (mine > 0) {
             if (k_boxes) {
-                if (warp == 9) tile_boxes<DP>(base, &k_map, st, table, h, t0, q.T, b_k, lane);
-                else if (lane == 0) mbar_arrive(b_k);
+                tile_boxes<DP>(base, &k_map, st, h, box_of<DP, 3>(st, table, t0, q.T, warp - 9, lane), b_k, lane);
             } else {
                 tile_rows<DP, 96>(base, j.k_plane, st, table, h, t0, 0, q.T, u);
                 cp_commit();
@@ -230,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         cp_wait<0>();
         if (pending) announce();
         // every load has landed when its sums are done; after a failure, wait for them here
-        if (warp == 9 && mine > 0) mbar_wait(b_k, 0, kWaitLimitNs);
+        if (mine > 0) mbar_wait(b_k, 0, kWaitLimitNs);
         if (i < mine)
             for (int k = i < kStages ? 0 : i - kStages; k < i; ++k) mbar_wait(b_full + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs);
     } else {
