@@ -326,9 +326,9 @@ AttendPlan attend_plan(const StepView& st, int sms) {
     const int64_t rows = (int64_t)st.max_q * st.group, units = (int64_t)st.kv_heads * st.requests;
     AttendPlan p{rows > 32, 1};
     if (p.tc) {
-        // One CTA of 256 rows to an SM: as many parts as keep the number of waves times a
+        // One CTA of two row tiles to an SM: as many parts as keep the number of waves times a
         // part's steps (of 128 keys, and about four of start and end) lowest.
-        const int64_t tiles = (rows + 255) / 256 * units, steps = (st.max_kv + 127) / 128;
+        const int64_t pair = 2 * tile_rows_of(st.group), tiles = (rows + pair - 1) / pair * units, steps = (st.max_kv + 127) / 128;
         int64_t best = -1;
         for (int64_t n = 1; n <= 64 && n <= (steps + 1) / 2; ++n) {
             const int64_t cost = (tiles * n + sms - 1) / sms * ((steps + n - 1) / n + 4);

@@ -1,20 +1,23 @@
 // kvs_attend_tc.cu -- attention of many packed rows: the products on the tensor cores.
 //
-// A CTA holds 256 packed rows (row = token * group + head) of one KV head as two tiles of 128
-// and goes over the keys 128 at a time:
+// A CTA holds up to 256 packed rows (row = token * group + head) of one KV head as two tiles of
+// whole tokens and goes over the keys 128 at a time:
 //
 //     S = Q K^T  (tensor memory)  ->  P = 2^(c S - c m)  (registers, back over S)  ->  O += P V
 //
-// While one tile's softmax runs on its warpgroup, the tensor cores work on the other's.
-// Warpgroups 0 and 1: a tile's softmax each, a row to a thread, so that maxima and sums need
-// no exchange.  Warpgroup 2 loads K and V through a ring of 32 KiB tiles: TMA boxes of whole
+// While one tile's softmax runs, the tensor cores work on the other's.  Two warpgroups do a
+// tile's softmax, half of a row's 64 + 64 keys to a thread: a step's softmax has to be done
+// within the other tile's two products, which one warp to a scheduler cannot do.  Of the fifth
+// warpgroup three warps load K and V through a ring of 32 KiB tiles -- TMA boxes of whole
 // blocks where the block size allows, cp.async row by row otherwise and for the tiles that
-// hold the ends of what may be read (there, rows outside become zeros).  One thread of
-// warpgroup 3 issues the products.
+// hold the ends of what may be read (there, rows outside become zeros) -- and one issues the
+// products.
 //
-// The running maximum m that O and the sums refer to is raised only when a row's maximum
-// outgrows it by 2^8: until then P is up to 2^8 instead of 1, which costs binary32 sums and
-// 16-bit floating P nothing, and O need not be rescaled, which most tiles then never do.
+// The running maximum m that O and the sums refer to is raised only when a score outgrows it
+// by 2^8: until then P is up to 2^8 instead of 1, which costs binary32 sums and 16-bit
+// floating P nothing, and O need not be rescaled, which most steps then never do.  So a step
+// takes its exponentials against the m at hand, and its maximum beside them, where it costs
+// nothing; the rare step whose maximum is too large is done again with m raised.
 //
 // Products run in the order in which one thread issues them, which the reuse of S's columns
 // for P relies on: S of the next tile is issued behind the product that reads P.
@@ -24,7 +27,7 @@ namespace kvs {
 namespace {
 
 constexpr int kM = 128, kN = 128;                  // rows of a tile, keys of a step
-constexpr int kThreads = 512;
+constexpr int kThreads = 640, kLoaders = 3;
 constexpr float kNone = -INFINITY;
 constexpr float kRaise = 8.0f;                     // log2 by which P may exceed 1
 
@@ -33,7 +36,8 @@ struct Plan {
     static constexpr int tile = kN * DP * 2;       // bytes of a tile of Q, K or V
     static constexpr int stages = DP == 128 ? 5 : 8;
     static constexpr int bars = 2 * kM * DP * 2 + stages * tile;
-    static constexpr int bytes = bars + 256 + 1024;
+    static constexpr int tops = bars + 256;        // [256] binary32: maxima, sums that a row's threads exchange
+    static constexpr int bytes = tops + 2048;
 };
 
 struct Bars {
@@ -43,12 +47,17 @@ struct Bars {
 
 template <bool HALF, int DP>
 __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j, const __grid_constant__ CUtensorMap k_map,
-                                                                    const __grid_constant__ CUtensorMap v_map, int32_t boxes) {
-    extern __shared__ char raw[];
+                                                                    const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap q_map,
+                                                                    int32_t boxes, int32_t q_boxes) {
+    extern __shared__ __align__(1024) char raw[];
     using N = Num<HALF>;
     using P = Plan<DP>;
     const StepView& st = j.step;
-    const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
+    const uint32_t base = smem_u32(raw);
+    if (base & 1023) {                               // the swizzle needs it; there is no room to round it up
+        record_error(st.err, KVS_ERR_UNSUPPORTED);
+        return;
+    }
     const uint32_t ring = base + 2 * P::tile, ctl = base + P::bars;
     const Bars bar(ctl, P::stages);
     const uint32_t tmem_at = bar.o + 8;
@@ -56,10 +65,11 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
 
     const int32_t tiles = gridDim.x / j.splits, split = blockIdx.x % j.splits;
     const int32_t r = blockIdx.z, h = blockIdx.y;
+    const int32_t per = tile_rows_of(st.group);
     // The last rows see the most keys: they come first, so that no long CTA starts last.
-    const int32_t row0 = (tiles - 1 - (int32_t)(blockIdx.x / j.splits)) * 2 * kM;
+    const int32_t row0 = (tiles - 1 - (int32_t)(blockIdx.x / j.splits)) * 2 * per;
     const Request q = load_request(st, r);
-    const int32_t rows = min(2 * kM, q.n * st.group - row0);
+    const int32_t rows = min(2 * per, q.n * st.group - row0);
     if (rows <= 0) return;
     Span all = seen_by(q, row0 / st.group, (row0 + rows - 1) / st.group, j.causal, j.window);
     const int32_t first = all.lo / kN, steps_all = all.hi > all.lo ? (all.hi + kN - 1) / kN - first : 0;
@@ -68,19 +78,19 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
 
     if (threadIdx.x == 0) {
-        mbar_init(bar.q, 256);
+        mbar_init(bar.q, q_boxes ? 1 : 512);
         for (int i = 0; i < P::stages; ++i) {
-            mbar_init(bar.full + 8 * i, 4);                   // a loading warp each
+            mbar_init(bar.full + 8 * i, kLoaders);
             mbar_init(bar.free + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar.s + 8 * i, 1);
-            mbar_init(bar.p + 8 * i, 4);
+            mbar_init(bar.p + 8 * i, 8);
         }
         mbar_init(bar.o, 1);
         mbar_init_fence();
     }
-    if (warp == 12) tmem_alloc(tmem_at, 512);
+    if (warp == 16) tmem_alloc(tmem_at, 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -96,10 +106,9 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
         return false;
     };
 
-    if (wg == 2) {
+    if (warp > 16) {
         // ---- K and V: tile i is K (even) or V (odd) of step i / 2 ------------------
-        regs_dec<56>();
-        const int t = threadIdx.x - 256;
+        const int t = threadIdx.x - 17 * 32, w = warp - 17;
         int pending = -1;                                    // cp.async tile not yet announced
         auto announce = [&]() {
             fence_async_smem();
@@ -110,12 +119,12 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
         int32_t i = 0;
         // K's and V's tiles of a step are in the same blocks; the next step's are looked up a step ahead
         Box box{}, next{};
-        if (boxes && steps > 0) next = box_of<DP, 4>(st, table, j0 * kN, q.T, warp & 3, lane);
+        if (boxes && steps > 0) next = box_of<DP, kLoaders>(st, table, j0 * kN, q.T, w, lane);
         for (; i < 2 * steps; ++i) {
             const int stage = i % P::stages;
             if (boxes && !(i & 1)) {
                 box = next;
-                if (i + 2 < 2 * steps) next = box_of<DP, 4>(st, table, (j0 + (i >> 1) + 1) * kN, q.T, warp & 3, lane);
+                if (i + 2 < 2 * steps) next = box_of<DP, kLoaders>(st, table, (j0 + (i >> 1) + 1) * kN, q.T, w, lane);
             }
             if (i >= P::stages) {
                 const bool ok = lane != 0 || wait(bar.free + 8 * stage, (i / P::stages - 1) & 1);
@@ -133,7 +142,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                 }
                 tile_boxes<DP>(dst, is_v ? &v_map : &k_map, st, h, box, bar.full + 8 * stage, lane);
             } else {
-                tile_rows<DP>(dst, is_v ? j.v_plane : j.k_plane, st, table, h, t0, all.lo, q.T, t);
+                tile_rows<DP, 32 * kLoaders>(dst, is_v ? j.v_plane : j.k_plane, st, table, h, t0, all.lo, q.T, t);
                 cp_commit();
                 if (pending >= 0) {
                     cp_wait<1>();
@@ -148,11 +157,21 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
         if (i < 2 * steps)
             for (int k = i - P::stages < 0 ? 0 : i - P::stages; k < i; ++k)
                 mbar_wait(bar.full + 8 * (k % P::stages), (k / P::stages) & 1, kWaitLimitNs);
-    } else if (wg == 3) {
-        regs_dec<56>();
-        if (warp == 12 && steps > 0) {
+    } else if (warp == 16) {
+        if (steps > 0) {
             // ---- the products: the warp waits together, one lane issues ------------------
-            constexpr uint32_t id_s = tc_idesc(HALF, kN, false), id_o = tc_idesc(HALF, DP, true);
+            // a negative scale's sign goes into the products, so that maxima of S are those of the scores
+            const uint32_t id_s = tc_idesc(HALF, kN, false) | (j.scale_log2 < 0.0f ? kNegA : 0u);
+            constexpr uint32_t id_o = tc_idesc(HALF, DP, true);
+            if (q_boxes && elect_one()) {
+                mbar_expect_tx(bar.q, (uint32_t)per * DP * 4);
+#pragma unroll
+                for (int k = 0; k < 2 * (DP / 64); ++k) {
+                    const int t = k / (DP / 64), c = k % (DP / 64);
+                    tma_load_3d(base + t * P::tile + c * kM * 128, &q_map, 64 * c, h * st.group, q.q0 + (row0 + t * per) / st.group, bar.q);
+                }
+            }
+            __syncwarp();
             const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
             const uint64_t q_desc = tc_desc(base, 16, 1024), k_desc = tc_desc(ring, 16, 1024), v_desc = tc_desc(ring, kN * 128, 1024);
             auto issue_s = [&](int t, int stage) {
@@ -220,173 +239,207 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
             }
             if (elect_one()) {
                 tc_commit(bar.o);
-                if (!ok) mbar_wait(bar.o, 0, kWaitLimitNs);
+                if (!ok) {
+                    mbar_wait(bar.q, 0, kWaitLimitNs);
+                    mbar_wait(bar.o, 0, kWaitLimitNs);
+                }
             }
         }
         __syncwarp();
     } else {
-        // ---- softmax: tile wg, one row to a thread -----------------------------------
-        regs_inc<200>();
-        const int t = threadIdx.x & 127;
-        const uint32_t qdst = base + wg * P::tile;
-        {
-            // Q: 16-byte vectors; a negative scale's sign goes into Q, so that maxima of S are those of the scores
+        // ---- softmax of tile tl: row t, keys 64 half ... of a step -----------------------
+        const int tl = wg >> 1, half = wg & 1, t = threadIdx.x & 127;
+        const uint32_t own = base + tl * P::tile;                    // the tile's Q, and at the end its results
+        if (!q_boxes && steps > 0) {
             constexpr int CH = DP / 8;
-            const uint32_t flip = j.scale_log2 < 0.0f ? 0x80008000u : 0u;
 #pragma unroll 4
-            for (int v = t; v < kM * CH; v += 128) {
-                const int i = v / CH, c = v % CH, p = row0 + wg * kM + i;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (wg * kM + i < rows && 8 * c < st.head_dim) {
-                    int32_t g;
-                    const int32_t tok = token_of(st, p, g), head = h * st.group + g;
-                    x = __ldg(reinterpret_cast<const uint4*>(j.q.base + 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)head * j.q.head + 8 * c)));
-                    x.x ^= flip;
-                    x.y ^= flip;
-                    x.z ^= flip;
-                    x.w ^= flip;
-                }
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                             :: "r"(qdst + (c >> 3) * kM * 128 + i * 128 + (((c & 7) ^ (i & 7)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+            for (int v = threadIdx.x & 255; v < kM * CH; v += 256) {
+                const int i = v / CH, c = v % CH;
+                const bool there = i < per && tl * per + i < rows && 8 * c < st.head_dim;
+                int32_t g;
+                const int32_t tok = token_of(st, there ? row0 + tl * per + i : 0, g);
+                cp_async16(own + (c >> 3) * kM * 128 + i * 128 + (((c & 7) ^ (i & 7)) << 4),
+                           j.q.base + (there ? 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)(h * st.group + g) * j.q.head + 8 * c) : 0), there);
             }
+            cp_commit();
+            cp_wait<0>();
             fence_async_smem();
             mbar_arrive(bar.q);
         }
+        // The warps of a row's two halves agree, and wait for one another, under a barrier of their
+        // own.  After a wait that ran out, both still go through all steps (on whatever is there).
+        const int pair = 1 + tl * 4 + (warp & 3);
+        float* tops = reinterpret_cast<float*>(raw + P::tops);
         const float c = fmaxf(fabsf(j.scale_log2), 1e-36f);         // a zero scale keeps -infinity * c what it is
         int32_t g;
-        const int32_t tok = token_of(st, row0 + wg * kM + t, g), head = h * st.group + g;
-        const bool live = wg * kM + t < rows;
+        const int32_t tok = token_of(st, row0 + tl * per + t, g);
+        const bool live = t < per && tl * per + t < rows;
         Span see{0, 0};
         if (live) see = seen_by(q, tok, tok, j.causal, j.window);
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // lane 32 (warp % 4) of tensor memory
+        const uint32_t s_own = s_at(tl) + lanes + 64 * half, o_own = o_at(tl) + lanes + DP / 2 * half;
         float m = kNone, l0 = 0.0f, l1 = 0.0f;
         bool ok = true;
         for (int32_t k = 0; k < steps; ++k) {
-            ok = __all_sync(0xffffffffu, wait(bar.s + 8 * wg, k & 1));
-            if (!ok) break;
+            ok = ok && __all_sync(0xffffffffu, wait(bar.s + 8 * tl, k & 1));
             tc_fence_after();
-            uint32_t sr[kN];
+            const int32_t t0 = (j0 + k) * kN + 64 * half;
+            const int32_t lo = see.lo - t0, hi = see.hi - t0;
+            const bool edge = __any_sync(0xffffffffu, lo > 0 || hi < 64);
+            auto masked = [&](float* s, int b) {
 #pragma unroll
-            for (int b = 0; b < 4; ++b) tmem_ld32(sr + 32 * b, s_at(wg) + lanes + 32 * b);
-            tmem_wait_ld();
+                for (int n = 0; n < 32; ++n) s[n] = 32 * b + n >= lo && 32 * b + n < hi ? s[n] : kNone;
+            };
+            bool exact = k == 0;                                     // against this step's own maximum
+            uint32_t pk[32];
+            float a0, a1;
+            while (true) {
+                if (exact) {
+                    float top = kNone;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) tmem_loaded32(sr + 32 * b);
-            float* s = reinterpret_cast<float*>(sr);
-            const int32_t t0 = (j0 + k) * kN;
-            const bool edge = t0 < see.lo || t0 + kN > see.hi;
-            if (__any_sync(0xffffffffu, edge)) {
-                const int32_t a = see.lo - t0, b = see.hi - t0;
-#pragma unroll
-                for (int n = 0; n < kN; ++n) s[n] = n >= a && n < b ? s[n] : kNone;
-            }
-            float mx[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-            for (int n = 4; n < kN; n += 8) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mx[e] = n + 4 + e < kN ? fmaxf(fmaxf(mx[e], s[n + e]), s[n + 4 + e]) : fmaxf(mx[e], s[n + e]);
-            }
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-            // raise the reference? (m = -infinity: nothing was summed yet, O is zero or not yet written)
-            const bool raise = top > m && !((top - m) * c <= kRaise);
-            if (__any_sync(0xffffffffu, raise)) {
-                const float f = raise && m != kNone ? exp2_fast((m - top) * c) : 1.0f;
-                if (raise) m = top;
-                l0 *= f;
-                l1 *= f;
-                if (k > 0) {
-                    // the products before are done: this step's S was issued behind them
-#pragma unroll
-                    for (int b = 0; b < DP / 32; ++b) {
-                        uint32_t o[32];
-                        tmem_ld32(o, o_at(wg) + lanes + 32 * b);
+                    for (int b = 0; b < 2; ++b) {
+                        uint32_t sr[32];
+                        tmem_ld32(sr, s_own + 32 * b);
                         tmem_wait_ld();
-                        tmem_loaded32(o);
+                        tmem_loaded32(sr);
+                        float* s = reinterpret_cast<float*>(sr);
+                        if (edge) masked(s, b);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tmem_st32(o_at(wg) + lanes + 32 * b, o);
+                        for (int n = 0; n < 32; n += 2) top = max3(top, s[n], s[n + 1]);
+                    }
+                    tops[half * 256 + tl * 128 + t] = top;
+                    bar_some(pair, 64);
+                    top = fmaxf(top, tops[(half ^ 1) * 256 + tl * 128 + t]);
+                    // m = -infinity: nothing was summed yet, and O is zero or not yet written
+                    const bool raise = top > m && !((top - m) * c <= kRaise);
+                    const float f = raise && m != kNone ? exp2_fast((m - top) * c) : 1.0f;
+                    if (raise) m = top;
+                    l0 *= f;
+                    l1 *= f;
+                    if (k > 0 && __any_sync(0xffffffffu, f != 1.0f)) {
+                        // the products before are done: this step's S was issued behind them
+#pragma unroll
+                        for (int b = 0; b < DP / 32; ++b) {
+                            uint32_t o[16];
+                            tmem_ld16(o, o_own + 16 * b);
+                            tmem_wait_ld();
+                            tmem_loaded16(o);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st16(o_own + 16 * b, o);
+                        }
                     }
                 }
-            }
-            const float off = m == kNone ? 0.0f : -m * c;
+                const float off = m == kNone ? 0.0f : -m * c;
+                float top0 = kNone, top1 = kNone;
+                a0 = a1 = 0.0f;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                uint32_t pk[32];
+                for (int b = 0; b < 2; ++b) {
+                    uint32_t sr[32];
+                    tmem_ld32(sr, s_own + 32 * b);
+                    tmem_wait_ld();
+                    tmem_loaded32(sr);
+                    float* s = reinterpret_cast<float*>(sr);
+                    if (edge) masked(s, b);
 #pragma unroll
-                for (int n = 0; n < 32; ++n) {
-                    float x = s[64 * b + 2 * n], y = s[64 * b + 2 * n + 1];
-                    fma2(x, y, c, off);
-                    x = exp2_fast(x);
-                    y = exp2_fast(y);
-                    add2(l0, l1, x, y);
-                    pk[n] = N::pack(x, y);
+                    for (int n = 0; n < 16; ++n) {
+                        float x = s[2 * n], y = s[2 * n + 1];
+                        fma2(x, y, c, off);
+                        if (n & 1) top1 = max3(top1, x, y);
+                        else top0 = max3(top0, x, y);
+                        x = exp2_fast(x);
+                        y = exp2_fast(y);
+                        add2(a0, a1, x, y);
+                        pk[16 * b + n] = N::pack(x, y);
+                    }
                 }
-                tmem_st32(s_at(wg) + lanes + 32 * b, pk);
+                // Both halves of S are read behind this: P goes over the first one's columns.
+                const bool again = bar_or(pair, 64, !exact && fmaxf(top0, top1) > kRaise);
+                if (!again) break;
+                exact = true;
             }
+            add2(l0, l1, a0, a1);
+            tmem_st32(s_at(tl) + lanes + 32 * half, pk);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar.p + 8 * wg);
+            if (lane == 0) mbar_arrive(bar.p + 8 * tl);
         }
         // ---- the rows' results --------------------------------------------------------
         if (steps > 0 && ok) ok = __all_sync(0xffffffffu, wait(bar.o, 0));
         tc_fence_after();
-        const float l = l0 + l1;
-        const int64_t heads = (int64_t)st.kv_heads * st.group, row = (int64_t)(q.q0 + tok) * heads + head;
-        const int64_t all_rows = st.total_q * heads, at = split * all_rows + row;
-        const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
-        const float m2 = m == kNone ? kNone : m * c;
+        float l = l0 + l1;
+        tops[512 * 0 + half * 256 + tl * 128 + t] = l;
+        bar_some(pair, 64);
+        l = tops[tl * 128 + t] + tops[256 + tl * 128 + t];
+        const int32_t heads = st.kv_heads * st.group;
+        const int64_t all_rows = (int64_t)st.total_q * heads;
         if (ok) {
+            if (live && half == 0) {
+                const float m2 = m == kNone ? kNone : m * c;
+                const int64_t row = (int64_t)(q.q0 + tok) * heads + h * st.group + g;
+                if (j.splits > 1) reinterpret_cast<float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim)[split * all_rows + row] = make_float2(m2, l);
+                else if (j.lse) j.lse[row] = l == 0.0f ? kNone : (m2 + log2f(l)) * 0.69314718055994531f;
+            }
+            // Through shared memory (32 rows of DP bytes to a warp, in Q's place), so that a row's
+            // bytes leave in one piece: 16-bit results at once, binary32 parts in two passes.
+            const bool parts = j.splits > 1;
+            const float f = parts ? 1.0f : (l > 0.0f ? 1.0f / l : l);
+            const uint32_t stage = own + half * (P::tile / 2) + (warp & 3) * (P::tile / 8);
+            constexpr int VR = DP / 16;                                                  // 16-byte vectors of a staged row
+            const int vec0 = parts ? DP / 8 * half : VR * half;                          // of the whole row, where this half's begin
+            const int vecs = (parts ? st.head_dim * 4 : st.head_dim * 2) / 16;
+            for (int pass = 0; pass < (parts ? 2 : 1); ++pass) {
 #pragma unroll
-            for (int b = 0; b < DP / 32; ++b) {
-                uint32_t o[32];
-                if (steps > 0) {
-                    tmem_ld32(o, o_at(wg) + lanes + 32 * b);
-                    tmem_wait_ld();
-                    tmem_loaded32(o);
-                } else {
+                for (int b = 0; b < DP / 32; ++b) {
+                    // 16 columns: two vectors of 16-bit numbers, or four of binary32
+                    if (parts && b / (DP / 64) != pass) continue;
+                    uint32_t o[16];
+                    if (steps > 0) {
+                        tmem_ld16(o, o_own + 16 * b);
+                        tmem_wait_ld();
+                        tmem_loaded16(o);
+                    }
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0;
-                }
-                if (l == 0.0f) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0;
-                }
-                if (live) {
-                    if (j.splits == 1) {
-                        char* dst = j.out.base + 2 * ((int64_t)(q.q0 + tok) * j.out.row + (int64_t)head * j.out.head + 32 * b);
+                    for (int e = 0; e < 16; ++e) o[e] = steps > 0 && l != 0.0f ? __float_as_uint(__uint_as_float(o[e]) * f) : 0u;
+                    if (parts) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            if (32 * b + 8 * e >= st.head_dim) break;
-                            uint4 w;
-                            uint32_t* pw = reinterpret_cast<uint32_t*>(&w);
-#pragma unroll
-                            for (int x = 0; x < 4; ++x)
-                                pw[x] = N::pack(__uint_as_float(o[8 * e + 2 * x]) * inv, __uint_as_float(o[8 * e + 2 * x + 1]) * inv);
-                            *reinterpret_cast<uint4*>(dst + 16 * e) = w;
+                            const int v = 4 * (b % (DP / 64)) + e;
+                            st_shared16(stage + lane * VR * 16 + ((v ^ (lane & (VR - 1))) << 4), o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                         }
                     } else {
-                        float* dst = j.partial + at * st.head_dim + 32 * b;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            if (32 * b + 4 * e >= st.head_dim) break;
-                            *reinterpret_cast<uint4*>(dst + 4 * e) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        for (int e = 0; e < 2; ++e) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) w[x] = N::pack(__uint_as_float(o[8 * e + 2 * x]), __uint_as_float(o[8 * e + 2 * x + 1]));
+                            st_shared16(stage + lane * VR * 16 + (((2 * b + e) ^ (lane & (VR - 1))) << 4), w[0], w[1], w[2], w[3]);
                         }
                     }
                 }
-            }
-            if (live) {
-                if (j.splits == 1) {
-                    if (j.lse) j.lse[row] = l == 0.0f ? kNone : (m2 + log2f(l)) * 0.69314718055994531f;
-                } else {
-                    reinterpret_cast<float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim)[at] = make_float2(m2, l);
+                __syncwarp();
+#pragma unroll 4
+                for (int i = lane; i < 32 * VR; i += 32) {
+                    const int row = i / VR, v = i % VR, at = (warp & 3) * 32 + row, vec = vec0 + pass * VR + v;
+                    if (at < per && tl * per + at < rows && vec < vecs) {
+                        int32_t gg;
+                        const int32_t tk = token_of(st, row0 + tl * per + at, gg);
+                        const uint4 x = ld_shared16(stage + row * VR * 16 + ((v ^ (row & (VR - 1))) << 4));
+                        char* dst;
+                        if (parts) dst = reinterpret_cast<char*>(j.partial + (split * all_rows + (int64_t)(q.q0 + tk) * heads + h * st.group + gg) * st.head_dim);
+                        else dst = j.out.base + 2 * ((int64_t)(q.q0 + tk) * j.out.row + (int64_t)(h * st.group + gg) * j.out.head);
+                        *reinterpret_cast<uint4*>(dst + 16 * vec) = x;
+                    }
                 }
+                __syncwarp();
             }
         }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 12) tmem_dealloc(tmem, 512);
+    if (warp == 16) tmem_dealloc(tmem, 512);
 }
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -441,10 +494,10 @@ cudaError_t attend_tc(const AttendJob& j, cudaStream_t s) {
     auto* k = kvs_attend_tc_kernel<HALF, DP>;
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<DP>::bytes);
     if (e != cudaSuccess) return e;
-    CUtensorMap km{}, vm{};
-    const bool boxes = plane_map(&km, j.step, j.k_plane, HALF) && plane_map(&vm, j.step, j.v_plane, HALF);
-    const int64_t tiles = ((int64_t)j.step.max_q * j.step.group + 2 * kM - 1) / (2 * kM);
-    k<<<dim3((unsigned)(tiles * j.splits), j.step.kv_heads, j.step.requests), kThreads, Plan<DP>::bytes, s>>>(j, km, vm, boxes);
+    CUtensorMap km{}, vm{}, qm{};
+    const bool boxes = plane_map(&km, j.step, j.k_plane, HALF) && plane_map(&vm, j.step, j.v_plane, HALF), q_boxes = rows_map(&qm, j.step, j.q, HALF);
+    const int64_t pair = 2 * tile_rows_of(j.step.group), tiles = ((int64_t)j.step.max_q * j.step.group + pair - 1) / pair;
+    k<<<dim3((unsigned)(tiles * j.splits), j.step.kv_heads, j.step.requests), kThreads, Plan<DP>::bytes, s>>>(j, km, vm, qm, boxes, q_boxes);
     return cudaGetLastError();
 }
 

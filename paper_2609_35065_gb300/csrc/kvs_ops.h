@@ -81,6 +81,8 @@ int launch_append(const AppendJob& j, bool half, cudaStream_t s);
 int launch_attend(const AttendJob& j, bool half, cudaStream_t s);
 int launch_weigh(const WeighJob& j, bool half, int sms, cudaStream_t s);
 int launch_evict(const EvictJob& j, cudaStream_t s);
+// Packed rows (token * group + head) of a 128-row tile: whole tokens, where a token's fit.
+inline __host__ __device__ int32_t tile_rows_of(int32_t group) { return group <= 128 ? 128 / group * group : 128; }
 // How attention goes about a step, by its bounds alone: the kernel, and the parts that a
 // request's cached tokens are split into.
 struct AttendPlan {

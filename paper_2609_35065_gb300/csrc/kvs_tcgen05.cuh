@@ -48,11 +48,29 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
         "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
         :: KVS_I8(r, 0), KVS_I8(r, 8), KVS_I8(r, 16), KVS_I8(r, 24), "r"(addr) : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t* r, uint32_t addr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : KVS_R8(r, 0), KVS_R8(r, 8) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+                 :: KVS_I8(r, 0), KVS_I8(r, 8), "r"(addr) : "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // Keeps the compiler from using r[0..32) before the wait that this stands behind.
 __device__ __forceinline__ void tmem_loaded32(uint32_t* r) {
     asm volatile("" : KVS_U8(r, 0), KVS_U8(r, 8), KVS_U8(r, 16), KVS_U8(r, 24) :: "memory");
+}
+__device__ __forceinline__ void tmem_loaded16(uint32_t* r) { asm volatile("" : KVS_U8(r, 0), KVS_U8(r, 8) :: "memory"); }
+
+__device__ __forceinline__ void st_shared16(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
 }
 
 // ---- matrix products ---------------------------------------------------------
@@ -63,7 +81,8 @@ __device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t lead, uint32
     return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 |
            1ull << 46 | 2ull << 61;
 }
-// 16-bit operands, 32-bit accumulators, M = 128.
+// 16-bit operands, 32-bit accumulators, M = 128.  kNegA: the products' sign is turned.
+constexpr uint32_t kNegA = 1u << 13;
 __host__ __device__ constexpr uint32_t tc_idesc(bool half, int n, bool b_mn_major) {
     return 1u << 4 | (half ? 0u : 1u) << 7 | (half ? 0u : 1u) << 10 | (b_mn_major ? 1u : 0u) << 16 | (uint32_t)(n / 8) << 17 | 8u << 24;
 }
@@ -184,11 +203,25 @@ __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.a
 // Barrier of `threads` threads under a number of its own (1 to 15).
 __device__ __forceinline__ void bar_some(int id, int threads) { asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory"); }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // (a0, a1) * (b, b) + (c, c), and sums, two binary32 numbers at a time.
 __device__ __forceinline__ void fma2(float& x, float& y, float b, float c) {
     asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %2};\n\tmov.b64 r, {%3, %3};\n\t"
         "fma.rn.f32x2 p, p, q, r;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(x), "+f"(y) : "f"(b), "f"(c));
 }
+// The same, and whether any of them says so.
+__device__ __forceinline__ bool bar_or(int id, int threads, bool p) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbar.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"(id), "r"(threads), "r"((uint32_t)p) : "memory");
+    return r != 0;
+}
+
 // (x, y) * (b, b) + (c, d)
 __device__ __forceinline__ void fma2(float& x, float& y, float b, float c, float d) {
     asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %2};\n\tmov.b64 r, {%3, %4};\n\t"

@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
     const Request q = load_request(st, r);
     if (t0 >= q.T) return;                                       // the whole cluster
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
-    const int32_t per = q_boxes ? 128 / st.group * st.group : 128;      // rows of a tile
+    const int32_t per = tile_rows_of(st.group);                  // rows of a tile
     const RowSpan any = rows_seeing(st, q, t0, min(t0 + 127, q.T - 1), j.causal, j.window);
     const int32_t tile0 = (int32_t)(any.first / per), tiles = any.end > any.first ? (int32_t)((any.end + per - 1) / per) - tile0 : 0;
     const int32_t mine = (tiles - rank + share - 1) / share;     // row tiles tile0 + rank + share * i
