@@ -14,10 +14,11 @@
 // products.
 //
 // The running maximum m that O and the sums refer to is raised only when a score outgrows it
-// by 2^8: until then P is up to 2^8 instead of 1, which costs binary32 sums and 16-bit
-// floating P nothing, and O need not be rescaled, which most steps then never do.  So a step
-// takes its exponentials against the m at hand, and its maximum beside them, where it costs
-// nothing; the rare step whose maximum is too large is done again with m raised.
+// by 2^20 (half: 2^15, which it can still hold): until then P is up to that instead of 1, which
+// costs the relative precision of P and of binary32 sums nothing, and O need not be rescaled,
+// which hardly any step then does (at 2^8 every third step of a long cache had a row that did).  So a step takes its exponentials against the m at hand, and
+// its maximum beside them, where it costs nothing; the rare step whose maximum is too large is
+// done again with m raised.
 //
 // Products run in the order in which one thread issues them, which the reuse of S's columns
 // for P relies on: S of the next tile is issued behind the product that reads P.
@@ -29,7 +30,6 @@ namespace {
 constexpr int kM = 128, kN = 128;                  // rows of a tile, keys of a step
 constexpr int kThreads = 640, kLoaders = 3;
 constexpr float kNone = -INFINITY;
-constexpr float kRaise = 8.0f;                     // log2 by which P may exceed 1
 
 template <int DP>
 struct Plan {
@@ -52,6 +52,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
     extern __shared__ __align__(1024) char raw[];
     using N = Num<HALF>;
     using P = Plan<DP>;
+    constexpr float kRaise = HALF ? 15.0f : 20.0f;
     const StepView& st = j.step;
     const uint32_t base = smem_u32(raw);
     if (base & 1023) {                               // the swizzle needs it; there is no room to round it up
@@ -101,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
 
     // A wait that does not end is recorded; every role then leaves its loop (the others' waits end too).
     auto wait = [&](uint32_t b, uint32_t parity) {
-        if (tc_wait(b, parity)) return true;
+        if (mbar_wait(b, parity, kWaitLimitNs)) return true;
         record_error(st.err, KVS_ERR_TIMEOUT);
         return false;
     };
@@ -208,22 +209,20 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                     stage = 0;
                     ++round;
                 }
-                ok = __all_sync(0xffffffffu, filled(vs, vr) && wait(bar.p, k & 1));
+                const int32_t ks = stage, kr = round;
+                if (more && ++stage == P::stages) {
+                    stage = 0;
+                    ++round;
+                }
+                // V of this step and K of the next were loaded long ago; P is what is waited for
+                ok = __all_sync(0xffffffffu, filled(vs, vr) && (!more || filled(ks, kr)) && wait(bar.p, k & 1));
                 if (!ok) break;
                 tc_fence_after();
-                if (elect_one()) issue_o(0, vs, k > 0);
-                __syncwarp();
-                const int32_t ks = stage;
-                if (more) {
-                    ok = __all_sync(0xffffffffu, filled(ks, round));
-                    if (!ok) break;
-                    if (elect_one()) issue_s(0, ks);
-                    __syncwarp();
-                    if (++stage == P::stages) {
-                        stage = 0;
-                        ++round;
-                    }
+                if (elect_one()) {
+                    issue_o(0, vs, k > 0);
+                    if (more) issue_s(0, ks);
                 }
+                __syncwarp();
                 ok = __all_sync(0xffffffffu, wait(bar.p + 8, k & 1));
                 if (!ok) break;
                 tc_fence_after();
@@ -330,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                         }
                     }
                 }
-                const float off = m == kNone ? 0.0f : -m * c;
+                const float off = m == kNone ? 0.0f : -m * c, most = m == kNone ? kNone : kRaise;
                 float top0 = kNone, top1 = kNone;
                 a0 = a1 = 0.0f;
 #pragma unroll
@@ -354,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                     }
                 }
                 // Both halves of S are read behind this: P goes over the first one's columns.
-                const bool again = bar_or(pair, 64, !exact && fmaxf(top0, top1) > kRaise);
+                const bool again = bar_or(pair, 64, !exact && fmaxf(top0, top1) > most);
                 if (!again) break;
                 exact = true;
             }

@@ -94,21 +94,6 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
     return p != 0;
 }
-// Bounded wait like mbar_wait, for loops that wait often: the timer, which is slow to read, is
-// looked at once in 64 tries (each of which suspends the thread for a while).
-__device__ __forceinline__ bool tc_wait_long(uint32_t bar, uint32_t parity) {
-    const uint64_t t0 = global_ns();
-    do {
-        for (int i = 0; i < 64; ++i)
-            if (mbar_try_wait(bar, parity)) return true;
-    } while (global_ns() - t0 < kWaitLimitNs);
-    return false;
-}
-__device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity) {
-    for (int i = 0; i < 8; ++i)
-        if (mbar_try_wait(bar, parity)) return true;
-    return tc_wait_long(bar, parity);
-}
 // d (+)= a b over 16 elements of K, both operands in shared memory.
 __device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile(

@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at) : "memory");
     auto wait = [&](uint32_t b, uint32_t parity) {
-        if (tc_wait(b, parity)) return true;
+        if (mbar_wait(b, parity, kWaitLimitNs)) return true;
         record_error(st.err, KVS_ERR_TIMEOUT);
         return false;
     };

@@ -59,6 +59,26 @@ def test_windows(window, new, lens):
     _check_attend(Small(new, lens, 2, 4, 128), causal=False, window=window)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,T,window", [(200, 700, 70), (64, 900, 33), (64, 900, 128), (250, 1500, 200)])
+def test_rows_that_see_nothing_of_the_first_keys(new, T, window, dtype):
+    """The last rows of a tile begin to see keys some steps after the first ones."""
+    _check_attend(Small([new], [T], 2, 4, 128, dtype=dtype, spread=0.05), window=window)
+    _check_attend(Small([new], [T], 1, 4, 128, dtype=dtype, spread=2.0), window=window, scale=0.3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new", [1, 150])
+def test_maxima_that_jump(new, dtype):
+    """Blocks of keys whose scores outgrow those before by up to e^300, and fall again."""
+    sm = Small([new], [1100], 2, 4, 64, dtype=dtype)
+    k = sm.cache[0].view(-1, sm.H, sm.D)
+    at = sm.slots(0, np.arange(1100))
+    size = torch.tensor([0.05, 0.5, 4.0, 1.0, 12.0, 0.1, 30.0, 8.0, 40.0])[torch.arange(1100) // 128]
+    k[at] *= size[:, None, None].to(k.dtype)
+    _check_attend(sm)
+
+
 @pytest.mark.parametrize("new,lens", [([3, 40], [1, 300]), ([130, 7], [129, 0]), ([300], [50])])
 def test_every_cached_token_is_seen_without_causality(new, lens):
     _check_attend(Small(new, lens, 2, 4, 64), causal=False)
