@@ -480,7 +480,7 @@ int kvs_retrieve_noalloc(const kvs_geometry* geom, const kvs_paged_cache* cache,
  * allocate nothing, and can be captured into a graph.  Calls are enqueued on the
  * caller's stream and return; tensors must stay valid until the stream has passed them.
  * A length, row range or block id outside the stated bounds is not followed: what it
- * concerns is left out (cached tokens read as zeros, output rows unwritten) and
+ * concerns is left out (cached tokens read as zeros, output rows are left undefined) and
  * KVS_ERR_BOUNDS recorded for kvs_check_errors().  With KVS_F_VALIDATE (the only flag)
  * a call synchronises the stream and returns that code itself.
  *

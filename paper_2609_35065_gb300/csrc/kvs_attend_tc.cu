@@ -13,12 +13,12 @@
 // hold the ends of what may be read (there, rows outside become zeros) -- and one issues the
 // products.
 //
-// The running maximum m that O and the sums refer to is raised only when a score outgrows it
-// by 2^20 (half: 2^15, which it can still hold): until then P is up to that instead of 1, which
+// The running maximum m that O and the sums refer to is raised only when weights outgrow it by
+// 2^20 (half: 2^15, which it can still hold): until then P is up to that instead of 1, which
 // costs the relative precision of P and of binary32 sums nothing, and O need not be rescaled,
-// which hardly any step then does (at 2^8 every third step of a long cache had a row that did).  So a step takes its exponentials against the m at hand, and
-// its maximum beside them, where it costs nothing; the rare step whose maximum is too large is
-// done again with m raised.
+// which hardly any step then does (at 2^8 every third step of a long cache had a row that did).
+// So a step takes its exponentials against the m at hand and sees by their sum that none was
+// too large; the rare step that had such a one is done again with m raised.
 //
 // Products run in the order in which one thread issues them, which the reuse of S's columns
 // for P relies on: S of the next tile is issued behind the product that reads P.
@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
     extern __shared__ __align__(1024) char raw[];
     using N = Num<HALF>;
     using P = Plan<DP>;
-    constexpr float kRaise = HALF ? 15.0f : 20.0f;
+    constexpr float kMost = HALF ? 32768.0f : 1048576.0f;            // of a thread's weights of a step
     const StepView& st = j.step;
     const uint32_t base = smem_u32(raw);
     if (base & 1023) {                               // the swizzle needs it; there is no room to round it up
@@ -285,11 +285,12 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
             const int32_t t0 = (j0 + k) * kN + 64 * half;
             const int32_t lo = see.lo - t0, hi = see.hi - t0;
             const bool edge = __any_sync(0xffffffffu, lo > 0 || hi < 64);
-            auto masked = [&](float* s, int b) {
+            auto masked = [&](float* s, int first, int count) {
 #pragma unroll
-                for (int n = 0; n < 32; ++n) s[n] = 32 * b + n >= lo && 32 * b + n < hi ? s[n] : kNone;
+                for (int n = 0; n < count; ++n) s[n] = first + n >= lo && first + n < hi ? s[n] : kNone;
             };
-            bool exact = k == 0;                                     // against this step's own maximum
+            // Against this step's own maximum: the first step, and the first that rows see any key of.
+            bool exact = k == 0 || __any_sync(0xffffffffu, m == kNone && see.lo < (j0 + k + 1) * kN && see.hi > (j0 + k) * kN);
             uint32_t pk[32];
             float a0, a1;
             while (true) {
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                         tmem_wait_ld();
                         tmem_loaded32(sr);
                         float* s = reinterpret_cast<float*>(sr);
-                        if (edge) masked(s, b);
+                        if (edge) masked(s, 32 * b, 32);
 #pragma unroll
                         for (int n = 0; n < 32; n += 2) top = max3(top, s[n], s[n + 1]);
                     }
@@ -310,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                     bar_some(pair, 64);
                     top = fmaxf(top, tops[(half ^ 1) * 256 + tl * 128 + t]);
                     // m = -infinity: nothing was summed yet, and O is zero or not yet written
-                    const bool raise = top > m && !((top - m) * c <= kRaise);
+                    const bool raise = top > m;
                     const float f = raise && m != kNone ? exp2_fast((m - top) * c) : 1.0f;
                     if (raise) m = top;
                     l0 *= f;
@@ -329,8 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                         }
                     }
                 }
-                const float off = m == kNone ? 0.0f : -m * c, most = m == kNone ? kNone : kRaise;
-                float top0 = kNone, top1 = kNone;
+                const float off = m == kNone ? 0.0f : -m * c;
                 a0 = a1 = 0.0f;
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
@@ -339,21 +339,20 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                     tmem_wait_ld();
                     tmem_loaded32(sr);
                     float* s = reinterpret_cast<float*>(sr);
-                    if (edge) masked(s, b);
+                    if (edge) masked(s, 32 * b, 32);
 #pragma unroll
                     for (int n = 0; n < 16; ++n) {
                         float x = s[2 * n], y = s[2 * n + 1];
                         fma2(x, y, c, off);
-                        if (n & 1) top1 = max3(top1, x, y);
-                        else top0 = max3(top0, x, y);
                         x = exp2_fast(x);
                         y = exp2_fast(y);
                         add2(a0, a1, x, y);
                         pk[16 * b + n] = N::pack(x, y);
                     }
                 }
-                // Both halves of S are read behind this: P goes over the first one's columns.
-                const bool again = bar_or(pair, 64, !exact && fmaxf(top0, top1) > most);
+                // No weight is above their sum.  Both halves of S are read behind this: P goes over the
+                // first one's columns.
+                const bool again = bar_or(pair, 64, !exact && a0 + a1 > kMost);
                 if (!again) break;
                 exact = true;
             }

@@ -210,6 +210,7 @@ int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     const AttendPlan plan = attend_plan(j.step, sms);
     j.tc = plan.tc;
     j.splits = plan.splits;
+    j.row_tiles = plan.row_tiles;
     const int64_t need = workspace_bytes(j.step, sms);
     if (need > 0) {
         if (!a->workspace) return ops_fail(KVS_ERR_INVALID_ARG, "workspace is NULL, %lld bytes are needed", (long long)need);
