@@ -273,7 +273,8 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
         int32_t g;
         const int32_t tok = token_of(st, row0 + tl * per + t, g);
         const bool live = t < per && tl * per + t < rows;
-        Span see{0, 0};
+        // a tile's rows without a token see everything, so that their warp need not mask for them
+        Span see{0, INT32_MAX};
         if (live) see = seen_by(q, tok, tok, j.causal, j.window);
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // lane 32 (warp % 4) of tensor memory
         const uint32_t s_own = s_at(tl) + lanes + 64 * half, o_own = o_at(tl) + lanes + DP / 2 * half;
@@ -285,12 +286,12 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
             const int32_t t0 = (j0 + k) * kN + 64 * half;
             const int32_t lo = see.lo - t0, hi = see.hi - t0;
             const bool edge = __any_sync(0xffffffffu, lo > 0 || hi < 64);
-            auto masked = [&](float* s, int first, int count) {
+            auto masked = [&](float* s, int b) {
 #pragma unroll
-                for (int n = 0; n < count; ++n) s[n] = first + n >= lo && first + n < hi ? s[n] : kNone;
+                for (int n = 0; n < 32; ++n) s[n] = 32 * b + n >= lo && 32 * b + n < hi ? s[n] : kNone;
             };
             // Against this step's own maximum: the first step, and the first that rows see any key of.
-            bool exact = k == 0 || __any_sync(0xffffffffu, m == kNone && see.lo < (j0 + k + 1) * kN && see.hi > (j0 + k) * kN);
+            bool exact = k == 0 || __any_sync(0xffffffffu, live && m == kNone && see.lo < (j0 + k + 1) * kN && see.hi > (j0 + k) * kN);
             uint32_t pk[32];
             float a0, a1;
             while (true) {
@@ -303,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                         tmem_wait_ld();
                         tmem_loaded32(sr);
                         float* s = reinterpret_cast<float*>(sr);
-                        if (edge) masked(s, 32 * b, 32);
+                        if (edge) masked(s, b);
 #pragma unroll
                         for (int n = 0; n < 32; n += 2) top = max3(top, s[n], s[n + 1]);
                     }
@@ -339,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                     tmem_wait_ld();
                     tmem_loaded32(sr);
                     float* s = reinterpret_cast<float*>(sr);
-                    if (edge) masked(s, 32 * b, 32);
+                    if (edge) masked(s, b);
 #pragma unroll
                     for (int n = 0; n < 16; ++n) {
                         float x = s[2 * n], y = s[2 * n + 1];
@@ -352,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                 }
                 // No weight is above their sum.  Both halves of S are read behind this: P goes over the
                 // first one's columns.
-                const bool again = bar_or(pair, 64, !exact && a0 + a1 > kMost);
+                const bool again = bar_or(pair, 64, !exact && live && a0 + a1 > kMost);
                 if (!again) break;
                 exact = true;
             }
