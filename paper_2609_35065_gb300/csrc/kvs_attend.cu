@@ -97,13 +97,16 @@ __global__ void __launch_bounds__(kWarps * 32) kvs_attend_rows_kernel(AttendJob 
     const uint32_t ring = base + warp * STAGES * STAGE;
     const int32_t count = (keys.hi - keys.lo + kKeys - 1) / kKeys;
     const int32_t mine = (count - warp + kWarps - 1) / kWarps;
+    // The row of this lane's key of stage i, looked up a stage before it is loaded.
+    auto look_up = [&](int32_t i) {
+        const int32_t t = keys.lo + kKeys * (warp + kWarps * i) + (lane & 15);
+        return i < mine && t < keys.hi ? row_of(st, table, t) : (int64_t)-1;
+    };
+    int64_t mrow = look_up(0);
     auto load = [&](int32_t i) {
         if (i < mine) {
-            const int32_t t0 = keys.lo + kKeys * (warp + kWarps * i);
             const uint32_t at = ring + (i % STAGES) * STAGE;
-            // lane's key, looked up once
-            const int32_t t = t0 + (lane & 15);
-            const int64_t mrow = t < keys.hi ? row_of(st, table, t) : -1;
+            const int64_t ahead = look_up(i + 1);
 #pragma unroll
             for (int v = lane; v < kKeys * CH; v += 32) {
                 const int k = v / CH, c = v % CH;
@@ -113,6 +116,7 @@ __global__ void __launch_bounds__(kWarps * 32) kvs_attend_rows_kernel(AttendJob 
                 cp_async16(at + swz<PITCH>(k, c), j.k_plane + off, there);
                 cp_async16(at + kKeys * PITCH + swz<PITCH>(k, c), j.v_plane + off, there);
             }
+            mrow = ahead;
         }
         cp_commit();
     };
@@ -298,17 +302,18 @@ __global__ void __launch_bounds__(kWarps * 32) kvs_attend_rows_kernel(AttendJob 
     }
 }
 
-// Joins the splits' parts: a warp per row.
+// Joins the splits' parts: a warp per row, whose lanes weigh a split each and whose loads of
+// the parts go out eight at a time.
 template <bool HALF>
 __global__ void __launch_bounds__(128) kvs_attend_join_kernel(AttendJob j) {
     const StepView& st = j.step;
     using N = Num<HALF>;
-    grid_wait();
     const int32_t heads = st.kv_heads * st.group;
     const int64_t all_rows = (int64_t)st.total_q * heads;
     const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
     if (row >= all_rows) return;
+    grid_wait();
     const float2* ml = reinterpret_cast<const float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim);
     float M = kNone;
     for (int k = lane; k < j.splits; k += 32) M = fmaxf(M, ml[k * all_rows + row].x);
@@ -317,16 +322,27 @@ __global__ void __launch_bounds__(128) kvs_attend_join_kernel(AttendJob j) {
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     float L = 0.0f;
     const bool has = 4 * lane < st.head_dim;
-    for (int k = 0; k < j.splits; ++k) {
-        const float2 v = ml[k * all_rows + row];
-        const float f = v.y == 0.0f ? 0.0f : exp2_fast(v.x - M);
-        L += f * v.y;
-        if (has) {
-            const float4 p = *reinterpret_cast<const float4*>(j.partial + (k * all_rows + row) * st.head_dim + 4 * lane);
-            o.x += f * p.x;
-            o.y += f * p.y;
-            o.z += f * p.z;
-            o.w += f * p.w;
+    const float* part = j.partial + row * st.head_dim + 4 * lane;
+    for (int k0 = 0; k0 < j.splits; k0 += 32) {
+        float2 v = make_float2(kNone, 0.0f);
+        if (k0 + lane < j.splits) v = ml[(k0 + lane) * all_rows + row];
+        const float f = v.y == 0.0f ? 0.0f : exp2_fast(v.x - M), g = f * v.y;
+        for (int k = 0; k < min(32, j.splits - k0); k += 8) {
+            float4 p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                p[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (has && k0 + k + e < j.splits) p[e] = *reinterpret_cast<const float4*>(part + (k0 + k + e) * all_rows * st.head_dim);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float w = __shfl_sync(0xffffffffu, f, k + e);
+                L += __shfl_sync(0xffffffffu, g, k + e);
+                o.x += w * p[e].x;
+                o.y += w * p[e].y;
+                o.z += w * p[e].z;
+                o.w += w * p[e].w;
+            }
         }
     }
     const float inv = L > 0.0f ? 1.0f / L : L;

@@ -28,7 +28,7 @@ __device__ __forceinline__ RowSpan rows_seeing(const StepView& st, const Request
 
 __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t h, int32_t t, float sum) {
     float* w = j.weights + r * j.request_stride + h * j.head_stride + t;
-    *w = j.decay == 0.0f ? sum : fmaf(j.decay, *w, sum);
+    *w = j.decay == 0.0f ? sum : j.decay * *w + sum;
 }
 
 // ---------------------------------------------------------------------------
@@ -310,13 +310,13 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
 }
 
 // ---------------------------------------------------------------------------
-// Few rows (a decode step): a warp takes 32 keys straight into the fragments of
-// mma.m16n8k16, and the rows 16 at a time.  The sum over a head's dims has no order, so lane 4i + c takes 16 contiguous
-// bytes of key i (dims 32 k + 8 c ...) for what the instruction calls dims 2c, 2c + 1, 2c + 8
-// and 2c + 9 of two of its steps, for keys and rows alike: no shared memory, no shuffles.
-// Bound by HBM: K is read once.
+// Few rows (a decode step): a warp takes 16 keys at a time straight into the fragments of
+// mma.m16n8k16, the next 16 in flight meanwhile, and the rows 16 at a time.  The sum over a
+// head's dims has no order, so lane 4i + c takes 16 contiguous bytes of key i (dims 32 k + 8 c
+// ...) for what the instruction calls dims 2c, 2c + 1, 2c + 8 and 2c + 9 of two of its steps,
+// for keys and rows alike: no shared memory, no shuffles.  Bound by HBM: K is read once.
 // ---------------------------------------------------------------------------
-constexpr int kRowWarps = 8, kRowKeys = 32;
+constexpr int kRowWarps = 8, kRowKeys = 16, kWaves = 4;
 
 template <bool HALF>
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -328,86 +328,133 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <bool HALF, int DP>
+// 16 rows' fragments, lse and what they see.
+template <int K>
+struct RowFrags {
+    uint4 q[2][K];               // rows i and i + 8
+    float lse[2];                // times -log2(e)
+    Span  see[2];
+};
+template <bool HALF, int K>
+__device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, const Request& q, int32_t h, int32_t p0, int lane) {
+    const StepView& st = j.step;
+    const int32_t total = q.n * st.group;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        const int32_t p = p0 + (lane >> 2) + 8 * m;
+        int32_t g = 0;
+        const int32_t tok = token_of(st, p, g), head = h * st.group + g;
+        f.see[m] = Span{0, 0};
+        f.lse[m] = 0.0f;
+        if (p < total) {
+            f.see[m] = seen_by(q, tok, tok, j.causal, j.window);
+            f.lse[m] = -kLog2e * __ldg(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + head);
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            f.q[m][k] = make_uint4(0, 0, 0, 0);
+            const int32_t d = 32 * k + 8 * (lane & 3);
+            if (p < total && d < st.head_dim)
+                f.q[m][k] = __ldg(reinterpret_cast<const uint4*>(j.q.base + 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)head * j.q.head + d)));
+        }
+    }
+}
+
+// ONE: the request has at most 16 rows, whose fragments stay.
+template <bool HALF, int DP, bool ONE>
 __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(WeighJob j) {
     constexpr int K = DP / 32;                                   // 16-byte vectors of a lane and key
     const StepView& st = j.step;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, i = lane >> 2;
     const int32_t h = blockIdx.y, r = blockIdx.z;
     const Request q = load_request(st, r);
-    const int32_t t0 = (blockIdx.x * kRowWarps + warp) * kRowKeys;
-    if (t0 >= q.T) return;
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
-    // keys t0 + 8 n + i
-    uint4 kv[4][K];
+    // this CTA's tiles of 16 keys, of which its warps take every eighth
+    const int32_t all = (q.T + kRowKeys - 1) / kRowKeys;
+    const int32_t first = (int32_t)((int64_t)all * blockIdx.x / gridDim.x), end = (int32_t)((int64_t)all * (blockIdx.x + 1) / gridDim.x);
+    const int32_t mine = (end - first - warp + kRowWarps - 1) / kRowWarps;
+    if (mine <= 0) return;
+    auto key0 = [&](int32_t n) { return (first + warp + kRowWarps * n) * kRowKeys; };
+    // a lane looks keys i and i + 8 of a tile up two tiles ahead, and loads them one ahead
+    auto look_up = [&](int32_t n, int64_t (&row)[2]) {
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-        const int32_t t = t0 + 8 * n + i;
-        const int64_t row = t < q.T ? row_of(st, table, t) : -1;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            kv[n][k] = make_uint4(0, 0, 0, 0);
-            const int32_t d = 32 * k + 8 * c;
-            if (row >= 0 && d < st.head_dim) kv[n][k] = *reinterpret_cast<const uint4*>(j.k_plane + 2 * (row + (int64_t)h * st.head_dim + d));
+        for (int e = 0; e < 2; ++e) {
+            const int32_t t = key0(n) + i + 8 * e;
+            row[e] = n < mine && t < q.T ? row_of(st, table, t) : -1;
         }
-    }
-    const int32_t total = q.n * st.group;
-    float sums[8];                                               // keys 8 n + 2 c and + 1
+    };
+    // lane 4 i + c, i < 4, adds to the weight of key 8 (i / 2) + 2 c + i % 2, which it loads with the keys
+    float* weights = j.weights + r * j.request_stride + h * j.head_stride;
+    auto load = [&](int32_t n, const int64_t (&row)[2], uint4 (&kv)[2][K], float& old) {
+        const int32_t t = key0(n) + 8 * (i >> 1) + 2 * c + (i & 1);
+        old = 0.0f;
+        if (j.decay != 0.0f && n < mine && i < 4 && t < q.T) old = j.decay * weights[t];
 #pragma unroll
-    for (int n = 0; n < 8; ++n) sums[n] = 0.0f;
-    for (int32_t p0 = 0; p0 < total; p0 += 16) {
-        // rows p0 + i and p0 + i + 8
-        uint4 qv[2][K];
-        float lse[2];
-        Span see[2];
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const int32_t p = p0 + i + 8 * m;
-            int32_t g = 0;
-            const int32_t tok = token_of(st, p, g), head = h * st.group + g;
-            see[m] = Span{0, 0};
-            lse[m] = 0.0f;
-            if (p < total) {
-                see[m] = seen_by(q, tok, tok, j.causal, j.window);
-                lse[m] = __ldg(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + head) * kLog2e;
-            }
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                qv[m][k] = make_uint4(0, 0, 0, 0);
+                kv[e][k] = make_uint4(0, 0, 0, 0);
                 const int32_t d = 32 * k + 8 * c;
-                if (p < total && d < st.head_dim)
-                    qv[m][k] = __ldg(reinterpret_cast<const uint4*>(j.q.base + 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)head * j.q.head + d)));
+                if (row[e] >= 0 && d < st.head_dim) kv[e][k] = *reinterpret_cast<const uint4*>(j.k_plane + 2 * (row[e] + (int64_t)h * st.head_dim + d));
             }
-        }
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                mma<HALF>(s, qv[0][k].x, qv[1][k].x, qv[0][k].y, qv[1][k].y, kv[n][k].x, kv[n][k].y);
-                mma<HALF>(s, qv[0][k].z, qv[1][k].z, qv[0][k].w, qv[1][k].w, kv[n][k].z, kv[n][k].w);
-            }
+    };
+    const int32_t total = q.n * st.group;
+    RowFrags<K> one;
+    auto weigh = [&](int32_t n, const uint4 (&kv)[2][K], float old) {
+        float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};                // keys 8 e + 2 c and + 1
+        auto add = [&](const RowFrags<K>& f) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int32_t t = t0 + 8 * n + 2 * c + e;
-                float x = 0.0f;
+                float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
-                    if (t >= see[m].lo && t < see[m].hi) x += exp2_fast(fmaf(s[2 * m + e], j.scale_log2, -lse[m]));
-                sums[2 * n + e] += x;
+                for (int k = 0; k < K; ++k) {
+                    mma<HALF>(s, f.q[0][k].x, f.q[1][k].x, f.q[0][k].y, f.q[1][k].y, kv[e][k].x, kv[e][k].y);
+                    mma<HALF>(u, f.q[0][k].z, f.q[1][k].z, f.q[0][k].w, f.q[1][k].w, kv[e][k].z, kv[e][k].w);
+                }
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int32_t t = key0(n) + 8 * e + 2 * c + b;
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+                        if (t >= f.see[m].lo && t < f.see[m].hi) sums[2 * e + b] += exp2_fast(fmaf(s[2 * m + b] + u[2 * m + b], j.scale_log2, f.lse[m]));
+                }
+            }
+        };
+        if (ONE) {
+            add(one);
+        } else {
+            for (int32_t p0 = 0; p0 < total; p0 += 16) {
+                RowFrags<K> f;
+                load_rows<HALF, K>(f, j, q, h, p0, lane);
+                add(f);
             }
         }
-    }
-    // the rows' sums join over the lanes of one c; lane 4 i + c writes key 8 (i / 2) + 2 c + i % 2
-    float mine = 0.0f;
+        // the rows' sums join over the lanes of one c
+        float x = 0.0f;
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
+        for (int e = 0; e < 4; ++e) {
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) sums[n] += __shfl_xor_sync(0xffffffffu, sums[n], d);
-        if (i == n) mine = sums[n];
+            for (int d = 4; d < 32; d <<= 1) sums[e] += __shfl_xor_sync(0xffffffffu, sums[e], d);
+            if (i == e) x = sums[e];
+        }
+        const int32_t t = key0(n) + 8 * (i >> 1) + 2 * c + (i & 1);
+        if (i < 4 && t < q.T) weights[t] = old + x;
+    };
+    uint4 ka[2][K], kb[2][K];
+    float wa, wb;
+    int64_t row[2];
+    look_up(0, row);
+    load(0, row, ka, wa);
+    look_up(1, row);
+    if (ONE) load_rows<HALF, K>(one, j, q, h, 0, lane);
+    for (int32_t n = 0; n < mine; n += 2) {
+        load(n + 1, row, kb, wb);
+        look_up(n + 2, row);
+        weigh(n, ka, wa);
+        load(n + 2, row, ka, wa);
+        look_up(n + 3, row);
+        if (n + 1 < mine) weigh(n + 1, kb, wb);
     }
-    const int32_t t = t0 + 8 * (i >> 1) + 2 * c + (i & 1);
-    if (t < q.T) add_weight(j, r, h, t, mine);
 }
 
 template <bool HALF, int DP>
@@ -415,8 +462,13 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     const StepView& st = j.step;
     const int64_t rows = (int64_t)st.max_q * st.group;
     if (rows <= 64) {
-        const unsigned x = (unsigned)((st.max_kv + kRowWarps * kRowKeys - 1) / (kRowWarps * kRowKeys));
-        kvs_weigh_rows_kernel<HALF, DP><<<dim3(x, st.kv_heads, st.requests), kRowWarps * 32, 0, s>>>(j);
+        // Two CTAs to an SM: enough of them that lengths even out, and not more than give a warp four tiles.
+        const int64_t pairs = (int64_t)st.kv_heads * st.requests, most = (st.max_kv + kRowWarps * kRowKeys * 4 - 1) / (kRowWarps * kRowKeys * 4);
+        int64_t x = (kWaves * 2 * sms + pairs - 1) / pairs;
+        x = x > most ? most : x;
+        const dim3 grid((unsigned)x, st.kv_heads, st.requests);
+        if (rows <= 16) kvs_weigh_rows_kernel<HALF, DP, true><<<grid, kRowWarps * 32, 0, s>>>(j);
+        else kvs_weigh_rows_kernel<HALF, DP, false><<<grid, kRowWarps * 32, 0, s>>>(j);
         return cudaGetLastError();
     }
     auto* k = kvs_weigh_tc_kernel<HALF, DP>;
