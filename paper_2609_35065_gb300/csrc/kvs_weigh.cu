@@ -170,40 +170,82 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
             const int32_t tok = token_of(st, (int32_t)p, g);
             return -kLog2e * __ldg(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + h * st.group + g);
         };
-        float e0 = lse_of(0, a0), e1 = lse_of(0, a1);
+        auto stage_free = [&](int32_t stage, int32_t round) {
+            const bool ok = round == 0 || lane != 0 || wait(b_free + 8 * stage, (round - 1) & 1);
+            return __all_sync(0xffffffffu, ok);
+        };
         int32_t stage = 0, round = 0, i = 0;
-        for (; i < mine; ++i) {
-            if (round > 0) {
-                const bool ok = lane != 0 || wait(b_free + 8 * stage, (round - 1) & 1);
-                if (!__all_sync(0xffffffffu, ok)) break;
+        auto next_stage = [&]() {
+            if (++stage == kStages) {
+                stage = 0;
+                ++round;
             }
-            const int32_t p0 = (tile0 + rank + share * i) * per;
-            const uint32_t dst = ring + stage * P::tile;
-            float* lse = reinterpret_cast<float*>(mem + P::lse) + stage * 128;
-            if (!q_boxes || warp > 9) {
-                if (a0 < 128) lse[a0] = e0;
+        };
+        if (q_boxes && warp > 9) {
+            // four tiles' lse ahead of the four that are announced: a load takes longer than a tile
+            if (pending) {
+                cp_wait<0>();
+                announce();
+            }
+            float now[4][2], next[4][2];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                now[e][0] = lse_of(e, a0);
+                now[e][1] = lse_of(e, a1);
+            }
+            bool ok = true;
+            for (; ok && i < mine; i += 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    next[e][0] = lse_of(i + 4 + e, a0);
+                    next[e][1] = lse_of(i + 4 + e, a1);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (!ok || i + e >= mine) break;
+                    ok = stage_free(stage, round);
+                    if (!ok) break;
+                    float* lse = reinterpret_cast<float*>(mem + P::lse) + stage * 128;
+                    lse[a0] = now[e][0];
+                    lse[a1] = now[e][1];
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(b_full + 8 * stage);
+                    next_stage();
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    now[e][0] = next[e][0];
+                    now[e][1] = next[e][1];
+                }
+            }
+        } else if (q_boxes) {
+            if (pending) {
+                cp_wait<0>();
+                announce();
+            }
+            for (; i < mine; ++i) {
+                if (!stage_free(stage, round)) break;
+                if (lane == 0) {
+                    const int32_t p0 = (tile0 + rank + share * i) * per;
+                    mbar_expect_tx(b_full + 8 * stage, (uint32_t)per * DP * 2);
+#pragma unroll
+                    for (int c = 0; c < DP / 64; ++c)
+                        tma_load_3d(ring + stage * P::tile + c * 128 * 128, &q_map, 64 * c, h * st.group, q.q0 + p0 / st.group, b_full + 8 * stage);
+                }
+                __syncwarp();
+                next_stage();
+            }
+        } else {
+            float e0 = lse_of(0, a0), e1 = lse_of(0, a1);
+            for (; i < mine; ++i) {
+                if (!stage_free(stage, round)) break;
+                const int32_t p0 = (tile0 + rank + share * i) * per;
+                const uint32_t dst = ring + stage * P::tile;
+                float* lse = reinterpret_cast<float*>(mem + P::lse) + stage * 128;
+                lse[a0] = e0;
                 if (a1 < 128) lse[a1] = e1;
                 e0 = lse_of(i + 1, a0);
                 e1 = lse_of(i + 1, a1);
-            }
-            if (q_boxes) {
-                if (pending) {
-                    cp_wait<0>();
-                    announce();
-                }
-                if (warp == 9) {
-                    if (lane == 0) {
-                        mbar_expect_tx(b_full + 8 * stage, (uint32_t)per * DP * 2);
-#pragma unroll
-                        for (int c = 0; c < DP / 64; ++c)
-                            tma_load_3d(dst + c * 128 * 128, &q_map, 64 * c, h * st.group, q.q0 + p0 / st.group, b_full + 8 * stage);
-                    }
-                    __syncwarp();
-                } else {
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(b_full + 8 * stage);
-                }
-            } else {
                 constexpr int CH = DP / 8;
 #pragma unroll 4
                 for (int v = u; v < 128 * CH; v += 96) {
@@ -220,17 +262,14 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
                     announce();
                 }
                 pending = b_full + 8 * stage;
-            }
-            if (++stage == kStages) {
-                stage = 0;
-                ++round;
+                next_stage();
             }
         }
         cp_wait<0>();
         if (pending) announce();
         // every load has landed when its sums are done; after a failure, wait for them here
         if (mine > 0) mbar_wait(b_k, 0, kWaitLimitNs);
-        if (i < mine)
+        if (i < mine && warp == 9)
             for (int k = i < kStages ? 0 : i - kStages; k < i; ++k) mbar_wait(b_full + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs);
     } else {
         // ---- sums: a key to a thread ---------------------------------------------------
