@@ -34,23 +34,24 @@ __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t
 // ---------------------------------------------------------------------------
 // Many rows: S^T = K Q^T on the tensor cores, a tile of 128 keys (the accumulator's lanes)
 // per CTA and the rows in tiles of at most 128 (its columns), so that a thread sums its key's
-// weights in registers.  Two warpgroups take the row tiles in turn, from four accumulators; in
-// the third one warp issues the products, one loads the next row tiles (TMA boxes of whole
-// tokens; cp.async by three warps where the rows have no such boxes) and two their lse.
+// weights in registers.  Four warpgroups take the row tiles in turn, from an accumulator each;
+// in the fifth one warp issues the products, one loads the next row tiles (TMA boxes of whole
+// tokens; cp.async by three warps where the rows have no such boxes) and two their lse, in a
+// ring of its own: a tile's rows are done with when the products are, its lse with the sums.
 // Bound by the exponentials, one for each score, and as much by the products.
 //
 // Where there are fewer key tiles than SMs, a cluster of CTAs shares a key tile's row tiles
 // and joins its sums, in the CTAs' order, through distributed shared memory.
 // ---------------------------------------------------------------------------
-constexpr int kThreads = 384, kStages = 5, kAccs = 4;
+constexpr int kThreads = 640, kStages = 5, kAccs = 4, kSlots = 8;
 
 template <int DP>
 struct WPlan {
     static constexpr int tile = 128 * DP * 2;
-    static constexpr int lse = tile * (1 + kStages);             // [stages][128] binary32, times -log2(e)
-    static constexpr int sums = lse + kStages * 512;             // [2][128]
-    static constexpr int bars = sums + 1024;
-    static constexpr int bytes = bars + 256 + 1024;
+    static constexpr int lse = tile * (1 + kStages);             // [kSlots][128] binary32, times -log2(e)
+    static constexpr int sums = lse + kSlots * 512;              // [kAccs][128]
+    static constexpr int bars = sums + kAccs * 512;
+    static constexpr int bytes = bars + 512 + 1024;
 };
 
 template <bool HALF, int DP>
@@ -63,7 +64,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
     char* mem = raw + (base - smem_u32(raw));
     const uint32_t ring = base + P::tile, ctl = base + P::bars;
     const uint32_t b_k = ctl, b_full = ctl + 8, b_free = b_full + 8 * kStages, b_s = b_free + 8 * kStages, b_e = b_s + 8 * kAccs, b_done = b_e + 8 * kAccs,
-                   tmem_at = b_done + 8;
+                   b_lse = b_done + 8, b_read = b_lse + 8 * kSlots, tmem_at = b_read + 8 * kSlots;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = threadIdx.x >> 7;
     const int32_t r = blockIdx.z, h = blockIdx.y, rank = blockIdx.x % share, t0 = (blockIdx.x / share) * 128;
     const Request q = load_request(st, r);
@@ -78,8 +79,12 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
     if (threadIdx.x == 0) {
         mbar_init(b_k, 3);
         for (int i = 0; i < kStages; ++i) {
-            mbar_init(b_full + 8 * i, 3);                        // the loading warps
-            mbar_init(b_free + 8 * i, 5);                        // the products, and the four warps that read lse
+            mbar_init(b_full + 8 * i, q_boxes ? 1 : 3);          // the loading warps
+            mbar_init(b_free + 8 * i, 1);
+        }
+        for (int i = 0; i < kSlots; ++i) {
+            mbar_init(b_lse + 8 * i, q_boxes ? 2 : 3);
+            mbar_init(b_read + 8 * i, 4);                        // a warpgroup's warps
         }
         for (int i = 0; i < kAccs; ++i) {
             mbar_init(b_s + 8 * i, 1);
@@ -88,7 +93,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         mbar_init(b_done, 1);
         mbar_init_fence();
     }
-    if (warp == 8) tmem_alloc(tmem_at, 128 * kAccs);
+    if (warp == 16) tmem_alloc(tmem_at, 128 * kAccs);
     // rows that no box fills are zeros for good, and weigh nothing
     for (int i = threadIdx.x; i < (128 - per) * (DP / 8) * kStages; i += kThreads) {
         const int stage = i / ((128 - per) * (DP / 8)), v = i % ((128 - per) * (DP / 8)), row = per + v / (DP / 8), c = v % (DP / 8);
@@ -108,7 +113,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
 
     float sum = 0.0f;
     const int t = threadIdx.x & 127;
-    if (warp == 8) {
+    if (warp == 16) {
         // ---- the products: the warp waits together, one lane issues ----------------------
         constexpr uint32_t id = tc_idesc(HALF, 128, false);
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
@@ -142,9 +147,9 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
             mbar_wait(b_done, 0, kWaitLimitNs);
         }
         __syncwarp();
-    } else if (wg == 2) {
+    } else if (warp > 16) {
         // ---- loads: warp 9 the rows, warps 10 and 11 their lse; by rows all three both ------
-        const int u = threadIdx.x - 9 * 32;                      // 0 to 95
+        const int u = threadIdx.x - 17 * 32;                     // 0 to 95
         uint32_t pending = 0;
         auto announce = [&]() {
             fence_async_smem();
@@ -154,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         };
         if (mine > 0) {
             if (k_boxes) {
-                tile_boxes<DP>(base, &k_map, st, h, box_of<DP, 3>(st, table, t0, q.T, warp - 9, lane), b_k, lane);
+                tile_boxes<DP>(base, &k_map, st, h, box_of<DP, 3>(st, table, t0, q.T, warp - 17, lane), b_k, lane);
             } else {
                 tile_rows<DP, 96>(base, j.k_plane, st, table, h, t0, 0, q.T, u);
                 cp_commit();
@@ -165,23 +170,35 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         const int a0 = q_boxes ? u - 32 : u, a1 = q_boxes ? u + 32 : u + 96;
         auto lse_of = [&](int32_t i, int row) {
             const int64_t p = (int64_t)(tile0 + rank + share * i) * per + row;
-            if (i >= mine || row < 0 || row >= per || p >= total) return -INFINITY;       // weighs nothing
+            float x = INFINITY;                                  // weighs nothing
             int32_t g;
-            const int32_t tok = token_of(st, (int32_t)p, g);
-            return -kLog2e * __ldg(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + h * st.group + g);
+            const int32_t tok = token_of(st, (int32_t)min(p, (int64_t)total), g);
+            if (i < mine && row >= 0 && row < per && p < total) x = __ldg(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + h * st.group + g);
+            return x;                                            // as it is: a product here would wait for the load
         };
         auto stage_free = [&](int32_t stage, int32_t round) {
             const bool ok = round == 0 || lane != 0 || wait(b_free + 8 * stage, (round - 1) & 1);
             return __all_sync(0xffffffffu, ok);
         };
         int32_t stage = 0, round = 0, i = 0;
+        auto slot_free = [&](int32_t i) {
+            const bool ok = i < kSlots || lane != 0 || wait(b_read + 8 * (i % kSlots), (i / kSlots - 1) & 1);
+            return __all_sync(0xffffffffu, ok);
+        };
+        auto put_lse = [&](int32_t i, float e0, float e1) {
+            float* lse = reinterpret_cast<float*>(mem + P::lse) + (i % kSlots) * 128;
+            lse[a0] = -kLog2e * e0;
+            if (a1 < 128) lse[a1] = -kLog2e * e1;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_lse + 8 * (i % kSlots));
+        };
         auto next_stage = [&]() {
             if (++stage == kStages) {
                 stage = 0;
                 ++round;
             }
         };
-        if (q_boxes && warp > 9) {
+        if (q_boxes && warp > 17) {
             // four tiles' lse ahead of the four that are announced: a load takes longer than a tile
             if (pending) {
                 cp_wait<0>();
@@ -203,14 +220,8 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (!ok || i + e >= mine) break;
-                    ok = stage_free(stage, round);
-                    if (!ok) break;
-                    float* lse = reinterpret_cast<float*>(mem + P::lse) + stage * 128;
-                    lse[a0] = now[e][0];
-                    lse[a1] = now[e][1];
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(b_full + 8 * stage);
-                    next_stage();
+                    ok = slot_free(i + e);
+                    if (ok) put_lse(i + e, now[e][0], now[e][1]);
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -238,12 +249,10 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         } else {
             float e0 = lse_of(0, a0), e1 = lse_of(0, a1);
             for (; i < mine; ++i) {
-                if (!stage_free(stage, round)) break;
+                if (!stage_free(stage, round) || !slot_free(i)) break;
                 const int32_t p0 = (tile0 + rank + share * i) * per;
                 const uint32_t dst = ring + stage * P::tile;
-                float* lse = reinterpret_cast<float*>(mem + P::lse) + stage * 128;
-                lse[a0] = e0;
-                if (a1 < 128) lse[a1] = e1;
+                put_lse(i, e0, e1);
                 e0 = lse_of(i + 1, a0);
                 e1 = lse_of(i + 1, a1);
                 constexpr int CH = DP / 8;
@@ -269,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         if (pending) announce();
         // every load has landed when its sums are done; after a failure, wait for them here
         if (mine > 0) mbar_wait(b_k, 0, kWaitLimitNs);
-        if (i < mine && warp == 9)
+        if (i < mine && warp == 17)
             for (int k = i < kStages ? 0 : i - kStages; k < i; ++k) mbar_wait(b_full + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs);
     } else {
         // ---- sums: a key to a thread ---------------------------------------------------
@@ -277,15 +286,16 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         const bool live = t0 + t < q.T;
         const RowSpan see = rows_seeing(st, q, t0 + t, t0 + t, j.causal, j.window);
         const float c = j.scale_log2;
-        for (int32_t i = wg; i < mine; i += 2) {
-            const int stage = i % kStages, acc = i % kAccs;
-            if (!__all_sync(0xffffffffu, wait(b_full + 8 * stage, (i / kStages) & 1) && wait(b_s + 8 * acc, (i / kAccs) & 1))) break;
+        const int acc = wg;
+        for (int32_t i = acc; i < mine; i += kAccs) {
+            const int slot = i % kSlots;
+            if (!__all_sync(0xffffffffu, wait(b_lse + 8 * slot, (i / kSlots) & 1) && wait(b_s + 8 * acc, (i / kAccs) & 1))) break;
             tc_fence_after();
             const int64_t p0 = (int64_t)(tile0 + rank + share * i) * per;
             const int32_t a = (int32_t)max((int64_t)0, min((int64_t)128, see.first - p0));
             const int32_t b = live ? (int32_t)max((int64_t)0, min((int64_t)128, see.end - p0)) : 0;
             const bool edge = __any_sync(0xffffffffu, a > 0 || b < per);
-            const float4* lse = reinterpret_cast<const float4*>(mem + P::lse) + stage * 32;
+            const float4* lse = reinterpret_cast<const float4*>(mem + P::lse) + slot * 32;
             float x0 = 0.0f, x1 = 0.0f;
             uint32_t sr[2][32];
             tmem_ld32(sr[0], tmem + 128 * acc + lanes);
@@ -319,17 +329,17 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
             }
             sum += x0 + x1;
             __syncwarp();
-            if (lane == 0) mbar_arrive(b_free + 8 * stage);      // lse of this stage is read
+            if (lane == 0) mbar_arrive(b_read + 8 * slot);
         }
         reinterpret_cast<float*>(mem + P::sums)[threadIdx.x] = sum;
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 8) tmem_dealloc(tmem, 128 * kAccs);
+    if (warp == 16) tmem_dealloc(tmem, 128 * kAccs);
     const float* sums = reinterpret_cast<const float*>(mem + P::sums);
     if (share == 1) {
-        if (threadIdx.x < 128 && t0 + t < q.T) add_weight(j, r, h, t0 + t, sums[t] + sums[128 + t]);
+        if (threadIdx.x < 128 && t0 + t < q.T) add_weight(j, r, h, t0 + t, (sums[t] + sums[128 + t]) + (sums[256 + t] + sums[384 + t]));
         return;
     }
     asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
@@ -337,11 +347,12 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         float x = 0.0f;
         for (int32_t k = 0; k < share; ++k) {
             uint32_t at;
-            float u, v;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(base + P::sums + 4 * t), "r"(k));
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u) : "r"(at) : "memory");
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at + 512) : "memory");
-            x += u + v;
+            for (int e = 0; e < kAccs; ++e) {
+                float u;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u) : "r"(at + 512 * e) : "memory");
+                x += u;
+            }
         }
         add_weight(j, r, h, t0 + t, x);
     }
