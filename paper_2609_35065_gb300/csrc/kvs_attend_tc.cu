@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
     const uint32_t ring = base + 2 * P::tile, ctl = base + P::bars;
     const Bars bar(ctl, P::stages);
     const uint32_t tmem_at = bar.o + 8;
-    const int wg = threadIdx.x >> 7, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_number(), wg = warp >> 2, lane = threadIdx.x & 31;
 
     const int32_t tiles = gridDim.x / j.splits, split = blockIdx.x % j.splits;
     const int32_t r = blockIdx.z, h = blockIdx.y;

@@ -88,6 +88,9 @@ __host__ __device__ constexpr uint32_t tc_idesc(bool half, int n, bool b_mn_majo
 }
 // The operand `bytes` further on.
 __device__ __forceinline__ uint64_t tc_ahead(uint64_t desc, uint32_t bytes) { return desc + (bytes >> 4); }
+// The warp's number, as a value that the compiler knows to be the same in all lanes: what
+// follows from it may then live in uniform registers, where tcgen05.mma takes its operands.
+__device__ __forceinline__ int warp_number() { return __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0); }
 // One lane of a converged warp, the same at every call.
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;

@@ -32,72 +32,75 @@ __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t
 }
 
 // ---------------------------------------------------------------------------
-// Many rows: S^T = K Q^T on the tensor cores, a tile of 128 keys (the accumulator's lanes)
-// per CTA and the rows in tiles of at most 128 (its columns), so that a thread sums its key's
-// weights in registers.  Four warpgroups take the row tiles in turn, from an accumulator each;
-// in the fifth one warp issues the products, one loads the next row tiles (TMA boxes of whole
-// tokens; cp.async by three warps where the rows have no such boxes) and two their lse, in a
-// ring of its own: a tile's rows are done with when the products are, its lse with the sums.
-// Bound by the exponentials, one for each score, and as much by the products.
+// Many rows: S^T = K Q^T on the tensor cores, two tiles of 128 keys (the accumulators' lanes)
+// per CTA and the rows in tiles of at most 128 (their columns), so that a thread sums its key's
+// weights in registers.  The keys stay in tensor memory: read from shared memory for every
+// product they took as much of its 128 bytes a cycle as the rows, and both together all of it.
+// Two warpgroups share a key tile, half of each row tile's columns to each; in the fifth warpgroup one warp issues the products, one
+// loads the next row tiles (TMA boxes of whole tokens; cp.async by three warps where the rows
+// have no such boxes) and two their lse, in a ring of its own: a tile's rows are done with when
+// the products are, its lse with the sums.  Bound by the products (about 570 cycles for 128 x
+// 128 scores) and nearly as much by the exponentials (512).
 //
 // Where there are fewer key tiles than SMs, a cluster of CTAs shares a key tile's row tiles
 // and joins its sums, in the CTAs' order, through distributed shared memory.
 // ---------------------------------------------------------------------------
-constexpr int kThreads = 640, kStages = 5, kAccs = 4, kSlots = 8;
+constexpr int kThreads = 640, kStages = 6, kAccs = 3, kSlots = 8, kKeysTc = 256;
 
 template <int DP>
 struct WPlan {
     static constexpr int tile = 128 * DP * 2;
-    static constexpr int lse = tile * (1 + kStages);             // [kSlots][128] binary32, times -log2(e)
-    static constexpr int sums = lse + kSlots * 512;              // [kAccs][128]
-    static constexpr int bars = sums + kAccs * 512;
+    static constexpr int lse = tile * kStages;                   // [kSlots][128] binary32, times -log2(e)
+    static constexpr int sums = lse + kSlots * 512;              // [2][2][128]
+    static constexpr int bars = sums + 2048;
     static constexpr int bytes = bars + 512 + 1024;
 };
 
 template <bool HALF, int DP>
-__global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap k_map,
-                                                                   const __grid_constant__ CUtensorMap q_map, int32_t k_boxes, int32_t q_boxes, int32_t share) {
+__global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap q_map, int32_t q_boxes,
+                                                                   int32_t share) {
     extern __shared__ char raw[];
     using P = WPlan<DP>;
     const StepView& st = j.step;
     const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
     char* mem = raw + (base - smem_u32(raw));
-    const uint32_t ring = base + P::tile, ctl = base + P::bars;
+    const uint32_t ring = base, ctl = base + P::bars;
     const uint32_t b_k = ctl, b_full = ctl + 8, b_free = b_full + 8 * kStages, b_s = b_free + 8 * kStages, b_e = b_s + 8 * kAccs, b_done = b_e + 8 * kAccs,
                    b_lse = b_done + 8, b_read = b_lse + 8 * kSlots, tmem_at = b_read + 8 * kSlots;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = threadIdx.x >> 7;
-    const int32_t r = blockIdx.z, h = blockIdx.y, rank = blockIdx.x % share, t0 = (blockIdx.x / share) * 128;
+    const int warp = warp_number(), lane = threadIdx.x & 31, wg = warp >> 2;
+    const int32_t r = blockIdx.z, h = blockIdx.y, rank = blockIdx.x % share, t0 = (blockIdx.x / share) * kKeysTc;
     const Request q = load_request(st, r);
     if (t0 >= q.T) return;                                       // the whole cluster
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
     const int32_t per = tile_rows_of(st.group);                  // rows of a tile
-    const RowSpan any = rows_seeing(st, q, t0, min(t0 + 127, q.T - 1), j.causal, j.window);
+    const int32_t key_tiles = t0 + 128 < q.T ? 2 : 1;
+    const RowSpan any = rows_seeing(st, q, t0, min(t0 + kKeysTc, q.T) - 1, j.causal, j.window);
     const int32_t tile0 = (int32_t)(any.first / per), tiles = any.end > any.first ? (int32_t)((any.end + per - 1) / per) - tile0 : 0;
     const int32_t mine = (tiles - rank + share - 1) / share;     // row tiles tile0 + rank + share * i
     const int32_t total = q.n * st.group;
 
     if (threadIdx.x == 0) {
-        mbar_init(b_k, 3);
+        mbar_init(b_k, 16);
         for (int i = 0; i < kStages; ++i) {
             mbar_init(b_full + 8 * i, q_boxes ? 1 : 3);          // the loading warps
             mbar_init(b_free + 8 * i, 1);
         }
         for (int i = 0; i < kSlots; ++i) {
             mbar_init(b_lse + 8 * i, q_boxes ? 2 : 3);
-            mbar_init(b_read + 8 * i, 4);                        // a warpgroup's warps
+            mbar_init(b_read + 8 * i, 8 * key_tiles);            // the key tiles' warps
         }
         for (int i = 0; i < kAccs; ++i) {
             mbar_init(b_s + 8 * i, 1);
-            mbar_init(b_e + 8 * i, 4);
+            mbar_init(b_e + 8 * i, 8);
         }
         mbar_init(b_done, 1);
         mbar_init_fence();
     }
-    if (warp == 16) tmem_alloc(tmem_at, 128 * kAccs);
+    if (warp == 16) tmem_alloc(tmem_at, 512);
     // rows that no box fills are zeros for good, and weigh nothing
     for (int i = threadIdx.x; i < (128 - per) * (DP / 8) * kStages; i += kThreads) {
         const int stage = i / ((128 - per) * (DP / 8)), v = i % ((128 - per) * (DP / 8)), row = per + v / (DP / 8), c = v % (DP / 8);
-        *reinterpret_cast<uint4*>(mem + P::tile * (1 + stage) + (c >> 3) * 128 * 128 + row * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(mem + P::tile * stage + (c >> 3) * 128 * 128 + row * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
     }
     fence_async_smem();
     tc_fence_before();
@@ -116,25 +119,28 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
     if (warp == 16) {
         // ---- the products: the warp waits together, one lane issues ----------------------
         constexpr uint32_t id = tc_idesc(HALF, 128, false);
-        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-        const uint64_t k_desc = tc_desc(base, 16, 1024), q_desc = tc_desc(ring, 16, 1024);
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), keys = tm + 128 * kAccs;     // 64 columns to a key tile
+        const uint64_t q_desc = tc_desc(ring, 16, 1024);
         bool ok = mine <= 0 || __all_sync(0xffffffffu, wait(b_k, 0));
         int32_t stage = 0, round = 0;
         for (int32_t i = 0; ok && i < mine; ++i) {
-            const int32_t acc = i % kAccs;
-            ok = __all_sync(0xffffffffu, wait(b_full + 8 * stage, round & 1) && (i < kAccs || wait(b_e + 8 * acc, (i / kAccs - 1) & 1)));
-            if (!ok) break;
-            tc_fence_after();
-            if (elect_one()) {
-                const uint64_t b = tc_ahead(q_desc, stage * P::tile);
+            ok = __all_sync(0xffffffffu, wait(b_full + 8 * stage, round & 1));
+            for (int32_t kt = 0; ok && kt < key_tiles; ++kt) {
+                const int32_t n = i * key_tiles + kt, acc = n % kAccs;
+                ok = __all_sync(0xffffffffu, n < kAccs || wait(b_e + 8 * acc, (n / kAccs - 1) & 1));
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t b = tc_ahead(q_desc, stage * P::tile);
 #pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const uint32_t off = (k >> 2) * 128 * 128 + (k & 3) * 32;
-                    tc_mma_ss(tm + 128 * acc, tc_ahead(k_desc, off), tc_ahead(b, off), id, k > 0);
+                    for (int k = 0; k < DP / 16; ++k)
+                        tc_mma_ts(tm + 128 * acc, keys + 64 * kt + 8 * k, tc_ahead(b, (k >> 2) * 128 * 128 + (k & 3) * 32), id, k > 0);
+                    tc_commit(b_s + 8 * acc);
+                    if (kt + 1 == key_tiles) tc_commit(b_free + 8 * stage);
                 }
-                tc_commit(b_free + 8 * stage);
-                tc_commit(b_s + 8 * acc);
+                __syncwarp();
             }
+            if (!ok) break;
             __syncwarp();
             if (++stage == kStages) {
                 stage = 0;
@@ -157,15 +163,6 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
             if (lane == 0) mbar_arrive(pending);
             pending = 0;
         };
-        if (mine > 0) {
-            if (k_boxes) {
-                tile_boxes<DP>(base, &k_map, st, h, box_of<DP, 3>(st, table, t0, q.T, warp - 17, lane), b_k, lane);
-            } else {
-                tile_rows<DP, 96>(base, j.k_plane, st, table, h, t0, 0, q.T, u);
-                cp_commit();
-                pending = b_k;
-            }
-        }
         // lse of the rows u and u + 96 (by boxes: of u - 32 and u + 32, by two warps) of tile i
         const int a0 = q_boxes ? u - 32 : u, a1 = q_boxes ? u + 32 : u + 96;
         auto lse_of = [&](int32_t i, int row) {
@@ -200,10 +197,6 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         };
         if (q_boxes && warp > 17) {
             // four tiles' lse ahead of the four that are announced: a load takes longer than a tile
-            if (pending) {
-                cp_wait<0>();
-                announce();
-            }
             float now[4][2], next[4][2];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -230,10 +223,6 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
                 }
             }
         } else if (q_boxes) {
-            if (pending) {
-                cp_wait<0>();
-                announce();
-            }
             for (; i < mine; ++i) {
                 if (!stage_free(stage, round)) break;
                 if (lane == 0) {
@@ -277,41 +266,62 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         cp_wait<0>();
         if (pending) announce();
         // every load has landed when its sums are done; after a failure, wait for them here
-        if (mine > 0) mbar_wait(b_k, 0, kWaitLimitNs);
         if (i < mine && warp == 17)
             for (int k = i < kStages ? 0 : i - kStages; k < i; ++k) mbar_wait(b_full + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs);
     } else {
         // ---- sums: a key to a thread ---------------------------------------------------
+        const int kt = wg >> 1, half = wg & 1;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        const bool live = t0 + t < q.T;
-        const RowSpan see = rows_seeing(st, q, t0 + t, t0 + t, j.causal, j.window);
+        const int32_t key = t0 + 128 * kt + t;
+        const bool live = key < q.T;
+        const RowSpan see = rows_seeing(st, q, key, key, j.causal, j.window);
         const float c = j.scale_log2;
-        const int acc = wg;
-        for (int32_t i = acc; i < mine; i += kAccs) {
-            const int slot = i % kSlots;
-            if (!__all_sync(0xffffffffu, wait(b_lse + 8 * slot, (i / kSlots) & 1) && wait(b_s + 8 * acc, (i / kAccs) & 1))) break;
-            tc_fence_after();
-            const int64_t p0 = (int64_t)(tile0 + rank + share * i) * per;
-            const int32_t a = (int32_t)max((int64_t)0, min((int64_t)128, see.first - p0));
-            const int32_t b = live ? (int32_t)max((int64_t)0, min((int64_t)128, see.end - p0)) : 0;
-            const bool edge = __any_sync(0xffffffffu, a > 0 || b < per);
-            const float4* lse = reinterpret_cast<const float4*>(mem + P::lse) + slot * 32;
-            float x0 = 0.0f, x1 = 0.0f;
-            uint32_t sr[2][32];
-            tmem_ld32(sr[0], tmem + 128 * acc + lanes);
+        if (kt < key_tiles) {
+            // this thread's key, DP / 2 of its dims, into tensor memory: lane = key, two dims to a column
+            const int64_t row = live ? row_of(st, table, key) : -1;
+            uint32_t w[DP / 4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int v = 0; v < DP / 16; ++v) {
+                const int32_t d = DP / 2 * half + 8 * v;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (row >= 0 && d < st.head_dim) x = *reinterpret_cast<const uint4*>(j.k_plane + 2 * (row + (int64_t)h * st.head_dim + d));
+                w[4 * v] = x.x;
+                w[4 * v + 1] = x.y;
+                w[4 * v + 2] = x.z;
+                w[4 * v + 3] = x.w;
+            }
+            const uint32_t to = tmem + 128 * kAccs + lanes + 64 * kt + DP / 4 * half;
+            if (DP == 128) tmem_st32(to, w);
+            else tmem_st16(to, w);
+            tmem_wait_st();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_k);
+        for (int32_t i = kt < key_tiles ? 0 : mine; i < mine; ++i) {
+            const int32_t n = i * key_tiles + kt;
+            const int slot = i % kSlots, acc = n % kAccs;
+            if (!__all_sync(0xffffffffu, wait(b_lse + 8 * slot, (i / kSlots) & 1) && wait(b_s + 8 * acc, (n / kAccs) & 1))) break;
+            tc_fence_after();
+            const int64_t p0 = (int64_t)(tile0 + rank + share * i) * per + 64 * half;
+            const int32_t a = (int32_t)max((int64_t)0, min((int64_t)64, see.first - p0));
+            const int32_t b = live ? (int32_t)max((int64_t)0, min((int64_t)64, see.end - p0)) : 0;
+            const bool edge = __any_sync(0xffffffffu, a > 0 || b < min(64, per - 64 * half));
+            const float4* lse = reinterpret_cast<const float4*>(mem + P::lse) + slot * 32 + 16 * half;
+            float x0 = 0.0f, x1 = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                uint32_t sr[32];
+                tmem_ld32(sr, tmem + 128 * acc + lanes + 64 * half + 32 * k);
                 tmem_wait_ld();
-                tmem_loaded32(sr[k & 1]);
-                if (k < 3) {
-                    tmem_ld32(sr[(k + 1) & 1], tmem + 128 * acc + lanes + 32 * (k + 1));
-                } else {
+                tmem_loaded32(sr);
+                if (k == 1) {
                     // the accumulator is read
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(b_e + 8 * acc);
                 }
-                float* s = reinterpret_cast<float*>(sr[k & 1]);
+                float* s = reinterpret_cast<float*>(sr);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float4 z = lse[8 * k + e];
@@ -336,25 +346,27 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 16) tmem_dealloc(tmem, 128 * kAccs);
-    const float* sums = reinterpret_cast<const float*>(mem + P::sums);
+    if (warp == 16) tmem_dealloc(tmem, 512);
+    const float* sums = reinterpret_cast<const float*>(mem + P::sums);        // [key tile][half][128]
+    const int32_t at_sum = (threadIdx.x >> 7) * 256 + t;
+    const int32_t key = t0 + (int32_t)threadIdx.x;               // of the first 256 threads: key tile by key tile
+    const bool mine_to_write = threadIdx.x < kKeysTc && key < q.T;
     if (share == 1) {
-        if (threadIdx.x < 128 && t0 + t < q.T) add_weight(j, r, h, t0 + t, (sums[t] + sums[128 + t]) + (sums[256 + t] + sums[384 + t]));
+        if (mine_to_write) add_weight(j, r, h, key, sums[at_sum] + sums[at_sum + 128]);
         return;
     }
     asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-    if (rank == 0 && threadIdx.x < 128 && t0 + t < q.T) {
+    if (rank == 0 && mine_to_write) {
         float x = 0.0f;
         for (int32_t k = 0; k < share; ++k) {
             uint32_t at;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(base + P::sums + 4 * t), "r"(k));
-            for (int e = 0; e < kAccs; ++e) {
-                float u;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u) : "r"(at + 512 * e) : "memory");
-                x += u;
-            }
+            float u, v;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(base + P::sums + 4 * at_sum), "r"(k));
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u) : "r"(at) : "memory");
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at + 512) : "memory");
+            x += u + v;
         }
-        add_weight(j, r, h, t0 + t, x);
+        add_weight(j, r, h, key, x);
     }
     asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
@@ -524,9 +536,9 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     auto* k = kvs_weigh_tc_kernel<HALF, DP>;
     cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, WPlan<DP>::bytes);
     if (e != cudaSuccess) return e;
-    CUtensorMap km{}, qm{};
-    const bool k_boxes = plane_map(&km, st, j.k_plane, HALF), q_boxes = rows_map(&qm, st, j.q, HALF);
-    const int64_t x = (st.max_kv + 127) / 128, tiles = x * st.kv_heads * st.requests, row_tiles = (rows + 127) / 128;
+    CUtensorMap qm{};
+    const bool q_boxes = rows_map(&qm, st, j.q, HALF);
+    const int64_t x = (st.max_kv + kKeysTc - 1) / kKeysTc, tiles = x * st.kv_heads * st.requests, row_tiles = (rows + 127) / 128;
     int share = 1;
     while (share < 8 && tiles * share * 2 <= sms && share * 2 <= row_tiles) share *= 2;
     cudaLaunchConfig_t cfg{};
@@ -540,7 +552,7 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = share > 1;
-    return cudaLaunchKernelEx(&cfg, k, j, km, qm, (int32_t)k_boxes, (int32_t)q_boxes, (int32_t)share);
+    return cudaLaunchKernelEx(&cfg, k, j, qm, (int32_t)q_boxes, (int32_t)share);
 }
 
 }  // namespace
