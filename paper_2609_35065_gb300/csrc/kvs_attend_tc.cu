@@ -214,17 +214,18 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                     stage = 0;
                     ++round;
                 }
-                // V of this step and K of the next were loaded long ago; P is what is waited for
-                ok = __all_sync(0xffffffffu, filled(vs, vr) && (!more || filled(ks, kr)) && wait(bar.p, k & 1));
-                if (!ok) break;
+                // V of this step and K of the next were loaded long ago; P is what is waited for.  A wait
+                // that ran out ends the loop at the next vote.
+                ok = filled(vs, vr) && (!more || filled(ks, kr));
+                ok = wait(bar.p, k & 1) && ok;
+                __syncwarp();
                 tc_fence_after();
                 if (elect_one()) {
                     issue_o(0, vs, k > 0);
                     if (more) issue_s(0, ks);
                 }
+                ok = wait(bar.p + 8, k & 1) && ok;
                 __syncwarp();
-                ok = __all_sync(0xffffffffu, wait(bar.p + 8, k & 1));
-                if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
                     issue_o(1, vs, k > 0);
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                         tc_commit(bar.free + 8 * ks);
                     }
                 }
-                __syncwarp();
+                ok = __all_sync(0xffffffffu, ok);
             }
             if (elect_one()) {
                 tc_commit(bar.o);

@@ -122,26 +122,28 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), keys = tm + 128 * kAccs;     // 64 columns to a key tile
         const uint64_t q_desc = tc_desc(ring, 16, 1024);
         bool ok = mine <= 0 || __all_sync(0xffffffffu, wait(b_k, 0));
-        int32_t stage = 0, round = 0;
+        int32_t stage = 0, round = 0, acc = 0, uses = 0;         // of the next row tile; of the next product
+        // A wait that ran out ends the loop at the next vote: what is issued meanwhile works on whatever is there.
         for (int32_t i = 0; ok && i < mine; ++i) {
-            ok = __all_sync(0xffffffffu, wait(b_full + 8 * stage, round & 1));
-            for (int32_t kt = 0; ok && kt < key_tiles; ++kt) {
-                const int32_t n = i * key_tiles + kt, acc = n % kAccs;
-                ok = __all_sync(0xffffffffu, n < kAccs || wait(b_e + 8 * acc, (n / kAccs - 1) & 1));
-                if (!ok) break;
+            ok = wait(b_full + 8 * stage, round & 1);
+            const uint64_t b = tc_ahead(q_desc, stage * P::tile);
+            for (int32_t kt = 0; kt < key_tiles; ++kt) {
+                if (uses > 0) ok = wait(b_e + 8 * acc, (uses - 1) & 1) && ok;
+                __syncwarp();
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint64_t b = tc_ahead(q_desc, stage * P::tile);
 #pragma unroll
                     for (int k = 0; k < DP / 16; ++k)
                         tc_mma_ts(tm + 128 * acc, keys + 64 * kt + 8 * k, tc_ahead(b, (k >> 2) * 128 * 128 + (k & 3) * 32), id, k > 0);
                     tc_commit(b_s + 8 * acc);
                     if (kt + 1 == key_tiles) tc_commit(b_free + 8 * stage);
                 }
-                __syncwarp();
+                if (++acc == kAccs) {
+                    acc = 0;
+                    ++uses;
+                }
             }
-            if (!ok) break;
-            __syncwarp();
+            ok = __all_sync(0xffffffffu, ok);
             if (++stage == kStages) {
                 stage = 0;
                 ++round;
