@@ -11,19 +11,17 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Packed rows [first, end) that see cached token t (all of them do between); and of a whole
-// tile of keys, the rows that see any.
+// Packed rows [first, end) that see any of the cached tokens t_lo .. t_hi (all of them do
+// between, of one token).  Their number is below 2^30.
 struct RowSpan {
-    int64_t first, end;
+    int32_t first, end;
 };
 __device__ __forceinline__ RowSpan rows_seeing(const StepView& st, const Request& q, int32_t t_lo, int32_t t_hi, int32_t causal, int32_t window) {
     const int64_t base = q.T - q.n;                              // position of new token 0
-    RowSpan s{0, q.n};
-    if (causal) s.first = max((int64_t)0, t_lo - base);
-    if (window > 0) s.end = min((int64_t)q.n, t_hi + window - base);
-    s.first *= st.group;
-    s.end = max(s.first, s.end * st.group);
-    return s;
+    int64_t first = 0, end = q.n;
+    if (causal) first = min(end, max((int64_t)0, t_lo - base));
+    if (window > 0) end = min(end, t_hi + window - base);
+    return RowSpan{(int32_t)first * st.group, (int32_t)max(first, end) * st.group};
 }
 
 __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t h, int32_t t, float sum) {
@@ -45,28 +43,28 @@ __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t
 // Where there are fewer key tiles than SMs, a cluster of CTAs shares a key tile's row tiles
 // and joins its sums, in the CTAs' order, through distributed shared memory.
 // ---------------------------------------------------------------------------
-constexpr int kThreads = 640, kStages = 6, kAccs = 3, kSlots = 8, kKeysTc = 256;
+constexpr int kThreads = 640, kStages = 4, kAccs = 3, kSlots = 8, kKeysTc = 256;
 
 template <int DP>
 struct WPlan {
     static constexpr int tile = 128 * DP * 2;
-    static constexpr int lse = tile * kStages;                   // [kSlots][128] binary32, times -log2(e)
+    static constexpr int lse = tile * (2 + kStages);             // [kSlots][128] binary32, times -log2(e)
     static constexpr int sums = lse + kSlots * 512;              // [2][2][128]
     static constexpr int bars = sums + 2048;
     static constexpr int bytes = bars + 512 + 1024;
 };
 
 template <bool HALF, int DP>
-__global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap q_map, int32_t q_boxes,
-                                                                   int32_t share) {
+__global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap k_map,
+                                                                   const __grid_constant__ CUtensorMap q_map, int32_t k_boxes, int32_t q_boxes, int32_t share) {
     extern __shared__ char raw[];
     using P = WPlan<DP>;
     const StepView& st = j.step;
     const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
     char* mem = raw + (base - smem_u32(raw));
-    const uint32_t ring = base, ctl = base + P::bars;
+    const uint32_t ring = base + 2 * P::tile, ctl = base + P::bars;
     const uint32_t b_k = ctl, b_full = ctl + 8, b_free = b_full + 8 * kStages, b_s = b_free + 8 * kStages, b_e = b_s + 8 * kAccs, b_done = b_e + 8 * kAccs,
-                   b_lse = b_done + 8, b_read = b_lse + 8 * kSlots, tmem_at = b_read + 8 * kSlots;
+                   b_load = b_done + 8, b_lse = b_load + 8, b_read = b_lse + 8 * kSlots, tmem_at = b_read + 8 * kSlots;
     const int warp = warp_number(), lane = threadIdx.x & 31, wg = warp >> 2;
     const int32_t r = blockIdx.z, h = blockIdx.y, rank = blockIdx.x % share, t0 = (blockIdx.x / share) * kKeysTc;
     const Request q = load_request(st, r);
@@ -75,11 +73,12 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
     const int32_t per = tile_rows_of(st.group);                  // rows of a tile
     const int32_t key_tiles = t0 + 128 < q.T ? 2 : 1;
     const RowSpan any = rows_seeing(st, q, t0, min(t0 + kKeysTc, q.T) - 1, j.causal, j.window);
-    const int32_t tile0 = (int32_t)(any.first / per), tiles = any.end > any.first ? (int32_t)((any.end + per - 1) / per) - tile0 : 0;
+    const int32_t tile0 = any.first / per, tiles = any.end > any.first ? (any.end + per - 1) / per - tile0 : 0;
     const int32_t mine = (tiles - rank + share - 1) / share;     // row tiles tile0 + rank + share * i
     const int32_t total = q.n * st.group;
 
     if (threadIdx.x == 0) {
+        mbar_init(b_load, 3 * key_tiles);
         mbar_init(b_k, 16);
         for (int i = 0; i < kStages; ++i) {
             mbar_init(b_full + 8 * i, q_boxes ? 1 : 3);          // the loading warps
@@ -100,7 +99,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
     // rows that no box fills are zeros for good, and weigh nothing
     for (int i = threadIdx.x; i < (128 - per) * (DP / 8) * kStages; i += kThreads) {
         const int stage = i / ((128 - per) * (DP / 8)), v = i % ((128 - per) * (DP / 8)), row = per + v / (DP / 8), c = v % (DP / 8);
-        *reinterpret_cast<uint4*>(mem + P::tile * stage + (c >> 3) * 128 * 128 + row * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(mem + P::tile * (2 + stage) + (c >> 3) * 128 * 128 + row * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
     }
     fence_async_smem();
     tc_fence_before();
@@ -165,6 +164,19 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
             if (lane == 0) mbar_arrive(pending);
             pending = 0;
         };
+        if (mine > 0) {
+            for (int32_t kt = 0; kt < key_tiles; ++kt) {
+                if (k_boxes) tile_boxes<DP>(base + kt * P::tile, &k_map, st, h, box_of<DP, 3>(st, table, t0 + 128 * kt, q.T, warp - 17, lane), b_load, lane);
+                else tile_rows<DP, 96>(base + kt * P::tile, j.k_plane, st, table, h, t0 + 128 * kt, 0, q.T, u);
+            }
+            if (!k_boxes) {
+                cp_commit();
+                cp_wait<0>();
+                __syncwarp();
+                if (lane == 0)
+                    for (int32_t kt = 0; kt < key_tiles; ++kt) mbar_arrive(b_load);
+            }
+        }
         // lse of the rows u and u + 96 (by boxes: of u - 32 and u + 32, by two warps) of tile i
         const int a0 = q_boxes ? u - 32 : u, a1 = q_boxes ? u + 32 : u + 96;
         auto lse_of = [&](int32_t i, int row) {
@@ -268,6 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         cp_wait<0>();
         if (pending) announce();
         // every load has landed when its sums are done; after a failure, wait for them here
+        if (mine > 0) mbar_wait(b_load, 0, kWaitLimitNs);
         if (i < mine && warp == 17)
             for (int k = i < kStages ? 0 : i - kStages; k < i; ++k) mbar_wait(b_full + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs);
     } else {
@@ -276,17 +289,19 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
         const int32_t key = t0 + 128 * kt + t;
         const bool live = key < q.T;
-        const RowSpan see = rows_seeing(st, q, key, key, j.causal, j.window);
+        RowSpan see = rows_seeing(st, q, key, key, j.causal, j.window);
+        if (!live) see.end = see.first;
         const float c = j.scale_log2;
+        const int32_t columns = min(64, per - 64 * half);
         if (kt < key_tiles) {
             // this thread's key, DP / 2 of its dims, into tensor memory: lane = key, two dims to a column
-            const int64_t row = live ? row_of(st, table, key) : -1;
+            if (mine > 0) wait(b_load, 0);
+            __syncwarp();
             uint32_t w[DP / 4];
 #pragma unroll
             for (int v = 0; v < DP / 16; ++v) {
-                const int32_t d = DP / 2 * half + 8 * v;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (row >= 0 && d < st.head_dim) x = *reinterpret_cast<const uint4*>(j.k_plane + 2 * (row + (int64_t)h * st.head_dim + d));
+                const int d = DP / 16 * half + v;
+                const uint4 x = ld_shared16(base + kt * P::tile + (d >> 3) * 128 * 128 + t * 128 + (((d & 7) ^ (t & 7)) << 4));
                 w[4 * v] = x.x;
                 w[4 * v + 1] = x.y;
                 w[4 * v + 2] = x.z;
@@ -305,10 +320,9 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
             const int slot = i % kSlots, acc = n % kAccs;
             if (!__all_sync(0xffffffffu, wait(b_lse + 8 * slot, (i / kSlots) & 1) && wait(b_s + 8 * acc, (n / kAccs) & 1))) break;
             tc_fence_after();
-            const int64_t p0 = (int64_t)(tile0 + rank + share * i) * per + 64 * half;
-            const int32_t a = (int32_t)max((int64_t)0, min((int64_t)64, see.first - p0));
-            const int32_t b = live ? (int32_t)max((int64_t)0, min((int64_t)64, see.end - p0)) : 0;
-            const bool edge = __any_sync(0xffffffffu, a > 0 || b < min(64, per - 64 * half));
+            const int32_t p0 = (tile0 + rank + share * i) * per + 64 * half;
+            const int32_t a = see.first - p0, b = see.end - p0;      // columns that see this thread's key
+            const bool edge = __any_sync(0xffffffffu, a > 0 || b < columns);
             const float4* lse = reinterpret_cast<const float4*>(mem + P::lse) + slot * 32 + 16 * half;
             float x0 = 0.0f, x1 = 0.0f;
 #pragma unroll
@@ -538,8 +552,8 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     auto* k = kvs_weigh_tc_kernel<HALF, DP>;
     cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, WPlan<DP>::bytes);
     if (e != cudaSuccess) return e;
-    CUtensorMap qm{};
-    const bool q_boxes = rows_map(&qm, st, j.q, HALF);
+    CUtensorMap km{}, qm{};
+    const bool k_boxes = plane_map(&km, st, j.k_plane, HALF), q_boxes = rows_map(&qm, st, j.q, HALF);
     const int64_t x = (st.max_kv + kKeysTc - 1) / kKeysTc, tiles = x * st.kv_heads * st.requests, row_tiles = (rows + 127) / 128;
     int share = 1;
     while (share < 8 && tiles * share * 2 <= sms && share * 2 <= row_tiles) share *= 2;
@@ -554,7 +568,7 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = share > 1;
-    return cudaLaunchKernelEx(&cfg, k, j, qm, (int32_t)q_boxes, (int32_t)share);
+    return cudaLaunchKernelEx(&cfg, k, j, km, qm, (int32_t)k_boxes, (int32_t)q_boxes, (int32_t)share);
 }
 
 }  // namespace
