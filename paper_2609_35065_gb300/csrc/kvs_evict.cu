@@ -10,9 +10,10 @@
 namespace kvs {
 namespace {
 
-constexpr int kSelect = 1024;          // threads of a selecting CTA
-constexpr int kOwn = 8;                // consecutive tokens of a thread
+constexpr int kSelect = 256;           // threads of a selecting CTA
+constexpr int kWarps = kSelect / 32;
 constexpr int kBins = 2048;
+constexpr int kCached = 16384;         // weights that a CTA keeps in shared memory
 constexpr int kCopy = 256;
 
 // Unsigned keys in the weights' order; NaN below all, always-kept tokens above all.
@@ -23,8 +24,12 @@ __device__ __forceinline__ uint32_t key_of(float w, int32_t t, int32_t T, const 
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Sum of v over the CTA's earlier threads; `total` gets the CTA's.
-__device__ __forceinline__ uint32_t scan(uint32_t v, uint32_t& total, uint32_t* warp_sums) {
+// The weight of a key, where the key tells it: not of always-kept tokens, NaN and zeros.
+__device__ __forceinline__ bool tells(uint32_t k) { return k != 0xffffffffu && k != 0 && k != 0x80000000u; }
+__device__ __forceinline__ float weight_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+
+// Sum of v over the CTA's earlier threads (warp_sums: kWarps).
+__device__ __forceinline__ uint32_t scan(uint32_t v, uint32_t* warp_sums) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t x = v;
 #pragma unroll
@@ -32,27 +37,27 @@ __device__ __forceinline__ uint32_t scan(uint32_t v, uint32_t& total, uint32_t* 
         const uint32_t y = __shfl_up_sync(0xffffffffu, x, d);
         if (lane >= d) x += y;
     }
-    __syncthreads();                                             // the sums of the scan before are read
     if (lane == 31) warp_sums[warp] = x;
     __syncthreads();
-    uint32_t s = warp_sums[lane];                                // 32 warps
+    uint32_t before = 0;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xffffffffu, s, d);
-        if (lane >= d) s += y;
-    }
-    total = __shfl_sync(0xffffffffu, s, 31);
-    const uint32_t before = __shfl_sync(0xffffffffu, s, warp ? warp - 1 : 0);
-    return (warp ? before : 0) + x - v;
+    for (int w = 0; w < kWarps; ++w) before += w < warp ? warp_sums[w] : 0;
+    return before + x - v;
 }
 
-// One CTA per (head, request, layer).  A cache of up to 8192 tokens stays in registers, eight
-// consecutive ones to a thread; a longer one is read again, from L2, by each pass.
+// One CTA per (head, request, layer), whose warps own a stretch of consecutive tokens each:
+// only the digits' counts and the warps' own are shared, so that a pass has few barriers.  Up
+// to 16384 keys stay in shared memory; of a longer cache each pass makes them again, from L2.
+// Bound by its instructions (some 60 per token and lane) and its chain of passes; several CTAs
+// to an SM overlap theirs.
+template <bool CACHED>
 __global__ void __launch_bounds__(kSelect) kvs_evict_select_kernel(EvictJob j) {
-    __shared__ uint32_t hist[kBins], warp_sums[32], found[2];
+    extern __shared__ __align__(16) uint32_t cache[];
+    __shared__ __align__(16) uint32_t hist[kBins];
+    __shared__ uint32_t sums[2][kWarps], found[3];
     const StepView& st = j.step;
     const int32_t h = blockIdx.x, r = blockIdx.y, l = blockIdx.z;
-    grid_trigger();                                              // the copy may come and wait
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int32_t T = __ldg(st.kv_lens + r);
     if (T < 0 || T > st.max_kv) {
         if (threadIdx.x == 0) record_error(st.err, KVS_ERR_BOUNDS);
@@ -64,86 +69,132 @@ __global__ void __launch_bounds__(kSelect) kvs_evict_select_kernel(EvictJob j) {
     const int64_t row = (((int64_t)l * st.requests + r) * st.kv_heads + h) * j.budget;
     int32_t* kept = j.kept + row;
     float* nw = j.new_weights ? j.new_weights + row : nullptr;
-
-    const int32_t chunk = kSelect * kOwn, chunks = (T + chunk - 1) / chunk;
-    float x[kOwn];
-    auto load = [&](int32_t n) {
-        const int32_t t0 = n * chunk + threadIdx.x * kOwn;
-#pragma unroll
-        for (int e = 0; e < kOwn; ++e) x[e] = t0 + e < T ? w[t0 + e] : 0.0f;
-    };
-    if (chunks > 0) load(0);
-
-    const bool all = T <= J;
-    uint32_t limit = 0, equal = 0;                               // keep keys above limit, and `equal` of those at it
-    if (!all) {
-        uint32_t mask = 0, need = J;
-#pragma unroll
-        for (int digit = 0; digit < 3; ++digit) {
-            const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? 1024 : kBins;
-            hist[threadIdx.x] = hist[threadIdx.x + kSelect] = 0;
-            __syncthreads();
-            for (int32_t n = 0; n < chunks; ++n) {
-                if (chunks > 1) load(n);
-                const int32_t t0 = n * chunk + threadIdx.x * kOwn;
-#pragma unroll
-                for (int e = 0; e < kOwn; ++e) {
-                    const uint32_t k = key_of(x[e], t0 + e, T, j);
-                    if (t0 + e < T && (k & mask) == limit) atomicAdd(&hist[k >> shift & (bins - 1)], 1u);
-                }
-            }
-            __syncthreads();
-            // the bin, from the top, in which the count reaches what is needed: two bins to a thread
-            const int b = kBins - 1 - 2 * (int)threadIdx.x;
-            const uint32_t hi = hist[b], lo = hist[b - 1];
-            uint32_t total;
-            const uint32_t before = scan(hi + lo, total, warp_sums);
-            if (before < need && need <= before + hi + lo) {
-                const bool first = need <= before + hi;
-                found[0] = first ? b : b - 1;
-                found[1] = need - before - (first ? 0 : hi);
-            }
-            __syncthreads();
-            limit |= found[0] << shift;
-            mask |= (uint32_t)(bins - 1) << shift;
-            need = found[1];
-            __syncthreads();
-        }
-        equal = need;
-    }
-    uint32_t above = 0, at = 0;                                  // of the chunks before
-    for (int32_t n = 0; n < chunks; ++n) {
-        if (chunks > 1) load(n);
-        const int32_t t0 = n * chunk + threadIdx.x * kOwn;
-        uint32_t gt = 0, eq = 0;                                 // bit e: token t0 + e
-#pragma unroll
-        for (int e = 0; e < kOwn; ++e) {
-            if (t0 + e < T) {
-                const uint32_t k = key_of(x[e], t0 + e, T, j);
-                if (all || k > limit) gt |= 1u << e;
-                else if (k == limit) eq |= 1u << e;
-            }
-        }
-        uint32_t total;
-        const uint32_t before = scan(__popc(gt) | __popc(eq) << 16, total, warp_sums);
-        uint32_t g = above + (before & 0xffffu), q = at + (before >> 16);
-#pragma unroll
-        for (int e = 0; e < kOwn; ++e) {
-            const bool is_eq = eq >> e & 1;
-            if ((gt >> e & 1) || (is_eq && q < equal)) {
-                const uint32_t p = g + min(q, equal);
-                kept[p] = t0 + e;
-                if (nw) nw[p] = x[e];
-            }
-            g += gt >> e & 1;
-            q += is_eq;
-        }
-        above += total & 0xffffu;
-        at += total >> 16;
-    }
     for (int32_t p = J + threadIdx.x; p < j.budget; p += kSelect) {
         kept[p] = -1;
         if (nw) nw[p] = 0.0f;
+    }
+    if (T <= J) {
+        for (int32_t t = threadIdx.x; t < T; t += kSelect) {
+            kept[t] = t;
+            if (nw) nw[t] = w[t];
+        }
+        return;
+    }
+
+    // Stretches of whole groups of 128 tokens, four to a lane.  What lies beyond T has the lowest
+    // key and comes last: it is never among the J < T that are kept.
+    const int32_t groups = (T + 127) / 128, per_warp = (groups + kWarps - 1) / kWarps;
+    const int32_t t_lo = min(groups, warp * per_warp) * 128 + 4 * lane, t_hi = min(groups, (warp + 1) * per_warp) * 128;
+    auto make = [&](int32_t t) { return t < T ? key_of(w[t], t, T, j) : 0u; };
+    auto keys = [&](int32_t t) {
+        return CACHED ? *reinterpret_cast<const uint4*>(cache + t) : make_uint4(make(t), make(t + 1), make(t + 2), make(t + 3));
+    };
+    if (CACHED) {
+#pragma unroll 16
+        for (int32_t t = t_lo - 3 * lane; t < t_hi; t += 32) cache[t] = make(t);
+        __syncwarp();
+    }
+    uint32_t limit = 0, mask = 0, need = J;                      // keep keys above limit in the mask's bits, and `need` of those at it
+#pragma unroll
+    for (int digit = 0; digit < 3; ++digit) {
+        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? 1024 : kBins;
+#pragma unroll
+        for (int b = 0; b < kBins; b += kSelect) hist[b + threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll 2
+        for (int32_t t = t_lo; t < t_hi; t += 128) {
+            const uint4 k = keys(t);
+            auto count = [&](uint32_t x) {
+                if ((x & mask) == limit) atomicAdd(&hist[x >> shift & (bins - 1)], 1u);
+            };
+            count(k.x);
+            count(k.y);
+            count(k.z);
+            count(k.w);
+        }
+        __syncthreads();
+        // the bin, from the top, in which the count reaches what is needed: eight bins to a thread
+        const int top = kBins - 1 - 8 * (int)threadIdx.x;
+        const uint4 hi = *reinterpret_cast<const uint4*>(hist + top - 3), lo = *reinterpret_cast<const uint4*>(hist + top - 7);
+        const uint32_t bin[8] = {hi.w, hi.z, hi.y, hi.x, lo.w, lo.z, lo.y, lo.x};
+        uint32_t sum = 0;
+#pragma unroll
+        for (int b = 0; b < 8; ++b) sum += bin[b];
+        uint32_t before = scan(sum, sums[digit & 1]);
+        if (before < need && need <= before + sum) {
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                if (before < need && need <= before + bin[b]) {
+                    found[0] = top - b;
+                    found[1] = need - before;
+                    found[2] = bin[b];
+                }
+                before += bin[b];
+            }
+        }
+        __syncthreads();
+        limit |= found[0] << shift;
+        mask |= (uint32_t)(bins - 1) << shift;
+        need = found[1];
+        if (need == found[2]) break;                             // the whole bin is kept: its order does not matter
+    }
+    __syncthreads();
+    // how many of each warp's are above and at the limit, then where each goes
+    auto classify = [&](const uint4& k, uint32_t (&gt)[4], uint32_t (&eq)[4]) {
+        const uint32_t x[4] = {k.x & mask, k.y & mask, k.z & mask, k.w & mask};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            gt[e] = x[e] > limit;
+            eq[e] = x[e] == limit;
+        }
+    };
+    uint32_t n_gt = 0, n_eq = 0;
+    for (int32_t t = t_lo; t < t_hi; t += 128) {
+        uint32_t gt[4], eq[4];
+        classify(keys(t), gt, eq);
+        n_gt += gt[0] + gt[1] + gt[2] + gt[3];
+        n_eq += eq[0] + eq[1] + eq[2] + eq[3];
+    }
+    n_gt = __reduce_add_sync(0xffffffffu, n_gt);
+    n_eq = __reduce_add_sync(0xffffffffu, n_eq);
+    if (lane == 0) {
+        sums[0][warp] = n_gt;
+        sums[1][warp] = n_eq;
+    }
+    __syncthreads();
+    uint32_t g = 0, q = 0;
+#pragma unroll
+    for (int n = 0; n < kWarps; ++n) {
+        g += n < warp ? sums[0][n] : 0;
+        q += n < warp ? sums[1][n] : 0;
+    }
+    for (int32_t t = t_lo; t < t_hi; t += 128) {
+        uint32_t gt[4], eq[4];
+        const uint4 k = keys(t);
+        const uint32_t key[4] = {k.x, k.y, k.z, k.w};
+        classify(k, gt, eq);
+        const uint32_t both = (gt[0] + gt[1] + gt[2] + gt[3]) | (eq[0] + eq[1] + eq[2] + eq[3]) << 16;
+        uint32_t x = both;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t y = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += y;
+        }
+        const uint32_t total = __shfl_sync(0xffffffffu, x, 31);
+        x -= both;
+        uint32_t my_g = g + (x & 0xffffu), my_q = q + (x >> 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (gt[e] || (eq[e] && my_q < need)) {
+                const uint32_t p = my_g + min(my_q, need);
+                kept[p] = t + e;
+                if (nw) nw[p] = tells(key[e]) ? weight_of(key[e]) : w[t + e];
+            }
+            my_g += gt[e];
+            my_q += eq[e];
+        }
+        g += total & 0xffffu;
+        q += total >> 16;
     }
 }
 
@@ -209,8 +260,15 @@ __global__ void __launch_bounds__(kCopy) kvs_evict_copy_kernel(EvictJob j, const
 
 int launch_evict(const EvictJob& j, cudaStream_t s) {
     const StepView& st = j.step;
-    kvs_evict_select_kernel<<<dim3(st.kv_heads, st.requests, j.layers), kSelect, 0, s>>>(j);
-    cudaError_t e = cudaGetLastError();
+    const dim3 units(st.kv_heads, st.requests, j.layers);
+    cudaError_t e = cudaSuccess;
+    if (st.max_kv <= kCached) {
+        e = cudaFuncSetAttribute(kvs_evict_select_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kCached * 4);
+        if (e == cudaSuccess) kvs_evict_select_kernel<true><<<units, kSelect, (st.max_kv + 127) / 128 * 512, s>>>(j);
+    } else {
+        kvs_evict_select_kernel<false><<<units, kSelect, 0, s>>>(j);
+    }
+    if (e == cudaSuccess) e = cudaGetLastError();
     if (e != cudaSuccess) return -(int)e;
     int n = 1;
     const int64_t rows = st.max_kv < j.budget ? st.max_kv : j.budget;
