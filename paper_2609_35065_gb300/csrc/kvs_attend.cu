@@ -378,21 +378,14 @@ cudaError_t attend_few(const AttendJob& j, cudaStream_t s) {
 
 AttendPlan attend_plan(const StepView& st, int sms) {
     const int64_t rows = (int64_t)st.max_q * st.group, units = (int64_t)st.kv_heads * st.requests;
-    AttendPlan p{rows > 64, 1, 1};
-    int64_t tiles, steps, start;
-    if (p.tc) {
-        // One CTA of two row tiles to an SM; steps of 128 keys, and about four of start and end.
-        const int64_t pair = 2 * tile_rows_of(st.group);
-        tiles = (rows + pair - 1) / pair * units;
-        steps = (st.max_kv + 127) / 128;
-        start = 4;
-    } else {
-        // One CTA of 16, 32 or (narrow heads) 64 rows to an SM; steps of 128 keys, too.
-        p.row_tiles = rows <= 16 ? 1 : rows <= 32 || st.head_dim > 64 ? 2 : 4;
-        tiles = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles) * units;
-        steps = (st.max_kv + 127) / 128;
-        start = 4;
-    }
+    // Up to 16 rows: mma.sync, whose work is in the shadow of the loads; above, the tensor cores (at
+    // 20 rows over 3000 to 8000 tokens 62 to 79 us against 65 to 91, at 48 rows 62 to 80 against 97 to 169).
+    AttendPlan p{rows > 16, 1, 1};
+    const int32_t tile = tile_rows_of(st.group);
+    if (p.tc && rows > tile) p.row_tiles = 2;
+    // One CTA to an SM (two of one narrow tile); steps of 128 keys, and about four of start and end.
+    const int64_t per = p.tc ? (int64_t)tile * p.row_tiles : 16, tiles = (rows + per - 1) / per * units, steps = (st.max_kv + 127) / 128, start = 4;
+    if (p.tc && p.row_tiles == 1 && st.head_dim <= 64) sms *= 2;
     // As many parts as keep the number of waves times a part's steps lowest.
     int64_t best = -1;
     for (int64_t n = 1; n <= 256 && n <= (steps + 1) / 2; ++n) {

@@ -1,7 +1,7 @@
 // kvs_attend_tc.cu -- attention of many packed rows: the products on the tensor cores.
 //
 // A CTA holds up to 256 packed rows (row = token * group + head) of one KV head as two tiles of
-// whole tokens and goes over the keys 128 at a time:
+// whole tokens (or one, where a request has no more) and goes over the keys 128 at a time:
 //
 //     S = Q K^T  (tensor memory)  ->  P = 2^(c S - c m)  (registers, back over S)  ->  O += P V
 //
@@ -28,16 +28,19 @@ namespace kvs {
 namespace {
 
 constexpr int kM = 128, kN = 128;                  // rows of a tile, keys of a step
-constexpr int kThreads = 640, kLoaders = 3;
+constexpr int kLoaders = 3;
 constexpr float kNone = -INFINITY;
 
-template <int DP>
+template <int DP, int TILES>
 struct Plan {
+    static constexpr int threads = 256 * TILES + 128;
     static constexpr int tile = kN * DP * 2;       // bytes of a tile of Q, K or V
-    static constexpr int stages = DP == 128 ? 5 : 8;
-    static constexpr int bars = 2 * kM * DP * 2 + stages * tile;
-    static constexpr int tops = bars + 256;        // [256] binary32: maxima, sums that a row's threads exchange
-    static constexpr int bytes = tops + 2048;
+    static constexpr int stages = DP == 128 ? 5 : TILES == 2 ? 8 : 5;
+    static constexpr int ctas = DP == 64 && TILES == 1 ? 2 : 1;       // to an SM
+    static constexpr int columns = 256 * TILES;    // of tensor memory: S of each tile, then O
+    static constexpr int bars = (TILES + stages) * tile;
+    static constexpr int tops = bars + 256;        // [2][TILES][128] binary32: maxima, sums that a row's threads exchange
+    static constexpr int bytes = tops + 1024 * TILES;
 };
 
 struct Bars {
@@ -45,13 +48,14 @@ struct Bars {
     __device__ Bars(uint32_t at, int stages) : q(at), full(at + 8), free(full + 8 * stages), s(free + 8 * stages), p(s + 16), o(p + 16) {}
 };
 
-template <bool HALF, int DP>
-__global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j, const __grid_constant__ CUtensorMap k_map,
+template <bool HALF, int DP, int TILES>
+__global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::ctas) kvs_attend_tc_kernel(AttendJob j, const __grid_constant__ CUtensorMap k_map,
                                                                     const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap q_map,
                                                                     int32_t boxes, int32_t q_boxes) {
     extern __shared__ __align__(1024) char raw[];
     using N = Num<HALF>;
-    using P = Plan<DP>;
+    using P = Plan<DP, TILES>;
+    constexpr int kIssuer = 8 * TILES;               // the issuing warp, behind the softmax's; then the loading ones
     constexpr float kMost = HALF ? 32768.0f : 1048576.0f;            // of a thread's weights of a step
     const StepView& st = j.step;
     const uint32_t base = smem_u32(raw);
@@ -59,7 +63,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
         record_error(st.err, KVS_ERR_UNSUPPORTED);
         return;
     }
-    const uint32_t ring = base + 2 * P::tile, ctl = base + P::bars;
+    const uint32_t ring = base + TILES * P::tile, ctl = base + P::bars;
     const Bars bar(ctl, P::stages);
     const uint32_t tmem_at = bar.o + 8;
     const int warp = warp_number(), wg = warp >> 2, lane = threadIdx.x & 31;
@@ -68,9 +72,9 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
     const int32_t r = blockIdx.z, h = blockIdx.y;
     const int32_t per = tile_rows_of(st.group);
     // The last rows see the most keys: they come first, so that no long CTA starts last.
-    const int32_t row0 = (tiles - 1 - (int32_t)(blockIdx.x / j.splits)) * 2 * per;
+    const int32_t row0 = (tiles - 1 - (int32_t)(blockIdx.x / j.splits)) * TILES * per;
     const Request q = load_request(st, r);
-    const int32_t rows = min(2 * per, q.n * st.group - row0);
+    const int32_t rows = min(TILES * per, q.n * st.group - row0);
     if (rows <= 0) return;
     Span all = seen_by(q, row0 / st.group, (row0 + rows - 1) / st.group, j.causal, j.window);
     const int32_t first = all.lo / kN, steps_all = all.hi > all.lo ? (all.hi + kN - 1) / kN - first : 0;
@@ -79,7 +83,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
 
     if (threadIdx.x == 0) {
-        mbar_init(bar.q, q_boxes ? 1 : 512);
+        mbar_init(bar.q, q_boxes ? 1 : 256 * TILES);
         for (int i = 0; i < P::stages; ++i) {
             mbar_init(bar.full + 8 * i, kLoaders);
             mbar_init(bar.free + 8 * i, 1);
@@ -91,14 +95,14 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
         mbar_init(bar.o, 1);
         mbar_init_fence();
     }
-    if (warp == 16) tmem_alloc(tmem_at, 512);
+    if (warp == kIssuer) tmem_alloc(tmem_at, P::columns);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at) : "memory");
     auto s_at = [&](int t) { return tmem + 128u * t; };
-    auto o_at = [&](int t) { return tmem + 256u + (uint32_t)DP * t; };
+    auto o_at = [&](int t) { return tmem + 128u * TILES + (uint32_t)DP * t; };
 
     // A wait that does not end is recorded; every role then leaves its loop (the others' waits end too).
     auto wait = [&](uint32_t b, uint32_t parity) {
@@ -107,9 +111,9 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
         return false;
     };
 
-    if (warp > 16) {
+    if (warp > kIssuer) {
         // ---- K and V: tile i is K (even) or V (odd) of step i / 2 ------------------
-        const int t = threadIdx.x - 17 * 32, w = warp - 17;
+        const int t = threadIdx.x - 32 * (kIssuer + 1), w = warp - kIssuer - 1;
         int pending = -1;                                    // cp.async tile not yet announced
         auto announce = [&]() {
             fence_async_smem();
@@ -158,16 +162,16 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
         if (i < 2 * steps)
             for (int k = i - P::stages < 0 ? 0 : i - P::stages; k < i; ++k)
                 mbar_wait(bar.full + 8 * (k % P::stages), (k / P::stages) & 1, kWaitLimitNs);
-    } else if (warp == 16) {
+    } else if (warp == kIssuer) {
         if (steps > 0) {
             // ---- the products: the warp waits together, one lane issues ------------------
             // a negative scale's sign goes into the products, so that maxima of S are those of the scores
             const uint32_t id_s = tc_idesc(HALF, kN, false) | (j.scale_log2 < 0.0f ? kNegA : 0u);
             constexpr uint32_t id_o = tc_idesc(HALF, DP, true);
             if (q_boxes && elect_one()) {
-                mbar_expect_tx(bar.q, (uint32_t)per * DP * 4);
+                mbar_expect_tx(bar.q, (uint32_t)per * DP * 2 * TILES);
 #pragma unroll
-                for (int k = 0; k < 2 * (DP / 64); ++k) {
+                for (int k = 0; k < TILES * (DP / 64); ++k) {
                     const int t = k / (DP / 64), c = k % (DP / 64);
                     tma_load_3d(base + t * P::tile + c * kM * 128, &q_map, 64 * c, h * st.group, q.q0 + (row0 + t * per) / st.group, bar.q);
                 }
@@ -188,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                 const uint64_t b = tc_ahead(v_desc, stage * P::tile);
 #pragma unroll
                 for (int k = 0; k < kN / 16; ++k)
-                    tc_mma_ts(tm + 256 + DP * t, tm + 128 * t + 8 * k, tc_ahead(b, k * 2048), id_o, add || k > 0);
+                    tc_mma_ts(tm + 128 * TILES + DP * t, tm + 128 * t + 8 * k, tc_ahead(b, k * 2048), id_o, add || k > 0);
             };
             auto filled = [&](int32_t stage, int32_t round) { return wait(bar.full + 8 * stage, round & 1); };
             bool ok = __all_sync(0xffffffffu, wait(bar.q, 0) && filled(0, 0));
@@ -196,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                 tc_fence_after();
                 if (elect_one()) {
                     issue_s(0, 0);
-                    issue_s(1, 0);
+                    if (TILES == 2) issue_s(1, 0);
                     tc_commit(bar.free);
                 }
                 __syncwarp();
@@ -222,17 +226,21 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
                 tc_fence_after();
                 if (elect_one()) {
                     issue_o(0, vs, k > 0);
+                    if (TILES == 1) tc_commit(bar.free + 8 * vs);
                     if (more) issue_s(0, ks);
+                    if (TILES == 1 && more) tc_commit(bar.free + 8 * ks);
                 }
-                ok = wait(bar.p + 8, k & 1) && ok;
-                __syncwarp();
-                tc_fence_after();
-                if (elect_one()) {
-                    issue_o(1, vs, k > 0);
-                    tc_commit(bar.free + 8 * vs);
-                    if (more) {
-                        issue_s(1, ks);
-                        tc_commit(bar.free + 8 * ks);
+                if (TILES == 2) {
+                    ok = wait(bar.p + 8, k & 1) && ok;
+                    __syncwarp();
+                    tc_fence_after();
+                    if (elect_one()) {
+                        issue_o(1, vs, k > 0);
+                        tc_commit(bar.free + 8 * vs);
+                        if (more) {
+                            issue_s(1, ks);
+                            tc_commit(bar.free + 8 * ks);
+                        }
                     }
                 }
                 ok = __all_sync(0xffffffffu, ok);
@@ -309,9 +317,9 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
 #pragma unroll
                         for (int n = 0; n < 32; n += 2) top = max3(top, s[n], s[n + 1]);
                     }
-                    tops[half * 256 + tl * 128 + t] = top;
+                    tops[half * 128 * TILES + tl * 128 + t] = top;
                     bar_some(pair, 64);
-                    top = fmaxf(top, tops[(half ^ 1) * 256 + tl * 128 + t]);
+                    top = fmaxf(top, tops[(half ^ 1) * 128 * TILES + tl * 128 + t]);
                     // m = -infinity: nothing was summed yet, and O is zero or not yet written
                     const bool raise = top > m;
                     const float f = raise && m != kNone ? exp2_fast((m - top) * c) : 1.0f;
@@ -369,9 +377,9 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
         if (steps > 0 && ok) ok = __all_sync(0xffffffffu, wait(bar.o, 0));
         tc_fence_after();
         float l = l0 + l1;
-        tops[512 * 0 + half * 256 + tl * 128 + t] = l;
+        tops[half * 128 * TILES + tl * 128 + t] = l;
         bar_some(pair, 64);
-        l = tops[tl * 128 + t] + tops[256 + tl * 128 + t];
+        l = tops[tl * 128 + t] + tops[128 * TILES + tl * 128 + t];
         const int32_t heads = st.kv_heads * st.group;
         const int64_t all_rows = (int64_t)st.total_q * heads;
         if (ok) {
@@ -439,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_tc_kernel(AttendJob j,
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 16) tmem_dealloc(tmem, 512);
+    if (warp == kIssuer) tmem_dealloc(tmem, P::columns);
 }
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -489,23 +497,27 @@ bool rows_map(void* map, const StepView& st, const RowsView& rows, bool half) {
 
 namespace {
 
-template <bool HALF, int DP>
+template <bool HALF, int DP, int TILES>
 cudaError_t attend_tc(const AttendJob& j, cudaStream_t s) {
-    auto* k = kvs_attend_tc_kernel<HALF, DP>;
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<DP>::bytes);
+    using P = Plan<DP, TILES>;
+    auto* k = kvs_attend_tc_kernel<HALF, DP, TILES>;
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, P::bytes);
     if (e != cudaSuccess) return e;
     CUtensorMap km{}, vm{}, qm{};
     const bool boxes = plane_map(&km, j.step, j.k_plane, HALF) && plane_map(&vm, j.step, j.v_plane, HALF), q_boxes = rows_map(&qm, j.step, j.q, HALF);
-    const int64_t pair = 2 * tile_rows_of(j.step.group), tiles = ((int64_t)j.step.max_q * j.step.group + pair - 1) / pair;
-    k<<<dim3((unsigned)(tiles * j.splits), j.step.kv_heads, j.step.requests), kThreads, Plan<DP>::bytes, s>>>(j, km, vm, qm, boxes, q_boxes);
+    const int64_t rows = TILES * tile_rows_of(j.step.group), tiles = ((int64_t)j.step.max_q * j.step.group + rows - 1) / rows;
+    k<<<dim3((unsigned)(tiles * j.splits), j.step.kv_heads, j.step.requests), P::threads, P::bytes, s>>>(j, km, vm, qm, boxes, q_boxes);
     return cudaGetLastError();
+}
+
+template <bool HALF>
+cudaError_t attend_tiles(const AttendJob& j, cudaStream_t s) {
+    if (j.step.head_dim <= 64) return j.row_tiles == 1 ? attend_tc<HALF, 64, 1>(j, s) : attend_tc<HALF, 64, 2>(j, s);
+    return j.row_tiles == 1 ? attend_tc<HALF, 128, 1>(j, s) : attend_tc<HALF, 128, 2>(j, s);
 }
 
 }  // namespace
 
-cudaError_t launch_attend_tc(const AttendJob& j, bool half, cudaStream_t s) {
-    if (j.step.head_dim <= 64) return half ? attend_tc<true, 64>(j, s) : attend_tc<false, 64>(j, s);
-    return half ? attend_tc<true, 128>(j, s) : attend_tc<false, 128>(j, s);
-}
+cudaError_t launch_attend_tc(const AttendJob& j, bool half, cudaStream_t s) { return half ? attend_tiles<true>(j, s) : attend_tiles<false>(j, s); }
 
 }  // namespace kvs

@@ -50,7 +50,7 @@ struct AttendJob {
     int32_t  causal, window;
     int32_t  splits;
     int32_t  tc;                     // 1: on the tensor cores' kernel
-    int32_t  row_tiles;              // 0: tiles of 16 rows to a CTA
+    int32_t  row_tiles;              // of a CTA there
 };
 
 struct WeighJob {
