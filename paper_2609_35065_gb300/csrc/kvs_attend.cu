@@ -15,6 +15,7 @@ namespace kvs {
 namespace {
 
 constexpr int kWarps = 8;
+constexpr int kRows = 16;              // packed rows of a CTA
 constexpr int kKeys = 16;              // keys of a warp's stage
 constexpr float kNone = -INFINITY;
 
@@ -56,48 +57,52 @@ __device__ __forceinline__ Span split_of(Span s, int32_t split, int32_t splits, 
 }
 
 // ---------------------------------------------------------------------------
-// Few packed rows (a decode step, a few drafted tokens): up to 16 MT rows to a CTA, whose eight
-// warps take stages of 16 keys in turn, each with its own running maximum, sum and output in
-// registers and its own ring of stages, filled by cp.async: no barrier between warps until they
-// join at the end.  Bound by HBM: a key's K and V are read once for all query heads of its KV
-// head and all rows of the CTA.
+// Up to 16 packed rows (a decode step): the eight warps of a CTA take stages of 16 keys in
+// turn, each with its own running maximum, sum and output in registers and its own ring of
+// stages, filled by cp.async: no barrier between warps until they join at the end.  Bound by
+// HBM: a key's K and V are read once for all query heads of its KV head.
 // ---------------------------------------------------------------------------
-template <int DP, int MT, int STAGES>
+template <int DP, int STAGES>
 struct RowsPlan {
     static constexpr int ring = kWarps * STAGES * 2 * kKeys * DP * 2;
-    static constexpr int queries = MT > 1 ? 16 * MT * DP * 2 : 0;      // a single tile's stay in registers
-    static constexpr int join = kWarps * 16 * ((DP + 4) * 4 + 8);      // one tile of rows at a time
-    static constexpr int bytes = (ring > join ? ring : join) + queries;
+    static constexpr int join = kWarps * kRows * ((DP + 4) * 4 + 8);
+    static constexpr int bytes = ring > join ? ring : join;
 };
 
-template <bool HALF, int DP, int MT, int STAGES>
+template <bool HALF, int DP, int STAGES>
 __global__ void __launch_bounds__(kWarps * 32) kvs_attend_rows_kernel(AttendJob j) {
     extern __shared__ __align__(1024) char smem[];
     using N = Num<HALF>;
-    using P = RowsPlan<DP, MT, STAGES>;
     constexpr int PITCH = DP * 2, CH = DP / 8;                 // 16-byte vectors of a row
     constexpr int STAGE = 2 * kKeys * PITCH;                   // K, then V
-    constexpr int ROWS = 16 * MT;
     const StepView& st = j.step;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int32_t split = blockIdx.x % j.splits, r = blockIdx.z, h = blockIdx.y;
-    const int32_t row0 = (blockIdx.x / j.splits) * ROWS;
+    const int32_t split = blockIdx.x, r = blockIdx.z, h = blockIdx.y;
     if (j.splits > 1) grid_trigger();                          // the join may come and wait
     const Request q = load_request(st, r);
-    const int32_t rows = min(ROWS, q.n * st.group - row0);
+    const int32_t rows = q.n * st.group;
     if (rows <= 0) return;
-    int32_t g0, g1;
-    const Span all = seen_by(q, token_of(st, row0, g0), token_of(st, row0 + rows - 1, g1), j.causal, j.window);
+    const Span all = seen_by(q, 0, q.n - 1, j.causal, j.window);
     const Span keys = split_of(all, split, j.splits, kKeys * kWarps);
-    const uint32_t base = smem_u32(smem), queries = MT > 1 ? base + P::bytes - P::queries : base;
+    const uint32_t base = smem_u32(smem);
     const int32_t vecs = st.head_dim / 8;
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
 
-    // This warp's stages: keys lo + 16 (warp + 8 i).
+    // Queries: through shared memory into the fragments of every warp.
+    for (int v = threadIdx.x; v < kRows * CH; v += kWarps * 32) {
+        const int i = v / CH, c = v % CH;
+        const bool there = i < rows && c < vecs;
+        int32_t g;
+        const int32_t tok = token_of(st, there ? i : 0, g);
+        const char* src = j.q.base + (there ? 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)(h * st.group + g) * j.q.head + c * 8) : 0);
+        cp_async16(base + swz<PITCH>(i, c), src, there);
+    }
+    cp_commit();
+    // This warp's stages: keys lo + 16 (warp + 8 i).  The row of this lane's key of a stage is
+    // looked up a stage before it is loaded.
     const uint32_t ring = base + warp * STAGES * STAGE;
     const int32_t count = (keys.hi - keys.lo + kKeys - 1) / kKeys;
     const int32_t mine = (count - warp + kWarps - 1) / kWarps;
-    // The row of this lane's key of stage i, looked up a stage before it is loaded.
     auto look_up = [&](int32_t i) {
         const int32_t t = keys.lo + kKeys * (warp + kWarps * i) + (lane & 15);
         return i < mine && t < keys.hi ? row_of(st, table, t) : (int64_t)-1;
@@ -120,184 +125,135 @@ __global__ void __launch_bounds__(kWarps * 32) kvs_attend_rows_kernel(AttendJob 
         }
         cp_commit();
     };
-    // Queries: the rows of the tile, through shared memory into the fragments of every warp.
-    for (int v = threadIdx.x; v < ROWS * CH; v += kWarps * 32) {
-        const int i = v / CH, c = v % CH;
-        const bool there = i < rows && c < vecs;
-        int32_t g;
-        const int32_t tok = token_of(st, there ? row0 + i : 0, g);
-        const char* src = j.q.base + (there ? 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)(h * st.group + g) * j.q.head + c * 8) : 0);
-        cp_async16(queries + swz<PITCH>(i, c), src, there);
-    }
-    cp_commit();
+    cp_wait<0>();
+    __syncthreads();
     uint32_t qf[DP / 16][4];
-    if (MT > 1) {
 #pragma unroll
-        for (int i = 0; i < STAGES - 1; ++i) load(i);
-        cp_wait<STAGES - 1>();
-        __syncthreads();
-    } else {
-        cp_wait<0>();
-        __syncthreads();
+    for (int k = 0; k < DP / 16; ++k) ldsm4(qf[k], base + swz<PITCH>(lane & 15, 2 * k + (lane >> 4)));
+    __syncthreads();                                             // the ring may go over them
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k) ldsm4(qf[k], queries + swz<PITCH>(lane & 15, 2 * k + (lane >> 4)));
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < STAGES - 1; ++i) load(i);
-    }
+    for (int i = 0; i < STAGES - 1; ++i) load(i);
 
-    float o[MT][DP / 8][4];
-    float m[MT][2], l[MT][2];
-    int32_t lo[MT][2], hi[MT][2];                              // what this lane's rows see
+    float o[DP / 8][4];
 #pragma unroll
-    for (int a = 0; a < MT; ++a) {
+    for (int n = 0; n < DP / 8; ++n)
 #pragma unroll
-        for (int n = 0; n < DP / 8; ++n)
+        for (int e = 0; e < 4; ++e) o[n][e] = 0.0f;
+    float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};
+    int32_t lo[2], hi[2];                                        // what this lane's rows see
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[a][n][e] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int i = 16 * a + (lane >> 2) + 8 * k;
-            m[a][k] = kNone;
-            l[a][k] = 0.0f;
-            int32_t g;
-            const int32_t tok = token_of(st, row0 + i, g);
-            const Span s = seen_by(q, tok, tok, j.causal, j.window);
-            lo[a][k] = i < rows ? s.lo : 0;
-            hi[a][k] = i < rows ? min(s.hi, keys.hi) : 0;
-        }
+    for (int k = 0; k < 2; ++k) {
+        const int i = (lane >> 2) + 8 * k;
+        int32_t g;
+        const int32_t tok = token_of(st, i, g);
+        const Span s = seen_by(q, tok, tok, j.causal, j.window);
+        lo[k] = i < rows ? s.lo : 0;
+        hi[k] = i < rows ? min(s.hi, keys.hi) : 0;
     }
     for (int32_t i = 0; i < mine; ++i) {
         cp_wait<STAGES - 2>();
         __syncwarp();
-        load(i + STAGES - 1);                                   // into the slot read last time
+        load(i + STAGES - 1);                                    // into the slot read last time
         const uint32_t at = ring + (i % STAGES) * STAGE;
-        float s[MT][2][4];
+        float s[2][4];
 #pragma unroll
-        for (int a = 0; a < MT; ++a)
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[a][n][e] = 0.0f;
+            for (int e = 0; e < 4; ++e) s[n][e] = 0.0f;
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k) {
             uint32_t b[4];                                       // keys 0-7 and 8-15, dims 16k and 16k + 8
             ldsm4(b, at + swz<PITCH>((lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
-#pragma unroll
-            for (int a = 0; a < MT; ++a) {
-                if (MT > 1) {
-                    uint32_t x[4];
-                    ldsm4(x, queries + swz<PITCH>(16 * a + (lane & 15), 2 * k + (lane >> 4)));
-                    mma16816<HALF>(s[a][0], x, b[0], b[1]);
-                    mma16816<HALF>(s[a][1], x, b[2], b[3]);
-                } else {
-                    mma16816<HALF>(s[a][0], qf[k], b[0], b[1]);
-                    mma16816<HALF>(s[a][1], qf[k], b[2], b[3]);
-                }
-            }
+            mma16816<HALF>(s[0], qf[k], b[0], b[1]);
+            mma16816<HALF>(s[1], qf[k], b[2], b[3]);
         }
         const int32_t t0 = keys.lo + kKeys * (warp + kWarps * i) + 2 * (lane & 3);
-        uint32_t p[MT][4];
+        float mx[2] = {kNone, kNone};
 #pragma unroll
-        for (int a = 0; a < MT; ++a) {
-            float mx[2] = {kNone, kNone};
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int32_t t = t0 + 8 * n + (e & 1);
-                    s[a][n][e] = t >= lo[a][e >> 1] && t < hi[a][e >> 1] ? s[a][n][e] * j.scale_log2 : kNone;
-                    mx[e >> 1] = fmaxf(mx[e >> 1], s[a][n][e]);
-                }
-            float f[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                mx[k] = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], 1));
-                mx[k] = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], 2));
-                const float to = fmaxf(m[a][k], mx[k]);
-                f[k] = to == m[a][k] ? 1.0f : exp2_fast(m[a][k] - to);
-                m[a][k] = to;
+            for (int e = 0; e < 4; ++e) {
+                const int32_t t = t0 + 8 * n + (e & 1);
+                s[n][e] = t >= lo[e >> 1] && t < hi[e >> 1] ? s[n][e] * j.scale_log2 : kNone;
+                mx[e >> 1] = fmaxf(mx[e >> 1], s[n][e]);
             }
-            if (__any_sync(0xffffffffu, f[0] != 1.0f || f[1] != 1.0f)) {
-                l[a][0] *= f[0];
-                l[a][1] *= f[1];
+        float f[2];
 #pragma unroll
-                for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[a][n][e] *= f[e >> 1];
-            }
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[a][n][e] = s[a][n][e] == kNone ? 0.0f : exp2_fast(s[a][n][e] - m[a][e >> 1]);
-                    l[a][e >> 1] += s[a][n][e];
-                }
-            p[a][0] = N::pack(s[a][0][0], s[a][0][1]);
-            p[a][1] = N::pack(s[a][0][2], s[a][0][3]);
-            p[a][2] = N::pack(s[a][1][0], s[a][1][1]);
-            p[a][3] = N::pack(s[a][1][2], s[a][1][3]);
+        for (int k = 0; k < 2; ++k) {
+            mx[k] = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], 1));
+            mx[k] = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], 2));
+            const float to = fmaxf(m[k], mx[k]);
+            f[k] = to == m[k] ? 1.0f : exp2_fast(m[k] - to);
+            m[k] = to;
         }
+        if (__any_sync(0xffffffffu, f[0] != 1.0f || f[1] != 1.0f)) {
+            l[0] *= f[0];
+            l[1] *= f[1];
+#pragma unroll
+            for (int n = 0; n < DP / 8; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][e] *= f[e >> 1];
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[n][e] = s[n][e] == kNone ? 0.0f : exp2_fast(s[n][e] - m[e >> 1]);
+                l[e >> 1] += s[n][e];
+            }
+        const uint32_t p[4] = {N::pack(s[0][0], s[0][1]), N::pack(s[0][2], s[0][3]), N::pack(s[1][0], s[1][1]), N::pack(s[1][2], s[1][3])};
 #pragma unroll
         for (int n = 0; n < DP / 16; ++n) {
             uint32_t b[4];                                       // dims 16n and 16n + 8, keys 0-7 and 8-15
             ldsm4t(b, at + kKeys * PITCH + swz<PITCH>(lane & 15, 2 * n + (lane >> 4)));
-#pragma unroll
-            for (int a = 0; a < MT; ++a) {
-                mma16816<HALF>(o[a][2 * n], p[a], b[0], b[1]);
-                mma16816<HALF>(o[a][2 * n + 1], p[a], b[2], b[3]);
-            }
+            mma16816<HALF>(o[2 * n], p, b[0], b[1]);
+            mma16816<HALF>(o[2 * n + 1], p, b[2], b[3]);
         }
         __syncwarp();
     }
     cp_wait<0>();
+    __syncthreads();                                             // the rings become the join's buffers
 
     // Join: every warp writes its part, then each thread sums the warps' for its outputs.
     constexpr int OP = DP + 4;                                   // floats of a row
     float* po = reinterpret_cast<float*>(smem);                  // [warp][row][OP]
-    float2* pml = reinterpret_cast<float2*>(smem + kWarps * 16 * OP * 4);
+    float2* pml = reinterpret_cast<float2*>(smem + kWarps * kRows * OP * 4);
 #pragma unroll
-    for (int a = 0; a < MT; ++a) {
-        __syncthreads();                                         // the rings, or the tile before, are read
+    for (int k = 0; k < 2; ++k) {
+        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
+        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            l[a][k] += __shfl_xor_sync(0xffffffffu, l[a][k], 1);
-            l[a][k] += __shfl_xor_sync(0xffffffffu, l[a][k], 2);
+        for (int n = 0; n < DP / 8; ++n)
+            *reinterpret_cast<float2*>(po + (warp * kRows + (lane >> 2) + 8 * k) * OP + 8 * n + 2 * (lane & 3)) = make_float2(o[n][2 * k], o[n][2 * k + 1]);
+        if ((lane & 3) == 0) pml[warp * kRows + (lane >> 2) + 8 * k] = make_float2(m[k], l[k]);
+    }
+    __syncthreads();
+    for (int v = threadIdx.x; v < rows * (DP / 2); v += kWarps * 32) {
+        const int i = v / (DP / 2), d = 2 * (v % (DP / 2));
+        float M = kNone, L = 0.0f, x = 0.0f, y = 0.0f;
 #pragma unroll
-            for (int n = 0; n < DP / 8; ++n)
-                *reinterpret_cast<float2*>(po + (warp * 16 + (lane >> 2) + 8 * k) * OP + 8 * n + 2 * (lane & 3)) =
-                    make_float2(o[a][n][2 * k], o[a][n][2 * k + 1]);
-            if ((lane & 3) == 0) pml[warp * 16 + (lane >> 2) + 8 * k] = make_float2(m[a][k], l[a][k]);
+        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, pml[w * kRows + i].x);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float2 ml = pml[w * kRows + i];
+            const float f = ml.y == 0.0f ? 0.0f : exp2_fast(ml.x - M);
+            const float2 p = *reinterpret_cast<const float2*>(po + (w * kRows + i) * OP + d);
+            L += f * ml.y;
+            x += f * p.x;
+            y += f * p.y;
         }
-        __syncthreads();
-        for (int v = threadIdx.x; v < min(16, rows - 16 * a) * (DP / 2); v += kWarps * 32) {
-            const int i = v / (DP / 2), d = 2 * (v % (DP / 2));
-            float M = kNone, L = 0.0f, x = 0.0f, y = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, pml[w * 16 + i].x);
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float2 ml = pml[w * 16 + i];
-                const float f = ml.y == 0.0f ? 0.0f : exp2_fast(ml.x - M);
-                const float2 p = *reinterpret_cast<const float2*>(po + (w * 16 + i) * OP + d);
-                L += f * ml.y;
-                x += f * p.x;
-                y += f * p.y;
-            }
-            if (d >= st.head_dim) continue;
-            int32_t g;
-            const int32_t tok = q.q0 + token_of(st, row0 + 16 * a + i, g), head = h * st.group + g;
-            const int64_t row = (int64_t)tok * (st.kv_heads * st.group) + head;
-            if (j.splits == 1) {
-                const float inv = L > 0.0f ? 1.0f / L : L;
-                *reinterpret_cast<uint32_t*>(j.out.base + 2 * ((int64_t)tok * j.out.row + (int64_t)head * j.out.head + d)) =
-                    N::pack(x * inv, y * inv);
-                if (d == 0 && j.lse) j.lse[row] = L == 0.0f ? kNone : (M + log2f(L)) * 0.69314718055994531f;
-            } else {
-                const int64_t all_rows = (int64_t)st.total_q * st.kv_heads * st.group, to = split * all_rows + row;
-                *reinterpret_cast<float2*>(j.partial + to * st.head_dim + d) = make_float2(x, y);
-                if (d == 0) reinterpret_cast<float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim)[to] = make_float2(M, L);
-            }
+        if (d >= st.head_dim) continue;
+        int32_t g;
+        const int32_t tok = q.q0 + token_of(st, i, g), head = h * st.group + g;
+        const int64_t row = (int64_t)tok * (st.kv_heads * st.group) + head;
+        if (j.splits == 1) {
+            const float inv = L > 0.0f ? 1.0f / L : L;
+            *reinterpret_cast<uint32_t*>(j.out.base + 2 * ((int64_t)tok * j.out.row + (int64_t)head * j.out.head + d)) = N::pack(x * inv, y * inv);
+            if (d == 0 && j.lse) j.lse[row] = L == 0.0f ? kNone : (M + log2f(L)) * 0.69314718055994531f;
+        } else {
+            const int64_t all_rows = (int64_t)st.total_q * st.kv_heads * st.group, to = split * all_rows + row;
+            *reinterpret_cast<float2*>(j.partial + to * st.head_dim + d) = make_float2(x, y);
+            if (d == 0) reinterpret_cast<float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim)[to] = make_float2(M, L);
         }
     }
 }
@@ -356,22 +312,19 @@ __global__ void __launch_bounds__(128) kvs_attend_join_kernel(AttendJob j) {
     if (lane == 0 && j.lse) j.lse[row] = L == 0.0f ? kNone : (M + log2f(L)) * 0.69314718055994531f;
 }
 
-template <bool HALF, int DP, int MT, int STAGES>
+template <bool HALF, int DP>
 cudaError_t attend_rows(const AttendJob& j, cudaStream_t s) {
-    auto* k = kvs_attend_rows_kernel<HALF, DP, MT, STAGES>;
-    constexpr int smem = RowsPlan<DP, MT, STAGES>::bytes;
-    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    constexpr int STAGES = 3, smem = RowsPlan<DP, STAGES>::bytes;
+    auto* k = kvs_attend_rows_kernel<HALF, DP, STAGES>;
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    const int tiles = (int)(((int64_t)j.step.max_q * j.step.group + 16 * MT - 1) / (16 * MT));
-    k<<<dim3((unsigned)(tiles * j.splits), j.step.kv_heads, j.step.requests), kWarps * 32, smem, s>>>(j);
+    k<<<dim3((unsigned)j.splits, j.step.kv_heads, j.step.requests), kWarps * 32, smem, s>>>(j);
     return cudaGetLastError();
 }
 
 template <bool HALF>
 cudaError_t attend_few(const AttendJob& j, cudaStream_t s) {
-    if (j.step.head_dim <= 64)
-        return j.row_tiles == 1 ? attend_rows<HALF, 64, 1, 3>(j, s) : j.row_tiles == 2 ? attend_rows<HALF, 64, 2, 3>(j, s) : attend_rows<HALF, 64, 4, 3>(j, s);
-    return j.row_tiles == 1 ? attend_rows<HALF, 128, 1, 3>(j, s) : attend_rows<HALF, 128, 2, 3>(j, s);
+    return j.step.head_dim <= 64 ? attend_rows<HALF, 64>(j, s) : attend_rows<HALF, 128>(j, s);
 }
 
 }  // namespace
@@ -384,12 +337,13 @@ AttendPlan attend_plan(const StepView& st, int sms) {
     const int32_t tile = tile_rows_of(st.group);
     if (p.tc && rows > tile) p.row_tiles = 2;
     // One CTA to an SM (two of one narrow tile); steps of 128 keys, and about four of start and end.
-    const int64_t per = p.tc ? (int64_t)tile * p.row_tiles : 16, tiles = (rows + per - 1) / per * units, steps = (st.max_kv + 127) / 128, start = 4;
+    const int64_t per = p.tc ? (int64_t)tile * p.row_tiles : 16, tiles = (rows + per - 1) / per * units, steps = (st.max_kv + 127) / 128, start = 4, join = p.row_tiles == 2 ? 6 : 3;
     if (p.tc && p.row_tiles == 1 && st.head_dim <= 64) sms *= 2;
-    // As many parts as keep the number of waves times a part's steps lowest.
+    // As many parts as keep the number of waves times a part's steps lowest; the join of more
+    // than one costs about three, of many rows six.
     int64_t best = -1;
     for (int64_t n = 1; n <= 256 && n <= (steps + 1) / 2; ++n) {
-        const int64_t cost = (tiles * n + sms - 1) / sms * ((steps + n - 1) / n + start);
+        const int64_t cost = (tiles * n + sms - 1) / sms * ((steps + n - 1) / n + start) + (n > 1 ? join : 0);
         if (best < 0 || cost < best) {
             best = cost;
             p.splits = (int)n;
