@@ -10,7 +10,7 @@
  * What it replaces cost 10 to 16 us for one chunk and 80 us for 128, most of a small
  * call; this takes about 1 us and 25 us.
  *
- * append, attend and weigh do the same for the model operators' tensors: whatever is not
+ * append, attend, weigh and evict do the same for the model operators' tensors: whatever is not
  * plainly right (a type, a shape, a stride) is left to the binding, which says what is wrong.
  */
 #define PY_SSIZE_T_CLEAN
@@ -293,7 +293,7 @@ static int int_tuple(PyObject* o, int n, int64_t* out) {
 
 typedef struct {
     uint64_t at;
-    int64_t  shape[3], stride[3];
+    int64_t  shape[4], stride[4];
 } Tensor;
 
 /* A tensor of `dims` dimensions and of that dtype: 1, 0 (something else), -1 (exception). */
@@ -506,8 +506,85 @@ static PyObject* weigh(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
     return run_op(got, fn, &st, layer, &a, stream, flags);
 }
 
+typedef int (*evict_fn)(const kvs_geometry*, const kvs_paged_cache*, const kvs_step*, const kvs_evict_args*, void*, uint32_t);
+
+static int contiguous(const Tensor* t, int dims) {
+    int64_t n = 1;
+    for (int k = dims - 1; k >= 0; --k) {
+        if (t->shape[k] > 1 && t->stride[k] != n) return 0;
+        n *= t->shape[k];
+    }
+    return 1;
+}
+
+/* ..., weights, dst_tables, budget, sinks, recent, kept, new_weights, new_lens (the layer is not used) */
+static PyObject* evict(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
+    (void)self;
+    int64_t fn, layer, stream, flags, budget = 0, sinks = 0, recent = 0;
+    StepRef st;
+    kvs_evict_args a;
+    memset(&a, 0, sizeof a);
+    if (nv != V_MORE + 8) {
+        PyErr_SetString(PyExc_TypeError, "evict takes 16 arguments");
+        return NULL;
+    }
+    int got = read_common(v, &fn, &st, &layer, &stream, &flags);
+    PyObject* const* w = v + V_MORE;
+    Tensor t;
+    memset(&t, 0, sizeof t);
+    const int64_t L = got == 1 ? st.geom->num_layers : 0, H = got == 1 ? st.geom->num_kv_heads : 0, R = got == 1 ? st.step->num_requests : 0;
+    TRY(small_int(w[2], 1, INT32_MAX, &budget));
+    TRY(small_int(w[3], INT32_MIN, INT32_MAX, &sinks));
+    TRY(small_int(w[4], INT32_MIN, INT32_MAX, &recent));
+    TRY(read_tensor(w[0], v[V_F32], 4, &t));
+    if (got == 1) {
+        got = t.shape[0] == L && t.shape[1] == R && t.shape[2] == H && t.shape[3] >= st.step->max_kv && t.stride[3] == 1;
+        a.weights = (const float*)(uintptr_t)t.at;
+        a.layer_stride = t.stride[0];
+        a.request_stride = t.stride[1];
+        a.head_stride = t.stride[2];
+    }
+    TRY(read_tensor(w[1], v[V_I32], 2, &t));
+    if (got == 1) {
+        const int64_t most = st.step->max_kv < budget ? st.step->max_kv : budget;
+        got = t.shape[0] == R && t.stride[1] == 1 && (R <= 1 || t.stride[0] >= t.shape[1]) && t.shape[1] <= INT32_MAX && t.stride[0] <= INT32_MAX &&
+              t.shape[1] * st.geom->block_size >= most;
+        a.dst_tables = (const int32_t*)(uintptr_t)t.at;
+        a.dst_stride = (int32_t)(R > 1 ? t.stride[0] : t.shape[1]);
+    }
+    TRY(read_tensor(w[5], v[V_I32], 4, &t));
+    if (got == 1) {
+        got = t.shape[0] == L && t.shape[1] == R && t.shape[2] == H && t.shape[3] == budget && contiguous(&t, 4);
+        a.kept = (int32_t*)(uintptr_t)t.at;
+    }
+    if (w[6] != Py_None) {
+        TRY(read_tensor(w[6], v[V_F32], 4, &t));
+        if (got == 1) {
+            got = t.shape[0] == L && t.shape[1] == R && t.shape[2] == H && t.shape[3] == budget && contiguous(&t, 4);
+            a.new_weights = (float*)(uintptr_t)t.at;
+        }
+    }
+    if (w[7] != Py_None) {
+        TRY(read_tensor(w[7], v[V_I32], 1, &t));
+        if (got == 1) {
+            got = t.shape[0] == R && contiguous(&t, 1);
+            a.new_lens = (int32_t*)(uintptr_t)t.at;
+        }
+    }
+    a.budget = (int32_t)budget;
+    a.sinks = (int32_t)sinks;
+    a.recent = (int32_t)recent;
+    if (got < 0) return NULL;
+    if (got == 0) Py_RETURN_NONE;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((evict_fn)(uintptr_t)fn)(st.geom, st.cache, st.step, &a, (void*)(uintptr_t)stream, (uint32_t)flags);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
-static PyMethodDef methods[] = {METHOD(call), METHOD(append), METHOD(attend), METHOD(weigh), {NULL, NULL, 0, NULL}};
+static PyMethodDef methods[] = {METHOD(call), METHOD(append), METHOD(attend), METHOD(weigh), METHOD(evict), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "kvs_pycall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit_kvs_pycall(void) {

@@ -303,7 +303,7 @@ def lib():
             L.kvs_selftest_wait_timeout.restype = ctypes.c_int
             for name in ("kvs_retrieve", "kvs_store", "kvs_retrieve_noalloc", "kvs_retrieve_fp8", "kvs_store_fp8",
                          "kvs_retrieve_layers", "kvs_store_layers", "kvs_retrieve_fp8_layers", "kvs_store_fp8_layers",
-                         "kvs_append", "kvs_attend", "kvs_weigh"):
+                         "kvs_append", "kvs_attend", "kvs_weigh", "kvs_evict"):
                 _address[name] = ctypes.cast(getattr(L, name), P).value
             _pycall = _build.load_pycall()
             _ops = getattr(_pycall, "__self__", None)
@@ -790,6 +790,10 @@ def kvs_evict(step: Step, weights, dst_tables, budget: int, sinks: int, recent: 
     blocks]); ``kept`` (int32) and ``new_weights`` (float32, optional) [layers, requests, KV heads,
     budget] and ``new_lens`` (int32 [requests], optional) receive which they were, their weights
     and how many."""
+    if _ops is not None:
+        rc = _ops.evict(_address["kvs_evict"], *step.ext, 0, stream, flags, weights, dst_tables, budget, sinks, recent, kept, new_weights, new_lens)
+        if rc is not None:
+            return _check(rc)
     import torch
     L, R, H = step.geom.num_layers, step.step.num_requests, step.geom.num_kv_heads
     if weights.dim() != 4 or weights.shape[3] < step.max_kv or weights.stride(3) != 1:

@@ -182,3 +182,81 @@ def test_binding_refuses_what_the_structs_cannot_say():
                  lambda: kvs.kvs_evict(s, torch.zeros(1, 2, 2, 64), torch.zeros(3, 4, dtype=i32), 8, 0, 0, torch.zeros(1, 2, 2, 8, dtype=i32))):
         with pytest.raises(ValueError):
             call()
+
+
+# ---- the extension against the binding's own marshalling --------------------
+def _fields(s):
+    return {n: (_fields(getattr(s, n)) if isinstance(getattr(s, n), ctypes.Structure) else getattr(s, n)) for n, _ in s._fields_}
+
+
+def _recorder(struct, layer, seen):
+    sig = [ctypes.c_void_p] * 3 + ([ctypes.c_int32] if layer else []) + [ctypes.POINTER(struct), ctypes.c_void_p, ctypes.c_uint32]
+
+    @ctypes.CFUNCTYPE(ctypes.c_int, *sig)
+    def fn(*a):
+        args = a[4 if layer else 3]
+        seen.append((a[:3], a[3] if layer else None, _fields(args.contents), a[-2], a[-1]))
+        return 0
+    return fn
+
+
+class _Stream:
+    cuda_stream = 4096
+
+
+def test_the_extension_hands_over_what_the_binding_would(monkeypatch):
+    import torch
+    if kvs.lib() is None or kvs._ops is None:
+        pytest.skip("no extension")
+    seen, keep, library = [], [], kvs.lib()
+
+    class Library:
+        def __getattr__(self, name):
+            return getattr(library, name)
+
+    fake = Library()
+    for name, struct in (("kvs_append", kvs.kvs_append_args), ("kvs_attend", kvs.kvs_attend_args), ("kvs_weigh", kvs.kvs_weigh_args),
+                         ("kvs_evict", kvs.kvs_evict_args)):
+        fn = _recorder(struct, name != "kvs_evict", seen)
+        keep.append(fn)
+        setattr(fake, name, fn)
+        monkeypatch.setitem(kvs._address, name, ctypes.cast(fn, ctypes.c_void_p).value)
+    i32 = torch.int32
+    step = _step(geom=(2, 2, 64, 2, 16, 256), planes=[X] * 4)
+    qkv = torch.zeros(2, 8 * 64, dtype=torch.bfloat16)
+    q, k, v = qkv[:, :256].view(2, 4, 64), qkv[:, 256:384].view(2, 2, 64), qkv[:, 384:].view(2, 2, 64)
+    out, lse, w = torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 4), torch.zeros(3, 2, 2, 80)[1]
+    rope, pos, ws = kvs.Rope(torch.zeros(16, 2), 32, True, 0.5), torch.zeros(2, dtype=i32), torch.zeros(99, dtype=torch.uint8)
+    allw, dst, kept, nw, nl = torch.zeros(2, 2, 2, 70)[..., 1:], torch.zeros(2, 3, dtype=i32)[:, :2], torch.zeros(2, 2, 2, 20, dtype=i32), torch.zeros(2, 2, 2, 20), pos
+    calls = [lambda: kvs.kvs_append(step, 1, q, k, v, out, rope, pos, _Stream(), 1), lambda: kvs.kvs_append(step, 0, None, k, v),
+             lambda: kvs.kvs_append(step, 0, out, k, v, None, None, None, 8),
+             lambda: kvs.kvs_attend(step, 1, q, out, lse, 0.25, False, 7, ws, _Stream(), 1), lambda: kvs.kvs_attend(step, 0, q, out),
+             lambda: kvs.kvs_weigh(step, 1, q, lse, w, 0.5, 0.25, True, 3, _Stream()), lambda: kvs.kvs_weigh(step, 0, q, lse, w),
+             lambda: kvs.kvs_evict(step, allw, dst, 20, 3, 4, kept, nw, nl, _Stream(), 1), lambda: kvs.kvs_evict(step, allw, dst, 20, 0, 0, kept)]
+    ops = kvs._ops
+    for call in calls:
+        monkeypatch.setattr(kvs, "_ops", ops)
+        n = len(seen)
+        call()
+        assert len(seen) == n + 1
+        monkeypatch.setattr(kvs, "_ops", None)
+        monkeypatch.setattr(kvs, "_lib", fake)
+        call()
+        monkeypatch.setattr(kvs, "_lib", library)
+        by_ext, by_binding = seen[n:]
+        assert by_ext[1:] == by_binding[1:]
+        assert by_ext[0] == by_binding[0]
+
+
+def test_the_extension_leaves_what_is_not_plain_to_the_binding():
+    import torch
+    if kvs.lib() is None or kvs._ops is None:
+        pytest.skip("no extension")
+    s, q, f = _step(), torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 4)
+    a = (kvs._address["kvs_attend"], *s.ext, 0, None, 0)
+    for args in ((q.half(), q, f, 0.1, True, 0, None), (q[:1], q, f, 0.1, True, 0, None), (q, q[:, :2], f, 0.1, True, 0, None), (q, q, f[:, :2], 0.1, True, 0, None),
+                 (q, q, f, 1, True, 0, None), (q, q, f, 0.1, 1, 0, None), (q, q, f, 0.1, True, 1 << 40, None), (q, q, f, 0.1, True, 0, f),
+                 (None, q, f, 0.1, True, 0, None), (q, 3, f, 0.1, True, 0, None), (torch.zeros(2, 4, 128, dtype=q.dtype)[..., ::2], q, f, 0.1, True, 0, None)):
+        assert kvs._ops.attend(*a, *args, torch.uint8) is None
+    with pytest.raises(TypeError):
+        kvs._ops.attend(*a, q, q)
