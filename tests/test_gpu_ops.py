@@ -333,3 +333,18 @@ def test_a_step_through_all_operators():
     out2 = torch.empty_like(out)
     kvs.kvs_attend(again, 0, q, out2, workspace=torch.empty(kvs.kvs_attend_workspace(again, 8) + 16, dtype=torch.uint8, device="cuda"))
     assert torch.equal(out, out2)
+
+
+def test_a_model_on_a_retrieved_prefix():
+    """The example's serving loop: a suffix on a retrieved prefix gives what the whole prompt's prefill gives."""
+    from paper_2609_35065_gb300 import prefix_step
+    for dtype in (torch.bfloat16, torch.float16):
+        r = prefix_step.run(prefix_step.Config(dtype=dtype))
+        # every rounding of the residual stream (4 layers, 3 products each, 8 or 11 bits) may differ once
+        unit = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -11
+        assert (r["suffix"] - r["whole"]).norm() <= 12 * unit * r["whole"].norm()
+        assert r["stored"] == 512 and len(r["suffix"]) == 178
+        kept = r["kept"].cpu().numpy()
+        T = r["cached"]
+        assert (np.diff(kept, axis=-1) > 0).all() and (kept[..., :4] == np.arange(4)).all() and (kept[..., -64:] == np.arange(T - 64, T)).all()
+        assert torch.isfinite(r["weights"]).all() and len(r["tokens"]) == 24
