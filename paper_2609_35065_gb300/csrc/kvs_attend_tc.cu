@@ -73,15 +73,9 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
     const int32_t per = tile_rows_of(st.group);
     // The last rows see the most keys: they come first, so that no long CTA starts last.
     const int32_t row0 = (tiles - 1 - (int32_t)(blockIdx.x / j.splits)) * TILES * per;
-    const Request q = load_request(st, r);
-    const int32_t rows = min(TILES * per, q.n * st.group - row0);
-    if (rows <= 0) return;
-    Span all = seen_by(q, row0 / st.group, (row0 + rows - 1) / st.group, j.causal, j.window);
-    const int32_t first = all.lo / kN, steps_all = all.hi > all.lo ? (all.hi + kN - 1) / kN - first : 0;
-    const int32_t j0 = first + (int32_t)((int64_t)steps_all * split / j.splits);
-    const int32_t steps = first + (int32_t)((int64_t)steps_all * (split + 1) / j.splits) - j0;
-    const int32_t* table = st.tables + (int64_t)r * st.table_stride;
-
+    // Set-up while the request's lengths are on their way.
+    const RawRequest fetched = fetch_request(st, r);
+    if (warp == kIssuer) tmem_alloc(tmem_at, P::columns);
     if (threadIdx.x == 0) {
         mbar_init(bar.q, q_boxes ? 1 : 256 * TILES);
         for (int i = 0; i < P::stages; ++i) {
@@ -95,7 +89,33 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
         mbar_init(bar.o, 1);
         mbar_init_fence();
     }
-    if (warp == kIssuer) tmem_alloc(tmem_at, P::columns);
+    if (warp == kIssuer + 1 && lane == 0) {
+        if (boxes) {
+            prefetch_map(&k_map);
+            prefetch_map(&v_map);
+        }
+        if (q_boxes) prefetch_map(&q_map);
+    }
+    const Request q = check_request(st, fetched);
+    const int32_t rows = min(TILES * per, q.n * st.group - row0);
+    if (rows <= 0) {
+        if (warp == kIssuer) {
+            __syncwarp();
+            uint32_t at;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(at) : "r"(tmem_at) : "memory");
+            tmem_dealloc(at, P::columns);
+        }
+        return;
+    }
+    const Span all = seen_by(q, row0 / st.group, (row0 + rows - 1) / st.group, j.causal, j.window);
+    const int32_t first = all.lo / kN, steps_all = all.hi > all.lo ? (all.hi + kN - 1) / kN - first : 0;
+    const int32_t j0 = first + (int32_t)((int64_t)steps_all * split / j.splits);
+    const int32_t steps = first + (int32_t)((int64_t)steps_all * (split + 1) / j.splits) - j0;
+    const int32_t* table = st.tables + (int64_t)r * st.table_stride;
+    // K's and V's tiles of a step are in the same blocks; the loading warps look the next step's up a step ahead
+    Box next{};
+    if (boxes && steps > 0 && warp > kIssuer) next = box_of<DP, kLoaders>(st, table, j0 * kN, q.T, warp - kIssuer - 1, lane);
+
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -122,9 +142,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
             pending = -1;
         };
         int32_t i = 0;
-        // K's and V's tiles of a step are in the same blocks; the next step's are looked up a step ahead
-        Box box{}, next{};
-        if (boxes && steps > 0) next = box_of<DP, kLoaders>(st, table, j0 * kN, q.T, w, lane);
+        Box box{};
         for (; i < 2 * steps; ++i) {
             const int stage = i % P::stages;
             if (boxes && !(i & 1)) {
@@ -397,6 +415,12 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
             constexpr int VR = DP / 16;                                                  // 16-byte vectors of a staged row
             const int vec0 = parts ? DP / 8 * half : VR * half;                          // of the whole row, where this half's begin
             const int vecs = (parts ? st.head_dim * 4 : st.head_dim * 2) / 16;
+            // where this thread's row goes; the row's writers get it from here
+            char* row_at = nullptr;
+            if (live) {
+                if (parts) row_at = reinterpret_cast<char*>(j.partial + (split * all_rows + (int64_t)(q.q0 + tok) * heads + h * st.group + g) * st.head_dim);
+                else row_at = j.out.base + 2 * ((int64_t)(q.q0 + tok) * j.out.row + (int64_t)(h * st.group + g) * j.out.head);
+            }
             for (int pass = 0; pass < (parts ? 2 : 1); ++pass) {
 #pragma unroll
                 for (int b = 0; b < DP / 32; ++b) {
@@ -427,18 +451,11 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
                     }
                 }
                 __syncwarp();
-#pragma unroll 4
-                for (int i = lane; i < 32 * VR; i += 32) {
-                    const int row = i / VR, v = i % VR, at = (warp & 3) * 32 + row, vec = vec0 + pass * VR + v;
-                    if (at < per && tl * per + at < rows && vec < vecs) {
-                        int32_t gg;
-                        const int32_t tk = token_of(st, row0 + tl * per + at, gg);
-                        const uint4 x = ld_shared16(stage + row * VR * 16 + ((v ^ (row & (VR - 1))) << 4));
-                        char* dst;
-                        if (parts) dst = reinterpret_cast<char*>(j.partial + (split * all_rows + (int64_t)(q.q0 + tk) * heads + h * st.group + gg) * st.head_dim);
-                        else dst = j.out.base + 2 * ((int64_t)(q.q0 + tk) * j.out.row + (int64_t)(h * st.group + gg) * j.out.head);
-                        *reinterpret_cast<uint4*>(dst + 16 * vec) = x;
-                    }
+#pragma unroll
+                for (int i = 0; i < VR; ++i) {
+                    const int row = i * (32 / VR) + lane / VR, v = lane % VR, vec = vec0 + pass * VR + v;
+                    char* dst = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, (unsigned long long)row_at, row));
+                    if (dst && vec < vecs) *reinterpret_cast<uint4*>(dst + 16 * vec) = ld_shared16(stage + row * VR * 16 + ((v ^ (row & (VR - 1))) << 4));
                 }
                 __syncwarp();
             }

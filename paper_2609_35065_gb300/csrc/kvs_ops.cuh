@@ -19,28 +19,26 @@ struct Request {
     int32_t q0, n, T;      // first row, new tokens, cached tokens
 };
 
-__device__ __forceinline__ Request load_request(const StepView& st, int32_t r) {
-    Request q;
-    q.T = __ldg(st.kv_lens + r);
-    if (st.q_starts) {
-        q.q0 = __ldg(st.q_starts + r);
-        const int32_t end = __ldg(st.q_starts + r + 1);
-        if (q.q0 < 0 || end < q.q0 || end > st.total_q || end - q.q0 > st.max_q) {
-            record_error(st.err, KVS_ERR_BOUNDS);
-            q.q0 = q.n = q.T = 0;
-            return q;
-        }
-        q.n = end - q.q0;
-    } else {
-        q.q0 = r;
-        q.n = 1;
-    }
-    if (q.T < 0 || q.T > st.max_kv) {
+// fetch_request starts the loads, check_request needs them.
+struct RawRequest {
+    int32_t T, q0, end;
+};
+__device__ __forceinline__ RawRequest fetch_request(const StepView& st, int32_t r) {
+    RawRequest w;
+    w.T = __ldg(st.kv_lens + r);
+    w.q0 = st.q_starts ? __ldg(st.q_starts + r) : r;
+    w.end = st.q_starts ? __ldg(st.q_starts + r + 1) : r + 1;
+    return w;
+}
+__device__ __forceinline__ Request check_request(const StepView& st, const RawRequest& w) {
+    Request q{w.q0, w.end - w.q0, w.T};
+    if (w.q0 < 0 || w.end < w.q0 || w.end > st.total_q || w.end - w.q0 > st.max_q || w.T < 0 || w.T > st.max_kv) {
         record_error(st.err, KVS_ERR_BOUNDS);
         q.q0 = q.n = q.T = 0;
     }
     return q;
 }
+__device__ __forceinline__ Request load_request(const StepView& st, int32_t r) { return check_request(st, fetch_request(st, r)); }
 
 __device__ __forceinline__ uint32_t block_of(const StepView& st, uint32_t t) {
     return (uint32_t)(((uint64_t)t * st.block_m) >> st.block_p);
