@@ -14,7 +14,6 @@
 namespace kvs {
 namespace {
 
-constexpr int kWarps = 8;
 constexpr int kRows = 16;              // packed rows of a CTA
 constexpr int kKeys = 16;              // keys of a warp's stage
 constexpr float kNone = -INFINITY;
@@ -39,6 +38,13 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// The 8 x 8 matrix of 16-bit elements whose rows lie two elements to a lane, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
 // Byte offset of the 16-byte vector `c` of row `r` in a tile of rows of PITCH bytes: the
 // vectors of eight neighbouring rows lie in different banks.
 template <int PITCH>
@@ -46,7 +52,7 @@ __device__ __forceinline__ uint32_t swz(uint32_t r, uint32_t c) {
     return r * PITCH + ((c ^ (r & 7)) << 4);
 }
 
-// Splits cut what a tile sees into parts of whole kKeys * kWarps keys.
+// Splits cut what a tile sees into parts of whole units of keys.
 __device__ __forceinline__ Span split_of(Span s, int32_t split, int32_t splits, int32_t unit) {
     const int32_t units = (s.hi - s.lo + unit - 1) / unit;
     const int32_t a = (int32_t)((int64_t)units * split / splits), b = (int32_t)((int64_t)units * (split + 1) / splits);
@@ -57,54 +63,64 @@ __device__ __forceinline__ Span split_of(Span s, int32_t split, int32_t splits, 
 }
 
 // ---------------------------------------------------------------------------
-// Up to 16 packed rows (a decode step): the eight warps of a CTA take stages of 16 keys in
+// Up to 16 packed rows (a decode step): the warps of a CTA take stages of 16 keys in
 // turn, each with its own running maximum, sum and output in registers and its own ring of
 // stages, filled by cp.async: no barrier between warps until they join at the end.  Bound by
 // HBM: a key's K and V are read once for all query heads of its KV head.
+//
+// The products are S^T = K Q^T and O^T = V^T P^T, keys and dims in the 16 rows of mma.m16n8k16
+// and the packed rows in its 8 columns: with the rows in the 16, most of them padding, the same
+// work took twice the instructions, and those of a decode step as long as its loads.  As on the
+// tensor cores the running maximum may lag behind, so that a stage need not exchange it.
+//
+// 14 warps with two stages each: 64 requests over 2k to 8k tokens take 203 us (1.34 GB, 6.6 TB/s);
+// 8 warps with three stages took 211, 5 with five 262 (with the products the other way round).
 // ---------------------------------------------------------------------------
-template <int DP, int STAGES>
+template <int DP, int WARPS, int STAGES>
 struct RowsPlan {
-    static constexpr int ring = kWarps * STAGES * 2 * kKeys * DP * 2;
-    static constexpr int join = kWarps * kRows * ((DP + 4) * 4 + 8);
+    static constexpr int ring = WARPS * STAGES * 2 * kKeys * DP * 2;
+    static constexpr int join = WARPS * kRows * ((DP + 4) * 4 + 8);
     static constexpr int bytes = ring > join ? ring : join;
 };
 
-template <bool HALF, int DP, int STAGES>
-__global__ void __launch_bounds__(kWarps * 32) kvs_attend_rows_kernel(AttendJob j) {
+// NT: column tiles of eight rows.
+template <bool HALF, int DP, int NT, int WARPS, int STAGES>
+__global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j) {
     extern __shared__ __align__(1024) char smem[];
     using N = Num<HALF>;
     constexpr int PITCH = DP * 2, CH = DP / 8;                 // 16-byte vectors of a row
     constexpr int STAGE = 2 * kKeys * PITCH;                   // K, then V
+    constexpr float kLag = HALF ? 14.0f : 20.0f;               // log2 by which a weight may exceed 1
     const StepView& st = j.step;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, i8 = lane >> 2;
     const int32_t split = blockIdx.x, r = blockIdx.z, h = blockIdx.y;
     if (j.splits > 1) grid_trigger();                          // the join may come and wait
     const Request q = load_request(st, r);
     const int32_t rows = q.n * st.group;
     if (rows <= 0) return;
     const Span all = seen_by(q, 0, q.n - 1, j.causal, j.window);
-    const Span keys = split_of(all, split, j.splits, kKeys * kWarps);
+    const Span keys = split_of(all, split, j.splits, kKeys * WARPS);
     const uint32_t base = smem_u32(smem);
     const int32_t vecs = st.head_dim / 8;
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
 
     // Queries: through shared memory into the fragments of every warp.
-    for (int v = threadIdx.x; v < kRows * CH; v += kWarps * 32) {
-        const int i = v / CH, c = v % CH;
-        const bool there = i < rows && c < vecs;
+    for (int v = threadIdx.x; v < 8 * NT * CH; v += WARPS * 32) {
+        const int i = v / CH, d = v % CH;
+        const bool there = i < rows && d < vecs;
         int32_t g;
         const int32_t tok = token_of(st, there ? i : 0, g);
-        const char* src = j.q.base + (there ? 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)(h * st.group + g) * j.q.head + c * 8) : 0);
-        cp_async16(base + swz<PITCH>(i, c), src, there);
+        const char* src = j.q.base + (there ? 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)(h * st.group + g) * j.q.head + d * 8) : 0);
+        cp_async16(base + swz<PITCH>(i, d), src, there);
     }
     cp_commit();
     // This warp's stages: keys lo + 16 (warp + 8 i).  The row of this lane's key of a stage is
     // looked up a stage before it is loaded.
     const uint32_t ring = base + warp * STAGES * STAGE;
     const int32_t count = (keys.hi - keys.lo + kKeys - 1) / kKeys;
-    const int32_t mine = (count - warp + kWarps - 1) / kWarps;
+    const int32_t mine = (count - warp + WARPS - 1) / WARPS;
     auto look_up = [&](int32_t i) {
-        const int32_t t = keys.lo + kKeys * (warp + kWarps * i) + (lane & 15);
+        const int32_t t = keys.lo + kKeys * (warp + WARPS * i) + (lane & 15);
         return i < mine && t < keys.hi ? row_of(st, table, t) : (int64_t)-1;
     };
     int64_t mrow = look_up(0);
@@ -114,12 +130,12 @@ __global__ void __launch_bounds__(kWarps * 32) kvs_attend_rows_kernel(AttendJob 
             const int64_t ahead = look_up(i + 1);
 #pragma unroll
             for (int v = lane; v < kKeys * CH; v += 32) {
-                const int k = v / CH, c = v % CH;
+                const int k = v / CH, d = v % CH;
                 const int64_t row = __shfl_sync(0xffffffffu, mrow, k);
-                const bool there = row >= 0 && c < vecs;
-                const int64_t off = there ? 2 * (row + (int64_t)h * st.head_dim + c * 8) : 0;
-                cp_async16(at + swz<PITCH>(k, c), j.k_plane + off, there);
-                cp_async16(at + kKeys * PITCH + swz<PITCH>(k, c), j.v_plane + off, there);
+                const bool there = row >= 0 && d < vecs;
+                const int64_t off = there ? 2 * (row + (int64_t)h * st.head_dim + d * 8) : 0;
+                cp_async16(at + swz<PITCH>(k, d), j.k_plane + off, there);
+                cp_async16(at + kKeys * PITCH + swz<PITCH>(k, d), j.v_plane + off, there);
             }
             mrow = ahead;
         }
@@ -127,87 +143,109 @@ __global__ void __launch_bounds__(kWarps * 32) kvs_attend_rows_kernel(AttendJob 
     };
     cp_wait<0>();
     __syncthreads();
-    uint32_t qf[DP / 16][4];
+    uint32_t qf[NT][DP / 16][2];                                 // columns: rows 8 n + i8, dims 16 k + 2 c and + 8
 #pragma unroll
-    for (int k = 0; k < DP / 16; ++k) ldsm4(qf[k], base + swz<PITCH>(lane & 15, 2 * k + (lane >> 4)));
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < DP / 16; k += 2) {
+            uint32_t x[4];
+            ldsm4(x, base + swz<PITCH>(8 * n + (lane & 7), 2 * k + (lane >> 3)));
+            qf[n][k][0] = x[0];
+            qf[n][k][1] = x[1];
+            qf[n][k + 1][0] = x[2];
+            qf[n][k + 1][1] = x[3];
+        }
     __syncthreads();                                             // the ring may go over them
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) load(i);
 
-    float o[DP / 8][4];
+    // This lane's rows 8 n + 2 c + e: reference maximum, sum (of its keys), span; output at dims i8 and i8 + 8 of each 16.
+    float o[NT][DP / 16][4], m[NT][2], l[NT][2];
+    int32_t lo[NT][2], hi[NT][2];
 #pragma unroll
-    for (int n = 0; n < DP / 8; ++n)
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[n][e] = 0.0f;
-    float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};
-    int32_t lo[2], hi[2];                                        // what this lane's rows see
+        for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int i = (lane >> 2) + 8 * k;
-        int32_t g;
-        const int32_t tok = token_of(st, i, g);
-        const Span s = seen_by(q, tok, tok, j.causal, j.window);
-        lo[k] = i < rows ? s.lo : 0;
-        hi[k] = i < rows ? min(s.hi, keys.hi) : 0;
+            for (int e = 0; e < 4; ++e) o[n][d][e] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int i = 8 * n + 2 * c + e;
+            m[n][e] = kNone;
+            l[n][e] = 0.0f;
+            int32_t g;
+            const int32_t tok = token_of(st, i, g);
+            const Span s = seen_by(q, tok, tok, j.causal, j.window);
+            lo[n][e] = i < rows ? s.lo : 0;
+            hi[n][e] = i < rows ? min(s.hi, keys.hi) : 0;
+        }
     }
     for (int32_t i = 0; i < mine; ++i) {
         cp_wait<STAGES - 2>();
         __syncwarp();
         load(i + STAGES - 1);                                    // into the slot read last time
         const uint32_t at = ring + (i % STAGES) * STAGE;
-        float s[2][4];
+        float s[NT][2][4];                                       // two sums, of even and odd dims' steps
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] = 0.0f;
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][b][e] = 0.0f;
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k) {
-            uint32_t b[4];                                       // keys 0-7 and 8-15, dims 16k and 16k + 8
-            ldsm4(b, at + swz<PITCH>((lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
-            mma16816<HALF>(s[0], qf[k], b[0], b[1]);
-            mma16816<HALF>(s[1], qf[k], b[2], b[3]);
-        }
-        const int32_t t0 = keys.lo + kKeys * (warp + kWarps * i) + 2 * (lane & 3);
-        float mx[2] = {kNone, kNone};
+            uint32_t a[4];                                       // keys 0-7 and 8-15, dims 16 k and + 8
+            ldsm4(a, at + swz<PITCH>(lane & 15, 2 * k + (lane >> 4)));
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < NT; ++n) mma16816<HALF>(s[n][k & 1], a, qf[n][k][0], qf[n][k][1]);
+        }
+        // keys t0 + i8 and + 8 of rows 2 c, 2 c + 1: elements 0, 1 and 2, 3
+        const int32_t t0 = keys.lo + kKeys * (warp + WARPS * i) + i8;
+        bool above = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int32_t t = t0 + 8 * n + (e & 1);
-                s[n][e] = t >= lo[e >> 1] && t < hi[e >> 1] ? s[n][e] * j.scale_log2 : kNone;
-                mx[e >> 1] = fmaxf(mx[e >> 1], s[n][e]);
+                const int32_t t = t0 + 8 * (e >> 1);
+                const float x = (s[n][0][e] + s[n][1][e]) * j.scale_log2;
+                s[n][0][e] = t >= lo[n][e & 1] && t < hi[n][e & 1] ? x : kNone;
+                above = above || s[n][0][e] > m[n][e & 1] + kLag;
             }
-        float f[2];
+        if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            mx[k] = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], 1));
-            mx[k] = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], 2));
-            const float to = fmaxf(m[k], mx[k]);
-            f[k] = to == m[k] ? 1.0f : exp2_fast(m[k] - to);
-            m[k] = to;
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float top = fmaxf(s[n][0][e], s[n][0][e + 2]);
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                    const float to = fmaxf(m[n][e], top), f = to == m[n][e] ? 1.0f : exp2_fast(m[n][e] - to);
+                    m[n][e] = to;
+                    l[n][e] *= f;
+#pragma unroll
+                    for (int d = 0; d < DP / 16; ++d) {
+                        o[n][d][e] *= f;
+                        o[n][d][e + 2] *= f;
+                    }
+                }
         }
-        if (__any_sync(0xffffffffu, f[0] != 1.0f || f[1] != 1.0f)) {
-            l[0] *= f[0];
-            l[1] *= f[1];
+        uint32_t p[NT][2];                                       // columns: rows 8 n + i8, keys 2 c and + 8
 #pragma unroll
-            for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[n][e] *= f[e >> 1];
-        }
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < NT; ++n) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[n][e] = s[n][e] == kNone ? 0.0f : exp2_fast(s[n][e] - m[e >> 1]);
-                l[e >> 1] += s[n][e];
+                s[n][0][e] = s[n][0][e] == kNone ? 0.0f : exp2_fast(s[n][0][e] - m[n][e & 1]);
+                l[n][e & 1] += s[n][0][e];
             }
-        const uint32_t p[4] = {N::pack(s[0][0], s[0][1]), N::pack(s[0][2], s[0][3]), N::pack(s[1][0], s[1][1]), N::pack(s[1][2], s[1][3])};
+            p[n][0] = transposed(N::pack(s[n][0][0], s[n][0][1]));
+            p[n][1] = transposed(N::pack(s[n][0][2], s[n][0][3]));
+        }
 #pragma unroll
-        for (int n = 0; n < DP / 16; ++n) {
-            uint32_t b[4];                                       // dims 16n and 16n + 8, keys 0-7 and 8-15
-            ldsm4t(b, at + kKeys * PITCH + swz<PITCH>(lane & 15, 2 * n + (lane >> 4)));
-            mma16816<HALF>(o[2 * n], p, b[0], b[1]);
-            mma16816<HALF>(o[2 * n + 1], p, b[2], b[3]);
+        for (int d = 0; d < DP / 16; ++d) {
+            uint32_t a[4];                                       // dims 16 d and + 8, keys 0-7 and 8-15
+            ldsm4t(a, at + kKeys * PITCH + swz<PITCH>((lane & 7) + ((lane >> 4) << 3), 2 * d + ((lane >> 3) & 1)));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma16816<HALF>(o[n][d], a, p[n][0], p[n][1]);
         }
         __syncwarp();
     }
@@ -217,24 +255,29 @@ __global__ void __launch_bounds__(kWarps * 32) kvs_attend_rows_kernel(AttendJob 
     // Join: every warp writes its part, then each thread sums the warps' for its outputs.
     constexpr int OP = DP + 4;                                   // floats of a row
     float* po = reinterpret_cast<float*>(smem);                  // [warp][row][OP]
-    float2* pml = reinterpret_cast<float2*>(smem + kWarps * kRows * OP * 4);
+    float2* pml = reinterpret_cast<float2*>(smem + WARPS * kRows * OP * 4);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
-        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int n = 0; n < DP / 8; ++n)
-            *reinterpret_cast<float2*>(po + (warp * kRows + (lane >> 2) + 8 * k) * OP + 8 * n + 2 * (lane & 3)) = make_float2(o[n][2 * k], o[n][2 * k + 1]);
-        if ((lane & 3) == 0) pml[warp * kRows + (lane >> 2) + 8 * k] = make_float2(m[k], l[k]);
-    }
+        for (int e = 0; e < 2; ++e) {
+            const int i = 8 * n + 2 * c + e;
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], x);
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) {
+                po[(warp * kRows + i) * OP + 16 * d + i8] = o[n][d][e];
+                po[(warp * kRows + i) * OP + 16 * d + 8 + i8] = o[n][d][e + 2];
+            }
+            if (i8 == 0) pml[warp * kRows + i] = make_float2(m[n][e], l[n][e]);
+        }
     __syncthreads();
-    for (int v = threadIdx.x; v < rows * (DP / 2); v += kWarps * 32) {
+    for (int v = threadIdx.x; v < rows * (DP / 2); v += WARPS * 32) {
         const int i = v / (DP / 2), d = 2 * (v % (DP / 2));
         float M = kNone, L = 0.0f, x = 0.0f, y = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, pml[w * kRows + i].x);
+        for (int w = 0; w < WARPS; ++w) M = fmaxf(M, pml[w * kRows + i].x);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = 0; w < WARPS; ++w) {
             const float2 ml = pml[w * kRows + i];
             const float f = ml.y == 0.0f ? 0.0f : exp2_fast(ml.x - M);
             const float2 p = *reinterpret_cast<const float2*>(po + (w * kRows + i) * OP + d);
@@ -312,19 +355,22 @@ __global__ void __launch_bounds__(128) kvs_attend_join_kernel(AttendJob j) {
     if (lane == 0 && j.lse) j.lse[row] = L == 0.0f ? kNone : (M + log2f(L)) * 0.69314718055994531f;
 }
 
-template <bool HALF, int DP>
+template <bool HALF, int DP, int NT>
 cudaError_t attend_rows(const AttendJob& j, cudaStream_t s) {
-    constexpr int STAGES = 3, smem = RowsPlan<DP, STAGES>::bytes;
-    auto* k = kvs_attend_rows_kernel<HALF, DP, STAGES>;
+    // 14 warps of two column tiles of wide heads would have too few registers
+    constexpr int WARPS = DP == 128 && NT == 2 ? 12 : 14, STAGES = 2, smem = RowsPlan<DP, WARPS, STAGES>::bytes;
+    auto* k = kvs_attend_rows_kernel<HALF, DP, NT, WARPS, STAGES>;
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    k<<<dim3((unsigned)j.splits, j.step.kv_heads, j.step.requests), kWarps * 32, smem, s>>>(j);
+    k<<<dim3((unsigned)j.splits, j.step.kv_heads, j.step.requests), WARPS * 32, smem, s>>>(j);
     return cudaGetLastError();
 }
 
 template <bool HALF>
 cudaError_t attend_few(const AttendJob& j, cudaStream_t s) {
-    return j.step.head_dim <= 64 ? attend_rows<HALF, 64>(j, s) : attend_rows<HALF, 128>(j, s);
+    const bool eight = j.step.max_q * j.step.group <= 8;
+    if (j.step.head_dim <= 64) return eight ? attend_rows<HALF, 64, 1>(j, s) : attend_rows<HALF, 64, 2>(j, s);
+    return eight ? attend_rows<HALF, 128, 1>(j, s) : attend_rows<HALF, 128, 2>(j, s);
 }
 
 }  // namespace
