@@ -389,12 +389,13 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
 
 // ---------------------------------------------------------------------------
 // Few rows (a decode step): a warp takes 16 keys at a time straight into the fragments of
-// mma.m16n8k16, the next 16 in flight meanwhile, and the rows 16 at a time.  The sum over a
-// head's dims has no order, so lane 4i + c takes 16 contiguous bytes of key i (dims 32 k + 8 c
-// ...) for what the instruction calls dims 2c, 2c + 1, 2c + 8 and 2c + 9 of two of its steps,
-// for keys and rows alike: no shared memory, no shuffles.  Bound by HBM: K is read once.
+// mma.m16n8k16, keys in its 16 rows, the next 16 in flight meanwhile, and the packed rows eight
+// at a time in its columns.  The sum over a head's dims has no order, so lane 4 i + c takes 16
+// contiguous bytes of key i (dims 32 k + 8 c ...) for what the instruction calls dims 2c, 2c + 1,
+// 2c + 8 and 2c + 9 of two of its steps, for keys and rows alike: no shared memory.  Bound by
+// HBM: K is read once.
 // ---------------------------------------------------------------------------
-constexpr int kRowWarps = 8, kRowKeys = 16, kWaves = 4;
+constexpr int kRowWarps = 8, kRowKeys = 16, kWaves = 2;
 
 template <bool HALF>
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -406,39 +407,40 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// 16 rows' fragments, lse and what they see.
+// Eight packed rows: fragments of row p0 + lane / 4; lse and span of rows p0 + 2 c + e.
 template <int K>
 struct RowFrags {
-    uint4 q[2][K];               // rows i and i + 8
+    uint4 q[K];
     float lse[2];                // times -log2(e)
     Span  see[2];
 };
-template <bool HALF, int K>
+template <int K>
 __device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, const Request& q, int32_t h, int32_t p0, int lane) {
     const StepView& st = j.step;
-    const int32_t total = q.n * st.group;
+    const int32_t total = q.n * st.group, c = lane & 3, p = p0 + (lane >> 2);
+    int32_t g = 0;
+    const int32_t tok = token_of(st, p < total ? p : 0, g);
+    const char* row = j.q.base + 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)(h * st.group + g) * j.q.head);
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-        const int32_t p = p0 + (lane >> 2) + 8 * m;
-        int32_t g = 0;
-        const int32_t tok = token_of(st, p, g), head = h * st.group + g;
-        f.see[m] = Span{0, 0};
-        f.lse[m] = 0.0f;
-        if (p < total) {
-            f.see[m] = seen_by(q, tok, tok, j.causal, j.window);
-            f.lse[m] = -kLog2e * __ldg(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + head);
-        }
+    for (int k = 0; k < K; ++k) {
+        f.q[k] = make_uint4(0, 0, 0, 0);
+        const int32_t d = 32 * k + 8 * c;
+        if (p < total && d < st.head_dim) f.q[k] = __ldg(reinterpret_cast<const uint4*>(row + 2 * d));
+    }
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            f.q[m][k] = make_uint4(0, 0, 0, 0);
-            const int32_t d = 32 * k + 8 * (lane & 3);
-            if (p < total && d < st.head_dim)
-                f.q[m][k] = __ldg(reinterpret_cast<const uint4*>(j.q.base + 2 * ((int64_t)(q.q0 + tok) * j.q.row + (int64_t)head * j.q.head + d)));
+    for (int e = 0; e < 2; ++e) {
+        const int32_t x = p0 + 2 * c + e;
+        f.see[e] = Span{0, 0};
+        f.lse[e] = 0.0f;
+        if (x < total) {
+            const int32_t t = token_of(st, x, g);
+            f.see[e] = seen_by(q, t, t, j.causal, j.window);
+            f.lse[e] = -kLog2e * __ldg(j.lse + (int64_t)(q.q0 + t) * (st.kv_heads * st.group) + h * st.group + g);
         }
     }
 }
 
-// ONE: the request has at most 16 rows, whose fragments stay.
+// ONE: the request has at most eight rows, whose fragments stay.
 template <bool HALF, int DP, bool ONE>
 __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(WeighJob j) {
     constexpr int K = DP / 32;                                   // 16-byte vectors of a lane and key
@@ -461,12 +463,12 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
             row[e] = n < mine && t < q.T ? row_of(st, table, t) : -1;
         }
     };
-    // lane 4 i + c, i < 4, adds to the weight of key 8 (i / 2) + 2 c + i % 2, which it loads with the keys
+    // lanes 4 i and 4 i + 1 add to the weights of keys i and i + 8, which they load with the keys
     float* weights = j.weights + r * j.request_stride + h * j.head_stride;
     auto load = [&](int32_t n, const int64_t (&row)[2], uint4 (&kv)[2][K], float& old) {
-        const int32_t t = key0(n) + 8 * (i >> 1) + 2 * c + (i & 1);
+        const int32_t t = key0(n) + i + 8 * c;
         old = 0.0f;
-        if (j.decay != 0.0f && n < mine && i < 4 && t < q.T) old = j.decay * weights[t];
+        if (j.decay != 0.0f && n < mine && c < 2 && t < q.T) old = weights[t];
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -479,44 +481,36 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
     const int32_t total = q.n * st.group;
     RowFrags<K> one;
     auto weigh = [&](int32_t n, const uint4 (&kv)[2][K], float old) {
-        float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};                // keys 8 e + 2 c and + 1
+        const int32_t t = key0(n) + i;
+        float sum[2] = {0.0f, 0.0f};                             // keys t and t + 8, of this lane's rows
         auto add = [&](const RowFrags<K>& f) {
+            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int k = 0; k < K; ++k) {
+                mma<HALF>(s, kv[0][k].x, kv[1][k].x, kv[0][k].y, kv[1][k].y, f.q[k].x, f.q[k].y);
+                mma<HALF>(u, kv[0][k].z, kv[1][k].z, kv[0][k].w, kv[1][k].w, f.q[k].z, f.q[k].w);
+            }
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    mma<HALF>(s, f.q[0][k].x, f.q[1][k].x, f.q[0][k].y, f.q[1][k].y, kv[e][k].x, kv[e][k].y);
-                    mma<HALF>(u, f.q[0][k].z, f.q[1][k].z, f.q[0][k].w, f.q[1][k].w, kv[e][k].z, kv[e][k].w);
-                }
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int32_t t = key0(n) + 8 * e + 2 * c + b;
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-                        if (t >= f.see[m].lo && t < f.see[m].hi) sums[2 * e + b] += exp2_fast(fmaf(s[2 * m + b] + u[2 * m + b], j.scale_log2, f.lse[m]));
-                }
+            for (int e = 0; e < 4; ++e) {
+                const int32_t key = t + 8 * (e >> 1);
+                if (key >= f.see[e & 1].lo && key < f.see[e & 1].hi) sum[e >> 1] += exp2_fast(fmaf(s[e] + u[e], j.scale_log2, f.lse[e & 1]));
             }
         };
         if (ONE) {
             add(one);
         } else {
-            for (int32_t p0 = 0; p0 < total; p0 += 16) {
+            for (int32_t p0 = 0; p0 < total; p0 += 8) {
                 RowFrags<K> f;
-                load_rows<HALF, K>(f, j, q, h, p0, lane);
+                load_rows<K>(f, j, q, h, p0, lane);
                 add(f);
             }
         }
-        // the rows' sums join over the lanes of one c
-        float x = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) sums[e] += __shfl_xor_sync(0xffffffffu, sums[e], d);
-            if (i == e) x = sums[e];
+        for (int e = 0; e < 2; ++e) {
+            sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 1);
+            sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 2);
         }
-        const int32_t t = key0(n) + 8 * (i >> 1) + 2 * c + (i & 1);
-        if (i < 4 && t < q.T) weights[t] = old + x;
+        if (c < 2 && t + 8 * c < q.T) weights[t + 8 * c] = j.decay * old + (c ? sum[1] : sum[0]);
     };
     uint4 ka[2][K], kb[2][K];
     float wa, wb;
@@ -524,7 +518,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
     look_up(0, row);
     load(0, row, ka, wa);
     look_up(1, row);
-    if (ONE) load_rows<HALF, K>(one, j, q, h, 0, lane);
+    if (ONE) load_rows<K>(one, j, q, h, 0, lane);
     for (int32_t n = 0; n < mine; n += 2) {
         load(n + 1, row, kb, wb);
         look_up(n + 2, row);
@@ -545,7 +539,7 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
         int64_t x = (kWaves * 2 * sms + pairs - 1) / pairs;
         x = x > most ? most : x;
         const dim3 grid((unsigned)x, st.kv_heads, st.requests);
-        if (rows <= 16) kvs_weigh_rows_kernel<HALF, DP, true><<<grid, kRowWarps * 32, 0, s>>>(j);
+        if (rows <= 8) kvs_weigh_rows_kernel<HALF, DP, true><<<grid, kRowWarps * 32, 0, s>>>(j);
         else kvs_weigh_rows_kernel<HALF, DP, false><<<grid, kRowWarps * 32, 0, s>>>(j);
         return cudaGetLastError();
     }
