@@ -393,9 +393,12 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
 // at a time in its columns.  The sum over a head's dims has no order, so lane 4 i + c takes 16
 // contiguous bytes of key i (dims 32 k + 8 c ...) for what the instruction calls dims 2c, 2c + 1,
 // 2c + 8 and 2c + 9 of two of its steps, for keys and rows alike: no shared memory.  Bound by
-// HBM: K is read once.
+// HBM, K being read once: a decode step of 16 requests with 4000 to 8000 cached tokens (201 MB
+// of K) in 40.7 us, 4.9 TB/s; two CTAs to an SM hold 128 registers a thread, most of them keys
+// in flight, and a third tile of them spills (55 us).  With the packed rows in the
+// instruction's 16 rows, half of them empty, it took 49 us.
 // ---------------------------------------------------------------------------
-constexpr int kRowWarps = 8, kRowKeys = 16, kWaves = 2;
+constexpr int kRowWarps = 8, kRowKeys = 16;
 
 template <bool HALF>
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -440,8 +443,10 @@ __device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, con
     }
 }
 
-// ONE: the request has at most eight rows, whose fragments stay.
-template <bool HALF, int DP, bool ONE>
+// STAY: the requests have at most eight times as many rows, whose fragments stay.  0: any number,
+// whose fragments are loaded (from L1) for every 16 keys; 16 rows take 27 us with and 38 without
+// them staying (8 requests x 8 heads of 64 dims, 8000 tokens), with 128 dims 45 and 48.
+template <bool HALF, int DP, int STAY>
 __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(WeighJob j) {
     constexpr int K = DP / 32;                                   // 16-byte vectors of a lane and key
     const StepView& st = j.step;
@@ -479,7 +484,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
             }
     };
     const int32_t total = q.n * st.group;
-    RowFrags<K> one;
+    RowFrags<K> stay[STAY ? STAY : 1];
     auto weigh = [&](int32_t n, const uint4 (&kv)[2][K], float old) {
         const int32_t t = key0(n) + i;
         float sum[2] = {0.0f, 0.0f};                             // keys t and t + 8, of this lane's rows
@@ -496,9 +501,9 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
                 if (key >= f.see[e & 1].lo && key < f.see[e & 1].hi) sum[e >> 1] += exp2_fast(fmaf(s[e] + u[e], j.scale_log2, f.lse[e & 1]));
             }
         };
-        if (ONE) {
-            add(one);
-        } else {
+#pragma unroll
+        for (int x = 0; x < STAY; ++x) add(stay[x]);
+        if (STAY == 0) {
             for (int32_t p0 = 0; p0 < total; p0 += 8) {
                 RowFrags<K> f;
                 load_rows<K>(f, j, q, h, p0, lane);
@@ -518,7 +523,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
     look_up(0, row);
     load(0, row, ka, wa);
     look_up(1, row);
-    if (ONE) load_rows<K>(one, j, q, h, 0, lane);
+#pragma unroll
+    for (int x = 0; x < STAY; ++x) load_rows<K>(stay[x], j, q, h, 8 * x, lane);
     for (int32_t n = 0; n < mine; n += 2) {
         load(n + 1, row, kb, wb);
         look_up(n + 2, row);
@@ -533,14 +539,18 @@ template <bool HALF, int DP>
 cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     const StepView& st = j.step;
     const int64_t rows = (int64_t)st.max_q * st.group;
-    if (rows <= 64) {
-        // Two CTAs to an SM: enough of them that lengths even out, and not more than give a warp four tiles.
+    // Up to 48 rows: 8 requests x 8 heads of 128 dims with 8000 tokens take 68 us at 32 rows (on the
+    // tensor cores' kernel 97), 90 at 48 (97) and 112 at 64 (92); of 64 dims 54 (90), 70 (90), 85 (82).
+    if (rows <= 48) {
+        // CTAs for two rounds of two to an SM (weigh of a decode step: one round 45.2 us, two 40.5,
+        // three 41.1, six 45.1), but not more than leave a warp four tiles.
         const int64_t pairs = (int64_t)st.kv_heads * st.requests, most = (st.max_kv + kRowWarps * kRowKeys * 4 - 1) / (kRowWarps * kRowKeys * 4);
-        int64_t x = (kWaves * 2 * sms + pairs - 1) / pairs;
+        int64_t x = (4 * sms + pairs - 1) / pairs;
         x = x > most ? most : x;
         const dim3 grid((unsigned)x, st.kv_heads, st.requests);
-        if (rows <= 8) kvs_weigh_rows_kernel<HALF, DP, true><<<grid, kRowWarps * 32, 0, s>>>(j);
-        else kvs_weigh_rows_kernel<HALF, DP, false><<<grid, kRowWarps * 32, 0, s>>>(j);
+        if (rows <= 8) kvs_weigh_rows_kernel<HALF, DP, 1><<<grid, kRowWarps * 32, 0, s>>>(j);
+        else if (rows <= 16) kvs_weigh_rows_kernel<HALF, DP, 2><<<grid, kRowWarps * 32, 0, s>>>(j);
+        else kvs_weigh_rows_kernel<HALF, DP, 0><<<grid, kRowWarps * 32, 0, s>>>(j);
         return cudaGetLastError();
     }
     auto* k = kvs_weigh_tc_kernel<HALF, DP>;
