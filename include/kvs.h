@@ -502,7 +502,7 @@ typedef struct kvs_step {
     int32_t table_stride;           /* entries of a table, at least max_kv / B          */
     int32_t total_q;                /* rows of the step's tensors                       */
     int32_t max_q;                  /* no request has more new tokens ...               */
-    int32_t max_kv;                 /* ... or cached ones                               */
+    int32_t max_kv;                 /* ... or cached ones; at most 2^30                 */
     int32_t dtype;                  /* KVS_DTYPE_* of planes and tensors                */
 } kvs_step;
 

@@ -27,7 +27,7 @@ SOURCES = [os.path.join(CSRC, f) for f in ("kvs_kernels.cu", "kvs_api.cpp", "kvs
                                            "kvs_tier.cpp", "kvs_ops_api.cpp", "kvs_append.cu", "kvs_attend.cu", "kvs_attend_tc.cu",
                                            "kvs_weigh.cu", "kvs_evict.cu")]
 DEPS = SOURCES + [os.path.join(CSRC, "kvs_internal.h"), os.path.join(CSRC, "kvs_async.cuh"),
-                  os.path.join(CSRC, "kvs_job.cuh"), os.path.join(CSRC, "kvs_div.h"),
+                  os.path.join(CSRC, "kvs_job.cuh"),
                   os.path.join(CSRC, "kvs_ops.h"), os.path.join(CSRC, "kvs_ops.cuh"), os.path.join(CSRC, "kvs_tcgen05.cuh"), os.path.join(INCLUDE, "kvs.h")]
 ARCH = "-gencode=arch=compute_103a,code=sm_103a"
 

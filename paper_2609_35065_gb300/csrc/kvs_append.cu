@@ -54,10 +54,10 @@ __device__ __forceinline__ Place place_of(const AppendJob& j, int32_t n) {
 // A warp takes one token at a time: its lanes go over (head, vector pair), eight pairs each.
 // VEC: halves of the rotated part begin at multiples of eight elements (or pairs are neighbours).
 template <bool HALF>
-__global__ void __launch_bounds__(256) kvs_append_kernel(AppendJob j, int32_t warps_per_token, int32_t lanes_per_head) {
-    const int32_t w = (int32_t)((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
+__global__ void __launch_bounds__(256) kvs_append_kernel(AppendJob j, uint32_t warps_per_token, int32_t lanes_per_head) {
+    const uint32_t w = blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5);       // at most 2^31 of them are needed
+    if (w / warps_per_token >= (uint32_t)j.step.total_q) return;
     const int32_t n = w / warps_per_token, part = w % warps_per_token;
-    if (n >= j.step.total_q) return;
     const int lane = threadIdx.x & 31;
     const Place pl = place_of(j, n);
     const int32_t D = j.step.head_dim, rot = j.rot_dim;
@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(256) kvs_append_kernel(AppendJob j, int32_t wa
 
     const int32_t c0 = lane % lanes_per_head, heads_at_once = 32 / lanes_per_head;
     if (lane / lanes_per_head >= heads_at_once) return;
-    const int32_t first = part * heads_at_once + lane / lanes_per_head, step = warps_per_token * heads_at_once;
+    const int32_t first = part * heads_at_once + lane / lanes_per_head, step = (int32_t)warps_per_token * heads_at_once;
     const int32_t total = (j.q.base ? j.q_heads : 0) + 2 * j.step.kv_heads;
     // A lane owns two groups of eight elements of a head.  Rotated halves: [8c, 8c + 8) and the
     // eight at rot / 2 behind; neighbours and the rest of the head: sixteen in a row.
@@ -148,8 +148,9 @@ __global__ void __launch_bounds__(256) kvs_append_kernel(AppendJob j, int32_t wa
 // a lane per pair, one element at a time.
 template <bool HALF>
 __global__ void __launch_bounds__(256) kvs_append_pairs_kernel(AppendJob j) {
-    const int32_t n = (int32_t)((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
-    if (n >= j.step.total_q) return;
+    const uint32_t w = blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5);
+    if (w >= (uint32_t)j.step.total_q) return;
+    const int32_t n = (int32_t)w;
     const int lane = threadIdx.x & 31;
     const Place pl = place_of(j, n);
     const int32_t D = j.step.head_dim, rot = j.rot_dim, H = j.step.kv_heads;
@@ -208,6 +209,14 @@ cudaError_t append(const AppendJob& j, cudaStream_t s) {
 }
 
 }  // namespace
+
+void set_divisors(StepView& st) {
+    const FastDiv block = make_fastdiv((uint32_t)st.block_size), group = make_fastdiv((uint32_t)(st.group ? st.group : 1));
+    st.block_m = block.m;
+    st.block_p = block.p;
+    st.group_m = group.m;
+    st.group_p = group.p;
+}
 
 int launch_append(const AppendJob& j, bool half, cudaStream_t s) {
     const cudaError_t e = half ? append<true>(j, s) : append<false>(j, s);

@@ -77,6 +77,8 @@ struct EvictJob {
     int32_t* new_lens;
 };
 
+// Fills in the reciprocals of block_size and group.
+void set_divisors(StepView& st);
 // Each enqueues its kernels and returns how many (negative: a cudaError_t, negated).
 int launch_append(const AppendJob& j, bool half, cudaStream_t s);
 int launch_attend(const AttendJob& j, bool half, cudaStream_t s);

@@ -9,7 +9,6 @@
 #include <new>
 
 #include "kvs.h"
-#include "kvs_div.h"
 #include "kvs_ops.h"
 
 namespace kvs {
@@ -53,6 +52,7 @@ int view_of(const kvs_geometry* g, const kvs_step* s, int32_t q_heads, StepView&
         return ops_fail(KVS_ERR_INVALID_ARG, "dtype must be KVS_DTYPE_BF16 or KVS_DTYPE_F16 (got %d)", s->dtype);
     if (s->num_requests < 0 || s->total_q < 0 || s->max_q < 0 || s->max_kv < 0 || s->table_stride < 0)
         return ops_fail(KVS_ERR_INVALID_ARG, "a step's counts must not be negative");
+    if (s->max_kv > 1 << 30) return ops_fail(KVS_ERR_UNSUPPORTED, "max_kv (%d) is above 2^30", s->max_kv);
     if (s->num_requests > 65535) return ops_fail(KVS_ERR_UNSUPPORTED, "at most 65535 requests in a step");
     if (s->num_requests > 0 && !s->kv_lens) return ops_fail(KVS_ERR_INVALID_ARG, "kv_lens is NULL");
     if (s->num_requests > 0 && s->max_kv > 0 && !s->block_tables) return ops_fail(KVS_ERR_INVALID_ARG, "block_tables is NULL");
@@ -73,15 +73,10 @@ int view_of(const kvs_geometry* g, const kvs_step* s, int32_t q_heads, StepView&
     v.max_q = s->max_q;
     v.max_kv = s->max_kv;
     v.block_size = g->block_size;
-    const FastDiv d = make_fastdiv((uint32_t)g->block_size);
-    v.block_m = d.m;
-    v.block_p = d.p;
     v.kv_heads = g->num_kv_heads;
     v.head_dim = g->head_dim;
     v.group = q_heads > 0 ? q_heads / g->num_kv_heads : 0;
-    const FastDiv gd = make_fastdiv((uint32_t)(v.group ? v.group : 1));
-    v.group_m = gd.m;
-    v.group_p = gd.p;
+    set_divisors(v);
     if ((int64_t)s->max_q * (v.group ? v.group : 1) > INT32_MAX / 2)
         return ops_fail(KVS_ERR_UNSUPPORTED, "max_q times the query heads of a KV head is above 2^30");
     return KVS_OK;
@@ -124,9 +119,13 @@ int flags_of(uint32_t flags) {
     return flags & ~KVS_F_VALIDATE ? ops_fail(KVS_ERR_INVALID_ARG, "the only flag is KVS_F_VALIDATE (got 0x%x)", flags) : KVS_OK;
 }
 
-int mask_of(float scale, int32_t window) {
+// A window that no request's tokens fill hides nothing: 0 then, so that the kernels' sums of
+// positions and windows stay in 32 bits.
+int mask_of(float scale, int32_t window, const kvs_step* s, int32_t& out) {
     if (!std::isfinite(scale)) return ops_fail(KVS_ERR_INVALID_ARG, "scale is not finite");
-    return window < 0 ? ops_fail(KVS_ERR_INVALID_ARG, "window is negative") : KVS_OK;
+    if (window < 0) return ops_fail(KVS_ERR_INVALID_ARG, "window is negative");
+    out = window >= s->max_kv ? 0 : window;
+    return KVS_OK;
 }
 
 // After a launcher: its status, its count, and the error word if the caller asked for it.
@@ -194,7 +193,7 @@ int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     KVS_TRY(view_of(g, st, a->num_q_heads, j.step));
     KVS_TRY(cache_of(g, c, layer, 2, j.step));
     KVS_TRY(flags_of(flags));
-    KVS_TRY(mask_of(a->scale, a->window));
+    KVS_TRY(mask_of(a->scale, a->window, st, j.window));
     if (st->total_q == 0 || st->num_requests == 0) return KVS_OK;
     KVS_TRY(rows_of(a->q, st->total_q, a->num_q_heads, "q", j.q));
     KVS_TRY(rows_of(a->out, st->total_q, a->num_q_heads, "out", j.out));
@@ -204,7 +203,6 @@ int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     j.lse = a->lse;
     j.scale_log2 = a->scale * kLog2e;
     j.causal = a->causal != 0;
-    j.window = a->window;
     int sms;
     KVS_TRY(ops_device(&j.step.err, &sms));
     const AttendPlan plan = attend_plan(j.step, sms);
@@ -229,7 +227,7 @@ int weigh_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* 
     KVS_TRY(view_of(g, st, a->num_q_heads, j.step));
     KVS_TRY(cache_of(g, c, layer, 1, j.step));
     KVS_TRY(flags_of(flags));
-    KVS_TRY(mask_of(a->scale, a->window));
+    KVS_TRY(mask_of(a->scale, a->window, st, j.window));
     if (!std::isfinite(a->decay)) return ops_fail(KVS_ERR_INVALID_ARG, "decay is not finite");
     if (st->num_requests == 0 || st->max_kv == 0) return KVS_OK;
     if (!a->weights) return ops_fail(KVS_ERR_INVALID_ARG, "weights is NULL");
@@ -249,7 +247,6 @@ int weigh_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* 
     j.scale_log2 = a->scale * kLog2e;
     j.decay = a->decay;
     j.causal = a->causal != 0;
-    j.window = a->window;
     int sms;
     KVS_TRY(ops_device(&j.step.err, &sms));
     return done(launch_weigh(j, st->dtype == KVS_DTYPE_F16, sms, s), s, flags);
@@ -262,6 +259,7 @@ int evict_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* 
     KVS_TRY(cache_of(g, c, 0, 2 * g->num_layers, j.step));
     KVS_TRY(flags_of(flags));
     if (a->budget < 1) return ops_fail(KVS_ERR_INVALID_ARG, "budget must be positive");
+    if (a->budget > 1 << 30) return ops_fail(KVS_ERR_UNSUPPORTED, "budget (%d) is above 2^30", a->budget);
     if (a->sinks < 0 || a->recent < 0 || (int64_t)a->sinks + a->recent > a->budget)
         return ops_fail(KVS_ERR_INVALID_ARG, "sinks (%d) and recent (%d) must fit the budget (%d)", a->sinks, a->recent, a->budget);
     if (a->layer_stride < 0 || a->request_stride < 0 || a->head_stride < 0)

@@ -184,11 +184,6 @@ __device__ __forceinline__ void tile_rows(uint32_t dst, const char* plane, const
     }
 }
 
-template <int N>
-__device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N)); }
-template <int N>
-__device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N)); }
-
 // Barrier of `threads` threads under a number of its own (1 to 15).
 __device__ __forceinline__ void bar_some(int id, int threads) { asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory"); }
 

@@ -348,3 +348,34 @@ def test_a_model_on_a_retrieved_prefix():
         T = r["cached"]
         assert (np.diff(kept, axis=-1) > 0).all() and (kept[..., :4] == np.arange(4)).all() and (kept[..., -64:] == np.arange(T - 64, T)).all()
         assert torch.isfinite(r["weights"]).all() and len(r["tokens"]) == 24
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 300])
+@pytest.mark.parametrize("new,lens", [([1, 5], [500, 3]), ([200, 130], [700, 60])])
+def test_a_window_beyond_every_position_hides_nothing(new, lens, window):
+    """Also where a request's first rows lie before its first cached token."""
+    sm = Small(new, lens, 2, 4, 64)
+    (a, za), (b, zb) = _attend(sm), _attend(sm, window=window)
+    assert torch.equal(a, b) and torch.equal(za, zb)
+    step, q, _, _, _cache = sm.on_gpu(kvs)
+    w = torch.zeros(2, 2, 2, step.max_kv, device="cuda")
+    kvs.kvs_weigh(step, 0, q, za, w[0])
+    kvs.kvs_weigh(step, 0, q, za, w[1], window=window)
+    assert torch.equal(w[0], w[1])
+
+
+@pytest.mark.parametrize("G,D,dtype", [(9, 128, "bf16"), (16, 64, "f16"), (17, 128, "f16"), (31, 80, "bf16"), (48, 64, "bf16"), (64, 128, "bf16"), (65, 96, "f16"),
+                                       (128, 64, "f16"), (129, 128, "bf16")])
+def test_weights_of_wide_groups(G, D, dtype):
+    """Nine to some hundred packed rows of a decode step, and of two new tokens."""
+    for new, lens in (([1, 1, 1], [129, 1, 700]), ([2, 0, 1], [300, 77, 15])):
+        sm = Small(new, lens, 1, G, D, dtype=dtype)
+        z = torch.from_numpy(sm.attend(D ** -0.5)[2].astype(np.float32))
+        rng = np.random.default_rng(5)
+        step, q, _, _, _cache = sm.on_gpu(kvs)
+        before = rng.random((3, 1, step.max_kv)).astype(np.float32)
+        w = torch.from_numpy(before).cuda()
+        kvs.kvs_weigh(step, 0, q, z.cuda(), w, decay=0.9, flags=kvs.KVS_F_VALIDATE)
+        want, bound = sm.weigh(z.numpy(), before, float(np.float32(0.9)), D ** -0.5)
+        off = np.abs(w.double().cpu().numpy() - want)
+        assert (off <= bound).all(), (off - bound).max()

@@ -260,3 +260,8 @@ def test_the_extension_leaves_what_is_not_plain_to_the_binding():
         assert kvs._ops.attend(*a, *args, torch.uint8) is None
     with pytest.raises(TypeError):
         kvs._ops.attend(*a, q, q)
+
+
+@pytest.mark.parametrize("op,path,value", [(o, "step.max_kv", (1 << 30) + 1) for o in ("append", "attend", "weigh", "evict")] + [("evict", "evict.budget", (1 << 30) + 1)])
+def test_positions_above_30_bits_are_refused(op, path, value):
+    test_refusals(op, path, value, U)
