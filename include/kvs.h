@@ -638,7 +638,7 @@ typedef struct kvs_evict_args {
     int64_t        layer_stride, request_stride, head_stride;
     const int32_t* dst_tables;      /* device [num_requests][dst_stride]                */
     int32_t        dst_stride;      /* at least budget / B                              */
-    int32_t        budget;          /* at least 1                                       */
+    int32_t        budget;          /* at least 1, at most 2^30                         */
     int32_t        sinks, recent;   /* together at most budget                          */
     int32_t*       kept;            /* device [L][num_requests][H][budget]              */
     float*         new_weights;     /* device [L][num_requests][H][budget], or NULL     */
