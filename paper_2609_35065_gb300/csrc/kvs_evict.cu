@@ -222,8 +222,8 @@ struct Planes {
 
 // A lane per 16-byte vector of a kept row of one head, K and V together; a CTA takes `tokens`
 // kept tokens of all heads, whose rows in the new blocks are contiguous, and two vectors of
-// each thread are in flight.  Bound by HBM: a kept row is read and written once, 2.1 million rows
-// of 256 bytes with K and V each (1.07 GB) in 159 us, 6.7 TB/s.
+// each thread are in flight.  Bound by HBM: a kept row is read and written once, 1.05 million rows
+// of 256 bytes of K and of V (1.07 GB) in 159 us, 6.7 TB/s.
 __global__ void __launch_bounds__(kCopy) kvs_evict_copy_kernel(EvictJob j, const __grid_constant__ Planes planes, int32_t layer0, uint32_t tokens) {
     const StepView& st = j.step;
     const int32_t l = blockIdx.z, r = blockIdx.y;
