@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kRows = 16;              // packed rows of a CTA
 constexpr int kKeys = 16;              // keys of a warp's stage
+constexpr int kCluster = 8;            // most parts that a cluster joins
 constexpr float kNone = -INFINITY;
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
@@ -73,6 +74,9 @@ __device__ __forceinline__ Span split_of(Span s, int32_t split, int32_t splits, 
 // work took twice the instructions, and those of a decode step as long as its loads.  As on the
 // tensor cores the running maximum may lag behind, so that a stage need not exchange it.
 //
+// Where a head's parts are up to eight and all clusters run at once, they are CTAs of a cluster
+// that join through distributed shared memory; otherwise a second kernel joins them.
+//
 // 14 warps with two stages each: 64 requests over 2k to 8k tokens take 203 us (1.34 GB, 6.6 TB/s);
 // 8 warps with three stages took 211, 5 with five 262 (with the products the other way round).
 // ---------------------------------------------------------------------------
@@ -80,8 +84,19 @@ template <int DP, int WARPS, int STAGES>
 struct RowsPlan {
     static constexpr int ring = WARPS * STAGES * 2 * kKeys * DP * 2;
     static constexpr int join = WARPS * kRows * ((DP + 4) * 4 + 8);
-    static constexpr int bytes = ring > join ? ring : join;
+    // [row][DP] and [row] (m, l) of the CTA, for its cluster
+    static constexpr int part = kRows * (DP * 4 + 8);
+    static constexpr int bytes = ring > join + part ? ring : join + part;
 };
+
+// Two numbers at `addr` of the cluster's CTA `rank`.
+__device__ __forceinline__ float2 cluster_ld2(uint32_t addr, int rank) {
+    uint32_t at;
+    float2 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+    return v;
+}
 
 // NT: column tiles of eight rows.
 template <bool HALF, int DP, int NT, int WARPS, int STAGES>
@@ -94,7 +109,7 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
     const StepView& st = j.step;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, i8 = lane >> 2;
     const int32_t split = blockIdx.x, r = blockIdx.z, h = blockIdx.y;
-    if (j.splits > 1) grid_trigger();                          // the join may come and wait
+    if (j.splits > 1 && !j.cluster) grid_trigger();            // the join may come and wait
     const Request q = load_request(st, r);
     const int32_t rows = q.n * st.group;
     if (rows <= 0) return;
@@ -256,6 +271,8 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
     constexpr int OP = DP + 4;                                   // floats of a row
     float* po = reinterpret_cast<float*>(smem);                  // [warp][row][OP]
     float2* pml = reinterpret_cast<float2*>(smem + WARPS * kRows * OP * 4);
+    float* part = reinterpret_cast<float*>(smem + RowsPlan<DP, WARPS, STAGES>::join);
+    float2* part_ml = reinterpret_cast<float2*>(part + kRows * DP);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -293,12 +310,49 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
             const float inv = L > 0.0f ? 1.0f / L : L;
             *reinterpret_cast<uint32_t*>(j.out.base + 2 * ((int64_t)tok * j.out.row + (int64_t)head * j.out.head + d)) = N::pack(x * inv, y * inv);
             if (d == 0 && j.lse) j.lse[row] = L == 0.0f ? kNone : (M + log2f(L)) * 0.69314718055994531f;
+        } else if (j.cluster) {
+            *reinterpret_cast<float2*>(part + i * DP + d) = make_float2(x, y);
+            if (d == 0) part_ml[i] = make_float2(M, L);
         } else {
             const int64_t all_rows = (int64_t)st.total_q * st.kv_heads * st.group, to = split * all_rows + row;
             *reinterpret_cast<float2*>(j.partial + to * st.head_dim + d) = make_float2(x, y);
             if (d == 0) reinterpret_cast<float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim)[to] = make_float2(M, L);
         }
     }
+    if (!j.cluster) return;
+    // The cluster's CTAs share out the outputs and read one another's parts of them, in order.
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    const int total = rows * (DP / 2), share = (total + j.splits - 1) / j.splits;
+    for (int v = split * share + threadIdx.x; v < min(total, (split + 1) * share); v += WARPS * 32) {
+        const int i = v / (DP / 2), d = 2 * (v % (DP / 2));
+        if (d >= st.head_dim) continue;
+        float2 ml[kCluster], p[kCluster];
+        float M = kNone, L = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kCluster; ++k) {
+            ml[k] = make_float2(kNone, 0.0f);
+            p[k] = make_float2(0.0f, 0.0f);
+            if (k < j.splits) {
+                ml[k] = cluster_ld2(smem_u32(part_ml + i), k);
+                p[k] = cluster_ld2(smem_u32(part + i * DP + d), k);
+            }
+            M = fmaxf(M, ml[k].x);
+        }
+#pragma unroll
+        for (int k = 0; k < kCluster; ++k) {
+            const float f = ml[k].y == 0.0f ? 0.0f : exp2_fast(ml[k].x - M);
+            L += f * ml[k].y;
+            x += f * p[k].x;
+            y += f * p[k].y;
+        }
+        int32_t g;
+        const int32_t tok = q.q0 + token_of(st, i, g), head = h * st.group + g;
+        const float inv = L > 0.0f ? 1.0f / L : L;
+        *reinterpret_cast<uint32_t*>(j.out.base + 2 * ((int64_t)tok * j.out.row + (int64_t)head * j.out.head + d)) = N::pack(x * inv, y * inv);
+        if (d == 0 && j.lse) j.lse[(int64_t)tok * (st.kv_heads * st.group) + head] = L == 0.0f ? kNone : (M + log2f(L)) * 0.69314718055994531f;
+    }
+    // no CTA leaves while another may read its part
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
 // Joins the splits' parts: a warp per row, whose lanes weigh a split each and whose loads of
@@ -362,8 +416,18 @@ cudaError_t attend_rows(const AttendJob& j, cudaStream_t s) {
     auto* k = kvs_attend_rows_kernel<HALF, DP, NT, WARPS, STAGES>;
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    k<<<dim3((unsigned)j.splits, j.step.kv_heads, j.step.requests), WARPS * 32, smem, s>>>(j);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)j.splits, j.step.kv_heads, j.step.requests);
+    cfg.blockDim = dim3(WARPS * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = j.splits;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = j.cluster;
+    return cudaLaunchKernelEx(&cfg, k, j);
 }
 
 template <bool HALF>
@@ -379,20 +443,26 @@ AttendPlan attend_plan(const StepView& st, int sms) {
     const int64_t rows = (int64_t)st.max_q * st.group, units = (int64_t)st.kv_heads * st.requests;
     // Up to 16 rows: mma.sync, whose work is in the shadow of the loads; above, the tensor cores (at
     // 20 rows over 3000 to 8000 tokens 62 to 79 us against 65 to 91, at 48 rows 62 to 80 against 97 to 169).
-    AttendPlan p{rows > 16, 1, 1};
+    AttendPlan p{rows > 16, 1, 1, 0};
     const int32_t tile = tile_rows_of(st.group);
     if (p.tc && rows > tile) p.row_tiles = 2;
     // One CTA to an SM (two of one narrow tile); steps of 128 keys, and about four of start and end.
-    const int64_t per = p.tc ? (int64_t)tile * p.row_tiles : 16, tiles = (rows + per - 1) / per * units, steps = (st.max_kv + 127) / 128, start = 4, join = p.row_tiles == 2 ? 6 : 3;
+    const int64_t per = p.tc ? (int64_t)tile * p.row_tiles : 16, tiles = (rows + per - 1) / per * units, steps = (st.max_kv + 127) / 128, start = 4, join = p.row_tiles == 2 ? 6 : p.tc ? 3 : 5;
     if (p.tc && p.row_tiles == 1 && st.head_dim <= 64) sms *= 2;
-    // As many parts as keep the number of waves times a part's steps lowest; the join of more
-    // than one costs about three, of many rows six.
+    // As many parts as keep the number of waves times a part's steps lowest.  The join of parts of
+    // few rows costs about five steps of theirs, within a cluster one (one decoding request over
+    // 2000 tokens 7.1 us with a cluster and 8.9 without, over 4000 8.1 and 10.7, over 8000 10.0 and
+    // 11.4, over 16000, in 19 parts, 13.2); of many rows three, of two tiles six.
     int64_t best = -1;
     for (int64_t n = 1; n <= 256 && n <= (steps + 1) / 2; ++n) {
-        const int64_t cost = (tiles * n + sms - 1) / sms * ((steps + n - 1) / n + start) + (n > 1 ? join : 0);
+        // Clusters have room where all of their CTAs run at once: a cluster's lie on neighbouring SMs, and
+        // of each such group up to n - 1 stay unused (16 clusters of 7 did not fit on 152 SMs: 16 us for 10).
+        const bool cluster = !p.tc && n > 1 && n <= kCluster && tiles * n <= sms - 10 * (n - 1);
+        const int64_t cost = (tiles * n + sms - 1) / sms * ((steps + n - 1) / n + start) + (n == 1 ? 0 : cluster ? 1 : join);
         if (best < 0 || cost < best) {
             best = cost;
             p.splits = (int)n;
+            p.cluster = cluster;
         }
     }
     return p;
@@ -401,7 +471,7 @@ AttendPlan attend_plan(const StepView& st, int sms) {
 int launch_attend(const AttendJob& j, bool half, cudaStream_t s) {
     cudaError_t e = j.tc ? launch_attend_tc(j, half, s) : half ? attend_few<true>(j, s) : attend_few<false>(j, s);
     if (e != cudaSuccess) return -(int)e;
-    if (j.splits == 1) return 1;
+    if (j.splits == 1 || j.cluster) return 1;
     // The join is launched programmatically: its CTAs are in place when the parts are done.
     const int64_t rows = (int64_t)j.step.total_q * j.step.kv_heads * j.step.group;
     cudaLaunchConfig_t cfg{};

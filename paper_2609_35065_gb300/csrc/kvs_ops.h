@@ -49,6 +49,7 @@ struct AttendJob {
     float    scale_log2;             // scale * log2(e)
     int32_t  causal, window;
     int32_t  splits;
+    int32_t  cluster;                // 1: a head's parts are CTAs of a cluster, which joins them
     int32_t  tc;                     // 1: on the tensor cores' kernel
     int32_t  row_tiles;              // of a CTA there
 };
@@ -89,7 +90,7 @@ inline __host__ __device__ int32_t tile_rows_of(int32_t group) { return group <=
 // How attention goes about a step, by its bounds alone: the kernel, and the parts that a
 // request's cached tokens are split into.
 struct AttendPlan {
-    int tc, splits, row_tiles;
+    int tc, splits, row_tiles, cluster;
 };
 AttendPlan attend_plan(const StepView& st, int sms);
 // A plane's TMA map (a CUtensorMap at `map`) in boxes of whole blocks, or of 128 tokens of one,

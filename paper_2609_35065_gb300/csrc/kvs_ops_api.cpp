@@ -182,8 +182,9 @@ int append_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
 }
 
 int64_t workspace_bytes(const StepView& v, int sms) {
-    const int n = attend_plan(v, sms).splits;
-    return n <= 1 ? 0 : (int64_t)n * v.total_q * v.kv_heads * v.group * (v.head_dim + 2) * 4;
+    const AttendPlan plan = attend_plan(v, sms);
+    const int n = plan.splits;
+    return n <= 1 || plan.cluster ? 0 : (int64_t)n * v.total_q * v.kv_heads * v.group * (v.head_dim + 2) * 4;
 }
 
 int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* st, int32_t layer, const kvs_attend_args* a,
@@ -208,6 +209,7 @@ int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     const AttendPlan plan = attend_plan(j.step, sms);
     j.tc = plan.tc;
     j.splits = plan.splits;
+    j.cluster = plan.cluster;
     j.row_tiles = plan.row_tiles;
     const int64_t need = workspace_bytes(j.step, sms);
     if (need > 0) {
