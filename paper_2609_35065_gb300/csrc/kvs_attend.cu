@@ -16,7 +16,6 @@ namespace {
 
 constexpr int kRows = 16;              // packed rows of a CTA
 constexpr int kKeys = 16;              // keys of a warp's stage
-constexpr int kCluster = 8;            // most parts that a cluster joins
 constexpr float kNone = -INFINITY;
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
@@ -88,15 +87,6 @@ struct RowsPlan {
     static constexpr int part = kRows * (DP * 4 + 8);
     static constexpr int bytes = ring > join + part ? ring : join + part;
 };
-
-// Two numbers at `addr` of the cluster's CTA `rank`.
-__device__ __forceinline__ float2 cluster_ld2(uint32_t addr, int rank) {
-    uint32_t at;
-    float2 v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
-    return v;
-}
 
 // NT: column tiles of eight rows.
 template <bool HALF, int DP, int NT, int WARPS, int STAGES>
@@ -321,7 +311,7 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
     }
     if (!j.cluster) return;
     // The cluster's CTAs share out the outputs and read one another's parts of them, in order.
-    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    cluster_sync();
     const int total = rows * (DP / 2), share = (total + j.splits - 1) / j.splits;
     for (int v = split * share + threadIdx.x; v < min(total, (split + 1) * share); v += WARPS * 32) {
         const int i = v / (DP / 2), d = 2 * (v % (DP / 2));
@@ -333,8 +323,8 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
             ml[k] = make_float2(kNone, 0.0f);
             p[k] = make_float2(0.0f, 0.0f);
             if (k < j.splits) {
-                ml[k] = cluster_ld2(smem_u32(part_ml + i), k);
-                p[k] = cluster_ld2(smem_u32(part + i * DP + d), k);
+                ml[k] = cluster_ld2(cluster_at(smem_u32(part_ml + i), k));
+                p[k] = cluster_ld2(cluster_at(smem_u32(part + i * DP + d), k));
             }
             M = fmaxf(M, ml[k].x);
         }
@@ -352,7 +342,7 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
         if (d == 0 && j.lse) j.lse[(int64_t)tok * (st.kv_heads * st.group) + head] = L == 0.0f ? kNone : (M + log2f(L)) * 0.69314718055994531f;
     }
     // no CTA leaves while another may read its part
-    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    cluster_sync();
 }
 
 // Joins the splits' parts: a warp per row, whose lanes weigh a split each and whose loads of
@@ -452,12 +442,14 @@ AttendPlan attend_plan(const StepView& st, int sms) {
     // As many parts as keep the number of waves times a part's steps lowest.  The join of parts of
     // few rows costs about five steps of theirs, within a cluster one (one decoding request over
     // 2000 tokens 7.1 us with a cluster and 8.9 without, over 4000 8.1 and 10.7, over 8000 10.0 and
-    // 11.4, over 16000, in 19 parts, 13.2); of many rows three, of two tiles six.
+    // 11.4, over 16000, in 19 parts, 13.2); of one tile three, or one (20 rows over 2000 tokens 10.0 us
+    // with a cluster, 12.2 without, over 4000 11.8 and 13.1; of eight requests over 1000 13.2 and 14.3),
+    // of two tiles six, where a cluster loses (293 tokens over 4000 37 us, 33 without).
     int64_t best = -1;
     for (int64_t n = 1; n <= 256 && n <= (steps + 1) / 2; ++n) {
         // Clusters have room where all of their CTAs run at once: a cluster's lie on neighbouring SMs, and
         // of each such group up to n - 1 stay unused (16 clusters of 7 did not fit on 152 SMs: 16 us for 10).
-        const bool cluster = !p.tc && n > 1 && n <= kCluster && tiles * n <= sms - 10 * (n - 1);
+        const bool cluster = p.row_tiles == 1 && n > 1 && n <= kCluster && tiles * n <= sms - 10 * (n - 1);
         const int64_t cost = (tiles * n + sms - 1) / sms * ((steps + n - 1) / n + start) + (n == 1 ? 0 : cluster ? 1 : join);
         if (best < 0 || cost < best) {
             best = cost;

@@ -48,6 +48,9 @@ struct Plan {
     static constexpr int bars = (TILES + stages) * tile;
     static constexpr int tops = bars + 256;        // [2][TILES][128] binary32: maxima, sums that a row's threads exchange
     static constexpr int bytes = tops + 1024 * TILES;
+    // for a cluster's join, in the ring: [row][DP] binary32 and [row] (m, l)
+    static constexpr int part = tile, part_ml = part + 128 * DP * 4;
+    static_assert(TILES == 2 || part_ml + 1024 <= bars, "the ring holds a CTA's part");
 };
 
 struct Bars {
@@ -65,6 +68,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
     constexpr int kIssuer = 8 * TILES;               // the issuing warp, behind the softmax's; then the loading ones
     constexpr float kMost = HALF ? 32768.0f : 1048576.0f;            // of a thread's weights of a step
     const StepView& st = j.step;
+    const bool cluster = TILES == 1 && j.cluster;    // no cluster joins the parts of two tiles
     const uint32_t base = smem_u32(raw);
     if (base & 1023) {                               // the swizzle needs it; there is no room to round it up
         record_error(st.err, KVS_ERR_UNSUPPORTED);
@@ -411,12 +415,32 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
             if (live && half == 0) {
                 const float m2 = m == kNone ? kNone : m * c;
                 const int64_t row = (int64_t)(q.q0 + tok) * heads + h * st.group + g;
-                if (j.splits > 1) reinterpret_cast<float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim)[split * all_rows + row] = make_float2(m2, l);
+                if (cluster) reinterpret_cast<float2*>(raw + P::part_ml)[t] = make_float2(m2, l);
+                else if (j.splits > 1) reinterpret_cast<float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim)[split * all_rows + row] = make_float2(m2, l);
                 else if (j.lse) j.lse[row] = l == 0.0f ? kNone : (m2 + log2f(l)) * 0.69314718055994531f;
             }
             // Through shared memory (32 rows of DP bytes to a warp, in Q's place), so that a row's
             // bytes leave in one piece: 16-bit results at once, binary32 parts in two passes.
             const bool parts = j.splits > 1;
+            if (cluster) {
+                // binary32 rows over the ring, which nothing needs any more, for the cluster's CTAs to read
+                const uint32_t at = base + P::part + t * DP * 4;
+#pragma unroll
+                for (int b = 0; b < DP / 32; ++b) {
+                    uint32_t o[16];
+                    if (steps > 0) {
+                        tmem_ld16(o, o_own + 16 * b);
+                        tmem_wait_ld();
+                        tmem_loaded16(o);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int v = DP / 8 * half + 4 * b + e;
+                        const bool some = steps > 0 && l != 0.0f;
+                        st_shared16(at + ((v ^ (t & 7)) << 4), some ? o[4 * e] : 0u, some ? o[4 * e + 1] : 0u, some ? o[4 * e + 2] : 0u, some ? o[4 * e + 3] : 0u);
+                    }
+                }
+            }
             const float f = parts ? 1.0f : (l > 0.0f ? 1.0f / l : l);
             const uint32_t stage = own + half * (P::tile / 2) + (warp & 3) * (P::tile / 8);
             constexpr int VR = DP / 16;                                                  // 16-byte vectors of a staged row
@@ -428,7 +452,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
                 if (parts) row_at = reinterpret_cast<char*>(j.partial + (split * all_rows + (int64_t)(q.q0 + tok) * heads + h * st.group + g) * st.head_dim);
                 else row_at = j.out.base + 2 * ((int64_t)(q.q0 + tok) * j.out.row + (int64_t)(h * st.group + g) * j.out.head);
             }
-            for (int pass = 0; pass < (parts ? 2 : 1); ++pass) {
+            for (int pass = 0; pass < (cluster ? 0 : parts ? 2 : 1); ++pass) {
 #pragma unroll
                 for (int b = 0; b < DP / 32; ++b) {
                     // 16 columns: two vectors of 16-bit numbers, or four of binary32
@@ -472,6 +496,45 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
     __syncthreads();
     tc_fence_after();
     if (warp == kIssuer) tmem_dealloc(tmem, P::columns);
+    if (!cluster) return;
+    // The cluster's CTAs share out the rows, four dims to a thread, and read one another's parts in order.
+    cluster_sync();
+    const int32_t share = (rows + j.splits - 1) / j.splits, row_end = min(rows, (split + 1) * share);
+    for (int32_t v = threadIdx.x; v < share * (DP / 4); v += P::threads) {
+        const int32_t x = split * share + v / (DP / 4), d = v % (DP / 4);
+        if (x >= row_end || 4 * d >= st.head_dim) continue;
+        float2 ml[kCluster];
+        float4 p[kCluster];
+        float M = kNone, L = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kCluster; ++k) {
+            ml[k] = make_float2(kNone, 0.0f);
+            p[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (k < j.splits) {
+                ml[k] = cluster_ld2(cluster_at(base + P::part_ml + 8 * x, k));
+                p[k] = cluster_ld4(cluster_at(base + P::part + x * DP * 4 + ((d ^ (x & 7)) << 4), k));
+            }
+            M = fmaxf(M, ml[k].x);
+        }
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < kCluster; ++k) {
+            const float f = ml[k].y == 0.0f ? 0.0f : exp2_fast(ml[k].x - M);
+            L += f * ml[k].y;
+            o.x += f * p[k].x;
+            o.y += f * p[k].y;
+            o.z += f * p[k].z;
+            o.w += f * p[k].w;
+        }
+        int32_t g;
+        const int32_t tok = q.q0 + token_of(st, row0 + x, g), head = h * st.group + g;
+        const float inv = L > 0.0f ? 1.0f / L : L;
+        *reinterpret_cast<uint2*>(j.out.base + 2 * ((int64_t)tok * j.out.row + (int64_t)head * j.out.head + 4 * d)) =
+            make_uint2(N::pack(o.x * inv, o.y * inv), N::pack(o.z * inv, o.w * inv));
+        if (d == 0 && j.lse) j.lse[(int64_t)tok * (st.kv_heads * st.group) + head] = L == 0.0f ? kNone : (M + log2f(L)) * 0.69314718055994531f;
+    }
+    // no CTA leaves while another may read its parts
+    cluster_sync();
 }
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -530,8 +593,18 @@ cudaError_t attend_tc(const AttendJob& j, cudaStream_t s) {
     CUtensorMap km{}, vm{}, qm{};
     const bool boxes = plane_map(&km, j.step, j.k_plane, HALF) && plane_map(&vm, j.step, j.v_plane, HALF), q_boxes = rows_map(&qm, j.step, j.q, HALF);
     const int64_t rows = TILES * tile_rows_of(j.step.group), tiles = ((int64_t)j.step.max_q * j.step.group + rows - 1) / rows;
-    k<<<dim3((unsigned)(tiles * j.splits), j.step.kv_heads, j.step.requests), P::threads, P::bytes, s>>>(j, km, vm, qm, boxes, q_boxes);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(tiles * j.splits), j.step.kv_heads, j.step.requests);
+    cfg.blockDim = dim3(P::threads);
+    cfg.dynamicSmemBytes = P::bytes;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = j.splits;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = j.cluster;
+    return cudaLaunchKernelEx(&cfg, k, j, km, vm, qm, (int32_t)boxes, (int32_t)q_boxes);
 }
 
 template <bool HALF>

@@ -109,6 +109,25 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
+// Of shared memory in the cluster's CTA `rank`, at this CTA's address.
+__device__ __forceinline__ uint32_t cluster_at(uint32_t addr, int rank) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ float2 cluster_ld2(uint32_t at) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 cluster_ld4(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+// All threads of all of the cluster's CTAs; what they wrote before is seen behind it.
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory"); }
+
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
     const int n = there ? 16 : 0;      // 0: the 16 bytes become zeros, src is not read
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(n) : "memory");

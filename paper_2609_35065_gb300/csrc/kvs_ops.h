@@ -92,6 +92,7 @@ inline __host__ __device__ int32_t tile_rows_of(int32_t group) { return group <=
 struct AttendPlan {
     int tc, splits, row_tiles, cluster;
 };
+constexpr int kCluster = 8;            // most parts that a cluster joins
 AttendPlan attend_plan(const StepView& st, int sms);
 // A plane's TMA map (a CUtensorMap at `map`) in boxes of whole blocks, or of 128 tokens of one,
 // of one head's 64 elements; false where blocks do not tile 128 tokens (kvs_attend_tc.cu).

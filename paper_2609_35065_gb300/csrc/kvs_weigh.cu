@@ -377,20 +377,19 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         if (mine_to_write) add_weight(j, r, h, key, sums[at_sum] + sums[at_sum + 128]);
         return;
     }
-    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    cluster_sync();
     if (rank == 0 && mine_to_write) {
         float x = 0.0f;
         for (int32_t k = 0; k < share; ++k) {
-            uint32_t at;
+            const uint32_t at = cluster_at(base + P::sums + 4 * at_sum, k);
             float u, v;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(base + P::sums + 4 * at_sum), "r"(k));
             asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u) : "r"(at) : "memory");
             asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at + 512) : "memory");
             x += u + v;
         }
         add_weight(j, r, h, key, x);
     }
-    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    cluster_sync();
 }
 
 // ---------------------------------------------------------------------------

@@ -379,3 +379,11 @@ def test_weights_of_wide_groups(G, D, dtype):
         want, bound = sm.weigh(z.numpy(), before, float(np.float32(0.9)), D ** -0.5)
         off = np.abs(w.double().cpu().numpy() - want)
         assert (off <= bound).all(), (off - bound).max()
+
+
+@pytest.mark.parametrize("new,lens,window", [([1], [1000], 0), ([3], [2500], 0), ([1, 1], [5000, 0], 0), ([2, 0, 1], [900, 3000, 40], 0), ([2], [4000], 300), ([5], [3], 0),
+                                             ([30], [2000], 0), ([64, 9], [1500, 700], 0), ([100], [5000], 333), ([20, 70], [0, 2600], 0), ([250], [900], 0)])
+@pytest.mark.parametrize("G,D,dtype", [(1, 8, "f16"), (4, 64, "bf16"), (5, 80, "bf16"), (7, 128, "f16"), (3, 120, "f16")])
+def test_one_head_in_parts(new, lens, window, G, D, dtype):
+    """Few heads: a head's keys are split, some of the parts see nothing of some rows, or are empty."""
+    _check_attend(Small(new, lens, 1, G, D, dtype=dtype), window=window)
