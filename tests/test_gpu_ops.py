@@ -387,3 +387,98 @@ def test_weights_of_wide_groups(G, D, dtype):
 def test_one_head_in_parts(new, lens, window, G, D, dtype):
     """Few heads: a head's keys are split, some of the parts see nothing of some rows, or are empty."""
     _check_attend(Small(new, lens, 1, G, D, dtype=dtype), window=window)
+
+
+@pytest.mark.parametrize("kind", ["random", "ties"])
+def test_evict_from_caches_of_more_than_16384_tokens(kind):
+    lens, budget, B = [20000, 16385, 300], 5000, 16
+    Wd = -(-budget // B)
+    sm = Small([0] * 3, lens, 2, 1, 8, B, extra_blocks=3 * Wd)
+    step, _, _, _, cache = sm.on_gpu(kvs)
+    w = np.random.default_rng(4).random((1, 3, 2, step.max_kv)).astype(np.float32)
+    if kind == "ties":
+        w = np.floor(w * 3).astype(np.float32)
+    free = np.setdiff1d(np.arange(sm.num_blocks), sm.tables.numpy().ravel())
+    dst = torch.from_numpy(free[: 3 * Wd].reshape(3, Wd).astype(np.int32))
+    kept = torch.full((1, 3, 2, budget), -7, dtype=torch.int32, device="cuda")
+    nw, nl = torch.full(kept.shape, -7.0, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    kvs.kvs_evict(step, torch.from_numpy(w).cuda(), dst.cuda(), budget, 4, 100, kept, nw, nl, None, kvs.KVS_F_VALIDATE)
+    want = ops_ref.evict(w, lens, budget, 4, 100)
+    assert (kept.cpu().numpy() == want).all() and nl.tolist() == [5000, 5000, 300]
+    flat = cache.view(2, -1, 2, 8)
+    for r in range(3):
+        j = np.arange(min(lens[r], budget))
+        to = torch.from_numpy(dst[r].numpy().astype(np.int64)[j // B] * B + j % B).cuda()
+        for h in range(2):
+            assert (nw[0, r, h, : len(j)].cpu().numpy() == w[0, r, h, want[0, r, h, : len(j)]]).all()
+            at = torch.from_numpy(sm.slots(r, want[0, r, h, : len(j)])).cuda()
+            assert torch.equal(flat[:, to, h], flat[:, at, h])
+
+
+@pytest.mark.parametrize("new,lens", [([1, 2], [600, 33]), ([30, 1], [600, 33]), ([200, 130], [600, 200])])
+def test_offsets_beyond_32_bits(new, lens):
+    """Blocks at the end of planes of more than 2^31 elements: what the same blocks give in small planes."""
+    sm = Small(new, lens, 8, 4, 128, extra_blocks=60)
+    step, q, k, v, cache = sm.on_gpu(kvs)
+    NB = (1 << 31) // (16 * 8 * 128) + 200
+    shift = NB - sm.num_blocks
+    far = torch.empty(2, NB, 16, 8, 128, dtype=cache.dtype, device="cuda")
+    far[:, shift:] = cache
+    tables, kv_lens, starts = step._keep[:3]
+    step2 = kvs.Step((1, 8, 128, 2, 16, 16), [far[0].data_ptr(), far[1].data_ptr()], NB, tables + shift, kv_lens, starts, total_q=sm.N, max_q=max(new))
+    free = np.setdiff1d(np.arange(sm.num_blocks), sm.tables.numpy().ravel())[:20].reshape(2, 10)
+    dst = torch.from_numpy(free.astype(np.int32)).cuda()
+    got = []
+    for s, d in ((step, dst), (step2, dst + shift)):
+        kvs.kvs_append(s, 0, None, k, v)
+        out, z = torch.empty(q.shape, dtype=q.dtype, device="cuda"), torch.empty(q.shape[:2], device="cuda")
+        kvs.kvs_attend(s, 0, q, out, z, workspace=torch.empty(kvs.kvs_attend_workspace(s, 32), dtype=torch.uint8, device="cuda"))
+        w = torch.zeros(1, 2, 8, s.max_kv, device="cuda")
+        kvs.kvs_weigh(s, 0, q, z, w[0])
+        kept = torch.empty(1, 2, 8, 160, dtype=torch.int32, device="cuda")
+        kvs.kvs_evict(s, w, d, 160, 4, 8, kept, flags=kvs.KVS_F_VALIDATE)
+        got.append((out, z, w, kept))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert torch.equal(far[:, shift:].view(torch.int16), cache.view(torch.int16))
+
+
+def test_a_graph_of_a_decode_step():
+    """Append, attention in parts, weights and eviction, captured once and replayed after the lengths changed."""
+    sm = Small([1, 1], [4000, 900], 1, 4, 64, extra_blocks=60)
+    step, q, k, v, cache = sm.on_gpu(kvs, decode=True)
+    q = q.contiguous()
+    out, z = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    ws = torch.zeros(kvs.kvs_attend_workspace(step, 4) + 16, dtype=torch.uint8, device="cuda")
+    w = torch.zeros(1, 2, 1, step.max_kv, device="cuda")
+    free = np.setdiff1d(np.arange(sm.num_blocks), sm.tables.numpy().ravel())[:20].reshape(2, 10)
+    dst, kept = torch.from_numpy(free.astype(np.int32)).cuda(), torch.zeros(1, 2, 1, 160, dtype=torch.int32, device="cuda")
+
+    def run(s):
+        kvs.kvs_append(step, 0, None, k, v, stream=s)
+        kvs.kvs_attend(step, 0, q, out, z, workspace=ws, stream=s)
+        kvs.kvs_weigh(step, 0, q, z, w[0], decay=0.0, stream=s)
+        kvs.kvs_evict(step, w, dst, 160, 4, 8, kept, stream=s)
+
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    run(s)
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        run(torch.cuda.current_stream())
+    for lengths in ([4000, 900], [3999, 1], [0, 700]):
+        step._keep[1].copy_(torch.tensor(lengths, dtype=torch.int32))
+        run(s)
+        s.synchronize()
+        want = [x.clone() for x in (out, z, w, kept, cache)]
+        for x in (out, z, w, kept):
+            x.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for x, y in zip((out, z, kept), want[:2] + want[3:4]):
+            assert torch.equal(x, y)
+        for r, T in enumerate(lengths):
+            assert torch.equal(w[:, r, :, :T], want[2][:, r, :, :T])
+        assert torch.equal(cache.view(torch.int16), want[4].view(torch.int16))
