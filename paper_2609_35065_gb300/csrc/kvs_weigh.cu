@@ -30,14 +30,17 @@ __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t
 }
 
 // ---------------------------------------------------------------------------
-// Many rows: S^T = K Q^T on the tensor cores, two tiles of 128 keys (the accumulators' lanes)
-// per CTA and the rows in tiles of at most 128 (their columns), so that a thread sums its key's
-// weights in registers.  The keys stay in tensor memory: read from shared memory for every
+// Many rows: S^T = K Q^T on the tensor cores, one or two tiles of 128 keys (the accumulators'
+// lanes) per CTA and the rows in tiles of at most 128 (their columns), so that a thread sums its
+// key's weights in registers.  The keys stay in tensor memory: read from shared memory for every
 // product they took as much of its 128 bytes a cycle as the rows, and both together all of it.
-// Two warpgroups share a key tile, half of each row tile's columns to each; in the fifth
+// Two warpgroups share a key tile, half of each row tile's columns to each; in the last
 // warpgroup one warp issues the products, one loads the next row tiles (TMA boxes of whole
 // tokens; cp.async by three warps where the rows have no such boxes) and two their lse, in a
 // ring of its own: a tile's rows are done with when the products are, its lse with the sums.
+//
+// Two CTAs of one key tile share an SM, and while one starts or ends the other works; of many row
+// tiles, two key tiles read each of them once for both.
 //
 // 128 x 128 scores take the tensor cores about 570 cycles and the exponentials 512; what bounds
 // it is their hand-over, some 850 cycles: 5120 rows against 13312 keys of 8 heads of 128 dims
@@ -49,26 +52,31 @@ __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t
 // Where there are fewer key tiles than SMs, a cluster of CTAs shares a key tile's row tiles
 // and joins its sums, in the CTAs' order, through distributed shared memory.
 // ---------------------------------------------------------------------------
-constexpr int kThreads = 640, kStages = 4, kAccs = 3, kSlots = 8, kKeysTc = 256;
+constexpr int kSlots = 8;
 
-template <int DP>
+// KT: key tiles of a CTA.
+template <int DP, int KT>
 struct WPlan {
+    static constexpr int issuer = 8 * KT;                        // the issuing warp, behind the sums'; then the loading ones
+    static constexpr int threads = 32 * (issuer + 4), keys = 128 * KT;
+    static constexpr int stages = KT == 2 ? 4 : 2, accs = KT == 2 ? 3 : 1, columns = 256 * KT;
     static constexpr int tile = 128 * DP * 2;
-    static constexpr int lse = tile * (2 + kStages);             // [kSlots][128] binary32, times -log2(e)
-    static constexpr int sums = lse + kSlots * 512;              // [2][2][128]
-    static constexpr int bars = sums + 2048;
+    static constexpr int lse = tile * (KT + stages);             // [kSlots][128] binary32, times -log2(e)
+    static constexpr int sums = lse + kSlots * 512;              // [KT][2][128]
+    static constexpr int bars = sums + 1024 * KT;
     static constexpr int bytes = bars + 512 + 1024;
 };
 
-template <bool HALF, int DP>
-__global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap k_map,
+template <bool HALF, int DP, int KT>
+__global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap k_map,
                                                                    const __grid_constant__ CUtensorMap q_map, int32_t k_boxes, int32_t q_boxes, int32_t share) {
     extern __shared__ char raw[];
-    using P = WPlan<DP>;
+    using P = WPlan<DP, KT>;
+    constexpr int kThreads = P::threads, kStages = P::stages, kAccs = P::accs, kKeysTc = P::keys, kIssuer = P::issuer;
     const StepView& st = j.step;
     const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
     char* mem = raw + (base - smem_u32(raw));
-    const uint32_t ring = base + 2 * P::tile, ctl = base + P::bars;
+    const uint32_t ring = base + KT * P::tile, ctl = base + P::bars;
     const uint32_t b_k = ctl, b_full = ctl + 8, b_free = b_full + 8 * kStages, b_s = b_free + 8 * kStages, b_e = b_s + 8 * kAccs, b_done = b_e + 8 * kAccs,
                    b_load = b_done + 8, b_lse = b_load + 8, b_read = b_lse + 8 * kSlots, tmem_at = b_read + 8 * kSlots;
     const int warp = warp_number(), lane = threadIdx.x & 31, wg = warp >> 2;
@@ -77,7 +85,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
     if (t0 >= q.T) return;                                       // the whole cluster
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
     const int32_t per = tile_rows_of(st.group);                  // rows of a tile
-    const int32_t key_tiles = t0 + 128 < q.T ? 2 : 1;
+    const int32_t key_tiles = KT == 2 && t0 + 128 < q.T ? 2 : 1;
     const RowSpan any = rows_seeing(st, q, t0, min(t0 + kKeysTc, q.T) - 1, j.causal, j.window);
     const int32_t tile0 = any.first / per, tiles = any.end > any.first ? (any.end + per - 1) / per - tile0 : 0;
     const int32_t mine = (tiles - rank + share - 1) / share;     // row tiles tile0 + rank + share * i
@@ -85,7 +93,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
 
     if (threadIdx.x == 0) {
         mbar_init(b_load, 3 * key_tiles);
-        mbar_init(b_k, 16);
+        mbar_init(b_k, 8 * KT);
         for (int i = 0; i < kStages; ++i) {
             mbar_init(b_full + 8 * i, q_boxes ? 1 : 3);          // the loading warps
             mbar_init(b_free + 8 * i, 1);
@@ -101,11 +109,11 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         mbar_init(b_done, 1);
         mbar_init_fence();
     }
-    if (warp == 16) tmem_alloc(tmem_at, 512);
+    if (warp == kIssuer) tmem_alloc(tmem_at, P::columns);
     // rows that no box fills are zeros for good, and weigh nothing
     for (int i = threadIdx.x; i < (128 - per) * (DP / 8) * kStages; i += kThreads) {
         const int stage = i / ((128 - per) * (DP / 8)), v = i % ((128 - per) * (DP / 8)), row = per + v / (DP / 8), c = v % (DP / 8);
-        *reinterpret_cast<uint4*>(mem + P::tile * (2 + stage) + (c >> 3) * 128 * 128 + row * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(mem + P::tile * (KT + stage) + (c >> 3) * 128 * 128 + row * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
     }
     fence_async_smem();
     tc_fence_before();
@@ -121,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
 
     float sum = 0.0f;
     const int t = threadIdx.x & 127;
-    if (warp == 16) {
+    if (warp == kIssuer) {
         // ---- the products: the warp waits together, one lane issues ----------------------
         constexpr uint32_t id = tc_idesc(HALF, 128, false);
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), keys = tm + 128 * kAccs;     // 64 columns to a key tile
@@ -160,9 +168,9 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
             mbar_wait(b_done, 0, kWaitLimitNs);
         }
         __syncwarp();
-    } else if (warp > 16) {
-        // ---- loads: warp 9 the rows, warps 10 and 11 their lse; by rows all three both ------
-        const int u = threadIdx.x - 17 * 32;                     // 0 to 95
+    } else if (warp > kIssuer) {
+        // ---- loads: one warp the rows, two their lse; by rows all three both ------
+        const int u = threadIdx.x - (kIssuer + 1) * 32;                     // 0 to 95
         uint32_t pending = 0;
         auto announce = [&]() {
             fence_async_smem();
@@ -172,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         };
         if (mine > 0) {
             for (int32_t kt = 0; kt < key_tiles; ++kt) {
-                if (k_boxes) tile_boxes<DP>(base + kt * P::tile, &k_map, st, h, box_of<DP, 3>(st, table, t0 + 128 * kt, q.T, warp - 17, lane), b_load, lane);
+                if (k_boxes) tile_boxes<DP>(base + kt * P::tile, &k_map, st, h, box_of<DP, 3>(st, table, t0 + 128 * kt, q.T, warp - kIssuer - 1, lane), b_load, lane);
                 else tile_rows<DP, 96>(base + kt * P::tile, j.k_plane, st, table, h, t0 + 128 * kt, 0, q.T, u);
             }
             if (!k_boxes) {
@@ -215,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
                 ++round;
             }
         };
-        if (q_boxes && warp > 17) {
+        if (q_boxes && warp > kIssuer + 1) {
             // four tiles' lse ahead of the four that are announced: a load takes longer than a tile
             float now[4][2], next[4][2];
 #pragma unroll
@@ -287,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
         if (pending) announce();
         // every load has landed when its sums are done; after a failure, wait for them here
         if (mine > 0) mbar_wait(b_load, 0, kWaitLimitNs);
-        if (i < mine && warp == 17)
+        if (i < mine && warp == kIssuer + 1)
             for (int k = i < kStages ? 0 : i - kStages; k < i; ++k) mbar_wait(b_full + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs);
     } else {
         // ---- sums: a key to a thread ---------------------------------------------------
@@ -368,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_weigh_tc_kernel(WeighJob j, c
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 16) tmem_dealloc(tmem, 512);
+    if (warp == kIssuer) tmem_dealloc(tmem, P::columns);
     const float* sums = reinterpret_cast<const float*>(mem + P::sums);        // [key tile][half][128]
     const int32_t at_sum = (threadIdx.x >> 7) * 256 + t;
     const int32_t key = t0 + (int32_t)threadIdx.x;               // of the first 256 threads: key tile by key tile
@@ -540,13 +548,40 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
     }
 }
 
+template <bool HALF, int DP, int KT>
+cudaError_t weigh_tc(const WeighJob& j, int sms, cudaStream_t s) {
+    using P = WPlan<DP, KT>;
+    const StepView& st = j.step;
+    const int64_t rows = (int64_t)st.max_q * st.group;
+    auto* k = kvs_weigh_tc_kernel<HALF, DP, KT>;
+    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, P::bytes);
+    if (e != cudaSuccess) return e;
+    CUtensorMap km{}, qm{};
+    const bool k_boxes = plane_map(&km, st, j.k_plane, HALF), q_boxes = rows_map(&qm, st, j.q, HALF);
+    const int64_t x = (st.max_kv + P::keys - 1) / P::keys, tiles = x * st.kv_heads * st.requests, row_tiles = (rows + 127) / 128;
+    int share = 1;
+    while (share < 8 && tiles * share * 2 <= sms && share * 2 <= row_tiles) share *= 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(x * share), st.kv_heads, st.requests);
+    cfg.blockDim = dim3(P::threads);
+    cfg.dynamicSmemBytes = P::bytes;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = share;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = share > 1;
+    return cudaLaunchKernelEx(&cfg, k, j, km, qm, (int32_t)k_boxes, (int32_t)q_boxes, (int32_t)share);
+}
+
 template <bool HALF, int DP>
 cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     const StepView& st = j.step;
     const int64_t rows = (int64_t)st.max_q * st.group;
-    // Up to 48 rows: 8 requests x 8 heads of 128 dims with 8000 tokens take 68 us at 32 rows (on the
-    // tensor cores' kernel 97), 90 at 48 (97) and 112 at 64 (92); of 64 dims 54 (90), 70 (90), 85 (82).
-    if (rows <= 48) {
+    // Up to 32 rows: 8 requests x 8 heads of 128 dims with 8000 tokens take 68 us at 32 rows and 90 at
+    // 48 (on the tensor cores' kernel 72); of 64 dims 54 and 70 (66).
+    if (rows <= 32) {
         // CTAs for two rounds of two to an SM (weigh of a decode step: one round 45.2 us, two 40.5,
         // three 41.1, six 45.1), but not more than leave a warp four tiles.
         const int64_t pairs = (int64_t)st.kv_heads * st.requests, most = (st.max_kv + kRowWarps * kRowKeys * 4 - 1) / (kRowWarps * kRowKeys * 4);
@@ -558,26 +593,9 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
         else kvs_weigh_rows_kernel<HALF, DP, 0><<<grid, kRowWarps * 32, 0, s>>>(j);
         return cudaGetLastError();
     }
-    auto* k = kvs_weigh_tc_kernel<HALF, DP>;
-    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, WPlan<DP>::bytes);
-    if (e != cudaSuccess) return e;
-    CUtensorMap km{}, qm{};
-    const bool k_boxes = plane_map(&km, st, j.k_plane, HALF), q_boxes = rows_map(&qm, st, j.q, HALF);
-    const int64_t x = (st.max_kv + kKeysTc - 1) / kKeysTc, tiles = x * st.kv_heads * st.requests, row_tiles = (rows + 127) / 128;
-    int share = 1;
-    while (share < 8 && tiles * share * 2 <= sms && share * 2 <= row_tiles) share *= 2;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(x * share), st.kv_heads, st.requests);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = WPlan<DP>::bytes;
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = share;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = share > 1;
-    return cudaLaunchKernelEx(&cfg, k, j, km, qm, (int32_t)k_boxes, (int32_t)q_boxes, (int32_t)share);
+    // One key tile to a CTA up to 2560 rows: against 8000 tokens of 8 requests x 8 heads of 128 dims 64 rows
+    // take 72 us (two tiles: 92), 256 79 (99), 1024 149 (167), 2048 250 (261), 4096 467 (450).
+    return rows <= 2560 ? weigh_tc<HALF, DP, 1>(j, sms, s) : weigh_tc<HALF, DP, 2>(j, sms, s);
 }
 
 }  // namespace

@@ -482,3 +482,17 @@ def test_a_graph_of_a_decode_step():
         for r, T in enumerate(lengths):
             assert torch.equal(w[:, r, :, :T], want[2][:, r, :, :T])
         assert torch.equal(cache.view(torch.int16), want[4].view(torch.int16))
+
+
+@pytest.mark.parametrize("new,T,G,D,dtype", [(650, 900, 4, 128, "bf16"), (645, 645, 4, 64, "f16"), (300, 1000, 9, 80, "bf16")])
+def test_weights_of_long_chunks(new, T, G, D, dtype):
+    """More rows than a small grid of key tiles has, around where a CTA takes two of them."""
+    sm = Small([new, 3], [T, 130], 1, G, D, dtype=dtype)
+    z = torch.from_numpy(sm.attend(D ** -0.5)[2].astype(np.float32))
+    step, q, _, _, _cache = sm.on_gpu(kvs)
+    before = np.random.default_rng(6).random((2, 1, step.max_kv)).astype(np.float32)
+    w = torch.from_numpy(before).cuda()
+    kvs.kvs_weigh(step, 0, q, z.cuda(), w, decay=0.5, flags=kvs.KVS_F_VALIDATE)
+    want, bound = sm.weigh(z.numpy(), before, 0.5, D ** -0.5)
+    off = np.abs(w.double().cpu().numpy() - want)
+    assert (off <= bound).all(), (off - bound).max()
