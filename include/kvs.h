@@ -493,7 +493,8 @@ int kvs_retrieve_noalloc(const kvs_geometry* geom, const kvs_paged_cache* cache,
 /* The requests of one forward step.  Request r's new tokens are rows q_starts[r] up to
  * q_starts[r + 1] of the step's tensors; kv_lens[r] tokens are in its cache, the new ones
  * (the last) among them.  Token t of request r is in slot
- * block_tables[r * table_stride + t / B] * B + t % B. */
+ * block_tables[r * table_stride + t / B] * B + t % B.  A step without requests does nothing,
+ * whatever total_q is: its arrays are not read. */
 typedef struct kvs_step {
     const int32_t* block_tables;    /* device [num_requests][table_stride]              */
     const int32_t* kv_lens;         /* device [num_requests]                            */

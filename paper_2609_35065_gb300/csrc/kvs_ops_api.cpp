@@ -162,7 +162,8 @@ int append_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
         j.interleaved = r.interleaved != 0;
         j.scale = r.scale;
     }
-    if (st->total_q == 0) return KVS_OK;
+    // without a request nothing is read of the step's arrays, which may have no entry
+    if (st->total_q == 0 || st->num_requests == 0) return KVS_OK;
     if (a->q.base) {
         KVS_TRY(rows_of(a->q, st->total_q, a->num_q_heads, "q", j.q));
         KVS_TRY(rows_of(a->q_out, st->total_q, a->num_q_heads, "q_out", j.q_out));

@@ -265,3 +265,11 @@ def test_the_extension_leaves_what_is_not_plain_to_the_binding():
 @pytest.mark.parametrize("op,path,value", [(o, "step.max_kv", (1 << 30) + 1) for o in ("append", "attend", "weigh", "evict")] + [("evict", "evict.budget", (1 << 30) + 1)])
 def test_positions_above_30_bits_are_refused(op, path, value):
     test_refusals(op, path, value, U)
+
+
+@pytest.mark.parametrize("op", ["append", "attend", "weigh", "evict"])
+def test_rows_without_a_request_need_no_device(op):
+    """An empty batch in tensors padded to a fixed number of rows: no array of the step has an entry to read."""
+    c = Call()
+    c.step.num_requests, c.step.kv_lens, c.step.block_tables = 0, None, None
+    assert c.run(op) == kvs.KVS_OK, kvs.kvs_last_error()
