@@ -482,7 +482,8 @@ int kvs_retrieve_noalloc(const kvs_geometry* geom, const kvs_paged_cache* cache,
  * A length, row range or block id outside the stated bounds is not followed: what it
  * concerns is left out (cached tokens read as zeros, output rows are left undefined) and
  * KVS_ERR_BOUNDS recorded for kvs_check_errors().  With KVS_F_VALIDATE (the only flag)
- * a call synchronises the stream and returns that code itself.
+ * a call synchronises the stream and returns that code itself.  Without it a call waits for
+ * no other thread's retrieval or store-back.
  *
  * geom->elem_bytes must be 2, head_dim a multiple of 8 up to 128, and every address and
  * stride a multiple of 16 bytes (KVS_ERR_UNSUPPORTED otherwise); chunk_tokens is unused.

@@ -18,6 +18,7 @@
 //                              one 2D copy per (chunk, block) across all planes
 //                              (equally spaced planes only; no SMs used).
 #include <algorithm>
+#include <atomic>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -123,7 +124,17 @@ struct DevState {
 
 std::mutex g_mu;
 std::vector<DevState> g_dev;
-int64_t g_launches = 0;
+std::atomic<int64_t> g_launches{0};
+
+// What the model operators need of a device's state, read without g_mu: a retrieval holds that
+// lock while it waits for an upload slot, and a decode step must not wait with it.  Written
+// under g_mu; err is not NULL from the device's first call until kvs_shutdown.
+struct OpsDevice {
+    std::atomic<int32_t*> err{nullptr};
+    std::atomic<int>      sms{0};
+};
+constexpr int kOpsDevices = 64;       // devices beyond take the lock
+OpsDevice g_ops_dev[kOpsDevices];
 
 int get_state(DevState** out) {
     int dev = 0;
@@ -178,6 +189,10 @@ int get_state(DevState** out) {
         st.report.chosen_store_host = st.store_host;
         st.report.chosen_kernel_device = st.kernel_device;
         st.ready = true;
+        if (dev < kOpsDevices) {
+            g_ops_dev[dev].sms.store(st.sms, std::memory_order_relaxed);
+            g_ops_dev[dev].err.store(st.err, std::memory_order_release);
+        }
     }
     *out = &st;
     return KVS_OK;
@@ -1395,6 +1410,12 @@ int hostlink_grid(bool retrieve) {
 }
 
 int ops_device(int32_t** err, int* sms) {
+    int dev = 0;
+    KVS_CUDA(cudaGetDevice(&dev));
+    if (dev < kOpsDevices && (*err = g_ops_dev[dev].err.load(std::memory_order_acquire))) {
+        *sms = g_ops_dev[dev].sms.load(std::memory_order_relaxed);
+        return KVS_OK;
+    }
     std::lock_guard<std::mutex> lk(g_mu);
     DevState* st = nullptr;
     const int rc = get_state(&st);
@@ -1404,10 +1425,7 @@ int ops_device(int32_t** err, int* sms) {
     return KVS_OK;
 }
 
-void ops_launched(int n) {
-    std::lock_guard<std::mutex> lk(g_mu);
-    g_launches += n;
-}
+void ops_launched(int n) { g_launches += n; }
 
 int ops_read_error(cudaStream_t s) {
     std::lock_guard<std::mutex> lk(g_mu);
@@ -1572,6 +1590,7 @@ int kvs_shutdown(void) {
         cudaGetDevice(&prev);
         for (auto& st : g_dev) {
             if (!st.ready) continue;
+            if (st.device < kOpsDevices) g_ops_dev[st.device].err.store(nullptr, std::memory_order_release);
             cudaSetDevice(st.device);
             cudaDeviceSynchronize();
             for (auto& sl : st.up) {
@@ -1610,10 +1629,7 @@ int kvs_shutdown(void) {
 
 int kvs_version(void) { return KVS_VERSION; }
 
-int64_t kvs_stat_launches(void) {
-    std::lock_guard<std::mutex> lk(g_mu);
-    return g_launches;
-}
+int64_t kvs_stat_launches(void) { return g_launches; }
 
 int kvs_selftest_wait_timeout(void* cuda_stream, int64_t limit_ns) {
     std::lock_guard<std::mutex> lk(g_mu);

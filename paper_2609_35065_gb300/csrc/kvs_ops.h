@@ -102,7 +102,8 @@ bool plane_map(void* map, const StepView& st, const void* plane, bool half);
 bool rows_map(void* map, const StepView& st, const RowsView& rows, bool half);
 cudaError_t launch_attend_tc(const AttendJob& j, bool half, cudaStream_t s);
 
-// The current device's error word and number of SMs (kvs_api.cpp); allocates them at the first call.
+// The current device's error word and number of SMs (kvs_api.cpp); allocates them at the first call,
+// and takes no lock later.
 int ops_device(int32_t** err, int* sms);
 // Counts kernels for kvs_stat_launches.
 void ops_launched(int n);
