@@ -37,7 +37,8 @@ int entry(F&& f) {
     }
 }
 
-int view_of(const kvs_geometry* g, const kvs_step* s, int32_t q_heads, StepView& v) {
+// rowless: the call uses no row of the step, which may then have none.
+int view_of(const kvs_geometry* g, const kvs_step* s, int32_t q_heads, StepView& v, bool rowless = false) {
     if (!g) return ops_fail(KVS_ERR_INVALID_ARG, "geometry is NULL");
     if (g->num_layers <= 0 || g->num_kv_heads <= 0 || g->head_dim <= 0)
         return ops_fail(KVS_ERR_INVALID_ARG, "layers, kv heads and head dim must be positive");
@@ -58,7 +59,8 @@ int view_of(const kvs_geometry* g, const kvs_step* s, int32_t q_heads, StepView&
     if (s->num_requests > 0 && s->max_kv > 0 && !s->block_tables) return ops_fail(KVS_ERR_INVALID_ARG, "block_tables is NULL");
     if ((int64_t)s->table_stride * g->block_size < s->max_kv)
         return ops_fail(KVS_ERR_BOUNDS, "tables of %d blocks of %d tokens do not hold max_kv = %d", s->table_stride, g->block_size, s->max_kv);
-    if (!s->q_starts && (s->total_q != s->num_requests || (s->num_requests > 0 && s->max_q < 1)))
+    const bool no_rows = rowless && s->total_q == 0 && s->max_q == 0;
+    if (!s->q_starts && !no_rows && (s->total_q != s->num_requests || (s->num_requests > 0 && s->max_q < 1)))
         return ops_fail(KVS_ERR_INVALID_ARG, "without q_starts a step has one row per request");
     if (s->max_q > s->total_q) return ops_fail(KVS_ERR_INVALID_ARG, "max_q (%d) is above total_q (%d)", s->max_q, s->total_q);
     if (q_heads >= 0 && (q_heads == 0 || q_heads % g->num_kv_heads))
@@ -258,7 +260,7 @@ int weigh_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* 
 int evict_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* st, const kvs_evict_args* a, cudaStream_t s, uint32_t flags) {
     if (!a) return ops_fail(KVS_ERR_INVALID_ARG, "args is NULL");
     EvictJob j{};
-    KVS_TRY(view_of(g, st, -1, j.step));
+    KVS_TRY(view_of(g, st, -1, j.step, true));
     KVS_TRY(cache_of(g, c, 0, 2 * g->num_layers, j.step));
     KVS_TRY(flags_of(flags));
     if (a->budget < 1) return ops_fail(KVS_ERR_INVALID_ARG, "budget must be positive");

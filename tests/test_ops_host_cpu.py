@@ -97,3 +97,21 @@ def test_operators_after_a_shutdown(library):
             assert _run(library, op, Call()) == kvs.KVS_OK
         assert library.kvs_shutdown() == kvs.KVS_OK
     assert _run(library, "attend", Call(), kvs.KVS_F_VALIDATE) == kvs.KVS_OK
+
+
+def _evict_rows(c, total_q, max_q):
+    c.step.q_starts, c.step.total_q, c.step.max_q = None, total_q, max_q
+    return c
+
+
+def test_eviction_needs_no_rows(library):
+    """kvs_evict uses no row of the step: without q_starts total_q may be 0, or one row per request."""
+    before = library.fake_ops()
+    for rows in ((0, 0), (2, 1)):
+        assert _run(library, "evict", _evict_rows(Call(), *rows)) == kvs.KVS_OK, library.kvs_last_error()
+    assert library.fake_ops() == before + 2
+    for rows in ((1, 1), (3, 1), (8, 5)):
+        assert _run(library, "evict", _evict_rows(Call(), *rows)) == kvs.KVS_ERR_INVALID_ARG
+    for op in ("append", "attend", "weigh"):
+        assert _run(library, op, _evict_rows(Call(), 0, 0)) == kvs.KVS_ERR_INVALID_ARG
+    assert library.fake_ops() == before + 2
