@@ -751,6 +751,8 @@ def kvs_attend(step: Step, layer: int, q, out, lse=None, scale: float | None = N
     if lse is not None:
         a.lse = _f32("lse", lse, q.shape[:2])
     if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace: must be contiguous")
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     a.scale, a.causal, a.window = scale, bool(causal), window
     g, c, s = step.refs

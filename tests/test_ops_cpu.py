@@ -273,3 +273,13 @@ def test_rows_without_a_request_need_no_device(op):
     c = Call()
     c.step.num_requests, c.step.kv_lens, c.step.block_tables = 0, None, None
     assert c.run(op) == kvs.KVS_OK, kvs.kvs_last_error()
+
+
+@pytest.mark.parametrize("spread", [lambda t: t.expand(1 << 20), lambda t: t.expand(64, 1 << 10), lambda t: t.new_zeros(2 << 20)[::2]])
+def test_a_workspace_with_fewer_bytes_than_entries_is_refused(spread):
+    """An expanded or strided tensor does not have numel() bytes behind its address."""
+    import torch
+    s = _step()
+    q = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="workspace"):
+        kvs.kvs_attend(s, 0, q, q.clone(), workspace=spread(torch.zeros(1, dtype=torch.uint8)))
