@@ -345,18 +345,21 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
     cluster_sync();
 }
 
-// Joins the splits' parts: a warp per row, whose lanes weigh a split each and whose loads of
-// the parts go out eight at a time.
+// Joins the splits' parts: a warp per row of a request, whose lanes weigh a split each and whose
+// loads of the parts go out eight at a time.  Rows of no request have no parts and are left alone.
+constexpr int kJoinWarps = 4;
 template <bool HALF>
-__global__ void __launch_bounds__(128) kvs_attend_join_kernel(AttendJob j) {
+__global__ void __launch_bounds__(32 * kJoinWarps) kvs_attend_join_kernel(AttendJob j) {
     const StepView& st = j.step;
     using N = Num<HALF>;
     const int32_t heads = st.kv_heads * st.group;
-    const int64_t all_rows = (int64_t)st.total_q * heads;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int64_t all_rows = (int64_t)st.total_q * heads, own = (int64_t)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
-    if (row >= all_rows) return;
+    // ranges and lengths were there before the parts' kernel began: no need to wait for it
+    const Request q = load_request(st, blockIdx.y);
     grid_wait();
+    if (own >= (int64_t)q.n * heads) return;
+    const int64_t row = (int64_t)q.q0 * heads + own;
     const float2* ml = reinterpret_cast<const float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim);
     float M = kNone;
     for (int k = lane; k < j.splits; k += 32) M = fmaxf(M, ml[k * all_rows + row].x);
@@ -465,10 +468,10 @@ int launch_attend(const AttendJob& j, bool half, cudaStream_t s) {
     if (e != cudaSuccess) return -(int)e;
     if (j.splits == 1 || j.cluster) return 1;
     // The join is launched programmatically: its CTAs are in place when the parts are done.
-    const int64_t rows = (int64_t)j.step.total_q * j.step.kv_heads * j.step.group;
+    const int64_t rows = (int64_t)j.step.max_q * j.step.kv_heads * j.step.group;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((rows + 3) / 4));
-    cfg.blockDim = dim3(128);
+    cfg.gridDim = dim3((unsigned)((rows + kJoinWarps - 1) / kJoinWarps), j.step.requests);
+    cfg.blockDim = dim3(32 * kJoinWarps);
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -496,3 +496,37 @@ def test_weights_of_long_chunks(new, T, G, D, dtype):
     want, bound = sm.weigh(z.numpy(), before, 0.5, D ** -0.5)
     off = np.abs(w.double().cpu().numpy() - want)
     assert (off <= bound).all(), (off - bound).max()
+
+
+def _in_padded_rows(sm, lead, trail):
+    """Step, q, k, v and cache of `sm` in tensors with rows before its first and behind its last request."""
+    step, q, k, v, cache = sm.on_gpu(kvs)
+    rows = lead + sm.N + trail
+    starts = step._keep[2] + lead
+    padded = kvs.Step((sm.L, sm.H, sm.D, 2, sm.B, sm.B), [cache[p].data_ptr() for p in range(2 * sm.L)], sm.num_blocks, step._keep[0], step._keep[1], starts,
+                      total_q=rows, max_q=max(sm.new + [0]), dtype=step.step.dtype)
+
+    def pad(x):
+        y = torch.full((rows, *x.shape[1:]), 3.0, dtype=x.dtype, device="cuda")
+        y[lead: lead + sm.N] = x
+        return y
+    return padded, pad(q), pad(k), pad(v), cache
+
+
+# the three ways to an output row: one part, parts joined by their cluster, parts joined by a kernel
+@pytest.mark.parametrize("new,lens,H,ways", [([1, 2], [100, 60], 2, "one"), ([40, 1], [120, 60], 8, "one"), ([1], [1000], 1, "cluster"), ([20], [1000], 1, "cluster"),
+                                             ([2, 1], [20000, 300], 1, "join"), ([140], [8200], 1, "join"), ([1, 140, 0], [5, 8200, 0], 1, "join")])
+def test_rows_of_no_request_keep_what_they_hold(new, lens, H, ways):
+    """Rows before q_starts[0] and behind its last entry are another call's."""
+    sm = Small(new, lens, H, 4, 128)
+    want, z_want = _attend(sm)
+    step, q, _, _, _cache = _in_padded_rows(sm, 3, 5)
+    need = kvs.kvs_attend_workspace(step, q.shape[1])
+    assert (need > 0) == (ways == "join")
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    z = torch.full(q.shape[:2], 7.0, device="cuda")
+    kvs.kvs_attend(step, 0, q, out, z, workspace=torch.full((need,), 255, dtype=torch.uint8, device="cuda"), flags=kvs.KVS_F_VALIDATE)
+    mine = slice(3, 3 + sm.N)
+    assert torch.equal(out[mine], want) and torch.equal(z[mine], z_want)
+    for x in (out, z):
+        assert (x[:3] == 7.0).all() and (x[3 + sm.N:] == 7.0).all()
