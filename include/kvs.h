@@ -479,6 +479,8 @@ int kvs_retrieve_noalloc(const kvs_geometry* geom, const kvs_paged_cache* cache,
  * serving loop keeps them: the calls read them on the GPU, plan nothing on the host,
  * allocate nothing, and can be captured into a graph.  Calls are enqueued on the
  * caller's stream and return; tensors must stay valid until the stream has passed them.
+ * Rows of the step's tensors that belong to no request (before q_starts[0], behind its last
+ * entry) are not written, and what they hold does not matter.
  * A length, row range or block id outside the stated bounds is not followed: what it
  * concerns is left out (cached tokens read as zeros, output rows are left undefined) and
  * KVS_ERR_BOUNDS recorded for kvs_check_errors().  With KVS_F_VALIDATE (the only flag)

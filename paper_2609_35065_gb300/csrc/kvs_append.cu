@@ -24,10 +24,12 @@ __device__ __forceinline__ void turn(int32_t pos, float2 f, float scale, float& 
     s *= scale;
 }
 
-// One token's (row of the tensors) place: its position, and its row in the planes (< 0: none).
+// One token's (row of the tensors) place: its position, its row in the planes (< 0: none), and
+// whether it is a request's at all.
 struct Place {
     int32_t pos;
     int64_t row;
+    bool    owned;
 };
 
 // Request of row n: the last one that starts at or before it.
@@ -48,7 +50,8 @@ __device__ __forceinline__ Place place_of(const AppendJob& j, int32_t n) {
     }
     const Request q = load_request(st, r);
     const int32_t t = q.T - q.n + (n - q.q0);
-    if (n >= q.q0 && n < q.q0 + q.n && t >= 0) pl.row = row_of(st, st.tables + (int64_t)r * st.table_stride, t);
+    pl.owned = n >= q.q0 && n < q.q0 + q.n;
+    if (pl.owned && t >= 0) pl.row = row_of(st, st.tables + (int64_t)r * st.table_stride, t);
     pl.pos = j.positions ? __ldg(j.positions + n) : max(t, 0);
     return pl;
 }
@@ -62,6 +65,7 @@ __global__ void __launch_bounds__(256) kvs_append_kernel(AppendJob j, uint32_t w
     const int32_t n = w / warps_per_token, part = w % warps_per_token;
     const int lane = threadIdx.x & 31;
     const Place pl = place_of(j, n);
+    if (!pl.owned) return;
     const int32_t D = j.step.head_dim, rot = j.rot_dim;
     using N = Num<HALF>;
 
@@ -155,6 +159,7 @@ __global__ void __launch_bounds__(256) kvs_append_pairs_kernel(AppendJob j) {
     const int32_t n = (int32_t)w;
     const int lane = threadIdx.x & 31;
     const Place pl = place_of(j, n);
+    if (!pl.owned) return;
     const int32_t D = j.step.head_dim, rot = j.rot_dim, H = j.step.kv_heads;
     using N = Num<HALF>;
     using T = typename N::T;

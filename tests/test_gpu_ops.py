@@ -530,3 +530,24 @@ def test_rows_of_no_request_keep_what_they_hold(new, lens, H, ways):
     assert torch.equal(out[mine], want) and torch.equal(z[mine], z_want)
     for x in (out, z):
         assert (x[:3] == 7.0).all() and (x[3 + sm.N:] == 7.0).all()
+
+
+@pytest.mark.parametrize("rot,inter", [(64, False), (20, False), (64, True)])
+@pytest.mark.parametrize("new,lens", [([3, 0, 4], [9, 0, 4]), ([5], [3]), ([1] * 40, [7] * 40)])
+def test_append_leaves_rows_of_no_request_alone(new, lens, rot, inter):
+    """Two calls for the two halves of a tensor's rows rotate each of its queries once."""
+    sm = Small(new, lens, 2, 3, 64)
+    turns, _ = kvs.kvs_rope_turns(rot)
+    rope = kvs.Rope(torch.from_numpy(turns).cuda(), rot, inter)
+    step, q, k, v, cache = sm.on_gpu(kvs)
+    want = torch.empty(q.shape, dtype=q.dtype, device="cuda")
+    kvs.kvs_append(step, 0, q, k, v, want, rope)
+    kept = cache.clone()
+    step, q, k, v, cache = _in_padded_rows(sm, 3, 5)
+    mine = slice(3, 3 + sm.N)
+    for out in (torch.full_like(q, 3.0), None):
+        kvs.kvs_append(step, 0, q, k, v, out, rope, flags=kvs.KVS_F_VALIDATE)
+        x = q if out is None else out
+        assert torch.equal(x[mine], want)
+        assert (x[:3] == 3.0).all() and (x[3 + sm.N:] == 3.0).all()
+    assert torch.equal(cache.view(torch.int16), kept.view(torch.int16))
