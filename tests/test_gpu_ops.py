@@ -551,3 +551,34 @@ def test_append_leaves_rows_of_no_request_alone(new, lens, rot, inter):
         assert torch.equal(x[mine], want)
         assert (x[:3] == 3.0).all() and (x[3 + sm.N:] == 3.0).all()
     assert torch.equal(cache.view(torch.int16), kept.view(torch.int16))
+
+
+def _with_starts(sm, starts, max_q):
+    step, q, k, v, cache = sm.on_gpu(kvs)
+    s = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    return kvs.Step((sm.L, sm.H, sm.D, 2, sm.B, sm.B), [cache[p].data_ptr() for p in range(2 * sm.L)], sm.num_blocks, step._keep[0], step._keep[1], s,
+                    total_q=sm.N, max_q=max_q), q, k, v, cache
+
+
+@pytest.mark.parametrize("op", ["append", "attend", "weigh"])
+@pytest.mark.parametrize("starts,lens", [([0, 5, 3, 8], [20, 20, 20]), ([0, 3, 4, 9], [20, 20, 20]), ([-1, 3, 4, 8], [20, 20, 20]), ([0, 3, 3, 8], [20, 33, 20]),
+                                         ([0, 3, 8, 8], [20, 20, -1]), ([0, 0, 8, 8], [-5, 20, 20])])
+def test_every_operator_records_a_request_out_of_bounds(op, starts, lens):
+    """Row ranges that fall, overlap or leave the tensor, and lengths out of bounds, also of requests without rows."""
+    sm = Small([3, 2, 3], [20, 20, 20], 2, 2, 64, B=16)
+    step, q, k, v, cache = _with_starts(sm, starts, 8)
+    step._keep[1].copy_(torch.tensor(lens, dtype=torch.int32))
+    before = cache.clone()
+    out, z = torch.empty(q.shape, dtype=q.dtype, device="cuda"), torch.zeros(q.shape[:2], device="cuda")
+    ws = torch.empty(kvs.kvs_attend_workspace(step, 4), dtype=torch.uint8, device="cuda")
+    w = torch.zeros(3, 2, step.max_kv, device="cuda")
+    call = {"append": lambda: kvs.kvs_append(step, 0, None, k, v, flags=kvs.KVS_F_VALIDATE),
+            "attend": lambda: kvs.kvs_attend(step, 0, q, out, z, workspace=ws, flags=kvs.KVS_F_VALIDATE),
+            "weigh": lambda: kvs.kvs_weigh(step, 0, q, z, w, flags=kvs.KVS_F_VALIDATE)}[op]
+    with pytest.raises(kvs.KvsError) as ei:
+        call()
+    assert ei.value.code == kvs.KVS_ERR_BOUNDS
+    used = np.concatenate([sm.slots(r, np.arange(20)) for r in range(3)])
+    rest = torch.from_numpy(np.setdiff1d(np.arange(sm.num_blocks * sm.B), used)).cuda()
+    flat, flat_before = (x.view(2, -1, sm.H, sm.D).view(torch.int16) for x in (cache, before))
+    assert torch.equal(flat[:, rest], flat_before[:, rest])
