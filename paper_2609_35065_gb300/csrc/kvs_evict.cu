@@ -236,9 +236,10 @@ __global__ void __launch_bounds__(kCopy) kvs_evict_copy_kernel(EvictJob j, const
     int32_t T = __ldg(st.kv_lens + r);
     if (T < 0 || T > st.max_kv) T = 0;
     const int32_t J = min(T, j.budget), j0 = blockIdx.x * tokens;
+    // The selection.  CTAs without tokens wait too: otherwise a copy of nothing could be over before it.
+    grid_wait();
     if (j0 >= J) return;
     const uint32_t items = min(tokens, (uint32_t)(J - j0)) * per_token;
-    grid_wait();                                                 // the selection
     constexpr int U = 2;
     for (uint32_t i0 = threadIdx.x; i0 < items; i0 += kCopy * U) {
         uint4 a[U], b[U];

@@ -582,3 +582,24 @@ def test_every_operator_records_a_request_out_of_bounds(op, starts, lens):
     rest = torch.from_numpy(np.setdiff1d(np.arange(sm.num_blocks * sm.B), used)).cuda()
     flat, flat_before = (x.view(2, -1, sm.H, sm.D).view(torch.int16) for x in (cache, before))
     assert torch.equal(flat[:, rest], flat_before[:, rest])
+
+
+def test_eviction_from_empty_caches_is_over_when_the_stream_has_passed_it():
+    """Nothing is kept, so that the copy has nothing to wait for but the selection, which writes `kept`."""
+    L, R, H, budget = 8, 64, 4, 500
+    sm = Small([0] * R, [0] * R, H, 1, 64, L=L, extra_blocks=R * 40)
+    lens = torch.zeros(R, dtype=torch.int32, device="cuda")
+    cache = sm.cache.cuda()
+    tables = torch.zeros(R, 40, dtype=torch.int32, device="cuda")
+    dst = torch.ones(R, 40, dtype=torch.int32, device="cuda")
+    step = kvs.Step((L, H, 64, 2, 16, 16), [cache[p].data_ptr() for p in range(2 * L)], sm.num_blocks, tables, lens, total_q=0, max_q=0)
+    w = torch.zeros(L, R, H, step.max_kv, device="cuda")
+    kept = torch.empty(L, R, H, budget, dtype=torch.int32, device="cuda")
+    nw, nl = torch.empty(kept.shape, device="cuda"), torch.empty(R, dtype=torch.int32, device="cuda")
+    for _ in range(20):
+        for x in (kept, nw, nl):
+            x.fill_(7)
+        kvs.kvs_evict(step, w, dst, budget, 4, 8, kept, nw, nl)
+        copies = [x.clone() for x in (kept, nw, nl)]              # right behind the copy
+        assert (copies[0] == -1).all() and (copies[1] == 0).all() and (copies[2] == 0).all()
+    kvs.kvs_check_errors()
