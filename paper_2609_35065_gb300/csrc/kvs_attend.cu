@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
     using N = Num<HALF>;
     constexpr int PITCH = DP * 2, CH = DP / 8;                 // 16-byte vectors of a row
     constexpr int STAGE = 2 * kKeys * PITCH;                   // K, then V
-    constexpr float kLag = HALF ? 14.0f : 20.0f;               // log2 by which a weight may exceed 1
+    constexpr float kLag = HALF ? 15.0f : 20.0f;               // log2 that a weight may reach before the reference is raised
     const StepView& st = j.step;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, i8 = lane >> 2;
     const int32_t split = blockIdx.x, r = blockIdx.z, h = blockIdx.y;
@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
     if (rows <= 0) return;
     const Span all = seen_by(q, 0, q.n - 1, j.causal, j.window);
     const Span keys = split_of(all, split, j.splits, kKeys * WARPS);
+    const float top_at = HALF ? half_top(keys.hi - keys.lo, 8) : 0.0f;       // log2 of the maximum's weight then (8 costs nothing here)
     const uint32_t base = smem_u32(smem);
     const int32_t vecs = st.head_dim / 8;
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
                     float top = fmaxf(s[n][0][e], s[n][0][e + 2]);
 #pragma unroll
                     for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-                    const float to = fmaxf(m[n][e], top), f = to == m[n][e] ? 1.0f : exp2_fast(m[n][e] - to);
+                    const float to = fmaxf(m[n][e], top - top_at), f = to == m[n][e] ? 1.0f : exp2_fast(m[n][e] - to);
                     m[n][e] = to;
                     l[n][e] *= f;
 #pragma unroll

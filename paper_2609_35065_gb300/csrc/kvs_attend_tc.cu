@@ -14,9 +14,11 @@
 // products.
 //
 // The running maximum m that O and the sums refer to is raised only when weights outgrow it by
-// 2^20 (half: 2^15, which it can still hold): until then P is up to that instead of 1, which
-// costs the relative precision of P and of binary32 sums nothing, and O need not be rescaled,
-// which hardly any step then does (at 2^8 every third step of a long cache had a row that did).
+// 2^20: until then P is up to that instead of 1, which costs the relative precision of P and of
+// binary32 sums nothing, and O need not be rescaled, which hardly any step then does (at 2^8
+// every third step of a long cache had a row that did).  Half holds multiples of 2^-24 up to 2^16
+// only: P is 2^3 to 2^10 at the maximum there, by the number of keys, so that the light ones of
+// many are not lost, and may outgrow it up to 2^16.
 // So a step takes its exponentials against the m at hand and sees by their sum that none was
 // too large; the rare step that had such a one is done again with m raised.
 //
@@ -66,7 +68,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
     using N = Num<HALF>;
     using P = Plan<DP, TILES>;
     constexpr int kIssuer = 8 * TILES;               // the issuing warp, behind the softmax's; then the loading ones
-    constexpr float kMost = HALF ? 32768.0f : 1048576.0f;            // of a thread's weights of a step
+    constexpr float kMost = HALF ? 65504.0f : 1048576.0f;            // of a thread's weights of a step (half: of either sum)
     const StepView& st = j.step;
     const bool cluster = TILES == 1 && j.cluster;    // no cluster joins the parts of two tiles
     const uint32_t base = smem_u32(raw);
@@ -316,6 +318,8 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
         if (live) see = seen_by(q, tok, tok, j.causal, j.window);
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // lane 32 (warp % 4) of tensor memory
         const uint32_t s_own = s_at(tl) + lanes + 64 * half, o_own = o_at(tl) + lanes + DP / 2 * half;
+        // log2 of a weight at the reference: at 3 half's time over 4096 and 12581 tokens is that at 0, at 8 it is 8 and 12% more
+        const float top_at = HALF ? half_top(steps * kN, 3) : 0.0f;
         float m = kNone, l0 = 0.0f, l1 = 0.0f;
         bool ok = true;
         for (int32_t k = 0; k < steps; ++k) {
@@ -369,7 +373,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
                         }
                     }
                 }
-                const float off = m == kNone ? 0.0f : -m * c;
+                const float off = m == kNone ? 0.0f : top_at - m * c;
                 a0 = a1 = 0.0f;
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
@@ -389,9 +393,9 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
                         pk[16 * b + n] = N::pack(x, y);
                     }
                 }
-                // No weight is above their sum.  Both halves of S are read behind this: P goes over the
+                // No weight is above its sum.  Both halves of S are read behind this: P goes over the
                 // first one's columns.
-                const bool again = bar_or(pair, 64, !exact && live && a0 + a1 > kMost);
+                const bool again = bar_or(pair, 64, !exact && live && (HALF ? fmaxf(a0, a1) : a0 + a1) > kMost);
                 if (!again) break;
                 exact = true;
             }
@@ -413,7 +417,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
         const int64_t all_rows = (int64_t)st.total_q * heads;
         if (ok) {
             if (live && half == 0) {
-                const float m2 = m == kNone ? kNone : m * c;
+                const float m2 = m == kNone ? kNone : m * c - top_at;
                 const int64_t row = (int64_t)(q.q0 + tok) * heads + h * st.group + g;
                 if (cluster) reinterpret_cast<float2*>(raw + P::part_ml)[t] = make_float2(m2, l);
                 else if (j.splits > 1) reinterpret_cast<float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim)[split * all_rows + row] = make_float2(m2, l);

@@ -102,6 +102,12 @@ struct Num<true> {
     }
 };
 
+// Attention weights in half are multiples of 2^-24, and none is above 65504: log2 of what the
+// heaviest of `tokens` is scaled to, so that a long cache's light ones are not lost beside it.
+// What their rounding takes from a sum is then below 2^-15 of the largest value (half's own
+// rounding is 2^-11), and above this lie 2^(16 - top) for weights that outgrow the reference.
+__device__ __forceinline__ float half_top(int32_t tokens, int32_t least) { return (float)min(10, max(least, 22 - __clz(tokens))); }
+
 // 2^x by the hardware's approximation (relative error about 2^-22); 0 at -infinity.
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;

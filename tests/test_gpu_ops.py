@@ -603,3 +603,27 @@ def test_eviction_from_empty_caches_is_over_when_the_stream_has_passed_it():
         copies = [x.clone() for x in (kept, nw, nl)]              # right behind the copy
         assert (copies[0] == -1).all() and (copies[1] == 0).all() and (copies[2] == 0).all()
     kvs.kvs_check_errors()
+
+
+@pytest.mark.parametrize("digits", [15, 20, 26, 30])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new,T,H", [(1, 40000, 1), (1, 1500, 4), (3, 300, 8), (40, 30000, 1), (150, 9000, 2), (150, 3000, 38)])
+def test_a_heavy_token_before_many_light_ones(new, T, H, dtype, digits):
+    """The first token has 2^digits times the weight of any other, and a value of zero: what comes out
+    is what the light ones add up to.  Half rounds weights to multiples of 2^-24, of which the heaviest one's
+    is 2^8 for few rows, and for many 2^3 or the tokens' number by 2^10."""
+    sm = Small([new], [T], H, 4, 64, dtype=dtype)
+    at = torch.from_numpy(sm.slots(0, np.arange(T)))
+    sm.cache[:, at] = 0.0
+    sm.cache[0, at[0], :, 0] = digits * np.log(2.0)
+    sm.cache[1, at[1:]] = 1.0
+    sm.qkv[:] = 0.0
+    sm.parts(sm.qkv)[0][:, :, 0] = 1.0
+    out, _ = _attend(sm, scale=1.0)
+    want, bound, _, _ = sm.attend(1.0)
+    if dtype == "f16":
+        # the rounding of the weights, and of an output below half's normal numbers
+        heaviest = 2.0 ** 8 if new * sm.G <= 16 else max(2.0 ** 3, T / 2.0 ** 10)
+        bound = bound - T * 2.0 ** -25 + T * 2.0 ** -25 / heaviest + 2.0 ** -25
+    off = np.abs(out.double().cpu().numpy() - want)
+    assert (off <= bound).all(), (off / bound).max()
