@@ -582,9 +582,11 @@ int kvs_append(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs
  * kv_len, or outside what a request's tokens see, may be anything (NaN too) and reaches
  * no output; a non-finite value of a token that some row of the request sees may reach
  * all of its rows.  causal = 0 attends to an encoder's states, or to a prefix alone.
- * Scores, softmax statistics and sums are binary32; the weights are rounded to dtype for
- * the product with V.  The workspace is device memory of kvs_attend_workspace() bytes
- * (any contents, 16-byte aligned, not shared by calls that may overlap on the GPU).
+ * Scores, softmax statistics and sums are binary32; where max_q times the query heads of a
+ * KV head is above 16, the weights are rounded to dtype for the product with V (half: to
+ * multiples of 2^-27 or less of the heaviest one).  The workspace is device memory of
+ * kvs_attend_workspace() bytes (any contents, 16-byte aligned, not shared by calls that may
+ * overlap on the GPU).
  */
 typedef struct kvs_attend_args {
     kvs_rows q, out;                /* [total_q][num_q_heads][head_dim]                 */

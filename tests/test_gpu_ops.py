@@ -627,3 +627,22 @@ def test_a_heavy_token_before_many_light_ones(new, T, H, dtype, digits):
         bound = bound - T * 2.0 ** -25 + T * 2.0 ** -25 / heaviest + 2.0 ** -25
     off = np.abs(out.double().cpu().numpy() - want)
     assert (off <= bound).all(), (off / bound).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,lens,H,G,D", [([1, 1], [900, 300], 2, 4, 128), ([1], [5000], 1, 8, 64), ([2, 3], [700, 90], 2, 5, 80), ([4], [3000], 1, 4, 128), ([1], [20000], 1, 1, 96)])
+def test_few_rows_lose_nothing_by_rounding_weights(new, lens, H, G, D, dtype):
+    """Up to 16 packed rows a weight goes into the product with V as two 16-bit numbers, so that what is off
+    is the output's own rounding, and the square of the type's of the weights."""
+    sm = Small(new, lens, H, G, D, dtype=dtype)
+    out, _ = _attend(sm)
+    want, bound, _, _ = sm.attend(D ** -0.5)
+    mean = Small(new, lens, H, G, D, dtype=dtype)
+    mean.cache[1] = mean.cache[1].abs()
+    a = mean.attend(D ** -0.5)[0]                                # the mean of |v|
+    u = ops_ref.UNIT[dtype]
+    bound = bound - 1.01 * u * a + u * u * a
+    if dtype == "f16":
+        bound = bound + 2.0 ** -25                               # of an output below half's normal numbers
+    off = np.abs(out.double().cpu().numpy() - want)
+    assert (off <= bound).all(), (off / bound).max()
