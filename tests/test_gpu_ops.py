@@ -646,3 +646,156 @@ def test_few_rows_lose_nothing_by_rounding_weights(new, lens, H, G, D, dtype):
         bound = bound + 2.0 ** -25                               # of an output below half's normal numbers
     off = np.abs(out.double().cpu().numpy() - want)
     assert (off <= bound).all(), (off / bound).max()
+
+
+# ---- what a request does not see, and what its neighbours hold ---------------
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,lens", [([2, 1, 3], [700, 650, 350]), ([5, 30, 4], [700, 650, 350]), ([33, 150, 7], [300, 650, 90])])
+def test_the_neighbours_of_a_request_do_not_matter(new, lens, dtype):
+    """The middle request's rows have the same bits whatever the requests around it hold, queries that are not
+    numbers right before and behind it among that."""
+    got = []
+    for fill in (None, 1.0, float("nan"), float("inf")):
+        sm = Small(new, lens, 2, 5, 128, dtype=dtype)
+        rows = slice(sm.starts[1], sm.starts[2])
+        if fill is not None:
+            for r in (0, 2):
+                sm.qkv[sm.starts[r]: sm.starts[r + 1]] = fill
+                sm.cache[:, torch.from_numpy(sm.slots(r, np.arange(lens[r])))] = fill
+        out, z = _attend(sm)
+        step, q, _, _, _cache = sm.on_gpu(kvs)
+        w = torch.ones(3, 2, step.max_kv, device="cuda")
+        kvs.kvs_weigh(step, 0, q, z, w, decay=0.5, flags=kvs.KVS_F_VALIDATE)
+        got.append((out[rows], z[rows], w[1]))
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,G", [(128, 4), (64, 3)])
+@pytest.mark.parametrize("new,T,window", [(1, 700, 100), (1, 20000, 300), (3, 500, 129), (30, 900, 64), (200, 1500, 200), (130, 4000, 17)])
+def test_tokens_before_the_window_may_be_anything(new, T, window, D, G, dtype):
+    """Keys and values that no row of the request sees are not numbers, and reach neither outputs nor weights."""
+    sm = Small([new, 2], [T, 60], 2, G, D, dtype=dtype)
+    first = T - new + 1 - window
+    sm.cache[:, torch.from_numpy(sm.slots(0, np.arange(first)))] = float("nan")
+    want = Small([new, 2], [T, 60], 2, G, D, dtype=dtype)
+    want.cache[:, torch.from_numpy(want.slots(0, np.arange(first)))] = 0.5
+    scale = D ** -0.5
+    ref, bound, lse, _ = want.attend(scale, True, window)
+    out, z = _attend(sm, window=window)
+    assert (np.abs(out.double().cpu().numpy() - ref) <= bound).all()
+    step, q, _, _, _cache = sm.on_gpu(kvs)
+    w = torch.full((2, 2, step.max_kv), 2.0, device="cuda")
+    kvs.kvs_weigh(step, 0, q, torch.from_numpy(lse.astype(np.float32)).cuda(), w, decay=0.5, window=window, flags=kvs.KVS_F_VALIDATE)
+    before = np.full((2, 2, step.max_kv), 2.0, np.float32)
+    ref_w, bound_w = want.weigh(lse.astype(np.float32), before, 0.5, scale, True, window)
+    for r, n in enumerate((T, 60)):
+        assert (np.abs(w[r, :, :n].double().cpu().numpy() - ref_w[r, :, :n]) <= bound_w[r, :, :n]).all()
+    assert (w[0, :, :first] == 1.0).all()
+
+
+# ---- entries out of bounds, found on the device -------------------------------
+@pytest.mark.parametrize("op", ["append", "weigh"])
+@pytest.mark.parametrize("new", [1, 3, 50])
+@pytest.mark.parametrize("what", ["length", "block", "negative block"])
+def test_out_of_bounds_entries_leave_the_other_requests_right(op, new, what):
+    """One request names a block that there is not, or has a length beyond max_kv: it alone is left out."""
+    lens = [130, 90]
+    good = Small([new, new], lens, 2, 4, 64)
+    bad = Small([new, new], lens, 2, 4, 64)
+    blk = 89 // bad.B                                             # of the last token, a new one
+    if what != "length":
+        bad.tables[1, blk] = bad.num_blocks if what == "block" else -1
+    lse = good.attend(good.D ** -0.5)[2].astype(np.float32)
+    got = []
+    for sm in (good, bad):
+        step, q, k, v, cache = sm.on_gpu(kvs)
+        if sm is bad and what == "length":
+            step._keep[1][1] = step.max_kv + 1
+        w = torch.full((2, 2, step.max_kv), 3.0, device="cuda")
+        flags = kvs.KVS_F_VALIDATE
+        call = (lambda: kvs.kvs_append(step, 0, None, k, v, flags=flags)) if op == "append" else \
+            (lambda: kvs.kvs_weigh(step, 0, q, torch.from_numpy(lse).cuda(), w, decay=0.0, flags=flags))
+        if sm is bad:
+            with pytest.raises(kvs.KvsError) as ei:
+                call()
+            assert ei.value.code == kvs.KVS_ERR_BOUNDS
+        else:
+            call()
+        got.append((cache.view(2, -1, sm.H, sm.D).view(torch.int16), w))
+    kvs.kvs_check_errors()                                        # the word is clear again
+    (cache_a, w_a), (cache_b, w_b) = got
+    if op == "weigh":
+        assert torch.equal(w_a[0], w_b[0])
+        if what == "length":
+            assert (w_b[1] == 3.0).all()
+        else:
+            assert torch.equal(w_a[1, :, : blk * bad.B], w_b[1, :, : blk * bad.B])
+        return
+    before = good.cache.cuda().view(torch.int16)
+    out = good.slots(1, np.arange(0 if what == "length" else blk * good.B, 90))
+    keep = torch.from_numpy(np.setdiff1d(np.arange(good.num_blocks * good.B), out)).cuda()
+    out = torch.from_numpy(out).cuda()
+    assert torch.equal(cache_a[:, keep], cache_b[:, keep])
+    assert torch.equal(cache_b[:, out], before[:, out])
+
+
+@pytest.mark.parametrize("what", ["length", "source block", "new block"])
+def test_eviction_with_entries_out_of_bounds(what):
+    lens, budget, B, H, D = [100, 90], 48, 16, 2, 64
+    sm = Small([0, 0], lens, H, 1, D, B, extra_blocks=10)
+    free = np.setdiff1d(np.arange(sm.num_blocks), sm.tables.numpy().ravel())[:6].reshape(2, 3)
+    dst = torch.from_numpy(free.astype(np.int32))
+    if what == "source block":
+        sm.tables[1, 2] = sm.num_blocks + 7
+    if what == "new block":
+        dst[1, 1] = -3
+    step, _, _, _, cache = sm.on_gpu(kvs)
+    if what == "length":
+        step._keep[1][1] = step.max_kv + 1
+    w = np.random.default_rng(8).random((1, 2, H, step.max_kv)).astype(np.float32)
+    kept = torch.full((1, 2, H, budget), -7, dtype=torch.int32, device="cuda")
+    nl = torch.full((2,), -7, dtype=torch.int32, device="cuda")
+    before = cache.clone()
+    with pytest.raises(kvs.KvsError) as ei:
+        kvs.kvs_evict(step, torch.from_numpy(w).cuda(), dst.cuda(), budget, 4, 8, kept, None, nl, None, kvs.KVS_F_VALIDATE)
+    assert ei.value.code == kvs.KVS_ERR_BOUNDS
+    want = ops_ref.evict(w, [100, 0 if what == "length" else 90], budget, 4, 8)
+    assert (kept.cpu().numpy() == want).all() and nl.tolist() == [48, 0 if what == "length" else 48]
+    flat = before.view(2, -1, H, D).clone()
+    for r in range(2):
+        for h in range(H):
+            for j, t in enumerate(want[0, r, h]):
+                b = int(dst[r, j // B])
+                if t < 0 or b < 0:
+                    continue
+                blk = int(sm.tables[r, t // B])
+                to = b * B + j % B
+                flat[:, to, h] = before.view(2, -1, H, D)[:, blk * B + t % B, h] if blk < sm.num_blocks else 0.0
+    assert torch.equal(cache.view(torch.int16), flat.view(cache.shape).view(torch.int16))
+
+
+@pytest.mark.parametrize("L", [224, 225, 500])
+def test_eviction_of_more_layers_than_a_launch_carries(L):
+    lens, budget, B, H, D = [40, 7], 12, 4, 1, 8
+    sm = Small([0, 0], lens, H, 1, D, B, L=L, extra_blocks=6)
+    step, _, _, _, cache = sm.on_gpu(kvs)
+    dst = torch.from_numpy(np.setdiff1d(np.arange(sm.num_blocks), sm.tables.numpy().ravel())[:6].reshape(2, 3).astype(np.int32))
+    w = np.random.default_rng(9).random((L, 2, H, step.max_kv)).astype(np.float32)
+    kept = torch.full((L, 2, H, budget), -7, dtype=torch.int32, device="cuda")
+    before = cache.view(2 * L, -1, H, D).clone()
+    launches = kvs.kvs_stat_launches()
+    kvs.kvs_evict(step, torch.from_numpy(w).cuda(), dst.cuda(), budget, 1, 2, kept, flags=kvs.KVS_F_VALIDATE)
+    assert kvs.kvs_stat_launches() - launches == 1 + -(-L // 224)
+    want = ops_ref.evict(w, lens, budget, 1, 2)
+    assert (kept.cpu().numpy() == want).all()
+    for r, T in enumerate(lens):
+        J = min(T, budget)
+        j = np.arange(J)
+        to = torch.from_numpy(dst[r].numpy().astype(np.int64)[j // B] * B + j % B).cuda()
+        for l in range(L):
+            at = torch.from_numpy(sm.slots(r, want[l, r, 0, :J])).cuda()
+            before[2 * l: 2 * l + 2, to] = before[2 * l: 2 * l + 2, at]
+    assert torch.equal(cache.view(torch.int16), before.view(cache.shape).view(torch.int16))
