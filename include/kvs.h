@@ -477,8 +477,9 @@ int kvs_retrieve_noalloc(const kvs_geometry* geom, const kvs_paged_cache* cache,
  *
  * Unlike a retrieval's, the lengths and block tables of a step are DEVICE arrays, as a
  * serving loop keeps them: the calls read them on the GPU, plan nothing on the host,
- * allocate nothing, and can be captured into a graph.  Calls are enqueued on the
- * caller's stream and return; tensors must stay valid until the stream has passed them.
+ * allocate nothing, and can be captured into a graph (but for the library's first call on a
+ * device, which allocates its state; kvs_attend_workspace() is one).  Calls are enqueued on
+ * the caller's stream and return; tensors must stay valid until the stream has passed them.
  * Rows of the step's tensors that belong to no request (before q_starts[0], behind its last
  * entry) are not written, and what they hold does not matter.
  * A length, row range or block id outside the stated bounds is not followed: what it
@@ -558,8 +559,9 @@ int kvs_rope_turns(const kvs_rope_spec* spec, float* turns_out, float* scale_out
  * positions[n] (device int32, NULL: t) is the token's rotary position, which differs
  * from t once tokens were evicted; |position| up to 2^24.  rope NULL: nothing is
  * rotated.  q may be NULL (keys and values only, or to rotate no queries); q_out may be
- * q itself.  New tokens beyond kv_lens (more new tokens than cached ones) are not
- * appended, only their queries rotated.  Products and sums are binary32, rounded once.
+ * q itself, and shares no element with it otherwise.  New tokens beyond kv_lens (more new
+ * tokens than cached ones) are not appended, only their queries rotated.  Products and sums
+ * are binary32, rounded once.
  */
 typedef struct kvs_append_args {
     kvs_rows q, q_out;              /* [total_q][num_q_heads][head_dim]                 */
