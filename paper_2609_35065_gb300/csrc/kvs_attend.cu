@@ -74,13 +74,13 @@ __device__ __forceinline__ Span split_of(Span s, int32_t split, int32_t splits, 
 // tensor cores the running maximum may lag behind, so that a stage need not exchange it.
 //
 // A weight goes into the product with V as the 16-bit number next to it and, in a second product,
-// what that rounding took: in the shadow of the loads up to eight rows (207 us for 206), 2% with
+// what that rounding took: in the shadow of the loads up to eight rows (0.2% of those 207 us), 2% with
 // nine to sixteen, and the outputs are as near as with weights of 32 bits.
 //
 // Where a head's parts are up to eight and all clusters run at once, they are CTAs of a cluster
 // that join through distributed shared memory; otherwise a second kernel joins them.
 //
-// 14 warps with two stages each: 64 requests over 2k to 8k tokens take 203 us (1.34 GB, 6.6 TB/s);
+// 14 warps with two stages each: 64 requests over 2k to 8k tokens take 207 us (1.34 GB, 6.5 TB/s);
 // 8 warps with three stages took 211, 5 with five 262 (with the products the other way round).
 // ---------------------------------------------------------------------------
 template <int DP, int WARPS, int STAGES>
@@ -462,6 +462,8 @@ AttendPlan attend_plan(const StepView& st, int sms) {
     // 11.4, over 16000, in 19 parts, 13.2); of one tile three, or one (20 rows over 2000 tokens 10.0 us
     // with a cluster, 12.2 without, over 4000 11.8 and 13.1; of eight requests over 1000 13.2 and 14.3),
     // of two tiles six, where a cluster loses (293 tokens over 4000 37 us, 33 without).
+    // The plan goes by max_kv, whatever the window: four decoding requests with a window of 4096
+    // in 131072 tokens take 32 us, with caches of 4096 tokens 18.5.
     int64_t best = -1;
     for (int64_t n = 1; n <= 256 && n <= (steps + 1) / 2; ++n) {
         // Clusters have room where all of their CTAs run at once: a cluster's lie on neighbouring SMs, and

@@ -19,15 +19,23 @@
 // every third step of a long cache had a row that did).  Half holds multiples of 2^-24 up to 2^16
 // only: P is 2^3 to 2^10 at the maximum there, by the number of keys, so that the light ones of
 // many are not lost, and may outgrow it up to 2^16.
+//
+// P is rounded to the 16-bit type of V, as the products take both operands of one such type:
+// what that takes would need a second product with V, half again of all of them (relative error
+// of the outputs 0.0023, with weights of 32 bits 0.0017).
+//
 // So a step takes its exponentials against the m at hand and sees by their sum that none was
 // too large; the rare step that had such a one is done again with m raised.
 //
-// 16 suffixes of 2048 tokens behind 2048, 32 query heads of 128 dims on 8 (1.65 PFLOP) take
+// 16 suffixes of 2048 tokens behind 2048, 32 query heads of 128 dims on 8 (1.65 TFLOP) take
 // 1075 to 1117 us, 1.48 to 1.53 PFLOP/s, at the GPU's power cap (1.36 kW, where its clock falls
 // from 2070 to 1860 MHz).  A question of 293 tokens about 12288, 40 query heads on 8, takes 62 to
-// 63 (75 GFLOP in 144 CTAs of 33 steps; the products keep the tensor cores busy for 62% of the
-// kernel, start, end and join are the rest).  35 rows over 4000 to 10000 tokens for each of 8
-// requests and 2 heads take 19 to 20: launch, join, and per step of one tile a chain of about 1 us.
+// 64 (75 GFLOP in 144 CTAs of 33 steps; some 53 of it are this kernel, whose products keep the
+// tensor cores busy for 62%; of the rest a CTA's start was measured at 1.6 us, what the other 18
+// wait for was not; 9 are the binary32 parts and their join).  35 rows over 4000 to 10000 tokens
+// for each of 8 requests and 2 heads take 18.4: with one tile nothing runs beside the softmax, S of
+// the next step being issued behind the product that reads P from the same columns, so that
+// S, softmax, P and O are one chain of about 1 us a step.
 //
 // Products run in the order in which one thread issues them, which the reuse of S's columns
 // for P relies on: S of the next tile is issued behind the product that reads P.
