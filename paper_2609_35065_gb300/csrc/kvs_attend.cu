@@ -457,11 +457,12 @@ AttendPlan attend_plan(const StepView& st, int sms) {
     const int64_t per = p.tc ? (int64_t)tile * p.row_tiles : 16, tiles = (rows + per - 1) / per * units, steps = (st.max_kv + 127) / 128, start = 4, join = p.row_tiles == 2 ? 6 : p.tc ? 3 : 5;
     if (p.tc && p.row_tiles == 1 && st.head_dim <= 64) sms *= 2;
     // As many parts as keep the number of waves times a part's steps lowest.  The join of parts of
-    // few rows costs about five steps of theirs, within a cluster one (one decoding request over
-    // 2000 tokens 7.1 us with a cluster and 8.9 without, over 4000 8.1 and 10.7, over 8000 10.0 and
-    // 11.4, over 16000, in 19 parts, 13.2); of one tile three, or one (20 rows over 2000 tokens 10.0 us
-    // with a cluster, 12.2 without, over 4000 11.8 and 13.1; of eight requests over 1000 13.2 and 14.3),
-    // of two tiles six, where a cluster loses (293 tokens over 4000 37 us, 33 without).
+    // few rows costs about five steps of theirs, within a cluster one (8 heads of 128 dims, captured
+    // in a graph: one decoding request over 2000 tokens 7.3 us with a cluster and 8.4 without, over
+    // 4000 9.8 and 11.2, over 8000 12.4 and 13.4, over 16000, in 19 parts, 18.2); of one tile three,
+    // or one (20 rows over 2000 tokens 10.0 us with a cluster, 11.8 without, over 4000 12.7 and 14.3;
+    // of eight requests and two heads over 1000 10.3 and 12.1), of two tiles six, where a cluster
+    // loses (293 tokens over 4000 37 us, 33 without, both before the join went by requests).
     // The plan goes by max_kv, whatever the window: four decoding requests with a window of 4096
     // in 131072 tokens take 32 us, with caches of 4096 tokens 18.5.
     int64_t best = -1;
