@@ -473,7 +473,8 @@ int kvs_retrieve_noalloc(const kvs_geometry* geom, const kvs_paged_cache* cache,
  * brought: kvs_append rotates their queries and keys and writes keys and values into
  * the planes, kvs_attend attends over the whole cache, kvs_weigh adds up the attention
  * weight that each cached token received and kvs_evict keeps the tokens of the most
- * weight.  Each call works on one layer (kvs_evict: on all) of the planes above.
+ * weight.  kvs_append_axes takes positions on several axes; kvs_attend_sinks and kvs_weigh_sinks
+ * are of a window beside which a request's first tokens stay visible.  Each call works on one layer (kvs_evict: on all) of the planes above.
  *
  * Unlike a retrieval's, the lengths and block tables of a step are DEVICE arrays, as a
  * serving loop keeps them: the calls read them on the GPU, plan nothing on the host,
@@ -575,6 +576,34 @@ int kvs_append(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs
                const kvs_append_args* args, void* cuda_stream, uint32_t flags);
 
 /*
+ * Append with positions on several axes (time, height and width of an image's or a video's
+ * tokens): as kvs_append, but pair j of a head turns by the token's position on axis
+ * axis[j], positions[axis[j] * stride + n].  rope and positions must be given.  A text token has
+ * the same position on every axis, and comes out as from kvs_append with that position.
+ * An entry of the axis table that is not below num_axes is recorded (KVS_ERR_BOUNDS) and its
+ * pair turned as at position 0.  kvs_rope_axes() fills both tables.
+ */
+#define KVS_MAX_AXES 4
+typedef struct kvs_axes {
+    const uint8_t* axis;            /* device [pairs]                                   */
+    int64_t        stride;          /* entries of positions from axis to axis, at least total_q */
+    int32_t        num_axes;        /* 1 to KVS_MAX_AXES                                */
+    int32_t        pairs;           /* half of rope's rot_dim                           */
+} kvs_axes;
+int kvs_append_axes(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
+                    const kvs_append_args* args, const kvs_axes* axes, void* cuda_stream, uint32_t flags);
+
+#define KVS_AXES_BLOCKS  0   /* the first parts[0] pairs are axis 0's, the next parts[1] axis 1's ...      */
+#define KVS_AXES_CYCLE   1   /* axis a > 0 has the pairs a, a + num_axes, ..., parts[a] of them; axis 0 the
+                                others                                                                    */
+#define KVS_AXES_RESTART 2   /* (or'ed) each axis has a whole range of frequencies, as if rot_dim were twice
+                                its parts; else pair j has the frequency that kvs_rope_turns gives it     */
+/* The tables of rot_dim / 2 = sum of parts[num_axes] pairs (all HOST memory): turns_out[rot_dim / 2][2],
+ * axis_out[rot_dim / 2] and *scale_out.  parts are positive; spec->rot_dim is twice their sum. */
+int kvs_rope_axes(const kvs_rope_spec* spec, const int32_t* parts, int32_t num_axes, int32_t order, float* turns_out,
+                  uint8_t* axis_out, float* scale_out);
+
+/*
  * Attention of each request's new tokens over its cached ones.  Query head i reads KV
  * head i / (num_q_heads / H).  The i-th of n new tokens is the cached token
  * p = kv_len - n + i; it sees the cached tokens t < kv_len with t <= p (if causal) and
@@ -606,6 +635,21 @@ int kvs_attend(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs
 int64_t kvs_attend_workspace(const kvs_geometry* geom, const kvs_step* step, int32_t num_q_heads);
 
 /*
+ * Attention with sinks: kvs_attend of a window beside which the request's first `sinks` tokens
+ * stay visible.  Token p sees the cached tokens t < kv_len with t <= p (if causal) and
+ * t > p - window or t < sinks.  args->window = 0 is no limit, as for kvs_attend.
+ * Of the block tables only entries are read whose blocks hold a token that some new token of the
+ * request sees: blocks between the sinks and the window may have been given back (entries of
+ * any value) and their memory may belong to others.  What a call costs goes by window, sinks and
+ * max_q, not by max_kv.  The workspace is kvs_attend_sinks_workspace() bytes for the same causal,
+ * window and sinks; all else as for kvs_attend.
+ */
+int kvs_attend_sinks(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
+                     const kvs_attend_args* args, int32_t sinks, void* cuda_stream, uint32_t flags);
+int64_t kvs_attend_sinks_workspace(const kvs_geometry* geom, const kvs_step* step, int32_t num_q_heads, int32_t causal,
+                                   int32_t window, int32_t sinks);
+
+/*
  * Accumulated attention weight, from the lse that kvs_attend returned for the same
  * arguments: for every request r, KV head h and cached token t < kv_len,
  *     weights[r * request_stride + h * head_stride + t] =
@@ -626,6 +670,14 @@ typedef struct kvs_weigh_args {
 } kvs_weigh_args;
 int kvs_weigh(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
               const kvs_weigh_args* args, void* cuda_stream, uint32_t flags);
+
+/*
+ * The same under kvs_attend_sinks' mask, from the lse that it returned.  Every cached token's
+ * weight is multiplied by decay, those of tokens that no new token sees too (decay = 1 leaves
+ * those untouched); only seen tokens' block table entries and keys are read.
+ */
+int kvs_weigh_sinks(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
+                    const kvs_weigh_args* args, int32_t sinks, void* cuda_stream, uint32_t flags);
 
 /*
  * Eviction, all layers at once (rows of q are not used; total_q and max_q may be 0).

@@ -92,8 +92,9 @@ struct RowsPlan {
     static constexpr int bytes = ring > join + part ? ring : join + part;
 };
 
-// NT: column tiles of eight rows.
-template <bool HALF, int DP, int NT, int WARPS, int STAGES>
+// NT: column tiles of eight rows.  HELD: a window with sinks, whose tokens the stages take as if there
+// were no others (places, of one token each).
+template <bool HALF, int DP, int NT, int WARPS, int STAGES, bool HELD>
 __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j) {
     extern __shared__ __align__(1024) char smem[];
     using N = Num<HALF>;
@@ -107,7 +108,12 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
     const Request q = load_request(st, r);
     const int32_t rows = q.n * st.group;
     if (rows <= 0) return;
-    const Span all = seen_by(q, 0, q.n - 1, j.causal, j.window);
+    Span all = seen_by(q, 0, q.n - 1, j.causal, j.window);
+    Held held{};
+    if (HELD) {
+        held = held_of(all.lo, j.sinks, 1);
+        all = Span{0, all.hi - held.shift};
+    }
     const Span keys = split_of(all, split, j.splits, kKeys * WARPS);
     const float top_at = HALF ? half_top(keys.hi - keys.lo, 8) : 0.0f;       // log2 of the maximum's weight then (8 costs nothing here)
     const uint32_t base = smem_u32(smem);
@@ -131,7 +137,7 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
     const int32_t mine = (count - warp + WARPS - 1) / WARPS;
     auto look_up = [&](int32_t i) {
         const int32_t t = keys.lo + kKeys * (warp + WARPS * i) + (lane & 15);
-        return i < mine && t < keys.hi ? row_of(st, table, t) : (int64_t)-1;
+        return i < mine && t < keys.hi ? row_of(st, table, HELD ? token_at(held, t) : t) : (int64_t)-1;
     };
     int64_t mrow = look_up(0);
     auto load = [&](int32_t i) {
@@ -185,7 +191,8 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
             l[n][e] = 0.0f;
             int32_t g;
             const int32_t tok = token_of(st, i, g);
-            const Span s = seen_by(q, tok, tok, j.causal, j.window);
+            Span s = seen_by(q, tok, tok, j.causal, j.window);
+            if (HELD) s = in_places(held, s);
             lo[n][e] = i < rows ? s.lo : 0;
             hi[n][e] = i < rows ? min(s.hi, keys.hi) : 0;
         }
@@ -218,7 +225,7 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
             for (int e = 0; e < 4; ++e) {
                 const int32_t t = t0 + 8 * (e >> 1);
                 const float x = (s[n][0][e] + s[n][1][e]) * j.scale_log2;
-                s[n][0][e] = t >= lo[n][e & 1] && t < hi[n][e & 1] ? x : kNone;
+                s[n][0][e] = (t >= lo[n][e & 1] || (HELD && t < j.sinks)) && t < hi[n][e & 1] ? x : kNone;
                 above = above || s[n][0][e] > m[n][e & 1] + kLag;
             }
         if (__any_sync(0xffffffffu, above)) {
@@ -416,11 +423,11 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kvs_attend_join_kernel(Attend
     if (lane == 0 && j.lse) j.lse[row] = L == 0.0f ? kNone : (M + log2f(L)) * 0.69314718055994531f;
 }
 
-template <bool HALF, int DP, int NT>
+template <bool HALF, int DP, int NT, bool HELD>
 cudaError_t attend_rows(const AttendJob& j, cudaStream_t s) {
     // 14 warps of two column tiles of wide heads would have too few registers
     constexpr int WARPS = DP == 128 && NT == 2 ? 12 : 14, STAGES = 2, smem = RowsPlan<DP, WARPS, STAGES>::bytes;
-    auto* k = kvs_attend_rows_kernel<HALF, DP, NT, WARPS, STAGES>;
+    auto* k = kvs_attend_rows_kernel<HALF, DP, NT, WARPS, STAGES, HELD>;
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
@@ -437,12 +444,14 @@ cudaError_t attend_rows(const AttendJob& j, cudaStream_t s) {
     return cudaLaunchKernelEx(&cfg, k, j);
 }
 
-template <bool HALF>
+template <bool HALF, bool HELD>
 cudaError_t attend_few(const AttendJob& j, cudaStream_t s) {
     const bool eight = j.step.max_q * j.step.group <= 8;
-    if (j.step.head_dim <= 64) return eight ? attend_rows<HALF, 64, 1>(j, s) : attend_rows<HALF, 64, 2>(j, s);
-    return eight ? attend_rows<HALF, 128, 1>(j, s) : attend_rows<HALF, 128, 2>(j, s);
+    if (j.step.head_dim <= 64) return eight ? attend_rows<HALF, 64, 1, HELD>(j, s) : attend_rows<HALF, 64, 2, HELD>(j, s);
+    return eight ? attend_rows<HALF, 128, 1, HELD>(j, s) : attend_rows<HALF, 128, 2, HELD>(j, s);
 }
+template <bool HALF>
+cudaError_t attend_few(const AttendJob& j, cudaStream_t s) { return j.held ? attend_few<HALF, true>(j, s) : attend_few<HALF, false>(j, s); }
 
 }  // namespace
 

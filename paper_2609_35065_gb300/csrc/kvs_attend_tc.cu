@@ -68,7 +68,8 @@ struct Bars {
     __device__ Bars(uint32_t at, int stages) : q(at), full(at + 8), free(full + 8 * stages), s(free + 8 * stages), p(s + 16), o(p + 16) {}
 };
 
-template <bool HALF, int DP, int TILES>
+// HELD: a window with sinks; the steps go over its places, units of which are boxes' tokens.
+template <bool HALF, int DP, int TILES, bool HELD>
 __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::ctas) kvs_attend_tc_kernel(AttendJob j, const __grid_constant__ CUtensorMap k_map,
                                                                     const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap q_map,
                                                                     int32_t boxes, int32_t q_boxes) {
@@ -128,14 +129,21 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
         }
         return;
     }
-    const Span all = seen_by(q, row0 / st.group, (row0 + rows - 1) / st.group, j.causal, j.window);
-    const int32_t first = all.lo / kN, steps_all = all.hi > all.lo ? (all.hi + kN - 1) / kN - first : 0;
+    Span all = seen_by(q, row0 / st.group, (row0 + rows - 1) / st.group, j.causal, j.window);
+    Held held{};
+    int32_t T = q.T;                                 // places (without HELD: tokens) of the cache
+    if (HELD) {
+        held = held_of(all.lo, j.sinks, boxes ? min(st.block_size, kN) : 1);
+        T -= held.shift;
+        all = in_places(held, all);
+    }
+    const int32_t first = HELD ? 0 : all.lo / kN, steps_all = all.hi > all.lo ? (all.hi + kN - 1) / kN - first : 0;
     const int32_t j0 = first + (int32_t)((int64_t)steps_all * split / j.splits);
     const int32_t steps = first + (int32_t)((int64_t)steps_all * (split + 1) / j.splits) - j0;
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
     // K's and V's tiles of a step are in the same blocks; the loading warps look the next step's up a step ahead
     Box next{};
-    if (boxes && steps > 0 && warp > kIssuer) next = box_of<DP, kLoaders>(st, table, j0 * kN, q.T, warp - kIssuer - 1, lane);
+    if (boxes && steps > 0 && warp > kIssuer) next = box_of<DP, kLoaders>(st, table, held, j0 * kN, T, warp - kIssuer - 1, lane);
 
     tc_fence_before();
     __syncthreads();
@@ -168,7 +176,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
             const int stage = i % P::stages;
             if (boxes && !(i & 1)) {
                 box = next;
-                if (i + 2 < 2 * steps) next = box_of<DP, kLoaders>(st, table, (j0 + (i >> 1) + 1) * kN, q.T, w, lane);
+                if (i + 2 < 2 * steps) next = box_of<DP, kLoaders>(st, table, held, (j0 + (i >> 1) + 1) * kN, T, w, lane);
             }
             if (i >= P::stages) {
                 const bool ok = lane != 0 || wait(bar.free + 8 * stage, (i / P::stages - 1) & 1);
@@ -178,7 +186,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
             const int32_t t0 = (j0 + (i >> 1)) * kN;
             const bool is_v = i & 1;
             // Beyond the cache, and before what the rows see, V has to be zeros; K may be anything there.
-            const bool whole = t0 >= all.lo && t0 + kN <= q.T;
+            const bool whole = (t0 >= all.lo || (HELD && min(t0 + kN, all.lo) <= j.sinks)) && t0 + kN <= T;
             if (boxes && (whole || !is_v)) {
                 if (pending >= 0) {
                     cp_wait<0>();
@@ -186,7 +194,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
                 }
                 tile_boxes<DP>(dst, is_v ? &v_map : &k_map, st, h, box, bar.full + 8 * stage, lane);
             } else {
-                tile_rows<DP, 32 * kLoaders>(dst, is_v ? j.v_plane : j.k_plane, st, table, h, t0, all.lo, q.T, t);
+                tile_rows<DP, 32 * kLoaders>(dst, is_v ? j.v_plane : j.k_plane, st, table, h, held, t0, all.lo, T, HELD ? j.sinks : 0, t);
                 cp_commit();
                 if (pending >= 0) {
                     cp_wait<1>();
@@ -323,7 +331,10 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
         const bool live = t < per && tl * per + t < rows;
         // a tile's rows without a token see everything, so that their warp need not mask for them
         Span see{0, INT32_MAX};
-        if (live) see = seen_by(q, tok, tok, j.causal, j.window);
+        if (live) {
+            see = seen_by(q, tok, tok, j.causal, j.window);
+            if (HELD) see = in_places(held, see);
+        }
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // lane 32 (warp % 4) of tensor memory
         const uint32_t s_own = s_at(tl) + lanes + 64 * half, o_own = o_at(tl) + lanes + DP / 2 * half;
         // log2 of a weight at the reference: at 3 half's time over 4096 and 12581 tokens is that at 0, at 8 it is 8 and 12% more
@@ -334,11 +345,11 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
             ok = ok && __all_sync(0xffffffffu, wait(bar.s + 8 * tl, k & 1));
             tc_fence_after();
             const int32_t t0 = (j0 + k) * kN + 64 * half;
-            const int32_t lo = see.lo - t0, hi = see.hi - t0;
+            const int32_t lo = see.lo - t0, hi = see.hi - t0, sinks = HELD ? j.sinks - t0 : 0;
             const bool edge = __any_sync(0xffffffffu, lo > 0 || hi < 64);
             auto masked = [&](float* s, int b) {
 #pragma unroll
-                for (int n = 0; n < 32; ++n) s[n] = 32 * b + n >= lo && 32 * b + n < hi ? s[n] : kNone;
+                for (int n = 0; n < 32; ++n) s[n] = (32 * b + n >= lo || (HELD && 32 * b + n < sinks)) && 32 * b + n < hi ? s[n] : kNone;
             };
             // Against this step's own maximum: the first step, and the first that rows see any key of.
             bool exact = k == 0 || __any_sync(0xffffffffu, live && m == kNone && see.lo < (j0 + k + 1) * kN && see.hi > (j0 + k) * kN);
@@ -596,10 +607,10 @@ bool rows_map(void* map, const StepView& st, const RowsView& rows, bool half) {
 
 namespace {
 
-template <bool HALF, int DP, int TILES>
+template <bool HALF, int DP, int TILES, bool HELD>
 cudaError_t attend_tc(const AttendJob& j, cudaStream_t s) {
     using P = Plan<DP, TILES>;
-    auto* k = kvs_attend_tc_kernel<HALF, DP, TILES>;
+    auto* k = kvs_attend_tc_kernel<HALF, DP, TILES, HELD>;
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, P::bytes);
     if (e != cudaSuccess) return e;
     CUtensorMap km{}, vm{}, qm{};
@@ -619,11 +630,13 @@ cudaError_t attend_tc(const AttendJob& j, cudaStream_t s) {
     return cudaLaunchKernelEx(&cfg, k, j, km, vm, qm, (int32_t)boxes, (int32_t)q_boxes);
 }
 
-template <bool HALF>
+template <bool HALF, bool HELD>
 cudaError_t attend_tiles(const AttendJob& j, cudaStream_t s) {
-    if (j.step.head_dim <= 64) return j.row_tiles == 1 ? attend_tc<HALF, 64, 1>(j, s) : attend_tc<HALF, 64, 2>(j, s);
-    return j.row_tiles == 1 ? attend_tc<HALF, 128, 1>(j, s) : attend_tc<HALF, 128, 2>(j, s);
+    if (j.step.head_dim <= 64) return j.row_tiles == 1 ? attend_tc<HALF, 64, 1, HELD>(j, s) : attend_tc<HALF, 64, 2, HELD>(j, s);
+    return j.row_tiles == 1 ? attend_tc<HALF, 128, 1, HELD>(j, s) : attend_tc<HALF, 128, 2, HELD>(j, s);
 }
+template <bool HALF>
+cudaError_t attend_tiles(const AttendJob& j, cudaStream_t s) { return j.held ? attend_tiles<HALF, true>(j, s) : attend_tiles<HALF, false>(j, s); }
 
 }  // namespace
 

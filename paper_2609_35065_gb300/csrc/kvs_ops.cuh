@@ -75,6 +75,27 @@ __device__ __forceinline__ Span seen_by(const Request& q, int32_t i0, int32_t i1
     return s;
 }
 
+// A window with sinks leaves the first tokens and the last ones visible, and blocks between them may
+// be gone.  The kernels go over such a cache as if it had no others: place u is token u below `cut`
+// and token u + shift behind it.  Places hold whole units of tokens, a unit being what one load
+// brings of a block, so a few tokens that nobody sees are among them: those of [sinks, lo - shift).
+struct Held {
+    int32_t cut, shift;
+};
+__device__ __forceinline__ Held held_of(int32_t lo, int32_t sinks, int32_t unit) {
+    const int32_t first = unit > 1 ? lo / unit * unit : lo, some = min(sinks, lo);
+    const int32_t cut = min(unit > 1 ? (some + unit - 1) / unit * unit : some, first);
+    return Held{cut, first - cut};
+}
+__device__ __forceinline__ int32_t token_at(const Held& h, int32_t u) { return u < h.cut ? u : u + h.shift; }
+// Where shift > 0, cut is at least `sinks`: so in places, too, a row sees [lo, hi) and [0, sinks) of it.
+__device__ __forceinline__ Span in_places(const Held& h, Span s) {
+    // a row that sees nothing has lo = 0 in a request that has no shift
+    s.lo -= h.shift;
+    s.hi -= h.shift;
+    return s;
+}
+
 template <bool HALF>
 struct Num;
 template <>

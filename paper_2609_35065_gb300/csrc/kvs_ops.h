@@ -38,6 +38,9 @@ struct AppendJob {
     const float2*  turns;
     float    scale;
     int32_t  rot_dim, interleaved, q_heads;
+    const uint8_t* axis;             // of each pair
+    int32_t  axes;                   // 0: positions has one entry to a row; else [axes][...] at axis_stride
+    int64_t  axis_stride;
 };
 
 struct AttendJob {
@@ -48,6 +51,8 @@ struct AttendJob {
     float*   partial;                // splits > 1: [splits][rows of total_q * heads][head_dim], then their (m, l) pairs
     float    scale_log2;             // scale * log2(e)
     int32_t  causal, window;
+    int32_t  held;                   // 1: a window with `sinks` first tokens that stay visible
+    int32_t  sinks;
     int32_t  splits;
     int32_t  cluster;                // 1: a head's parts are CTAs of a cluster, which joins them
     int32_t  tc;                     // 1: on the tensor cores' kernel
@@ -63,6 +68,7 @@ struct WeighJob {
     int64_t  request_stride, head_stride;
     float    scale_log2, decay;
     int32_t  causal, window;
+    int32_t  held, sinks;            // as in attention
 };
 
 struct EvictJob {
@@ -82,6 +88,7 @@ struct EvictJob {
 void set_divisors(StepView& st);
 // Each enqueues its kernels and returns how many (negative: a cudaError_t, negated).
 int launch_append(const AppendJob& j, bool half, cudaStream_t s);
+cudaError_t launch_append_axes(const AppendJob& j, bool half, cudaStream_t s);
 int launch_attend(const AttendJob& j, bool half, cudaStream_t s);
 int launch_weigh(const WeighJob& j, bool half, int sms, cudaStream_t s);
 int launch_evict(const EvictJob& j, cudaStream_t s);

@@ -1,5 +1,5 @@
 // kvs_ops_api.cpp -- C entries of the model operators on the paged cache (kvs_append,
-// kvs_attend, kvs_weigh, kvs_evict): arguments are checked on the host before any CUDA
+// kvs_attend, kvs_weigh, kvs_evict and the forms with axes and sinks): arguments are checked on the host before any CUDA
 // call, and the kernels are enqueued on the caller's stream.  Nothing is allocated after
 // the device's first call.
 #include <cmath>
@@ -7,6 +7,7 @@
 #include <cstdio>
 #include <exception>
 #include <new>
+#include <vector>
 
 #include "kvs.h"
 #include "kvs_ops.h"
@@ -23,6 +24,12 @@ int ops_fail(int code, const char* fmt, ...) {
     set_last_error(buf);
     return code;
 }
+
+#define KVS_TRY(call)            \
+    do {                         \
+        const int rc_ = (call);  \
+        if (rc_) return rc_;     \
+    } while (0)
 
 // No C++ exception leaves a C entry.
 template <class F>
@@ -130,6 +137,16 @@ int mask_of(float scale, int32_t window, const kvs_step* s, int32_t& out) {
     return KVS_OK;
 }
 
+// The same with sinks: where the last token of a request of max_kv sees them all, nothing is hidden.
+int held_of(float scale, int32_t window, int32_t sinks, const kvs_step* s, int32_t& window_out, int32_t& held, int32_t& sinks_out) {
+    KVS_TRY(mask_of(scale, window, s, window_out));
+    if (sinks < 0) return ops_fail(KVS_ERR_INVALID_ARG, "sinks is negative");
+    if ((int64_t)window + sinks >= s->max_kv) window_out = 0;
+    held = window_out > 0;
+    sinks_out = held ? sinks : 0;
+    return KVS_OK;
+}
+
 // After a launcher: its status, its count, and the error word if the caller asked for it.
 int done(int launched, cudaStream_t s, uint32_t flags) {
     if (launched < 0) return ops_fail(KVS_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString((cudaError_t)-launched));
@@ -137,15 +154,10 @@ int done(int launched, cudaStream_t s, uint32_t flags) {
     return flags & KVS_F_VALIDATE ? ops_read_error(s) : KVS_OK;
 }
 
-#define KVS_TRY(call)            \
-    do {                         \
-        const int rc_ = (call);  \
-        if (rc_) return rc_;     \
-    } while (0)
-
 constexpr float kLog2e = 1.4426950408889634f;
 
-int append_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* st, int32_t layer, const kvs_append_args* a,
+// axes NULL: positions are on one.
+int append_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* st, int32_t layer, const kvs_append_args* a, const kvs_axes* axes,
                 cudaStream_t s, uint32_t flags) {
     if (!a) return ops_fail(KVS_ERR_INVALID_ARG, "args is NULL");
     AppendJob j{};
@@ -164,8 +176,22 @@ int append_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
         j.interleaved = r.interleaved != 0;
         j.scale = r.scale;
     }
+    if (axes) {
+        if (!a->rope) return ops_fail(KVS_ERR_INVALID_ARG, "rope is NULL");
+        if (axes->num_axes < 1 || axes->num_axes > KVS_MAX_AXES)
+            return ops_fail(KVS_ERR_INVALID_ARG, "num_axes must be in [1, %d] (got %d)", KVS_MAX_AXES, axes->num_axes);
+        if (2 * (int64_t)axes->pairs != a->rope->rot_dim)
+            return ops_fail(KVS_ERR_INVALID_ARG, "axes of %d pairs, rot_dim is %d", axes->pairs, a->rope->rot_dim);
+        if (!axes->axis) return ops_fail(KVS_ERR_INVALID_ARG, "axis is NULL");
+        if (axes->num_axes > 1 && axes->stride < st->total_q)
+            return ops_fail(KVS_ERR_INVALID_ARG, "axes' stride (%lld) is below total_q (%d)", (long long)axes->stride, st->total_q);
+        j.axis = axes->axis;
+        j.axes = axes->num_axes;
+        j.axis_stride = axes->stride;
+    }
     // without a request nothing is read of the step's arrays, which may have no entry
     if (st->total_q == 0 || st->num_requests == 0) return KVS_OK;
+    if (axes && !a->positions) return ops_fail(KVS_ERR_INVALID_ARG, "positions is NULL");
     if (a->q.base) {
         KVS_TRY(rows_of(a->q, st->total_q, a->num_q_heads, "q", j.q));
         KVS_TRY(rows_of(a->q_out, st->total_q, a->num_q_heads, "q_out", j.q_out));
@@ -184,20 +210,31 @@ int append_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     return done(launch_append(j, st->dtype == KVS_DTYPE_F16, s), s, flags);
 }
 
-int64_t workspace_bytes(const StepView& v, int sms) {
-    const AttendPlan plan = attend_plan(v, sms);
+// With sinks a plan goes by the tokens that a CTA's rows may see: the sinks and the window of a tile's
+// tokens, of all of a request's where few rows share a CTA or nothing is hidden behind a token.
+AttendPlan held_plan(StepView v, int32_t held, int32_t causal, int32_t window, int32_t sinks, int sms) {
+    if (held) {
+        const int64_t group = v.group, tile = 2 * tile_rows_of(v.group) / group;
+        const int64_t most = (int64_t)window + sinks + (causal && v.max_q > tile ? tile : v.max_q);
+        if (most < v.max_kv) v.max_kv = (int32_t)most;
+    }
+    return attend_plan(v, sms);
+}
+
+int64_t workspace_bytes(const StepView& v, const AttendPlan& plan) {
     const int n = plan.splits;
     return n <= 1 || plan.cluster ? 0 : (int64_t)n * v.total_q * v.kv_heads * v.group * (v.head_dim + 2) * 4;
 }
 
-int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* st, int32_t layer, const kvs_attend_args* a,
+int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* st, int32_t layer, const kvs_attend_args* a, const int32_t* sinks,
                 cudaStream_t s, uint32_t flags) {
     if (!a) return ops_fail(KVS_ERR_INVALID_ARG, "args is NULL");
     AttendJob j{};
     KVS_TRY(view_of(g, st, a->num_q_heads, j.step));
     KVS_TRY(cache_of(g, c, layer, 2, j.step));
     KVS_TRY(flags_of(flags));
-    KVS_TRY(mask_of(a->scale, a->window, st, j.window));
+    if (sinks) KVS_TRY(held_of(a->scale, a->window, *sinks, st, j.window, j.held, j.sinks));
+    else KVS_TRY(mask_of(a->scale, a->window, st, j.window));
     if (st->total_q == 0 || st->num_requests == 0) return KVS_OK;
     KVS_TRY(rows_of(a->q, st->total_q, a->num_q_heads, "q", j.q));
     KVS_TRY(rows_of(a->out, st->total_q, a->num_q_heads, "out", j.out));
@@ -209,12 +246,12 @@ int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     j.causal = a->causal != 0;
     int sms;
     KVS_TRY(ops_device(&j.step.err, &sms));
-    const AttendPlan plan = attend_plan(j.step, sms);
+    const AttendPlan plan = held_plan(j.step, j.held, j.causal, j.window, j.sinks, sms);
     j.tc = plan.tc;
     j.splits = plan.splits;
     j.cluster = plan.cluster;
     j.row_tiles = plan.row_tiles;
-    const int64_t need = workspace_bytes(j.step, sms);
+    const int64_t need = workspace_bytes(j.step, plan);
     if (need > 0) {
         if (!a->workspace) return ops_fail(KVS_ERR_INVALID_ARG, "workspace is NULL, %lld bytes are needed", (long long)need);
         if (a->workspace_bytes < need)
@@ -225,14 +262,15 @@ int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     return done(launch_attend(j, st->dtype == KVS_DTYPE_F16, s), s, flags);
 }
 
-int weigh_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* st, int32_t layer, const kvs_weigh_args* a,
+int weigh_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* st, int32_t layer, const kvs_weigh_args* a, const int32_t* sinks,
                cudaStream_t s, uint32_t flags) {
     if (!a) return ops_fail(KVS_ERR_INVALID_ARG, "args is NULL");
     WeighJob j{};
     KVS_TRY(view_of(g, st, a->num_q_heads, j.step));
     KVS_TRY(cache_of(g, c, layer, 1, j.step));
     KVS_TRY(flags_of(flags));
-    KVS_TRY(mask_of(a->scale, a->window, st, j.window));
+    if (sinks) KVS_TRY(held_of(a->scale, a->window, *sinks, st, j.window, j.held, j.sinks));
+    else KVS_TRY(mask_of(a->scale, a->window, st, j.window));
     if (!std::isfinite(a->decay)) return ops_fail(KVS_ERR_INVALID_ARG, "decay is not finite");
     if (st->num_requests == 0 || st->max_kv == 0) return KVS_OK;
     if (!a->weights) return ops_fail(KVS_ERR_INVALID_ARG, "weights is NULL");
@@ -341,6 +379,46 @@ int rope_turns(const kvs_rope_spec* sp, float* out, float* scale) {
     return KVS_OK;
 }
 
+int rope_axes(const kvs_rope_spec* sp, const int32_t* parts, int32_t n, int32_t order, float* turns, uint8_t* axis, float* scale) {
+    if (!sp || !parts || !turns || !axis || !scale) return ops_fail(KVS_ERR_INVALID_ARG, "spec, parts, turns_out, axis_out or scale_out is NULL");
+    if (n < 1 || n > KVS_MAX_AXES) return ops_fail(KVS_ERR_INVALID_ARG, "num_axes must be in [1, %d] (got %d)", KVS_MAX_AXES, n);
+    if (order & ~(KVS_AXES_CYCLE | KVS_AXES_RESTART)) return ops_fail(KVS_ERR_INVALID_ARG, "unknown order %d", order);
+    int64_t pairs = 0;
+    for (int a = 0; a < n; ++a) {
+        if (parts[a] < 1) return ops_fail(KVS_ERR_INVALID_ARG, "axis %d has %d pairs", a, parts[a]);
+        pairs += parts[a];
+    }
+    if (sp->rot_dim != 2 * pairs) return ops_fail(KVS_ERR_INVALID_ARG, "rot_dim (%d) is not twice the %lld pairs", sp->rot_dim, (long long)pairs);
+    if (order & KVS_AXES_CYCLE) {
+        for (int64_t k = 0; k < pairs; ++k) axis[k] = 0;
+        for (int a = 1; a < n; ++a) {
+            if (a + (int64_t)n * (parts[a] - 1) >= pairs) return ops_fail(KVS_ERR_INVALID_ARG, "axis %d has no turn for %d pairs", a, parts[a]);
+            for (int64_t k = 0; k < parts[a]; ++k) axis[a + n * k] = (uint8_t)a;
+        }
+    } else {
+        int64_t k = 0;
+        for (int a = 0; a < n; ++a)
+            for (int32_t m = 0; m < parts[a]; ++m) axis[k++] = (uint8_t)a;
+    }
+    KVS_TRY(rope_turns(sp, turns, scale));
+    if (!(order & KVS_AXES_RESTART)) return KVS_OK;
+    // each axis's own table, of which its pairs take the entries in turn
+    std::vector<float> own;
+    for (int a = 0; a < n; ++a) {
+        kvs_rope_spec one = *sp;
+        one.rot_dim = 2 * parts[a];
+        own.resize(2 * (size_t)parts[a]);
+        KVS_TRY(rope_turns(&one, own.data(), scale));
+        for (int64_t k = 0, at = 0; k < pairs; ++k) {
+            if (axis[k] != a) continue;
+            turns[2 * k] = own[2 * at];
+            turns[2 * k + 1] = own[2 * at + 1];
+            ++at;
+        }
+    }
+    return KVS_OK;
+}
+
 }  // namespace
 }  // namespace kvs
 
@@ -352,14 +430,32 @@ int kvs_rope_turns(const kvs_rope_spec* spec, float* turns_out, float* scale_out
     return entry([&] { return rope_turns(spec, turns_out, scale_out); });
 }
 
+int kvs_rope_axes(const kvs_rope_spec* spec, const int32_t* parts, int32_t num_axes, int32_t order, float* turns_out,
+                  uint8_t* axis_out, float* scale_out) {
+    return entry([&] { return rope_axes(spec, parts, num_axes, order, turns_out, axis_out, scale_out); });
+}
+
 int kvs_append(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
                const kvs_append_args* args, void* cuda_stream, uint32_t flags) {
-    return entry([&] { return append_call(geom, cache, step, layer, args, (cudaStream_t)cuda_stream, flags); });
+    return entry([&] { return append_call(geom, cache, step, layer, args, nullptr, (cudaStream_t)cuda_stream, flags); });
+}
+
+int kvs_append_axes(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
+                    const kvs_append_args* args, const kvs_axes* axes, void* cuda_stream, uint32_t flags) {
+    return entry([&] {
+        if (!axes) return ops_fail(KVS_ERR_INVALID_ARG, "axes is NULL");
+        return append_call(geom, cache, step, layer, args, axes, (cudaStream_t)cuda_stream, flags);
+    });
 }
 
 int kvs_attend(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
                const kvs_attend_args* args, void* cuda_stream, uint32_t flags) {
-    return entry([&] { return attend_call(geom, cache, step, layer, args, (cudaStream_t)cuda_stream, flags); });
+    return entry([&] { return attend_call(geom, cache, step, layer, args, nullptr, (cudaStream_t)cuda_stream, flags); });
+}
+
+int kvs_attend_sinks(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
+                     const kvs_attend_args* args, int32_t sinks, void* cuda_stream, uint32_t flags) {
+    return entry([&] { return attend_call(geom, cache, step, layer, args, &sinks, (cudaStream_t)cuda_stream, flags); });
 }
 
 int64_t kvs_attend_workspace(const kvs_geometry* geom, const kvs_step* step, int32_t num_q_heads) {
@@ -370,7 +466,24 @@ int64_t kvs_attend_workspace(const kvs_geometry* geom, const kvs_step* step, int
         int32_t* err;
         int sms;
         KVS_TRY(ops_device(&err, &sms));
-        bytes = workspace_bytes(v, sms);
+        bytes = workspace_bytes(v, attend_plan(v, sms));
+        return (int)KVS_OK;
+    });
+    return rc ? rc : bytes;
+}
+
+int64_t kvs_attend_sinks_workspace(const kvs_geometry* geom, const kvs_step* step, int32_t num_q_heads, int32_t causal,
+                                   int32_t window, int32_t sinks) {
+    int64_t bytes = 0;
+    const int rc = entry([&] {
+        StepView v;
+        int32_t held = 0;
+        KVS_TRY(view_of(geom, step, num_q_heads, v));
+        KVS_TRY(held_of(1.0f, window, sinks, step, window, held, sinks));
+        int32_t* err;
+        int sms;
+        KVS_TRY(ops_device(&err, &sms));
+        bytes = workspace_bytes(v, held_plan(v, held, causal, window, sinks, sms));
         return (int)KVS_OK;
     });
     return rc ? rc : bytes;
@@ -378,7 +491,12 @@ int64_t kvs_attend_workspace(const kvs_geometry* geom, const kvs_step* step, int
 
 int kvs_weigh(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
               const kvs_weigh_args* args, void* cuda_stream, uint32_t flags) {
-    return entry([&] { return weigh_call(geom, cache, step, layer, args, (cudaStream_t)cuda_stream, flags); });
+    return entry([&] { return weigh_call(geom, cache, step, layer, args, nullptr, (cudaStream_t)cuda_stream, flags); });
+}
+
+int kvs_weigh_sinks(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
+                    const kvs_weigh_args* args, int32_t sinks, void* cuda_stream, uint32_t flags) {
+    return entry([&] { return weigh_call(geom, cache, step, layer, args, &sinks, (cudaStream_t)cuda_stream, flags); });
 }
 
 int kvs_evict(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step,

@@ -10,7 +10,7 @@
  * What it replaces cost 10 to 16 us for one chunk and 80 us for 128, most of a small
  * call; this takes about 1 us and 25 us.
  *
- * append, attend, weigh and evict do the same for the model operators' tensors: whatever is not
+ * append, attend, weigh (and their forms with axes and sinks) and evict do the same for the model operators' tensors: whatever is not
  * plainly right (a type, a shape, a stride) is left to the binding, which says what is wrong.
  */
 #define PY_SSIZE_T_CLEAN
@@ -386,10 +386,54 @@ static PyObject* run_op(int got, int64_t fn, const StepRef* st, int64_t layer, c
     return PyLong_FromLong(rc);
 }
 
+typedef int (*sinks_fn)(const kvs_geometry*, const kvs_paged_cache*, const kvs_step*, int32_t, const void*, int32_t, void*, uint32_t);
+
+static PyObject* run_sinks_op(int got, int64_t fn, const StepRef* st, int64_t layer, const void* args, int64_t sinks, int64_t stream, int64_t flags) {
+    if (got < 0) return NULL;
+    if (got == 0) Py_RETURN_NONE;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((sinks_fn)(uintptr_t)fn)(st->geom, st->cache, st->step, (int32_t)layer, args, (int32_t)sinks, (void*)(uintptr_t)stream, (uint32_t)flags);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 #define TRY(call)                   \
     do {                            \
         if (got == 1) got = (call); \
     } while (0)
+
+/* The struct behind an object's ref (its address); 1 / 0. */
+static int read_ref(PyObject* o, const void** out) {
+    int64_t x = 0;
+    PyObject* ref = PyObject_GetAttr(o, s_ref);
+    const int ok = ref && small_int(ref, 1, INT64_MAX, &x);
+    Py_XDECREF(ref);
+    if (PyErr_Occurred()) PyErr_Clear();
+    *out = (const void*)(uintptr_t)x;
+    return ok;
+}
+
+/* q, k, v, q_out, rope */
+static int read_append(PyObject* const* v, const StepRef* st, int got, kvs_append_args* a) {
+    PyObject* const* w = v + V_MORE;
+    int64_t heads = 0;
+    if (w[0] != Py_None) {
+        TRY(read_rows(w[0], v[V_DTYPE], st, &heads, &a->q));
+        a->num_q_heads = (int32_t)heads;
+        if (w[3] == Py_None) a->q_out = a->q;
+        else TRY(read_rows(w[3], v[V_DTYPE], st, &heads, &a->q_out));
+    }
+    int64_t H = got == 1 ? st->geom->num_kv_heads : 1;
+    TRY(read_rows(w[1], v[V_DTYPE], st, &H, &a->k));
+    TRY(read_rows(w[2], v[V_DTYPE], st, &H, &a->v));
+    if (w[4] != Py_None) {
+        const void* p = NULL;
+        TRY(read_ref(w[4], &p));
+        a->rope = (const kvs_rope*)p;
+    }
+    return got;
+}
 
 /* ..., q, k, v, q_out, rope, positions */
 static PyObject* append(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
@@ -402,29 +446,11 @@ static PyObject* append(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
         PyErr_SetString(PyExc_TypeError, "append takes 14 arguments");
         return NULL;
     }
-    int got = read_common(v, &fn, &st, &layer, &stream, &flags);
-    PyObject* const* w = v + V_MORE;
-    int64_t heads = 0;
-    if (w[0] != Py_None) {
-        TRY(read_rows(w[0], v[V_DTYPE], &st, &heads, &a.q));
-        a.num_q_heads = (int32_t)heads;
-        if (w[3] == Py_None) a.q_out = a.q;
-        else TRY(read_rows(w[3], v[V_DTYPE], &st, &heads, &a.q_out));
-    }
-    int64_t H = got == 1 ? st.geom->num_kv_heads : 1;
-    TRY(read_rows(w[1], v[V_DTYPE], &st, &H, &a.k));
-    TRY(read_rows(w[2], v[V_DTYPE], &st, &H, &a.v));
-    if (w[4] != Py_None && got == 1) {
-        PyObject* ref = PyObject_GetAttr(w[4], s_ref);
-        int64_t x = 0;
-        got = ref && small_int(ref, 1, INT64_MAX, &x);
-        Py_XDECREF(ref);
-        if (PyErr_Occurred()) PyErr_Clear();
-        a.rope = (const kvs_rope*)(uintptr_t)x;
-    }
-    if (w[5] != Py_None) {
+    int got = read_append(v, &st, read_common(v, &fn, &st, &layer, &stream, &flags), &a);
+    PyObject* positions = v[V_MORE + 5];
+    if (positions != Py_None) {
         Tensor t;
-        TRY(read_tensor(w[5], v[V_I32], 1, &t));
+        TRY(read_tensor(positions, v[V_I32], 1, &t));
         if (got == 1) {
             got = t.shape[0] == st.step->total_q && (t.shape[0] <= 1 || t.stride[0] == 1);
             a.positions = (const int32_t*)(uintptr_t)t.at;
@@ -433,10 +459,76 @@ static PyObject* append(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
     return run_op(got, fn, &st, layer, &a, stream, flags);
 }
 
+typedef int (*axes_fn)(const kvs_geometry*, const kvs_paged_cache*, const kvs_step*, int32_t, const void*, const kvs_axes*, void*, uint32_t);
+
+/* ..., q, k, v, q_out, rope, axes, positions */
+static PyObject* append_axes(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
+    (void)self;
+    int64_t fn, layer, stream, flags;
+    StepRef st;
+    kvs_append_args a;
+    kvs_axes x;
+    memset(&a, 0, sizeof a);
+    memset(&x, 0, sizeof x);
+    if (nv != V_MORE + 7) {
+        PyErr_SetString(PyExc_TypeError, "append_axes takes 15 arguments");
+        return NULL;
+    }
+    int got = read_append(v, &st, read_common(v, &fn, &st, &layer, &stream, &flags), &a);
+    PyObject* const* w = v + V_MORE;
+    const void* p = NULL;
+    Tensor t;
+    if (w[4] == Py_None) got = got < 0 ? got : 0;
+    TRY(read_ref(w[5], &p));
+    if (got == 1) memcpy(&x, p, sizeof x);
+    TRY(read_tensor(w[6], v[V_I32], 2, &t));
+    if (got == 1) {
+        got = t.shape[0] == x.num_axes && t.shape[1] == st.step->total_q && (t.shape[1] <= 1 || t.stride[1] == 1);
+        a.positions = (const int32_t*)(uintptr_t)t.at;
+        x.stride = t.stride[0];
+    }
+    if (got < 0) return NULL;
+    if (got == 0) Py_RETURN_NONE;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((axes_fn)(uintptr_t)fn)(st.geom, st.cache, st.step, (int32_t)layer, &a, &x, (void*)(uintptr_t)stream, (uint32_t)flags);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* q, out, lse, scale, causal, window */
+static int read_attend(PyObject* const* v, const StepRef* st, int got, kvs_attend_args* a) {
+    PyObject* const* w = v + V_MORE;
+    int64_t heads = 0, window = 0;
+    TRY(read_rows(w[0], v[V_DTYPE], st, &heads, &a->q));
+    TRY(read_rows(w[1], v[V_DTYPE], st, &heads, &a->out));
+    if (w[2] != Py_None) {
+        void* p = NULL;
+        TRY(read_lse(w[2], v[V_F32], st, heads, &p));
+        a->lse = (float*)p;
+    }
+    TRY(read_float(w[3], &a->scale));
+    TRY(read_bool(w[4], &a->causal));
+    TRY(small_int(w[5], INT32_MIN, INT32_MAX, &window));
+    a->window = (int32_t)window;
+    a->num_q_heads = (int32_t)heads;
+    return got;
+}
+
+static int read_workspace(PyObject* o, PyObject* byte, kvs_attend_args* a) {
+    Tensor t;
+    if (o == Py_None) return 1;
+    const int ok = read_tensor(o, byte, 1, &t);
+    if (ok != 1) return ok;
+    a->workspace = (void*)(uintptr_t)t.at;
+    a->workspace_bytes = t.shape[0];
+    return t.stride[0] == 1 || t.shape[0] <= 1;
+}
+
 /* ..., q, out, lse, scale, causal, window, workspace, uint8 */
 static PyObject* attend(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
     (void)self;
-    int64_t fn, layer, stream, flags, window = 0;
+    int64_t fn, layer, stream, flags;
     StepRef st;
     kvs_attend_args a;
     memset(&a, 0, sizeof a);
@@ -444,37 +536,57 @@ static PyObject* attend(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
         PyErr_SetString(PyExc_TypeError, "attend takes 16 arguments");
         return NULL;
     }
-    int got = read_common(v, &fn, &st, &layer, &stream, &flags);
-    PyObject* const* w = v + V_MORE;
-    int64_t heads = 0;
-    TRY(read_rows(w[0], v[V_DTYPE], &st, &heads, &a.q));
-    TRY(read_rows(w[1], v[V_DTYPE], &st, &heads, &a.out));
-    if (w[2] != Py_None) {
-        void* p = NULL;
-        TRY(read_lse(w[2], v[V_F32], &st, heads, &p));
-        a.lse = (float*)p;
-    }
-    TRY(read_float(w[3], &a.scale));
-    TRY(read_bool(w[4], &a.causal));
-    TRY(small_int(w[5], INT32_MIN, INT32_MAX, &window));
-    if (w[6] != Py_None) {
-        Tensor t;
-        TRY(read_tensor(w[6], w[7], 1, &t));
-        if (got == 1) {
-            got = t.stride[0] == 1 || t.shape[0] <= 1;
-            a.workspace = (void*)(uintptr_t)t.at;
-            a.workspace_bytes = t.shape[0];
-        }
-    }
-    a.window = (int32_t)window;
-    a.num_q_heads = (int32_t)heads;
+    int got = read_attend(v, &st, read_common(v, &fn, &st, &layer, &stream, &flags), &a);
+    TRY(read_workspace(v[V_MORE + 6], v[V_MORE + 7], &a));
     return run_op(got, fn, &st, layer, &a, stream, flags);
+}
+
+/* ..., q, out, lse, scale, causal, window, sinks, workspace, uint8 */
+static PyObject* attend_sinks(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
+    (void)self;
+    int64_t fn, layer, stream, flags, sinks = 0;
+    StepRef st;
+    kvs_attend_args a;
+    memset(&a, 0, sizeof a);
+    if (nv != V_MORE + 9) {
+        PyErr_SetString(PyExc_TypeError, "attend_sinks takes 17 arguments");
+        return NULL;
+    }
+    int got = read_attend(v, &st, read_common(v, &fn, &st, &layer, &stream, &flags), &a);
+    TRY(small_int(v[V_MORE + 6], INT32_MIN, INT32_MAX, &sinks));
+    TRY(read_workspace(v[V_MORE + 7], v[V_MORE + 8], &a));
+    return run_sinks_op(got, fn, &st, layer, &a, sinks, stream, flags);
+}
+
+/* q, lse, weights, scale, decay, causal, window */
+static int read_weigh(PyObject* const* v, const StepRef* st, int got, kvs_weigh_args* a) {
+    PyObject* const* w = v + V_MORE;
+    int64_t heads = 0, window = 0;
+    void* p = NULL;
+    Tensor t;
+    TRY(read_rows(w[0], v[V_DTYPE], st, &heads, &a->q));
+    TRY(read_lse(w[1], v[V_F32], st, heads, &p));
+    TRY(read_tensor(w[2], v[V_F32], 3, &t));
+    if (got == 1) {
+        got = t.shape[0] == st->step->num_requests && t.shape[1] == st->geom->num_kv_heads && t.shape[2] >= st->step->max_kv && t.stride[2] == 1;
+        a->weights = (float*)(uintptr_t)t.at;
+        a->request_stride = t.stride[0];
+        a->head_stride = t.stride[1];
+    }
+    TRY(read_float(w[3], &a->scale));
+    TRY(read_float(w[4], &a->decay));
+    TRY(read_bool(w[5], &a->causal));
+    TRY(small_int(w[6], INT32_MIN, INT32_MAX, &window));
+    a->lse = (const float*)p;
+    a->window = (int32_t)window;
+    a->num_q_heads = (int32_t)heads;
+    return got;
 }
 
 /* ..., q, lse, weights, scale, decay, causal, window */
 static PyObject* weigh(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
     (void)self;
-    int64_t fn, layer, stream, flags, window = 0;
+    int64_t fn, layer, stream, flags;
     StepRef st;
     kvs_weigh_args a;
     memset(&a, 0, sizeof a);
@@ -482,28 +594,24 @@ static PyObject* weigh(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
         PyErr_SetString(PyExc_TypeError, "weigh takes 15 arguments");
         return NULL;
     }
-    int got = read_common(v, &fn, &st, &layer, &stream, &flags);
-    PyObject* const* w = v + V_MORE;
-    int64_t heads = 0;
-    void* p = NULL;
-    Tensor t;
-    TRY(read_rows(w[0], v[V_DTYPE], &st, &heads, &a.q));
-    TRY(read_lse(w[1], v[V_F32], &st, heads, &p));
-    TRY(read_tensor(w[2], v[V_F32], 3, &t));
-    if (got == 1) {
-        got = t.shape[0] == st.step->num_requests && t.shape[1] == st.geom->num_kv_heads && t.shape[2] >= st.step->max_kv && t.stride[2] == 1;
-        a.weights = (float*)(uintptr_t)t.at;
-        a.request_stride = t.stride[0];
-        a.head_stride = t.stride[1];
-    }
-    TRY(read_float(w[3], &a.scale));
-    TRY(read_float(w[4], &a.decay));
-    TRY(read_bool(w[5], &a.causal));
-    TRY(small_int(w[6], INT32_MIN, INT32_MAX, &window));
-    a.lse = (const float*)p;
-    a.window = (int32_t)window;
-    a.num_q_heads = (int32_t)heads;
+    const int got = read_weigh(v, &st, read_common(v, &fn, &st, &layer, &stream, &flags), &a);
     return run_op(got, fn, &st, layer, &a, stream, flags);
+}
+
+/* ..., q, lse, weights, scale, decay, causal, window, sinks */
+static PyObject* weigh_sinks(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
+    (void)self;
+    int64_t fn, layer, stream, flags, sinks = 0;
+    StepRef st;
+    kvs_weigh_args a;
+    memset(&a, 0, sizeof a);
+    if (nv != V_MORE + 8) {
+        PyErr_SetString(PyExc_TypeError, "weigh_sinks takes 16 arguments");
+        return NULL;
+    }
+    int got = read_weigh(v, &st, read_common(v, &fn, &st, &layer, &stream, &flags), &a);
+    TRY(small_int(v[V_MORE + 7], INT32_MIN, INT32_MAX, &sinks));
+    return run_sinks_op(got, fn, &st, layer, &a, sinks, stream, flags);
 }
 
 typedef int (*evict_fn)(const kvs_geometry*, const kvs_paged_cache*, const kvs_step*, const kvs_evict_args*, void*, uint32_t);
@@ -584,7 +692,8 @@ static PyObject* evict(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
 }
 
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
-static PyMethodDef methods[] = {METHOD(call), METHOD(append), METHOD(attend), METHOD(weigh), METHOD(evict), {NULL, NULL, 0, NULL}};
+static PyMethodDef methods[] = {METHOD(call), METHOD(append), METHOD(append_axes), METHOD(attend), METHOD(attend_sinks),
+                                METHOD(weigh), METHOD(weigh_sinks), METHOD(evict), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "kvs_pycall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit_kvs_pycall(void) {

@@ -27,6 +27,33 @@ __device__ __forceinline__ RowSpan rows_seeing(const StepView& st, const Request
     return RowSpan{(int32_t)first * st.group, (int32_t)max(first, end) * st.group};
 }
 
+// The same of places u_lo .. u_hi of a window with sinks (token_at): sinks are seen by all rows from
+// theirs on; a place that is neither a sink nor in the first row's window is seen by none.
+__device__ __forceinline__ RowSpan rows_seeing(const StepView& st, const Request& q, const Held& held, int32_t u_lo, int32_t u_hi, int32_t causal, int32_t window,
+                                               int32_t sinks) {
+    return rows_seeing(st, q, token_at(held, u_lo), token_at(held, u_hi), causal, u_lo < sinks ? 0 : window);
+}
+
+// Tokens without a place, [cut, cut + shift): nobody sees them, and only what they had before fades.
+// This is part `part` of `parts` of the request's and head's.
+__device__ __forceinline__ void fade(const WeighJob& j, int32_t r, int32_t h, const Held& held, int32_t part, int32_t parts) {
+    if (j.decay == 1.0f) return;
+    float* w = j.weights + r * j.request_stride + h * j.head_stride + held.cut;
+    const int32_t a = (int32_t)((int64_t)held.shift * part / parts), b = (int32_t)((int64_t)held.shift * (part + 1) / parts);
+    constexpr int kFlight = 8;
+    for (int32_t t0 = a + threadIdx.x; t0 < b; t0 += kFlight * blockDim.x) {
+        float x[kFlight];
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+            x[k] = 0.0f;
+            if (j.decay != 0.0f && t0 + k * (int32_t)blockDim.x < b) x[k] = w[t0 + k * (int32_t)blockDim.x];
+        }
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k)
+            if (t0 + k * (int32_t)blockDim.x < b) w[t0 + k * (int32_t)blockDim.x] = j.decay * x[k];
+    }
+}
+
 __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t h, int32_t t, float sum) {
     float* w = j.weights + r * j.request_stride + h * j.head_stride + t;
     *w = j.decay == 0.0f ? sum : j.decay * *w + sum;
@@ -70,9 +97,12 @@ struct WPlan {
     static constexpr int bytes = bars + 512 + 1024;
 };
 
-template <bool HALF, int DP, int KT>
+// HELD: a window with sinks.  Key tiles are of its places then, and clusters behind their `places`
+// ones let the tokens fade that have none.
+template <bool HALF, int DP, int KT, bool HELD>
 __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap k_map,
-                                                                   const __grid_constant__ CUtensorMap q_map, int32_t k_boxes, int32_t q_boxes, int32_t share) {
+                                                                   const __grid_constant__ CUtensorMap q_map, int32_t k_boxes, int32_t q_boxes, int32_t share,
+                                                                   int32_t places) {
     extern __shared__ char raw[];
     using P = WPlan<DP, KT>;
     constexpr int kThreads = P::threads, kStages = P::stages, kAccs = P::accs, kKeysTc = P::keys, kIssuer = P::issuer;
@@ -85,11 +115,22 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
     const int warp = warp_number(), lane = threadIdx.x & 31, wg = warp >> 2;
     const int32_t r = blockIdx.z, h = blockIdx.y, rank = blockIdx.x % share, t0 = (blockIdx.x / share) * kKeysTc;
     const Request q = load_request(st, r);
-    if (t0 >= q.T) return;                                       // the whole cluster
+    Held held{};
+    int32_t T = q.T;                                             // places (without HELD: tokens) of the cache
+    if (HELD) {
+        held = held_of(seen_by(q, 0, max(q.n, 1) - 1, j.causal, j.window).lo, j.sinks, k_boxes ? min(st.block_size, 128) : 1);
+        T -= held.shift;
+        if (blockIdx.x >= places) {
+            fade(j, r, h, held, blockIdx.x - places, gridDim.x - places);
+            return;                                              // as all of its cluster does
+        }
+    }
+    if (t0 >= T) return;                                         // the whole cluster
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
     const int32_t per = tile_rows_of(st.group);                  // rows of a tile
-    const int32_t key_tiles = KT == 2 && t0 + 128 < q.T ? 2 : 1;
-    const RowSpan any = rows_seeing(st, q, t0, min(t0 + kKeysTc, q.T) - 1, j.causal, j.window);
+    const int32_t key_tiles = KT == 2 && t0 + 128 < T ? 2 : 1;
+    const RowSpan any = HELD ? rows_seeing(st, q, held, t0, min(t0 + kKeysTc, T) - 1, j.causal, j.window, j.sinks)
+                             : rows_seeing(st, q, t0, min(t0 + kKeysTc, T) - 1, j.causal, j.window);
     const int32_t tile0 = any.first / per, tiles = any.end > any.first ? (any.end + per - 1) / per - tile0 : 0;
     const int32_t mine = (tiles - rank + share - 1) / share;     // row tiles tile0 + rank + share * i
     const int32_t total = q.n * st.group;
@@ -183,8 +224,8 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
         };
         if (mine > 0) {
             for (int32_t kt = 0; kt < key_tiles; ++kt) {
-                if (k_boxes) tile_boxes<DP>(base + kt * P::tile, &k_map, st, h, box_of<DP, 3>(st, table, t0 + 128 * kt, q.T, warp - kIssuer - 1, lane), b_load, lane);
-                else tile_rows<DP, 96>(base + kt * P::tile, j.k_plane, st, table, h, t0 + 128 * kt, 0, q.T, u);
+                if (k_boxes) tile_boxes<DP>(base + kt * P::tile, &k_map, st, h, box_of<DP, 3>(st, table, held, t0 + 128 * kt, T, warp - kIssuer - 1, lane), b_load, lane);
+                else tile_rows<DP, 96>(base + kt * P::tile, j.k_plane, st, table, h, held, t0 + 128 * kt, 0, T, 0, u);
             }
             if (!k_boxes) {
                 cp_commit();
@@ -305,8 +346,8 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
         const int kt = wg >> 1, half = wg & 1;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
         const int32_t key = t0 + 128 * kt + t;
-        const bool live = key < q.T;
-        RowSpan see = rows_seeing(st, q, key, key, j.causal, j.window);
+        const bool live = key < T;
+        RowSpan see = HELD ? rows_seeing(st, q, held, key, key, j.causal, j.window, j.sinks) : rows_seeing(st, q, key, key, j.causal, j.window);
         if (!live) see.end = see.first;
         const float c = j.scale_log2;
         const int32_t columns = min(64, per - 64 * half);
@@ -383,9 +424,9 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
     const float* sums = reinterpret_cast<const float*>(mem + P::sums);        // [key tile][half][128]
     const int32_t at_sum = (threadIdx.x >> 7) * 256 + t;
     const int32_t key = t0 + (int32_t)threadIdx.x;               // of the first 256 threads: key tile by key tile
-    const bool mine_to_write = threadIdx.x < kKeysTc && key < q.T;
+    const bool mine_to_write = threadIdx.x < kKeysTc && key < T;
     if (share == 1) {
-        if (mine_to_write) add_weight(j, r, h, key, sums[at_sum] + sums[at_sum + 128]);
+        if (mine_to_write) add_weight(j, r, h, token_at(held, key), sums[at_sum] + sums[at_sum + 128]);
         return;
     }
     cluster_sync();
@@ -398,7 +439,7 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
             asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at + 512) : "memory");
             x += u + v;
         }
-        add_weight(j, r, h, key, x);
+        add_weight(j, r, h, token_at(held, key), x);
     }
     cluster_sync();
 }
@@ -436,8 +477,8 @@ struct RowFrags {
     float lse[2];                // times -log2(e)
     Span  see[2];
 };
-template <int K>
-__device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, const Request& q, int32_t h, int32_t p0, int lane) {
+template <int K, bool HELD>
+__device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, const Request& q, const Held& held, int32_t h, int32_t p0, int lane) {
     const StepView& st = j.step;
     const int32_t total = q.n * st.group, c = lane & 3, p = p0 + (lane >> 2);
     int32_t g = 0;
@@ -457,6 +498,7 @@ __device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, con
         if (x < total) {
             const int32_t t = token_of(st, x, g);
             f.see[e] = seen_by(q, t, t, j.causal, j.window);
+            if (HELD) f.see[e] = in_places(held, f.see[e]);
             f.lse[e] = -kLog2e * __ldg(j.lse + (int64_t)(q.q0 + t) * (st.kv_heads * st.group) + h * st.group + g);
         }
     }
@@ -466,7 +508,9 @@ __device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, con
 // whose fragments are loaded (from L1) for every 16 keys; 16 rows take 27 us with and 38 without
 // them staying (8 requests x 8 heads of 64 dims, 8000 tokens), with 128 dims 45 and 48 (where two
 // of them spill some 150 bytes, and what a call cannot do without is 19 us).
-template <bool HALF, int DP, int STAY>
+// HELD: a window with sinks.  The tiles are of its places (of one token each), and a CTA lets its share
+// of the tokens fade that have none.
+template <bool HALF, int DP, int STAY, bool HELD>
 __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(WeighJob j) {
     constexpr int K = DP / 32;                                   // 16-byte vectors of a lane and key
     const StepView& st = j.step;
@@ -474,8 +518,15 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
     const int32_t h = blockIdx.y, r = blockIdx.z;
     const Request q = load_request(st, r);
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
+    Held held{};
+    int32_t T = q.T;                                             // places (without HELD: tokens) of the cache
+    if (HELD) {
+        held = held_of(seen_by(q, 0, max(q.n, 1) - 1, j.causal, j.window).lo, j.sinks, 1);
+        T -= held.shift;
+        fade(j, r, h, held, blockIdx.x, gridDim.x);
+    }
     // this CTA's tiles of 16 keys, of which its warps take every eighth
-    const int32_t all = (q.T + kRowKeys - 1) / kRowKeys;
+    const int32_t all = (T + kRowKeys - 1) / kRowKeys;
     const int32_t first = (int32_t)((int64_t)all * blockIdx.x / gridDim.x), end = (int32_t)((int64_t)all * (blockIdx.x + 1) / gridDim.x);
     const int32_t mine = (end - first - warp + kRowWarps - 1) / kRowWarps;
     if (mine <= 0) return;
@@ -485,7 +536,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int32_t t = key0(n) + i + 8 * e;
-            row[e] = n < mine && t < q.T ? row_of(st, table, t) : -1;
+            row[e] = n < mine && t < T ? row_of(st, table, token_at(held, t)) : -1;
         }
     };
     // lanes 4 i and 4 i + 1 add to the weights of keys i and i + 8, which they load with the keys
@@ -493,7 +544,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
     auto load = [&](int32_t n, const int64_t (&row)[2], uint4 (&kv)[2][K], float& old) {
         const int32_t t = key0(n) + i + 8 * c;
         old = 0.0f;
-        if (j.decay != 0.0f && n < mine && c < 2 && t < q.T) old = weights[t];
+        if (j.decay != 0.0f && n < mine && c < 2 && t < T) old = weights[token_at(held, t)];
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -518,7 +569,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int32_t key = t + 8 * (e >> 1);
-                if (key >= f.see[e & 1].lo && key < f.see[e & 1].hi) sum[e >> 1] += exp2_fast(fmaf(s[e] + u[e], j.scale_log2, f.lse[e & 1]));
+                if ((key >= f.see[e & 1].lo || (HELD && key < j.sinks)) && key < f.see[e & 1].hi) sum[e >> 1] += exp2_fast(fmaf(s[e] + u[e], j.scale_log2, f.lse[e & 1]));
             }
         };
 #pragma unroll
@@ -526,7 +577,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
         if (STAY == 0) {
             for (int32_t p0 = 0; p0 < total; p0 += 8) {
                 RowFrags<K> f;
-                load_rows<K>(f, j, q, h, p0, lane);
+                load_rows<K, HELD>(f, j, q, held, h, p0, lane);
                 add(f);
             }
         }
@@ -535,7 +586,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
             sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 1);
             sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 2);
         }
-        if (c < 2 && t + 8 * c < q.T) weights[t + 8 * c] = j.decay * old + (c ? sum[1] : sum[0]);
+        if (c < 2 && t + 8 * c < T) weights[token_at(held, t + 8 * c)] = j.decay * old + (c ? sum[1] : sum[0]);
     };
     uint4 ka[2][K], kb[2][K];
     float wa, wb;
@@ -544,7 +595,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
     load(0, row, ka, wa);
     look_up(1, row);
 #pragma unroll
-    for (int x = 0; x < STAY; ++x) load_rows<K>(stay[x], j, q, h, 8 * x, lane);
+    for (int x = 0; x < STAY; ++x) load_rows<K, HELD>(stay[x], j, q, held, h, 8 * x, lane);
     for (int32_t n = 0; n < mine; n += 2) {
         load(n + 1, row, kb, wb);
         look_up(n + 2, row);
@@ -555,21 +606,30 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
     }
 }
 
-template <bool HALF, int DP, int KT>
+// Places of a window with sinks, at most.
+int64_t places_of(const WeighJob& j, int64_t unit) {
+    const int64_t most = (int64_t)j.sinks + j.window + j.step.max_q + 2 * unit;
+    return most < j.step.max_kv ? most : j.step.max_kv;
+}
+
+template <bool HALF, int DP, int KT, bool HELD>
 cudaError_t weigh_tc(const WeighJob& j, int sms, cudaStream_t s) {
     using P = WPlan<DP, KT>;
     const StepView& st = j.step;
     const int64_t rows = (int64_t)st.max_q * st.group;
-    auto* k = kvs_weigh_tc_kernel<HALF, DP, KT>;
+    auto* k = kvs_weigh_tc_kernel<HALF, DP, KT, HELD>;
     cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, P::bytes);
     if (e != cudaSuccess) return e;
     CUtensorMap km{}, qm{};
     const bool k_boxes = plane_map(&km, st, j.k_plane, HALF), q_boxes = rows_map(&qm, st, j.q, HALF);
-    const int64_t x = (st.max_kv + P::keys - 1) / P::keys, tiles = x * st.kv_heads * st.requests, row_tiles = (rows + 127) / 128;
+    const int64_t tokens = HELD ? places_of(j, 128) : st.max_kv;
+    const int64_t x = (tokens + P::keys - 1) / P::keys, tiles = x * st.kv_heads * st.requests, row_tiles = (rows + 127) / 128;
     int share = 1;
     while (share < 8 && tiles * share * 2 <= sms && share * 2 <= row_tiles) share *= 2;
+    // a CTA for every 16384 tokens that fade
+    const int64_t fading = HELD && j.decay != 1.0f ? (st.max_kv + 16383) / 16384 : 0;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(x * share), st.kv_heads, st.requests);
+    cfg.gridDim = dim3((unsigned)((x + (fading + share - 1) / share) * share), st.kv_heads, st.requests);
     cfg.blockDim = dim3(P::threads);
     cfg.dynamicSmemBytes = P::bytes;
     cfg.stream = s;
@@ -579,10 +639,10 @@ cudaError_t weigh_tc(const WeighJob& j, int sms, cudaStream_t s) {
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = share > 1;
-    return cudaLaunchKernelEx(&cfg, k, j, km, qm, (int32_t)k_boxes, (int32_t)q_boxes, (int32_t)share);
+    return cudaLaunchKernelEx(&cfg, k, j, km, qm, (int32_t)k_boxes, (int32_t)q_boxes, (int32_t)share, (int32_t)(x * share));
 }
 
-template <bool HALF, int DP>
+template <bool HALF, int DP, bool HELD>
 cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     const StepView& st = j.step;
     const int64_t rows = (int64_t)st.max_q * st.group;
@@ -591,26 +651,30 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     if (rows <= 32) {
         // CTAs for two rounds of two to an SM (weigh of a decode step: one round 45.2 us, two 40.5,
         // three 41.1, six 45.1), but not more than leave a warp four tiles.
-        const int64_t pairs = (int64_t)st.kv_heads * st.requests, most = (st.max_kv + kRowWarps * kRowKeys * 4 - 1) / (kRowWarps * kRowKeys * 4);
+        const int64_t tokens = HELD ? places_of(j, 1) : st.max_kv;
+        const int64_t pairs = (int64_t)st.kv_heads * st.requests, most = (tokens + kRowWarps * kRowKeys * 4 - 1) / (kRowWarps * kRowKeys * 4);
         int64_t x = (4 * sms + pairs - 1) / pairs;
         x = x > most ? most : x;
         const dim3 grid((unsigned)x, st.kv_heads, st.requests);
-        if (rows <= 8) kvs_weigh_rows_kernel<HALF, DP, 1><<<grid, kRowWarps * 32, 0, s>>>(j);
-        else if (rows <= 16) kvs_weigh_rows_kernel<HALF, DP, 2><<<grid, kRowWarps * 32, 0, s>>>(j);
-        else kvs_weigh_rows_kernel<HALF, DP, 0><<<grid, kRowWarps * 32, 0, s>>>(j);
+        if (rows <= 8) kvs_weigh_rows_kernel<HALF, DP, 1, HELD><<<grid, kRowWarps * 32, 0, s>>>(j);
+        else if (rows <= 16) kvs_weigh_rows_kernel<HALF, DP, 2, HELD><<<grid, kRowWarps * 32, 0, s>>>(j);
+        else kvs_weigh_rows_kernel<HALF, DP, 0, HELD><<<grid, kRowWarps * 32, 0, s>>>(j);
         return cudaGetLastError();
     }
     // One key tile to a CTA up to 2560 rows: against 8000 tokens of 8 requests x 8 heads of 128 dims 64 rows
     // take 72 us (two tiles: 92), 256 79 (99), 1024 149 (167), 2048 250 (261), 4096 467 (450).
-    return rows <= 2560 ? weigh_tc<HALF, DP, 1>(j, sms, s) : weigh_tc<HALF, DP, 2>(j, sms, s);
+    return rows <= 2560 ? weigh_tc<HALF, DP, 1, HELD>(j, sms, s) : weigh_tc<HALF, DP, 2, HELD>(j, sms, s);
 }
+
+template <bool HALF, bool HELD>
+cudaError_t weigh_dims(const WeighJob& j, int sms, cudaStream_t s) { return j.step.head_dim <= 64 ? weigh<HALF, 64, HELD>(j, sms, s) : weigh<HALF, 128, HELD>(j, sms, s); }
+template <bool HALF>
+cudaError_t weigh_dims(const WeighJob& j, int sms, cudaStream_t s) { return j.held ? weigh_dims<HALF, true>(j, sms, s) : weigh_dims<HALF, false>(j, sms, s); }
 
 }  // namespace
 
 int launch_weigh(const WeighJob& j, bool half, int sms, cudaStream_t s) {
-    cudaError_t e;
-    if (j.step.head_dim <= 64) e = half ? weigh<true, 64>(j, sms, s) : weigh<false, 64>(j, sms, s);
-    else e = half ? weigh<true, 128>(j, sms, s) : weigh<false, 128>(j, sms, s);
+    const cudaError_t e = half ? weigh_dims<true>(j, sms, s) : weigh_dims<false>(j, sms, s);
     return e == cudaSuccess ? 1 : -(int)e;
 }
 

@@ -49,6 +49,10 @@ KVS_F_LAYER_SIGNAL = 1 << 7
 KVS_F_FORCE_DMA = 1 << 8
 KVS_F_PREFETCH_L2 = 1 << 9
 KVS_F_FEW_SMS = 1 << 10
+KVS_MAX_AXES = 4
+KVS_AXES_BLOCKS = 0
+KVS_AXES_CYCLE = 1
+KVS_AXES_RESTART = 2
 KVS_DIR_RETRIEVE = 0
 KVS_DIR_STORE = 1
 
@@ -75,7 +79,8 @@ EXPORTED = ("kvs_retrieve", "kvs_store", "kvs_query_bw", "kvs_get_choice", "kvs_
             "kvs_tier_create", "kvs_tier_destroy", "kvs_tier_commit", "kvs_tier_staged",
             "kvs_tier_begin_retrieval", "kvs_tier_end_retrieval", "kvs_tier_cancel", "kvs_tier_ordinary",
             "kvs_tier_claim_state", "kvs_tier_object", "kvs_tier_stats_get", "kvs_tier_slot",
-            "kvs_rope_turns", "kvs_append", "kvs_attend", "kvs_attend_workspace", "kvs_weigh", "kvs_evict")
+            "kvs_rope_turns", "kvs_append", "kvs_attend", "kvs_attend_workspace", "kvs_weigh", "kvs_evict",
+            "kvs_rope_axes", "kvs_append_axes", "kvs_attend_sinks", "kvs_attend_sinks_workspace", "kvs_weigh_sinks")
 KVS_CLAIM_NONE, KVS_CLAIM_PLANNED, KVS_CLAIM_STAGING, KVS_CLAIM_STAGE_READY = 0, 1, 2, 3
 KVS_CLAIM_TRANSFERRING, KVS_CLAIM_RELEASED, KVS_CLAIM_CANCELLED, KVS_CLAIM_ORDINARY = 4, 5, 6, 7
 CLAIM_NAMES = {0: "None", 1: "Planned", 2: "Staging", 3: "StageReady", 4: "Transferring",
@@ -175,6 +180,10 @@ class kvs_rope_spec(ctypes.Structure):
     _fields_ = [("rot_dim", ctypes.c_int32), ("kind", ctypes.c_int32), ("base", ctypes.c_double),
                 ("factor", ctypes.c_double), ("context", ctypes.c_double), ("low", ctypes.c_double),
                 ("high", ctypes.c_double)]
+
+
+class kvs_axes(ctypes.Structure):
+    _fields_ = [("axis", ctypes.c_void_p), ("stride", ctypes.c_int64), ("num_axes", ctypes.c_int32), ("pairs", ctypes.c_int32)]
 
 
 class kvs_append_args(ctypes.Structure):
@@ -279,6 +288,14 @@ def lib():
                 fn.restype = ctypes.c_int
             L.kvs_evict.argtypes = [P, P, P, P, P, ctypes.c_uint32]
             L.kvs_evict.restype = ctypes.c_int
+            for name, more in (("kvs_append_axes", P), ("kvs_attend_sinks", ctypes.c_int32), ("kvs_weigh_sinks", ctypes.c_int32)):
+                fn = getattr(L, name)
+                fn.argtypes = [P, P, P, ctypes.c_int32, P, more, P, ctypes.c_uint32]
+                fn.restype = ctypes.c_int
+            L.kvs_attend_sinks_workspace.argtypes = [P, P] + [ctypes.c_int32] * 4
+            L.kvs_attend_sinks_workspace.restype = ctypes.c_int64
+            L.kvs_rope_axes.argtypes = [P, I32P, ctypes.c_int32, ctypes.c_int32, P, P, ctypes.POINTER(ctypes.c_float)]
+            L.kvs_rope_axes.restype = ctypes.c_int
             L.kvs_attend_workspace.argtypes = [P, P, ctypes.c_int32]
             L.kvs_attend_workspace.restype = ctypes.c_int64
             L.kvs_rope_turns.argtypes = [P, P, ctypes.POINTER(ctypes.c_float)]
@@ -303,7 +320,7 @@ def lib():
             L.kvs_selftest_wait_timeout.restype = ctypes.c_int
             for name in ("kvs_retrieve", "kvs_store", "kvs_retrieve_noalloc", "kvs_retrieve_fp8", "kvs_store_fp8",
                          "kvs_retrieve_layers", "kvs_store_layers", "kvs_retrieve_fp8_layers", "kvs_store_fp8_layers",
-                         "kvs_append", "kvs_attend", "kvs_weigh", "kvs_evict"):
+                         "kvs_append", "kvs_attend", "kvs_weigh", "kvs_evict", "kvs_append_axes", "kvs_attend_sinks", "kvs_weigh_sinks"):
                 _address[name] = ctypes.cast(getattr(L, name), P).value
             _pycall = _build.load_pycall()
             _ops = getattr(_pycall, "__self__", None)
@@ -705,6 +722,17 @@ def kvs_append(step: Step, layer: int, q, k, v, q_out=None, rope: Rope | None = 
         rc = _ops.append(_address["kvs_append"], *step.ext, layer, stream, flags, q, k, v, q_out, rope, positions)
         if rc is not None:
             return _check(rc)
+    a = _append_args(step, q, k, v, q_out, rope)
+    if positions is not None:
+        _int32_tensor("positions", positions, 1)
+        if positions.shape[0] != step.total_q:
+            raise ValueError("positions has one entry per row")
+        a.positions = positions.data_ptr()
+    g, c, s = step.refs
+    return _check(lib().kvs_append(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+
+
+def _append_args(step, q, k, v, q_out, rope) -> kvs_append_args:
     a = kvs_append_args()
     if q is not None:
         a.q = _rows("q", step, q, 0)
@@ -712,15 +740,58 @@ def kvs_append(step: Step, layer: int, q, k, v, q_out=None, rope: Rope | None = 
         a.q_out = a.q if q_out is None else _rows("q_out", step, q_out, q.shape[1])
     H = step.geom.num_kv_heads
     a.k, a.v = _rows("k", step, k, H), _rows("v", step, v, H)
-    if positions is not None:
-        _int32_tensor("positions", positions, 1)
-        if positions.shape[0] != step.total_q:
-            raise ValueError("positions has one entry per row")
-        a.positions = positions.data_ptr()
     if rope is not None:
         a.rope = rope.ref
+    return a
+
+
+@dataclass
+class Axes:
+    """Which axis each rotated pair turns by: ``axis`` uint8 [rot_dim / 2] on the GPU (see
+    :func:`kvs_rope_axes`), with entries below ``num_axes``."""
+    axis: object
+    num_axes: int
+
+    def __post_init__(self):
+        import torch
+        if self.axis.dtype != torch.uint8 or self.axis.dim() != 1 or not self.axis.is_contiguous():
+            raise ValueError("axis: a contiguous uint8 tensor of 1 dimension is needed")
+        self.struct = kvs_axes(self.axis.data_ptr(), 0, int(self.num_axes), self.axis.shape[0])
+        self.ref = ctypes.addressof(self.struct)
+
+
+def kvs_rope_axes(parts: Sequence[int], base: float = 10000.0, kind: int = KVS_ROPE_PLAIN, factor: float = 1.0, context: float = 0.0,
+                  low: float = 0.0, high: float = 0.0, cycle: bool = False, restart: bool = False):
+    """(turns, axis, scale) of ``parts[a]`` rotated pairs on each axis: the float32 [pairs, 2] table of
+    :class:`Rope` and the uint8 [pairs] table of :class:`Axes` as numpy arrays, and the factor that goes
+    with them.  Pairs belong to the axes in blocks or (``cycle``) in turn; with ``restart`` each axis has
+    the whole range of frequencies."""
+    parts = [int(x) for x in parts]
+    pairs = sum(parts)
+    spec = kvs_rope_spec(2 * pairs, int(kind), float(base), float(factor), float(context), float(low), float(high))
+    turns, axis, scale = np.zeros((max(1, pairs), 2), dtype=np.float32), np.zeros(max(1, pairs), dtype=np.uint8), ctypes.c_float(0.0)
+    order = (KVS_AXES_CYCLE if cycle else KVS_AXES_BLOCKS) | (KVS_AXES_RESTART if restart else 0)
+    _check(lib().kvs_rope_axes(ctypes.byref(spec), (ctypes.c_int32 * max(1, len(parts)))(*parts), len(parts), order, turns.ctypes.data,
+                               axis.ctypes.data, ctypes.byref(scale)))
+    return turns, axis, float(scale.value)
+
+
+def kvs_append_axes(step: Step, layer: int, q, k, v, q_out, rope: Rope, axes: Axes, positions, stream=None, flags: int = 0) -> int:
+    """:func:`kvs_append` with positions on several axes: pair j turns by ``positions[axes.axis[j]]``,
+    ``positions`` int32 [axes.num_axes, total_q] on the GPU.  ``q_out`` may be None (in place), and ``q``
+    too."""
+    if _ops is not None:
+        rc = _ops.append_axes(_address["kvs_append_axes"], *step.ext, layer, stream, flags, q, k, v, q_out, rope, axes, positions)
+        if rc is not None:
+            return _check(rc)
+    a = _append_args(step, q, k, v, q_out, rope)
+    _int32_tensor("positions", positions, 2)
+    if tuple(positions.shape) != (axes.num_axes, step.total_q) or (step.total_q > 1 and positions.stride(1) != 1):
+        raise ValueError(f"positions: [{axes.num_axes}, {step.total_q}], contiguous in its last dimension")
+    a.positions = positions.data_ptr()
+    x = kvs_axes(axes.struct.axis, positions.stride(0), axes.struct.num_axes, axes.struct.pairs)
     g, c, s = step.refs
-    return _check(lib().kvs_append(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+    return _check(lib().kvs_append_axes(g, c, s, layer, ctypes.byref(a), ctypes.byref(x), _stream(stream), flags))
 
 
 def kvs_attend_workspace(step: Step, num_q_heads: int) -> int:
@@ -744,6 +815,12 @@ def kvs_attend(step: Step, layer: int, q, out, lse=None, scale: float | None = N
         rc = _ops.attend(_address["kvs_attend"], *step.ext, layer, stream, flags, q, out, lse, scale, causal, window, workspace, step.byte)
         if rc is not None:
             return _check(rc)
+    a = _attend_args(step, q, out, lse, scale, causal, window, workspace)
+    g, c, s = step.refs
+    return _check(lib().kvs_attend(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+
+
+def _attend_args(step, q, out, lse, scale, causal, window, workspace) -> kvs_attend_args:
     a = kvs_attend_args()
     a.q = _rows("q", step, q, 0)
     a.out = _rows("out", step, out, q.shape[1])
@@ -755,8 +832,33 @@ def kvs_attend(step: Step, layer: int, q, out, lse=None, scale: float | None = N
             raise ValueError("workspace: must be contiguous")
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     a.scale, a.causal, a.window = scale, bool(causal), window
+    return a
+
+
+def kvs_attend_sinks_workspace(step: Step, num_q_heads: int, causal: bool = True, window: int = 0, sinks: int = 0) -> int:
+    """Bytes of workspace that :func:`kvs_attend_sinks` needs for this step and mask."""
+    g, _, s = step.refs
+    n = int(lib().kvs_attend_sinks_workspace(g, s, int(num_q_heads), bool(causal), int(window), int(sinks)))
+    if n < 0:
+        _check(n)
+    return n
+
+
+def kvs_attend_sinks(step: Step, layer: int, q, out, lse=None, scale: float | None = None, causal: bool = True, window: int = 0,
+                     sinks: int = 0, workspace=None, stream=None, flags: int = 0) -> int:
+    """:func:`kvs_attend` of a ``window`` beside which each request's first ``sinks`` tokens stay visible.
+    Blocks of the cache that neither reaches may have been given back; ``workspace``: a uint8 tensor of
+    :func:`kvs_attend_sinks_workspace` bytes (may be None if that is 0)."""
+    if scale is None:
+        scale = step.scale
+    if _ops is not None:
+        rc = _ops.attend_sinks(_address["kvs_attend_sinks"], *step.ext, layer, stream, flags, q, out, lse, scale, causal, window, sinks, workspace,
+                               step.byte)
+        if rc is not None:
+            return _check(rc)
+    a = _attend_args(step, q, out, lse, scale, causal, window, workspace)
     g, c, s = step.refs
-    return _check(lib().kvs_attend(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+    return _check(lib().kvs_attend_sinks(g, c, s, layer, ctypes.byref(a), sinks, _stream(stream), flags))
 
 
 def kvs_weigh(step: Step, layer: int, q, lse, weights, scale: float | None = None, decay: float = 1.0, causal: bool = True,
@@ -770,6 +872,12 @@ def kvs_weigh(step: Step, layer: int, q, lse, weights, scale: float | None = Non
         rc = _ops.weigh(_address["kvs_weigh"], *step.ext, layer, stream, flags, q, lse, weights, scale, decay, causal, window)
         if rc is not None:
             return _check(rc)
+    a = _weigh_args(step, q, lse, weights, scale, decay, causal, window)
+    g, c, s = step.refs
+    return _check(lib().kvs_weigh(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+
+
+def _weigh_args(step, q, lse, weights, scale, decay, causal, window) -> kvs_weigh_args:
     a = kvs_weigh_args()
     a.q = _rows("q", step, q, 0)
     a.num_q_heads = q.shape[1]
@@ -780,8 +888,22 @@ def kvs_weigh(step: Step, layer: int, q, lse, weights, scale: float | None = Non
     a.weights = _f32("weights", weights, (R, H, weights.shape[2]), contiguous=False)
     a.request_stride, a.head_stride = weights.stride(0), weights.stride(1)
     a.scale, a.decay, a.causal, a.window = scale, decay, bool(causal), window
+    return a
+
+
+def kvs_weigh_sinks(step: Step, layer: int, q, lse, weights, scale: float | None = None, decay: float = 1.0, causal: bool = True,
+                    window: int = 0, sinks: int = 0, stream=None, flags: int = 0) -> int:
+    """:func:`kvs_weigh` under the mask of :func:`kvs_attend_sinks`, from the ``lse`` that it returned;
+    weights of tokens that nobody sees are multiplied by ``decay`` too."""
+    if scale is None:
+        scale = step.scale
+    if _ops is not None:
+        rc = _ops.weigh_sinks(_address["kvs_weigh_sinks"], *step.ext, layer, stream, flags, q, lse, weights, scale, decay, causal, window, sinks)
+        if rc is not None:
+            return _check(rc)
+    a = _weigh_args(step, q, lse, weights, scale, decay, causal, window)
     g, c, s = step.refs
-    return _check(lib().kvs_weigh(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+    return _check(lib().kvs_weigh_sinks(g, c, s, layer, ctypes.byref(a), sinks, _stream(stream), flags))
 
 
 def kvs_evict(step: Step, weights, dst_tables, budget: int, sinks: int, recent: int, kept, new_weights=None, new_lens=None,
