@@ -97,12 +97,13 @@ struct WPlan {
     static constexpr int bytes = bars + 512 + 1024;
 };
 
-// HELD: a window with sinks.  Key tiles are of its places then, and clusters behind their `places`
-// ones let the tokens fade that have none.
+// HELD: a window with sinks.  Key tiles are of its places then, and CTAs behind `key_tiles_all` of them
+// let the tokens fade that have none.  The grid goes by key tiles first: the sinks, which far more rows
+// see than other keys, start in all heads before anything else.
 template <bool HALF, int DP, int KT, bool HELD>
 __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap k_map,
                                                                    const __grid_constant__ CUtensorMap q_map, int32_t k_boxes, int32_t q_boxes, int32_t share,
-                                                                   int32_t places) {
+                                                                   int32_t key_tiles_all) {
     extern __shared__ char raw[];
     using P = WPlan<DP, KT>;
     constexpr int kThreads = P::threads, kStages = P::stages, kAccs = P::accs, kKeysTc = P::keys, kIssuer = P::issuer;
@@ -113,15 +114,24 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
     const uint32_t b_k = ctl, b_full = ctl + 8, b_free = b_full + 8 * kStages, b_s = b_free + 8 * kStages, b_e = b_s + 8 * kAccs, b_done = b_e + 8 * kAccs,
                    b_load = b_done + 8, b_lse = b_load + 8, b_read = b_lse + 8 * kSlots, tmem_at = b_read + 8 * kSlots;
     const int warp = warp_number(), lane = threadIdx.x & 31, wg = warp >> 2;
-    const int32_t r = blockIdx.z, h = blockIdx.y, rank = blockIdx.x % share, t0 = (blockIdx.x / share) * kKeysTc;
+    int32_t r = blockIdx.z, h = blockIdx.y, tile = blockIdx.x / share;
+    const int32_t rank = blockIdx.x % share;
+    if (HELD) {
+        const int32_t pairs = st.kv_heads * st.requests, at = tile;
+        tile = at / pairs;
+        r = (at - tile * pairs) / st.kv_heads;
+        h = at - tile * pairs - r * st.kv_heads;
+    }
+    const int32_t t0 = tile * kKeysTc;
     const Request q = load_request(st, r);
     Held held{};
     int32_t T = q.T;                                             // places (without HELD: tokens) of the cache
     if (HELD) {
         held = held_of(seen_by(q, 0, max(q.n, 1) - 1, j.causal, j.window).lo, j.sinks, k_boxes ? min(st.block_size, 128) : 1);
         T -= held.shift;
-        if (blockIdx.x >= places) {
-            fade(j, r, h, held, blockIdx.x - places, gridDim.x - places);
+        if (tile >= key_tiles_all) {
+            const int32_t behind = gridDim.x / (share * st.kv_heads * st.requests) - key_tiles_all;
+            fade(j, r, h, held, (tile - key_tiles_all) * share + rank, behind * share);
             return;                                              // as all of its cluster does
         }
     }
@@ -508,10 +518,10 @@ __device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, con
 // whose fragments are loaded (from L1) for every 16 keys; 16 rows take 27 us with and 38 without
 // them staying (8 requests x 8 heads of 64 dims, 8000 tokens), with 128 dims 45 and 48 (where two
 // of them spill some 150 bytes, and what a call cannot do without is 19 us).
-// HELD: a window with sinks.  The tiles are of its places (of one token each), and a CTA lets its share
-// of the tokens fade that have none.
+// HELD: a window with sinks.  The tiles are of its places (of one token each), and CTAs behind the `parts`
+// of them let the tokens fade that have none.
 template <bool HALF, int DP, int STAY, bool HELD>
-__global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(WeighJob j) {
+__global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(WeighJob j, int32_t parts) {
     constexpr int K = DP / 32;                                   // 16-byte vectors of a lane and key
     const StepView& st = j.step;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, i = lane >> 2;
@@ -523,11 +533,14 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
     if (HELD) {
         held = held_of(seen_by(q, 0, max(q.n, 1) - 1, j.causal, j.window).lo, j.sinks, 1);
         T -= held.shift;
-        fade(j, r, h, held, blockIdx.x, gridDim.x);
+        if ((int32_t)blockIdx.x >= parts) {
+            fade(j, r, h, held, blockIdx.x - parts, gridDim.x - parts);
+            return;
+        }
     }
     // this CTA's tiles of 16 keys, of which its warps take every eighth
     const int32_t all = (T + kRowKeys - 1) / kRowKeys;
-    const int32_t first = (int32_t)((int64_t)all * blockIdx.x / gridDim.x), end = (int32_t)((int64_t)all * (blockIdx.x + 1) / gridDim.x);
+    const int32_t first = (int32_t)((int64_t)all * blockIdx.x / parts), end = (int32_t)((int64_t)all * (blockIdx.x + 1) / parts);
     const int32_t mine = (end - first - warp + kRowWarps - 1) / kRowWarps;
     if (mine <= 0) return;
     auto key0 = [&](int32_t n) { return (first + warp + kRowWarps * n) * kRowKeys; };
@@ -606,14 +619,163 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
     }
 }
 
-// Places of a window with sinks, at most.
+// The same of a window with sinks for nine to 32 rows.  A lane's vectors wait in shared memory, where it
+// alone writes (cp.async) and reads them: the registers that hold keys in flight above hold more rows'
+// fragments, and STAGES - 1 tiles of a warp are in flight instead of one.  16 requests x 8 heads of 128 dims
+// with a window of 4096: 16 rows 37 us, with keys in registers 44 (8 rows 32.4 and 32.1); eight requests, 30 rows
+// 28 and 31.
+template <int DP, int STAGES>
+struct HeldPlan {
+    static constexpr int K = DP / 32;
+    static constexpr int stage = 32 * (2 * K * 16 + 4);          // [2 K][lane] vectors, [lane] weights
+    static constexpr int bytes = kRowWarps * STAGES * stage;
+};
+template <bool HALF, int DP, int STAY, int STAGES, int CTAS>
+__global__ void __launch_bounds__(kRowWarps * 32, CTAS) kvs_weigh_held_kernel(WeighJob j, int32_t parts) {
+    extern __shared__ __align__(16) char ring[];
+    using P = HeldPlan<DP, STAGES>;
+    constexpr int K = P::K;
+    const StepView& st = j.step;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, i = lane >> 2;
+    const int32_t h = blockIdx.y, r = blockIdx.z;
+    const Request q = load_request(st, r);
+    const Held held = held_of(seen_by(q, 0, max(q.n, 1) - 1, j.causal, j.window).lo, j.sinks, 1);
+    if ((int32_t)blockIdx.x >= parts) {
+        fade(j, r, h, held, blockIdx.x - parts, gridDim.x - parts);
+        return;
+    }
+    const int32_t* table = st.tables + (int64_t)r * st.table_stride;
+    const int32_t T = q.T - held.shift, all = (T + kRowKeys - 1) / kRowKeys;
+    const int32_t first = (int32_t)((int64_t)all * blockIdx.x / parts), end = (int32_t)((int64_t)all * (blockIdx.x + 1) / parts);
+    const int32_t mine = (end - first - warp + kRowWarps - 1) / kRowWarps;
+    if (mine <= 0) return;
+    auto key0 = [&](int32_t n) { return (first + warp + kRowWarps * n) * kRowKeys; };
+    auto look_up = [&](int32_t n, int64_t (&row)[2]) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int32_t u = key0(n) + i + 8 * e;
+            row[e] = n < mine && u < T ? row_of(st, table, token_at(held, u)) : -1;
+        }
+    };
+    float* weights = j.weights + r * j.request_stride + h * j.head_stride;
+    const uint32_t own = smem_u32(ring) + warp * STAGES * P::stage;
+    auto load = [&](int32_t n, const int64_t (&row)[2]) {
+        const uint32_t at = own + (n % STAGES) * P::stage;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int32_t d = 32 * k + 8 * c;
+                const bool there = row[e] >= 0 && d < st.head_dim;
+                cp_async16(at + ((e * K + k) * 32 + lane) * 16, j.k_plane + (there ? 2 * (row[e] + (int64_t)h * st.head_dim + d) : 0), there);
+            }
+        const int32_t u = key0(n) + i + 8 * c;
+        const bool there = j.decay != 0.0f && n < mine && c < 2 && u < T;
+        cp_async4(at + 2 * K * 512 + 4 * lane, weights + (there ? token_at(held, u) : 0), there);
+        cp_commit();
+    };
+    int64_t row[2];
+#pragma unroll
+    for (int n = 0; n < STAGES - 1; ++n) {
+        look_up(n, row);
+        load(n, row);
+    }
+    look_up(STAGES - 1, row);
+    RowFrags<K> stay[STAY];
+#pragma unroll
+    for (int x = 0; x < STAY; ++x) load_rows<K, true>(stay[x], j, q, held, h, 8 * x, lane);
+    for (int32_t n = 0; n < mine; ++n) {
+        cp_wait<STAGES - 2>();
+        const uint32_t at = own + (n % STAGES) * P::stage;
+        uint4 kv[2][K];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int k = 0; k < K; ++k) kv[e][k] = ld_shared16(at + ((e * K + k) * 32 + lane) * 16);
+        const float old = *reinterpret_cast<const float*>(ring + warp * STAGES * P::stage + (n % STAGES) * P::stage + 2 * K * 512 + 4 * lane);
+        load(n + STAGES - 1, row);                               // where the tile before lay, which this lane has read
+        look_up(n + STAGES, row);
+        const int32_t u = key0(n) + i;
+        float sum[2] = {0.0f, 0.0f};                             // keys u and u + 8, of this lane's rows
+        auto add = [&](const RowFrags<K>& f) {
+            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                mma<HALF>(s, kv[0][k].x, kv[1][k].x, kv[0][k].y, kv[1][k].y, f.q[k].x, f.q[k].y);
+                mma<HALF>(t, kv[0][k].z, kv[1][k].z, kv[0][k].w, kv[1][k].w, f.q[k].z, f.q[k].w);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int32_t key = u + 8 * (e >> 1);
+                if ((key >= f.see[e & 1].lo || key < j.sinks) && key < f.see[e & 1].hi) sum[e >> 1] += exp2_fast(fmaf(s[e] + t[e], j.scale_log2, f.lse[e & 1]));
+            }
+        };
+#pragma unroll
+        for (int x = 0; x < STAY; ++x) add(stay[x]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 1);
+            sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 2);
+        }
+        if (c < 2 && u + 8 * c < T) weights[token_at(held, u + 8 * c)] = j.decay * old + (c ? sum[1] : sum[0]);
+    }
+    cp_wait<0>();
+}
+
+// Places of a window with sinks, at most, in units of so many tokens.
 int64_t places_of(const WeighJob& j, int64_t unit) {
-    const int64_t most = (int64_t)j.sinks + j.window + j.step.max_q + 2 * unit;
+    const int64_t most = (int64_t)j.sinks + j.window + (j.step.max_q > 0 ? j.step.max_q - 1 : 0) + 2 * (unit - 1);
     return most < j.step.max_kv ? most : j.step.max_kv;
+}
+// The most tokens that a box of a key tile holds.
+int64_t box_tokens(const StepView& st) { return 128 % st.block_size == 0 ? st.block_size : st.block_size % 128 == 0 ? 128 : 1; }
+
+// CTAs that let tokens fade: one for 16384 of a head.
+int64_t fading_of(const WeighJob& j) { return j.decay == 1.0f ? 0 : (j.step.max_kv + 16383) / 16384; }
+
+// How the tensor cores' kernel goes about a window with sinks: key tiles of a CTA, and the CTAs that
+// share a key tile's rows.  Only rows within the window see a key tile, so that a CTA has few row
+// tiles and its start counts; the sinks' CTAs, which have all rows, are the longest.  Measured, in units of
+// 0.65 us: a row tile takes a key tile 1.3 where a CTA has an SM to itself, and 1 of the SM's time
+// where two share it or a CTA has two key tiles; the start and end of a CTA take 10, which the other
+// one's work covers.  8 KV heads of 128 dims, 5 query heads each: 1024 new tokens and a window as long, one key
+// tile to a CTA, 45 us with one CTA to it, 34 with two, 27 with four and 41 with eight (two key tiles: 67, 38,
+// 32, 57); 2048 and a window of 128 85, 48, 30, 42; 4 x 1500 and 600 72, 75, 102, 157; 8 x 100 and 1024 21, 33, 57, 119.
+struct HeldWeighPlan {
+    int key_tiles, share;
+};
+HeldWeighPlan held_weigh_plan(const WeighJob& j, int sms) {
+    const StepView& st = j.step;
+    const int64_t per = tile_rows_of(st.group), pairs = (int64_t)st.kv_heads * st.requests;
+    auto tiles_of = [&](int64_t tokens) { return ((tokens < st.max_q ? tokens : st.max_q) * st.group + per - 1) / per; };
+    HeldWeighPlan best{1, 1};
+    double least = -1.0;
+    for (int kt = 1; kt <= 2; ++kt) {
+        const int64_t keys = 128 * kt, tiles = (places_of(j, box_tokens(st)) + keys - 1) / keys * pairs;
+        const int64_t most = tiles_of(st.max_q), usual = tiles_of(j.window + keys);
+        for (int share = 1; share <= 8 && share <= most; share *= 2) {
+            const double ctas = (double)(tiles * share), n = (double)((usual + share - 1) / share), l = (double)((most + share - 1) / share);
+            double all, longest;
+            if (kt == 2) {
+                all = (2 * n + 10) * (ctas > sms ? ctas / sms : 1);
+                longest = 2 * l + 10;
+            } else {
+                const double alone = 1.3 * n + 10, last = 1.3 * l + 10;
+                all = ctas <= sms ? alone : ctas <= 2 * sms ? (alone > 2 * n ? alone : 2 * n) : ctas / sms * (n > alone / 2 ? n : alone / 2);
+                longest = ctas <= sms || last > 2 * l ? last : 2 * l;
+            }
+            const double cost = longest > all ? longest : all;
+            if (least < 0 || cost < least) {
+                least = cost;
+                best = HeldWeighPlan{kt, share};
+            }
+        }
+    }
+    return best;
 }
 
 template <bool HALF, int DP, int KT, bool HELD>
-cudaError_t weigh_tc(const WeighJob& j, int sms, cudaStream_t s) {
+cudaError_t weigh_tc(const WeighJob& j, int sms, int held_share, cudaStream_t s) {
     using P = WPlan<DP, KT>;
     const StepView& st = j.step;
     const int64_t rows = (int64_t)st.max_q * st.group;
@@ -622,14 +784,19 @@ cudaError_t weigh_tc(const WeighJob& j, int sms, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     CUtensorMap km{}, qm{};
     const bool k_boxes = plane_map(&km, st, j.k_plane, HALF), q_boxes = rows_map(&qm, st, j.q, HALF);
-    const int64_t tokens = HELD ? places_of(j, 128) : st.max_kv;
+    const int64_t tokens = HELD ? places_of(j, box_tokens(st)) : st.max_kv;
     const int64_t x = (tokens + P::keys - 1) / P::keys, tiles = x * st.kv_heads * st.requests, row_tiles = (rows + 127) / 128;
     int share = 1;
-    while (share < 8 && tiles * share * 2 <= sms && share * 2 <= row_tiles) share *= 2;
-    // a CTA for every 16384 tokens that fade
-    const int64_t fading = HELD && j.decay != 1.0f ? (st.max_kv + 16383) / 16384 : 0;
+    if (HELD) share = held_share;
+    else while (share < 8 && tiles * share * 2 <= sms && share * 2 <= row_tiles) share *= 2;
+    const int64_t fading = HELD ? fading_of(j) : 0;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((x + (fading + share - 1) / share) * share), st.kv_heads, st.requests);
+    cfg.gridDim = dim3((unsigned)(x * share), st.kv_heads, st.requests);
+    if (HELD) {
+        const int64_t ctas = (x + (fading + share - 1) / share) * share * st.kv_heads * st.requests;
+        if (ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
+        cfg.gridDim = dim3((unsigned)ctas);
+    }
     cfg.blockDim = dim3(P::threads);
     cfg.dynamicSmemBytes = P::bytes;
     cfg.stream = s;
@@ -639,7 +806,17 @@ cudaError_t weigh_tc(const WeighJob& j, int sms, cudaStream_t s) {
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = share > 1;
-    return cudaLaunchKernelEx(&cfg, k, j, km, qm, (int32_t)k_boxes, (int32_t)q_boxes, (int32_t)share, (int32_t)(x * share));
+    return cudaLaunchKernelEx(&cfg, k, j, km, qm, (int32_t)k_boxes, (int32_t)q_boxes, (int32_t)share, (int32_t)x);
+}
+
+template <bool HALF, int DP, int STAY, int STAGES, int CTAS>
+cudaError_t weigh_held(const WeighJob& j, dim3 grid, int64_t parts, cudaStream_t s) {
+    auto* k = kvs_weigh_held_kernel<HALF, DP, STAY, STAGES, CTAS>;
+    constexpr int bytes = HeldPlan<DP, STAGES>::bytes;
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    k<<<grid, kRowWarps * 32, bytes, s>>>(j, (int32_t)parts);
+    return cudaGetLastError();
 }
 
 template <bool HALF, int DP, bool HELD>
@@ -654,16 +831,27 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
         const int64_t tokens = HELD ? places_of(j, 1) : st.max_kv;
         const int64_t pairs = (int64_t)st.kv_heads * st.requests, most = (tokens + kRowWarps * kRowKeys * 4 - 1) / (kRowWarps * kRowKeys * 4);
         int64_t x = (4 * sms + pairs - 1) / pairs;
+        // with the fragments of 32 rows a CTA has an SM to itself, and its start is long: one round
+        if (HELD && rows > 16) x = pairs < sms ? sms / pairs : 1;
         x = x > most ? most : x;
-        const dim3 grid((unsigned)x, st.kv_heads, st.requests);
-        if (rows <= 8) kvs_weigh_rows_kernel<HALF, DP, 1, HELD><<<grid, kRowWarps * 32, 0, s>>>(j);
-        else if (rows <= 16) kvs_weigh_rows_kernel<HALF, DP, 2, HELD><<<grid, kRowWarps * 32, 0, s>>>(j);
-        else kvs_weigh_rows_kernel<HALF, DP, 0, HELD><<<grid, kRowWarps * 32, 0, s>>>(j);
+        const dim3 grid((unsigned)(x + (HELD ? fading_of(j) : 0)), st.kv_heads, st.requests);
+        if (rows <= 8) {
+            kvs_weigh_rows_kernel<HALF, DP, 1, HELD><<<grid, kRowWarps * 32, 0, s>>>(j, (int32_t)x);
+        } else if constexpr (HELD) {
+            return rows <= 16 ? weigh_held<HALF, DP, 2, 3, 2>(j, grid, x, s) : weigh_held<HALF, DP, 4, 5, 1>(j, grid, x, s);
+        } else {
+            if (rows <= 16) kvs_weigh_rows_kernel<HALF, DP, 2, HELD><<<grid, kRowWarps * 32, 0, s>>>(j, (int32_t)x);
+            else kvs_weigh_rows_kernel<HALF, DP, 0, HELD><<<grid, kRowWarps * 32, 0, s>>>(j, (int32_t)x);
+        }
         return cudaGetLastError();
+    }
+    if (HELD) {
+        const HeldWeighPlan plan = held_weigh_plan(j, sms);
+        return plan.key_tiles == 1 ? weigh_tc<HALF, DP, 1, HELD>(j, sms, plan.share, s) : weigh_tc<HALF, DP, 2, HELD>(j, sms, plan.share, s);
     }
     // One key tile to a CTA up to 2560 rows: against 8000 tokens of 8 requests x 8 heads of 128 dims 64 rows
     // take 72 us (two tiles: 92), 256 79 (99), 1024 149 (167), 2048 250 (261), 4096 467 (450).
-    return rows <= 2560 ? weigh_tc<HALF, DP, 1, HELD>(j, sms, s) : weigh_tc<HALF, DP, 2, HELD>(j, sms, s);
+    return rows <= 2560 ? weigh_tc<HALF, DP, 1, HELD>(j, sms, 1, s) : weigh_tc<HALF, DP, 2, HELD>(j, sms, 1, s);
 }
 
 template <bool HALF, bool HELD>
