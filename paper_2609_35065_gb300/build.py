@@ -24,7 +24,7 @@ INCLUDE = os.path.join(ROOT, "include")
 OUT_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT_DIR, "libkvs.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("kvs_kernels.cu", "kvs_api.cpp", "kvs_noalloc.cu", "kvs_fp8.cu",
-                                           "kvs_tier.cpp", "kvs_ops_api.cpp", "kvs_append.cu", "kvs_append_axes.cu", "kvs_attend.cu", "kvs_attend_tc.cu",
+                                           "kvs_tier.cpp", "kvs_ops_api.cpp", "kvs_append.cu", "kvs_append_axes.cu", "kvs_attend.cu", "kvs_attend_tc.cu", "kvs_attend_held.cu",
                                            "kvs_weigh.cu", "kvs_evict.cu")]
 DEPS = SOURCES + [os.path.join(CSRC, "kvs_internal.h"), os.path.join(CSRC, "kvs_async.cuh"),
                   os.path.join(CSRC, "kvs_job.cuh"),

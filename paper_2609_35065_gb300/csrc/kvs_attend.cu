@@ -490,7 +490,7 @@ AttendPlan attend_plan(const StepView& st, int sms) {
 }
 
 int launch_attend(const AttendJob& j, bool half, cudaStream_t s) {
-    cudaError_t e = j.tc ? launch_attend_tc(j, half, s) : half ? attend_few<true>(j, s) : attend_few<false>(j, s);
+    cudaError_t e = j.stay ? launch_attend_held(j, half, j.stay, s) : j.tc ? launch_attend_tc(j, half, s) : half ? attend_few<true>(j, s) : attend_few<false>(j, s);
     if (e != cudaSuccess) return -(int)e;
     if (j.splits == 1 || j.cluster) return 1;
     // The join is launched programmatically: its CTAs are in place when the parts are done.

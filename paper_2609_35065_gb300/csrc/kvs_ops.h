@@ -57,6 +57,7 @@ struct AttendJob {
     int32_t  cluster;                // 1: a head's parts are CTAs of a cluster, which joins them
     int32_t  tc;                     // 1: on the tensor cores' kernel
     int32_t  row_tiles;              // of a CTA there
+    int32_t  stay;                   // SMs that CTAs stay on, going over all pairs of row tiles; 0: a CTA to each
 };
 
 struct WeighJob {
@@ -108,6 +109,9 @@ bool plane_map(void* map, const StepView& st, const void* plane, bool half);
 // at most 128 packed rows.
 bool rows_map(void* map, const StepView& st, const RowsView& rows, bool half);
 cudaError_t launch_attend_tc(const AttendJob& j, bool half, cudaStream_t s);
+// Of a window with sinks, on CTAs that stay: pairs of row tiles that there may be at most, and the launch.
+int64_t held_items(const StepView& st);
+cudaError_t launch_attend_held(const AttendJob& j, bool half, int sms, cudaStream_t s);
 
 // The current device's error word and number of SMs (kvs_api.cpp); allocates them at the first call,
 // and takes no lock later.

@@ -221,6 +221,11 @@ AttendPlan held_plan(StepView v, int32_t held, int32_t causal, int32_t window, i
     return attend_plan(v, sms);
 }
 
+int64_t pairs_of_tiles(const StepView& v) {
+    const int64_t rows = 2 * tile_rows_of(v.group);
+    return ((int64_t)v.max_q * v.group + rows - 1) / rows * v.kv_heads * v.requests;
+}
+
 int64_t workspace_bytes(const StepView& v, const AttendPlan& plan) {
     const int n = plan.splits;
     return n <= 1 || plan.cluster ? 0 : (int64_t)n * v.total_q * v.kv_heads * v.group * (v.head_dim + 2) * 4;
@@ -251,6 +256,8 @@ int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     j.splits = plan.splits;
     j.cluster = plan.cluster;
     j.row_tiles = plan.row_tiles;
+    // more pairs of row tiles than SMs: CTAs that stay
+    j.stay = j.held && plan.tc && plan.splits == 1 && plan.row_tiles == 2 && pairs_of_tiles(j.step) > sms && pairs_of_tiles(j.step) <= INT32_MAX ? sms : 0;
     const int64_t need = workspace_bytes(j.step, plan);
     if (need > 0) {
         if (!a->workspace) return ops_fail(KVS_ERR_INVALID_ARG, "workspace is NULL, %lld bytes are needed", (long long)need);

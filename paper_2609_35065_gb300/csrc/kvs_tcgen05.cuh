@@ -186,6 +186,36 @@ __device__ __forceinline__ void tile_rows(uint32_t dst, const char* plane, const
     }
 }
 
+// A tile of V by boxes, and by rows with cp.async where a box holds places that no row sees: those become zeros.
+// A warp brings the boxes that are its own either way; its arrival on `bar` has to follow.
+template <int DP>
+__device__ __forceinline__ void tile_mixed(uint32_t dst, const CUtensorMap* map, const char* plane, const StepView& st, int32_t h, const Box& x, uint32_t bar,
+                                           int32_t t0, int32_t lo, int32_t hi, int32_t sinks, int lane) {
+    constexpr int HALVES = DP / 64, CH = DP / 8;
+    const int32_t size = min(st.block_size, 128), a = t0 + x.at, b = a + size;
+    const bool whole = (a >= lo || min(b, lo) <= sinks) && b <= hi;
+    const uint32_t boxed = __ballot_sync(0xffffffffu, x.block >= 0 && whole);
+    uint32_t split = __ballot_sync(0xffffffffu, x.at < 128 && !whole && lane % HALVES == 0);
+    if (lane == 0 && boxed) mbar_expect_more(bar, (uint32_t)__popc(boxed) * size * 128);
+    __syncwarp();
+    if (x.block >= 0 && whole) {
+        const int c = lane % HALVES;
+        tma_load_4d(dst + c * 128 * 128 + x.at * 128, map, 64 * c, h, x.row, x.block, bar);
+    }
+    while (split) {
+        const int from = __ffs(split) - 1;
+        split &= split - 1;
+        const int32_t at = __shfl_sync(0xffffffffu, x.at, from), block = __shfl_sync(0xffffffffu, x.block, from), row0 = __shfl_sync(0xffffffffu, x.row, from);
+        for (int v = lane; v < size * CH; v += 32) {
+            const int k = v / CH, c = v % CH;
+            const int32_t u = t0 + at + k;
+            const bool there = (uint32_t)block < (uint32_t)st.num_blocks && (u >= lo || u < sinks) && u < hi && 8 * c < st.head_dim;
+            const int64_t row = there ? (((int64_t)block * st.block_size + row0 + k) * st.kv_heads + h) * st.head_dim + 8 * c : 0;
+            cp_async16(dst + (c >> 3) * 128 * 128 + (at + k) * 128 + (((c & 7) ^ ((at + k) & 7)) << 4), plane + 2 * row, there);
+        }
+    }
+}
+
 // Barrier of `threads` threads under a number of its own (1 to 15).
 __device__ __forceinline__ void bar_some(int id, int threads) { asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory"); }
 

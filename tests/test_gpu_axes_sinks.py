@@ -111,6 +111,24 @@ def test_what_hides_nothing_is_plain_attention(new, lens):
         assert torch.equal(out, out2) and torch.equal(z, z2)
 
 
+# more pairs of row tiles than SMs: CTAs go from one to the next
+@pytest.mark.parametrize("new,lens,window,sinks,H,G,D,B,dtype,causal", [
+    ([1500, 3, 0, 700], [1500, 50, 9, 3000], 100, 4, 8, 4, 128, 16, "bf16", True), ([2100, 1999], [2100, 1999], 128, 4, 4, 8, 64, 16, "f16", True),
+    ([1400], [5000], 1024, 64, 8, 4, 128, 16, "bf16", True), ([700, 900], [900, 905], 33, 130, 8, 5, 96, 8, "bf16", True),
+    ([1400, 20], [1800, 700], 64, 3, 8, 4, 80, 1, "f16", True), ([1400], [1800], 200, 300, 8, 4, 128, 128, "bf16", True),
+    ([1400], [1800], 90, 5, 8, 4, 64, 256, "bf16", True), ([900], [500], 70, 4, 8, 7, 128, 32, "bf16", True), ([2600], [2600], 77, 4, 8, 2, 32, 16, "bf16", True),
+    ([200], [330], 50, 4, 2, 130, 64, 16, "bf16", True), ([1400], [1700], 40, 17, 8, 4, 128, 16, "f16", False), ([50] * 100, [400] * 100, 60, 4, 2, 4, 128, 16, "bf16", True),
+    ([1400], [1700], 1, 1, 8, 4, 64, 16, "bf16", True), ([700] * 3, [700, 1300, 350], 300, 0, 4, 8, 128, 3, "f16", True)])
+def test_many_row_tiles(new, lens, window, sinks, H, G, D, B, dtype, causal):
+    sm = Long(new, lens, window, sinks, H, G, D, B, dtype=dtype, causal=causal)
+    on = sm.on_gpu(kvs)
+    assert kvs.kvs_attend_sinks_workspace(on[0], H * G, causal, window, sinks) == 0
+    first = _attend(sm, on=on)
+    _check(sm, *first)
+    for a, b in zip(first, _attend(sm, on=on)):
+        assert torch.equal(a, b)
+
+
 def test_the_neighbours_of_a_request_do_not_matter():
     sm = Long([2, 150, 1], [700, 650, 350], 90, 6, 2, 4, 128)
     a, za = _attend(sm)
