@@ -55,7 +55,7 @@ struct Walk {
 template <bool HALF, int DP>
 __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(AttendJob j, const __grid_constant__ CUtensorMap k_map,
                                                                             const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap q_map,
-                                                                            int32_t boxes, int32_t q_boxes, uint32_t tiles, uint32_t total) {
+                                                                            int32_t boxes, int32_t q_boxes, FastDiv tiles, FastDiv heads_of, uint32_t total) {
     extern __shared__ __align__(1024) char raw[];
     using N = Num<HALF>;
     using P = Plan<DP>;
@@ -72,32 +72,34 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
     const int warp = warp_number(), wg = warp >> 2, lane = threadIdx.x & 31;
     const int32_t per = tile_rows_of(st.group);
 
-    auto pair_of = [&](uint32_t w, uint32_t& tile) {
-        const uint32_t p = w / tiles;
-        tile = w - p * tiles;
-        return p;
-    };
+    // the item's pair of request and KV head, and its pair of row tiles
     auto fetch = [&](Walk& k) {
-        uint32_t tile;
-        if (k.w < total) k.raw = fetch_request(st, pair_of(k.w, tile) / st.kv_heads);
+        if (k.w < total) k.raw = fetch_request(st, fdiv(fdiv(k.w, tiles), heads_of));
     };
     Walk walk{blockIdx.x, {}};
     fetch(walk);
+    const int32_t unit = boxes ? min(st.block_size, kN) : 1;
+    // floor and ceiling in units, of which there is one to a box: divided as block_of divides, or by 128
+    auto units = [&](int32_t t) { return unit == 1 ? t : unit == st.block_size ? (int32_t)block_of(st, t) : t >> 7; };
     auto next_item = [&](Item& it) {
         while (walk.w < total) {
-            uint32_t tile;
-            const uint32_t p = pair_of(walk.w, tile);
+            const uint32_t p = fdiv(walk.w, tiles), tile = walk.w - p * tiles.d;
             const RawRequest mine = walk.raw;
             walk.w += gridDim.x;
             fetch(walk);
-            it.r = p / st.kv_heads;
-            it.h = p - it.r * st.kv_heads;
+            it.r = fdiv(p, heads_of);
+            it.h = p - it.r * heads_of.d;
             it.row0 = (int32_t)tile * kTiles * per;
             it.q = check_request(st, mine);
             it.rows = min(kTiles * per, it.q.n * st.group - it.row0);
             if (it.rows <= 0) continue;
-            it.all = seen_by(it.q, it.row0 / st.group, (it.row0 + it.rows - 1) / st.group, j.causal, j.window);
-            it.held = held_of(it.all.lo, j.sinks, boxes ? min(st.block_size, kN) : 1);
+            int32_t g;
+            const int32_t tok = token_of(st, it.row0, g);
+            it.all = seen_by(it.q, tok, token_of(st, it.row0 + it.rows - 1, g), j.causal, j.window);
+            // as held_of
+            const int32_t first = units(it.all.lo) * unit;
+            it.held.cut = min(units(min(j.sinks, it.all.lo) + unit - 1) * unit, first);
+            it.held.shift = first - it.held.cut;
             it.all = in_places(it.held, it.all);
             it.T = it.q.T - it.held.shift;
             it.steps = it.all.hi > it.all.lo ? (it.all.hi + kN - 1) / kN : 0;
@@ -151,6 +153,9 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
         return false;
     };
 
+    // The softmax's warps get registers of the others' (512 x 104 + 128 x 64 = 640 x 96).
+    if (warp >= kIssuer) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
     if (warp > kIssuer) {
         // ---- K and V: the ring's tile i is K (even) or V (odd) of step i / 2 of all items' -----
         const int t = threadIdx.x - 32 * (kIssuer + 1), w = warp - kIssuer - 1;
@@ -394,10 +399,22 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                 auto below = [&](int32_t x) { return x - t0 <= 0 ? 0ull : x - t0 >= 64 ? ~0ull : (1ull << (x - t0)) - 1; };
                 const uint64_t seen = below(see.hi) & (~below(see.lo) | below(j.sinks));
                 const uint32_t bits[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
-                const bool edge = __any_sync(0xffffffffu, seen != ~0ull), none = !__any_sync(0xffffffffu, live && seen);
-                auto masked = [&](float* s, int b) {
+                // of either 32: whether some of the warp's rows do not see all of them, and whether some see any
+                bool edge[2], some[2];
 #pragma unroll
-                    for (int n = 0; n < 32; ++n) s[n] = bits[b] >> n & 1 ? s[n] : kNone;
+                for (int b = 0; b < 2; ++b) {
+                    edge[b] = __any_sync(0xffffffffu, bits[b] != ~0u);
+                    some[b] = __any_sync(0xffffffffu, live && bits[b]);
+                }
+                auto load_s = [&](uint32_t* sr, int b) {
+                    tmem_ld32(sr, s_own + 32 * b);
+                    tmem_wait_ld();
+                    tmem_loaded32(sr);
+                    float* s = reinterpret_cast<float*>(sr);
+                    if (edge[b]) {
+#pragma unroll
+                        for (int n = 0; n < 32; ++n) s[n] = bits[b] >> n & 1 ? s[n] : kNone;
+                    }
                 };
                 // Against this step's own maximum: the first step, and the first that rows see any key of.
                 bool exact = k == 0 || __any_sync(0xffffffffu, live && m == kNone && see.lo < (k + 1) * kN && see.hi > k * kN);
@@ -406,18 +423,14 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                 while (true) {
                     if (exact) {
                         float top = kNone;
-                        if (!none) {
 #pragma unroll
-                            for (int b = 0; b < 2; ++b) {
-                                uint32_t sr[32];
-                                tmem_ld32(sr, s_own + 32 * b);
-                                tmem_wait_ld();
-                                tmem_loaded32(sr);
-                                float* s = reinterpret_cast<float*>(sr);
-                                if (edge) masked(s, b);
+                        for (int b = 0; b < 2; ++b) {
+                            if (!some[b]) continue;
+                            uint32_t sr[32];
+                            load_s(sr, b);
+                            float* s = reinterpret_cast<float*>(sr);
 #pragma unroll
-                                for (int n = 0; n < 32; n += 2) top = max3(top, s[n], s[n + 1]);
-                            }
+                            for (int n = 0; n < 32; n += 2) top = max3(top, s[n], s[n + 1]);
                         }
                         tops[half * 128 * kTiles + tl * 128 + t] = top;
                         bar_some(pair, 64);
@@ -444,27 +457,24 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                     }
                     const float off = m == kNone ? 0.0f : top_at - m * c;
                     a0 = a1 = 0.0f;
-                    if (none) {
 #pragma unroll
-                        for (int n = 0; n < 32; ++n) pk[n] = 0;
-                    } else {
+                    for (int b = 0; b < 2; ++b) {
+                        if (!some[b]) {
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            uint32_t sr[32];
-                            tmem_ld32(sr, s_own + 32 * b);
-                            tmem_wait_ld();
-                            tmem_loaded32(sr);
-                            float* s = reinterpret_cast<float*>(sr);
-                            if (edge) masked(s, b);
+                            for (int n = 0; n < 16; ++n) pk[16 * b + n] = 0;
+                            continue;
+                        }
+                        uint32_t sr[32];
+                        load_s(sr, b);
+                        float* s = reinterpret_cast<float*>(sr);
 #pragma unroll
-                            for (int n = 0; n < 16; ++n) {
-                                float x = s[2 * n], y = s[2 * n + 1];
-                                fma2(x, y, c, off);
-                                x = exp2_fast(x);
-                                y = exp2_fast(y);
-                                add2(a0, a1, x, y);
-                                pk[16 * b + n] = N::pack(x, y);
-                            }
+                        for (int n = 0; n < 16; ++n) {
+                            float x = s[2 * n], y = s[2 * n + 1];
+                            fma2(x, y, c, off);
+                            x = exp2_fast(x);
+                            y = exp2_fast(y);
+                            add2(a0, a1, x, y);
+                            pk[16 * b + n] = N::pack(x, y);
                         }
                     }
                     // No weight is above its sum.  Both halves of S are read behind this: P goes over the
@@ -538,7 +548,8 @@ cudaError_t attend_held(const AttendJob& j, int sms, cudaStream_t s) {
     CUtensorMap km{}, vm{}, qm{};
     const bool boxes = plane_map(&km, j.step, j.k_plane, HALF) && plane_map(&vm, j.step, j.v_plane, HALF), q_boxes = rows_map(&qm, j.step, j.q, HALF);
     const int64_t total = held_items(j.step), tiles = total / ((int64_t)j.step.kv_heads * j.step.requests);
-    k<<<(unsigned)(total < sms ? total : sms), P::threads, P::bytes, s>>>(j, km, vm, qm, (int32_t)boxes, (int32_t)q_boxes, (uint32_t)tiles, (uint32_t)total);
+    k<<<(unsigned)(total < sms ? total : sms), P::threads, P::bytes, s>>>(j, km, vm, qm, (int32_t)boxes, (int32_t)q_boxes, make_fastdiv((uint32_t)tiles),
+                                                                             make_fastdiv((uint32_t)j.step.kv_heads), (uint32_t)total);
     return cudaGetLastError();
 }
 
