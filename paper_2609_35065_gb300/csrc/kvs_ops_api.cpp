@@ -210,15 +210,46 @@ int append_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     return done(launch_append(j, st->dtype == KVS_DTYPE_F16, s), s, flags);
 }
 
-// With sinks a plan goes by the tokens that a CTA's rows may see: the sinks and the window of a tile's
-// tokens, of all of a request's where few rows share a CTA or nothing is hidden behind a token.
-AttendPlan held_plan(StepView v, int32_t held, int32_t causal, int32_t window, int32_t sinks, int sms) {
-    if (held) {
-        const int64_t group = v.group, tile = 2 * tile_rows_of(v.group) / group;
-        const int64_t most = (int64_t)window + sinks + (causal && v.max_q > tile ? tile : v.max_q);
-        if (most < v.max_kv) v.max_kv = (int32_t)most;
+// With sinks a plan goes by the tokens that a CTA's rows may see: the sinks and the window of its tiles'
+// tokens, or of all of a request's where few rows share a CTA or nothing is hidden behind a token.
+StepView held_view(StepView v, int32_t causal, int32_t window, int32_t sinks, int64_t tokens) {
+    const int64_t most = (int64_t)window + sinks + (causal && v.max_q > tokens ? tokens : v.max_q);
+    if (most < v.max_kv) v.max_kv = (int32_t)most;
+    return v;
+}
+
+// Costs in us, fitted to measurements (8 KV heads of 128 dims, 5 query heads each, a request of 293 new tokens
+// and sinks of 64, in a graph): CTAs that stay and take two row tiles at a time 35.5 with a window of 2048, 16.7 with 512;
+// a CTA to a row tile 30.6 and 16.9; two row tiles to a CTA, in three parts that a second kernel joins, 28.0 and
+// 22.0, with a window of 8192 51.1 against 112.  Parts that their cluster joins: 35 rows of 64 dims of 16 heads over 1000 tokens
+// 8.7 in five, 10.1 in four, 16.6 in one.
+AttendPlan held_plan(const StepView& v, int32_t held, int32_t causal, int32_t window, int32_t sinks, int sms) {
+    if (!held) return attend_plan(v, sms);
+    const int64_t rows = (int64_t)v.max_q * v.group, units = (int64_t)v.kv_heads * v.requests, per = tile_rows_of(v.group);
+    if (rows <= 16) return attend_plan(held_view(v, causal, window, sinks, v.max_q), sms);
+    AttendPlan best{1, 1, 1, 0};
+    double least = -1.0;
+    auto offer = [&](int row_tiles, int64_t parts, int cluster, double cost) {
+        if (least >= 0.0 && cost >= least) return;
+        least = cost;
+        best = AttendPlan{1, (int)parts, row_tiles, cluster};
+    };
+    for (int rt = 1; rt <= 2; ++rt) {
+        if (rt == 2 && rows <= per) break;
+        const int64_t tiles = (rows + per * rt - 1) / (per * rt) * units, slots = rt == 1 && v.head_dim <= 64 ? 2 * sms : sms;
+        // places of the last sink's block and of the window's first one may be nobody's
+        const int64_t block = v.block_size < 128 ? v.block_size : 128;
+        const int64_t steps = ((int64_t)held_view(v, causal, window, sinks, per * rt / v.group + 1).max_kv + 2 * block + 125) / 128;
+        for (int64_t n = 1; n <= 256 && n <= steps; ++n) {
+            const int64_t ctas = tiles * n;
+            const double each = (double)((steps + n - 1) / n), waves = (double)((ctas + slots - 1) / slots);
+            if (n == 1) offer(rt, 1, 0, rt == 2 ? 7.3 + 1.6 * each * waves + 5.0 * (waves - 1.0) : waves * (1.17 * each + 9.0));
+            // clusters have room as in attend_plan
+            else if (rt == 1 && n <= kCluster && ctas <= sms - 10 * (n - 1)) offer(1, n, 1, 1.15 * each + 8.0);
+            else if (n <= (steps + 1) / 2) offer(rt, n, 0, rt == 2 ? waves * (1.5 * each + 7.0) + 12.0 : waves * (1.17 * each + 9.0) + 4.0 + 0.02 * n);
+        }
     }
-    return attend_plan(v, sms);
+    return best;
 }
 
 int64_t pairs_of_tiles(const StepView& v) {
@@ -256,8 +287,7 @@ int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     j.splits = plan.splits;
     j.cluster = plan.cluster;
     j.row_tiles = plan.row_tiles;
-    // more pairs of row tiles than SMs: CTAs that stay
-    j.stay = j.held && plan.tc && plan.splits == 1 && plan.row_tiles == 2 && pairs_of_tiles(j.step) > sms && pairs_of_tiles(j.step) <= INT32_MAX ? sms : 0;
+    j.stay = j.held && plan.tc && plan.splits == 1 && plan.row_tiles == 2 && pairs_of_tiles(j.step) <= INT32_MAX ? sms : 0;
     const int64_t need = workspace_bytes(j.step, plan);
     if (need > 0) {
         if (!a->workspace) return ops_fail(KVS_ERR_INVALID_ARG, "workspace is NULL, %lld bytes are needed", (long long)need);
