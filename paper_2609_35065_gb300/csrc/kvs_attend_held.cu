@@ -24,9 +24,11 @@ template <int DP>
 struct Plan {
     static constexpr int threads = 256 * kTiles + 128;
     static constexpr int tile = kN * DP * 2;       // bytes of a tile of Q, K or V
-    static constexpr int stages = DP == 128 ? 5 : 8;
+    static constexpr int stages = 4;
     static constexpr int columns = 512;            // of tensor memory: S of each tile, then O
-    static constexpr int bars = (kTiles + stages) * tile;
+    static constexpr bool staged = DP == 128;
+    static constexpr int out = (kTiles + stages) * tile;             // [warp][32 rows][64 bytes], if staged
+    static constexpr int bars = out + (staged ? 8 * kTiles * 2048 : 0);
     static constexpr int tops = bars + 256;        // [2][kTiles][128] binary32: maxima, sums that a row's threads exchange
     static constexpr int bytes = tops + 1024 * kTiles;
 };
@@ -44,12 +46,6 @@ struct Item {
     Span    all;                                   // places that some row sees
     Held    held;
     int32_t r, h, row0, rows, steps, T;            // T: places of the cache
-};
-
-// Goes over a CTA's items; the next one's lengths are on their way meanwhile.
-struct Walk {
-    uint32_t   w;
-    RawRequest raw;
 };
 
 template <bool HALF, int DP>
@@ -72,25 +68,19 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
     const int warp = warp_number(), wg = warp >> 2, lane = threadIdx.x & 31;
     const int32_t per = tile_rows_of(st.group);
 
-    // the item's pair of request and KV head, and its pair of row tiles
-    auto fetch = [&](Walk& k) {
-        if (k.w < total) k.raw = fetch_request(st, fdiv(fdiv(k.w, tiles), heads_of));
-    };
-    Walk walk{blockIdx.x, {}};
-    fetch(walk);
+    uint32_t at_item = blockIdx.x;
     const int32_t unit = boxes ? min(st.block_size, kN) : 1;
     // floor and ceiling in units, of which there is one to a box: divided as block_of divides, or by 128
     auto units = [&](int32_t t) { return unit == 1 ? t : unit == st.block_size ? (int32_t)block_of(st, t) : t >> 7; };
     auto next_item = [&](Item& it) {
-        while (walk.w < total) {
-            const uint32_t p = fdiv(walk.w, tiles), tile = walk.w - p * tiles.d;
-            const RawRequest mine = walk.raw;
-            walk.w += gridDim.x;
-            fetch(walk);
+        while (at_item < total) {
+            // the item's pair of request and KV head, and its pair of row tiles
+            const uint32_t p = fdiv(at_item, tiles), tile = at_item - p * tiles.d;
+            at_item += gridDim.x;
             it.r = fdiv(p, heads_of);
             it.h = p - it.r * heads_of.d;
             it.row0 = (int32_t)tile * kTiles * per;
-            it.q = check_request(st, mine);
+            it.q = load_request(st, it.r);
             it.rows = min(kTiles * per, it.q.n * st.group - it.row0);
             if (it.rows <= 0) continue;
             int32_t g;
@@ -191,11 +181,11 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                 // Where no row sees anything V has to be zeros; K may be anything there.
                 const bool whole = (t0 >= it.all.lo || min(t0 + kN, it.all.lo) <= j.sinks) && t0 + kN <= it.T;
                 if (boxes && (whole || !is_v)) {
+                    tile_boxes<DP>(dst, is_v ? &v_map : &k_map, st, it.h, box, bar.full + 8 * stage, lane);
                     if (pending >= 0) {
                         cp_wait<0>();
                         announce();
                     }
-                    tile_boxes<DP>(dst, is_v ? &v_map : &k_map, st, it.h, box, bar.full + 8 * stage, lane);
                 } else {
                     if (boxes) {
                         tile_mixed<DP>(dst, &v_map, j.v_plane, st, it.h, box, bar.full + 8 * stage, t0, it.all.lo, it.T, j.sinks, lane);
@@ -362,9 +352,17 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
         const int32_t heads = st.kv_heads * st.group;
         uint32_t gone = 0, items = 0;
         bool ok = true;
-        Item it;
-        while (next_item(it)) {
-            const int32_t steps = it.steps;
+        // Of the item at hand: this thread's row -- whether there is one, what it sees, where its results go
+        // (of rows of all tensors: its first element in `out`, its entry of lse) -- and the steps.
+        Span see{};
+        char* row_at = nullptr;
+        int64_t lse_at = 0;
+        int32_t steps = 0;
+        bool live = false;
+        auto take = [&]() {
+            Item it;
+            if (!next_item(it)) return false;
+            steps = it.steps;
             if (!q_boxes && steps > 0) {
                 if (items > 0) ok = ok && __all_sync(0xffffffffu, wait(bar.q_free + 8 * tl, (items - 1) & 1));
                 constexpr int CH = DP / 8;
@@ -384,10 +382,19 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
             }
             int32_t g;
             const int32_t tok = token_of(st, it.row0 + tl * per + t, g);
-            const bool live = t < per && tl * per + t < it.rows;
+            live = t < per && tl * per + t < it.rows;
             // a tile's rows without a token see everything, so that their warp need not mask for them
-            Span see{0, INT32_MAX};
-            if (live) see = in_places(it.held, seen_by(it.q, tok, tok, j.causal, j.window));
+            see = Span{0, INT32_MAX};
+            row_at = nullptr;
+            if (live) {
+                see = in_places(it.held, seen_by(it.q, tok, tok, j.causal, j.window));
+                row_at = j.out.base + 2 * ((int64_t)(it.q.q0 + tok) * j.out.row + (int64_t)(it.h * st.group + g) * j.out.head);
+                lse_at = (int64_t)(it.q.q0 + tok) * heads + it.h * st.group + g;
+            }
+            return true;
+        };
+        bool have = take();
+        while (have) {
             // log2 of a weight at the reference
             const float top_at = HALF ? half_top(steps * kN, 3) : 0.0f;
             float m = kNone, l0 = 0.0f, l1 = 0.0f;
@@ -416,8 +423,23 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                         for (int n = 0; n < 32; ++n) s[n] = bits[b] >> n & 1 ? s[n] : kNone;
                     }
                 };
-                // Against this step's own maximum: the first step, and the first that rows see any key of.
-                bool exact = k == 0 || __any_sync(0xffffffffu, live && m == kNone && see.lo < (k + 1) * kN && see.hi > k * kN);
+                if (k == 0) {
+                    // The first reference is the maximum of the first 32 places, the sinks among them, which both
+                    // halves take for themselves: one that both shared of all 128 had the row wait twice as long.
+                    auto up_to = [](int32_t x) { return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1; };
+                    const uint32_t first = up_to(see.hi) & (~up_to(see.lo) | up_to(j.sinks));
+                    uint32_t sr[32];
+                    tmem_ld32(sr, s_at(tl) + lanes);
+                    tmem_wait_ld();
+                    tmem_loaded32(sr);
+                    float* s = reinterpret_cast<float*>(sr);
+#pragma unroll
+                    for (int n = 0; n < 32; ++n) s[n] = first >> n & 1 ? s[n] : kNone;
+#pragma unroll
+                    for (int n = 0; n < 32; n += 2) m = max3(m, s[n], s[n + 1]);
+                }
+                // Against this step's own maximum: the first step that rows see any key of.
+                bool exact = __any_sync(0xffffffffu, live && m == kNone && see.lo < (k + 1) * kN && see.hi > k * kN);
                 uint32_t pk[32];
                 float a0, a1;
                 while (true) {
@@ -491,44 +513,58 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                 if (lane == 0) mbar_arrive(bar.p + 8 * tl);
             }
             // ---- the rows' results --------------------------------------------------------
-            if (steps > 0) {
-                ok = ok && __all_sync(0xffffffffu, wait(bar.o + 8 * tl, items & 1));
-                ++items;
-            }
-            tc_fence_after();
             float l = l0 + l1;
             tops[half * 128 * kTiles + tl * 128 + t] = l;
             bar_some(pair, 64);
             l = tops[tl * 128 + t] + tops[128 * kTiles + tl * 128 + t];
             bar_some(pair, 64);                                      // the next item's maxima go over them
-            char* row_at = nullptr;
-            if (live && ok) {
-                row_at = j.out.base + 2 * ((int64_t)(it.q.q0 + tok) * j.out.row + (int64_t)(it.h * st.group + g) * j.out.head);
-                if (half == 0 && j.lse)
-                    j.lse[(int64_t)(it.q.q0 + tok) * heads + it.h * st.group + g] = l == 0.0f ? kNone : ((m == kNone ? kNone : m * c - top_at) + log2f(l)) * 0.69314718055994531f;
-            }
+            if (live && ok && half == 0 && j.lse) j.lse[lse_at] = l == 0.0f ? kNone : ((m == kNone ? kNone : m * c - top_at) + log2f(l)) * 0.69314718055994531f;
+            const bool some_o = steps > 0;
+            char* to = ok ? row_at : nullptr;
+            if (some_o) ++items;
+            // the next item's rows while the last product with V is under way (its queries, where these warps bring
+            // them, go to a place that the last S has left)
+            have = take();
+            if (some_o && !__all_sync(0xffffffffu, !ok || wait(bar.o + 8 * tl, (items - 1) & 1))) ok = false;
+            if (!ok) to = nullptr;
+            tc_fence_after();
             const float f = l > 0.0f ? 1.0f / l : l;
+            // Through shared memory, 64 bytes of 32 rows at a time, so that four lanes write a row's piece.
+            // Narrow rows are written as they are: by way of shared memory four prompts of 4096 tokens with 64 dims take 157 us, 148 so.
+            const uint32_t stage = base + P::out + warp * 2048;
 #pragma unroll
-            for (int b = 0; b < DP / 32; ++b) {
-                // 16 columns: two vectors, a sector of the row
-                uint32_t o[16];
-                if (steps > 0) {
-                    tmem_ld16(o, o_own + 16 * b);
-                    tmem_wait_ld();
-                    tmem_loaded16(o);
+            for (int b = 0; b < DP / 64; ++b) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    uint32_t o[16];
+                    if (some_o) {
+                        tmem_ld16(o, o_own + 32 * b + 16 * x);
+                        tmem_wait_ld();
+                        tmem_loaded16(o);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = some_o && l != 0.0f ? __float_as_uint(__uint_as_float(o[e]) * f) : 0u;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        uint32_t y[4];
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) y[n] = N::pack(__uint_as_float(o[8 * e + 2 * n]), __uint_as_float(o[8 * e + 2 * n + 1]));
+                        const int d = DP / 2 * half + 32 * b + 16 * x + 8 * e;
+                        if (!P::staged) {
+                            if (to && d < st.head_dim) *reinterpret_cast<uint4*>(to + 2 * d) = make_uint4(y[0], y[1], y[2], y[3]);
+                        } else st_shared16(stage + lane * 64 + (((2 * x + e) ^ (lane >> 1 & 3)) << 4), y[0], y[1], y[2], y[3]);
+                    }
                 }
+                if (!P::staged) continue;
+                __syncwarp();
+                const int d = DP / 2 * half + 32 * b + 8 * (lane & 3);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = steps > 0 && l != 0.0f ? __float_as_uint(__uint_as_float(o[e]) * f) : 0u;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    uint4 x;
-                    x.x = N::pack(__uint_as_float(o[8 * e]), __uint_as_float(o[8 * e + 1]));
-                    x.y = N::pack(__uint_as_float(o[8 * e + 2]), __uint_as_float(o[8 * e + 3]));
-                    x.z = N::pack(__uint_as_float(o[8 * e + 4]), __uint_as_float(o[8 * e + 5]));
-                    x.w = N::pack(__uint_as_float(o[8 * e + 6]), __uint_as_float(o[8 * e + 7]));
-                    const int d = DP / 2 * half + 16 * b + 8 * e;
-                    if (row_at && d < st.head_dim) *reinterpret_cast<uint4*>(row_at + 2 * d) = x;
+                for (int i = 0; i < 4; ++i) {
+                    const int row = 8 * i + (lane >> 2);
+                    char* dst = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, (unsigned long long)to, row));
+                    if (dst && d < st.head_dim) *reinterpret_cast<uint4*>(dst + 2 * d) = ld_shared16(stage + row * 64 + (((lane & 3) ^ (row >> 1 & 3)) << 4));
                 }
+                __syncwarp();
             }
             tc_fence_before();
         }
