@@ -9,23 +9,22 @@
 // warps still write the results.
 //
 // Steps go over the places of the cache (Held): the sinks' blocks, then those from the window's first token on.
-#include "kvs_tcgen05.cuh"
+#include "kvs_attend_held.cuh"
 
 namespace kvs {
 namespace {
 
-constexpr int kM = 128, kN = 128;                  // rows of a tile, keys of a step
-constexpr int kTiles = 2;
-constexpr int kLoaders = 3;
-constexpr int kIssuer = 8 * kTiles;                // the issuing warp, behind the softmax's; then the loading ones
-constexpr float kNone = -INFINITY;
-
 template <int DP>
 struct Plan {
-    static constexpr int threads = 256 * kTiles + 128;
     static constexpr int tile = kN * DP * 2;       // bytes of a tile of Q, K or V
     static constexpr int stages = 4;
     static constexpr int columns = 512;            // of tensor memory: S of each tile, then O
+    // Issuing and loading warps.  A narrow tile's products and loads are both short, and a warp to each tile's products
+    // keeps one tile from waiting for the other (four prompts of 4096 tokens with 64 dims and a window of 128: 123 us,
+    // with one for both 131); a wide tile's 16 boxes want three warps to load (16 suffixes of 2048 tokens with 128 dims
+    // and a window of 1024: 446 us, with two 482).
+    static constexpr int issuers = DP == 128 ? 1 : 2, loaders = 4 - issuers;
+    static_assert(loaders < stages, "a loading warp is less than a round ahead of the others");
     static constexpr bool staged = DP == 128;
     static constexpr int out = (kTiles + stages) * tile;             // [warp][32 rows][64 bytes], if staged
     static constexpr int bars = out + (staged ? 8 * kTiles * 2048 : 0);
@@ -33,25 +32,16 @@ struct Plan {
     static constexpr int bytes = tops + 1024 * kTiles;
 };
 
-// q, q_free, s, p and o: one of each tile.
+// q, s, p and o: one of each tile.
 struct Bars {
-    uint32_t q, q_free, s, p, o, full, free, done;
-    __device__ Bars(uint32_t at, int stages)
-        : q(at), q_free(at + 16), s(at + 32), p(at + 48), o(at + 64), full(at + 80), free(full + 8 * stages), done(free + 8 * stages) {}
-};
-
-// What a CTA works on: two tiles of a request's packed rows, of one KV head.
-struct Item {
-    Request q;
-    Span    all;                                   // places that some row sees
-    Held    held;
-    int32_t r, h, row0, rows, steps, T;            // T: places of the cache
+    uint32_t q, s, p, o, full, free, done;
+    __device__ Bars(uint32_t at, int stages) : q(at), s(at + 16), p(at + 32), o(at + 48), full(at + 64), free(full + 8 * stages), done(free + 8 * stages) {}
 };
 
 template <bool HALF, int DP>
-__global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(AttendJob j, const __grid_constant__ CUtensorMap k_map,
+__global__ void __launch_bounds__(kThreads, 1) kvs_attend_held_kernel(AttendJob j, const __grid_constant__ CUtensorMap k_map,
                                                                             const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap q_map,
-                                                                            int32_t boxes, int32_t q_boxes, FastDiv tiles, FastDiv heads_of, uint32_t total) {
+                                                                            ItemList list, int32_t q_boxes) {
     extern __shared__ __align__(1024) char raw[];
     using N = Num<HALF>;
     using P = Plan<DP>;
@@ -64,64 +54,29 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
     }
     const uint32_t ring = base + kTiles * P::tile, ctl = base + P::bars;
     const Bars bar(ctl, P::stages);
-    const uint32_t tmem_at = bar.done + 8;
+    const uint32_t tmem_at = bar.done + 16;
     const int warp = warp_number(), wg = warp >> 2, lane = threadIdx.x & 31;
-    const int32_t per = tile_rows_of(st.group);
-
-    uint32_t at_item = blockIdx.x;
-    const int32_t unit = boxes ? min(st.block_size, kN) : 1;
-    // floor and ceiling in units, of which there is one to a box: divided as block_of divides, or by 128
-    auto units = [&](int32_t t) { return unit == 1 ? t : unit == st.block_size ? (int32_t)block_of(st, t) : t >> 7; };
-    auto next_item = [&](Item& it) {
-        while (at_item < total) {
-            // the item's pair of request and KV head, and its pair of row tiles
-            const uint32_t p = fdiv(at_item, tiles), tile = at_item - p * tiles.d;
-            at_item += gridDim.x;
-            it.r = fdiv(p, heads_of);
-            it.h = p - it.r * heads_of.d;
-            it.row0 = (int32_t)tile * kTiles * per;
-            it.q = load_request(st, it.r);
-            it.rows = min(kTiles * per, it.q.n * st.group - it.row0);
-            if (it.rows <= 0) continue;
-            int32_t g;
-            const int32_t tok = token_of(st, it.row0, g);
-            it.all = seen_by(it.q, tok, token_of(st, it.row0 + it.rows - 1, g), j.causal, j.window);
-            // as held_of
-            const int32_t first = units(it.all.lo) * unit;
-            it.held.cut = min(units(min(j.sinks, it.all.lo) + unit - 1) * unit, first);
-            it.held.shift = first - it.held.cut;
-            it.all = in_places(it.held, it.all);
-            it.T = it.q.T - it.held.shift;
-            it.steps = it.all.hi > it.all.lo ? (it.all.hi + kN - 1) / kN : 0;
-            return true;
-        }
-        return false;
-    };
-    // ... of those whose rows see something
-    auto next_active = [&](Item& it) {
-        bool some;
-        do some = next_item(it);
-        while (some && it.steps == 0);
-        return some;
-    };
+    const bool boxes = list.boxes;
+    Walk walk(j, list);
+    const int32_t per = walk.per;
 
     if (warp == kIssuer) tmem_alloc(tmem_at, P::columns);
     if (threadIdx.x == 0) {
         for (int t = 0; t < kTiles; ++t) {
             mbar_init(bar.q + 8 * t, q_boxes ? 1 : 256);
-            mbar_init(bar.q_free + 8 * t, 1);
             mbar_init(bar.s + 8 * t, 1);
             mbar_init(bar.p + 8 * t, 8);
             mbar_init(bar.o + 8 * t, 1);
         }
         for (int i = 0; i < P::stages; ++i) {
-            mbar_init(bar.full + 8 * i, kLoaders);
-            mbar_init(bar.free + 8 * i, 1);
+            mbar_init(bar.full + 8 * i, 1);
+            mbar_init(bar.free + 8 * i, P::issuers);
         }
-        mbar_init(bar.done, 1);
+        for (int i = 0; i < P::issuers; ++i) mbar_init(bar.done + 8 * i, 1);
         mbar_init_fence();
     }
-    if (warp == kIssuer + 1 && lane == 0) {
+    constexpr int kLoader = kIssuer + P::issuers;
+    if (warp == kLoader && lane == 0) {
         if (boxes) {
             prefetch_map(&k_map);
             prefetch_map(&v_map);
@@ -146,97 +101,80 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
     // The softmax's warps get registers of the others' (512 x 104 + 128 x 64 = 640 x 96).
     if (warp >= kIssuer) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     else asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-    if (warp > kIssuer) {
+    if (warp >= kLoader) {
         // ---- K and V: the ring's tile i is K (even) or V (odd) of step i / 2 of all items' -----
-        const int t = threadIdx.x - 32 * (kIssuer + 1), w = warp - kIssuer - 1;
-        int pending = -1;                                    // cp.async tile not yet announced
+        // A warp brings every P::loaders-th tile whole: its waits and look-ups are beside the others' then.  A stage is
+        // free in the order of the ring, so that a wait for a stage's last user follows those before it.
+        const int w = warp - kLoader;
+        int pending = -1;                                    // tile with cp.async rows, not yet announced
         auto announce = [&]() {
+            cp_wait<0>();
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar.full + 8 * pending);
             pending = -1;
         };
-        Item it, after;
-        bool have = next_active(it), ok = true;
-        Box box{}, next{};
-        if (have && boxes) next = box_of<DP, kLoaders>(st, st.tables + (int64_t)it.r * st.table_stride, it.held, 0, it.T, w, lane);
-        uint32_t i = 0, stage = 0, round = 0, items = 0, rows_of[kTiles] = {};        // items whose rows each tile's place was sent
-        while (have && ok) {
-            const bool more = next_active(after);
-            const int32_t* table = st.tables + (int64_t)it.r * st.table_stride;
-            for (int32_t k = 0; k < 2 * it.steps; ++k, ++i) {
-                if (boxes && !(k & 1)) {
-                    // K's and V's tiles of a step are in the same blocks; the next step's are looked up a step ahead
-                    box = next;
-                    if (k + 2 < 2 * it.steps) next = box_of<DP, kLoaders>(st, table, it.held, ((k >> 1) + 1) * kN, it.T, w, lane);
-                    else if (more) next = box_of<DP, kLoaders>(st, st.tables + (int64_t)after.r * st.table_stride, after.held, 0, after.T, w, lane);
-                }
-                if (round > 0) {
-                    ok = __all_sync(0xffffffffu, lane != 0 || wait(bar.free + 8 * stage, (round - 1) & 1));
-                    if (!ok) break;
-                }
-                const uint32_t dst = ring + stage * P::tile;
-                const int32_t t0 = (k >> 1) * kN;
-                const bool is_v = k & 1;
-                // Where no row sees anything V has to be zeros; K may be anything there.
-                const bool whole = (t0 >= it.all.lo || min(t0 + kN, it.all.lo) <= j.sinks) && t0 + kN <= it.T;
-                if (boxes && (whole || !is_v)) {
-                    tile_boxes<DP>(dst, is_v ? &v_map : &k_map, st, it.h, box, bar.full + 8 * stage, lane);
-                    if (pending >= 0) {
-                        cp_wait<0>();
-                        announce();
-                    }
-                } else {
-                    if (boxes) {
-                        tile_mixed<DP>(dst, &v_map, j.v_plane, st, it.h, box, bar.full + 8 * stage, t0, it.all.lo, it.T, j.sinks, lane);
-                    } else {
-                        tile_rows<DP, 32 * kLoaders>(dst, is_v ? j.v_plane : j.k_plane, st, table, it.h, it.held, t0, it.all.lo, it.T, j.sinks, t);
-                    }
-                    cp_commit();
-                    if (pending >= 0) {
-                        cp_wait<1>();
-                        announce();
-                    }
-                    pending = stage;
-                }
-                if (k == 0 && w == 0 && q_boxes) {
-                    // the item's rows, where the last one's lay
-                    for (int x = 0; ok && x < kTiles; ++x) {
-                        if (items > 0) ok = __all_sync(0xffffffffu, lane != 0 || wait(bar.q_free + 8 * x, (items - 1) & 1));
-                        if (!ok) break;
-                        rows_of[x] = items + 1;
-                        if (lane == 0) {
-                            mbar_expect_tx(bar.q + 8 * x, (uint32_t)per * DP * 2);
-#pragma unroll
-                            for (int c = 0; c < DP / 64; ++c)
-                                tma_load_3d(base + x * P::tile + c * kM * 128, &q_map, 64 * c, it.h * st.group, it.q.q0 + (it.row0 + x * per) / st.group, bar.q + 8 * x);
-                        }
-                        __syncwarp();
-                    }
-                }
-                if (++stage == P::stages) {
-                    stage = 0;
-                    ++round;
-                }
-                if (!ok) {
-                    ++i;
-                    break;
-                }
+        // The tile at hand, k of an item, and whether there is one.
+        struct Cursor {
+            Item    it;
+            int32_t k;
+            bool    have;
+        };
+        auto ahead = [&](Cursor& c, int32_t n) {
+            c.k += n;
+            while (c.have && c.k >= 2 * c.it.steps) {
+                c.k -= 2 * c.it.steps;
+                c.have = walk.next_active(c.it);
             }
-            ++items;
-            it = after;
-            have = more;
+        };
+        auto look_up = [&](const Cursor& c) {
+            return c.have && boxes ? box_of<DP, 1>(st, st.tables + (int64_t)c.it.r * st.table_stride, c.it.held, (c.k >> 1) * kN, c.it.T, 0, lane) : Box{};
+        };
+        Cursor now{{}, 0, false};
+        now.have = walk.next_active(now.it);
+        ahead(now, w);
+        Box box = look_up(now);
+        uint32_t i = w;
+        bool ok = true;
+        while (now.have && ok) {
+            Cursor next = now;
+            ahead(next, P::loaders);
+            const Box after = look_up(next);
+            const uint32_t stage = i % P::stages, round = i / P::stages;
+            if (round > 0) {
+                ok = __all_sync(0xffffffffu, lane != 0 || wait(bar.free + 8 * stage, (round - 1) & 1));
+                if (!ok) break;
+            }
+            const Item& it = now.it;
+            const uint32_t dst = ring + stage * P::tile;
+            const int32_t t0 = (now.k >> 1) * kN;
+            const bool is_v = now.k & 1;
+            if (boxes && (!is_v || tile_whole(it, t0, j.sinks))) {
+                tile_boxes<DP>(dst, is_v ? &v_map : &k_map, st, it.h, box, bar.full + 8 * stage, lane);
+                if (pending >= 0) announce();
+            } else {
+                if (pending >= 0) announce();
+                if (boxes) tile_mixed<DP>(dst, &v_map, j.v_plane, st, it.h, box, bar.full + 8 * stage, t0, it.all.lo, it.T, j.sinks, lane);
+                else tile_rows<DP, 32>(dst, is_v ? j.v_plane : j.k_plane, st, st.tables + (int64_t)it.r * st.table_stride, it.h, it.held, t0, it.all.lo, it.T, j.sinks, lane);
+                cp_commit();
+                pending = stage;
+            }
+            // A tile of V may wait for its rows until this warp's next tile is sent for: what frees that one's stage does not
+            // need it.  Of tiles of K by rows that would not hold.
+            if (pending >= 0 && !boxes) announce();
+            i += P::loaders;
+            now = next;
+            box = after;
         }
-        cp_wait<0>();
         if (pending >= 0) announce();
         // Before the CTA leaves, every load has landed (all of them have when the products are done).
         if (!ok) {
-            for (uint32_t k = i < P::stages ? 0 : i - P::stages; k < i; ++k) mbar_wait(bar.full + 8 * (k % P::stages), (k / P::stages) & 1, kWaitLimitNs);
-            for (int x = 0; x < kTiles; ++x)
-                if (rows_of[x] > 0) mbar_wait(bar.q + 8 * x, (rows_of[x] - 1) & 1, kWaitLimitNs);
+            for (uint32_t k = w; k <= i; k += P::loaders)
+                if (k + P::stages > i) mbar_wait(bar.full + 8 * (k % P::stages), (k / P::stages) & 1, kWaitLimitNs);
         }
-    } else if (warp == kIssuer) {
-        // ---- the products: the warp waits together, one lane issues ------------------
+    } else if (warp >= kIssuer) {
+        // ---- the products of tiles t0 to t1: the warp waits together, one lane issues ---
+        const int t0 = P::issuers == 2 ? warp - kIssuer : 0, t1 = P::issuers == 2 ? t0 + 1 : kTiles;
         // a negative scale's sign goes into the products, so that maxima of S are those of the scores
         const uint32_t id_s = tc_idesc(HALF, kN, false) | (j.scale_log2 < 0.0f ? kNegA : 0u);
         constexpr uint32_t id_o = tc_idesc(HALF, DP, true);
@@ -250,6 +188,16 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                 tc_mma_ss(tm + 128 * t, tc_ahead(a, off), tc_ahead(b, off), id_s, k > 0);
             }
             tc_commit(bar.s + 8 * t);
+        };
+        // An item's rows to a tile's place, when the products that read the last ones are done.
+        auto send_rows = [&](const Item& x, int t) {
+            if (elect_one()) {
+                mbar_expect_tx(bar.q + 8 * t, (uint32_t)per * DP * 2);
+#pragma unroll
+                for (int c = 0; c < DP / 64; ++c)
+                    tma_load_3d(base + t * P::tile + c * kM * 128, &q_map, 64 * c, x.h * st.group, x.q.q0 + (x.row0 + t * per) / st.group, bar.q + 8 * t);
+            }
+            __syncwarp();
         };
         auto issue_o = [&](int t, int stage, bool add) {
             const uint64_t b = tc_ahead(v_desc, stage * P::tile);
@@ -268,21 +216,21 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
         };
         auto filled = [&](int32_t stage, int32_t round) { return wait(bar.full + 8 * stage, round & 1); };
         Item it;
-        bool have = next_active(it);
+        bool have = walk.next_active(it);
         int32_t steps = it.steps;
         uint32_t gone = 0, items = 0;                        // steps and items that are done with
         bool ok = true;
         if (have) {
             int32_t ks, kr;
             take(ks, kr);
-            ok = __all_sync(0xffffffffu, wait(bar.q, 0) && wait(bar.q + 8, 0) && filled(ks, kr));
+            if (q_boxes)
+                for (int t = t0; t < t1; ++t) send_rows(it, t);
+            for (int t = t0; t < t1; ++t) ok = wait(bar.q + 8 * t, 0) && ok;
+            ok = __all_sync(0xffffffffu, filled(ks, kr) && ok);
             if (ok) {
                 tc_fence_after();
                 if (elect_one()) {
-                    for (int t = 0; t < kTiles; ++t) {
-                        issue_s(t, ks);
-                        if (steps == 1) tc_commit(bar.q_free + 8 * t);
-                    }
+                    for (int t = t0; t < t1; ++t) issue_s(t, ks);
                     tc_commit(bar.free + 8 * ks);
                 }
                 __syncwarp();
@@ -290,17 +238,21 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
         }
         while (have && ok) {
             Item after;
-            const bool follows = next_active(after);
+            const bool follows = walk.next_active(after);
             for (int32_t k = 0; ok && k < steps; ++k, ++gone) {
                 const bool last = k + 1 == steps, more = !last || follows;
-                // whether Q is done with when the next step's S is
-                const bool frees = last ? after.steps == 1 : k + 2 == steps;
                 int32_t vs, vr, ks = 0, kr = 0;
                 take(vs, vr);
                 if (more) take(ks, kr);
+                if (last && more && q_boxes) {
+                    for (int t = t0; t < t1; ++t) {
+                        ok = wait(bar.s + 8 * t, gone & 1) && ok;
+                        if (__all_sync(0xffffffffu, ok)) send_rows(after, t);
+                    }
+                }
                 // V of this step and K of the next were loaded long ago; P is what is waited for.  A wait
                 // that ran out ends the loop at the next vote.
-                ok = filled(vs, vr) && (!more || filled(ks, kr));
+                ok = filled(vs, vr) && (!more || filled(ks, kr)) && ok;
                 // the next item's rows, where the softmax warps bring them, come behind this one's results
                 const bool later = last && more && !q_boxes;
                 auto next_s = [&](int t) {
@@ -309,23 +261,22 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                     tc_fence_after();
                     if (elect_one()) {
                         issue_s(t, ks);
-                        if (frees) tc_commit(bar.q_free + 8 * t);
-                        if (t == kTiles - 1) tc_commit(bar.free + 8 * ks);
+                        if (t == t1 - 1) tc_commit(bar.free + 8 * ks);
                     }
                 };
-                for (int t = 0; t < kTiles; ++t) {
+                for (int t = t0; t < t1; ++t) {
                     ok = wait(bar.p + 8 * t, gone & 1) && ok;
                     __syncwarp();
                     tc_fence_after();
                     if (elect_one()) {
                         issue_o(t, vs, k > 0);
                         if (last) tc_commit(bar.o + 8 * t);
-                        if (t == kTiles - 1) tc_commit(bar.free + 8 * vs);
+                        if (t == t1 - 1) tc_commit(bar.free + 8 * vs);
                     }
                     if (more && !later) next_s(t);
                 }
                 if (later)
-                    for (int t = 0; t < kTiles; ++t) next_s(t);
+                    for (int t = t0; t < t1; ++t) next_s(t);
                 ok = __all_sync(0xffffffffu, ok);
             }
             ++items;
@@ -334,8 +285,12 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
         }
         if (!ok && elect_one()) {
             // what was issued is done before the CTA leaves
-            tc_commit(bar.done);
-            mbar_wait(bar.done, 0, kWaitLimitNs);
+            tc_commit(bar.done + 8 * (warp - kIssuer));
+            mbar_wait(bar.done + 8 * (warp - kIssuer), 0, kWaitLimitNs);
+            for (int t = t0; t < t1; ++t) {
+                mbar_wait(bar.q + 8 * t, 0, kWaitLimitNs);
+                mbar_wait(bar.q + 8 * t, 1, kWaitLimitNs);
+            }
         }
         __syncwarp();
     } else {
@@ -349,22 +304,15 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
         const float c = fmaxf(fabsf(j.scale_log2), 1e-36f);         // a zero scale keeps -infinity * c what it is
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // lane 32 (warp % 4) of tensor memory
         const uint32_t s_own = s_at(tl) + lanes + 64 * half, o_own = o_at(tl) + lanes + DP / 2 * half;
-        const int32_t heads = st.kv_heads * st.group;
         uint32_t gone = 0, items = 0;
         bool ok = true;
-        // Of the item at hand: this thread's row -- whether there is one, what it sees, where its results go
-        // (of rows of all tensors: its first element in `out`, its entry of lse) -- and the steps.
-        Span see{};
-        char* row_at = nullptr;
-        int64_t lse_at = 0;
+        RowOf row{};                                                 // this thread's of the item at hand
         int32_t steps = 0;
-        bool live = false;
         auto take = [&]() {
             Item it;
-            if (!next_item(it)) return false;
+            if (!walk.next(it)) return false;
             steps = it.steps;
             if (!q_boxes && steps > 0) {
-                if (items > 0) ok = ok && __all_sync(0xffffffffu, wait(bar.q_free + 8 * tl, (items - 1) & 1));
                 constexpr int CH = DP / 8;
 #pragma unroll 4
                 for (int v = threadIdx.x & 255; v < kM * CH; v += 256) {
@@ -380,17 +328,7 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                 fence_async_smem();
                 mbar_arrive(bar.q + 8 * tl);
             }
-            int32_t g;
-            const int32_t tok = token_of(st, it.row0 + tl * per + t, g);
-            live = t < per && tl * per + t < it.rows;
-            // a tile's rows without a token see everything, so that their warp need not mask for them
-            see = Span{0, INT32_MAX};
-            row_at = nullptr;
-            if (live) {
-                see = in_places(it.held, seen_by(it.q, tok, tok, j.causal, j.window));
-                row_at = j.out.base + 2 * ((int64_t)(it.q.q0 + tok) * j.out.row + (int64_t)(it.h * st.group + g) * j.out.head);
-                lse_at = (int64_t)(it.q.q0 + tok) * heads + it.h * st.group + g;
-            }
+            row = row_of_item(j, it, per, tl, t);
             return true;
         };
         bool have = take();
@@ -404,14 +342,14 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                 // the keys of this half that the row sees, a bit to each
                 const int32_t t0 = k * kN + 64 * half;
                 auto below = [&](int32_t x) { return x - t0 <= 0 ? 0ull : x - t0 >= 64 ? ~0ull : (1ull << (x - t0)) - 1; };
-                const uint64_t seen = below(see.hi) & (~below(see.lo) | below(j.sinks));
+                const uint64_t seen = below(row.see.hi) & (~below(row.see.lo) | below(j.sinks));
                 const uint32_t bits[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
                 // of either 32: whether some of the warp's rows do not see all of them, and whether some see any
                 bool edge[2], some[2];
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     edge[b] = __any_sync(0xffffffffu, bits[b] != ~0u);
-                    some[b] = __any_sync(0xffffffffu, live && bits[b]);
+                    some[b] = __any_sync(0xffffffffu, row.live && bits[b]);
                 }
                 auto load_s = [&](uint32_t* sr, int b) {
                     tmem_ld32(sr, s_own + 32 * b);
@@ -426,8 +364,7 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                 if (k == 0) {
                     // The first reference is the maximum of the first 32 places, the sinks among them, which both
                     // halves take for themselves: one that both shared of all 128 had the row wait twice as long.
-                    auto up_to = [](int32_t x) { return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1; };
-                    const uint32_t first = up_to(see.hi) & (~up_to(see.lo) | up_to(j.sinks));
+                    const uint32_t first = bits_below(row.see.hi) & (~bits_below(row.see.lo) | bits_below(j.sinks));
                     uint32_t sr[32];
                     tmem_ld32(sr, s_at(tl) + lanes);
                     tmem_wait_ld();
@@ -439,7 +376,7 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                     for (int n = 0; n < 32; n += 2) m = max3(m, s[n], s[n + 1]);
                 }
                 // Against this step's own maximum: the first step that rows see any key of.
-                bool exact = __any_sync(0xffffffffu, live && m == kNone && see.lo < (k + 1) * kN && see.hi > k * kN);
+                bool exact = __any_sync(0xffffffffu, row.live && m == kNone && row.see.lo < (k + 1) * kN && row.see.hi > k * kN);
                 uint32_t pk[32];
                 float a0, a1;
                 while (true) {
@@ -501,7 +438,7 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                     }
                     // No weight is above its sum.  Both halves of S are read behind this: P goes over the
                     // first one's columns.
-                    const bool again = bar_or(pair, 64, !exact && live && (HALF ? fmaxf(a0, a1) : a0 + a1) > kMost);
+                    const bool again = bar_or(pair, 64, !exact && row.live && (HALF ? fmaxf(a0, a1) : a0 + a1) > kMost);
                     if (!again) break;
                     exact = true;
                 }
@@ -518,9 +455,9 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
             bar_some(pair, 64);
             l = tops[tl * 128 + t] + tops[128 * kTiles + tl * 128 + t];
             bar_some(pair, 64);                                      // the next item's maxima go over them
-            if (live && ok && half == 0 && j.lse) j.lse[lse_at] = l == 0.0f ? kNone : ((m == kNone ? kNone : m * c - top_at) + log2f(l)) * 0.69314718055994531f;
+            if (row.live && ok && half == 0 && j.lse) j.lse[row.lse] = l == 0.0f ? kNone : ((m == kNone ? kNone : m * c - top_at) + log2f(l)) * 0.69314718055994531f;
             const bool some_o = steps > 0;
-            char* to = ok ? row_at : nullptr;
+            char* to = ok ? row.out : nullptr;
             if (some_o) ++items;
             // the next item's rows while the last product with V is under way (its queries, where these warps bring
             // them, go to a place that the last S has left)
@@ -560,9 +497,9 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
                 const int d = DP / 2 * half + 32 * b + 8 * (lane & 3);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int row = 8 * i + (lane >> 2);
-                    char* dst = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, (unsigned long long)to, row));
-                    if (dst && d < st.head_dim) *reinterpret_cast<uint4*>(dst + 2 * d) = ld_shared16(stage + row * 64 + (((lane & 3) ^ (row >> 1 & 3)) << 4));
+                    const int r = 8 * i + (lane >> 2);
+                    char* dst = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, (unsigned long long)to, r));
+                    if (dst && d < st.head_dim) *reinterpret_cast<uint4*>(dst + 2 * d) = ld_shared16(stage + r * 64 + (((lane & 3) ^ (r >> 1 & 3)) << 4));
                 }
                 __syncwarp();
             }
@@ -578,14 +515,15 @@ __global__ void __launch_bounds__(Plan<DP>::threads, 1) kvs_attend_held_kernel(A
 template <bool HALF, int DP>
 cudaError_t attend_held(const AttendJob& j, int sms, cudaStream_t s) {
     using P = Plan<DP>;
-    auto* k = kvs_attend_held_kernel<HALF, DP>;
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, P::bytes);
-    if (e != cudaSuccess) return e;
     CUtensorMap km{}, vm{}, qm{};
     const bool boxes = plane_map(&km, j.step, j.k_plane, HALF) && plane_map(&vm, j.step, j.v_plane, HALF), q_boxes = rows_map(&qm, j.step, j.q, HALF);
     const int64_t total = held_items(j.step), tiles = total / ((int64_t)j.step.kv_heads * j.step.requests);
-    k<<<(unsigned)(total < sms ? total : sms), P::threads, P::bytes, s>>>(j, km, vm, qm, (int32_t)boxes, (int32_t)q_boxes, make_fastdiv((uint32_t)tiles),
-                                                                             make_fastdiv((uint32_t)j.step.kv_heads), (uint32_t)total);
+    const ItemList list{make_fastdiv((uint32_t)tiles), make_fastdiv((uint32_t)j.step.kv_heads), (uint32_t)total, boxes};
+    const unsigned grid = (unsigned)(total < sms ? total : sms);
+    auto* k = kvs_attend_held_kernel<HALF, DP>;
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, P::bytes);
+    if (e != cudaSuccess) return e;
+    k<<<grid, kThreads, P::bytes, s>>>(j, km, vm, qm, list, (int32_t)q_boxes);
     return cudaGetLastError();
 }
 

@@ -206,12 +206,18 @@ __device__ __forceinline__ void tile_mixed(uint32_t dst, const CUtensorMap* map,
         const int from = __ffs(split) - 1;
         split &= split - 1;
         const int32_t at = __shfl_sync(0xffffffffu, x.at, from), block = __shfl_sync(0xffffffffu, x.block, from), row0 = __shfl_sync(0xffffffffu, x.row, from);
-        for (int v = lane; v < size * CH; v += 32) {
-            const int k = v / CH, c = v % CH;
+        // lane: vector c of every (32 / CH)-th row from k on; rows of eight begin at multiples of eight of the tile
+        constexpr int STEP = 32 / CH;
+        const int c = lane % CH;
+        const int64_t pitch = (int64_t)st.kv_heads * st.head_dim * 2;
+        const bool can = (uint32_t)block < (uint32_t)st.num_blocks && 8 * c < st.head_dim;
+        const char* src = plane + (can ? ((int64_t)block * st.block_size + row0 + lane / CH) * pitch + (h * st.head_dim + 8 * c) * 2 : 0);
+        const uint32_t to = dst + (c >> 3) * 128 * 128 + at * 128;
+#pragma unroll 4
+        for (int k = lane / CH; k < size; k += STEP) {
             const int32_t u = t0 + at + k;
-            const bool there = (uint32_t)block < (uint32_t)st.num_blocks && (u >= lo || u < sinks) && u < hi && 8 * c < st.head_dim;
-            const int64_t row = there ? (((int64_t)block * st.block_size + row0 + k) * st.kv_heads + h) * st.head_dim + 8 * c : 0;
-            cp_async16(dst + (c >> 3) * 128 * 128 + (at + k) * 128 + (((c & 7) ^ ((at + k) & 7)) << 4), plane + 2 * row, there);
+            cp_async16(to + k * 128 + (((c ^ k) & 7) << 4), src, can && (u >= lo || u < sinks) && u < hi);
+            if (can) src += STEP * pitch;
         }
     }
 }
