@@ -219,9 +219,9 @@ StepView held_view(StepView v, int32_t causal, int32_t window, int32_t sinks, in
 }
 
 // Costs in us, fitted to measurements (8 KV heads of 128 dims, 5 query heads each, a request of 293 new tokens
-// and sinks of 64, in a graph): CTAs that stay and take two row tiles at a time 35.5 with a window of 2048, 16.7 with 512;
-// a CTA to a row tile 30.6 and 16.9; two row tiles to a CTA, in three parts that a second kernel joins, 28.0 and
-// 22.0, with a window of 8192 51.1 against 112.  Parts that their cluster joins: 35 rows of 64 dims of 16 heads over 1000 tokens
+// and sinks of 64, in a graph): CTAs that stay and take two row tiles at a time 31.4 with a window of 2048, 14.4 with 512;
+// a CTA to a row tile 30.5 and 16.9; two row tiles to a CTA, in three parts that a second kernel joins, 28.0 and
+// 22.0, with a window of 4096 36.4 against 54.7.  Parts that their cluster joins: 35 rows of 64 dims of 16 heads over 1000 tokens
 // 8.7 in five, 10.1 in four, 16.6 in one.
 AttendPlan held_plan(const StepView& v, int32_t held, int32_t causal, int32_t window, int32_t sinks, int sms) {
     if (!held) return attend_plan(v, sms);
@@ -243,7 +243,7 @@ AttendPlan held_plan(const StepView& v, int32_t held, int32_t causal, int32_t wi
         for (int64_t n = 1; n <= 256 && n <= steps; ++n) {
             const int64_t ctas = tiles * n;
             const double each = (double)((steps + n - 1) / n), waves = (double)((ctas + slots - 1) / slots);
-            if (n == 1) offer(rt, 1, 0, rt == 2 ? 7.3 + 1.6 * each * waves + 5.0 * (waves - 1.0) : waves * (1.17 * each + 9.0));
+            if (n == 1) offer(rt, 1, 0, rt == 2 ? 5.8 + 1.43 * each * waves + 3.0 * (waves - 1.0) : waves * (1.17 * each + 9.0));
             // clusters have room as in attend_plan
             else if (rt == 1 && n <= kCluster && ctas <= sms - 10 * (n - 1)) offer(1, n, 1, 1.15 * each + 8.0);
             else if (n <= (steps + 1) / 2) offer(rt, n, 0, rt == 2 ? waves * (1.5 * each + 7.0) + 12.0 : waves * (1.17 * each + 9.0) + 4.0 + 0.02 * n);
