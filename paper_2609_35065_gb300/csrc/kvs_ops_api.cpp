@@ -426,18 +426,15 @@ int rope_axes(const kvs_rope_spec* sp, const int32_t* parts, int32_t n, int32_t 
         pairs += parts[a];
     }
     if (sp->rot_dim != 2 * pairs) return ops_fail(KVS_ERR_INVALID_ARG, "rot_dim (%d) is not twice the %lld pairs", sp->rot_dim, (long long)pairs);
-    if (order & KVS_AXES_CYCLE) {
-        for (int64_t k = 0; k < pairs; ++k) axis[k] = 0;
-        for (int a = 1; a < n; ++a) {
-            if (a + (int64_t)n * (parts[a] - 1) >= pairs) return ops_fail(KVS_ERR_INVALID_ARG, "axis %d has no turn for %d pairs", a, parts[a]);
-            for (int64_t k = 0; k < parts[a]; ++k) axis[a + n * k] = (uint8_t)a;
-        }
-    } else {
-        int64_t k = 0;
-        for (int a = 0; a < n; ++a)
-            for (int32_t m = 0; m < parts[a]; ++m) axis[k++] = (uint8_t)a;
-    }
+    const bool cycle = order & KVS_AXES_CYCLE;
+    for (int a = 1; cycle && a < n; ++a)
+        if (a + (int64_t)n * (parts[a] - 1) >= pairs) return ops_fail(KVS_ERR_INVALID_ARG, "axis %d has no turn for %d pairs", a, parts[a]);
     KVS_TRY(rope_turns(sp, turns, scale));
+    int64_t k = 0;
+    for (int a = 0; a < n; ++a)
+        for (int32_t m = 0; m < parts[a]; ++m) axis[k++] = cycle ? 0 : (uint8_t)a;
+    for (int a = 1; cycle && a < n; ++a)
+        for (int64_t m = 0; m < parts[a]; ++m) axis[a + n * m] = (uint8_t)a;
     if (!(order & KVS_AXES_RESTART)) return KVS_OK;
     // each axis's own table, of which its pairs take the entries in turn
     std::vector<float> own;

@@ -34,6 +34,11 @@ __device__ __forceinline__ RowSpan rows_seeing(const StepView& st, const Request
     return rows_seeing(st, q, token_at(held, u_lo), token_at(held, u_hi), causal, u_lo < sinks ? 0 : window);
 }
 
+// What a request's new tokens leave visible; of one that has none, nothing.
+__device__ __forceinline__ Held held_by(const Request& q, const WeighJob& j, int32_t unit) {
+    return q.n > 0 ? held_of(seen_by(q, 0, q.n - 1, j.causal, j.window).lo, j.sinks, unit) : Held{0, q.T};
+}
+
 // Tokens without a place, [cut, cut + shift): nobody sees them, and only what they had before fades.
 // This is part `part` of `parts` of the request's and head's.
 __device__ __forceinline__ void fade(const WeighJob& j, int32_t r, int32_t h, const Held& held, int32_t part, int32_t parts) {
@@ -127,7 +132,7 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
     Held held{};
     int32_t T = q.T;                                             // places (without HELD: tokens) of the cache
     if (HELD) {
-        held = held_of(seen_by(q, 0, max(q.n, 1) - 1, j.causal, j.window).lo, j.sinks, k_boxes ? min(st.block_size, 128) : 1);
+        held = held_by(q, j, k_boxes ? min(st.block_size, 128) : 1);
         T -= held.shift;
         if (tile >= key_tiles_all) {
             const int32_t behind = gridDim.x / (share * st.kv_heads * st.requests) - key_tiles_all;
@@ -531,7 +536,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
     Held held{};
     int32_t T = q.T;                                             // places (without HELD: tokens) of the cache
     if (HELD) {
-        held = held_of(seen_by(q, 0, max(q.n, 1) - 1, j.causal, j.window).lo, j.sinks, 1);
+        held = held_by(q, j, 1);
         T -= held.shift;
         if ((int32_t)blockIdx.x >= parts) {
             fade(j, r, h, held, blockIdx.x - parts, gridDim.x - parts);
@@ -639,7 +644,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, CTAS) kvs_weigh_held_kernel(We
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, i = lane >> 2;
     const int32_t h = blockIdx.y, r = blockIdx.z;
     const Request q = load_request(st, r);
-    const Held held = held_of(seen_by(q, 0, max(q.n, 1) - 1, j.causal, j.window).lo, j.sinks, 1);
+    const Held held = held_by(q, j, 1);
     if ((int32_t)blockIdx.x >= parts) {
         fade(j, r, h, held, blockIdx.x - parts, gridDim.x - parts);
         return;

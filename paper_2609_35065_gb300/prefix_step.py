@@ -11,10 +11,15 @@
    (``kvs_weigh``);
 4. the cache is cut to a budget (``kvs_evict``) and decoding goes on over what was kept.
 
+With ``--session`` the decoder is one for long sessions over pictures: positions on three axes
+(``kvs_append_axes``), a window beside which the first tokens stay visible (``kvs_attend_sinks``,
+``kvs_weigh_sinks``), and blocks that nobody sees any more given back before decoding.
+
 It prints how far B's suffix comes out from a prefill of the whole prompt.
 """
 from __future__ import annotations
 
+import sys
 from dataclasses import dataclass
 
 import numpy as np
@@ -34,6 +39,9 @@ class Config:
     num_blocks: int = 512
     vocab: int = 1000
     dtype: torch.dtype = torch.bfloat16
+    window: int = 0                    # tokens that a token sees; 0: all before it
+    sinks: int = 0                     # first tokens that it sees beside a window
+    axes: tuple = ()                   # rotated pairs of each axis; (): positions are on one
 
 
 class Decoder:
@@ -54,20 +62,27 @@ class Decoder:
         self.cache = torch.zeros(2 * cfg.layers, cfg.num_blocks, cfg.block, H, D, dtype=cfg.dtype, device=device)
         self.geom = (cfg.layers, H, D, 2, cfg.block, cfg.chunk)
         self.planes = [self.cache[p].data_ptr() for p in range(2 * cfg.layers)]
-        turns, scale = kvs.kvs_rope_turns(D, 10000.0)
-        self.rope = kvs.Rope(torch.from_numpy(turns).to(device), D, scale=scale)
+        self.axes = None
+        if cfg.axes:
+            turns, axis, scale = kvs.kvs_rope_axes(cfg.axes, 10000.0)
+            self.axes = kvs.Axes(torch.from_numpy(axis).to(device), len(cfg.axes))
+        else:
+            turns, scale = kvs.kvs_rope_turns(D, 10000.0)
+        self.rope = kvs.Rope(torch.from_numpy(turns).to(device), 2 * len(turns), scale=scale)
 
     def step(self, tables, kv_lens, q_starts=None, total_q=None, max_q=None):
         return kvs.Step(self.geom, self.planes, self.cfg.num_blocks, tables, kv_lens, q_starts, total_q=total_q, max_q=max_q,
                         dtype=kvs.KVS_DTYPE_F16 if self.cfg.dtype == torch.float16 else kvs.KVS_DTYPE_BF16)
 
     def forward(self, step, tokens, positions=None, weights=None):
-        """Logits of the step's new tokens, which are appended to the cache; ``weights`` [layers,
-        requests, KV heads, tokens] are added to."""
+        """Logits of the step's new tokens, which are appended to the cache; ``positions`` [tokens], or [axes,
+        tokens] where there are several; ``weights`` [layers, requests, KV heads, tokens] are added to."""
         cfg = self.cfg
         H, G, D = cfg.kv_heads, cfg.group, cfg.head_dim
         n, s = len(tokens), torch.cuda.current_stream()
-        workspace = torch.empty(kvs.kvs_attend_workspace(step, H * G), dtype=torch.uint8, device=self.device)
+        mask = dict(window=cfg.window, sinks=cfg.sinks)
+        need = kvs.kvs_attend_sinks_workspace(step, H * G, **mask) if cfg.window else kvs.kvs_attend_workspace(step, H * G)
+        workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
         lse = torch.empty(n, H * G, device=self.device)
         x = self.embed[tokens]
         for layer in range(cfg.layers):
@@ -76,13 +91,37 @@ class Decoder:
             q = qkv[:, : H * G * D].view(n, H * G, D)
             k = qkv[:, H * G * D: H * (G + 1) * D].view(n, H, D)
             v = qkv[:, H * (G + 1) * D:].view(n, H, D)
-            kvs.kvs_append(step, layer, q, k, v, None, self.rope, positions, s)
+            if self.axes is None:
+                kvs.kvs_append(step, layer, q, k, v, None, self.rope, positions, s)
+            else:
+                kvs.kvs_append_axes(step, layer, q, k, v, None, self.rope, self.axes, positions, s)
             out = torch.empty(n, H * G, D, dtype=cfg.dtype, device=self.device)
-            kvs.kvs_attend(step, layer, q, out, lse, workspace=workspace, stream=s)
-            if weights is not None:
+            if cfg.window:
+                kvs.kvs_attend_sinks(step, layer, q, out, lse, workspace=workspace, stream=s, **mask)
+            else:
+                kvs.kvs_attend(step, layer, q, out, lse, workspace=workspace, stream=s)
+            if weights is not None and cfg.window:
+                kvs.kvs_weigh_sinks(step, layer, q, lse, weights[layer], stream=s, **mask)
+            elif weights is not None:
                 kvs.kvs_weigh(step, layer, q, lse, weights[layer], stream=s)
             x = x + out.view(n, -1) @ self.out[layer]
         return x.float() @ self.embed.float().T
+
+
+def prompt_positions(cfg: Config, n: int) -> torch.Tensor:
+    """int32 positions of a prompt's tokens; on several axes every 100 tokens of text are followed by a picture of
+    8 x 12, whose last two axes are a row and a column."""
+    if not cfg.axes:
+        return torch.arange(n, dtype=torch.int32)
+    at, p = torch.empty(len(cfg.axes), n + 200, dtype=torch.int32), 0
+    for start in range(0, n, 196):
+        at[:, start: start + 100] = p + torch.arange(100)
+        k = torch.arange(96)
+        at[:, start + 100: start + 196] = p + 100
+        at[-2, start + 100: start + 196] += k // 12
+        at[-1, start + 100: start + 196] += k % 12
+        p += 112
+    return at[:, :n].contiguous()
 
 
 def run(cfg: Config = Config(), prefix: int = 600, suffix: int = 90, decode: int = 12, budget: int = 320, seed: int = 0) -> dict:
@@ -93,13 +132,14 @@ def run(cfg: Config = Config(), prefix: int = 600, suffix: int = 90, decode: int
     per = -(-(prefix + suffix + 2 * decode) // cfg.block)
     tables = [perm[k * per: (k + 1) * per] for k in range(3)]
     prompt = torch.from_numpy(rng.integers(0, cfg.vocab, prefix + suffix)).to(dev)
+    at = prompt_positions(cfg, prefix + suffix).to(dev)
 
     def one(table, cached, new):
         i32 = dict(dtype=torch.int32, device=dev)
         return model.step(torch.from_numpy(table)[None].to(dev), torch.tensor([cached], **i32), torch.tensor([0, new], **i32), new, new)
 
     # 1: the whole prompt, and its complete chunks to the fast tier
-    whole = model.forward(one(tables[0], prefix + suffix, prefix + suffix), prompt)
+    whole = model.forward(one(tables[0], prefix + suffix, prefix + suffix), prompt, at)
     stored = prefix // cfg.chunk * cfg.chunk
     elems = 2 * cfg.layers * cfg.chunk * cfg.kv_heads * cfg.head_dim
     chunks = [torch.empty(elems, dtype=cfg.dtype, pin_memory=True) for _ in range(stored // cfg.chunk)]
@@ -108,13 +148,19 @@ def run(cfg: Config = Config(), prefix: int = 600, suffix: int = 90, decode: int
     # 2: the prefix into request B's blocks, and the rest of its prompt on top
     kvs.kvs_retrieve(model.geom, model.planes, cfg.num_blocks, [kvs.RequestArg(tables[1], [kvs.ChunkArg(c, cfg.chunk) for c in chunks])])
     rest = len(prompt) - stored
-    logits = model.forward(one(tables[1], len(prompt), rest), prompt[stored:])
+    logits = model.forward(one(tables[1], len(prompt), rest), prompt[stored:], at[..., stored:].contiguous())
 
-    # 3: decoding, with the weight that each cached token receives
-    table, cached = torch.from_numpy(tables[1])[None].to(dev), len(prompt)
+    # 3: decoding, with the weight that each cached token receives; what no token will see is another's by now
+    cached = len(prompt)
+    if cfg.window:
+        block = np.arange(per)
+        gone = (block * cfg.block >= cfg.sinks) & ((block + 1) * cfg.block <= cached + 1 - cfg.window)
+        model.cache[:, tables[1][gone]] = float("nan")
+        tables[1][gone] = -1
+    table = torch.from_numpy(tables[1])[None].to(dev)
     weights = torch.zeros(cfg.layers, 1, cfg.kv_heads, per * cfg.block, device=dev)
     lens = torch.tensor([cached], dtype=torch.int32, device=dev)
-    position = torch.tensor([cached], dtype=torch.int32, device=dev)
+    position = (at[..., -1:] + 1 if cfg.axes else torch.tensor([cached], dtype=torch.int32, device=dev)).contiguous()
     token, tokens = logits[-1:].argmax(-1), []
 
     def decode_some(step, weights):
@@ -130,6 +176,11 @@ def run(cfg: Config = Config(), prefix: int = 600, suffix: int = 90, decode: int
     decode_some(model.step(table, lens), weights)
     lens.sub_(1)
 
+    if cfg.window:
+        kvs.kvs_check_errors()
+        return {"whole": whole[stored:], "suffix": logits, "stored": stored, "tokens": torch.cat(tokens), "kept": None, "weights": weights,
+                "cached": len(prompt) + decode, "gone": int(gone.sum())}
+
     # 4: at most `budget` tokens of every head, in fresh blocks; rotary positions go on
     cut = torch.from_numpy(tables[2])[None].to(dev)
     kept = torch.empty(cfg.layers, 1, cfg.kv_heads, budget, dtype=torch.int32, device=dev)
@@ -143,9 +194,18 @@ def run(cfg: Config = Config(), prefix: int = 600, suffix: int = 90, decode: int
             "cached": len(prompt) + decode}
 
 
+def session() -> Config:
+    """A decoder for long sessions over pictures."""
+    return Config(window=128, sinks=4, axes=(8, 12, 12))
+
+
 def main() -> None:
-    r = run()
+    r = run(session() if "--session" in sys.argv[1:] else Config())
     off = (r["suffix"] - r["whole"]).norm() / r["whole"].norm()
+    if r["kept"] is None:
+        print(f"{r['stored']} tokens retrieved, {len(r['suffix'])} prefilled on top: logits {off:.2%} off those of the whole prompt's prefill; "
+              f"{r['gone']} blocks given back, {len(r['tokens'])} decoded over the rest")
+        return
     print(f"{r['stored']} tokens retrieved, {len(r['suffix'])} prefilled on top: logits {off:.2%} off those of the whole prompt's prefill, "
           f"{(r['suffix'].argmax(-1) == r['whole'].argmax(-1)).float().mean():.0%} of the next tokens the same; "
           f"{len(r['tokens'])} decoded, the cache cut from {r['cached']} to {r['kept'].shape[-1]} tokens on the way")

@@ -272,6 +272,21 @@ def test_weights_of_many_rows(new, G, D):
     _check_weigh(Long([new], [1100], 90, 5, 1, G, D), 0.5)
 
 
+@pytest.mark.parametrize("new", [[0, 1], [0, 20], [0, 150]])
+@pytest.mark.parametrize("decay", [0.0, 0.5, 1.0])
+def test_a_request_without_new_tokens_only_fades(new, decay):
+    """No token sees its cache, of which no block table entry is read."""
+    sm = Long(new, [700, 650], 90, 6, 2, 4, 64)
+    sm.tables[0] = -1
+    step, q, _, _, _cache = sm.on_gpu(kvs)
+    z = _attend(sm, on=(step, q, None, None, _cache))[1]
+    w = torch.rand(2, 2, step.max_kv, device="cuda")
+    before = w.clone()
+    kvs.kvs_weigh_sinks(step, 0, q, z, w, None, decay, True, 90, 6, flags=kvs.KVS_F_VALIDATE)
+    assert torch.equal(w[0, :, :700], before[0, :, :700] * decay)
+    assert torch.equal(w[0, :, 700:], before[0, :, 700:])
+
+
 def test_weights_add_up_to_the_rows():
     sm = Long([3, 150], [700, 650], 90, 6, 2, 4, 128)
     step, q, _, _, _cache = sm.on_gpu(kvs)
@@ -470,3 +485,43 @@ def test_a_step_through_all_operators(new, lens):
     for r, T in enumerate(lens):
         # the sinks and the window are what a step of one token leaves of weight
         assert (kept[0, r].cpu().numpy() == np.r_[:sinks, T - window: T]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_a_long_session_on_a_retrieved_prefix(dtype):
+    """The example's decoder over pictures: a suffix on a retrieved prefix gives what the whole prompt's prefill gives,
+    and decoding goes on over the blocks that are left."""
+    from dataclasses import replace
+
+    from paper_2609_35065_gb300 import prefix_step
+    cfg = replace(prefix_step.session(), dtype=ops_ref.TYPE[dtype])
+    r = prefix_step.run(cfg)
+    # every rounding of the residual stream (4 layers, 3 products each, 8 or 11 bits) may differ once
+    assert (r["suffix"] - r["whole"]).norm() <= 12 * ops_ref.UNIT[dtype] * r["whole"].norm()
+    assert r["stored"] == 512 and len(r["suffix"]) == 178 and r["gone"] > 30
+    T = r["cached"]
+    w = r["weights"]
+    assert torch.isfinite(w).all() and len(r["tokens"]) == 12
+    # each of twelve tokens gives one unit per query head to what it sees: the sinks and a window that moves
+    assert ((w.sum(-1) - 12 * cfg.group).abs() <= 12 * cfg.group * 1e-4).all()
+    first = T - 12 + 1 - cfg.window
+    assert (w[..., cfg.sinks: first] == 0).all() and (w[..., : cfg.sinks] > 0).all() and (w[..., first: T] > 0).all()
+
+
+def test_pictures_positions_tell_the_axes_apart():
+    """The decoder's logits follow a picture's rows and columns: with all axes alike they are others."""
+    from paper_2609_35065_gb300 import prefix_step
+    cfg = prefix_step.Config(axes=(8, 12, 12))
+    a = prefix_step.run(cfg)
+    flat = prefix_step.prompt_positions
+    try:
+        prefix_step.prompt_positions = lambda c, n: flat(prefix_step.Config(), n).expand(3, -1).contiguous()
+        b = prefix_step.run(cfg)
+    finally:
+        prefix_step.prompt_positions = flat
+    c = prefix_step.run(prefix_step.Config())
+    # One axis and three alike are the same model: 4 layers x 3 products, whose roundings of 8 bits may differ once each, are
+    # off by 12 * 2^-8 at most, and logits that are further off are another model's.
+    rounding = 12 * 2.0 ** -8 * c["whole"].norm()
+    assert (b["whole"] - c["whole"]).norm() <= rounding
+    assert (a["whole"] - b["whole"]).norm() > rounding
