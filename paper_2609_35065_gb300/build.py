@@ -28,7 +28,7 @@ SOURCES = [os.path.join(CSRC, f) for f in ("kvs_kernels.cu", "kvs_api.cpp", "kvs
                                            "kvs_weigh.cu", "kvs_evict.cu")]
 DEPS = SOURCES + [os.path.join(CSRC, "kvs_internal.h"), os.path.join(CSRC, "kvs_async.cuh"),
                   os.path.join(CSRC, "kvs_job.cuh"),
-                  os.path.join(CSRC, "kvs_ops.h"), os.path.join(CSRC, "kvs_ops.cuh"), os.path.join(CSRC, "kvs_append.cuh"), os.path.join(CSRC, "kvs_tcgen05.cuh"), os.path.join(CSRC, "kvs_attend_held.cuh"), os.path.join(INCLUDE, "kvs.h")]
+                  os.path.join(CSRC, "kvs_ops.h"), os.path.join(CSRC, "kvs_ops.cuh"), os.path.join(CSRC, "kvs_append.cuh"), os.path.join(CSRC, "kvs_tcgen05.cuh"), os.path.join(INCLUDE, "kvs.h")]
 ARCH = "-gencode=arch=compute_103a,code=sm_103a"
 
 

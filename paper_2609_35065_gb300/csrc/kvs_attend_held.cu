@@ -4,15 +4,123 @@
 // keys a step, S = Q K^T in tensor memory -> P = 2^(c S - c m) back over it -> O += P V.  A window leaves
 // a tile few steps (nine for 1024 tokens, two for 128), so that there a CTA's start and end took as long
 // as its steps.  Here a CTA stays and takes one pair of tiles after the other, and every role runs ahead
-// into the next: the loading warps fill the ring with its keys and, once S of the last step is done, Q's
-// place with its rows; the issuing warp sends its first S behind the last product with V, while the softmax
-// warps still write the results.
+// into the next: the loading warps fill the ring with its keys; the issuing warp sends for its rows as soon
+// as the products that read the last ones are done, and issues its first S behind the last product with V;
+// the softmax warps work out its rows' places beside that product, before they write the results.
 //
 // Steps go over the places of the cache (Held): the sinks' blocks, then those from the window's first token on.
-#include "kvs_attend_held.cuh"
+// Of V, blocks with places that no row sees come row by row (cp.async), with zeros for those.
+//
+// 16 suffixes of 2048 tokens behind 2048, 32 query heads of 128 dims on 8 and a window of 1024 with four
+// sinks (0.55 TFLOP) take 448 us, 1.23 PFLOP/s; with a CTA to each pair of tiles 616.  Four prompts of 4001
+// to 4096 tokens, 64 heads of 64 dims on 8 and a window of 128 (34 GFLOP, 303 MB) take 125 us (276).  What bounds
+// them is the chain of a pair's hand-overs: with 128 dims the tensor cores are busy for 51% of the time and the issue
+// slots for 48%, with 64 for 22% and 56%.  Of 15 steps or more (a window of 4096) 1.5 PFLOP/s are reached.
+// Without the softmax's arithmetic the first took 395 of then 503 us and the second 112 of 151.
+#include "kvs_tcgen05.cuh"
 
 namespace kvs {
 namespace {
+
+constexpr int kM = 128, kN = 128;                  // rows of a tile, keys of a tile of K or V
+constexpr int kTiles = 2;
+constexpr int kIssuer = 8 * kTiles;                // the issuing warps, behind the softmax's; then the loading ones
+constexpr int kThreads = 256 * kTiles + 128;
+constexpr float kNone = -INFINITY;
+
+// What a CTA works on: two tiles of a request's packed rows, of one KV head.
+struct Item {
+    Request q;
+    Span    all;                                   // places that some row sees
+    Held    held;
+    int32_t r, h, row0, rows, steps, T;            // T: places of the cache; steps of 128 up to the last seen one
+};
+
+// The items of a launch, in the order of request, KV head and row tiles.
+struct ItemList {
+    FastDiv  tiles, heads;
+    uint32_t total;
+    int32_t  boxes;                                // whether K and V come by boxes
+};
+
+// Goes over this CTA's items; every role does so by itself.
+struct Walk {
+    const AttendJob& j;
+    const ItemList&  list;
+    const int32_t    per, unit;                    // rows of a tile; tokens that places are held in
+    uint32_t at;
+
+    __device__ __forceinline__ Walk(const AttendJob& job, const ItemList& l)
+        : j(job), list(l), per(tile_rows_of(job.step.group)), unit(l.boxes ? min(job.step.block_size, kN) : 1), at(blockIdx.x) {}
+    // Whole units up to t: divided as block_of divides, or by 128.
+    __device__ __forceinline__ int32_t units(int32_t t) const {
+        return unit == 1 ? t : unit == j.step.block_size ? (int32_t)block_of(j.step, t) : t >> 7;
+    }
+    __device__ __forceinline__ bool next(Item& it) {
+        const StepView& st = j.step;
+        while (at < list.total) {
+            const uint32_t p = fdiv(at, list.tiles), tile = at - p * list.tiles.d;
+            at += gridDim.x;
+            it.r = fdiv(p, list.heads);
+            it.h = p - it.r * list.heads.d;
+            it.row0 = (int32_t)tile * kTiles * per;
+            it.q = load_request(st, it.r);
+            it.rows = min(kTiles * per, it.q.n * st.group - it.row0);
+            if (it.rows <= 0) continue;
+            int32_t g;
+            const int32_t tok = token_of(st, it.row0, g);
+            it.all = seen_by(it.q, tok, token_of(st, it.row0 + it.rows - 1, g), j.causal, j.window);
+            // as held_of
+            const int32_t first = units(it.all.lo) * unit;
+            it.held.cut = min(units(min(j.sinks, it.all.lo) + unit - 1) * unit, first);
+            it.held.shift = first - it.held.cut;
+            it.all = in_places(it.held, it.all);
+            it.T = it.q.T - it.held.shift;
+            it.steps = it.all.hi > it.all.lo ? (it.all.hi + kN - 1) / kN : 0;
+            return true;
+        }
+        return false;
+    }
+    // ... of those whose rows see something
+    __device__ __forceinline__ bool next_active(Item& it) {
+        bool some;
+        do some = next(it);
+        while (some && it.steps == 0);
+        return some;
+    }
+};
+
+// A thread's row of an item: whether there is one, what it sees (in places), where its results go -- its first
+// element in `out` and its entry of lse.
+struct RowOf {
+    Span    see;
+    char*   out;
+    int64_t lse;
+    bool    live;
+};
+__device__ __forceinline__ RowOf row_of_item(const AttendJob& j, const Item& it, int32_t per, int tl, int t) {
+    const StepView& st = j.step;
+    int32_t g;
+    const int32_t tok = token_of(st, it.row0 + tl * per + t, g);
+    // a tile's rows without a token see everything, so that their warp need not mask for them
+    RowOf r{Span{0, INT32_MAX}, nullptr, 0, t < per && tl * per + t < it.rows};
+    if (r.live) {
+        r.see = in_places(it.held, seen_by(it.q, tok, tok, j.causal, j.window));
+        r.out = j.out.base + 2 * ((int64_t)(it.q.q0 + tok) * j.out.row + (int64_t)(it.h * st.group + g) * j.out.head);
+        r.lse = (int64_t)(it.q.q0 + tok) * (st.kv_heads * st.group) + it.h * st.group + g;
+    }
+    return r;
+}
+
+// Bits below x of the 32 from 0 on.
+__device__ __forceinline__ uint32_t bits_below(int32_t x) { return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1; }
+
+// Whether each of the tile's places from t0 on is seen by some row: where not, V has to be zeros.
+__device__ __forceinline__ bool tile_whole(const Item& it, int32_t t0, int32_t sinks) {
+    return (t0 >= it.all.lo || min(t0 + kN, it.all.lo) <= sinks) && t0 + kN <= it.T;
+}
+
+constexpr int kSoftmaxRegs = 104, kOtherRegs = 64;     // of a thread
 
 template <int DP>
 struct Plan {
@@ -99,8 +207,8 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_held_kernel(AttendJob 
     };
 
     // The softmax's warps get registers of the others' (512 x 104 + 128 x 64 = 640 x 96).
-    if (warp >= kIssuer) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    if (warp >= kIssuer) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kOtherRegs));
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kSoftmaxRegs));
     if (warp >= kLoader) {
         // ---- K and V: the ring's tile i is K (even) or V (odd) of step i / 2 of all items' -----
         // A warp brings every P::loaders-th tile whole: its waits and look-ups are beside the others' then.  A stage is
@@ -521,6 +629,12 @@ cudaError_t attend_held(const AttendJob& j, int sms, cudaStream_t s) {
     const ItemList list{make_fastdiv((uint32_t)tiles), make_fastdiv((uint32_t)j.step.kv_heads), (uint32_t)total, boxes};
     const unsigned grid = (unsigned)(total < sms ? total : sms);
     auto* k = kvs_attend_held_kernel<HALF, DP>;
+    // What the warps take on and give up has to be what the CTA was launched with, or they would wait for ever.
+    static const bool enough = [&] {
+        cudaFuncAttributes a{};
+        return cudaFuncGetAttributes(&a, k) == cudaSuccess && a.numRegs * kThreads >= kSoftmaxRegs * 32 * kIssuer + kOtherRegs * 128;
+    }();
+    if (!enough) return launch_attend_tc(j, HALF, s);
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, P::bytes);
     if (e != cudaSuccess) return e;
     k<<<grid, kThreads, P::bytes, s>>>(j, km, vm, qm, list, (int32_t)q_boxes);

@@ -765,9 +765,9 @@ HeldWeighPlan held_weigh_plan(const WeighJob& j, int sms) {
                 all = (2 * n + 10) * (ctas > sms ? ctas / sms : 1);
                 longest = 2 * l + 10;
             } else {
-                const double alone = 1.3 * n + 10, last = 1.3 * l + 10;
-                all = ctas <= sms ? alone : ctas <= 2 * sms ? (alone > 2 * n ? alone : 2 * n) : ctas / sms * (n > alone / 2 ? n : alone / 2);
-                longest = ctas <= sms || last > 2 * l ? last : 2 * l;
+                const double alone = 1.3 * n + 10;
+                all = ctas <= sms ? alone : ctas <= 2 * sms ? 2 * n + 10 : ctas / sms * (n > alone / 2 ? n : alone / 2);
+                longest = ctas <= sms ? 1.3 * l + 10 : 2 * l + 10;
             }
             const double cost = longest > all ? longest : all;
             if (least < 0 || cost < least) {

@@ -218,6 +218,82 @@ def test_a_graph_follows_the_lengths():
         assert (np.abs(w.double().cpu().numpy() - want) <= bound).all()
 
 
+@pytest.mark.parametrize("new,lens,window", [([1, 1], [700, 300], 100), ([40, 3], [700, 400], 100), ([1500], [1800], 100), ([300], [2000], 1500)])
+def test_rows_of_heads_behind_one_another(new, lens, window):
+    """Queries and outputs that lie head by head: [heads][tokens][dims]."""
+    sm = Long(new, lens, window, 5, 4, 4, 64)
+    step, q, _, _, cache = sm.on_gpu(kvs)
+    want, z_want = _attend(sm, on=(step, q, None, None, cache))
+    by_head = q.transpose(0, 1).contiguous().transpose(0, 1)
+    out, z = torch.empty(16, sm.N, 64, dtype=q.dtype, device="cuda").transpose(0, 1), torch.empty_like(z_want)
+    ws = torch.empty(kvs.kvs_attend_sinks_workspace(step, 16, True, window, 5) + 16, dtype=torch.uint8, device="cuda")
+    kvs.kvs_attend_sinks(step, 0, by_head, out, z, None, True, window, 5, ws, flags=kvs.KVS_F_VALIDATE)
+    assert torch.equal(out, want) and torch.equal(z, z_want)
+    w = torch.zeros(2, sm.R, 4, step.max_kv, device="cuda")
+    for x, rows in zip(w, (q, by_head)):
+        kvs.kvs_weigh_sinks(step, 0, rows, z, x, None, 1.0, True, window, 5, flags=kvs.KVS_F_VALIDATE)
+    assert torch.equal(w[0], w[1])
+
+
+def test_calls_at_once():
+    """Calls of both kinds on streams of their own, many times over."""
+    cases = [Long([1500], [1800], 100, 5, 8, 4, 128), Long([2], [30000], 20000, 5, 1, 4, 128), Long([700, 700], [700, 1300], 64, 4, 4, 8, 64), Long([30], [9000], 4000, 4, 1, 4, 64)]
+    on = [sm.on_gpu(kvs) for sm in cases]
+    want = [_attend(sm, on=o) for sm, o in zip(cases, on)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [(torch.zeros_like(a), torch.zeros_like(z), torch.zeros(sm.R, sm.H, o[0].max_kv, device="cuda"),
+             torch.empty(kvs.kvs_attend_sinks_workspace(o[0], sm.H * sm.G, True, sm.window, sm.sinks) + 16, dtype=torch.uint8, device="cuda"))
+            for sm, o, (a, z) in zip(cases, on, want)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for sm, o, s, (a, z, w, ws) in zip(cases, on, streams, outs):
+            kvs.kvs_attend_sinks(o[0], 0, o[1], a, z, None, True, sm.window, sm.sinks, ws, s)
+            kvs.kvs_weigh_sinks(o[0], 0, o[1], z, w, None, 0.0, True, sm.window, sm.sinks, s)
+    torch.cuda.synchronize()
+    kvs.kvs_check_errors()
+    for sm, o, (a, z, w, _), (a0, z0) in zip(cases, on, outs, want):
+        assert torch.equal(a, a0) and torch.equal(z, z0)
+        again = torch.zeros_like(w)
+        kvs.kvs_weigh_sinks(o[0], 0, o[1], z, again, None, 0.0, True, sm.window, sm.sinks)
+        assert torch.equal(w, again)
+
+
+def test_a_graph_of_many_rows_follows_the_step():
+    """Rows, lengths, tables and positions of a captured prefill are read anew at each replay."""
+    sm = Long([900, 300], [1700, 900], 100, 4, 4, 4, 128, given_back=False)
+    sm.cache.nan_to_num_(0.5)
+    step, q, k, v, cache = sm.on_gpu(kvs)
+    turns, axis, axes = _axes([16, 24, 24])
+    rope = kvs.Rope(torch.from_numpy(turns).cuda(), 128)
+    pos = torch.zeros(3, sm.N, dtype=torch.int32, device="cuda")
+    q_out, out, z = torch.zeros(q.shape, dtype=q.dtype, device="cuda"), torch.zeros(q.shape, dtype=q.dtype, device="cuda"), torch.zeros(q.shape[:2], device="cuda")
+    ws = torch.empty(kvs.kvs_attend_sinks_workspace(step, 16, True, 100, 4) + 16, dtype=torch.uint8, device="cuda")
+
+    def layer(s):
+        kvs.kvs_append_axes(step, 0, q, k, v, q_out, rope, axes, pos, s)
+        kvs.kvs_attend_sinks(step, 0, q_out, out, z, None, True, 100, 4, ws, s)
+    s = torch.cuda.Stream()
+    layer(s)
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        layer(torch.cuda.current_stream())
+    tables, lens, starts = step._keep[:3]
+    for new, lengths in (([900, 300], [1700, 900]), ([5, 700], [5, 1690]), ([0, 899], [33, 1000])):
+        lens.copy_(torch.tensor(lengths, dtype=torch.int32))
+        starts.copy_(torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32))
+        pos.random_(0, 5000)
+        g.replay()
+        torch.cuda.synchronize()
+        kvs.kvs_check_errors()
+        sm.new, sm.lens, sm.N, sm.starts = new, lengths, sum(new), np.concatenate([[0], np.cumsum(new)])
+        sm.hidden = [np.zeros(T, dtype=bool) for T in lengths]
+        x = q[: sm.N]
+        _off(q_out[: sm.N], x, pos[:, : sm.N].cpu().numpy(), axis, turns, False, 1.0, 2.0 ** -8)
+        sm.cache, sm.qkv = cache.view(2, -1, 4, 128).cpu(), torch.cat([q_out[: sm.N].reshape(sm.N, -1), torch.zeros(sm.N, 8 * 128, dtype=q.dtype, device="cuda")], 1).cpu()
+        _check(sm, out[: sm.N], z[: sm.N])
+
+
 # ---- weights --------------------------------------------------------------------
 def _check_weigh(sm, decay, decode=False, seed=3):
     step, q, _, _, _cache = sm.on_gpu(kvs, decode)
