@@ -186,6 +186,11 @@ __device__ __forceinline__ void tile_rows(uint32_t dst, const char* plane, const
     }
 }
 
+// Adds `bytes` to the phase's expected transaction count; the arrival is still to come.
+__device__ __forceinline__ void mbar_expect_more(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+
 // A tile of V by boxes, and by rows with cp.async where a box holds places that no row sees: those become zeros.
 // A warp brings the boxes that are its own either way; its arrival on `bar` has to follow.
 template <int DP>
