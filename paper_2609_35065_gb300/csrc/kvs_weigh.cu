@@ -738,42 +738,31 @@ int64_t box_tokens(const StepView& st) { return 128 % st.block_size == 0 ? st.bl
 // CTAs that let tokens fade: one for 16384 of a head.
 int64_t fading_of(const WeighJob& j) { return j.decay == 1.0f ? 0 : (j.step.max_kv + 16383) / 16384; }
 
-// How the tensor cores' kernel goes about a window with sinks: key tiles of a CTA, and the CTAs that
-// share a key tile's rows.  Only rows within the window see a key tile, so that a CTA has few row
-// tiles and its start counts; the sinks' CTAs, which have all rows, are the longest.  Measured, in units of
-// 0.65 us: a row tile takes a key tile 1.3 where a CTA has an SM to itself, and 1 of the SM's time
-// where two share it or a CTA has two key tiles; the start and end of a CTA take 10, which the other
-// one's work covers.  8 KV heads of 128 dims, 5 query heads each: 1024 new tokens and a window as long, one key
-// tile to a CTA, 45 us with one CTA to it, 34 with two, 27 with four and 41 with eight (two key tiles: 67, 38,
-// 32, 57); 2048 and a window of 128 85, 48, 30, 42; 4 x 1500 and 600 72, 75, 102, 157; 8 x 100 and 1024 21, 33, 57, 119.
-struct HeldWeighPlan {
-    int key_tiles, share;
-};
-HeldWeighPlan held_weigh_plan(const WeighJob& j, int sms) {
+// The CTAs of the tensor cores' kernel that share a key tile's rows, under a window with sinks.  Only rows
+// within the window see a key tile, so that a CTA has few row tiles and its start counts; the sinks' CTAs,
+// which have all rows, are the longest.  Measured, in units of 0.65 us: a row tile takes 1.3 where a CTA
+// has an SM to itself, and 1 of the SM's time where two share it, 1.7 of a long CTA's while shorter ones come and
+// go; the start and end of a CTA take 10, which the other one's work covers.  Clusters of eight wait for eight places
+// at once.  8 KV heads of 128 dims, 5 query heads each: 1024 new tokens and a window as long 45 us with one CTA
+// to a key tile, 34 with two, 27 with four and 41 with eight; 2048 and a window of 128 86, 48, 30, 42; 4 x 1500
+// and 600 72, 75, 102, 157; 8 x 100 and 1024 21, 33, 57, 119; one head of 72 dims, 2 x 288 and 23 17, 13, 9.4, 8.6.
+// Two key tiles to a CTA, as kvs_weigh has them for many rows, took 67, 38, 32 and 57 for the first, and gained
+// nothing on any of thirty other calls.
+int held_weigh_share(const WeighJob& j, int sms) {
     const StepView& st = j.step;
     const int64_t per = tile_rows_of(st.group), pairs = (int64_t)st.kv_heads * st.requests;
     auto tiles_of = [&](int64_t tokens) { return ((tokens < st.max_q ? tokens : st.max_q) * st.group + per - 1) / per; };
-    HeldWeighPlan best{1, 1};
+    const int64_t tiles = (places_of(j, box_tokens(st)) + 127) / 128 * pairs, most = tiles_of(st.max_q), usual = tiles_of((int64_t)j.window + 128);
+    int best = 1;
     double least = -1.0;
-    for (int kt = 1; kt <= 2; ++kt) {
-        const int64_t keys = 128 * kt, tiles = (places_of(j, box_tokens(st)) + keys - 1) / keys * pairs;
-        const int64_t most = tiles_of(st.max_q), usual = tiles_of(j.window + keys);
-        for (int share = 1; share <= 8 && share <= most; share *= 2) {
-            const double ctas = (double)(tiles * share), n = (double)((usual + share - 1) / share), l = (double)((most + share - 1) / share);
-            double all, longest;
-            if (kt == 2) {
-                all = (2 * n + 10) * (ctas > sms ? ctas / sms : 1);
-                longest = 2 * l + 10;
-            } else {
-                const double alone = 1.3 * n + 10;
-                all = ctas <= sms ? alone : ctas <= 2 * sms ? 2 * n + 10 : ctas / sms * (n > alone / 2 ? n : alone / 2);
-                longest = ctas <= sms ? 1.3 * l + 10 : 2 * l + 10;
-            }
-            const double cost = longest > all ? longest : all;
-            if (least < 0 || cost < least) {
-                least = cost;
-                best = HeldWeighPlan{kt, share};
-            }
+    for (int share = 1; share <= 8 && share <= most; share *= 2) {
+        const double ctas = (double)(tiles * share), n = (double)((usual + share - 1) / share), l = (double)((most + share - 1) / share);
+        const double alone = 1.3 * n + 10, longest = (ctas <= sms ? 1.3 : 1.7) * l + 10;
+        const double all = ctas <= sms ? alone : ctas <= 2 * sms ? 2 * n + 10 : ctas / sms * (n > alone / 2 ? n : alone / 2) * (share == 8 ? 1.35 : 1);
+        const double cost = longest > all ? longest : all;
+        if (least < 0 || cost < least) {
+            least = cost;
+            best = share;
         }
     }
     return best;
@@ -850,10 +839,7 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
         }
         return cudaGetLastError();
     }
-    if (HELD) {
-        const HeldWeighPlan plan = held_weigh_plan(j, sms);
-        return plan.key_tiles == 1 ? weigh_tc<HALF, DP, 1, HELD>(j, sms, plan.share, s) : weigh_tc<HALF, DP, 2, HELD>(j, sms, plan.share, s);
-    }
+    if constexpr (HELD) return weigh_tc<HALF, DP, 1, HELD>(j, sms, held_weigh_share(j, sms), s);
     // One key tile to a CTA up to 2560 rows: against 8000 tokens of 8 requests x 8 heads of 128 dims 64 rows
     // take 72 us (two tiles: 92), 256 79 (99), 1024 149 (167), 2048 250 (261), 4096 467 (450).
     return rows <= 2560 ? weigh_tc<HALF, DP, 1, HELD>(j, sms, 1, s) : weigh_tc<HALF, DP, 2, HELD>(j, sms, 1, s);
