@@ -5,16 +5,20 @@ binding's marshalling extension beside it.
 ``paper_2609_35065_gb300/_build/`` (git-ignored) and are rebuilt when a source or the
 public header is newer.  The extension is optional: where it cannot be built or loaded (no
 Python headers, no C compiler, a folder that cannot be written) the binding marshals with
-numpy and ctypes, after a warning.
+numpy and ctypes, after a warning.  So is the reader of tensors beside it, which is compiled against the
+headers of the installed torch; without it tensors are read by their attributes.
 """
 from __future__ import annotations
 
+import importlib.metadata
 import importlib.util
 import os
+import re
 import shutil
 import subprocess
 import sys
 import sysconfig
+import threading
 import warnings
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -34,6 +38,16 @@ ARCH = "-gencode=arch=compute_103a,code=sm_103a"
 
 PYCALL_SOURCE = os.path.join(CSRC, "kvs_pycall.c")
 PYCALL = os.path.join(OUT_DIR, "kvs_pycall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
+
+
+TENSOR_SOURCE = os.path.join(CSRC, "kvs_tensor.cpp")
+TENSOR_HEADER = os.path.join(CSRC, "kvs_tensor.h")
+
+
+def tensor_reader() -> str:
+    """The reader's file, named after the installed torch: another one's is not loaded."""
+    version = re.sub(r"\W", "_", importlib.metadata.version("torch"))
+    return os.path.join(OUT_DIR, f"kvs_tensor_{version}" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 
 def _has_python_headers() -> bool:
@@ -60,6 +74,17 @@ def pycall_command(out: str = PYCALL) -> list[str]:
             PYCALL_SOURCE, "-o", out]
 
 
+def tensor_command(out: str) -> list[str]:
+    cxx = shutil.which("g++") or shutil.which("c++")
+    torch = importlib.util.find_spec("torch")
+    if cxx is None or torch is None:
+        raise RuntimeError("a C++ compiler and torch are required to build the reader of tensors")
+    at = torch.submodule_search_locations[0]
+    return [cxx, "-O2", "-std=c++17", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"],
+            "-isystem", os.path.join(at, "include"), "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+            TENSOR_SOURCE, "-o", out, "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+
+
 def _older(out: str, deps) -> bool:
     if not os.path.exists(out):
         return True
@@ -72,7 +97,7 @@ def stale(out: str = LIB) -> bool:
 
 
 def pycall_stale() -> bool:
-    return _older(PYCALL, [PYCALL_SOURCE, os.path.join(INCLUDE, "kvs.h")])
+    return _older(PYCALL, [PYCALL_SOURCE, TENSOR_HEADER, os.path.join(INCLUDE, "kvs.h")])
 
 
 def _usable_pycall(force: bool = False, verbose: bool = False) -> bool:
@@ -105,26 +130,62 @@ def load_pycall():
     return mod.call
 
 
-def build_pycall(verbose: bool = False) -> None:
-    os.makedirs(OUT_DIR, exist_ok=True)
-    tmp = PYCALL + f".{os.getpid()}.tmp"
-    cmd = pycall_command(tmp)
+def load_tensor_reader() -> int:
+    """Address of the reader of tensors, built now if need be; 0 where it cannot be built or loaded.
+    torch must have been imported."""
+    try:
+        path = tensor_reader()
+        if _older(path, [TENSOR_SOURCE, TENSOR_HEADER]):
+            build_tensor_reader()
+        spec = importlib.util.spec_from_file_location("kvs_tensor", path)
+        mod = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(mod)
+    except (ImportError, OSError, RuntimeError, subprocess.SubprocessError) as e:
+        warnings.warn(f"the reader of tensors cannot be built or loaded, their attributes are read: {e}", RuntimeWarning, stacklevel=2)
+        return 0
+    return mod.reader
+
+
+def _compile(cmd: list[str], tmp: str, out: str, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), file=sys.stderr)
     subprocess.run(cmd, check=True)
-    os.replace(tmp, PYCALL)
+    os.replace(tmp, out)
+
+
+def build_pycall(verbose: bool = False) -> None:
+    os.makedirs(OUT_DIR, exist_ok=True)
+    tmp = PYCALL + f".{os.getpid()}.tmp"
+    _compile(pycall_command(tmp), tmp, PYCALL, verbose)
+
+
+def build_tensor_reader(verbose: bool = False) -> None:
+    os.makedirs(OUT_DIR, exist_ok=True)
+    out = tensor_reader()
+    tmp = out + f".{os.getpid()}.tmp"
+    _compile(tensor_command(tmp), tmp, out, verbose)
+
+
+def _try_tensor_reader(force: bool, verbose: bool) -> None:
+    """The reader, beside the library: what fails here is said when it is loaded."""
+    try:
+        if _has_python_headers() and (force or _older(tensor_reader(), [TENSOR_SOURCE, TENSOR_HEADER])):
+            build_tensor_reader(verbose)
+    except (ImportError, OSError, RuntimeError, subprocess.SubprocessError):
+        pass
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
     os.makedirs(OUT_DIR, exist_ok=True)
     _usable_pycall(force, verbose)
-    if force or stale():
-        tmp = LIB + f".{os.getpid()}.tmp"
-        cmd = command(tmp)
-        if verbose:
-            print(" ".join(cmd), file=sys.stderr)
-        subprocess.run(cmd, check=True)
-        os.replace(tmp, LIB)
+    beside = threading.Thread(target=_try_tensor_reader, args=(force, verbose))
+    beside.start()
+    try:
+        if force or stale():
+            tmp = LIB + f".{os.getpid()}.tmp"
+            _compile(command(tmp), tmp, LIB, verbose)
+    finally:
+        beside.join()
     return LIB
 
 

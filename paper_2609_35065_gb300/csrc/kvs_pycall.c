@@ -11,7 +11,8 @@
  * call; this takes about 1 us and 25 us.
  *
  * append, attend, weigh (and their forms with axes and sinks) and evict do the same for the model operators' tensors: whatever is not
- * plainly right (a type, a shape, a stride) is left to the binding, which says what is wrong.
+ * plainly right (a type, a shape, a stride) is left to the binding, which says what is wrong.  Tensors are read
+ * by their attributes, or by the reader that use_reader() was given.
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -21,6 +22,7 @@
 #include <string.h>
 
 #include "kvs.h"
+#include "kvs_tensor.h"
 
 static PyObject *s_data_ptr, *s_block_table, *s_chunks, *s_first_token, *s_num_tokens, *s_base, *s_residency;
 
@@ -291,13 +293,28 @@ static int int_tuple(PyObject* o, int n, int64_t* out) {
     return 1;
 }
 
-typedef struct {
-    uint64_t at;
-    int64_t  shape[4], stride[4];
-} Tensor;
+typedef kvs_tensor Tensor;
+
+static kvs_read_tensor_fn reader = NULL;                     /* reads a plain tensor without its attributes, where there is one */
+
+/* use_reader(address of a kvs_read_tensor_fn, 0 for none) */
+static PyObject* use_reader(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
+    (void)self;
+    int64_t x;
+    if (nv != 1 || !small_int(v[0], 0, INT64_MAX, &x)) {
+        PyErr_SetString(PyExc_TypeError, "use_reader takes an address");
+        return NULL;
+    }
+    reader = (kvs_read_tensor_fn)(uintptr_t)x;
+    Py_RETURN_NONE;
+}
 
 /* A tensor of `dims` dimensions and of that dtype: 1, 0 (something else), -1 (exception). */
 static int read_tensor(PyObject* o, PyObject* dtype, int dims, Tensor* t) {
+    if (reader) {
+        const int got = reader(o, dtype, dims, t);
+        if (got != 2) return got;
+    }
     PyObject* x = PyObject_GetAttr(o, s_dtype);
     int ok = x == dtype;
     Py_XDECREF(x);
@@ -693,7 +710,7 @@ static PyObject* evict(PyObject* self, PyObject* const* v, Py_ssize_t nv) {
 
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(call), METHOD(append), METHOD(append_axes), METHOD(attend), METHOD(attend_sinks),
-                                METHOD(weigh), METHOD(weigh_sinks), METHOD(evict), {NULL, NULL, 0, NULL}};
+                                METHOD(weigh), METHOD(weigh_sinks), METHOD(evict), METHOD(use_reader), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "kvs_pycall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit_kvs_pycall(void) {

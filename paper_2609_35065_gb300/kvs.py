@@ -660,6 +660,21 @@ class Step:
         self.byte = torch.uint8
         self.scale = self.geom.head_dim ** -0.5
         lib()
+        _use_reader()
+
+
+_reader = None               # address of the reader of tensors, 0: there is none
+
+
+def _use_reader() -> None:
+    """Has the extension read tensors by the reader compiled for the installed torch."""
+    global _reader
+    if _reader is None and _ops is not None:
+        with _lock:
+            if _reader is None:
+                address = _build.load_tensor_reader()
+                _ops.use_reader(address)
+                _reader = address
 
 
 def _int32_tensor(name, t, dims):
