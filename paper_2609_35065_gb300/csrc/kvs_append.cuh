@@ -28,6 +28,7 @@ struct Place {
 };
 
 // Request of row n: the last one that starts at or before it.
+template <bool LATE = false>
 __device__ __forceinline__ Place place_of(const AppendJob& j, int32_t n) {
     const StepView& st = j.step;
     Place pl;
@@ -38,25 +39,26 @@ __device__ __forceinline__ Place place_of(const AppendJob& j, int32_t n) {
         int32_t lo = 0, hi = st.requests;            // q_starts[lo] <= n < q_starts[hi], if they are in order
         while (hi - lo > 1) {
             const int32_t mid = (lo + hi) >> 1;
-            if (__ldg(st.q_starts + mid) <= n) lo = mid;
+            if (load_of<LATE>(st.q_starts + mid) <= n) lo = mid;
             else hi = mid;
         }
         r = lo;
     }
-    const Request q = load_request(st, r);
+    const Request q = load_request<LATE>(st, r);
     const int32_t t = q.T - q.n + (n - q.q0);
     pl.owned = n >= q.q0 && n < q.q0 + q.n;
-    if (pl.owned && t >= 0) pl.row = row_of(st, st.tables + (int64_t)r * st.table_stride, t);
-    pl.pos = j.positions ? __ldg(j.positions + n) : max(t, 0);
+    if (pl.owned && t >= 0) pl.row = row_of<LATE>(st, st.tables + (int64_t)r * st.table_stride, t);
+    pl.pos = j.positions ? load_of<LATE>(j.positions + n) : max(t, 0);
     return pl;
 }
 
 // A request out of bounds may have no row that leads to it (its range falls, or is empty): the
 // grid has warps behind the rows' own that look at 32 requests each (looking behind their own work,
 // the rows' warps took 1.5% longer).
+template <bool LATE = false>
 __device__ __forceinline__ void check_requests(const StepView& st, uint32_t group) {
     const uint32_t r = 32 * group + (threadIdx.x & 31);
-    if (st.q_starts && r < (uint32_t)st.requests) load_request(st, r);
+    if (st.q_starts && r < (uint32_t)st.requests) load_request<LATE>(st, r);
 }
 inline uint32_t warps_of(const StepView& st, int64_t row_warps) { return (uint32_t)(row_warps + (st.q_starts ? (st.requests + 31) / 32 : 0)); }
 

@@ -53,7 +53,7 @@ __device__ __forceinline__ int32_t request_of(const StepView& st, int32_t n, int
     int32_t lo = 0, hi = st.requests;                // q_starts[lo] <= n < q_starts[hi], if they are in order
     while (hi - lo > 1) {
         const int32_t step = (hi - lo + 31) / 32, at = lo + step * lane;
-        const uint32_t behind = __ballot_sync(0xffffffffu, lane > 0 && (at >= hi || __ldg(st.q_starts + at) > n));
+        const uint32_t behind = __ballot_sync(0xffffffffu, lane > 0 && (at >= hi || st.q_starts[at] > n));
         const int32_t some = behind ? __ffs(behind) - 1 : 32;
         hi = min(hi, lo + step * some);
         lo += step * (some - 1);
@@ -67,10 +67,11 @@ __device__ __forceinline__ int32_t request_of(const StepView& st, int32_t n, int
 // a decode step of 16 tokens 3.8 us in a graph.
 template <bool HALF, bool PAIRS>
 __global__ void __launch_bounds__(256) kvs_append_axes_kernel(AppendJob j, uint32_t warps_per_token, int32_t groups) {
+    grid_wait();
     const uint32_t w = blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5);       // at most 2^31 + 2^11 of them are needed
     const uint32_t own = (uint32_t)j.step.total_q * warps_per_token;
     if (w >= own) {
-        check_requests(j.step, w - own);
+        check_requests<true>(j.step, w - own);
         return;
     }
     using N = Num<HALF>;
@@ -79,8 +80,8 @@ __global__ void __launch_bounds__(256) kvs_append_axes_kernel(AppendJob j, uint3
     const int lane = threadIdx.x & 31;
     Where where;
 #pragma unroll
-    for (int a = 0; a < kAxes; ++a) where.at[a] = a < j.axes ? __ldg(j.positions + a * j.axis_stride + n) : 0;
-    const Place pl = place_of(j, n);
+    for (int a = 0; a < kAxes; ++a) where.at[a] = a < j.axes ? j.positions[a * j.axis_stride + n] : 0;
+    const Place pl = place_of<true>(j, n);
     if (!pl.owned) return;
     const int32_t D = j.step.head_dim, rot = j.rot_dim, H = j.step.kv_heads;
     const int32_t lanes = min(32, groups), heads_at_once = 32 / lanes;
@@ -109,7 +110,7 @@ __global__ void __launch_bounds__(256) kvs_append_axes_kernel(AppendJob j, uint3
             const int32_t pair = (PAIRS ? e0 / 2 : e0) + k;
             c[k] = 1.0f;
             s[k] = 0.0f;
-            if (turned && pair < rot / 2) turn(where.on(j, __ldg(j.axis + pair)), __ldg(j.turns + pair), j.scale, c[k], s[k]);
+            if (turned && pair < rot / 2) turn(where.on(j, j.axis[pair]), j.turns[pair], j.scale, c[k], s[k]);
         }
         for (int32_t h0 = first; h0 < total; h0 += kAtOnce * step) {
             Piece<W> a[kAtOnce], b[kAtOnce];
@@ -165,10 +166,11 @@ constexpr int kWarps = 8;
 template <bool HALF, int W>
 __global__ void __launch_bounds__(32 * kWarps) kvs_append_axes_staged_kernel(AppendJob j, uint32_t warps_per_token, int32_t chunk, uint32_t vec_m) {
     extern __shared__ __align__(16) char staged[];
+    grid_wait();
     const uint32_t w = blockIdx.x * kWarps + (threadIdx.x >> 5);
     const uint32_t all = (uint32_t)j.step.total_q * warps_per_token;
     if (w >= all) {
-        check_requests(j.step, w - all);
+        check_requests<true>(j.step, w - all);
         return;
     }
     using N = Num<HALF>;
@@ -177,7 +179,7 @@ __global__ void __launch_bounds__(32 * kWarps) kvs_append_axes_staged_kernel(App
     const int lane = threadIdx.x & 31;
     Where where;
 #pragma unroll
-    for (int a = 0; a < kAxes; ++a) where.at[a] = a < j.axes ? __ldg(j.positions + a * j.axis_stride + n) : 0;
+    for (int a = 0; a < kAxes; ++a) where.at[a] = a < j.axes ? j.positions[a * j.axis_stride + n] : 0;
     const int32_t D = j.step.head_dim, half = j.rot_dim / 2, H = j.step.kv_heads, vecs = D / 8, pieces = half / W;
     const int32_t qh = j.q.base ? j.q_heads : 0, total = qh + 2 * H, step = (int32_t)warps_per_token * chunk;
     char* own = staged + (threadIdx.x >> 5) * chunk * D * 2;
@@ -194,7 +196,7 @@ __global__ void __launch_bounds__(32 * kWarps) kvs_append_axes_staged_kernel(App
     if (part * chunk < total) bring(part * chunk);
     // the row's request, then that one's lengths, with the sines in between, then its block
     const int32_t r = request_of(j.step, n, lane);
-    const RawRequest fetched = fetch_request(j.step, r);
+    const RawRequest fetched = fetch_request<true>(j.step, r);
     // piece c0 % pieces of every at_once-th head is this lane's; of more than 32 pieces (W is 1 then) also c0 + 32
     const int32_t at_once = pieces < 32 ? 32 / pieces : 1;
     float c[2 * V], s[2 * V];
@@ -202,13 +204,13 @@ __global__ void __launch_bounds__(32 * kWarps) kvs_append_axes_staged_kernel(App
         if (c0 >= pieces * at_once) return;
         const int32_t e = W * (c0 % pieces);
 #pragma unroll
-        for (int k = 0; k < W; ++k) turn(where.on(j, __ldg(j.axis + e + k)), __ldg(j.turns + e + k), j.scale, c[k], s[k]);
+        for (int k = 0; k < W; ++k) turn(where.on(j, j.axis[e + k]), j.turns[e + k], j.scale, c[k], s[k]);
     };
     sines(lane);
     const Request q = check_request(j.step, fetched);
     const bool owned = n >= q.q0 && n < q.q0 + q.n;
     const int32_t t = q.T - q.n + (n - q.q0);
-    const int64_t row = owned && t >= 0 ? row_of(j.step, j.step.tables + (int64_t)r * j.step.table_stride, t) : -1;
+    const int64_t row = owned && t >= 0 ? row_of<true>(j.step, j.step.tables + (int64_t)r * j.step.table_stride, t) : -1;
     cp_wait<0>();
     if (!owned) return;
     for (int32_t h0 = part * chunk; h0 < total; h0 += step) {
@@ -263,9 +265,8 @@ cudaError_t append_staged(const AppendJob& j, cudaStream_t s) {
     int parts = (total + 3) / 4;
     while (parts > 1 && rows * parts > 152 * 64) parts = (parts + 1) / 2;
     const int32_t share = (total + parts - 1) / parts, chunk = share < room ? share : room;
-    kvs_append_axes_staged_kernel<HALF, W><<<(warps_of(j.step, rows * parts) + kWarps - 1) / kWarps, 32 * kWarps, kWarps * chunk * D * 2, s>>>(
-        j, parts, chunk, (65536 + vecs - 1) / vecs);
-    return cudaGetLastError();
+    return launch_behind(kvs_append_axes_staged_kernel<HALF, W>, dim3((warps_of(j.step, rows * parts) + kWarps - 1) / kWarps), 32 * kWarps,
+                         kWarps * chunk * D * 2, s, j, parts, chunk, (65536 + vecs - 1) / vecs);
 }
 
 template <bool HALF, bool PAIRS>
@@ -277,8 +278,7 @@ cudaError_t append_axes(const AppendJob& j, cudaStream_t s) {
     const int64_t rows = j.step.total_q;
     int parts = (total + at_once - 1) / at_once;
     while (parts > 1 && rows * parts > 152 * 64) parts = (parts + 1) / 2;
-    kvs_append_axes_kernel<HALF, PAIRS><<<(warps_of(j.step, rows * parts) + 7) / 8, 256, 0, s>>>(j, parts, groups);
-    return cudaGetLastError();
+    return launch_behind(kvs_append_axes_kernel<HALF, PAIRS>, dim3((warps_of(j.step, rows * parts) + 7) / 8), 256, 0, s, j, parts, groups);
 }
 
 template <bool HALF>

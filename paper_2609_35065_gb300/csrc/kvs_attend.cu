@@ -104,8 +104,9 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
     const StepView& st = j.step;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, i8 = lane >> 2;
     const int32_t split = blockIdx.x, r = blockIdx.z, h = blockIdx.y;
+    if (HELD) grid_wait();                                     // HELD: launched behind the kernel before
     if (j.splits > 1 && !j.cluster) grid_trigger();            // the join may come and wait
-    const Request q = load_request(st, r);
+    const Request q = load_request<HELD>(st, r);
     const int32_t rows = q.n * st.group;
     if (rows <= 0) return;
     Span all = seen_by(q, 0, q.n - 1, j.causal, j.window);
@@ -137,7 +138,7 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
     const int32_t mine = (count - warp + WARPS - 1) / WARPS;
     auto look_up = [&](int32_t i) {
         const int32_t t = keys.lo + kKeys * (warp + WARPS * i) + (lane & 15);
-        return i < mine && t < keys.hi ? row_of(st, table, HELD ? token_at(held, t) : t) : (int64_t)-1;
+        return i < mine && t < keys.hi ? row_of<HELD>(st, table, HELD ? token_at(held, t) : t) : (int64_t)-1;
     };
     int64_t mrow = look_up(0);
     auto load = [&](int32_t i) {
@@ -435,12 +436,9 @@ cudaError_t attend_rows(const AttendJob& j, cudaStream_t s) {
     cfg.blockDim = dim3(WARPS * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = j.splits;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
     cfg.attrs = at;
-    cfg.numAttrs = j.cluster;
+    cfg.numAttrs = launch_attributes(at, j.cluster ? j.splits : 1, HELD);
     return cudaLaunchKernelEx(&cfg, k, j);
 }
 

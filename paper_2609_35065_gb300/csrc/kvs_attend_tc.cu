@@ -78,6 +78,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
     using P = Plan<DP, TILES>;
     constexpr int kIssuer = 8 * TILES;               // the issuing warp, behind the softmax's; then the loading ones
     constexpr float kMost = HALF ? 65504.0f : 1048576.0f;            // of a thread's weights of a step (half: of either sum)
+    if (HELD) grid_wait();                           // HELD: launched behind the kernel before
     const StepView& st = j.step;
     const bool cluster = TILES == 1 && j.cluster;    // no cluster joins the parts of two tiles
     const uint32_t base = smem_u32(raw);
@@ -96,7 +97,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
     // The last rows see the most keys: they come first, so that no long CTA starts last.
     const int32_t row0 = (tiles - 1 - (int32_t)(blockIdx.x / j.splits)) * TILES * per;
     // Set-up while the request's lengths are on their way.
-    const RawRequest fetched = fetch_request(st, r);
+    const RawRequest fetched = fetch_request<HELD>(st, r);
     if (warp == kIssuer) tmem_alloc(tmem_at, P::columns);
     if (threadIdx.x == 0) {
         mbar_init(bar.q, q_boxes ? 1 : 256 * TILES);
@@ -143,7 +144,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
     // K's and V's tiles of a step are in the same blocks; the loading warps look the next step's up a step ahead
     Box next{};
-    if (boxes && steps > 0 && warp > kIssuer) next = box_of<DP, kLoaders>(st, table, held, j0 * kN, T, warp - kIssuer - 1, lane);
+    if (boxes && steps > 0 && warp > kIssuer) next = box_of<DP, kLoaders, HELD>(st, table, held, j0 * kN, T, warp - kIssuer - 1, lane);
 
     tc_fence_before();
     __syncthreads();
@@ -176,7 +177,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
             const int stage = i % P::stages;
             if (boxes && !(i & 1)) {
                 box = next;
-                if (i + 2 < 2 * steps) next = box_of<DP, kLoaders>(st, table, held, (j0 + (i >> 1) + 1) * kN, T, w, lane);
+                if (i + 2 < 2 * steps) next = box_of<DP, kLoaders, HELD>(st, table, held, (j0 + (i >> 1) + 1) * kN, T, w, lane);
             }
             if (i >= P::stages) {
                 const bool ok = lane != 0 || wait(bar.free + 8 * stage, (i / P::stages - 1) & 1);
@@ -194,7 +195,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
                 }
                 tile_boxes<DP>(dst, is_v ? &v_map : &k_map, st, h, box, bar.full + 8 * stage, lane);
             } else {
-                tile_rows<DP, 32 * kLoaders>(dst, is_v ? j.v_plane : j.k_plane, st, table, h, held, t0, all.lo, T, HELD ? j.sinks : 0, t);
+                tile_rows<DP, 32 * kLoaders, HELD>(dst, is_v ? j.v_plane : j.k_plane, st, table, h, held, t0, all.lo, T, HELD ? j.sinks : 0, t);
                 cp_commit();
                 if (pending >= 0) {
                     cp_wait<1>();
@@ -621,12 +622,9 @@ cudaError_t attend_tc(const AttendJob& j, cudaStream_t s) {
     cfg.blockDim = dim3(P::threads);
     cfg.dynamicSmemBytes = P::bytes;
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = j.splits;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
     cfg.attrs = at;
-    cfg.numAttrs = j.cluster;
+    cfg.numAttrs = launch_attributes(at, j.cluster ? j.splits : 1, HELD);
     return cudaLaunchKernelEx(&cfg, k, j, km, vm, qm, (int32_t)boxes, (int32_t)q_boxes);
 }
 

@@ -140,7 +140,7 @@ struct Box {
     int32_t block, row, at;                                      // block (num_blocks: reads as zeros), first token in it, token of the tile
 };
 // T and t0 count places (of Held{}: tokens), whose units are boxes.
-template <int DP, int WARPS>
+template <int DP, int WARPS, bool LATE = false>
 __device__ __forceinline__ Box box_of(const StepView& st, const int32_t* table, const Held& held, int32_t t0, int32_t T, int w, int lane) {
     constexpr int HALVES = DP / 64;
     const int32_t size = min(st.block_size, 128), i = (lane / HALVES) * WARPS + w;      // this lane's box of the tile
@@ -148,7 +148,7 @@ __device__ __forceinline__ Box box_of(const StepView& st, const int32_t* table, 
     if (x.at < 128 && t0 + x.at < T) {
         const int32_t tok = token_at(held, t0 + x.at);
         const uint32_t blk = block_of(st, tok);
-        x.block = __ldg(table + blk);
+        x.block = load_of<LATE>(table + blk);
         x.row = tok - blk * st.block_size;
         if ((uint32_t)x.block >= (uint32_t)st.num_blocks) {
             record_error(st.err, KVS_ERR_BOUNDS);
@@ -171,7 +171,7 @@ __device__ __forceinline__ void tile_boxes(uint32_t dst, const CUtensorMap* map,
 }
 // By rows: THREADS threads, of which this is t, with cp.async; places outside [lo, hi) become zeros, but
 // for those below `sinks`.
-template <int DP, int THREADS = 128>
+template <int DP, int THREADS = 128, bool LATE = false>
 __device__ __forceinline__ void tile_rows(uint32_t dst, const char* plane, const StepView& st, const int32_t* table, int32_t h, const Held& held, int32_t t0,
                                           int32_t lo, int32_t hi, int32_t sinks, int t) {
     constexpr int CH = DP / 8;                                   // 16-byte vectors of a row
@@ -179,7 +179,7 @@ __device__ __forceinline__ void tile_rows(uint32_t dst, const char* plane, const
     for (int v = t; v < 128 * CH; v += THREADS) {
         const int k = v / CH, c = v % CH;
         const int32_t u = t0 + k;
-        const int64_t row = (u >= lo || u < sinks) && u < hi ? row_of(st, table, token_at(held, u)) : -1;
+        const int64_t row = (u >= lo || u < sinks) && u < hi ? row_of<LATE>(st, table, token_at(held, u)) : -1;
         const bool there = row >= 0 && 8 * c < st.head_dim;
         cp_async16(dst + (c >> 3) * 128 * 128 + k * 128 + (((c & 7) ^ (k & 7)) << 4),
                    plane + (there ? 2 * (row + (int64_t)h * st.head_dim + 8 * c) : 0), there);

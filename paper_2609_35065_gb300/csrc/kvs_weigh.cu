@@ -112,6 +112,7 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
     extern __shared__ char raw[];
     using P = WPlan<DP, KT>;
     constexpr int kThreads = P::threads, kStages = P::stages, kAccs = P::accs, kKeysTc = P::keys, kIssuer = P::issuer;
+    if (HELD) grid_wait();                                       // HELD: launched behind the kernel before
     const StepView& st = j.step;
     const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
     char* mem = raw + (base - smem_u32(raw));
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
         h = at - tile * pairs - r * st.kv_heads;
     }
     const int32_t t0 = tile * kKeysTc;
-    const Request q = load_request(st, r);
+    const Request q = load_request<HELD>(st, r);
     Held held{};
     int32_t T = q.T;                                             // places (without HELD: tokens) of the cache
     if (HELD) {
@@ -239,8 +240,8 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
         };
         if (mine > 0) {
             for (int32_t kt = 0; kt < key_tiles; ++kt) {
-                if (k_boxes) tile_boxes<DP>(base + kt * P::tile, &k_map, st, h, box_of<DP, 3>(st, table, held, t0 + 128 * kt, T, warp - kIssuer - 1, lane), b_load, lane);
-                else tile_rows<DP, 96>(base + kt * P::tile, j.k_plane, st, table, h, held, t0 + 128 * kt, 0, T, 0, u);
+                if (k_boxes) tile_boxes<DP>(base + kt * P::tile, &k_map, st, h, box_of<DP, 3, HELD>(st, table, held, t0 + 128 * kt, T, warp - kIssuer - 1, lane), b_load, lane);
+                else tile_rows<DP, 96, HELD>(base + kt * P::tile, j.k_plane, st, table, h, held, t0 + 128 * kt, 0, T, 0, u);
             }
             if (!k_boxes) {
                 cp_commit();
@@ -257,7 +258,7 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
             float x = INFINITY;                                  // weighs nothing
             int32_t g;
             const int32_t tok = token_of(st, (int32_t)min(p, (int64_t)total), g);
-            if (i < mine && row >= 0 && row < per && p < total) x = __ldg(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + h * st.group + g);
+            if (i < mine && row >= 0 && row < per && p < total) x = load_of<HELD>(j.lse + (int64_t)(q.q0 + tok) * (st.kv_heads * st.group) + h * st.group + g);
             return x;                                            // as it is: a product here would wait for the load
         };
         auto stage_free = [&](int32_t stage, int32_t round) {
@@ -503,7 +504,7 @@ __device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, con
     for (int k = 0; k < K; ++k) {
         f.q[k] = make_uint4(0, 0, 0, 0);
         const int32_t d = 32 * k + 8 * c;
-        if (p < total && d < st.head_dim) f.q[k] = __ldg(reinterpret_cast<const uint4*>(row + 2 * d));
+        if (p < total && d < st.head_dim) f.q[k] = load_of<HELD>(reinterpret_cast<const uint4*>(row + 2 * d));
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
@@ -514,7 +515,7 @@ __device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, con
             const int32_t t = token_of(st, x, g);
             f.see[e] = seen_by(q, t, t, j.causal, j.window);
             if (HELD) f.see[e] = in_places(held, f.see[e]);
-            f.lse[e] = -kLog2e * __ldg(j.lse + (int64_t)(q.q0 + t) * (st.kv_heads * st.group) + h * st.group + g);
+            f.lse[e] = -kLog2e * load_of<HELD>(j.lse + (int64_t)(q.q0 + t) * (st.kv_heads * st.group) + h * st.group + g);
         }
     }
 }
@@ -528,10 +529,11 @@ __device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, con
 template <bool HALF, int DP, int STAY, bool HELD>
 __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(WeighJob j, int32_t parts) {
     constexpr int K = DP / 32;                                   // 16-byte vectors of a lane and key
+    if (HELD) grid_wait();
     const StepView& st = j.step;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, i = lane >> 2;
     const int32_t h = blockIdx.y, r = blockIdx.z;
-    const Request q = load_request(st, r);
+    const Request q = load_request<HELD>(st, r);
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
     Held held{};
     int32_t T = q.T;                                             // places (without HELD: tokens) of the cache
@@ -554,7 +556,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int32_t t = key0(n) + i + 8 * e;
-            row[e] = n < mine && t < T ? row_of(st, table, token_at(held, t)) : -1;
+            row[e] = n < mine && t < T ? row_of<HELD>(st, table, token_at(held, t)) : -1;
         }
     };
     // lanes 4 i and 4 i + 1 add to the weights of keys i and i + 8, which they load with the keys
@@ -640,10 +642,11 @@ __global__ void __launch_bounds__(kRowWarps * 32, CTAS) kvs_weigh_held_kernel(We
     extern __shared__ __align__(16) char ring[];
     using P = HeldPlan<DP, STAGES>;
     constexpr int K = P::K;
+    grid_wait();
     const StepView& st = j.step;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, i = lane >> 2;
     const int32_t h = blockIdx.y, r = blockIdx.z;
-    const Request q = load_request(st, r);
+    const Request q = load_request<true>(st, r);
     const Held held = held_by(q, j, 1);
     if ((int32_t)blockIdx.x >= parts) {
         fade(j, r, h, held, blockIdx.x - parts, gridDim.x - parts);
@@ -659,7 +662,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, CTAS) kvs_weigh_held_kernel(We
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int32_t u = key0(n) + i + 8 * e;
-            row[e] = n < mine && u < T ? row_of(st, table, token_at(held, u)) : -1;
+            row[e] = n < mine && u < T ? row_of<true>(st, table, token_at(held, u)) : -1;
         }
     };
     float* weights = j.weights + r * j.request_stride + h * j.head_stride;
@@ -794,12 +797,9 @@ cudaError_t weigh_tc(const WeighJob& j, int sms, int held_share, cudaStream_t s)
     cfg.blockDim = dim3(P::threads);
     cfg.dynamicSmemBytes = P::bytes;
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = share;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
     cfg.attrs = at;
-    cfg.numAttrs = share > 1;
+    cfg.numAttrs = launch_attributes(at, share, HELD);
     return cudaLaunchKernelEx(&cfg, k, j, km, qm, (int32_t)k_boxes, (int32_t)q_boxes, (int32_t)share, (int32_t)x);
 }
 
@@ -809,8 +809,7 @@ cudaError_t weigh_held(const WeighJob& j, dim3 grid, int64_t parts, cudaStream_t
     constexpr int bytes = HeldPlan<DP, STAGES>::bytes;
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
-    k<<<grid, kRowWarps * 32, bytes, s>>>(j, (int32_t)parts);
-    return cudaGetLastError();
+    return launch_behind(k, grid, kRowWarps * 32, bytes, s, j, (int32_t)parts);
 }
 
 template <bool HALF, int DP, bool HELD>
@@ -829,12 +828,12 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
         if (HELD && rows > 16) x = pairs < sms ? sms / pairs : 1;
         x = x > most ? most : x;
         const dim3 grid((unsigned)(x + (HELD ? fading_of(j) : 0)), st.kv_heads, st.requests);
-        if (rows <= 8) {
-            kvs_weigh_rows_kernel<HALF, DP, 1, HELD><<<grid, kRowWarps * 32, 0, s>>>(j, (int32_t)x);
-        } else if constexpr (HELD) {
+        if constexpr (HELD) {
+            if (rows <= 8) return launch_behind(kvs_weigh_rows_kernel<HALF, DP, 1, HELD>, grid, kRowWarps * 32, 0, s, j, (int32_t)x);
             return rows <= 16 ? weigh_held<HALF, DP, 2, 3, 2>(j, grid, x, s) : weigh_held<HALF, DP, 4, 5, 1>(j, grid, x, s);
         } else {
-            if (rows <= 16) kvs_weigh_rows_kernel<HALF, DP, 2, HELD><<<grid, kRowWarps * 32, 0, s>>>(j, (int32_t)x);
+            if (rows <= 8) kvs_weigh_rows_kernel<HALF, DP, 1, HELD><<<grid, kRowWarps * 32, 0, s>>>(j, (int32_t)x);
+            else if (rows <= 16) kvs_weigh_rows_kernel<HALF, DP, 2, HELD><<<grid, kRowWarps * 32, 0, s>>>(j, (int32_t)x);
             else kvs_weigh_rows_kernel<HALF, DP, 0, HELD><<<grid, kRowWarps * 32, 0, s>>>(j, (int32_t)x);
         }
         return cudaGetLastError();

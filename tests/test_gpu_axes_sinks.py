@@ -258,6 +258,63 @@ def test_calls_at_once():
         assert torch.equal(w, again)
 
 
+@pytest.mark.parametrize("new,lens,window,H,G,D,B", [([1, 1], [700, 300], 100, 2, 4, 64, 16), ([1], [9000], 4000, 1, 4, 128, 16), ([6, 3], [700, 300], 100, 2, 4, 64, 16),
+                                                      ([40, 3], [700, 400], 100, 2, 4, 128, 48), ([300], [3000], 2000, 2, 4, 128, 16), ([1500], [1800], 100, 4, 4, 64, 16),
+                                                      ([1500], [1800], 100, 4, 4, 72, 1)])
+def test_calls_behind_kernels_that_write_what_they_read(new, lens, window, H, G, D, B):
+    """Queries, tables, lengths, positions and the turns' tables are each the last thing written before a call, by a kernel that has not ended
+    when the call is made; what a call writes is read by the next."""
+    sm = Long(new, lens, window, 5, H, G, D, B, given_back=False)
+    sm.cache.nan_to_num_(0.5)
+    step, q, k, v, cache = sm.on_gpu(kvs)
+    tables, kv_lens = step._keep[:2]
+    turns, axis, scale = kvs.kvs_rope_axes([D // 4, D // 4], restart=True)
+    turns, axis = torch.from_numpy(turns).cuda(), torch.from_numpy(axis).cuda()
+    rope, axes = kvs.Rope(turns, D, scale=scale), kvs.Axes(axis, 2)
+    positions = torch.randint(0, 5000, (2, sm.N), device="cuda").int()
+    inputs = [q, tables, kv_lens, positions, turns, axis]
+    fewer = [int(n) for n in (torch.tensor(lens) - 1).clamp(min=1)]
+    states = [[x.clone() for x in inputs] for _ in range(2)]
+    states[1][0].mul_(-0.5)
+    full = min(fewer) // B
+    states[1][1][:, :full] = tables[:, :full].flip(1)
+    states[1][2].copy_(torch.tensor(fewer, dtype=torch.int32))
+    states[1][3].add_(77)
+    states[1][4].mul_(1.5)
+    states[1][5].copy_(axis.flip(0))
+    heads, first = H * G, cache.clone()
+    ws = torch.empty(kvs.kvs_attend_sinks_workspace(step, heads, True, window, 5) + 16, dtype=torch.uint8, device="cuda")
+    big = torch.zeros(1 << 26, device="cuda")
+
+    def run(state, last, wait):
+        cache.copy_(first)
+        q_out, out = torch.zeros_like(q), torch.zeros_like(q)
+        z, w = torch.zeros(sm.N, heads, device="cuda"), torch.zeros(sm.R, H, step.max_kv, device="cuda")
+        for x in range(len(inputs)):
+            at = (last + 1 + x) % len(inputs)
+            if x == len(inputs) - 1 and not wait:
+                big.add_(1.0)                                    # so that the calls are made while the writes are still to come
+            torch.add(states[state][at], 0, out=inputs[at])
+        calls = [lambda: kvs.kvs_append_axes(step, 0, q, k, v, q_out, rope, axes, positions),
+                 lambda: kvs.kvs_attend_sinks(step, 0, q_out, out, z, None, True, window, 5, ws),
+                 lambda: kvs.kvs_weigh_sinks(step, 0, q_out, z, w, None, 0.5, True, window, 5),
+                 lambda: kvs.kvs_attend_sinks(step, 0, q, out, z, None, True, window, 5, ws),
+                 lambda: kvs.kvs_weigh_sinks(step, 0, q, z, w, None, 0.5, True, window, 5)]
+        for f in calls:
+            f()
+            if wait:
+                torch.cuda.synchronize()
+        return [q_out, out, z, w, cache.clone()]
+
+    want = [run(s, 0, True) for s in range(2)]
+    for i in range(6 * len(inputs)):
+        got = run(i % 2, i // 2, False)
+        for a, b in zip(got, want[i % 2]):
+            assert torch.equal(a, b), i
+    torch.cuda.synchronize()
+    kvs.kvs_check_errors()
+
+
 def test_a_graph_of_many_rows_follows_the_step():
     """Rows, lengths, tables and positions of a captured prefill are read anew at each replay."""
     sm = Long([900, 300], [1700, 900], 100, 4, 4, 4, 128, given_back=False)
