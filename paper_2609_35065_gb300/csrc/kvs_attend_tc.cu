@@ -58,9 +58,9 @@ struct Plan {
     static constexpr int bars = (TILES + stages) * tile;
     static constexpr int tops = bars + 256;        // [2][TILES][128] binary32: maxima, sums that a row's threads exchange
     static constexpr int bytes = tops + 1024 * TILES;
-    // for a cluster's join, in the ring: [row][DP] binary32 and [row] (m, l)
-    static constexpr int part = tile, part_ml = part + 128 * DP * 4;
-    static_assert(TILES == 2 || part_ml + 1024 <= bars, "the ring holds a CTA's part");
+    // for a cluster's join, in the ring: [tile's row][DP] binary32 and [tile's row] (m, l)
+    static constexpr int part = TILES * tile, part_ml = part + TILES * 128 * DP * 4;
+    static_assert(part_ml + TILES * 1024 <= bars, "the ring holds a CTA's part");
 };
 
 struct Bars {
@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
     constexpr float kMost = HALF ? 65504.0f : 1048576.0f;            // of a thread's weights of a step (half: of either sum)
     if (HELD) grid_wait();                           // HELD: launched behind the kernel before
     const StepView& st = j.step;
-    const bool cluster = TILES == 1 && j.cluster;    // no cluster joins the parts of two tiles
+    const bool cluster = (TILES == 1 || HELD) && j.cluster;      // parts of two tiles: only of places
     const uint32_t base = smem_u32(raw);
     if (base & 1023) {                               // the swizzle needs it; there is no room to round it up
         record_error(st.err, KVS_ERR_UNSUPPORTED);
@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
             if (live && half == 0) {
                 const float m2 = m == kNone ? kNone : m * c - top_at;
                 const int64_t row = (int64_t)(q.q0 + tok) * heads + h * st.group + g;
-                if (cluster) reinterpret_cast<float2*>(raw + P::part_ml)[t] = make_float2(m2, l);
+                if (cluster) reinterpret_cast<float2*>(raw + P::part_ml)[128 * tl + t] = make_float2(m2, l);
                 else if (j.splits > 1) reinterpret_cast<float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim)[split * all_rows + row] = make_float2(m2, l);
                 else if (j.lse) j.lse[row] = l == 0.0f ? kNone : (m2 + log2f(l)) * 0.69314718055994531f;
             }
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
             const bool parts = j.splits > 1;
             if (cluster) {
                 // binary32 rows over the ring, which nothing needs any more, for the cluster's CTAs to read
-                const uint32_t at = base + P::part + t * DP * 4;
+                const uint32_t at = base + P::part + (128 * tl + t) * DP * 4;
 #pragma unroll
                 for (int b = 0; b < DP / 32; ++b) {
                     uint32_t o[16];
@@ -522,27 +522,29 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
     if (warp == kIssuer) tmem_dealloc(tmem, P::columns);
     if (!cluster) return;
     // The cluster's CTAs share out the rows, four dims to a thread, and read one another's parts in order.
+    constexpr int kParts = TILES == 1 ? kCluster : kClusterPairs;
     cluster_sync();
     const int32_t share = (rows + j.splits - 1) / j.splits, row_end = min(rows, (split + 1) * share);
     for (int32_t v = threadIdx.x; v < share * (DP / 4); v += P::threads) {
         const int32_t x = split * share + v / (DP / 4), d = v % (DP / 4);
         if (x >= row_end || 4 * d >= st.head_dim) continue;
-        float2 ml[kCluster];
-        float4 p[kCluster];
+        const int32_t at = x + (x < per ? 0 : 128 - per);        // among the rows of tiles
+        float2 ml[kParts];
+        float4 p[kParts];
         float M = kNone, L = 0.0f;
 #pragma unroll
-        for (int k = 0; k < kCluster; ++k) {
+        for (int k = 0; k < kParts; ++k) {
             ml[k] = make_float2(kNone, 0.0f);
             p[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (k < j.splits) {
-                ml[k] = cluster_ld2(cluster_at(base + P::part_ml + 8 * x, k));
-                p[k] = cluster_ld4(cluster_at(base + P::part + x * DP * 4 + ((d ^ (x & 7)) << 4), k));
+                ml[k] = cluster_ld2(cluster_at(base + P::part_ml + 8 * at, k));
+                p[k] = cluster_ld4(cluster_at(base + P::part + at * DP * 4 + ((d ^ (at & 7)) << 4), k));
             }
             M = fmaxf(M, ml[k].x);
         }
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int k = 0; k < kCluster; ++k) {
+        for (int k = 0; k < kParts; ++k) {
             const float f = ml[k].y == 0.0f ? 0.0f : exp2_fast(ml[k].x - M);
             L += f * ml[k].y;
             o.x += f * p[k].x;

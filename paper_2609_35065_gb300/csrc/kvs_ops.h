@@ -101,6 +101,13 @@ struct AttendPlan {
     int tc, splits, row_tiles, cluster;
 };
 constexpr int kCluster = 8;            // most parts that a cluster joins
+constexpr int kClusterPairs = 4;       // ... of two row tiles
+// Whether `ctas` CTAs, one to an SM, all run at once in clusters of n.  A cluster's lie on neighbouring SMs, of which
+// some stay unused: what the occupancy calculator says of 152 SMs.
+inline bool clusters_fit(int64_t ctas, int64_t n, int sms) {
+    constexpr int room[kCluster + 1] = {0, 152, 152, 138, 144, 140, 138, 105, 120};
+    return n <= kCluster && ctas * 152 <= (int64_t)room[n] * sms;
+}
 AttendPlan attend_plan(const StepView& st, int sms);
 // A plane's TMA map (a CUtensorMap at `map`) in boxes of whole blocks, or of 128 tokens of one,
 // of one head's 64 elements; false where blocks do not tile 128 tokens (kvs_attend_tc.cu).

@@ -218,15 +218,33 @@ StepView held_view(StepView v, int32_t causal, int32_t window, int32_t sinks, in
     return v;
 }
 
-// Costs in us, fitted to measurements (8 KV heads of 128 dims, 5 query heads each, a request of 293 new tokens
-// and sinks of 64, in a graph): CTAs that stay and take two row tiles at a time 31.4 with a window of 2048, 14.4 with 512;
-// a CTA to a row tile 30.5 and 16.9; two row tiles to a CTA, in three parts that a second kernel joins, 28.0 and
-// 22.0, with a window of 4096 36.4 against 54.7.  Parts that their cluster joins: 35 rows of 64 dims of 16 heads over 1000 tokens
-// 8.7 in five, 10.1 in four, 16.6 in one.
+// Costs in us, fitted to measurements of some sixty steps (in a graph), most of them within a tenth: of a step of 128
+// keys and of a CTA's start and end.  8 KV heads of 128 dims, 5 query heads each, a request of 293 new tokens: CTAs that stay and take two row
+// tiles at a time 31.7 with a window of 2048, 14.5 with 512; a CTA to a row tile 30.5 and 16.7; two row tiles in
+// two parts that their cluster joins 26.7 and 18.6, in three that a second kernel joins 27.9 and 21.6, with a window of 4096 36.6
+// against 54.8 where they stay.  35 rows of 64 dims of 16 heads over 1000 tokens: parts of a cluster 8.7 in
+// five, 10.1 in four, 16.6 in one.  Blocks of 1 or 12 tokens come by rows, and a step takes as long as those: 293 tokens as above 130 where CTAs stay, 145
+// with a CTA to a row tile, 69 in three parts.
 AttendPlan held_plan(const StepView& v, int32_t held, int32_t causal, int32_t window, int32_t sinks, int sms) {
     if (!held) return attend_plan(v, sms);
     const int64_t rows = (int64_t)v.max_q * v.group, units = (int64_t)v.kv_heads * v.requests, per = tile_rows_of(v.group);
-    if (rows <= 16) return attend_plan(held_view(v, causal, window, sinks, v.max_q), sms);
+    if (rows <= 16) {
+        // attend_plan's costs of few rows, with what is known of clusters' room by now (four requests with a window of 4096 11.1 us for 12.8)
+        const int64_t steps = ((int64_t)held_view(v, causal, window, sinks, v.max_q).max_kv + 127) / 128;
+        AttendPlan best{0, 1, 1, 0};
+        int64_t least = -1;
+        for (int64_t n = 1; n <= 256 && n <= (steps + 1) / 2; ++n) {
+            const bool cluster = n > 1 && clusters_fit(units * n, n, sms);
+            const int64_t cost = (units * n + sms - 1) / sms * ((steps + n - 1) / n + 4) + (n == 1 ? 0 : cluster ? 1 : 5);
+            if (least >= 0 && cost >= least) continue;
+            least = cost;
+            best = AttendPlan{0, (int)n, 1, cluster};
+        }
+        return best;
+    }
+    const bool narrow = v.head_dim <= 64, boxes = v.block_size % 8 == 0 && (128 % v.block_size == 0 || v.block_size % 128 == 0) && v.head_dim >= 64;
+    const double step1 = boxes ? (narrow ? 0.95 : 1.17) : narrow ? 3.5 : 7.4, start1 = narrow ? (boxes ? 8.0 : 9.0) : boxes ? 9.0 : 0.5;
+    const double step2 = boxes ? 1.43 : narrow ? 5.3 : 6.6, both = boxes && narrow ? 1.6 : step1;        // both: of two CTAs on an SM
     AttendPlan best{1, 1, 1, 0};
     double least = -1.0;
     auto offer = [&](int row_tiles, int64_t parts, int cluster, double cost) {
@@ -235,18 +253,22 @@ AttendPlan held_plan(const StepView& v, int32_t held, int32_t causal, int32_t wi
         best = AttendPlan{1, (int)parts, row_tiles, cluster};
     };
     for (int rt = 1; rt <= 2; ++rt) {
-        if (rt == 2 && rows <= per) break;
-        const int64_t tiles = (rows + per * rt - 1) / (per * rt) * units, slots = rt == 1 && v.head_dim <= 64 ? 2 * sms : sms;
+        const int64_t tiles = (rows + per * rt - 1) / (per * rt) * units, slots = rt == 1 && narrow ? 2 * sms : sms;
         // places of the last sink's block and of the window's first one may be nobody's
         const int64_t block = v.block_size < 128 ? v.block_size : 128;
         const int64_t steps = ((int64_t)held_view(v, causal, window, sinks, per * rt / v.group + 1).max_kv + 2 * block + 125) / 128;
-        for (int64_t n = 1; n <= 256 && n <= steps; ++n) {
+        // one row tile is given to CTAs that stay, too: they start sooner (62 requests of 13 tokens, 2 x 2 heads of 96 dims, a window of
+        // 167 9.7 us, 12.2 otherwise)
+        const int64_t most = rt == 2 && rows <= per ? 1 : 256;
+        for (int64_t n = 1; n <= most && n <= steps; ++n) {
             const int64_t ctas = tiles * n;
             const double each = (double)((steps + n - 1) / n), waves = (double)((ctas + slots - 1) / slots);
-            if (n == 1) offer(rt, 1, 0, rt == 2 ? 5.8 + 1.43 * each * waves + 3.0 * (waves - 1.0) : waves * (1.17 * each + 9.0));
-            // clusters have room as in attend_plan
-            else if (rt == 1 && n <= kCluster && ctas <= sms - 10 * (n - 1)) offer(1, n, 1, 1.15 * each + 8.0);
-            else if (n <= (steps + 1) / 2) offer(rt, n, 0, rt == 2 ? waves * (1.5 * each + 7.0) + 12.0 : waves * (1.17 * each + 9.0) + 4.0 + 0.02 * n);
+            const double alone = waves * ((ctas > sms ? both : step1) * each + start1);
+            if (n == 1) offer(rt, 1, 0, rt == 2 ? 5.8 + step2 * each * waves + 3.0 * (waves - 1.0) : alone);
+            else if (rt == 1 && clusters_fit(ctas, n, sms)) offer(1, n, 1, step1 * each + start1 + (narrow ? 1.0 : 2.4) * (rows < per ? (double)rows / per : 1.0));
+            else if (rt == 1 && n <= kCluster && ctas <= slots - 5 * (n - 1)) offer(1, n, 1, boxes ? 1.1 * each + 11.5 : step1 * each + 2.0);
+            else if (rt == 2 && n <= kClusterPairs && clusters_fit(ctas, n, sms)) offer(2, n, 1, step2 * each + 13.5);
+            else if (n <= (steps + 1) / 2) offer(rt, n, 0, rt == 2 ? waves * (step2 * each + 7.0) + 12.0 : alone + 4.0 + 0.02 * n);
         }
     }
     return best;

@@ -129,6 +129,23 @@ def test_many_row_tiles(new, lens, window, sinks, H, G, D, B, dtype, causal):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("new,lens,window,H,G,D,dtype,causal", [
+    ([293], [2600], 2048, 8, 5, 128, "bf16", True), ([150], [2600], 2048, 8, 5, 128, "f16", True), ([200], [2600], 2048, 8, 4, 72, "bf16", False),
+    ([100, 280], [2500, 290], 2000, 4, 5, 128, "bf16", True), ([280, 0, 100], [3000, 7, 100], 2500, 4, 5, 128, "f16", True), ([400], [1900], 1500, 8, 8, 64, "bf16", True)])
+def test_parts_of_two_row_tiles(new, lens, window, H, G, D, dtype, causal):
+    """Parts of a pair of row tiles, joined by their cluster; some of the requests have fewer steps than there are parts."""
+    sm = Long(new, lens, window, 5, H, G, D, dtype=dtype, causal=causal)
+    _check_attend(sm)
+    a, b = _attend(sm), _attend(sm)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("new,lens,window,H,G,D,B", [([13] * 30, [400] * 30, 100, 2, 2, 96, 8), ([6, 0, 3] * 9, [300, 5, 3] * 9, 28, 8, 7, 96, 16), ([20, 1], [700, 40], 100, 4, 4, 64, 16),
+                                                     ([20, 1], [700, 40], 100, 4, 4, 128, 1)])
+def test_one_row_tile_on_ctas_that_stay(new, lens, window, H, G, D, B):
+    _check_attend(Long(new, lens, window, 3, H, G, D, B))
+
+
 def test_the_neighbours_of_a_request_do_not_matter():
     sm = Long([2, 150, 1], [700, 650, 350], 90, 6, 2, 4, 128)
     a, za = _attend(sm)
