@@ -75,7 +75,9 @@ __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t
 // ring of its own: a tile's rows are done with when the products are, its lse with the sums.
 //
 // Two CTAs of one key tile share an SM, and while one starts or ends the other works; of many row
-// tiles, two key tiles read each of them once for both.
+// tiles, two key tiles read each of them once for both.  With one key tile the warpgroups' columns are products
+// of their own, so that neither waits until the other has read its scores (1024 new tokens and a window as long, 40
+// query heads on 8: 26.4 us -> 25.4; before a CTA's set-up was beside the load of the request's lengths 27.2).
 //
 // 128 x 128 scores take the tensor cores about 570 cycles and the exponentials 512; what bounds
 // it is their hand-over, some 850 cycles: 5120 rows against 13312 keys of 8 heads of 128 dims
@@ -111,13 +113,13 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
                                                                    int32_t key_tiles_all) {
     extern __shared__ char raw[];
     using P = WPlan<DP, KT>;
-    constexpr int kThreads = P::threads, kStages = P::stages, kAccs = P::accs, kKeysTc = P::keys, kIssuer = P::issuer;
+    constexpr int kThreads = P::threads, kStages = P::stages, kAccs = P::accs, kKeysTc = P::keys, kIssuer = P::issuer, kParts = KT == 1 ? 2 : kAccs;
     if (HELD) grid_wait();                                       // HELD: launched behind the kernel before
     const StepView& st = j.step;
     const uint32_t base = (smem_u32(raw) + 1023) & ~1023u;
     char* mem = raw + (base - smem_u32(raw));
     const uint32_t ring = base + KT * P::tile, ctl = base + P::bars;
-    const uint32_t b_k = ctl, b_full = ctl + 8, b_free = b_full + 8 * kStages, b_s = b_free + 8 * kStages, b_e = b_s + 8 * kAccs, b_done = b_e + 8 * kAccs,
+    const uint32_t b_k = ctl, b_full = ctl + 8, b_free = b_full + 8 * kStages, b_s = b_free + 8 * kStages, b_e = b_s + 8 * kParts, b_done = b_e + 8 * kParts,
                    b_load = b_done + 8, b_lse = b_load + 8, b_read = b_lse + 8 * kSlots, tmem_at = b_read + 8 * kSlots;
     const int warp = warp_number(), lane = threadIdx.x & 31, wg = warp >> 2;
     int32_t r = blockIdx.z, h = blockIdx.y, tile = blockIdx.x / share;
@@ -129,19 +131,44 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
         h = at - tile * pairs - r * st.kv_heads;
     }
     const int32_t t0 = tile * kKeysTc;
-    const Request q = load_request<HELD>(st, r);
+    const int32_t unit = HELD && k_boxes ? min(st.block_size, 128) : 1;
+    if (HELD && tile >= key_tiles_all) {
+        const int32_t behind = gridDim.x / (share * st.kv_heads * st.requests) - key_tiles_all;
+        fade(j, r, h, held_by(load_request<HELD>(st, r), j, unit), (tile - key_tiles_all) * share + rank, behind * share);
+        return;                                                  // as all of its cluster does
+    }
+    // Set-up while the request's lengths are on their way.
+    const RawRequest fetched = fetch_request<HELD>(st, r);
+    if (warp == kIssuer) tmem_alloc(tmem_at, P::columns);
+    if (threadIdx.x == 0) {
+        mbar_init(b_k, 8 * KT);
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(b_full + 8 * i, q_boxes ? 1 : 3);          // the loading warps
+            mbar_init(b_free + 8 * i, 1);
+        }
+        for (int i = 0; i < kSlots; ++i) mbar_init(b_lse + 8 * i, q_boxes ? 2 : 3);
+        for (int i = 0; i < kParts; ++i) {
+            mbar_init(b_s + 8 * i, 1);
+            mbar_init(b_e + 8 * i, KT == 1 ? 4 : 8);
+        }
+        mbar_init(b_done, 1);
+    }
+    const Request q = check_request(st, fetched);
     Held held{};
     int32_t T = q.T;                                             // places (without HELD: tokens) of the cache
     if (HELD) {
-        held = held_by(q, j, k_boxes ? min(st.block_size, 128) : 1);
+        held = held_by(q, j, unit);
         T -= held.shift;
-        if (tile >= key_tiles_all) {
-            const int32_t behind = gridDim.x / (share * st.kv_heads * st.requests) - key_tiles_all;
-            fade(j, r, h, held, (tile - key_tiles_all) * share + rank, behind * share);
-            return;                                              // as all of its cluster does
-        }
     }
-    if (t0 >= T) return;                                         // the whole cluster
+    if (t0 >= T) {                                               // the whole cluster
+        if (warp == kIssuer) {
+            __syncwarp();
+            uint32_t at;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(at) : "r"(tmem_at) : "memory");
+            tmem_dealloc(at, P::columns);
+        }
+        return;
+    }
     const int32_t* table = st.tables + (int64_t)r * st.table_stride;
     const int32_t per = tile_rows_of(st.group);                  // rows of a tile
     const int32_t key_tiles = KT == 2 && t0 + 128 < T ? 2 : 1;
@@ -153,23 +180,11 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
 
     if (threadIdx.x == 0) {
         mbar_init(b_load, 3 * key_tiles);
-        mbar_init(b_k, 8 * KT);
-        for (int i = 0; i < kStages; ++i) {
-            mbar_init(b_full + 8 * i, q_boxes ? 1 : 3);          // the loading warps
-            mbar_init(b_free + 8 * i, 1);
-        }
-        for (int i = 0; i < kSlots; ++i) {
-            mbar_init(b_lse + 8 * i, q_boxes ? 2 : 3);
-            mbar_init(b_read + 8 * i, 8 * key_tiles);            // the key tiles' warps
-        }
-        for (int i = 0; i < kAccs; ++i) {
-            mbar_init(b_s + 8 * i, 1);
-            mbar_init(b_e + 8 * i, 8);
-        }
-        mbar_init(b_done, 1);
+        for (int i = 0; i < kSlots; ++i) mbar_init(b_read + 8 * i, 8 * key_tiles);       // the key tiles' warps
         mbar_init_fence();
     }
-    if (warp == kIssuer) tmem_alloc(tmem_at, P::columns);
+    Box k_box{-1, 0, 0};
+    if (KT == 1 && k_boxes && warp > kIssuer && mine > 0) k_box = box_of<DP, 3, HELD>(st, table, held, t0, T, warp - kIssuer - 1, lane);
     // rows that no box fills are zeros for good, and weigh nothing
     for (int i = threadIdx.x; i < (128 - per) * (DP / 8) * kStages; i += kThreads) {
         const int stage = i / ((128 - per) * (DP / 8)), v = i % ((128 - per) * (DP / 8)), row = per + v / (DP / 8), c = v % (DP / 8);
@@ -191,7 +206,7 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
     const int t = threadIdx.x & 127;
     if (warp == kIssuer) {
         // ---- the products: the warp waits together, one lane issues ----------------------
-        constexpr uint32_t id = tc_idesc(HALF, 128, false);
+        constexpr uint32_t id = tc_idesc(HALF, KT == 1 ? 64 : 128, false);
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), keys = tm + 128 * kAccs;     // 64 columns to a key tile
         const uint64_t q_desc = tc_desc(ring, 16, 1024);
         bool ok = mine <= 0 || __all_sync(0xffffffffu, wait(b_k, 0));
@@ -200,7 +215,21 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
         for (int32_t i = 0; ok && i < mine; ++i) {
             ok = wait(b_full + 8 * stage, round & 1);
             const uint64_t b = tc_ahead(q_desc, stage * P::tile);
-            for (int32_t kt = 0; kt < key_tiles; ++kt) {
+            if (KT == 1) {
+                // the two warpgroups' columns one after the other: neither waits for the other's
+                for (int hf = 0; hf < 2; ++hf) {
+                    if (i > 0) ok = wait(b_e + 8 * hf, (i - 1) & 1) && ok;
+                    __syncwarp();
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < DP / 16; ++k)
+                            tc_mma_ts(tm + 64 * hf, keys + 8 * k, tc_ahead(b, hf * 64 * 128 + (k >> 2) * 128 * 128 + (k & 3) * 32), id, k > 0);
+                        tc_commit(b_s + 8 * hf);
+                        if (hf) tc_commit(b_free + 8 * stage);
+                    }
+                }
+            } else for (int32_t kt = 0; kt < key_tiles; ++kt) {
                 if (uses > 0) ok = wait(b_e + 8 * acc, (uses - 1) & 1) && ok;
                 __syncwarp();
                 tc_fence_after();
@@ -240,7 +269,7 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
         };
         if (mine > 0) {
             for (int32_t kt = 0; kt < key_tiles; ++kt) {
-                if (k_boxes) tile_boxes<DP>(base + kt * P::tile, &k_map, st, h, box_of<DP, 3, HELD>(st, table, held, t0 + 128 * kt, T, warp - kIssuer - 1, lane), b_load, lane);
+                if (k_boxes) tile_boxes<DP>(base + kt * P::tile, &k_map, st, h, KT == 1 ? k_box : box_of<DP, 3, HELD>(st, table, held, t0 + 128 * kt, T, warp - kIssuer - 1, lane), b_load, lane);
                 else tile_rows<DP, 96, HELD>(base + kt * P::tile, j.k_plane, st, table, h, held, t0 + 128 * kt, 0, T, 0, u);
             }
             if (!k_boxes) {
@@ -392,7 +421,7 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
         for (int32_t i = kt < key_tiles ? 0 : mine; i < mine; ++i) {
             const int32_t n = i * key_tiles + kt;
             const int slot = i % kSlots, acc = n % kAccs;
-            if (!__all_sync(0xffffffffu, wait(b_lse + 8 * slot, (i / kSlots) & 1) && wait(b_s + 8 * acc, (n / kAccs) & 1))) break;
+            if (!__all_sync(0xffffffffu, wait(b_lse + 8 * slot, (i / kSlots) & 1) && wait(KT == 1 ? b_s + 8 * half : b_s + 8 * acc, (n / kAccs) & 1))) break;
             tc_fence_after();
             const int32_t p0 = (tile0 + rank + share * i) * per + 64 * half;
             const int32_t a = see.first - p0, b = see.end - p0;      // columns that see this thread's key
@@ -409,7 +438,7 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
                     // the accumulator is read
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(b_e + 8 * acc);
+                    if (lane == 0) mbar_arrive(KT == 1 ? b_e + 8 * half : b_e + 8 * acc);
                 }
                 float* s = reinterpret_cast<float*>(sr);
 #pragma unroll
@@ -747,7 +776,7 @@ int64_t fading_of(const WeighJob& j) { return j.decay == 1.0f ? 0 : (j.step.max_
 // has an SM to itself, and 1 of the SM's time where two share it, 1.7 of a long CTA's while shorter ones come and
 // go; the start and end of a CTA take 10, which the other one's work covers.  Clusters of eight wait for eight places
 // at once.  8 KV heads of 128 dims, 5 query heads each: 1024 new tokens and a window as long 45 us with one CTA
-// to a key tile, 34 with two, 27 with four and 41 with eight; 2048 and a window of 128 86, 48, 30, 42; 4 x 1500
+// to a key tile, 34 with two, 27 (by now 25.4) with four and 41 with eight; 2048 and a window of 128 86, 48, 30, 42; 4 x 1500
 // and 600 72, 75, 102, 157; 8 x 100 and 1024 21, 33, 57, 119; one head of 72 dims, 2 x 288 and 23 17, 13, 9.4, 8.6.
 // Two key tiles to a CTA, as kvs_weigh has them for many rows, took 67, 38, 32 and 57 for the first, and gained
 // nothing on any of thirty other calls.
