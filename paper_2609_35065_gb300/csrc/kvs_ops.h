@@ -70,6 +70,8 @@ struct WeighJob {
     float    scale_log2, decay;
     int32_t  causal, window;
     int32_t  held, sinks;            // as in attention
+    float    scale, scale_low;       // by_places: as given; what scale_log2 lacks (kvs_weigh.cu)
+    int32_t  by_places;              // 1: of kvs_weigh_sinks, hidden tokens or not
 };
 
 struct EvictJob {

@@ -348,6 +348,8 @@ int weigh_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step* 
     j.head_stride = hs;
     j.scale_log2 = a->scale * kLog2e;
     j.decay = a->decay;
+    j.scale = a->scale;
+    j.by_places = sinks != nullptr;
     j.causal = a->causal != 0;
     int sms;
     KVS_TRY(ops_device(&j.step.err, &sms));

@@ -7,12 +7,14 @@
 //
 // With every row's lse known a key's sum needs no other key: keys go to different CTAs, warps
 // or lanes, and no sum is shared.  Rows are packed as in attention (row = token * group + head).
+#include <cmath>
+
 #include "kvs_tcgen05.cuh"
 
 namespace kvs {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = (float)(1.4426950408889634 - (double)kLog2e);
 
 // Packed rows [first, end) that see any of the cached tokens t_lo .. t_hi (all of them do
 // between, of one token).  Their number is below 2^30.
@@ -77,7 +79,8 @@ __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t
 // Two CTAs of one key tile share an SM, and while one starts or ends the other works; of many row
 // tiles, two key tiles read each of them once for both.  With one key tile the warpgroups' columns are products
 // of their own, so that neither waits until the other has read its scores (1024 new tokens and a window as long, 40
-// query heads on 8: 26.4 us -> 25.4; before a CTA's set-up was beside the load of the request's lengths 27.2).
+// query heads on 8: 26.4 us -> 25.4, by now 26.7 with the scale in two numbers; before a CTA's set-up was beside the load
+// of the request's lengths 27.2).
 // What is left there are the starts of 3.8 CTAs to an SM (lengths, table and keys one behind the other): copies with half
 // of the sums' work took 21, with half the products, half the rows' loads or a quarter of the exponentials 25.
 //
@@ -92,6 +95,7 @@ __device__ __forceinline__ void add_weight(const WeighJob& j, int32_t r, int32_t
 // and joins its sums, in the CTAs' order, through distributed shared memory.
 // ---------------------------------------------------------------------------
 constexpr int kSlots = 8;
+constexpr int kFewRows = 32;           // up to which keys go straight into registers
 
 // KT: key tiles of a CTA.
 template <int DP, int KT>
@@ -303,8 +307,8 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
         };
         auto put_lse = [&](int32_t i, float e0, float e1) {
             float* lse = reinterpret_cast<float*>(mem + P::lse) + (i % kSlots) * 128;
-            lse[a0] = -kLog2e * e0;
-            if (a1 < 128) lse[a1] = -kLog2e * e1;
+            lse[a0] = HELD ? fmaf(-kLog2e, e0, -kLog2eLow * e0) : -kLog2e * e0;
+            if (a1 < 128) lse[a1] = HELD ? fmaf(-kLog2e, e1, -kLog2eLow * e1) : -kLog2e * e1;
             __syncwarp();
             if (lane == 0) mbar_arrive(b_lse + 8 * (i % kSlots));
         };
@@ -446,8 +450,14 @@ __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_k
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float4 z = lse[8 * k + e];
+                    float low[4] = {s[4 * e], s[4 * e + 1], s[4 * e + 2], s[4 * e + 3]};
                     fma2(s[4 * e], s[4 * e + 1], c, z.x, z.y);
                     fma2(s[4 * e + 2], s[4 * e + 3], c, z.z, z.w);
+                    if (!HELD) continue;
+                    fma2(low[0], low[1], j.scale_low, s[4 * e], s[4 * e + 1]);
+                    fma2(low[2], low[3], j.scale_low, s[4 * e + 2], s[4 * e + 3]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) s[4 * e + x] = low[x];
                 }
 #pragma unroll
                 for (int e = 0; e < 32; ++e) s[e] = exp2_fast(s[e]);
@@ -778,7 +788,7 @@ int64_t fading_of(const WeighJob& j) { return j.decay == 1.0f ? 0 : (j.step.max_
 // has an SM to itself, and 1 of the SM's time where two share it, 1.7 of a long CTA's while shorter ones come and
 // go; the start and end of a CTA take 10, which the other one's work covers.  Clusters of eight wait for eight places
 // at once.  8 KV heads of 128 dims, 5 query heads each: 1024 new tokens and a window as long 45 us with one CTA
-// to a key tile, 34 with two, 27 (by now 25.4) with four and 41 with eight; 2048 and a window of 128 86, 48, 30, 42; 4 x 1500
+// to a key tile, 34 with two, 27 with four and 41 with eight; 2048 and a window of 128 86, 48, 30, 42; 4 x 1500
 // and 600 72, 75, 102, 157; 8 x 100 and 1024 21, 33, 57, 119; one head of 72 dims, 2 x 288 and 23 17, 13, 9.4, 8.6.
 // Two key tiles to a CTA, as kvs_weigh has them for many rows, took 67, 38, 32 and 57 for the first, and gained
 // nothing on any of thirty other calls.
@@ -849,7 +859,7 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     const int64_t rows = (int64_t)st.max_q * st.group;
     // Up to 32 rows: 8 requests x 8 heads of 128 dims with 8000 tokens take 68 us at 32 rows and 90 at
     // 48 (on the tensor cores' kernel 72); of 64 dims 54 and 70 (66).
-    if (rows <= 32) {
+    if (rows <= kFewRows) {
         // CTAs for two rounds of two to an SM (weigh of a decode step: one round 45.2 us, two 40.5,
         // three 41.1, six 45.1), but not more than leave a warp four tiles.
         const int64_t tokens = HELD ? places_of(j, 1) : st.max_kv;
@@ -882,7 +892,29 @@ cudaError_t weigh_dims(const WeighJob& j, int sms, cudaStream_t s) { return j.he
 
 }  // namespace
 
-int launch_weigh(const WeighJob& j, bool half, int sms, cudaStream_t s) {
+// A heavy token's weight is the exponential of a small difference of two large numbers, its score and lse, so that a score's
+// relative error is multiplied by lse, and where it has the same sign for all rows no sum evens it out.  The scale
+// times log2(e) as one binary32 number is up to 6e-8 off, and the tensor cores cut sums off where others round: measured
+// against 64 bits, with keys along their queries, scores come out 3.1e-8 (half) or 1.8e-8 of themselves too small for every
+// 16 dims.  kvs_weigh_sinks on the tensor cores makes up for both, with the scale in two numbers, the second of the
+// first's sign so that infinite scores stay what they are: 429 new tokens of 72 dims in half,
+// weights 1.7e-7 off (of their norm) for 1.5e-6; it takes 4% longer.
+void exact_scale(WeighJob& j, bool half) {
+    const double c = (double)j.scale * 1.4426950408889634 * (1.0 + j.step.head_dim / 16.0 * (half ? 3.1e-8 : 1.8e-8));
+    j.scale_log2 = (float)c;
+    if (std::fabs((double)j.scale_log2) > std::fabs(c)) j.scale_log2 = std::nextafter(j.scale_log2, 0.0f);
+    j.scale_low = std::isfinite(j.scale_log2) ? (float)(c - (double)j.scale_log2) : 0.0f;
+}
+
+int launch_weigh(const WeighJob& job, bool half, int sms, cudaStream_t s) {
+    WeighJob j = job;
+    if (j.by_places && (int64_t)j.step.max_q * j.step.group > kFewRows) {
+        if (!j.held) {                                           // nothing is hidden: a window that all tokens fill
+            j.held = 1;
+            j.window = j.step.max_kv;
+        }
+        exact_scale(j, half);
+    }
     const cudaError_t e = half ? weigh_dims<true>(j, sms, s) : weigh_dims<false>(j, sms, s);
     return e == cudaSuccess ? 1 : -(int)e;
 }
