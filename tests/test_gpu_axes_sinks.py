@@ -437,6 +437,36 @@ def test_a_request_without_new_tokens_only_fades(new, decay):
     assert torch.equal(w[0, :, 700:], before[0, :, 700:])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 72, 96, 128])
+@pytest.mark.parametrize("window", [300, 0])
+def test_weights_of_heavy_tokens(dtype, D, window):
+    """Keys of eight tokens lie along all queries, whose lse is near 20: a weight is the exponential of a small difference of two such
+    numbers, and an error of the score that all rows share stays.  Products of 16 dims are cut off at 2^-23 of their sum and again where that
+    is added, 2 D / 16 times 2^-23 of the score at most as these sums only grow; what is made up for on average is less than
+    that.  The exponent's parts, up to log2(e) 21 < 32, are rounded twice, by 2^-20 each, and the exponential once, by 2^-22."""
+    new, T, G = 400, 700, 2
+    sm = Long([new], [T], window, 8, 1, G, D, 16, dtype=dtype, given_back=False)
+    sm.cache.nan_to_num_(0.5)
+    g = torch.Generator().manual_seed(1)
+    along = torch.randn(D, generator=g)
+    q, _, _ = sm.parts(sm.qkv)
+    q.copy_((along + 0.1 * torch.randn(q.shape, generator=g)).to(q.dtype))
+    sm.cache[0, torch.from_numpy(sm.slots(0, np.arange(8))), 0] = (20.0 / D ** 0.5 * along).to(q.dtype)
+    step, qg, _, _, _cache = sm.on_gpu(kvs)
+    scale = D ** -0.5
+    x, *_ = zip(*[sm.scores(0, 0, i, float(np.float32(scale)), True, window) for i in range(G)])
+    x = np.stack(x, 1)                                                       # [new, G, T]
+    lse = torch.from_numpy(np.log(np.exp(x).sum(-1))).float()
+    assert lse.mean() > 15
+    want = np.exp(x - lse.double().numpy()[..., None]).sum((0, 1))
+    w = torch.zeros(1, 1, step.max_kv, device="cuda")
+    kvs.kvs_weigh_sinks(step, 0, qg, lse.cuda(), w, scale, 0.0, True, window, 8)
+    off = w[0, 0, :T].double().cpu().numpy() - want
+    bound = 21 * (2 * -(-D // 16)) * 2.0 ** -23 + 2 * 2.0 ** -20 * np.log(2) + 2.0 ** -22
+    assert np.linalg.norm(off) <= bound * np.linalg.norm(want)
+
+
 def test_weights_add_up_to_the_rows():
     sm = Long([3, 150], [700, 650], 90, 6, 2, 4, 128)
     step, q, _, _, _cache = sm.on_gpu(kvs)
