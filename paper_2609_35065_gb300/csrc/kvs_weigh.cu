@@ -894,13 +894,11 @@ cudaError_t weigh_dims(const WeighJob& j, int sms, cudaStream_t s) { return j.he
 
 // A heavy token's weight is the exponential of a small difference of two large numbers, its score and lse, so that a score's
 // relative error is multiplied by lse, and where it has the same sign for all rows no sum evens it out.  The scale
-// times log2(e) as one binary32 number is up to 6e-8 off, and the tensor cores cut sums off where others round: measured
-// against 64 bits, with keys along their queries, scores come out 3.1e-8 (half) or 1.8e-8 of themselves too small for every
-// 16 dims.  kvs_weigh_sinks on the tensor cores makes up for both, with the scale in two numbers, the second of the
-// first's sign so that infinite scores stay what they are: 429 new tokens of 72 dims in half,
-// weights 1.7e-7 off (of their norm) for 1.5e-6; it takes 4% longer.
-void exact_scale(WeighJob& j, bool half) {
-    const double c = (double)j.scale * 1.4426950408889634 * (1.0 + j.step.head_dim / 16.0 * (half ? 3.1e-8 : 1.8e-8));
+// times log2(e) as one binary32 number is up to 7e-8 off: kvs_weigh_sinks on the tensor cores takes it in two, the second of the
+// first's sign so that infinite scores stay what they are.  What the tensor cores cut off a sum depends on the terms' signs and
+// magnitudes, so that nothing is made up for it here: kvs_attend_sinks' lse is of scores that were cut off alike.
+void exact_scale(WeighJob& j) {
+    const double c = (double)j.scale * 1.4426950408889634;
     j.scale_log2 = (float)c;
     if (std::fabs((double)j.scale_log2) > std::fabs(c)) j.scale_log2 = std::nextafter(j.scale_log2, 0.0f);
     j.scale_low = std::isfinite(j.scale_log2) ? (float)(c - (double)j.scale_log2) : 0.0f;
@@ -913,7 +911,7 @@ int launch_weigh(const WeighJob& job, bool half, int sms, cudaStream_t s) {
             j.held = 1;
             j.window = j.step.max_kv;
         }
-        exact_scale(j, half);
+        exact_scale(j);
     }
     const cudaError_t e = half ? weigh_dims<true>(j, sms, s) : weigh_dims<false>(j, sms, s);
     return e == cudaSuccess ? 1 : -(int)e;

@@ -1,0 +1,76 @@
+"""The operators with axes and with sinks where a single binary32 number shows, on requests that have no new tokens, and
+together with what comes before and after them."""
+import numpy as np
+import pytest
+import torch
+
+from long_ref import Long
+from paper_2609_35065_gb300 import kvs
+
+pytestmark = pytest.mark.gpu
+LOG2E = 1.4426950408889634
+
+
+def _scales(near, count):
+    """Binary32 scales from `near` / log2(e) up whose products with log2(e), taken in binary32, are 6e-8 of themselves too small."""
+    found, s = [], np.float32(near / LOG2E)
+    while len(found) < count:
+        s = np.nextafter(s, np.float32(1))
+        if float(s * np.float32(LOG2E)) < (1 - 6e-8) * float(s) * LOG2E:
+            found.append(float(s))
+    return found
+
+
+class Exact(Long):
+    """Sums of products that are exact in binary32, whatever their order and however many bits a sum keeps beyond 16: queries are
+    +-1, the same for all heads, keys multiples of 1/32 below 8.  A new token's queries have `most` at most, 0.9 of that at least, as
+    their product with its own key, and 0 with those of the tokens before the new ones."""
+
+    def __init__(self, new, lens, window, sinks, G, D, dtype, most, seed=5):
+        super().__init__(new, lens, window, sinks, 1, G, D, 16, dtype=dtype, given_back=False)
+        self.cache.nan_to_num_(0.5)
+        g = torch.Generator().manual_seed(seed)
+        q = self.parts(self.qkv)[0]
+        q.copy_((torch.randint(0, 2, (len(q), 1, D), generator=g) * 2 - 1).to(q.dtype))
+        step = 2.0 ** -5
+        top = int(most / D / step)
+        for r, (n, T) in enumerate(zip(new, lens)):
+            own = (torch.randint(int(0.9 * top) + 1, top + 1, (n, 1), generator=g) * step).to(q.dtype) * q[self.starts[r]: self.starts[r + 1], 0]
+            self.cache[0, torch.from_numpy(self.slots(r, np.arange(T))), 0] = 0.0
+            self.cache[0, torch.from_numpy(self.slots(r, np.arange(T - n, T))), 0] = own
+
+    def lse(self, scale):
+        """In 64 bits, [rows, heads]."""
+        out = np.zeros((self.N, self.G))
+        for r in range(self.R):
+            for i in range(self.G):
+                s = self.scores(r, 0, i, scale, True, self.window)[0]
+                m = s.max(1, keepdims=True)
+                out[self.starts[r]: self.starts[r + 1], i] = (m + np.log(np.exp(s - m).sum(1, keepdims=True)))[:, 0]
+        return out
+
+    def own(self, r):
+        """Request r's new tokens."""
+        return slice(self.lens[r] - self.new[r], self.lens[r])
+
+
+# ---- the scale as it is given ----------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("new,window", [(40, 300), (400, 300), (400, 0)])
+def test_weights_of_exact_scores(dtype, D, new, window):
+    """Weights near 1, exponentials of a difference of two numbers below 32, of which the score is exact.  Off are: lse's product with
+    log2(e) by 2^-20, the difference (below 1/4) and its correction by 2^-26 each, the exponential by 2^-22, and each addition to the
+    sum of two such weights by 2^-23 or, where that is less, by what is added."""
+    scale = _scales(2.0 ** -4, 1)[0]
+    sm = Exact([new], [700], window, 4, 2, D, dtype, 508)
+    step, q, _, _, _cache = sm.on_gpu(kvs)
+    lse = torch.from_numpy(sm.lse(scale)).float()
+    assert 18 < lse.min() and lse.max() < 32 / LOG2E
+    w = torch.zeros(1, 1, step.max_kv, device="cuda")
+    kvs.kvs_weigh_sinks(step, 0, q, lse.cuda(), w, scale, 0.0, True, window, 4, flags=kvs.KVS_F_VALIDATE)
+    each = np.concatenate([np.exp(sm.scores(0, 0, i, scale, True, window)[0] - lse[:, i, None].double().numpy()) for i in range(2)])
+    want = each.sum(0)
+    off = np.abs(w.double().cpu().numpy()[0, 0, :700] - want)
+    bound = want * (np.log(2) * (2.0 ** -20 + 2 * 2.0 ** -26) + 2.0 ** -22) + np.minimum(each, 2.0 ** -23).sum(0)
+    assert (off <= bound)[sm.own(0)].all(), (off / bound)[sm.own(0)].max()
