@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(WARPS * 32) kvs_attend_rows_kernel(AttendJob j
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int32_t t = t0 + 8 * (e >> 1);
-                const float x = (s[n][0][e] + s[n][1][e]) * j.scale_log2;
+                const float y = s[n][0][e] + s[n][1][e], x = HELD ? fmaf(y, j.scale_low, y * j.scale_log2) : y * j.scale_log2;
                 s[n][0][e] = (t >= lo[n][e & 1] || (HELD && t < j.sinks)) && t < hi[n][e & 1] ? x : kNone;
                 above = above || s[n][0][e] > m[n][e & 1] + kLag;
             }

@@ -410,6 +410,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_held_kernel(AttendJob 
         const int pair = 1 + tl * 4 + (warp & 3);
         float* tops = reinterpret_cast<float*>(raw + P::tops);
         const float c = fmaxf(fabsf(j.scale_log2), 1e-36f);         // a zero scale keeps -infinity * c what it is
+        const float c_low = j.scale_log2 < 0.0f ? -j.scale_low : j.scale_low;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // lane 32 (warp % 4) of tensor memory
         const uint32_t s_own = s_at(tl) + lanes + 64 * half, o_own = o_at(tl) + lanes + DP / 2 * half;
         uint32_t gone = 0, items = 0;
@@ -563,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_held_kernel(AttendJob 
             bar_some(pair, 64);
             l = tops[tl * 128 + t] + tops[128 * kTiles + tl * 128 + t];
             bar_some(pair, 64);                                      // the next item's maxima go over them
-            if (row.live && ok && half == 0 && j.lse) j.lse[row.lse] = l == 0.0f ? kNone : ((m == kNone ? kNone : m * c - top_at) + log2f(l)) * 0.69314718055994531f;
+            if (row.live && ok && half == 0 && j.lse) j.lse[row.lse] = l == 0.0f ? kNone : ((m == kNone ? kNone : fmaf(m, c_low, m * c - top_at)) + log2f(l)) * 0.69314718055994531f;
             const bool some_o = steps > 0;
             char* to = ok ? row.out : nullptr;
             if (some_o) ++items;

@@ -327,6 +327,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
         const int pair = 1 + tl * 4 + (warp & 3);
         float* tops = reinterpret_cast<float*>(raw + P::tops);
         const float c = fmaxf(fabsf(j.scale_log2), 1e-36f);         // a zero scale keeps -infinity * c what it is
+        const float c_low = j.scale_log2 < 0.0f ? -j.scale_low : j.scale_low;
         int32_t g;
         const int32_t tok = token_of(st, row0 + tl * per + t, g);
         const bool live = t < per && tl * per + t < rows;
@@ -437,7 +438,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
         const int64_t all_rows = (int64_t)st.total_q * heads;
         if (ok) {
             if (live && half == 0) {
-                const float m2 = m == kNone ? kNone : m * c - top_at;
+                const float m2 = m == kNone ? kNone : HELD ? fmaf(m, c_low, m * c - top_at) : m * c - top_at;
                 const int64_t row = (int64_t)(q.q0 + tok) * heads + h * st.group + g;
                 if (cluster) reinterpret_cast<float2*>(raw + P::part_ml)[128 * tl + t] = make_float2(m2, l);
                 else if (j.splits > 1) reinterpret_cast<float2*>(j.partial + (int64_t)j.splits * all_rows * st.head_dim)[split * all_rows + row] = make_float2(m2, l);

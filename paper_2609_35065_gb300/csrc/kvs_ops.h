@@ -2,6 +2,7 @@
 // kernels.  Not part of the public ABI.
 #pragma once
 
+#include <cmath>
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -50,6 +51,7 @@ struct AttendJob {
     float*   lse;
     float*   partial;                // splits > 1: [splits][rows of total_q * heads][head_dim], then their (m, l) pairs
     float    scale_log2;             // scale * log2(e)
+    float    scale_low;              // held: what scale_log2 lacks of that
     int32_t  causal, window;
     int32_t  held;                   // 1: a window with `sinks` first tokens that stay visible
     int32_t  sinks;
@@ -70,7 +72,7 @@ struct WeighJob {
     float    scale_log2, decay;
     int32_t  causal, window;
     int32_t  held, sinks;            // as in attention
-    float    scale, scale_low;       // by_places: as given; what scale_log2 lacks (kvs_weigh.cu)
+    float    scale, scale_low;       // held: as given; what scale_log2 lacks
     int32_t  by_places;              // 1: of kvs_weigh_sinks, hidden tokens or not
 };
 
@@ -86,6 +88,16 @@ struct EvictJob {
     float*   new_weights;
     int32_t* new_lens;
 };
+
+// scale log2(e) as a binary32 number, cut towards zero: what it lacks (scale_rest) has its sign then, so that infinite scores
+// times both stay what they are.
+inline double scale_times_log2e(float scale) { return (double)scale * 1.4426950408889634; }
+inline float scale_cut(float scale) {
+    const double c = scale_times_log2e(scale);
+    const float high = (float)c;
+    return std::fabs((double)high) > std::fabs(c) ? std::nextafter(high, 0.0f) : high;
+}
+inline float scale_rest(float scale, float high) { return std::isfinite(high) ? (float)(scale_times_log2e(scale) - (double)high) : 0.0f; }
 
 // Fills in the reciprocals of block_size and group.
 void set_divisors(StepView& st);

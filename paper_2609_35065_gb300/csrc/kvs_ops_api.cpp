@@ -300,11 +300,14 @@ int attend_call(const kvs_geometry* g, const kvs_paged_cache* c, const kvs_step*
     j.k_plane = (const char*)c->kv_planes[2 * layer];
     j.v_plane = (const char*)c->kv_planes[2 * layer + 1];
     j.lse = a->lse;
-    j.scale_log2 = a->scale * kLog2e;
     j.causal = a->causal != 0;
     int sms;
     KVS_TRY(ops_device(&j.step.err, &sms));
     const AttendPlan plan = held_plan(j.step, j.held, j.causal, j.window, j.sinks, sms);
+    // With sinks lse is of the scale as given, as kvs_weigh_sinks takes it.  On the tensor cores' kernels what one binary32 number lacks is
+    // added to the maximum at the end; the others multiply every score by both.
+    j.scale_log2 = j.held && !plan.tc ? scale_cut(a->scale) : a->scale * kLog2e;
+    if (j.held) j.scale_low = scale_rest(a->scale, j.scale_log2);
     j.tc = plan.tc;
     j.splits = plan.splits;
     j.cluster = plan.cluster;

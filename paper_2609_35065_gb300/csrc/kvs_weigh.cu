@@ -3,12 +3,10 @@
 //     w_t = decay * w_t + sum over rows of 2^(c q . k_t - lse'),  c = scale log2(e), lse' = lse log2(e)
 //
 // The exponent is one binary32 number, whose rounding a weight shows: 8e-7 of it where 12288 tokens
-// share it, against 2e-7 for a difference taken before it is scaled.
+// share it, against 2e-7 for a difference taken before it is scaled.  Of kvs_weigh_sinks c is two (launch_weigh).
 //
 // With every row's lse known a key's sum needs no other key: keys go to different CTAs, warps
 // or lanes, and no sum is shared.  Rows are packed as in attention (row = token * group + head).
-#include <cmath>
-
 #include "kvs_tcgen05.cuh"
 
 namespace kvs {
@@ -556,7 +554,8 @@ __device__ __forceinline__ void load_rows(RowFrags<K>& f, const WeighJob& j, con
             const int32_t t = token_of(st, x, g);
             f.see[e] = seen_by(q, t, t, j.causal, j.window);
             if (HELD) f.see[e] = in_places(held, f.see[e]);
-            f.lse[e] = -kLog2e * load_of<HELD>(j.lse + (int64_t)(q.q0 + t) * (st.kv_heads * st.group) + h * st.group + g);
+            const float z = load_of<HELD>(j.lse + (int64_t)(q.q0 + t) * (st.kv_heads * st.group) + h * st.group + g);
+            f.lse[e] = HELD ? fmaf(-kLog2e, z, -kLog2eLow * z) : -kLog2e * z;
         }
     }
 }
@@ -630,7 +629,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) kvs_weigh_rows_kernel(Weigh
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int32_t key = t + 8 * (e >> 1);
-                if ((key >= f.see[e & 1].lo || (HELD && key < j.sinks)) && key < f.see[e & 1].hi) sum[e >> 1] += exp2_fast(fmaf(s[e] + u[e], j.scale_log2, f.lse[e & 1]));
+                const float y = s[e] + u[e], x = fmaf(y, j.scale_log2, f.lse[e & 1]);
+                if ((key >= f.see[e & 1].lo || (HELD && key < j.sinks)) && key < f.see[e & 1].hi) sum[e >> 1] += exp2_fast(HELD ? fmaf(y, j.scale_low, x) : x);
             }
         };
 #pragma unroll
@@ -756,7 +756,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, CTAS) kvs_weigh_held_kernel(We
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int32_t key = u + 8 * (e >> 1);
-                if ((key >= f.see[e & 1].lo || key < j.sinks) && key < f.see[e & 1].hi) sum[e >> 1] += exp2_fast(fmaf(s[e] + t[e], j.scale_log2, f.lse[e & 1]));
+                const float y = s[e] + t[e];
+                if ((key >= f.see[e & 1].lo || key < j.sinks) && key < f.see[e & 1].hi) sum[e >> 1] += exp2_fast(fmaf(y, j.scale_low, fmaf(y, j.scale_log2, f.lse[e & 1])));
             }
         };
 #pragma unroll
@@ -894,16 +895,9 @@ cudaError_t weigh_dims(const WeighJob& j, int sms, cudaStream_t s) { return j.he
 
 // A heavy token's weight is the exponential of a small difference of two large numbers, its score and lse, so that a score's
 // relative error is multiplied by lse, and where it has the same sign for all rows no sum evens it out.  The scale
-// times log2(e) as one binary32 number is up to 7e-8 off: kvs_weigh_sinks on the tensor cores takes it in two, the second of the
-// first's sign so that infinite scores stay what they are.  What the tensor cores cut off a sum depends on the terms' signs and
-// magnitudes, so that nothing is made up for it here: kvs_attend_sinks' lse is of scores that were cut off alike.
-void exact_scale(WeighJob& j) {
-    const double c = (double)j.scale * 1.4426950408889634;
-    j.scale_log2 = (float)c;
-    if (std::fabs((double)j.scale_log2) > std::fabs(c)) j.scale_log2 = std::nextafter(j.scale_log2, 0.0f);
-    j.scale_low = std::isfinite(j.scale_log2) ? (float)(c - (double)j.scale_log2) : 0.0f;
-}
-
+// times log2(e) as one binary32 number is up to 7e-8 off: under a window with sinks it is taken in two, here and for the lse of
+// kvs_attend_sinks.  What the tensor cores cut off a sum depends on the terms' signs and magnitudes, so that nothing is made up
+// for it here: that lse is of scores that were cut off alike.
 int launch_weigh(const WeighJob& job, bool half, int sms, cudaStream_t s) {
     WeighJob j = job;
     if (j.by_places && (int64_t)j.step.max_q * j.step.group > kFewRows) {
@@ -911,7 +905,10 @@ int launch_weigh(const WeighJob& job, bool half, int sms, cudaStream_t s) {
             j.held = 1;
             j.window = j.step.max_kv;
         }
-        exact_scale(j);
+    }
+    if (j.held) {
+        j.scale_log2 = scale_cut(j.scale);
+        j.scale_low = scale_rest(j.scale, j.scale_log2);
     }
     const cudaError_t e = half ? weigh_dims<true>(j, sms, s) : weigh_dims<false>(j, sms, s);
     return e == cudaSuccess ? 1 : -(int)e;

@@ -57,7 +57,7 @@ class Exact(Long):
 # ---- the scale as it is given ----------------------------------------------------
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("D", [64, 72, 128])
-@pytest.mark.parametrize("new,window", [(40, 300), (400, 300), (400, 0)])
+@pytest.mark.parametrize("new,window", [(3, 300), (16, 300), (40, 300), (400, 300), (400, 0)])
 def test_weights_of_exact_scores(dtype, D, new, window):
     """Weights near 1, exponentials of a difference of two numbers below 32, of which the score is exact.  Off are: lse's product with
     log2(e) by 2^-20, the difference (below 1/4) and its correction by 2^-26 each, the exponential by 2^-22, and each addition to the
@@ -74,3 +74,32 @@ def test_weights_of_exact_scores(dtype, D, new, window):
     off = np.abs(w.double().cpu().numpy()[0, 0, :700] - want)
     bound = want * (np.log(2) * (2.0 ** -20 + 2 * 2.0 ** -26) + 2.0 ** -22) + np.minimum(each, 2.0 ** -23).sum(0)
     assert (off <= bound)[sm.own(0)].all(), (off / bound)[sm.own(0)].max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("new,lens", [([1] * 40, list(range(300, 700, 10))), ([20], [700]), ([40, 3], [700, 400]), ([400], [700])])
+def test_weights_with_the_lse_that_attention_returned(dtype, D, new, lens):
+    """A new token's own weight is off by the roundings of lse and of its product with log2(e), whatever the scale: on average over many
+    tokens and scales by little, as a mean of n independent errors of at most h each is off by more than h sqrt(2 ln(2 / p) / n) with a
+    probability of p at most (Hoeffding).  h: 2^-20 of lse itself, and log2(e)'s multiple of it is rounded three times, by 2^-20 each (as
+    the maximum times the scale, with the sum's logarithm, and as the weight's subtrahend); the exponentials, of lse's sum and of the weight,
+    may be off by 2^-22 each, always alike.  Products are exact; scores come in 64ths of the largest at least, lse in far more."""
+    sm = Exact(new, lens, 250, 4, 2, D, dtype, 508)
+    scales = _scales(2.0 ** -4, 16)
+    step, q, _, _, _cache = sm.on_gpu(kvs, decode=new == [1] * len(new))
+    ws = torch.empty(kvs.kvs_attend_sinks_workspace(step, 2, True, 250, 4), dtype=torch.uint8, device="cuda")
+    out, z = torch.empty_like(q), torch.empty(sm.N, 2, device="cuda")
+    off = []
+    for scale in scales:
+        w = torch.zeros(sm.R, 1, step.max_kv, device="cuda")
+        kvs.kvs_attend_sinks(step, 0, q, out, z, scale, True, 250, 4, ws)
+        kvs.kvs_weigh_sinks(step, 0, q, z, w, scale, 0.0, True, 250, 4, flags=kvs.KVS_F_VALIDATE)
+        want, _ = sm.weigh(sm.lse(scale), np.zeros(w.shape), 0.0, scale, True, 250)
+        got = w.double().cpu().numpy()
+        off += [(got / np.where(want > 0, want, 1))[r, 0][sm.own(r)] - 1 for r in range(sm.R)]
+    off = np.concatenate(off)
+    h = np.sqrt(1 + 3 * np.log(2) ** 2) * 2.0 ** -20
+    n = len(scales) * min(sm.N, len(np.unique(sm.lse(scales[0]).round(6))))
+    bound = h * np.sqrt(2 * np.log(2 / 1e-6) / n) + 2 * 2.0 ** -22
+    assert abs(off.mean()) <= bound, (off.mean(), bound)
