@@ -900,13 +900,11 @@ cudaError_t weigh_dims(const WeighJob& j, int sms, cudaStream_t s) { return j.he
 // for it here: that lse is of scores that were cut off alike.
 int launch_weigh(const WeighJob& job, bool half, int sms, cudaStream_t s) {
     WeighJob j = job;
-    if (j.by_places && (int64_t)j.step.max_q * j.step.group > kFewRows) {
-        if (!j.held) {                                           // nothing is hidden: a window that all tokens fill
+    if (j.by_places) {
+        if (!j.held) {                                           // nothing is hidden: a window that all tokens fill, so that a request without new tokens reads nothing
             j.held = 1;
             j.window = j.step.max_kv;
         }
-    }
-    if (j.held) {
         j.scale_log2 = scale_cut(j.scale);
         j.scale_low = scale_rest(j.scale, j.scale_log2);
     }

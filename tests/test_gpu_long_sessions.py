@@ -103,3 +103,26 @@ def test_weights_with_the_lse_that_attention_returned(dtype, D, new, lens):
     n = len(scales) * min(sm.N, len(np.unique(sm.lse(scales[0]).round(6))))
     bound = h * np.sqrt(2 * np.log(2 / 1e-6) / n) + 2 * 2.0 ** -22
     assert abs(off.mean()) <= bound, (off.mean(), bound)
+
+
+# ---- requests without new tokens ---------------------------------------------------
+@pytest.mark.parametrize("new", [[0, 1], [0, 5], [0, 20], [0, 150]])
+@pytest.mark.parametrize("window,sinks", [(0, 6), (0, 0), (704, 1), (600, 104), (2 ** 31 - 1, 0)])
+@pytest.mark.parametrize("decay", [0.0, 0.5, 1.0])
+def test_a_request_without_new_tokens_reads_no_table_entry(new, window, sinks, decay):
+    """Where the mask hides nothing, too: its weights fade, and the other request gets its own."""
+    sm = Long(new, [700, 650], window, sinks, 2, 4, 64)
+    sm.tables[0] = -1
+    step, q, _, _, _cache = sm.on_gpu(kvs)
+    ws = torch.empty(kvs.kvs_attend_sinks_workspace(step, 8, True, window, sinks), dtype=torch.uint8, device="cuda")
+    out, z = torch.empty_like(q), torch.empty(sm.N, 8, device="cuda")
+    kvs.kvs_attend_sinks(step, 0, q, out, z, None, True, window, sinks, ws, flags=kvs.KVS_F_VALIDATE)
+    w = torch.rand(2, 2, step.max_kv, device="cuda")
+    before = w.clone()
+    kvs.kvs_weigh_sinks(step, 0, q, z, w, None, decay, True, window, sinks, flags=kvs.KVS_F_VALIDATE)
+    assert torch.equal(w[0, :, :700], before[0, :, :700] * decay)
+    assert torch.equal(w[0, :, 700:], before[0, :, 700:])
+    one = Long(new[1:], [650], window, sinks, 2, 4, 64)                   # as the second request alone
+    one.tables, one.qkv, one.cache, one.num_blocks = sm.tables[1:], sm.qkv, sm.cache, sm.num_blocks
+    want, bound = one.weigh(z.cpu().numpy(), before[1:, :, :650].cpu().numpy(), decay, 64 ** -0.5, True, 0)
+    assert (np.abs(w[1:, :, :650].double().cpu().numpy() - want) <= bound).all()
