@@ -124,6 +124,11 @@ def prompt_positions(cfg: Config, n: int) -> torch.Tensor:
     return at[:, :n].contiguous()
 
 
+def next_position(at: torch.Tensor) -> torch.Tensor:
+    """Position of a token of text behind those at `at` ([tokens] or [axes, tokens]): behind the largest, the same on every axis."""
+    return (at.amax() + 1).to(torch.int32).repeat(at.shape[:-1] + (1,))
+
+
 def run(cfg: Config = Config(), prefix: int = 600, suffix: int = 90, decode: int = 12, budget: int = 320, seed: int = 0) -> dict:
     """The four steps above; returns what they gave."""
     model = Decoder(cfg, seed)
@@ -160,7 +165,7 @@ def run(cfg: Config = Config(), prefix: int = 600, suffix: int = 90, decode: int
     table = torch.from_numpy(tables[1])[None].to(dev)
     weights = torch.zeros(cfg.layers, 1, cfg.kv_heads, per * cfg.block, device=dev)
     lens = torch.tensor([cached], dtype=torch.int32, device=dev)
-    position = (at[..., -1:] + 1 if cfg.axes else torch.tensor([cached], dtype=torch.int32, device=dev)).contiguous()
+    position = next_position(at)
     token, tokens = logits[-1:].argmax(-1), []
 
     def decode_some(step, weights):

@@ -126,3 +126,21 @@ def test_a_request_without_new_tokens_reads_no_table_entry(new, window, sinks, d
     one.tables, one.qkv, one.cache, one.num_blocks = sm.tables[1:], sm.qkv, sm.cache, sm.num_blocks
     want, bound = one.weigh(z.cpu().numpy(), before[1:, :, :650].cpu().numpy(), decay, 64 ** -0.5, True, 0)
     assert (np.abs(w[1:, :, :650].double().cpu().numpy() - want) <= bound).all()
+
+
+# ---- the example ------------------------------------------------------------------
+@pytest.mark.parametrize("prefix,suffix", [(600, 90), (600, 10), (500, 70)])
+def test_a_session_decodes_behind_its_prompt(prefix, suffix, monkeypatch):
+    """What is decoded is text: its tokens have the same position on all axes, the first the one behind the prompt's largest."""
+    from paper_2609_35065_gb300 import prefix_step
+    cfg, seen, append = prefix_step.session(), [], kvs.kvs_append_axes
+
+    def recorded(step, layer, q, k, v, q_out, rope, axes, positions, *a):
+        if layer == 0 and positions.shape[1] == 1:
+            seen.append(positions[:, 0].tolist())
+        return append(step, layer, q, k, v, q_out, rope, axes, positions, *a)
+
+    monkeypatch.setattr(kvs, "kvs_append_axes", recorded)
+    prefix_step.run(cfg, prefix, suffix, decode=5)
+    first = int(prefix_step.prompt_positions(cfg, prefix + suffix).max()) + 1
+    assert seen == [[first + k] * 3 for k in range(5)]
