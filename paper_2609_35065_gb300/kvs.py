@@ -14,6 +14,7 @@ legacy default stream.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 import threading
 from dataclasses import dataclass, field
@@ -685,6 +686,12 @@ def _int32_tensor(name, t, dims):
         raise ValueError(f"{name}: must be contiguous")
 
 
+def _i32(x) -> int:
+    """A whole number as an int32 field of a struct takes it, beyond the ends the nearest (ctypes would keep the low bits): a window of 2^32
+    tokens hides as little as one of 2^31 - 1, a layer of that number is as little there."""
+    return max(-2 ** 31, min(2 ** 31 - 1, operator.index(x)))
+
+
 def _f32(name, t, shape, contiguous=True):
     import torch
     if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or (contiguous and not t.is_contiguous()):
@@ -744,7 +751,7 @@ def kvs_append(step: Step, layer: int, q, k, v, q_out=None, rope: Rope | None = 
             raise ValueError("positions has one entry per row")
         a.positions = positions.data_ptr()
     g, c, s = step.refs
-    return _check(lib().kvs_append(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+    return _check(lib().kvs_append(g, c, s, _i32(layer), ctypes.byref(a), _stream(stream), flags))
 
 
 def _append_args(step, q, k, v, q_out, rope) -> kvs_append_args:
@@ -806,13 +813,13 @@ def kvs_append_axes(step: Step, layer: int, q, k, v, q_out, rope: Rope, axes: Ax
     a.positions = positions.data_ptr()
     x = kvs_axes(axes.struct.axis, positions.stride(0), axes.struct.num_axes, axes.struct.pairs)
     g, c, s = step.refs
-    return _check(lib().kvs_append_axes(g, c, s, layer, ctypes.byref(a), ctypes.byref(x), _stream(stream), flags))
+    return _check(lib().kvs_append_axes(g, c, s, _i32(layer), ctypes.byref(a), ctypes.byref(x), _stream(stream), flags))
 
 
 def kvs_attend_workspace(step: Step, num_q_heads: int) -> int:
     """Bytes of workspace that :func:`kvs_attend` needs for this step."""
     g, _, s = step.refs
-    n = int(lib().kvs_attend_workspace(g, s, int(num_q_heads)))
+    n = int(lib().kvs_attend_workspace(g, s, _i32(int(num_q_heads))))
     if n < 0:
         _check(n)
     return n
@@ -832,7 +839,7 @@ def kvs_attend(step: Step, layer: int, q, out, lse=None, scale: float | None = N
             return _check(rc)
     a = _attend_args(step, q, out, lse, scale, causal, window, workspace)
     g, c, s = step.refs
-    return _check(lib().kvs_attend(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+    return _check(lib().kvs_attend(g, c, s, _i32(layer), ctypes.byref(a), _stream(stream), flags))
 
 
 def _attend_args(step, q, out, lse, scale, causal, window, workspace) -> kvs_attend_args:
@@ -846,14 +853,14 @@ def _attend_args(step, q, out, lse, scale, causal, window, workspace) -> kvs_att
         if not workspace.is_contiguous():
             raise ValueError("workspace: must be contiguous")
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    a.scale, a.causal, a.window = scale, bool(causal), window
+    a.scale, a.causal, a.window = scale, bool(causal), _i32(window)
     return a
 
 
 def kvs_attend_sinks_workspace(step: Step, num_q_heads: int, causal: bool = True, window: int = 0, sinks: int = 0) -> int:
     """Bytes of workspace that :func:`kvs_attend_sinks` needs for this step and mask."""
     g, _, s = step.refs
-    n = int(lib().kvs_attend_sinks_workspace(g, s, int(num_q_heads), bool(causal), int(window), int(sinks)))
+    n = int(lib().kvs_attend_sinks_workspace(g, s, _i32(int(num_q_heads)), bool(causal), _i32(int(window)), _i32(int(sinks))))
     if n < 0:
         _check(n)
     return n
@@ -873,7 +880,7 @@ def kvs_attend_sinks(step: Step, layer: int, q, out, lse=None, scale: float | No
             return _check(rc)
     a = _attend_args(step, q, out, lse, scale, causal, window, workspace)
     g, c, s = step.refs
-    return _check(lib().kvs_attend_sinks(g, c, s, layer, ctypes.byref(a), sinks, _stream(stream), flags))
+    return _check(lib().kvs_attend_sinks(g, c, s, _i32(layer), ctypes.byref(a), _i32(sinks), _stream(stream), flags))
 
 
 def kvs_weigh(step: Step, layer: int, q, lse, weights, scale: float | None = None, decay: float = 1.0, causal: bool = True,
@@ -889,7 +896,7 @@ def kvs_weigh(step: Step, layer: int, q, lse, weights, scale: float | None = Non
             return _check(rc)
     a = _weigh_args(step, q, lse, weights, scale, decay, causal, window)
     g, c, s = step.refs
-    return _check(lib().kvs_weigh(g, c, s, layer, ctypes.byref(a), _stream(stream), flags))
+    return _check(lib().kvs_weigh(g, c, s, _i32(layer), ctypes.byref(a), _stream(stream), flags))
 
 
 def _weigh_args(step, q, lse, weights, scale, decay, causal, window) -> kvs_weigh_args:
@@ -902,7 +909,7 @@ def _weigh_args(step, q, lse, weights, scale, decay, causal, window) -> kvs_weig
         raise ValueError("weights: [requests, KV heads, at least max_kv], contiguous in its last dimension")
     a.weights = _f32("weights", weights, (R, H, weights.shape[2]), contiguous=False)
     a.request_stride, a.head_stride = weights.stride(0), weights.stride(1)
-    a.scale, a.decay, a.causal, a.window = scale, decay, bool(causal), window
+    a.scale, a.decay, a.causal, a.window = scale, decay, bool(causal), _i32(window)
     return a
 
 
@@ -918,7 +925,7 @@ def kvs_weigh_sinks(step: Step, layer: int, q, lse, weights, scale: float | None
             return _check(rc)
     a = _weigh_args(step, q, lse, weights, scale, decay, causal, window)
     g, c, s = step.refs
-    return _check(lib().kvs_weigh_sinks(g, c, s, layer, ctypes.byref(a), sinks, _stream(stream), flags))
+    return _check(lib().kvs_weigh_sinks(g, c, s, _i32(layer), ctypes.byref(a), _i32(sinks), _stream(stream), flags))
 
 
 def kvs_evict(step: Step, weights, dst_tables, budget: int, sinks: int, recent: int, kept, new_weights=None, new_lens=None,
@@ -947,7 +954,7 @@ def kvs_evict(step: Step, weights, dst_tables, budget: int, sinks: int, recent: 
     a.dst_stride = dst_tables.stride(0) if R > 1 else dst_tables.shape[1]
     if dst_tables.shape[1] * step.geom.block_size < min(step.max_kv, budget):
         raise KvsError(KVS_ERR_BOUNDS, f"new tables of {dst_tables.shape[1]} blocks do not hold {min(step.max_kv, budget)} tokens")
-    a.budget, a.sinks, a.recent = int(budget), int(sinks), int(recent)
+    a.budget, a.sinks, a.recent = _i32(int(budget)), _i32(int(sinks)), _i32(int(recent))
     if kept.dtype != torch.int32 or tuple(kept.shape) != (L, R, H, budget) or not kept.is_contiguous():
         raise ValueError(f"kept: a contiguous int32 tensor of shape {(L, R, H, budget)} is needed")
     a.kept = kept.data_ptr()
