@@ -115,6 +115,7 @@ template <bool HALF, int DP, int KT, bool HELD>
 __global__ void __launch_bounds__(WPlan<DP, KT>::threads, 3 - KT) kvs_weigh_tc_kernel(WeighJob j, const __grid_constant__ CUtensorMap k_map,
                                                                    const __grid_constant__ CUtensorMap q_map, int32_t k_boxes, int32_t q_boxes, int32_t share,
                                                                    int32_t key_tiles_all) {
+    static_assert(KT == 1 || !HELD, "places go by one key tile to a CTA");
     extern __shared__ char raw[];
     using P = WPlan<DP, KT>;
     constexpr int kThreads = P::threads, kStages = P::stages, kAccs = P::accs, kKeysTc = P::keys, kIssuer = P::issuer, kParts = KT == 1 ? 2 : kAccs;
@@ -883,7 +884,7 @@ cudaError_t weigh(const WeighJob& j, int sms, cudaStream_t s) {
     if constexpr (HELD) return weigh_tc<HALF, DP, 1, HELD>(j, sms, held_weigh_share(j, sms), s);
     // One key tile to a CTA up to 2560 rows: against 8000 tokens of 8 requests x 8 heads of 128 dims 64 rows
     // take 72 us (two tiles: 92), 256 79 (99), 1024 149 (167), 2048 250 (261), 4096 467 (450).
-    return rows <= 2560 ? weigh_tc<HALF, DP, 1, HELD>(j, sms, 1, s) : weigh_tc<HALF, DP, 2, HELD>(j, sms, 1, s);
+    else return rows <= 2560 ? weigh_tc<HALF, DP, 1, HELD>(j, sms, 1, s) : weigh_tc<HALF, DP, 2, HELD>(j, sms, 1, s);
 }
 
 template <bool HALF, bool HELD>

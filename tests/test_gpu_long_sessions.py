@@ -144,3 +144,19 @@ def test_a_session_decodes_behind_its_prompt(prefix, suffix, monkeypatch):
     prefix_step.run(cfg, prefix, suffix, decode=5)
     first = int(prefix_step.prompt_positions(cfg, prefix + suffix).max()) + 1
     assert seen == [[first + k] * 3 for k in range(5)]
+
+
+# ---- many row tiles -----------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,window,sinks,H,G,D", [(2400, 40, 130, 1, 4, 64), (1200, 500, 260, 8, 4, 128), (1200, 1100, 4, 16, 2, 64), (1300, 1200, 4, 30, 1, 64)])
+def test_weights_of_shared_row_tiles(dtype, new, window, sinks, H, G, D):
+    """The sinks' rows shared by 8, 4 and 2 CTAs and by none, each of which has more row tiles than lse has slots."""
+    sm = Long([new], [new + 60], window, sinks, H, G, D, dtype=dtype)
+    step, q, _, _, _cache = sm.on_gpu(kvs)
+    lse = sm.attend(D ** -0.5, True, window)[2].astype(np.float32)
+    w = torch.rand(1, H, step.max_kv, device="cuda")
+    before = w.cpu().numpy()
+    kvs.kvs_weigh_sinks(step, 0, q, torch.from_numpy(lse).cuda(), w, None, 0.5, True, window, sinks, flags=kvs.KVS_F_VALIDATE)
+    want, bound = sm.weigh(lse, before, 0.5, D ** -0.5, True, window)
+    T = new + 60
+    assert (np.abs(w.double().cpu().numpy() - want) <= bound)[..., :T].all()
