@@ -477,9 +477,10 @@ int kvs_retrieve_noalloc(const kvs_geometry* geom, const kvs_paged_cache* cache,
  * are of a window beside which a request's first tokens stay visible.  Each call works on one layer (kvs_evict: on all) of the planes above.
  *
  * Unlike a retrieval's, the lengths and block tables of a step are DEVICE arrays, as a
- * serving loop keeps them: the calls read them on the GPU, plan nothing on the host,
- * allocate nothing, and can be captured into a graph (but for the library's first call on a
- * device, which allocates its state; kvs_attend_workspace() is one).  Calls are enqueued on
+ * serving loop keeps them: the calls read them on the GPU, allocate nothing, and can be
+ * captured into a graph (but for the library's first call on a device, which allocates its
+ * state; kvs_attend_workspace() is one).  What is planned on the host goes by the step's bounds
+ * and the call's numbers alone, and takes a few us at most (a window of 65536).  Calls are enqueued on
  * the caller's stream and return; tensors must stay valid until the stream has passed them.
  * Rows of the step's tensors that belong to no request (before q_starts[0], behind its last
  * entry) are not written, and what they hold does not matter.
@@ -675,6 +676,9 @@ int kvs_weigh(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_
  * The same under kvs_attend_sinks' mask, from the lse that it returned.  Every cached token's
  * weight is multiplied by decay, those of tokens that no new token sees too (decay = 1 leaves
  * those untouched); only seen tokens' block table entries and keys are read.
+ * kvs_evict takes any of kv_len tokens, those whose blocks were given back too, whose entries it
+ * would then read (KVS_ERR_BOUNDS).  Give them NaN for a weight (fading with a decay other than 0 leaves
+ * it): they are kept last, and none of them while the budget is no larger than the number of the others.
  */
 int kvs_weigh_sinks(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
                     const kvs_weigh_args* args, int32_t sinks, void* cuda_stream, uint32_t flags);

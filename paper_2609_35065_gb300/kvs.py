@@ -916,7 +916,8 @@ def _weigh_args(step, q, lse, weights, scale, decay, causal, window) -> kvs_weig
 def kvs_weigh_sinks(step: Step, layer: int, q, lse, weights, scale: float | None = None, decay: float = 1.0, causal: bool = True,
                     window: int = 0, sinks: int = 0, stream=None, flags: int = 0) -> int:
     """:func:`kvs_weigh` under the mask of :func:`kvs_attend_sinks`, from the ``lse`` that it returned;
-    weights of tokens that nobody sees are multiplied by ``decay`` too."""
+    weights of tokens that nobody sees are multiplied by ``decay`` too.  NaN, which fading leaves, for tokens whose blocks were given
+    back has :func:`kvs_evict` keep them last."""
     if scale is None:
         scale = step.scale
     if _ops is not None:

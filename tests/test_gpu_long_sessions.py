@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+import ops_ref
 from long_ref import Long
 from paper_2609_35065_gb300 import kvs
 
@@ -160,3 +161,38 @@ def test_weights_of_shared_row_tiles(dtype, new, window, sinks, H, G, D):
     want, bound = sm.weigh(lse, before, 0.5, D ** -0.5, True, window)
     T = new + 60
     assert (np.abs(w.double().cpu().numpy() - want) <= bound)[..., :T].all()
+
+
+# ---- eviction where blocks were given back --------------------------------------------
+@pytest.mark.parametrize("decay", [0.5, 1.0])
+@pytest.mark.parametrize("new,lens", [([1, 1], [700, 390]), ([40, 3], [600, 300]), ([20, 0], [600, 64])])
+def test_tokens_that_were_given_back_are_kept_last(new, lens, decay):
+    """Their weights are NaN, which fading leaves and eviction ranks behind every number: while the budget is no larger than what is left, no
+    table entry of theirs is read."""
+    window, sinks, budget = 64, 4, 76
+    sm = Long(new, lens, window, sinks, 2, 4, 64, extra_blocks=40)
+    step, q, _, _, cache = sm.on_gpu(kvs)
+    ws = torch.empty(kvs.kvs_attend_sinks_workspace(step, 8, True, window, sinks), dtype=torch.uint8, device="cuda")
+    out, z = torch.empty_like(q), torch.empty(sm.N, 8, device="cuda")
+    kvs.kvs_attend_sinks(step, 0, q, out, z, None, True, window, sinks, ws, flags=kvs.KVS_F_VALIDATE)
+    w = torch.rand(1, 2, 2, step.max_kv, generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    gone = np.zeros((2, step.max_kv), dtype=bool)
+    for r, T in enumerate(lens):
+        block = sm.tables[r].numpy()[np.arange(T) // sm.B]
+        gone[r, :T] = (block < 0) | (block >= sm.num_blocks)
+    assert gone[0].any()
+    w.masked_fill_(torch.from_numpy(gone).cuda()[None, :, None], float("nan"))
+    kvs.kvs_weigh_sinks(step, 0, q, z, w[0], None, decay, True, window, sinks, flags=kvs.KVS_F_VALIDATE)
+    free = np.setdiff1d(np.arange(sm.num_blocks), sm.tables.numpy().ravel())[:10].reshape(2, 5).astype(np.int32)
+    kept, lens_out = torch.empty(1, 2, 2, budget, dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    kvs.kvs_evict(step, w, torch.from_numpy(free).cuda(), budget, sinks, 60, kept, None, lens_out, flags=kvs.KVS_F_VALIDATE)
+    got = kept.cpu().numpy()
+    assert (got == ops_ref.evict(w.cpu().numpy(), lens, budget, sinks, 60)).all()
+    for r, T in enumerate(lens):
+        J = min(T, budget)
+        assert lens_out[r] == J and not gone[r][got[0, r, :, :J]].any()
+        flat = cache.view(2, -1, 2, 64)
+        for h in range(2):
+            src = torch.from_numpy(sm.slots(r, got[0, r, h, :J])).cuda()
+            dst = torch.from_numpy(free[r][np.arange(J) // sm.B].astype(np.int64) * sm.B + np.arange(J) % sm.B).cuda()
+            assert torch.equal(flat[:, dst, h].view(torch.int16), flat[:, src, h].view(torch.int16))
