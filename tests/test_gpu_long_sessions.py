@@ -196,3 +196,21 @@ def test_tokens_that_were_given_back_are_kept_last(new, lens, decay):
             src = torch.from_numpy(sm.slots(r, got[0, r, h, :J])).cuda()
             dst = torch.from_numpy(free[r][np.arange(J) // sm.B].astype(np.int64) * sm.B + np.arange(J) % sm.B).cuda()
             assert torch.equal(flat[:, dst, h].view(torch.int16), flat[:, src, h].view(torch.int16))
+
+
+# ---- more query heads to a KV head than a tile has rows ---------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,lens,G,D", [([1, 1], [300, 40], 130, 64), ([3, 0, 2], [300, 9, 500], 200, 128), ([1], [900], 300, 72)])
+def test_more_heads_than_a_tile_has_rows(dtype, new, lens, G, D):
+    sm = Long(new, lens, 100, 5, 1, G, D, dtype=dtype)
+    step, q, _, _, _cache = sm.on_gpu(kvs)
+    ws = torch.empty(kvs.kvs_attend_sinks_workspace(step, G, True, 100, 5), dtype=torch.uint8, device="cuda")
+    out, z = torch.empty_like(q), torch.empty(sm.N, G, device="cuda")
+    kvs.kvs_attend_sinks(step, 0, q, out, z, None, True, 100, 5, ws, flags=kvs.KVS_F_VALIDATE)
+    want, bound, lse, lse_bound = sm.attend(D ** -0.5, True, 100)
+    assert (np.abs(out.double().cpu().numpy() - want) <= bound).all()
+    assert (np.abs(z.double().cpu().numpy() - lse) <= lse_bound).all()
+    w = torch.zeros(sm.R, 1, step.max_kv, device="cuda")
+    kvs.kvs_weigh_sinks(step, 0, q, z, w, None, 0.0, True, 100, 5, flags=kvs.KVS_F_VALIDATE)
+    want, bound = sm.weigh(z.cpu().numpy(), np.zeros((sm.R, 1, max(lens))), 0.0, D ** -0.5, True, 100)
+    assert (np.abs(w.double().cpu().numpy()[..., : max(lens)] - want) <= bound).all()
