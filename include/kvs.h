@@ -643,7 +643,7 @@ int64_t kvs_attend_workspace(const kvs_geometry* geom, const kvs_step* step, int
  * request sees: blocks between the sinks and the window may have been given back (entries of
  * any value) and their memory may belong to others.  What a call costs goes by window, sinks and
  * max_q, not by max_kv.  The workspace is kvs_attend_sinks_workspace() bytes for the same causal,
- * window and sinks; all else as for kvs_attend.
+ * window and sinks; all else as for kvs_attend, the weights' rounding above 16 rows too.
  */
 int kvs_attend_sinks(const kvs_geometry* geom, const kvs_paged_cache* cache, const kvs_step* step, int32_t layer,
                      const kvs_attend_args* args, int32_t sinks, void* cuda_stream, uint32_t flags);

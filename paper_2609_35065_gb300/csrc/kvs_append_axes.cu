@@ -63,7 +63,7 @@ __device__ __forceinline__ int32_t request_of(const StepView& st, int32_t n, int
 
 // A warp takes one token (or a share of its heads); a lane owns two pieces of eight elements of a head: of
 // the rotated part eight of its first half and those that they pair with, of the rest, and of neighbours
-// (PAIRS), sixteen in a row.  32768 tokens of 32 + 2 x 8 heads of 128 dims (805 MB) on three axes in 125 us, 6.4 TB/s;
+// (PAIRS), sixteen in a row.  32768 tokens of 32 + 2 x 8 heads of 128 dims (805 MB) on three axes in 125 us, 6.4 TB/s (PAIRS: 131);
 // a decode step of 16 tokens 3.8 us in a graph.
 template <bool HALF, bool PAIRS>
 __global__ void __launch_bounds__(256) kvs_append_axes_kernel(AppendJob j, uint32_t warps_per_token, int32_t groups) {
