@@ -13,7 +13,7 @@
 // blocks, everything does: with blocks of one token the calls below take 1870 and 504 us.
 //
 // 16 suffixes of 2048 tokens behind 2048, 32 query heads of 128 dims on 8 and a window of 1024 with four
-// sinks (0.55 TFLOP) take 446 to 481 us by box and power, 1.15 to 1.24 PFLOP/s; with a CTA to each pair of tiles 616.  Four prompts of 4001
+// sinks (0.55 TFLOP) take 446 to 481 us by card and power, 1.15 to 1.24 PFLOP/s; with a CTA to each pair of tiles 616.  Four prompts of 4001
 // to 4096 tokens, 64 heads of 64 dims on 8 and a window of 128 (34 GFLOP, 303 MB) take 125 to 128 us (276).  What bounds
 // them is the chain of a pair's hand-overs: with 128 dims the tensor cores are busy for 51% of the time and the issue
 // slots for 48%, with 64 for 22% and 56%.  Of 15 steps or more (a window of 4096) 1.5 PFLOP/s are reached.

@@ -106,6 +106,40 @@ def test_weights_with_the_lse_that_attention_returned(dtype, D, new, lens):
     assert abs(off.mean()) <= bound, (off.mean(), bound)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("signs", ["one", "both"])
+def test_rows_of_heavy_tokens_add_up(signs, D, dtype):
+    """Eight tokens have nearly all of the weight of rows whose lse is near 20, by products of one sign or of both.  Scores are not exact,
+    but both calls cut their sums off alike, so that a row's weights add up to one but for roundings: those of
+    test_weights_with_the_lse_that_attention_returned, and of up to 308 additions to either sum, by 2^-24 of it each."""
+    new, T, G, window = 400, 700, 2, 300
+    sm = Long([new], [T], window, 8, 1, G, D, 16, dtype=dtype, given_back=False)
+    sm.cache.nan_to_num_(0.5)
+    g = torch.Generator().manual_seed(1)
+    along = torch.randn(D, generator=g)
+    along *= D ** 0.5 / along.norm()
+    q = sm.parts(sm.qkv)[0]
+    x, keys = along + 0.1 * torch.randn(q.shape, generator=g), 17.0 / D ** 0.5 * along.expand(8, D)
+    if signs == "both":
+        x = x + 2.0 * (torch.randint(0, 2, q.shape, generator=g) * 2 - 1)
+        keys = keys + 0.5 * (torch.randint(0, 2, (8, D), generator=g) * 2 - 1)
+    q.copy_(x.to(q.dtype))
+    sm.cache[0, torch.from_numpy(sm.slots(0, np.arange(8))), 0] = keys.to(q.dtype)
+    step, qg, _, _, _cache = sm.on_gpu(kvs)
+    ws = torch.empty(kvs.kvs_attend_sinks_workspace(step, G, True, window, 8), dtype=torch.uint8, device="cuda")
+    out, z = torch.empty_like(qg), torch.empty(new, G, device="cuda")
+    w = torch.zeros(1, 1, step.max_kv, device="cuda")
+    kvs.kvs_attend_sinks(step, 0, qg, out, z, None, True, window, 8, ws)
+    kvs.kvs_weigh_sinks(step, 0, qg, z, w, None, 0.0, True, window, 8, flags=kvs.KVS_F_VALIDATE)
+    assert 17 < z.mean() < 23 and w[0, 0, :8].sum() > 0.9 * new * G
+    off = float(w.double().sum()) / (new * G) - 1
+    unit = 2.0 ** -25 * 2.0 ** np.ceil(np.log2(float(z.max()) * LOG2E))
+    h = np.sqrt((1 + 3 * np.log(2) ** 2) * unit ** 2 + 2 * 308 * 2.0 ** -48)
+    bound = h * np.sqrt(2 * np.log(2 / 1e-6) / (new * G)) + 2 * 2.0 ** -22
+    assert abs(off) <= bound, (off, bound)
+
+
 # ---- requests without new tokens ---------------------------------------------------
 @pytest.mark.parametrize("new", [[0, 1], [0, 5], [0, 20], [0, 150]])
 @pytest.mark.parametrize("window,sinks", [(0, 6), (0, 0), (704, 1), (600, 104), (2 ** 31 - 1, 0)])
