@@ -486,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvs_attend_held_kernel(AttendJob 
                     for (int n = 0; n < 32; n += 2) m = max3(m, s[n], s[n + 1]);
                 }
                 // Against this step's own maximum: the first step that rows see any key of.
-                bool exact = __any_sync(0xffffffffu, row.live && m == kNone && row.see.lo < (k + 1) * kN && row.see.hi > k * kN);
+                bool exact = __any_sync(0xffffffffu, row.live && m == kNone && (row.see.lo < (k + 1) * kN || j.sinks > k * kN) && row.see.hi > k * kN);
                 uint32_t pk[32];
                 float a0, a1;
                 while (true) {

@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(Plan<DP, TILES>::threads, Plan<DP, TILES>::cta
                 for (int n = 0; n < 32; ++n) s[n] = (32 * b + n >= lo || (HELD && 32 * b + n < sinks)) && 32 * b + n < hi ? s[n] : kNone;
             };
             // Against this step's own maximum: the first step, and the first that rows see any key of.
-            bool exact = k == 0 || __any_sync(0xffffffffu, live && m == kNone && see.lo < (j0 + k + 1) * kN && see.hi > (j0 + k) * kN);
+            bool exact = k == 0 || __any_sync(0xffffffffu, live && m == kNone && (see.lo < (j0 + k + 1) * kN || (HELD && j.sinks > (j0 + k) * kN)) && see.hi > (j0 + k) * kN);
             uint32_t pk[32];
             float a0, a1;
             while (true) {

@@ -248,3 +248,37 @@ def test_more_heads_than_a_tile_has_rows(dtype, new, lens, G, D):
     kvs.kvs_weigh_sinks(step, 0, q, z, w, None, 0.0, True, 100, 5, flags=kvs.KVS_F_VALIDATE)
     want, bound = sm.weigh(z.cpu().numpy(), np.zeros((sm.R, 1, max(lens))), 0.0, D ** -0.5, True, 100)
     assert (np.abs(w.double().cpu().numpy()[..., : max(lens)] - want) <= bound).all()
+
+
+# ---- sinks whose scores are -infinity ------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,R,sinks,out", [(3, 2, 60, 40), (40, 2, 60, 40), (150, 1, 300, 200), (400, 12, 60, 40), (400, 12, 300, 200)])
+def test_sinks_of_no_weight(new, R, sinks, out, D, dtype):
+    """The first `out` sinks score -infinity for every row: they weigh nothing, and the others are weighed against one another, however
+    small their scores.  Off are the weights by one rounding, the outputs by another, both of at most the largest value, and by 2^-9 of a
+    rounding for all else."""
+    sm = Long([new] * R, [new + 300] * R, 100, sinks, 1, 2, D, 16, dtype=dtype, given_back=False)
+    sm.cache.nan_to_num_(0.5)
+    q = sm.parts(sm.qkv)[0]
+    q[..., 0] = 1.0
+    q[..., 1] = 16.0
+    sm.cache[0, ..., 0] = 0.0
+    sm.cache[0, ..., 1] = -16.0                                             # e^-22 to e^-32 against a reference of 0
+    for r in range(R):
+        sm.cache[0, torch.from_numpy(sm.slots(r, np.arange(out))), 0, 0] = float("-inf")
+    step, qg, _, _, _cache = sm.on_gpu(kvs)
+    ws = torch.empty(kvs.kvs_attend_sinks_workspace(step, 2, True, 100, sinks), dtype=torch.uint8, device="cuda")
+    got, z = torch.empty_like(qg), torch.empty(sm.N, 2, device="cuda")
+    kvs.kvs_attend_sinks(step, 0, qg, got, z, None, True, 100, sinks, ws, flags=kvs.KVS_F_VALIDATE)
+    for r in range(R):
+        for i in range(2):
+            s, _, v = sm.scores(r, 0, i, D ** -0.5, True, 100)
+            assert np.isneginf(s[:, :out]).all()
+            p = np.exp(s - s.max(1, keepdims=True))
+            want = p @ v / p.sum(1, keepdims=True)
+            rows = slice(int(sm.starts[r]), int(sm.starts[r + 1]))
+            off = np.abs(got[rows, i].double().cpu().numpy() - want)
+            assert (off <= (2 + 2.0 ** -9) * ops_ref.UNIT[dtype] * np.abs(v).max()).all()
+            lse = s.max(1) + np.log(p.sum(1))
+            assert (np.abs(z[rows, i].double().cpu().numpy() - lse) <= 2.0 ** -14).all()
